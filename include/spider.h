@@ -384,6 +384,124 @@ int spd_decode(const spd_model* m, const uint16_t* x, int n_seqs, const int32_t*
                void* stream);
 
 /* ------------------------------------------------------------------------------------------ */
+/* Answering from the cache: drafted tokens, logit rules, a cache within a budget               */
+/* ------------------------------------------------------------------------------------------ */
+
+/* A tree of drafted tokens per sequence, as mask rows (host only). parent[i] (host int32, packed by q_cu) is the
+ * node before node i on its path, within its sequence and before it (-1: the node hangs under the context).
+ * mask (host uint32 [n_q][words]): bit j % 32 of word j / 32 set where node i sees draft j, its ancestors and itself.
+ * depth (host int32 [n_q], may be NULL): ancestors of a node; its rotary position is the sequence's next one plus that.
+ * Errors: SPD_EINVAL (a parent that does not come first, more than 32 * words nodes). */
+int spd_tree_mask(int n_seqs, const int32_t* q_cu, const int32_t* parent, int words, uint32_t* mask,
+                  int32_t* depth);
+
+/* Workspace bytes of spd_tree_attention (0 on invalid arguments). */
+size_t spd_tree_attention_workspace_size(int n_q, int n_seqs, int n_heads, int n_kv_heads, int head_dim);
+
+/* Attention of drafted tokens over one layer of a KV cache. Sequence b has ctx_len[b] committed rows in its cache slot
+ * and behind them, at slots ctx_len[b] + i, the rows of its nodes i = 0 .. q_cu[b + 1] - q_cu[b] - 1. Per head (head h
+ * reads K/V head h / (n_heads / n_kv_heads)), over the committed rows and the drafts of its own sequence that node i sees:
+ *   o_i = sum_j softmax_j(q_i . k_j / sqrt(head_dim)) v_j,   lse_i = log sum_j exp(q_i . k_j / sqrt(head_dim)).
+ * A row that sees nothing gets o = 0 and lse = -inf. What a row does not see contributes nothing, whatever it holds.
+ * One node a sequence is a decode step; a chain (tree_mask NULL) is a causal window.
+ * q, o (dev) bf16 [n_q][n_heads * head_dim], the nodes of sequence b in rows [q_cu[b], q_cu[b + 1]) (none is allowed);
+ * q_cu (HOST) int32 [n_seqs + 1] from 0 to n_q; ctx_len (HOST) int32 [n_seqs]; tree_mask (dev) uint32
+ * [n_q][mask_words] as spd_tree_mask makes it (any bits are allowed, a row of zeros too), or NULL: node i sees drafts
+ * 0..i; kv (dev) bf16 [n_seqs][max_len][K | V], a layer's block of the cache, K rotated; lse (dev) fp32 [n_q][n_heads],
+ * natural logarithm, may be NULL. head_dim 64 or 128; q, o and kv 16-byte aligned.
+ * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ENOSPC, SPD_ECUDA; device timeouts in the workspace's status word. */
+int spd_tree_attention(const uint16_t* q, int n_q, const int32_t* q_cu, const int32_t* ctx_len, int n_seqs,
+                       const uint32_t* tree_mask, int mask_words, const uint16_t* kv, int max_len, int n_heads,
+                       int n_kv_heads, int head_dim, uint16_t* o, float* lse, void* ws, size_t ws_bytes,
+                       void* stream);
+
+/* Workspace bytes of spd_tree_commit for paths of n_path nodes in all. */
+size_t spd_tree_commit_workspace_size(int n_seqs, int n_path);
+
+/* The accepted drafts join the context: in every layer the cache rows of sequence b's nodes path[path_cu[b]] ..
+ * path[path_cu[b + 1] - 1] (HOST int32, ascending) move from slots ctx_len[b] + node to slots ctx_len[b], ctx_len[b] + 1,
+ * ..., in place. The caller's context grows by the length of the path. kv_cache (dev) bf16
+ * [n_layers][n_seqs][max_len][K | V], 16-byte aligned; pos (dev, may be NULL) int32 [n_layers][n_seqs][n_kv_heads][max_len]
+ * receives next_pos[b] + i (HOST int32 [n_seqs]) in the new slots, acc (dev, may be NULL) fp32 of the same shape zeros.
+ * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ENOSPC, SPD_ECUDA. */
+int spd_tree_commit(uint16_t* kv_cache, int n_layers, int n_seqs, const int32_t* path, const int32_t* path_cu,
+                    const int32_t* ctx_len, int max_len, int n_kv_heads, int head_dim, const int32_t* next_pos,
+                    int32_t* pos, float* acc, void* ws, size_t ws_bytes, void* stream);
+
+/* The attention weight that every cached row receives, added to its running total. In each layer and for each K/V head g:
+ *   acc_out[slot] = decay * acc_in[slot] + sum over the sequence's rows i and the heads h of g's group of
+ *                   exp(q_ih . k_slot / sqrt(head_dim) - lse_ih),
+ * row i of the n rows of a sequence of lens[b] cached rows seeing slots 0 .. lens[b] - n + i: the rows are the last n
+ * cached tokens in order (the accepted drafts after a step, or a window at the end of the prompt). Rows whose lse is
+ * -inf add nothing.
+ * q (dev) bf16 [n_layers][n_q][n_heads * head_dim] and lse (dev) fp32 [n_layers][n_q][n_heads], of spd_tree_attention
+ * or spd_decode_tree; rows (dev) int32: the query row of every row, sequence b's at [rows_cu[b], rows_cu[b + 1]) (HOST
+ * int32 [n_seqs + 1] from 0), NULL = row i is query row i; indices outside [0, n_q) add nothing. lens (HOST) int32 [n_seqs]; kv_cache as
+ * spd_tree_commit; acc_in, acc_out (dev) fp32 [n_layers][n_seqs][n_kv_heads][max_len], the same buffer or apart; slots
+ * from lens[b] on are not written. head_dim 64 or 128; q and kv_cache 16-byte aligned.
+ * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ECUDA. */
+int spd_cache_weights(const uint16_t* q, const float* lse, int n_q, const int32_t* rows, const int32_t* rows_cu,
+                      const uint16_t* kv_cache, int n_layers, int n_seqs, const int32_t* lens, int max_len,
+                      int n_heads, int n_kv_heads, int head_dim, float decay, const float* acc_in,
+                      float* acc_out, void* stream);
+
+/* Workspace bytes of spd_cache_evict (0 on invalid arguments). */
+size_t spd_cache_evict_workspace_size(int n_layers, int n_seqs, int n_kv_heads, int budget);
+
+/* Eviction: of each sequence's lens[b] cached rows the min(lens[b], budget) best stay, chosen for every layer and K/V
+ * head by itself (different heads keep different tokens; all keep the same number, the sequence's new length). Rows
+ * whose position is below n_sink or at least next_pos[b] - n_recent come first (the lower slot first), the others follow by
+ * acc_in (larger first, the lower slot first among equals, NaN as -inf).
+ * Kept rows below the new length stay in their slots; the j-th kept row past it moves into the j-th slot that an evicted
+ * row left, both in slot order. So rows are not in the order of their positions afterwards, which attention does not ask
+ * for: K is rotated. In place; slots past the new length keep what they held.
+ * kv_cache as spd_tree_commit; lens, next_pos (HOST) int32 [n_seqs] (next_pos NULL = lens); acc_in, acc_out (dev) fp32
+ * and pos_in, pos_out (dev) int32, all [n_layers][n_seqs][n_kv_heads][max_len]: weight and rotary position of every
+ * slot, moved along; an out may be its in, or apart; slots from the new length to lens[b] get 0 and -1. pos_in NULL = the slot
+ * is the position (then pos_out may be NULL). src (dev, may be NULL) int32 [n_layers][n_seqs][n_kv_heads][budget]: the
+ * slot that every kept row came from. At most 393216 rows in a sequence that loses some.
+ * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ENOSPC, SPD_ECUDA. */
+int spd_cache_evict(uint16_t* kv_cache, int n_layers, int n_seqs, const int32_t* lens, int max_len, int n_kv_heads,
+                    int head_dim, int budget, int n_sink, int n_recent, const int32_t* next_pos,
+                    const float* acc_in, const int32_t* pos_in, float* acc_out, int32_t* pos_out, int32_t* src,
+                    void* ws, size_t ws_bytes, void* stream);
+
+/* Rules on logits. All arrays are (dev); a NULL list switches its rule off. */
+typedef struct {
+  const int32_t* seq_of;    /* [n_rows] sequence of a row (NULL: row r is sequence r); outside [0, n_seqs): no sequence */
+  int n_seqs;
+  const int32_t* hist;      /* [n_hist] tokens of prompt and answer; tokens outside the vocabulary (an image's
+                               placeholders) count for nothing */
+  const int32_t* hist_cu;   /* [n_seqs + 1] sequence b's tokens are hist[hist_cu[b] .. hist_cu[b + 1]) */
+  const int32_t* gen_start; /* [n_seqs] index into hist of the first generated token */
+  int n_hist;
+  const int32_t* path;      /* [n_path] further generated tokens of single rows (the drafts on a node's path) */
+  const int32_t* path_cu;   /* [n_rows + 1] */
+  int n_path;
+  const float* repetition;  /* [n_seqs] > 0; NULL: 1 */
+  const float* frequency;   /* [n_seqs]; NULL: 0 */
+  const float* presence;    /* [n_seqs]; NULL: 0 */
+  const int32_t* bias_cu;   /* [n_seqs + 1] */
+  const int32_t* bias_id;   /* [n_bias] tokens, ascending within a sequence (one listed twice gets both) */
+  const float* bias;        /* [n_bias] */
+  int n_bias;
+  const int32_t* allow;     /* [n_rules][(vocab + 31) / 32] grammars: bit t % 32 of word t / 32 set = token t is allowed */
+  int n_rules;
+  const int32_t* rule;      /* [n_rows] the row's grammar; outside [0, n_rules): everything is allowed */
+} spd_logits_rules;
+
+/* Penalties, biases and grammar masks, and the best token left. For every row, token t with n_t occurrences among the
+ * generated tokens of its sequence and its own path, each step one fp32 operation in this order:
+ *   x = z > 0 ? z / repetition : z * repetition   where t occurs in prompt, answer or path;
+ *   x = x - frequency * n_t - presence            where n_t > 0;
+ *   x = x + bias;    x = -inf where the grammar does not allow t.
+ * logits (dev) fp32 [n_rows] rows of vocab values, stride ld; out (dev) fp32, stride ld_out (in place: the same buffer
+ * and stride); best (dev, may be NULL) int32 [n_rows]: the first token of the largest x, NaN left out, -1 where every
+ * token is -inf. Up to 819200 words. Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ECUDA. */
+int spd_logits_process(const float* logits, int n_rows, int vocab, int ld, const spd_logits_rules* rules,
+                       float* out, int ld_out, int32_t* best, void* stream);
+
+/* ------------------------------------------------------------------------------------------ */
 /* Single kernels, exposed for composition and per-kernel tests                                 */
 /* ------------------------------------------------------------------------------------------ */
 

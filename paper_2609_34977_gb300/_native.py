@@ -31,7 +31,10 @@ EXPORTS = ("spd_last_error", "spd_workspace_status", "spd_selftest_bounded_wait"
            "spd_trace_read", "spd_prune_workspace", "spd_prefill_workspace", "spd_gather_bf16",
            "spd_last_error_detail", "spd_check", "spd_plan_from_layer_mask", "spd_prefill_admit",
            "spd_stamp_enable", "spd_stamp_read", "spd_stamp_launch", "spd_set_deterministic",
-           "spd_step_workspace_size", "spd_step", "spd_step_status")
+           "spd_step_workspace_size", "spd_step", "spd_step_status",
+           "spd_tree_mask", "spd_tree_attention_workspace_size", "spd_tree_attention",
+           "spd_tree_commit_workspace_size", "spd_tree_commit", "spd_cache_weights",
+           "spd_cache_evict_workspace_size", "spd_cache_evict", "spd_logits_process")
 TRACE_GEMM, TRACE_ATTN, TRACE_ROWS, TRACE_PRUNE = 0, 1, 2, 3
 
 
@@ -66,6 +69,14 @@ class SkipPolicy(C.Structure):
     _fields_ = [("t_skip", C.c_float), ("w1", C.c_float), ("w2", C.c_float), ("window", C.c_int),
                 ("slc_norm", C.c_void_p), ("layer_target", C.c_void_p), ("is_visual", C.c_void_p),
                 ("ablate", C.c_int), ("device_plan", C.c_int)]
+
+
+class LogitsRules(C.Structure):
+    _fields_ = [("seq_of", C.c_void_p), ("n_seqs", C.c_int), ("hist", C.c_void_p), ("hist_cu", C.c_void_p),
+                ("gen_start", C.c_void_p), ("n_hist", C.c_int), ("path", C.c_void_p), ("path_cu", C.c_void_p),
+                ("n_path", C.c_int), ("repetition", C.c_void_p), ("frequency", C.c_void_p),
+                ("presence", C.c_void_p), ("bias_cu", C.c_void_p), ("bias_id", C.c_void_p), ("bias", C.c_void_p),
+                ("n_bias", C.c_int), ("allow", C.c_void_p), ("n_rules", C.c_int), ("rule", C.c_void_p)]
 
 
 SPD_SKIP_NO_ENTROPY = 1
@@ -146,6 +157,15 @@ def lib():
                                    C.POINTER(C.c_double)]),
             "spd_trace_read": (i, [i, C.POINTER(ll), C.POINTER(C.c_double), C.POINTER(C.c_double),
                                    C.POINTER(C.c_double)]),
+            "spd_tree_mask": (i, [i, vp, vp, i, vp, vp]),
+            "spd_tree_attention_workspace_size": (sz, [i, i, i, i, i]),
+            "spd_tree_attention": (i, [vp, i, vp, vp, i, vp, i, vp, i, i, i, i, vp, vp, vp, sz, vp]),
+            "spd_tree_commit_workspace_size": (sz, [i, i]),
+            "spd_tree_commit": (i, [vp, i, i, vp, vp, vp, i, i, i, vp, vp, vp, vp, sz, vp]),
+            "spd_cache_weights": (i, [vp, vp, i, vp, vp, vp, i, i, vp, i, i, i, i, C.c_float, vp, vp, vp]),
+            "spd_cache_evict_workspace_size": (sz, [i, i, i, i]),
+            "spd_cache_evict": (i, [vp, i, i, vp, i, i, i, i, i, i, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+            "spd_logits_process": (i, [vp, i, i, i, C.POINTER(LogitsRules), vp, i, vp, vp]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -497,6 +517,134 @@ def spd_last_error_detail() -> str:
     buf = C.create_string_buffer(512)
     lib().spd_last_error_detail(buf, 512)
     return buf.value.decode()
+
+
+def spd_tree_mask(parent, q_cu, words=None):
+    """Mask rows (uint32 [n_q][words]) and depths of a tree of drafted tokens per sequence, from every node's parent."""
+    cu = np.ascontiguousarray(q_cu, dtype=np.int32)
+    up = _host(parent, np.int32, int(cu[-1]), "parent")
+    if words is None:
+        words = max(1, (int(np.diff(cu).max()) + 31) // 32)
+    mask = np.zeros((int(cu[-1]), words), np.uint32)
+    depth = np.zeros(int(cu[-1]), np.int32)
+    _check(lib().spd_tree_mask(len(cu) - 1, _p(cu), _p(up), words, _p(mask), _p(depth)))
+    return mask, depth
+
+
+def spd_tree_attention_workspace_size(n_q: int, n_seqs: int, n_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    return int(lib().spd_tree_attention_workspace_size(n_q, n_seqs, n_heads, n_kv_heads, head_dim))
+
+
+def spd_tree_attention(q, q_cu, ctx_len, tree_mask, kv, max_len, n_heads, n_kv_heads, head_dim, o, lse, ws,
+                       stream=None):
+    """Attention of the nodes q of a draft tree per sequence over the ctx_len committed rows and the drafts' rows of one
+    layer's cache block kv [n_seqs][max_len][K | V]; tree_mask: int32 device words [n_q][words] or None (chains)."""
+    cu = np.ascontiguousarray(q_cu, dtype=np.int32)
+    B, n_q = len(cu) - 1, int(cu[-1])
+    ctx = _host(ctx_len, np.int32, B, "ctx_len")
+    words = 0 if tree_mask is None else tree_mask.shape[-1]
+    qd = n_heads * head_dim
+    wp, wb = _ws(ws)
+    _check(lib().spd_tree_attention(_dev(q, "bf16", n_q * qd, "q"), n_q, _p(cu), _p(ctx), B,
+                                    _dev(tree_mask, "i32", n_q * words, "tree_mask", True), words,
+                                    _dev(kv, "bf16", B * max_len * 2 * n_kv_heads * head_dim, "kv"), max_len, n_heads,
+                                    n_kv_heads, head_dim, _dev(o, "bf16", n_q * qd, "o"),
+                                    _dev(lse, "f32", n_q * n_heads, "lse", True), wp, wb, _stream(stream)))
+
+
+def spd_tree_commit_workspace_size(n_seqs: int, n_path: int) -> int:
+    return int(lib().spd_tree_commit_workspace_size(n_seqs, n_path))
+
+
+def spd_tree_commit(kv_cache, n_layers, path, path_cu, ctx_len, max_len, n_kv_heads, head_dim, ws, next_pos=None,
+                    pos=None, acc=None, stream=None):
+    """Moves every sequence's accepted nodes (host path, delimited by path_cu, ascending) behind its context."""
+    cu = np.ascontiguousarray(path_cu, dtype=np.int32)
+    B = len(cu) - 1
+    pa = _host(path, np.int32, int(cu[-1]), "path")
+    ctx = _host(ctx_len, np.int32, B, "ctx_len")
+    nxt = None if next_pos is None else _host(next_pos, np.int32, B, "next_pos")
+    units = n_layers * B * n_kv_heads * max_len
+    wp, wb = _ws(ws)
+    _check(lib().spd_tree_commit(_dev(kv_cache, "bf16", units * 2 * head_dim, "kv_cache"), n_layers, B, _p(pa), _p(cu),
+                                 _p(ctx), max_len, n_kv_heads, head_dim, _p(nxt), _dev(pos, "i32", units, "pos", True),
+                                 _dev(acc, "f32", units, "acc", True), wp, wb, _stream(stream)))
+
+
+def spd_cache_weights(q, lse, rows, rows_cu, kv_cache, lens, max_len, n_heads, n_kv_heads, head_dim, decay, acc_in,
+                      acc_out, stream=None):
+    """acc_out = decay * acc_in + the attention weight that every cached row receives from the sequences' last rows; q
+    [n_layers][n_q][n_heads * head_dim], rows: query row of every row (device int32) or None."""
+    cu = np.ascontiguousarray(rows_cu, dtype=np.int32)
+    L, n_q, B = q.shape[0], q.shape[1], len(cu) - 1
+    ln = _host(lens, np.int32, B, "lens")
+    units = L * B * n_kv_heads * max_len
+    _check(lib().spd_cache_weights(_dev(q, "bf16", L * n_q * n_heads * head_dim, "q"), _dev(lse, "f32", L * n_q * n_heads, "lse"),
+                                   n_q, _dev(rows, "i32", int(cu[-1]), "rows", True), _p(cu),
+                                   _dev(kv_cache, "bf16", units * 2 * head_dim, "kv_cache"), L, B, _p(ln), max_len, n_heads,
+                                   n_kv_heads, head_dim, float(decay), _dev(acc_in, "f32", units, "acc_in"),
+                                   _dev(acc_out, "f32", units, "acc_out"), _stream(stream)))
+
+
+def spd_cache_evict_workspace_size(n_layers: int, n_seqs: int, n_kv_heads: int, budget: int) -> int:
+    return int(lib().spd_cache_evict_workspace_size(n_layers, n_seqs, n_kv_heads, budget))
+
+
+def spd_cache_evict(kv_cache, lens, max_len, n_kv_heads, head_dim, budget, n_sink, n_recent, next_pos, acc_in, pos_in,
+                    acc_out, pos_out, src, ws, stream=None):
+    """Keeps the `budget` best rows of every layer, sequence and K/V head of kv_cache (in place); acc_* and pos_* are
+    [n_layers][n_seqs][n_kv_heads][max_len]. Returns the new lengths (host int32)."""
+    ln = np.ascontiguousarray(lens, dtype=np.int32)
+    L, B = acc_in.shape[0], len(ln)
+    nxt = None if next_pos is None else _host(next_pos, np.int32, B, "next_pos")
+    n = L * B * n_kv_heads
+    units = n * max_len
+    wp, wb = _ws(ws)
+    _check(lib().spd_cache_evict(_dev(kv_cache, "bf16", units * 2 * head_dim, "kv_cache"), L, B, _p(ln), max_len, n_kv_heads,
+                                 head_dim, budget, n_sink, n_recent, _p(nxt), _dev(acc_in, "f32", units, "acc_in"),
+                                 _dev(pos_in, "i32", units, "pos_in", True), _dev(acc_out, "f32", units, "acc_out"),
+                                 _dev(pos_out, "i32", units, "pos_out", True), _dev(src, "i32", n * budget, "src", True),
+                                 wp, wb, _stream(stream)))
+    return np.minimum(ln, budget)
+
+
+def _rows_f32(t, name):
+    """Pointer and row stride of a 2-D fp32 CUDA tensor whose rows are contiguous."""
+    if not getattr(t, "is_cuda", False):
+        raise TypeError(f"{name}: device arguments of libspider must be CUDA tensors")
+    if str(t.dtype) != "torch.float32" or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: expected fp32 [rows][vocab] with contiguous rows")
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError(f"{name}: rows overlap")
+    return t.data_ptr(), max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+
+
+def spd_logits_process(logits, out, best=None, *, seq_of=None, hist=None, hist_cu=None, gen_start=None, path=None,
+                       path_cu=None, repetition=None, frequency=None, presence=None, bias_cu=None, bias_id=None, bias=None,
+                       allow=None, rule=None, stream=None):
+    """Penalties, biases and grammar masks on logits [n_rows][vocab] (rows may have a stride), into out (may be logits)
+    and the best token of every row into best. Lists are device tensors; None switches a rule off."""
+    zp, ld = _rows_f32(logits, "logits")
+    op, ldo = _rows_f32(out, "out")
+    n, v = logits.shape
+    if tuple(out.shape) != (n, v):
+        raise ValueError(f"out: shape {tuple(out.shape)}, logits are {(n, v)}")
+    per_seq = [t for t in (gen_start, repetition, frequency, presence) if t is not None]
+    starts = [t for t in (hist_cu, bias_cu) if t is not None]
+    B = min([t.numel() for t in per_seq] + [t.numel() - 1 for t in starts], default=n if seq_of is None else 0)
+    cnt = lambda t: 0 if t is None else t.numel()  # noqa: E731
+    n_bias = cnt(bias) if bias_id is None else min(cnt(bias), cnt(bias_id))
+    words = (v + 31) // 32
+    n_rules = 0 if allow is None else allow.numel() // words
+    r = LogitsRules(_dev(seq_of, "i32", n, "seq_of", True), max(B, 0), _dev(hist, "i32", 0, "hist", True),
+                    _dev(hist_cu, "i32", B + 1, "hist_cu", True), _dev(gen_start, "i32", B, "gen_start", True), cnt(hist),
+                    _dev(path, "i32", 0, "path", True), _dev(path_cu, "i32", n + 1, "path_cu", True), cnt(path),
+                    _dev(repetition, "f32", B, "repetition", True), _dev(frequency, "f32", B, "frequency", True),
+                    _dev(presence, "f32", B, "presence", True), _dev(bias_cu, "i32", B + 1, "bias_cu", True),
+                    _dev(bias_id, "i32", n_bias, "bias_id", True), _dev(bias, "f32", n_bias, "bias", True), n_bias,
+                    _dev(allow, "i32", n_rules * words, "allow", True), n_rules, _dev(rule, "i32", n, "rule", True))
+    _check(lib().spd_logits_process(zp, n, v, ld, C.byref(r), op, ldo, _dev(best, "i32", n, "best", True),
+                                    _stream(stream)))
 
 
 def spd_linear_workspace_size(M: int, N: int) -> int:

@@ -1,0 +1,584 @@
+// Keeping a KV cache within a budget: the weight its rows receive, the eviction of those that receive least, and the
+// move of an accepted path of drafts to the end of the context.
+//
+// Cache rows are [K of every K/V head | V of every K/V head], bf16, at row (layer * n_seqs + seq) * max_len + slot. A
+// "unit" is one layer, sequence and K/V head: rows of a unit are evicted by the unit's own weights, so a slot holds
+// different tokens in different units, and `pos` (int32 a unit and slot) says which.
+#include <cooperative_groups.h>
+#include <cuda_bf16.h>
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <algorithm>
+#include <vector>
+
+#include "internal.h"
+#include "ptx.cuh"
+#include "trace.h"
+
+namespace spd {
+namespace {
+
+namespace cg = cooperative_groups;
+
+// ---- eviction ------------------------------------------------------------------------------------
+// Of a unit's n rows the `keep` best stay: those that `pos` protects (the first n_sink positions and the n_recent
+// before next_pos), then by accumulated weight, the lower slot first among equals. Kept rows below slot `keep` stay
+// where they are; the j-th kept row past it moves into the j-th hole. Sources and targets of the moves are disjoint,
+// so they run in place, all at once, and a step that evicts a few rows of a long cache moves a few rows. (Closing the
+// gaps in order would move every row behind the first hole.)
+//
+// Selection: the weights as order-preserving 32-bit keys in shared memory (a cluster of CTAs where a unit has more than
+// one holds), the keep-th largest found two bits a round by counting the keys that reach each of three candidates (no
+// atomics: the usual histograms of exponent bits put most keys on a handful of addresses), then two prefix sums.
+constexpr int kSelThreads = 1024;
+constexpr int kSelWarps = kSelThreads / 32;
+constexpr int kSelMost = 49152;     // keys a CTA holds (192 KB)
+constexpr int kSelMaxCluster = 8;
+constexpr int kMaxSeqs = 240;       // sequences whose sizes fit in a launch's parameters
+constexpr uint32_t kHeld = 0xffffffffu;
+
+struct EvictSeqs {  // by value in the launch's parameters: no copy, no wait for one
+  int len[kMaxSeqs];
+  int next_pos[kMaxSeqs];
+};
+
+struct EvictArgs {
+  int n_seqs, seq0, launch_seqs, n_kv_heads, max_len, budget, n_sink, n_recent;
+  const float* acc_in;
+  const int32_t* pos_in;
+  float* acc_out;
+  int32_t* pos_out;
+  int32_t* src;
+  int32_t *fill, *hole, *moves;  // [unit][budget] x 2, [unit]
+};
+
+__device__ __forceinline__ uint32_t weight_key(float a) {
+  if (isnan(a)) a = -INFINITY;
+  const uint32_t u = __float_as_uint(a + 0.0f);  // -0 as 0
+  return (u >> 31) ? ~u : u | 0x80000000u;
+}
+
+// Exclusive prefix sum over the block of a value below 2^16 a thread; *total the block's sum. tmp: kSelWarps ints.
+__device__ int block_before(int v, int* tmp, int* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int x = v;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, off);
+    if (lane >= off) x += y;
+  }
+  if (lane == 31) tmp[warp] = x;
+  __syncthreads();
+  int w = tmp[lane];
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, w, off);
+    if (lane >= off) w += y;
+  }
+  const int before = (warp ? __shfl_sync(0xffffffffu, w, warp - 1) : 0) + x - v;
+  *total = __shfl_sync(0xffffffffu, w, 31);
+  __syncthreads();
+  return before;
+}
+
+__global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_constant__ EvictArgs p,
+                                                                   const __grid_constant__ EvictSeqs seqs, int per) {
+  extern __shared__ uint32_t key[];  // [per]: this CTA's slots
+  __shared__ int tmp[kSelWarps];
+  __shared__ int part[kSelWarps][3];
+  __shared__ int counts[2][3];       // of this CTA, by round parity: keys that reach each candidate
+  __shared__ int shared_total[2];    // ties; holes (low half) and fills (high half are separate words)
+  __shared__ int shared_moves[2];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int C = int(cluster.num_blocks()), rank = int(cluster.block_rank());
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int per_layer = p.launch_seqs * p.n_kv_heads;
+  const int local = int(blockIdx.x) / C, layer = local / per_layer, at = local - layer * per_layer;
+  const int ls = at / p.n_kv_heads, g = at - ls * p.n_kv_heads;
+  const size_t unit = (size_t(layer) * p.n_seqs + p.seq0 + ls) * p.n_kv_heads + g;
+  const int n = seqs.len[ls], keep = min(n, p.budget), next = seqs.next_pos[ls];
+  pdl_launch_dependents();
+  pdl_wait();
+  const float* acc = p.acc_in + unit * p.max_len;
+  const int32_t* pos = p.pos_in ? p.pos_in + unit * p.max_len : nullptr;
+  float* acc_out = p.acc_out + unit * p.max_len;
+  int32_t* pos_out = p.pos_out ? p.pos_out + unit * p.max_len : nullptr;
+  int32_t* src = p.src ? p.src + unit * p.budget : nullptr;
+  const int lo = min(n, rank * per), cnt = min(n, lo + per) - lo;  // this CTA's slots
+  if (n <= p.budget) {  // nothing leaves (every CTA of the cluster agrees)
+    for (int i = tid; i < cnt; i += kSelThreads) {
+      acc_out[lo + i] = acc[lo + i];
+      if (pos_out) pos_out[lo + i] = pos ? pos[lo + i] : lo + i;
+      if (src) src[lo + i] = lo + i;
+    }
+    if (rank == 0 && tid == 0) p.moves[unit] = 0;
+    return;
+  }
+  for (int i = tid; i < per; i += kSelThreads) {
+    uint32_t k = 0;  // below every weight's key
+    if (i < cnt) {
+      const int q = pos ? pos[lo + i] : lo + i;
+      k = q < p.n_sink || q >= next - p.n_recent ? kHeld : weight_key(acc[lo + i]);
+    }
+    key[i] = k;
+  }
+  __syncthreads();
+  // the largest threshold that at least `keep` keys reach
+  uint32_t thr = 0;
+  int reach = n;
+  for (int bit = 30, round = 0; bit >= 0; bit -= 2, ++round) {
+    int c1 = 0, c2 = 0, c3 = 0;
+    const uint32_t t1 = thr | (1u << bit), t2 = thr | (2u << bit), t3 = thr | (3u << bit);
+    for (int i = 4 * tid; i < per; i += 4 * kSelThreads) {
+      const uint4 k = *reinterpret_cast<const uint4*>(key + i);
+      c1 += (k.x >= t1) + (k.y >= t1) + (k.z >= t1) + (k.w >= t1);
+      c2 += (k.x >= t2) + (k.y >= t2) + (k.z >= t2) + (k.w >= t2);
+      c3 += (k.x >= t3) + (k.y >= t3) + (k.z >= t3) + (k.w >= t3);
+    }
+    c1 = __reduce_add_sync(0xffffffffu, c1);
+    c2 = __reduce_add_sync(0xffffffffu, c2);
+    c3 = __reduce_add_sync(0xffffffffu, c3);
+    if (lane == 0) {
+      part[warp][0] = c1;
+      part[warp][1] = c2;
+      part[warp][2] = c3;
+    }
+    __syncthreads();
+    if (warp < 3) {
+      const int s = __reduce_add_sync(0xffffffffu, part[lane][warp]);
+      if (lane == 0) counts[round & 1][warp] = s;
+    }
+    if (C > 1) cluster.sync();
+    else __syncthreads();
+    int r1 = 0, r2 = 0, r3 = 0;
+    for (int c = 0; c < C; ++c) {
+      const int* q = C > 1 ? cluster.map_shared_rank(&counts[round & 1][0], c) : &counts[round & 1][0];
+      r1 += q[0];
+      r2 += q[1];
+      r3 += q[2];
+    }
+    if (r3 >= keep) thr = t3, reach = r3;
+    else if (r2 >= keep) thr = t2, reach = r2;
+    else if (r1 >= keep) thr = t1, reach = r1;
+    if (reach == keep) break;  // the same in every thread: the keys that reach it are the kept ones
+  }
+  // a thread's slots are consecutive, so that prefix sums run in slot order
+  const int each = (per + kSelThreads - 1) / kSelThreads;
+  const int i0 = min(cnt, tid * each), i1 = min(cnt, i0 + each);
+  int ties = 0, above = 0;
+  for (int i = i0; i < i1; ++i) {
+    ties += key[i] == thr;
+    above += key[i] > thr;
+  }
+  int tie_total, all_above;
+  int tie_before = block_before(ties, tmp, &tie_total);
+  block_before(above, tmp, &all_above);
+  if (tid == 0) {
+    shared_total[0] = tie_total;
+    shared_total[1] = all_above;
+  }
+  if (C > 1) cluster.sync();
+  else __syncthreads();
+  int take = keep;  // ties that stay: the lowest slots
+  for (int c = 0; c < C; ++c) {
+    const int* q = C > 1 ? cluster.map_shared_rank(shared_total, c) : shared_total;
+    take -= q[1];
+    if (c < rank) tie_before += q[0];
+  }
+  int holes = 0, fills = 0, t = tie_before;
+  for (int i = i0; i < i1; ++i) {
+    const bool kept = key[i] > thr || (key[i] == thr && t++ < take);
+    holes += !kept && lo + i < keep;
+    fills += kept && lo + i >= keep;
+  }
+  int hole_total, fill_total;
+  int hole_at = block_before(holes, tmp, &hole_total), fill_at = block_before(fills, tmp, &fill_total);
+  if (tid == 0) {
+    shared_moves[0] = hole_total;
+    shared_moves[1] = fill_total;
+  }
+  if (C > 1) cluster.sync();
+  else __syncthreads();
+  int moves = 0;
+  for (int c = 0; c < C; ++c) {
+    const int* q = C > 1 ? cluster.map_shared_rank(shared_moves, c) : shared_moves;
+    moves += q[0];
+    if (c < rank) {
+      hole_at += q[0];
+      fill_at += q[1];
+    }
+  }
+  int32_t *fill = p.fill + unit * p.budget, *hole = p.hole + unit * p.budget;
+  t = tie_before;
+  for (int i = i0; i < i1; ++i) {
+    const int s = lo + i;
+    const bool kept = key[i] > thr || (key[i] == thr && t++ < take);
+    if (s < keep) {
+      if (kept) {
+        acc_out[s] = acc[s];
+        if (pos_out) pos_out[s] = pos ? pos[s] : s;
+        if (src) src[s] = s;
+      } else {
+        hole[hole_at++] = s;
+      }
+    } else if (kept) {
+      fill[fill_at++] = s;
+    }
+  }
+  __threadfence();  // the lists, for the other CTAs of the cluster
+  if (C > 1) cluster.sync();
+  else __syncthreads();
+  for (int j = rank * kSelThreads + tid; j < moves; j += C * kSelThreads) {
+    const int s = __ldcg(hole + j), f = __ldcg(fill + j);
+    acc_out[s] = acc[f];
+    if (pos_out) pos_out[s] = pos ? pos[f] : f;
+    if (src) src[s] = f;
+  }
+  if (rank == 0 && tid == 0) p.moves[unit] = moves;
+  if (C > 1) cluster.sync();  // before the slots past the budget are cleared, which may be the ones read above
+  else __syncthreads();
+  for (int s = keep + rank * kSelThreads + tid; s < n; s += C * kSelThreads) {
+    acc_out[s] = 0.0f;
+    if (pos_out) pos_out[s] = -1;
+  }
+}
+
+// The rows themselves: a warp a move, 16 bytes a lane (half a warp K, half V; HD = 64: a quarter each), four moves in
+// flight a warp.
+constexpr int kMoveWarps = 8, kMoveDepth = 4;
+template <int HD>
+__global__ void __launch_bounds__(kMoveWarps * 32) evict_move_kernel(uint16_t* kv, const __grid_constant__ EvictArgs p) {
+  constexpr int VEC = HD / 8;  // 16-byte pieces of a head's K or V row
+  constexpr int ROWS = 32 / (2 * VEC);  // moves a warp takes at once
+  pdl_launch_dependents();
+  pdl_wait();
+  const int local = blockIdx.y, per_layer = p.launch_seqs * p.n_kv_heads, layer = local / per_layer;
+  const int at = local - layer * per_layer, ls = at / p.n_kv_heads, g = at - ls * p.n_kv_heads;
+  const size_t seq = size_t(layer) * p.n_seqs + p.seq0 + ls, unit = seq * p.n_kv_heads + g;
+  const int moves = p.moves[unit];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int sub = lane / (2 * VEC), e = lane % (2 * VEC), kvd = p.n_kv_heads * HD;
+  const int col = (e / VEC) * kvd + g * HD + (e % VEC) * 8;
+  uint16_t* base = kv + seq * p.max_len * (2 * size_t(kvd)) + col;
+  const int32_t *fill = p.fill + unit * p.budget, *hole = p.hole + unit * p.budget;
+  const int j0 = (blockIdx.x * kMoveWarps + warp) * (kMoveDepth * ROWS) + sub;
+  uint4 v[kMoveDepth];
+#pragma unroll
+  for (int u = 0; u < kMoveDepth; ++u)
+    if (j0 + u * ROWS < moves)
+      v[u] = *reinterpret_cast<const uint4*>(base + size_t(fill[j0 + u * ROWS]) * (2 * kvd));
+#pragma unroll
+  for (int u = 0; u < kMoveDepth; ++u)
+    if (j0 + u * ROWS < moves) *reinterpret_cast<uint4*>(base + size_t(hole[j0 + u * ROWS]) * (2 * kvd)) = v[u];
+}
+
+// ---- commit ----------------------------------------------------------------------------------------
+// Sequence b's accepted drafts path[cu[b] .. cu[b + 1]) (ascending node numbers) move from slots ctx + node to slots
+// ctx, ctx + 1, ... of every layer. A target is at or before its source and before every later source, so one thread
+// that walks a column of the row through the path in order needs no second buffer.
+struct CommitArgs {
+  int n_seqs, max_len, row16;  // row16: 16-byte pieces of a cache row
+  int n_kv_heads;
+  const int32_t *path, *cu, *ctx, *pos0;
+  int32_t* pos;                // [unit][max_len] or null
+  float* acc;                  // [unit][max_len] or null
+};
+__global__ void __launch_bounds__(256) commit_kernel(uint4* kv, const __grid_constant__ CommitArgs p) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int b = blockIdx.y, layer = blockIdx.z;
+  const int c0 = p.cu[b], n = p.cu[b + 1] - c0, ctx = p.ctx[b];
+  const size_t seq = size_t(layer) * p.n_seqs + b;
+  const int col = blockIdx.x * 256 + threadIdx.x;
+  if (col < p.row16) {
+    uint4* base = kv + (seq * p.max_len + ctx) * p.row16 + col;
+    for (int i0 = 0; i0 < n; i0 += 8) {  // eight rows in flight: later targets lie before their sources
+      uint4 v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (i0 + u < n) v[u] = base[size_t(p.path[c0 + i0 + u]) * p.row16];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (i0 + u < n && p.path[c0 + i0 + u] != i0 + u) base[size_t(i0 + u) * p.row16] = v[u];
+    }
+  }
+  if (blockIdx.x == 0) {
+    for (int e = threadIdx.x; e < n * p.n_kv_heads; e += 256) {
+      const size_t at = (seq * p.n_kv_heads + e / n) * p.max_len + ctx + e % n;
+      if (p.pos) p.pos[at] = p.pos0[b] + e % n;
+      if (p.acc) p.acc[at] = 0.0f;
+    }
+  }
+}
+
+// ---- received weight ---------------------------------------------------------------------------------
+struct WeightSeqs {
+  int len[kMaxSeqs];
+  int cu[kMaxSeqs + 1];
+};
+struct WeightArgs {
+  const __nv_bfloat16* q;
+  const float* lse;
+  const int32_t* rows;
+  const __nv_bfloat16* kv;
+  int n_q, n_seqs, seq0, max_len, n_heads, n_kv_heads;
+  float scale, decay;
+  const float* acc_in;
+  float* acc_out;
+};
+
+// One warp a key: every row's score is a dot product over the lanes.
+template <int HD>
+__global__ void __launch_bounds__(256) weights_kernel(const __grid_constant__ WeightArgs p,
+                                                      const __grid_constant__ WeightSeqs seqs) {
+  constexpr int D = HD / 32;
+  pdl_launch_dependents();
+  pdl_wait();
+  const int ls = blockIdx.y / p.n_kv_heads, g = blockIdx.y % p.n_kv_heads, layer = blockIdx.z;
+  const int len = seqs.len[ls], c0 = seqs.cu[ls], n = seqs.cu[ls + 1] - c0, G = p.n_heads / p.n_kv_heads;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, slot = blockIdx.x * 8 + warp;
+  if (slot >= len) return;
+  const size_t seq = size_t(layer) * p.n_seqs + p.seq0 + ls;
+  const __nv_bfloat16* k = p.kv + (seq * p.max_len + slot) * (2 * size_t(p.n_kv_heads) * HD) + g * HD + D * lane;
+  float kf[D];
+#pragma unroll
+  for (int e = 0; e < D; ++e) kf[e] = __bfloat162float(k[e]);
+  float sum = 0.0f;
+  for (int i = 0; i < n; ++i) {
+    if (slot >= len - n + i + 1) continue;
+    const int at = p.rows ? p.rows[c0 + i] : c0 + i;
+    if (at < 0 || at >= p.n_q) continue;
+    const size_t row = size_t(layer) * p.n_q + at;
+    for (int m = 0; m < G; ++m) {
+      const __nv_bfloat16* q = p.q + (row * p.n_heads + g * G + m) * HD + D * lane;
+      float s = 0.0f;
+#pragma unroll
+      for (int e = 0; e < D; ++e) s = fmaf(__bfloat162float(q[e]), kf[e], s);
+#pragma unroll
+      for (int off = 16; off; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+      const float l = p.lse[row * p.n_heads + g * G + m];
+      if (l > -INFINITY) sum += expf(s * p.scale - l);
+    }
+  }
+  if (lane == 0) {
+    const size_t to = (seq * p.n_kv_heads + g) * p.max_len + slot;
+    p.acc_out[to] = fmaf(p.decay, p.acc_in[to], sum);
+  }
+}
+
+}  // namespace
+}  // namespace spd
+
+using namespace spd;
+
+extern "C" size_t spd_cache_evict_workspace_size(int n_layers, int n_seqs, int n_kv_heads, int budget) {
+  if (n_layers < 1 || n_seqs < 1 || n_kv_heads < 1 || budget < 1) return 0;
+  const size_t units = size_t(n_layers) * n_seqs * n_kv_heads;
+  Carve cv(nullptr, ~size_t(0));
+  cv.take<int32_t>(units * budget);
+  cv.take<int32_t>(units * budget);
+  cv.take<int32_t>(units);
+  return cv.used;
+}
+
+extern "C" int spd_cache_evict(uint16_t* kv_cache, int n_layers, int n_seqs, const int32_t* lens, int max_len,
+                               int n_kv_heads, int head_dim, int budget, int n_sink, int n_recent,
+                               const int32_t* next_pos, const float* acc_in, const int32_t* pos_in, float* acc_out,
+                               int32_t* pos_out, int32_t* src, void* ws, size_t ws_bytes, void* stream) {
+  if (!kv_cache || !lens || !acc_in || !acc_out || !ws || n_layers < 1 || n_seqs < 1 || n_kv_heads < 1 || max_len < 1 ||
+      budget < 1 || n_sink < 0 || n_recent < 0)
+    return fail(SPD_EINVAL, "bad eviction arguments");
+  if (head_dim != 64 && head_dim != 128) return fail(SPD_EUNSUPPORTED, "head_dim must be 64 or 128");
+  if (pos_in && !next_pos) return fail(SPD_EINVAL, "positions need next_pos");
+  if (pos_in && !pos_out) return fail(SPD_EINVAL, "positions need pos_out");
+  if (reinterpret_cast<uintptr_t>(kv_cache) & 15) return fail(SPD_EINVAL, "the cache must be 16-byte aligned");
+  int longest = 0, most_moves = 0;
+  for (int b = 0; b < n_seqs; ++b) {
+    if (lens[b] < 0 || lens[b] > max_len) return fail(SPD_EINVAL, "length of sequence %d outside [0, max_len]", b);
+    if (lens[b] > budget) {
+      longest = std::max(longest, lens[b]);
+      most_moves = std::max(most_moves, std::min(budget, lens[b] - budget));
+    }
+  }
+  if (longest > kSelMost * kSelMaxCluster)
+    return fail(SPD_EUNSUPPORTED, "eviction from more than %d rows", kSelMost * kSelMaxCluster);
+  const size_t units = size_t(n_layers) * n_seqs * n_kv_heads;
+  if (units > 65535) return fail(SPD_EUNSUPPORTED, "more than 65535 layers x sequences x K/V heads");
+  Carve cv(ws, ws_bytes);
+  EvictArgs p{};
+  p.fill = cv.take<int32_t>(units * budget);
+  p.hole = cv.take<int32_t>(units * budget);
+  p.moves = cv.take<int32_t>(units);
+  if (!cv.fits()) return fail(SPD_ENOSPC, "eviction workspace too small (%zu < %zu)", ws_bytes, cv.used);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  p.n_seqs = n_seqs;
+  p.n_kv_heads = n_kv_heads;
+  p.max_len = max_len;
+  p.budget = budget;
+  p.n_sink = n_sink;
+  p.n_recent = n_recent;
+  p.acc_in = acc_in;
+  p.pos_in = pos_in;
+  p.acc_out = acc_out;
+  p.pos_out = pos_out;
+  p.src = src;
+  int C = 1;
+  while (C < kSelMaxCluster && longest > 16384 * C) C *= 2;
+  int per = (std::max(longest, 1) + C - 1) / C;
+  for (int b = 0; b < n_seqs; ++b) per = std::max(per, (std::min(lens[b], budget) + C - 1) / C);
+  per = (per + 3) & ~3;
+  SPD_CUDA_TRY(cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelMost * 4));
+  const size_t smem = longest ? size_t(per) * 4 : 16;
+  for (int s0 = 0; s0 < n_seqs; s0 += kMaxSeqs) {
+    EvictSeqs sq;
+    p.seq0 = s0;
+    p.launch_seqs = std::min(kMaxSeqs, n_seqs - s0);
+    double rows = 0.0, moved = 0.0;
+    for (int b = 0; b < p.launch_seqs; ++b) {
+      sq.len[b] = lens[s0 + b];
+      sq.next_pos[b] = next_pos ? next_pos[s0 + b] : lens[s0 + b];
+      rows += lens[s0 + b];
+      if (lens[s0 + b] > budget) moved += std::min(budget, lens[s0 + b] - budget);
+    }
+    const int n = n_layers * p.launch_seqs * n_kv_heads;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(n * C);
+    cfg.blockDim = dim3(kSelThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = C;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    int slot = trace_begin(st);
+    SPD_CUDA_TRY(cudaLaunchKernelEx(&cfg, evict_select_kernel, p, sq, per));
+    trace_end(slot, st, TR_ROWS, 0.0, 16.0 * rows * n_layers * n_kv_heads);
+    if (most_moves > 0) {
+      const int rows_cta = kMoveWarps * kMoveDepth * (128 / head_dim);
+      const dim3 grid((most_moves + rows_cta - 1) / rows_cta, n);
+      slot = trace_begin(st);
+      SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? evict_move_kernel<128> : evict_move_kernel<64>, grid, dim3(kMoveWarps * 32), 0,
+                              st, kv_cache, p));
+      trace_end(slot, st, TR_ROWS, 0.0, 8.0 * head_dim * moved * n_layers * n_kv_heads);
+    }
+  }
+  return SPD_OK;
+}
+
+extern "C" size_t spd_tree_commit_workspace_size(int n_seqs, int n_path) {
+  if (n_seqs < 1 || n_path < 0) return 0;
+  Carve cv(nullptr, ~size_t(0));
+  cv.take<int32_t>(size_t(n_path) + 3 * size_t(n_seqs) + 1);
+  return cv.used;
+}
+
+extern "C" int spd_tree_commit(uint16_t* kv_cache, int n_layers, int n_seqs, const int32_t* path, const int32_t* path_cu,
+                               const int32_t* ctx_len, int max_len, int n_kv_heads, int head_dim, const int32_t* next_pos,
+                               int32_t* pos, float* acc, void* ws, size_t ws_bytes, void* stream) {
+  if (!kv_cache || !path_cu || !ctx_len || !ws || n_layers < 1 || n_seqs < 1 || max_len < 1 || n_kv_heads < 1)
+    return fail(SPD_EINVAL, "bad commit arguments");
+  if (head_dim != 64 && head_dim != 128) return fail(SPD_EUNSUPPORTED, "head_dim must be 64 or 128");
+  if (pos && !next_pos) return fail(SPD_EINVAL, "positions need next_pos");
+  if (reinterpret_cast<uintptr_t>(kv_cache) & 15) return fail(SPD_EINVAL, "the cache must be 16-byte aligned");
+  if (n_seqs > 65535 || n_layers > 65535) return fail(SPD_EUNSUPPORTED, "more than 65535 sequences or layers");
+  if (path_cu[0] != 0) return fail(SPD_EINVAL, "path_cu must start at 0");
+  for (int b = 0; b < n_seqs; ++b) {
+    if (path_cu[b + 1] < path_cu[b]) return fail(SPD_EINVAL, "path_cu decreases at sequence %d", b);
+    if (ctx_len[b] < 0 || ctx_len[b] > max_len) return fail(SPD_EINVAL, "context of sequence %d outside [0, max_len]", b);
+    for (int i = path_cu[b]; i < path_cu[b + 1]; ++i) {
+      if (!path) return fail(SPD_EINVAL, "null path");
+      if (path[i] < (i > path_cu[b] ? path[i - 1] + 1 : 0) || path[i] >= max_len - ctx_len[b])
+        return fail(SPD_EINVAL, "sequence %d: path nodes must ascend within the cache slot", b);
+    }
+  }
+  const int n_path = path_cu[n_seqs];
+  if (n_path == 0) return SPD_OK;
+  Carve cv(ws, ws_bytes);
+  const size_t ints = size_t(n_path) + 3 * size_t(n_seqs) + 1;
+  int32_t* d = cv.take<int32_t>(ints);
+  if (!cv.fits()) return fail(SPD_ENOSPC, "commit workspace too small (%zu < %zu)", ws_bytes, cv.used);
+  static thread_local std::vector<int32_t> host;
+  host.resize(ints);
+  memcpy(host.data(), path, n_path * 4);
+  memcpy(host.data() + n_path, path_cu, (n_seqs + 1) * 4);
+  memcpy(host.data() + n_path + n_seqs + 1, ctx_len, n_seqs * 4);
+  for (int b = 0; b < n_seqs; ++b) host[n_path + 2 * n_seqs + 1 + b] = next_pos ? next_pos[b] : 0;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  SPD_CUDA_TRY(cudaMemcpyAsync(d, host.data(), ints * 4, cudaMemcpyHostToDevice, st));
+  CommitArgs p{};
+  p.n_seqs = n_seqs;
+  p.max_len = max_len;
+  p.row16 = n_kv_heads * head_dim / 4;
+  p.n_kv_heads = n_kv_heads;
+  p.path = d;
+  p.cu = d + n_path;
+  p.ctx = d + n_path + n_seqs + 1;
+  p.pos0 = d + n_path + 2 * n_seqs + 1;
+  p.pos = pos;
+  p.acc = acc;
+  const int slot = trace_begin(st);
+  SPD_CUDA_TRY(launch_pdl(commit_kernel, dim3((p.row16 + 255) / 256, n_seqs, n_layers), dim3(256), 0, st,
+                          reinterpret_cast<uint4*>(kv_cache), p));
+  trace_end(slot, st, TR_ROWS, 0.0, 32.0 * p.row16 * n_path * n_layers);
+  return SPD_OK;
+}
+
+extern "C" int spd_cache_weights(const uint16_t* q, const float* lse, int n_q, const int32_t* rows, const int32_t* rows_cu,
+                                 const uint16_t* kv_cache, int n_layers, int n_seqs, const int32_t* lens, int max_len,
+                                 int n_heads, int n_kv_heads, int head_dim, float decay, const float* acc_in, float* acc_out,
+                                 void* stream) {
+  if (!q || !lse || !rows_cu || !kv_cache || !lens || !acc_in || !acc_out || n_q < 0 || n_layers < 1 || n_seqs < 1 ||
+      max_len < 1 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads)
+    return fail(SPD_EINVAL, "bad cache weight arguments");
+  if (head_dim != 64 && head_dim != 128) return fail(SPD_EUNSUPPORTED, "head_dim must be 64 or 128");
+  if (rows_cu[0] != 0) return fail(SPD_EINVAL, "rows_cu must start at 0");
+  int longest = 0;
+  for (int b = 0; b < n_seqs; ++b) {
+    if (lens[b] < 0 || lens[b] > max_len) return fail(SPD_EINVAL, "length of sequence %d outside [0, max_len]", b);
+    if (rows_cu[b + 1] < rows_cu[b] || rows_cu[b + 1] - rows_cu[b] > lens[b])
+      return fail(SPD_EINVAL, "sequence %d: rows_cu decreases, or more rows than cached tokens", b);
+    longest = std::max(longest, lens[b]);
+  }
+  if (!rows && rows_cu[n_seqs] > n_q) return fail(SPD_EINVAL, "rows_cu runs past the queries");
+  if (longest == 0) return SPD_OK;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  WeightArgs p{};
+  p.q = reinterpret_cast<const __nv_bfloat16*>(q);
+  p.lse = lse;
+  p.rows = rows;
+  p.kv = reinterpret_cast<const __nv_bfloat16*>(kv_cache);
+  p.n_q = n_q;
+  p.n_seqs = n_seqs;
+  p.max_len = max_len;
+  p.n_heads = n_heads;
+  p.n_kv_heads = n_kv_heads;
+  p.scale = 1.0f / sqrtf(float(head_dim));
+  p.decay = decay;
+  p.acc_in = acc_in;
+  p.acc_out = acc_out;
+  for (int s0 = 0; s0 < n_seqs; s0 += kMaxSeqs) {
+    WeightSeqs sq;
+    const int m = std::min(kMaxSeqs, n_seqs - s0);
+    p.seq0 = s0;
+    double keys = 0.0, pairs = 0.0;
+    for (int b = 0; b < m; ++b) {
+      sq.len[b] = lens[s0 + b];
+      keys += lens[s0 + b];
+      pairs += double(lens[s0 + b]) * (rows_cu[s0 + b + 1] - rows_cu[s0 + b]);
+    }
+    for (int b = 0; b <= m; ++b) sq.cu[b] = rows_cu[s0 + b];
+    const int slot = trace_begin(st);
+    SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? weights_kernel<128> : weights_kernel<64>,
+                            dim3((longest + 7) / 8, m * n_kv_heads, n_layers), dim3(256), 0, st, p, sq));
+    trace_end(slot, st, TR_ATTN, 2.0 * head_dim * n_heads * pairs * n_layers,
+              keys * n_layers * n_kv_heads * (2.0 * head_dim + 8.0));
+  }
+  return SPD_OK;
+}

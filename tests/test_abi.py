@@ -227,3 +227,41 @@ def test_binding_refuses_short_plans_and_residual_buffers(lib):
         N.spd_prefill(M, x, T, [0, 5, T], None, h, _FakeCuda("float32", 10), ws)
     with pytest.raises(ValueError):  # per-token plan shorter than the tokens
         N.spd_prefill_admit(M, x, T, [0, T], np.zeros(T - 1, np.int16), np.ones(T, np.uint8), h, None, ws)
+
+
+def test_tree_masks_hold_the_ancestors(lib):
+    # two sequences: 0 - 1 - 3, 0 - 2, and 4 under the context; a chain of 40 in two words
+    parent = [-1, 0, 0, 1, -1] + list(range(-1, 39))
+    mask, depth = N.spd_tree_mask(parent, [0, 5, 45])
+    assert mask.shape == (45, 2)
+    np.testing.assert_array_equal(mask[:5, 0], [1, 3, 5, 11, 16])
+    np.testing.assert_array_equal(depth[:5], [0, 1, 1, 2, 0])
+    for i in range(40):
+        assert int(mask[5 + i, 0]) | int(mask[5 + i, 1]) << 32 == (1 << (i + 1)) - 1 and depth[5 + i] == i
+
+
+def test_tree_masks_refuse_what_is_no_tree(lib):
+    for parent, cu, words in (([0], [0, 1], 1), ([-1, 2, 0], [0, 3], 1), ([-2], [0, 1], 1),   # not before it
+                              ([-1] * 33, [0, 33], 1)):                                   # more nodes than bits
+        with pytest.raises(N.SpiderError) as e:
+            N.spd_tree_mask(parent, cu, words)
+        assert e.value.code == N.SPD_EINVAL
+    with pytest.raises(ValueError):
+        N.spd_tree_mask([-1, 0], [0, 3])
+
+
+def test_answer_calls_refuse_short_and_mistyped_buffers(lib):
+    ws = _FakeCuda("uint8", 1 << 20)
+    bf, f32, i32 = (lambda n, t=t: _FakeCuda(t, n) for t in ("bfloat16", "float32", "int32"))
+    ok = dict(q=bf(3 * 128), kv=bf(2 * 16 * 256), o=bf(3 * 128), lse=f32(6), ctx=[1, 1])
+    for bad in (dict(q=bf(3 * 128 - 1)), dict(kv=bf(2 * 16 * 256 - 1)), dict(o=f32(3 * 128)), dict(lse=f32(5)), dict(ctx=[1])):
+        a = ok | bad
+        with pytest.raises(ValueError):
+            N.spd_tree_attention(a["q"], [0, 2, 3], a["ctx"], None, a["kv"], 16, 2, 2, 64, a["o"], a["lse"], ws)
+    for path, kv, pos in (([0], bf(2 * 16 * 256), None), ([0, 1], bf(10), None), ([0, 1], bf(2 * 16 * 256), i32(3))):
+        with pytest.raises(ValueError):
+            N.spd_tree_commit(kv, 1, path, [0, 2, 2], [1, 1], 16, 2, 64, ws, next_pos=[1, 1], pos=pos)
+    import torch
+    z = torch.zeros(2, 8)
+    with pytest.raises(TypeError):
+        N.spd_logits_process(z, z)
