@@ -5,6 +5,20 @@
 // committed rows and the drafts j whose bit is set in its mask (its ancestors and itself for a tree):
 //   s_ij = q_i . k_j / sqrt(head_dim),  lse_i = log sum_j e^s_ij,  o_i = sum_j e^(s_ij - lse_i) v_j,
 // o = 0 and lse = -inf for a row that sees nothing. Keys a row does not see contribute nothing, whatever they hold.
+//
+// The K/V stream is what a call cannot do without (4 head_dim bytes a key and K/V head), so every key is read once for
+// all the rows that see it: the up to 128 rows of an MMA tile are the nodes of a sequence times the query heads of a
+// K/V head's group. An item is one such tile over a range of keys; the ranges are cut so that the items fill the GPU
+// (two CTAs an SM) and every item of a batch of different lengths has about the same number of keys. Parts of a row's
+// keys leave (m, l, O) in fp32, merged by tree_merge_kernel in the order of the keys: the same bits in every run.
+//   warp 4     TMA producer: blocks of 64 keys of K and of V into rings
+//   warp 5     MMA issuer: S = Q K^T into TMEM, then O += P V with P read from TMEM, V in place as an MN-major operand
+//   warps 0-3  a thread a row: the block's 64 scores in registers, online softmax in fp32; a weight is held as the sum of two
+//              bf16 terms (16 bits of it, two products: the tensor pipe has the time while K and V stream), the row
+//              sum over the whole weights
+// Only blocks that reach past the committed rows are masked; there the softmax warps also clear the rows of V behind the last
+// draft (recycled memory) and those that are not finite, which a weight of zero would turn into NaN for rows that
+// do not see them; rows that do see one add it at the end.
 #include <cuda_bf16.h>
 #include <math.h>
 #include <stdint.h>
@@ -19,86 +33,489 @@
 namespace spd {
 namespace {
 
-constexpr int kMaxSeqs = 240;  // sequences whose sizes fit in a launch's parameters
-struct TreeSeqs {              // by value in the launch's parameters: no copy, no wait for one
-  int cu[kMaxSeqs + 1];
-  int ctx[kMaxSeqs];
+constexpr int kMaxSeqs = 128;          // sequences whose sizes fit in a launch's parameters (4 KB)
+constexpr int kTK = 64;                // keys a block
+constexpr uint32_t kQBox = 128 * 128;  // 64 columns of the Q tile
+constexpr uint32_t kKBox = kTK * 128;  // 64 columns of a block of K or V
+constexpr int kThreads = 192;
+constexpr uint32_t kTmemCols = 256;    // S: two buffers [0, 64) and [64, 128); O: [128, 128 + HD)
+constexpr int kItems = 304;            // items that fill the GPU: two CTAs on each of 152 SMs
+constexpr int kMinBlocks = 2;          // key blocks an item has at the least where keys are split
+
+// Sequences of a launch, the longest first (by value in the parameters: no copy, no wait for one). Items
+// [item0[e], item0[e + 1]) are sequence e's: (K/V head, part of the keys, tile), the tile fastest, so that the tiles that read
+// the same keys run side by side.
+struct TreeSeqs {
+  int n, item0[kMaxSeqs + 1];
+  int q0[kMaxSeqs], nodes[kMaxSeqs], ctx[kMaxSeqs], seq[kMaxSeqs];
+  int16_t parts[kMaxSeqs];
+  int part0[kMaxSeqs];  // first slot of the sequence's parts in the workspace (parts > 1)
 };
 struct TreeArgs {
   const __nv_bfloat16* q;
   const uint32_t* mask;
   int words;
   const __nv_bfloat16* kv;
-  int seq0, max_len, n_heads, n_kv_heads;
-  float scale;
+  int max_len, n_heads, n_kv_heads;
+  int group, chunk, chunks, nodes_tile;  // heads a group; of them in a tile; tiles across; nodes a tile
+  float scale_log2;
   __nv_bfloat16* o;
   float* lse;
+  float* part_o;   // [part][rows_part][HD]
+  float2* part_ml; // [part][rows_part]: maximum (log2 units), sum
+  int rows_part;
+  int* status;
+  long long budget;
+  unsigned long long* stamp;
 };
 
-// One CTA a node and head: every warp takes every eighth key, a key's dot product runs over the lanes.
 template <int HD>
-__global__ void __launch_bounds__(256) tree_kernel(const __grid_constant__ TreeArgs p, const __grid_constant__ TreeSeqs sq) {
-  constexpr int D = HD / 32;
-  __shared__ float wm[8], wl[8], wo[8][HD];
+struct TreeSmem {
+  static constexpr int kChunks = HD / 64;
+  static constexpr int kStages = 256 / HD;  // 64 KB of K and V in flight a CTA
+  static constexpr uint32_t q = 0;
+  static constexpr uint32_t k = q + kChunks * kQBox;
+  static constexpr uint32_t v = k + kStages * kChunks * kKBox;
+  static constexpr uint32_t bars = v + kStages * kChunks * kKBox;
+  static constexpr uint32_t bytes = bars + 256 + 1024;  // + alignment slack
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<uint32_t*>(&v);
+}
+__device__ __forceinline__ bool not_finite(uint32_t two) {  // either of two bf16
+  return (two & 0x7f80u) == 0x7f80u || (two & 0x7f800000u) == 0x7f800000u;
+}
+
+// Bits d0 .. d0 + 63 of what node i (mask row `row`) of n sees; d < 0: a committed row, which every node sees.
+__device__ __forceinline__ uint64_t seen64(const TreeArgs& p, size_t row, int i, int n, int d0) {
+  const int at = max(d0, 0);
+  uint64_t bits;
+  if (!p.mask) {
+    bits = i >= at ? (i - at >= 63 ? ~0ull : (2ull << (i - at)) - 1) : 0ull;
+  } else {
+    const uint32_t* m = p.mask + row * p.words;
+    const int w = at >> 5;
+    const uint32_t a = w < p.words ? m[w] : 0u, b = w + 1 < p.words ? m[w + 1] : 0u, c = w + 2 < p.words ? m[w + 2] : 0u;
+    bits = (uint64_t(__funnelshift_r(b, c, at & 31)) << 32) | __funnelshift_r(a, b, at & 31);
+  }
+  const int left = n - at;  // drafts there are
+  if (left < 64) bits &= left > 0 ? (1ull << left) - 1 : 0ull;
+  if (d0 <= -64) return ~0ull;
+  return d0 < 0 ? (bits << -d0) | ((1ull << -d0) - 1) : bits;
+}
+
+template <int HD>
+__global__ void __launch_bounds__(kThreads, 2)
+    tree_attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ TreeArgs p,
+                     const __grid_constant__ TreeSeqs sq) {
+  using L = TreeSmem<HD>;
+  constexpr int NS = L::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + L::bars);  // [NS] K block landed
+  uint64_t* k_empty = k_full + NS;                                 // [NS] its S product has completed
+  uint64_t* v_full = k_empty + NS;                                 // [NS] V block landed
+  uint64_t* v_empty = v_full + NS;                                 // [NS] its PV products have completed
+  uint64_t* q_full = v_empty + NS;   // the Q tile is in shared memory
+  uint64_t* s_full = q_full + 1;     // [2] S of block j is in TMEM buffer j % 2
+  uint64_t* p_full = s_full + 2;     // [2] P of block j written and O rescaled
+  uint64_t* o_done = p_full + 2;     // PV products of the current block completed
+  uint64_t* drain = o_done + 1;      // every MMA completed: O is final
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int* odd_v = reinterpret_cast<int*>(tmem_slot + 2);  // some visible V is not finite
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // the item's sequence: the last entry that starts at or before it
+  int e = 0;
+  for (int hi = sq.n; hi - e > 1;) {
+    const int mid = (e + hi) >> 1;
+    if (sq.item0[mid] <= int(blockIdx.x)) e = mid;
+    else hi = mid;
+  }
+  const int n = sq.nodes[e], ctx = sq.ctx[e], parts = sq.parts[e];
+  const int tiles = (n + p.nodes_tile - 1) / p.nodes_tile * p.chunks;
+  int u = int(blockIdx.x) - sq.item0[e];
+  const int slot = sq.part0[e] + u;
+  const int tile = u % tiles;
+  u /= tiles;
+  const int part = u % parts, hk = u / parts;
+  const int n0 = tile / p.chunks * p.nodes_tile, h0 = tile % p.chunks * p.chunk;  // first node, first head of the group
+  const int nodes = min(p.nodes_tile, n - n0), rows = nodes * p.chunk;
+  const int heads = min(p.chunk, p.group - h0);  // of the chunk's heads, those there are
+  const int total = ctx + n, blocks = (total + kTK - 1) / kTK;
+  const int b0 = int((long long)part * blocks / parts), nkb = int((long long)(part + 1) * blocks / parts) - b0;
+  const int row0 = sq.seq[e] * p.max_len;  // the cache slot's first row
+  const int nw = (rows + 31) / 32;         // softmax warps with rows
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < NS; ++s) {
+      mbar_init(&k_full[s], 1);
+      mbar_init(&k_empty[s], 1);
+      mbar_init(&v_full[s], 1);
+      mbar_init(&v_empty[s], 1);
+    }
+    mbar_init(q_full, nw);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&s_full[s], 1);
+      mbar_init(&p_full[s], nw);  // one arrival per softmax warp
+    }
+    mbar_init(o_done, 1);
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    *odd_v = 0;
+    fence_mbar_init();
+    prefetch_tmap(&map_kv);
+  }
+  if (warp == 4) {
+    tmem_alloc(tmem_slot, kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const uint32_t t_o = tmem + 2 * kTK;
+
   pdl_launch_dependents();
   pdl_wait();
-  const int h = blockIdx.x, g = h / (p.n_heads / p.n_kv_heads), ls = blockIdx.z;
-  const int i = blockIdx.y, n = sq.cu[ls + 1] - sq.cu[ls], ctx = sq.ctx[ls];
-  if (i >= n) return;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const size_t row = sq.cu[ls] + i;
-  float qf[D], o[D];
+  if (threadIdx.x == 0) stamp_start(p.stamp);
+
+  int issued_k = 0, issued_v = 0;
+  if (warp == 4) {
+    if (lane == 0) {
+      // ---- TMA producer ----
+      const uint64_t pol = tiles > 1 ? policy_evict_last() : policy_evict_first();
+      auto load = [&](int j, uint64_t* full, uint64_t* empty, uint32_t at, int x0) -> bool {
+        const int s = j % NS;
+        if (j >= NS && !mbar_wait(&empty[s], (j / NS - 1) & 1, abort_flag, p.budget)) {
+          *abort_flag = 1;
+          set_status(p.status, SPD_ETIMEOUT);
+          return false;
+        }
+        mbar_arrive_expect_tx(&full[s], L::kChunks * kKBox);
+        for (int c = 0; c < L::kChunks; ++c)
+          tma_load_2d(smem + at + (s * L::kChunks + c) * kKBox, &map_kv, &full[s], x0 + hk * HD + c * 64,
+                      row0 + (b0 + j) * kTK, pol);
+        return true;
+      };
+      for (int j = 0; j < nkb; ++j) {
+        if (!load(j, k_full, k_empty, L::k, 0)) break;
+        issued_k = j + 1;
+        if (!load(j, v_full, v_empty, L::v, p.n_kv_heads * HD)) break;
+        issued_v = j + 1;
+      }
+    }
+  } else if (warp == 5) {
+    if (lane == 0) {
+      // ---- MMA issuer ----
+      const uint32_t id_s = idesc_bf16_f32(128, kTK);
+      const uint32_t id_o = idesc_bf16_f32(128, HD) | (1u << 16);  // V is MN-major
+      const uint32_t sa = smem_u32(smem + L::q);
+      bool ok = mbar_wait(q_full, 0, abort_flag, p.budget);
+      auto issue_s = [&](int j) -> bool {
+        const int s = j % NS;
+        if (!mbar_wait(&k_full[s], (j / NS) & 1, abort_flag, p.budget)) return false;
+        // S buffer j % 2 holds P of block j - 2 until its PV products have completed
+        if (j > 1 && !mbar_wait(o_done, j & 1, abort_flag, p.budget)) return false;
+        tc_fence_after();
+        const uint32_t sk = smem_u32(smem + L::k + s * L::kChunks * kKBox);
 #pragma unroll
-  for (int e = 0; e < D; ++e) {
-    qf[e] = __bfloat162float(p.q[(row * p.n_heads + h) * HD + D * lane + e]);
-    o[e] = 0.0f;
+        for (int kk = 0; kk < HD / 16; ++kk)
+          mma_bf16(tmem + kTK * (j & 1), sdesc_k128(sa + (kk >> 2) * kQBox + (kk & 3) * 32),
+                   sdesc_k128(sk + (kk >> 2) * kKBox + (kk & 3) * 32), id_s, kk > 0 ? 1u : 0u);
+        mma_commit(&s_full[j & 1]);
+        mma_commit(&k_empty[s]);
+        return true;
+      };
+      if (ok) ok = issue_s(0);
+      for (int j = 0; j < nkb && ok; ++j) {
+        const int s = j % NS;
+        if (j + 1 < nkb && !(ok = issue_s(j + 1))) break;
+        if (!(ok = mbar_wait(&v_full[s], (j / NS) & 1, abort_flag, p.budget))) break;
+        if (!(ok = mbar_wait(&p_full[j & 1], (j >> 1) & 1, abort_flag, p.budget))) break;
+        tc_fence_after();
+        const uint32_t sv = smem_u32(smem + L::v + s * L::kChunks * kKBox);
+#pragma unroll
+        for (int kk = 0; kk < 2 * (kTK / 16); ++kk)  // the weights' first terms, then their second
+          mma_bf16_ts(t_o, tmem + kTK * (j & 1) + 8 * kk, sdesc_mn128(sv + (kk % (kTK / 16)) * 2048, kKBox), id_o,
+                      (j > 0 || kk > 0) ? 1u : 0u);
+        mma_commit(o_done);
+        mma_commit(&v_empty[s]);
+      }
+      if (!ok) {
+        *abort_flag = 1;
+        set_status(p.status, SPD_ETIMEOUT);
+      }
+      mma_commit(drain);  // arrives once every MMA issued above has completed
+      volatile int no_abort = 0;
+      if (!mbar_wait(drain, 0, &no_abort, p.budget)) set_status(p.status, SPD_ETIMEOUT);
+    }
+  } else if (warp < nw) {
+    // ---- softmax: warp w reads TMEM lanes [32 w, 32 w + 32) ----
+    const int r = warp * 32 + lane, T = nw * 32;
+    const int node = n0 + min(r / p.chunk, nodes - 1), hc = r % p.chunk;
+    const bool valid = r < rows && hc < heads;
+    const int head = hk * p.group + h0 + min(hc, heads - 1);
+    const size_t qrow = sq.q0[e] + node;  // rows without a node repeat the last one's, and are not stored
+    const __nv_bfloat16* qsrc = p.q + (qrow * p.n_heads + head) * HD;
+    const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
+    {  // the Q tile in the 128-byte swizzle: 16-byte piece j of row r at j ^ (r % 8)
+      uint4 v[HD / 8];
+#pragma unroll
+      for (int j = 0; j < HD / 8; ++j) v[j] = reinterpret_cast<const uint4*>(qsrc)[j];
+#pragma unroll
+      for (int j = 0; j < HD / 8; ++j)
+        *reinterpret_cast<uint4*>(smem + L::q + (j >> 3) * kQBox + r * 128 + (((j & 7) ^ (r & 7)) << 4)) = v[j];
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_full);
+    }
+    float m_run = -INFINITY, l_run = 0.0f;  // the row's maximum so far (raw scores) and sum of weights
+    bool ok = true;
+    for (int j = 0; j < nkb; ++j) {
+      const uint32_t t_s = tmem + kTK * (j & 1) + lanes;
+      const int kb = (b0 + j) * kTK;
+      const bool drafts = kb + kTK > ctx;  // the block holds keys that not every row sees, or none at all
+      if (drafts) {
+        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&v_full[j % NS], (j / NS) & 1, abort_flag, p.budget)))) break;
+        bool odd = false;
+        for (int x = threadIdx.x; x < kTK * L::kChunks; x += T) {
+          uint4* vr = reinterpret_cast<uint4*>(smem + L::v + (j % NS) * L::kChunks * kKBox + x * 128);
+          bool clear = kb + x % kTK >= total;
+          if (!clear && kb + x % kTK >= ctx) {
+#pragma unroll
+            for (int y = 0; y < 8; ++y) {
+              const uint4 w = vr[y];
+              clear |= not_finite(w.x) || not_finite(w.y) || not_finite(w.z) || not_finite(w.w);
+            }
+            odd |= clear;
+          }
+          if (clear) {
+#pragma unroll
+            for (int y = 0; y < 8; ++y) vr[y] = make_uint4(0u, 0u, 0u, 0u);
+          }
+        }
+        if (odd) atomicOr(odd_v, 1);
+        fence_proxy_async_smem();
+        // (every softmax warp arrives on p_full after its share, so the products see all of them)
+      }
+      if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s_full[j & 1], (j >> 1) & 1, abort_flag, p.budget)))) break;
+      tc_fence_after();
+      float v[kTK];
+      tmem_ld64(t_s, v);
+      if (drafts) {
+        const uint64_t see = seen64(p, qrow, node, n, kb - ctx);
+        const uint32_t lo = uint32_t(see), hi = uint32_t(see >> 32);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          if (!((lo >> i) & 1u)) v[i] = -INFINITY;
+          if (!((hi >> i) & 1u)) v[32 + i] = -INFINITY;
+        }
+      }
+      float m4[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+      for (int i = 4; i < kTK; ++i) m4[i & 3] = fmaxf(m4[i & 3], v[i]);
+      const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+      if (j == 0) {
+        m_run = mx;
+      } else if (__any_sync(0xffffffffu, mx > m_run)) {
+        // the previous products have completed (those before had when these scores came): O can be rescaled
+        if (!(ok = __all_sync(0xffffffffu, mbar_wait(o_done, (j - 1) & 1, abort_flag, p.budget)))) break;
+        tc_fence_after();
+        const float m_new = fmaxf(m_run, mx);
+        const float corr = m_new == m_run ? 1.0f : ex2((m_run - m_new) * p.scale_log2);
+        m_run = m_new;
+        l_run *= corr;
+#pragma unroll 1
+        for (int c = 0; c < HD / 32; ++c) {
+          float ov[32];
+          tmem_ld32(t_o + lanes + c * 32, ov);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) ov[i] *= corr;
+          tmem_st32(t_o + lanes + c * 32, ov);
+        }
+      }
+      const float off = m_run == -INFINITY ? 0.0f : m_run * p.scale_log2;  // nothing seen yet: all weights are 0
+      float r4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      float first[32], second[32];  // the two terms of keys 2 i and 2 i + 1 in word i
+#pragma unroll
+      for (int i = 0; i < kTK; i += 2) {
+        const float p0 = ex2(fmaf(v[i], p.scale_log2, -off)), p1 = ex2(fmaf(v[i + 1], p.scale_log2, -off));
+        r4[i & 2] += p0;
+        r4[(i & 2) + 1] += p1;
+        const uint32_t hi = pack_bf16(p0, p1);
+        first[i >> 1] = __uint_as_float(hi);
+        second[i >> 1] =
+            __uint_as_float(pack_bf16(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u)));
+      }
+      l_run += (r4[0] + r4[1]) + (r4[2] + r4[3]);
+      tmem_st32(t_s, first);  // over the scores
+      tmem_st32(t_s + 32, second);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&p_full[j & 1]);
+    }
+    if (ok) ok = __all_sync(0xffffffffu, mbar_wait(drain, 0, abort_flag, p.budget));
+    if (!ok) {
+      *abort_flag = 1;
+      set_status(p.status, SPD_ETIMEOUT);
+    } else {
+      tc_fence_after();
+      if (*reinterpret_cast<volatile int*>(odd_v)) {
+        // drafts whose V was cleared: rows that see one add p v in fp32 (the score again from q and k)
+        const float off = m_run == -INFINITY ? 0.0f : m_run * p.scale_log2;
+        for (int d = max(0, b0 * kTK - ctx); d < min(n, (b0 + nkb) * kTK - ctx); ++d) {
+          const bool sees = valid && (seen64(p, qrow, node, n, d) & 1ull);
+          const __nv_bfloat16* kr = p.kv + size_t(row0 + ctx + d) * (2 * size_t(p.n_kv_heads) * HD) + hk * HD;
+          const __nv_bfloat16* vr = kr + size_t(p.n_kv_heads) * HD;
+          for (int c = 0; c < L::kChunks; ++c) {
+            const uint32_t two = *reinterpret_cast<const uint32_t*>(vr + c * 64 + 2 * lane);
+            if (!__any_sync(0xffffffffu, not_finite(two))) continue;
+            float s = 0.0f;
+            if (sees)
+              for (int x = 0; x < HD; ++x) s = fmaf(__bfloat162float(qsrc[x]), __bfloat162float(kr[x]), s);
+            const float w = ex2(fmaf(s, p.scale_log2, -off));
+#pragma unroll 1
+            for (int b = 0; b < 2; ++b) {
+              float ov[32];
+              tmem_ld32(t_o + lanes + c * 64 + b * 32, ov);
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (sees) ov[i] = fmaf(w, __bfloat162float(vr[c * 64 + b * 32 + i]), ov[i]);
+              tmem_st32(t_o + lanes + c * 64 + b * 32, ov);
+            }
+          }
+        }
+      }
+      const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
+      const float m2 = m_run * p.scale_log2;
+      if (parts > 1) {
+        float* po = p.part_o + (size_t(slot) * p.rows_part + r) * HD;
+        if (valid) p.part_ml[size_t(slot) * p.rows_part + r] = make_float2(m2, l_run);
+#pragma unroll 1
+        for (int c = 0; c < HD / 32; ++c) {
+          float v[32];
+          tmem_ld32(t_o + lanes + c * 32, v);
+          if (valid) {
+#pragma unroll
+            for (int y = 0; y < 8; ++y)
+              reinterpret_cast<float4*>(po + c * 32)[y] = make_float4(v[4 * y], v[4 * y + 1], v[4 * y + 2], v[4 * y + 3]);
+          }
+        }
+      } else {
+        __nv_bfloat16* orow = p.o + (qrow * p.n_heads + head) * HD;
+        if (valid && p.lse) p.lse[qrow * p.n_heads + head] = fmaf(m2, 0.6931471805599453f, logf(l_run));
+#pragma unroll 1
+        for (int c = 0; c < HD / 32; ++c) {
+          float v[32];
+          tmem_ld32(t_o + lanes + c * 32, v);
+          if (valid) {
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+              reinterpret_cast<uint4*>(orow + c * 32)[y] =
+                  make_uint4(pack_bf16(v[8 * y] * inv, v[8 * y + 1] * inv), pack_bf16(v[8 * y + 2] * inv, v[8 * y + 3] * inv),
+                             pack_bf16(v[8 * y + 4] * inv, v[8 * y + 5] * inv), pack_bf16(v[8 * y + 6] * inv, v[8 * y + 7] * inv));
+          }
+        }
+      }
+    }
   }
-  const int kvd = p.n_kv_heads * HD;
-  const __nv_bfloat16* base = p.kv + size_t(p.seq0 + ls) * p.max_len * (2 * kvd) + g * HD + D * lane;
-  float m = -INFINITY, l = 0.0f;
-  for (int k = warp; k < ctx + n; k += 8) {
-    const int d = k - ctx;
-    if (d >= 0 && (p.mask ? !((p.mask[row * p.words + d / 32] >> (d % 32)) & 1u) : d > i)) continue;
-    const __nv_bfloat16* kr = base + size_t(k) * (2 * kvd);
-    float s = 0.0f;
-#pragma unroll
-    for (int e = 0; e < D; ++e) s = fmaf(qf[e], __bfloat162float(kr[e]), s);
-#pragma unroll
-    for (int off = 16; off; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-    s *= p.scale;
-    const float mn = fmaxf(m, s), c = m == -INFINITY ? 0.0f : expf(m - mn), w = expf(s - mn);
-    l = l * c + w;
-#pragma unroll
-    for (int e = 0; e < D; ++e) o[e] = o[e] * c + w * __bfloat162float(kr[kvd + e]);
-    m = mn;
-  }
-  if (lane == 0) {
-    wm[warp] = m;
-    wl[warp] = l;
-  }
-#pragma unroll
-  for (int e = 0; e < D; ++e) wo[warp][D * lane + e] = o[e];
+  tc_fence_before();
   __syncthreads();
-  float mt = -INFINITY, lt = 0.0f;
-  for (int w = 0; w < 8; ++w) mt = fmaxf(mt, wm[w]);
-  for (int w = 0; w < 8; ++w) lt += wm[w] == -INFINITY ? 0.0f : wl[w] * expf(wm[w] - mt);
-  for (int d = threadIdx.x; d < HD; d += 256) {
-    float s = 0.0f;
-    for (int w = 0; w < 8; ++w)
-      if (wm[w] != -INFINITY) s += wo[w][d] * expf(wm[w] - mt);
-    p.o[(row * p.n_heads + h) * HD + d] = __float2bfloat16_rn(mt == -INFINITY ? 0.0f : s / lt);
+  if (threadIdx.x == 128 && *abort_flag) {
+    // loads issued but never consumed land before the CTA exits
+    volatile int no_abort = 0;
+    for (int j = max(0, issued_k - NS); j < issued_k; ++j) mbar_wait(&k_full[j % NS], (j / NS) & 1, &no_abort, p.budget);
+    for (int j = max(0, issued_v - NS); j < issued_v; ++j) mbar_wait(&v_full[j % NS], (j / NS) & 1, &no_abort, p.budget);
   }
-  if (p.lse && threadIdx.x == 0) p.lse[row * p.n_heads + h] = mt == -INFINITY ? -INFINITY : mt + logf(lt);
+  __syncwarp();
+  tc_fence_after();
+  if (warp == 4) tmem_dealloc(tmem, kTmemCols);
+  if (threadIdx.x == 0) stamp_end(p.stamp);
 }
+
+// Rows whose keys were split: states (m_i, l_i, O_i) merged in key order, m = max m_i, l = sum l_i 2^(m_i - m),
+// O = sum O_i 2^(m_i - m). A warp a row (node and head).
+constexpr int kMergeWarps = 4;
+template <int HD>
+__global__ void __launch_bounds__(kMergeWarps * 32)
+    tree_merge_kernel(const __grid_constant__ TreeArgs p, const __grid_constant__ TreeSeqs sq) {
+  constexpr int D = HD / 32;
+  pdl_launch_dependents();
+  pdl_wait();
+  const int e = blockIdx.y, n = sq.nodes[e], parts = sq.parts[e];
+  const int row = blockIdx.x * kMergeWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (parts < 2 || row >= n * p.n_heads) return;
+  const int node = row / p.n_heads, head = row % p.n_heads, hk = head / p.group, hg = head % p.group;
+  const int tiles = (n + p.nodes_tile - 1) / p.nodes_tile * p.chunks;
+  const int tile = node / p.nodes_tile * p.chunks + hg / p.chunk;
+  const int r = node % p.nodes_tile * p.chunk + hg % p.chunk;
+  const size_t first = (size_t(sq.part0[e]) + size_t(hk) * parts * tiles + tile) * p.rows_part + r;
+  const size_t step = size_t(tiles) * p.rows_part;
+  float m = -INFINITY;
+  for (int s = lane; s < parts; s += 32) m = fmaxf(m, p.part_ml[first + s * step].x);
+#pragma unroll
+  for (int off = 16; off; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+  float l = 0.0f, o[D];
+#pragma unroll
+  for (int x = 0; x < D; ++x) o[x] = 0.0f;
+#pragma unroll 4
+  for (int s = 0; s < parts; ++s) {
+    const float2 ml = p.part_ml[first + s * step];
+    const float f = ml.x == -INFINITY ? 0.0f : exp2f(ml.x - m);
+    const float* po = p.part_o + (first + s * step) * HD + D * lane;
+    l = fmaf(ml.y, f, l);
+#pragma unroll
+    for (int x = 0; x < D; ++x) o[x] = fmaf(po[x], f, o[x]);
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const size_t at = size_t(sq.q0[e] + node) * p.n_heads + head;
+  uint32_t* to = reinterpret_cast<uint32_t*>(p.o + at * HD + D * lane);
+#pragma unroll
+  for (int x = 0; x < D / 2; ++x) to[x] = pack_bf16(o[2 * x] * inv, o[2 * x + 1] * inv);
+  if (p.lse && lane == 0) p.lse[at] = fmaf(m, 0.6931471805599453f, logf(l));
+}
+
+struct TreeTile {
+  int group, chunk, chunks, nodes;
+};
+TreeTile tree_tile(int n_heads, int n_kv_heads) {
+  TreeTile t;
+  t.group = n_heads / n_kv_heads;
+  t.chunk = std::min(t.group, 128);
+  t.chunks = (t.group + 127) / 128;
+  t.nodes = 128 / t.chunk;
+  return t;
+}
+// Rows kept of a part, and parts there can be at once: keys are split only where a sequence has more blocks than an even
+// share of kItems items, which gives at most 2 kItems of them.
+int rows_of_part(const TreeTile& t, int n_q) { return std::min(t.nodes, n_q) * t.chunk; }
+constexpr int kMaxParts = 2 * kItems;
 
 }  // namespace
 
-size_t tree_attention_bytes(int, int, int, int, int) { return 256; }
+size_t tree_attention_bytes(int n_q, int, int n_heads, int n_kv_heads, int head_dim) {
+  const size_t rows = size_t(kMaxParts) * rows_of_part(tree_tile(n_heads, n_kv_heads), n_q);
+  Carve cv(nullptr, ~size_t(0));
+  cv.take<float>(rows * head_dim);
+  cv.take<float2>(rows);
+  return cv.used;
+}
 
 int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, int n_seqs, const uint32_t* mask, int words,
                        const void* kv, int max_len, int n_heads, int n_kv_heads, int head_dim, void* o, float* lse, void* ws,
-                       size_t, cudaStream_t st) {
-  (void)ws;
+                       size_t ws_bytes, cudaStream_t st) {
+  const TreeTile t = tree_tile(n_heads, n_kv_heads);
+  const int kvd = n_kv_heads * head_dim;
+  CUtensorMap map;
+  if (int rc = make_operand_map(&map, kv, 2 * kvd, n_seqs * max_len, kTK)) return rc;
   TreeArgs p{};
   p.q = static_cast<const __nv_bfloat16*>(q);
   p.mask = mask;
@@ -107,29 +524,79 @@ int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, i
   p.max_len = max_len;
   p.n_heads = n_heads;
   p.n_kv_heads = n_kv_heads;
-  p.scale = 1.0f / sqrtf(float(head_dim));
+  p.group = t.group;
+  p.chunk = t.chunk;
+  p.chunks = t.chunks;
+  p.nodes_tile = t.nodes;
+  p.scale_log2 = float(1.4426950408889634 / sqrt(double(head_dim)));
   p.o = static_cast<__nv_bfloat16*>(o);
   p.lse = lse;
+  Carve cv(ws, ws_bytes);
+  p.rows_part = rows_of_part(t, q_cu[n_seqs]);
+  const size_t rows = size_t(kMaxParts) * p.rows_part;
+  p.part_o = cv.take<float>(rows * head_dim);
+  p.part_ml = cv.take<float2>(rows);
+  p.status = cv.status();
+  p.budget = kWaitBudget;
+  static bool attr = false;
+  if (!attr) {
+    SPD_CUDA_TRY(cudaFuncSetAttribute(tree_attn_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                      int(TreeSmem<128>::bytes)));
+    SPD_CUDA_TRY(cudaFuncSetAttribute(tree_attn_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                      int(TreeSmem<64>::bytes)));
+    attr = true;
+  }
+  std::vector<int> order;
   for (int s0 = 0; s0 < n_seqs; s0 += kMaxSeqs) {
-    TreeSeqs sq;
     const int m = std::min(kMaxSeqs, n_seqs - s0);
-    p.seq0 = s0;
-    int most = 0;
+    order.clear();
+    long long work = 0;  // key blocks of all items
     double pairs = 0.0, keys = 0.0;
-    for (int b = 0; b < m; ++b) {
-      const int n = q_cu[s0 + b + 1] - q_cu[s0 + b];
-      sq.ctx[b] = ctx[s0 + b];
-      most = std::max(most, n);
-      keys += ctx[s0 + b] + n;
-      pairs += double(n) * (ctx[s0 + b] + n);
+    auto count = [&](int b) { return q_cu[b + 1] - q_cu[b]; };
+    auto blocks = [&](int b) { return (ctx[b] + count(b) + kTK - 1) / kTK; };
+    auto units = [&](int b) { return (long long)((count(b) + t.nodes - 1) / t.nodes) * t.chunks * n_kv_heads; };
+    for (int b = s0; b < s0 + m; ++b) {
+      if (count(b) == 0) continue;
+      order.push_back(b);
+      work += units(b) * blocks(b);
+      keys += ctx[b] + count(b);
+      pairs += double(count(b)) * (ctx[b] + count(b));
     }
-    for (int b = 0; b <= m; ++b) sq.cu[b] = q_cu[s0 + b];
-    if (most == 0) continue;
+    if (order.empty()) continue;
+    std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return blocks(x) > blocks(y); });
+    // blocks an item: an even share of the GPU's places, and no less than kMinBlocks
+    const long long share = std::max<long long>(kMinBlocks, (work + kItems - 1) / kItems);
+    TreeSeqs sq{};
+    long long items = 0;
+    int parts = 0, most = 0;
+    for (int b : order) {
+      const int e = sq.n++;
+      const int k = int((blocks(b) + share - 1) / share);
+      sq.item0[e] = int(items);
+      sq.q0[e] = q_cu[b];
+      sq.nodes[e] = count(b);
+      sq.ctx[e] = ctx[b];
+      sq.seq[e] = b;
+      sq.parts[e] = int16_t(k);
+      sq.part0[e] = parts;
+      if (k > 1) {
+        parts += int(units(b)) * k;
+        most = std::max(most, count(b));
+      }
+      items += units(b) * k;
+    }
+    if (items > 0x7fffffff) return fail(SPD_EUNSUPPORTED, "tree attention of more than 2^31 tiles");
+    sq.item0[sq.n] = int(items);
+    const double fl = 4.0 * head_dim * n_heads * pairs;
+    const double by = 4.0 * kvd * keys + 4.0 * n_heads * head_dim * (q_cu[s0 + m] - q_cu[s0]);
+    p.stamp = stamp_slot(TR_ATTN, fl, by);
     const int slot = trace_begin(st);
-    SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? tree_kernel<128> : tree_kernel<64>, dim3(n_heads, most, m), dim3(256), 0, st, p,
-                            sq));
-    trace_end(slot, st, TR_ATTN, 4.0 * head_dim * n_heads * pairs,
-              4.0 * n_kv_heads * head_dim * keys + 4.0 * n_heads * head_dim * (sq.cu[m] - sq.cu[0]));
+    SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? tree_attn_kernel<128> : tree_attn_kernel<64>, dim3(unsigned(items)), dim3(kThreads),
+                            head_dim == 128 ? TreeSmem<128>::bytes : TreeSmem<64>::bytes, st, map, p, sq));
+    if (most > 0)
+      SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? tree_merge_kernel<128> : tree_merge_kernel<64>,
+                              dim3((most * n_heads + kMergeWarps - 1) / kMergeWarps, sq.n), dim3(kMergeWarps * 32), 0, st, p, sq));
+    trace_end(slot, st, TR_ATTN, fl, by);
   }
   return SPD_OK;
 }
@@ -186,6 +653,7 @@ extern "C" int spd_tree_attention(const uint16_t* q, int n_q, const int32_t* q_c
       return fail(SPD_EINVAL, "sequence %d: context and drafts exceed max_len", b);
     if (tree_mask && n > 32 * mask_words) return fail(SPD_EINVAL, "sequence %d: %d nodes, %d mask words", b, n, mask_words);
   }
+  if ((long long)n_seqs * max_len > 0x7fffffffLL) return fail(SPD_EUNSUPPORTED, "more than 2^31 - 1 cache rows in a layer");
   const size_t need = tree_attention_bytes(n_q, n_seqs, n_heads, n_kv_heads, head_dim);
   if (ws_bytes < need) return fail(SPD_ENOSPC, "tree attention workspace too small (%zu < %zu)", ws_bytes, need);
   return tree_attention_run(q, q_cu, ctx_len, n_seqs, tree_mask, mask_words, kv, max_len, n_heads, n_kv_heads, head_dim, o, lse,
