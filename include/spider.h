@@ -438,12 +438,13 @@ int spd_tree_commit(uint16_t* kv_cache, int n_layers, int n_seqs, const int32_t*
  * or spd_decode_tree; rows (dev) int32: the query row of every row, sequence b's at [rows_cu[b], rows_cu[b + 1]) (HOST
  * int32 [n_seqs + 1] from 0), NULL = row i is query row i; indices outside [0, n_q) add nothing. lens (HOST) int32 [n_seqs]; kv_cache as
  * spd_tree_commit; acc_in, acc_out (dev) fp32 [n_layers][n_seqs][n_kv_heads][max_len], the same buffer or apart; slots
- * from lens[b] on are not written. head_dim 64 or 128; q and kv_cache 16-byte aligned.
- * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ECUDA. */
+ * from lens[b] on are not written. head_dim 64 or 128; q and kv_cache 16-byte aligned. ws (dev, at least 4 bytes, may be
+ * NULL): only its status word is used, for device timeouts (NULL: not reported).
+ * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ENOSPC, SPD_ECUDA. */
 int spd_cache_weights(const uint16_t* q, const float* lse, int n_q, const int32_t* rows, const int32_t* rows_cu,
                       const uint16_t* kv_cache, int n_layers, int n_seqs, const int32_t* lens, int max_len,
                       int n_heads, int n_kv_heads, int head_dim, float decay, const float* acc_in,
-                      float* acc_out, void* stream);
+                      float* acc_out, void* ws, size_t ws_bytes, void* stream);
 
 /* Workspace bytes of spd_cache_evict (0 on invalid arguments). */
 size_t spd_cache_evict_workspace_size(int n_layers, int n_seqs, int n_kv_heads, int budget);

@@ -162,7 +162,7 @@ def lib():
             "spd_tree_attention": (i, [vp, i, vp, vp, i, vp, i, vp, i, i, i, i, vp, vp, vp, sz, vp]),
             "spd_tree_commit_workspace_size": (sz, [i, i]),
             "spd_tree_commit": (i, [vp, i, i, vp, vp, vp, i, i, i, vp, vp, vp, vp, sz, vp]),
-            "spd_cache_weights": (i, [vp, vp, i, vp, vp, vp, i, i, vp, i, i, i, i, C.c_float, vp, vp, vp]),
+            "spd_cache_weights": (i, [vp, vp, i, vp, vp, vp, i, i, vp, i, i, i, i, C.c_float, vp, vp, vp, sz, vp]),
             "spd_cache_evict_workspace_size": (sz, [i, i, i, i]),
             "spd_cache_evict": (i, [vp, i, i, vp, i, i, i, i, i, i, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
             "spd_logits_process": (i, [vp, i, i, i, C.POINTER(LogitsRules), vp, i, vp, vp]),
@@ -572,9 +572,10 @@ def spd_tree_commit(kv_cache, n_layers, path, path_cu, ctx_len, max_len, n_kv_he
 
 
 def spd_cache_weights(q, lse, rows, rows_cu, kv_cache, lens, max_len, n_heads, n_kv_heads, head_dim, decay, acc_in,
-                      acc_out, stream=None):
+                      acc_out, ws=None, stream=None):
     """acc_out = decay * acc_in + the attention weight that every cached row receives from the sequences' last rows; q
-    [n_layers][n_q][n_heads * head_dim], rows: query row of every row (device int32) or None."""
+    [n_layers][n_q][n_heads * head_dim], rows: query row of every row (device int32) or None; ws: a device buffer whose
+    first word receives a device-side failure, or None."""
     cu = np.ascontiguousarray(rows_cu, dtype=np.int32)
     L, n_q, B = q.shape[0], q.shape[1], len(cu) - 1
     ln = _host(lens, np.int32, B, "lens")
@@ -583,7 +584,8 @@ def spd_cache_weights(q, lse, rows, rows_cu, kv_cache, lens, max_len, n_heads, n
                                    n_q, _dev(rows, "i32", int(cu[-1]), "rows", True), _p(cu),
                                    _dev(kv_cache, "bf16", units * 2 * head_dim, "kv_cache"), L, B, _p(ln), max_len, n_heads,
                                    n_kv_heads, head_dim, float(decay), _dev(acc_in, "f32", units, "acc_in"),
-                                   _dev(acc_out, "f32", units, "acc_out"), _stream(stream)))
+                                   _dev(acc_out, "f32", units, "acc_out"), *((None, 0) if ws is None else _ws(ws)),
+                                   _stream(stream)))
 
 
 def spd_cache_evict_workspace_size(n_layers: int, n_seqs: int, n_kv_heads: int, budget: int) -> int:

@@ -13,7 +13,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIBDIR = os.path.join(PKG, "lib")
 LIB = os.path.join(LIBDIR, "libspider.so")
-SOURCES = ["api.cu", "gemm.cu", "attention.cu", "norm.cu", "prune.cu", "trace.cu", "tree.cu", "cache.cu", "logits.cu"]
+SOURCES = ["api.cu", "gemm.cu", "attention.cu", "norm.cu", "prune.cu", "trace.cu", "tree.cu", "weights.cu", "cache.cu",
+           "logits.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC,-O2", "--expt-relaxed-constexpr",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]

@@ -1,11 +1,10 @@
-// Keeping a KV cache within a budget: the weight its rows receive, the eviction of those that receive least, and the
-// move of an accepted path of drafts to the end of the context.
+// Keeping a KV cache within a budget: the eviction of the rows that receive least attention, and the move of an accepted
+// path of drafts to the end of the context.
 //
 // Cache rows are [K of every K/V head | V of every K/V head], bf16, at row (layer * n_seqs + seq) * max_len + slot. A
 // "unit" is one layer, sequence and K/V head: rows of a unit are evicted by the unit's own weights, so a slot holds
 // different tokens in different units, and `pos` (int32 a unit and slot) says which.
 #include <cooperative_groups.h>
-#include <cuda_bf16.h>
 #include <math.h>
 #include <stdint.h>
 #include <string.h>
@@ -313,61 +312,6 @@ __global__ void __launch_bounds__(256) commit_kernel(uint4* kv, const __grid_con
   }
 }
 
-// ---- received weight ---------------------------------------------------------------------------------
-struct WeightSeqs {
-  int len[kMaxSeqs];
-  int cu[kMaxSeqs + 1];
-};
-struct WeightArgs {
-  const __nv_bfloat16* q;
-  const float* lse;
-  const int32_t* rows;
-  const __nv_bfloat16* kv;
-  int n_q, n_seqs, seq0, max_len, n_heads, n_kv_heads;
-  float scale, decay;
-  const float* acc_in;
-  float* acc_out;
-};
-
-// One warp a key: every row's score is a dot product over the lanes.
-template <int HD>
-__global__ void __launch_bounds__(256) weights_kernel(const __grid_constant__ WeightArgs p,
-                                                      const __grid_constant__ WeightSeqs seqs) {
-  constexpr int D = HD / 32;
-  pdl_launch_dependents();
-  pdl_wait();
-  const int ls = blockIdx.y / p.n_kv_heads, g = blockIdx.y % p.n_kv_heads, layer = blockIdx.z;
-  const int len = seqs.len[ls], c0 = seqs.cu[ls], n = seqs.cu[ls + 1] - c0, G = p.n_heads / p.n_kv_heads;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, slot = blockIdx.x * 8 + warp;
-  if (slot >= len) return;
-  const size_t seq = size_t(layer) * p.n_seqs + p.seq0 + ls;
-  const __nv_bfloat16* k = p.kv + (seq * p.max_len + slot) * (2 * size_t(p.n_kv_heads) * HD) + g * HD + D * lane;
-  float kf[D];
-#pragma unroll
-  for (int e = 0; e < D; ++e) kf[e] = __bfloat162float(k[e]);
-  float sum = 0.0f;
-  for (int i = 0; i < n; ++i) {
-    if (slot >= len - n + i + 1) continue;
-    const int at = p.rows ? p.rows[c0 + i] : c0 + i;
-    if (at < 0 || at >= p.n_q) continue;
-    const size_t row = size_t(layer) * p.n_q + at;
-    for (int m = 0; m < G; ++m) {
-      const __nv_bfloat16* q = p.q + (row * p.n_heads + g * G + m) * HD + D * lane;
-      float s = 0.0f;
-#pragma unroll
-      for (int e = 0; e < D; ++e) s = fmaf(__bfloat162float(q[e]), kf[e], s);
-#pragma unroll
-      for (int off = 16; off; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-      const float l = p.lse[row * p.n_heads + g * G + m];
-      if (l > -INFINITY) sum += expf(s * p.scale - l);
-    }
-  }
-  if (lane == 0) {
-    const size_t to = (seq * p.n_kv_heads + g) * p.max_len + slot;
-    p.acc_out[to] = fmaf(p.decay, p.acc_in[to], sum);
-  }
-}
-
 }  // namespace
 }  // namespace spd
 
@@ -527,58 +471,5 @@ extern "C" int spd_tree_commit(uint16_t* kv_cache, int n_layers, int n_seqs, con
   SPD_CUDA_TRY(launch_pdl(commit_kernel, dim3((p.row16 + 255) / 256, n_seqs, n_layers), dim3(256), 0, st,
                           reinterpret_cast<uint4*>(kv_cache), p));
   trace_end(slot, st, TR_ROWS, 0.0, 32.0 * p.row16 * n_path * n_layers);
-  return SPD_OK;
-}
-
-extern "C" int spd_cache_weights(const uint16_t* q, const float* lse, int n_q, const int32_t* rows, const int32_t* rows_cu,
-                                 const uint16_t* kv_cache, int n_layers, int n_seqs, const int32_t* lens, int max_len,
-                                 int n_heads, int n_kv_heads, int head_dim, float decay, const float* acc_in, float* acc_out,
-                                 void* stream) {
-  if (!q || !lse || !rows_cu || !kv_cache || !lens || !acc_in || !acc_out || n_q < 0 || n_layers < 1 || n_seqs < 1 ||
-      max_len < 1 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads)
-    return fail(SPD_EINVAL, "bad cache weight arguments");
-  if (head_dim != 64 && head_dim != 128) return fail(SPD_EUNSUPPORTED, "head_dim must be 64 or 128");
-  if (rows_cu[0] != 0) return fail(SPD_EINVAL, "rows_cu must start at 0");
-  int longest = 0;
-  for (int b = 0; b < n_seqs; ++b) {
-    if (lens[b] < 0 || lens[b] > max_len) return fail(SPD_EINVAL, "length of sequence %d outside [0, max_len]", b);
-    if (rows_cu[b + 1] < rows_cu[b] || rows_cu[b + 1] - rows_cu[b] > lens[b])
-      return fail(SPD_EINVAL, "sequence %d: rows_cu decreases, or more rows than cached tokens", b);
-    longest = std::max(longest, lens[b]);
-  }
-  if (!rows && rows_cu[n_seqs] > n_q) return fail(SPD_EINVAL, "rows_cu runs past the queries");
-  if (longest == 0) return SPD_OK;
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  WeightArgs p{};
-  p.q = reinterpret_cast<const __nv_bfloat16*>(q);
-  p.lse = lse;
-  p.rows = rows;
-  p.kv = reinterpret_cast<const __nv_bfloat16*>(kv_cache);
-  p.n_q = n_q;
-  p.n_seqs = n_seqs;
-  p.max_len = max_len;
-  p.n_heads = n_heads;
-  p.n_kv_heads = n_kv_heads;
-  p.scale = 1.0f / sqrtf(float(head_dim));
-  p.decay = decay;
-  p.acc_in = acc_in;
-  p.acc_out = acc_out;
-  for (int s0 = 0; s0 < n_seqs; s0 += kMaxSeqs) {
-    WeightSeqs sq;
-    const int m = std::min(kMaxSeqs, n_seqs - s0);
-    p.seq0 = s0;
-    double keys = 0.0, pairs = 0.0;
-    for (int b = 0; b < m; ++b) {
-      sq.len[b] = lens[s0 + b];
-      keys += lens[s0 + b];
-      pairs += double(lens[s0 + b]) * (rows_cu[s0 + b + 1] - rows_cu[s0 + b]);
-    }
-    for (int b = 0; b <= m; ++b) sq.cu[b] = rows_cu[s0 + b];
-    const int slot = trace_begin(st);
-    SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? weights_kernel<128> : weights_kernel<64>,
-                            dim3((longest + 7) / 8, m * n_kv_heads, n_layers), dim3(256), 0, st, p, sq));
-    trace_end(slot, st, TR_ATTN, 2.0 * head_dim * n_heads * pairs * n_layers,
-              keys * n_layers * n_kv_heads * (2.0 * head_dim + 8.0));
-  }
   return SPD_OK;
 }
