@@ -9,10 +9,10 @@
 //   best = the first t of the largest x_t       (-1 when nothing is left)
 // every step one fp32 operation in this order.
 //
-// A row moves 8 V bytes and one occurrence count a token has to be found for it. The counts need no memory of the
-// GPU's: a cluster of CTAs shares a row's vocabulary, each holds the counts of its slice in shared memory (one word a
-// token), and every CTA adds its share of the history into the slices of all through distributed shared memory.
-#include <cooperative_groups.h>
+// A row moves 8 V bytes; the occurrence counts live in shared memory (a word a token of the CTA's slice), so they cost no
+// traffic and leave no state between calls. Up to 16 CTAs share a row; every one walks the whole history (4 bytes a token from L2)
+// and counts what falls into its slice, while its logits are on their way into registers. They meet only at the end, as a
+// cluster, for the best token.
 #include <math.h>
 #include <stdint.h>
 
@@ -23,9 +23,9 @@
 namespace spd {
 namespace {
 
-namespace cg = cooperative_groups;
-
-constexpr int kThreads = 512;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kHeld = 5;                    // 16-byte pieces of its slice that a thread holds in registers
+constexpr int kBatch = kThreads * 4 * kHeld; // tokens a CTA holds at once
 constexpr int kMaxSlice = 51200;             // tokens a CTA holds counts for (200 KB)
 constexpr uint32_t kPrompt = 1u << 31;       // the token is in the prompt
 constexpr uint32_t kBiased = 1u << 30;       // the sequence has a bias for it
@@ -57,155 +57,210 @@ __device__ __forceinline__ int2 range_of(const int32_t* cu, int i, int n) {
   return make_int2(lo, min(max(cu[i + 1], lo), n));
 }
 
-// A value's place in the order of floats (NaN below all), the token in the low half so that the first of equals wins.
+// A value's place in the order of floats (no NaN comes here), the token in the low half so that the first of equals wins.
 __device__ __forceinline__ unsigned long long order_key(float x, int token) {
   const uint32_t u = __float_as_uint(x + 0.0f);
-  const uint32_t k = isnan(x) ? 0u : (u >> 31) ? ~u : u | 0x80000000u;
-  return (static_cast<unsigned long long>(k) << 32) | (0xffffffffu - uint32_t(token));
+  return (static_cast<unsigned long long>((u >> 31) ? ~u : u | 0x80000000u) << 32) | (0xffffffffu - uint32_t(token));
 }
 
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
 template <bool VEC>
-__global__ void __launch_bounds__(kThreads) logit_rules_kernel(const LogitRules p) {
+__global__ void __launch_bounds__(kThreads, 5) logit_rules_kernel(const __grid_constant__ LogitRules p, int C) {
   extern __shared__ uint4 smem4[];
-  __shared__ unsigned long long warp_best[kThreads / 32];
-  __shared__ unsigned long long cta_best;
-  uint32_t* word = reinterpret_cast<uint32_t*>(smem4);  // [slice]
-  cg::cluster_group cluster = cg::this_cluster();
-  const int rank = int(cluster.block_rank()), C = int(cluster.num_blocks());
-  const int row = blockIdx.x / C, tid = threadIdx.x;
+  __shared__ unsigned long long warp_best[16 * kWarps];  // of every warp of the row, in the cluster's first CTA
+  uint32_t* word = reinterpret_cast<uint32_t*>(smem4);   // [slice]
+  const int rank = blockIdx.x % C, row = blockIdx.x / C, tid = threadIdx.x, lane = tid & 31;
   const int t0 = rank * p.slice, n = max(0, min(p.slice, p.vocab - t0));  // this CTA's tokens
+  cluster_arrive();  // waited for before the first access to another CTA's shared memory
   for (int i = tid; i < p.slice / 4; i += kThreads) smem4[i] = make_uint4(0u, 0u, 0u, 0u);
   pdl_launch_dependents();
   pdl_wait();
-  cluster.sync();
-  const int seq = p.seq_of ? p.seq_of[row] : row;
-  const bool has_seq = seq >= 0 && seq < p.n_seqs;
-  if (has_seq && p.hist) {
-    const int2 h = range_of(p.hist_cu, seq, p.n_hist);
-    const int gen = p.gen_start[seq];
-    for (int i = h.x + rank * kThreads + (tid & ~31); i < h.y; i += C * kThreads) {
-      const int at = i + (tid & 31);
-      const int t = at < h.y ? p.hist[at] : -1;
-      const bool fine = t >= 0 && t < p.vocab;  // placeholders of an image lie outside the vocabulary
-      const bool made = at >= gen;
-      // texts repeat few tokens: one addition for all of a warp's occurrences
-      const unsigned same = __match_any_sync(0xffffffffu, fine ? 2 * t + int(made) : -1);
-      if (fine && (tid & 31) == __ffs(same) - 1) {
-        uint32_t* w = cluster.map_shared_rank(word, t / p.slice) + t % p.slice;
-        if (made) atomicAdd(w, uint32_t(__popc(same)));
-        else atomicOr(w, kPrompt);
-      }
-    }
-  }
-  if (p.path) {
-    const int2 h = range_of(p.path_cu, row, p.n_path);
-    for (int i = h.x + tid; i < h.y; i += kThreads) {
-      const int t = p.path[i] - t0;
-      if (t >= 0 && t < n) atomicAdd(&word[t], 1u);
-    }
-  }
-  int2 bl = make_int2(0, 0);
-  if (has_seq && p.bias) {
-    bl = range_of(p.bias_cu, seq, p.n_bias);
-    for (int i = bl.x + tid; i < bl.y; i += kThreads) {
-      const int t = p.bias_id[i] - t0;
-      if (t >= 0 && t < n) atomicOr(&word[t], kBiased);
-    }
-  }
-  cluster.sync();  // every CTA's share of the history has arrived
-
-  const float rep = has_seq && p.rep ? p.rep[seq] : 1.0f;
-  const float freq = has_seq && p.freq ? p.freq[seq] : 0.0f, pres = has_seq && p.pres ? p.pres[seq] : 0.0f;
-  const int rule = p.allow && p.rule ? p.rule[row] : -1;
-  const uint32_t* allow = rule >= 0 && rule < p.n_rules ? p.allow + size_t(rule) * p.words + t0 / 32 : nullptr;
   const float* z = p.z + size_t(row) * p.ld_in + t0;
   float* out = p.out + size_t(row) * p.ld_out + t0;
-  unsigned long long best = 0;
-  auto one = [&](float x, uint32_t w, int i) {
+  // the slice's first batch is on its way while the history is counted
+  float4 x[kHeld];
+  auto load = [&](int base) {
+    if constexpr (VEC) {
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k) {
+        const int i = base + 4 * (k * kThreads + tid);
+        if (i < n) x[k] = __ldcs(reinterpret_cast<const float4*>(z + i));
+      }
+    }
+  };
+  const int seq = p.seq_of ? p.seq_of[row] : row;
+  const bool has_seq = seq >= 0 && seq < p.n_seqs;
+  const int2 hl = has_seq && p.hist ? range_of(p.hist_cu, seq, p.n_hist) : make_int2(0, 0);
+  const int gen = hl.y > hl.x ? min(max(p.gen_start[seq], hl.x), hl.y) : 0;
+  const int2 bl = has_seq && p.bias ? range_of(p.bias_cu, seq, p.n_bias) : make_int2(0, 0);
+  const int2 pl = p.path ? range_of(p.path_cu, row, p.n_path) : make_int2(0, 0);
+  const int rule = p.allow ? p.rule[row] : -1;
+  const uint32_t* allow = rule >= 0 && rule < p.n_rules ? p.allow + size_t(rule) * p.words + t0 / 32 : nullptr;
+  const float rep = has_seq && p.rep ? p.rep[seq] : 1.0f;
+  const float freq = has_seq && p.freq ? p.freq[seq] : 0.0f, pres = has_seq && p.pres ? p.pres[seq] : 0.0f;
+  int first[8];  // of the history, ahead of the logits
+#pragma unroll
+  for (int u = 0; u < 8; ++u) first[u] = hl.x + tid + u * kThreads < hl.y ? p.hist[hl.x + tid + u * kThreads] : -1;
+  // the thread's first entry of the bias list, and the logit that it concerns
+  const bool has_bias = bl.x + tid < bl.y;
+  const int b_id = has_bias ? p.bias_id[bl.x + tid] : -1;
+  const uint32_t b_tok = has_bias ? uint32_t(b_id - t0) : ~0u;
+  const float b_z = b_tok < uint32_t(n) ? z[b_tok] : 0.0f;
+  const float b_add = b_tok < uint32_t(n) ? p.bias[bl.x + tid] : 0.0f;
+  load(0);
+  __syncthreads();  // the words are zero
+  // Placeholders of an image lie outside the vocabulary and so outside every slice. (unsigned: negatives too)
+  auto count = [&](int token, int i) {
+    const uint32_t t = uint32_t(token) - uint32_t(t0);
+    if (token < 0 || t >= uint32_t(n)) return;
+    if (i >= gen) atomicAdd(&word[t], 1u);
+    else if (!(word[t] & kPrompt)) atomicOr(&word[t], kPrompt);  // a prompt may repeat one token throughout
+  };
+#pragma unroll
+  for (int u = 0; u < 8; ++u) count(first[u], hl.x + tid + u * kThreads);
+#pragma unroll 8
+  for (int i = hl.x + tid + 8 * kThreads; i < hl.y; i += kThreads) count(p.hist[i], i);
+  for (int i = pl.x + tid; i < pl.y; i += kThreads) {
+    const uint32_t t = uint32_t(p.path[i] - t0);
+    if (t < uint32_t(n)) atomicAdd(&word[t], 1u);
+  }
+  if (b_tok < uint32_t(n)) atomicOr(&word[b_tok], kBiased);
+  for (int i = bl.x + tid + kThreads; i < bl.y; i += kThreads) {
+    const uint32_t t = uint32_t(p.bias_id[i] - t0);
+    if (t < uint32_t(n)) atomicOr(&word[t], kBiased);
+  }
+  __syncthreads();
+
+  float best = -INFINITY;
+  int best_at = -1;
+  auto penalised = [&](float v, uint32_t w) {
     if (w & (kCount | kPrompt)) {
-      x = x > 0.0f ? __fdiv_rn(x, rep) : __fmul_rn(x, rep);
-      if (w & kCount) x = __fsub_rn(__fsub_rn(x, __fmul_rn(freq, float(w & kCount))), pres);
+      v = v > 0.0f ? __fdiv_rn(v, rep) : __fmul_rn(v, rep);
+      if (w & kCount) v = __fsub_rn(__fsub_rn(v, __fmul_rn(freq, float(w & kCount))), pres);
     }
-    if (w & kBiased) {  // the list ascends: the first entry of the token, then all of its entries in order
-      int lo = bl.x, hi = bl.y;
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (p.bias_id[mid] < t0 + i) lo = mid + 1;
-        else hi = mid;
-      }
-      float add = 0.0f;
-      for (; lo < bl.y && p.bias_id[lo] == t0 + i; ++lo) add = __fadd_rn(add, p.bias[lo]);
-      x = __fadd_rn(x, add);
+    return v;
+  };
+  auto take = [&](float v, int i) {  // a thread's tokens ascend: the first of equals stays
+    if (v > best) {
+      best = v;
+      best_at = t0 + i;
     }
-    return x;
   };
-  auto take = [&](float x, int i) {
-    const unsigned long long k = order_key(x, t0 + i);
-    best = k > best ? k : best;
+  // A thread a biased token (the list ascends: at its first entry, which adds up all of the token's). Nobody else
+  // touches its logit, so this also holds in place.
+  float biased_best = -INFINITY;
+  int biased_at = -1;
+  auto biased = [&](int i, int id, uint32_t t, float v, float add) {
+    if (i > bl.x && p.bias_id[i - 1] == id) return;
+    for (int j = i + 1; j < bl.y && p.bias_id[j] == id; ++j) add = __fadd_rn(add, p.bias[j]);
+    v = __fadd_rn(penalised(v, word[t]), add);
+    if (allow && !((allow[t / 32] >> (t % 32)) & 1u)) v = -INFINITY;
+    out[t] = v;
+    if (v > biased_best) {
+      biased_best = v;
+      biased_at = id;
+    }
   };
+  if (b_tok < uint32_t(n)) biased(bl.x + tid, b_id, b_tok, b_z, b_add);
+  for (int i = bl.x + tid + kThreads; i < bl.y; i += kThreads) {
+    const int id = p.bias_id[i];
+    const uint32_t t = uint32_t(id - t0);
+    if (t < uint32_t(n)) biased(i, id, t, z[t], p.bias[i]);
+  }
   if constexpr (VEC) {
-    for (int i = 4 * tid; i < n; i += 4 * kThreads) {
-      float4 x = *reinterpret_cast<const float4*>(z + i);
-      const uint4 w = smem4[i / 4];
-      const uint32_t a = allow ? allow[i / 32] >> (i % 32) : 15u;
-      if (w.x | w.y | w.z | w.w) {
-        x.x = one(x.x, w.x, i);
-        x.y = one(x.y, w.y, i + 1);
-        x.z = one(x.z, w.z, i + 2);
-        x.w = one(x.w, w.w, i + 3);
+    for (int base = 0; base < n; base += kBatch) {
+      if (base > 0) load(base);
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k) {
+        const int i = base + 4 * (k * kThreads + tid);
+        if (i < n) {
+          const uint4 w = smem4[i / 4];
+          const uint32_t a = allow ? allow[i / 32] >> (i % 32) : 15u, any = w.x | w.y | w.z | w.w;
+          float4 v = x[k];
+          if (any) {
+            v.x = penalised(v.x, w.x);
+            v.y = penalised(v.y, w.y);
+            v.z = penalised(v.z, w.z);
+            v.w = penalised(v.w, w.w);
+          }
+          if (!(a & 1u)) v.x = -INFINITY;
+          if (!(a & 2u)) v.y = -INFINITY;
+          if (!(a & 4u)) v.z = -INFINITY;
+          if (!(a & 8u)) v.w = -INFINITY;
+          if (any & kBiased) {  // the biased ones are left to the threads of the bias list
+            const float e[4] = {v.x, v.y, v.z, v.w};
+            const uint32_t f[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              if (!(f[c] & kBiased)) {
+                out[i + c] = e[c];
+                take(e[c], i + c);
+              }
+          } else {
+            *reinterpret_cast<float4*>(out + i) = v;
+            if (fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)) > best) {
+              take(v.x, i);
+              take(v.y, i + 1);
+              take(v.z, i + 2);
+              take(v.w, i + 3);
+            }
+          }
+        }
       }
-      if (!(a & 1u)) x.x = -INFINITY;
-      if (!(a & 2u)) x.y = -INFINITY;
-      if (!(a & 4u)) x.z = -INFINITY;
-      if (!(a & 8u)) x.w = -INFINITY;
-      *reinterpret_cast<float4*>(out + i) = x;
-      take(x.x, i);
-      take(x.y, i + 1);
-      take(x.z, i + 2);
-      take(x.w, i + 3);
     }
   } else {
     for (int i = tid; i < n; i += kThreads) {
-      float x = one(z[i], word[i], i);
-      if (allow && !((allow[i / 32] >> (i % 32)) & 1u)) x = -INFINITY;
-      out[i] = x;
-      take(x, i);
+      const uint32_t w = word[i];
+      if (w & kBiased) continue;
+      float v = penalised(z[i], w);
+      if (allow && !((allow[i / 32] >> (i % 32)) & 1u)) v = -INFINITY;
+      out[i] = v;
+      take(v, i);
     }
   }
   if (p.best) {
+    unsigned long long k = best_at >= 0 ? order_key(best, best_at) : 0;  // 0: nothing left
+    if (biased_at >= 0) {
+      const unsigned long long y = order_key(biased_best, biased_at);
+      k = y > k ? y : k;
+    }
 #pragma unroll
     for (int off = 16; off; off >>= 1) {
-      const unsigned long long k = __shfl_xor_sync(0xffffffffu, best, off);
-      best = k > best ? k : best;
+      const unsigned long long y = __shfl_xor_sync(0xffffffffu, k, off);
+      k = y > k ? y : k;
     }
-    if ((tid & 31) == 0) warp_best[tid >> 5] = best;
-    __syncthreads();
-    if (tid == 0) {
-      for (int w = 1; w < kThreads / 32; ++w) best = warp_best[w] > best ? warp_best[w] : best;
-      cta_best = best;
+    cluster_wait();  // every CTA of the row has started
+    if (lane == 0) {
+      const uint32_t to = dsmem_addr(&warp_best[rank * kWarps + (tid >> 5)], 0);
+      asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to), "l"(k) : "memory");
     }
-    cluster.sync();
-    if (rank == 0 && tid == 0) {
-      for (int c = 1; c < C; ++c) {
-        const unsigned long long k = *cluster.map_shared_rank(&cta_best, c);
-        best = k > best ? k : best;
+    __syncwarp();
+    cluster_arrive();
+    if (rank != 0) return;  // nobody reads this CTA's shared memory
+    cluster_wait();
+    if (tid < 32) {
+      k = 0;
+      for (int i = tid; i < C * kWarps; i += 32) k = warp_best[i] > k ? warp_best[i] : k;
+#pragma unroll
+      for (int off = 16; off; off >>= 1) {
+        const unsigned long long y = __shfl_xor_sync(0xffffffffu, k, off);
+        k = y > k ? y : k;
       }
-      // nothing left: every value is -inf (order key 0x007fffff) or NaN (0)
-      p.best[row] = (best >> 32) <= 0x007fffffull ? -1 : int32_t(0xffffffffu - uint32_t(best));
+      if (tid == 0) p.best[row] = k ? int32_t(0xffffffffu - uint32_t(k)) : -1;
     }
-    cluster.sync();  // the others' shared memory outlives the read
   }
 }
 
 }  // namespace
 
-// Cluster and slice for a vocabulary: eight CTAs a row, more where their slices would not fit in shared memory (16 is
-// the most a cluster has), fewer below 1024 tokens a CTA.
+// Cluster and slice for a vocabulary: as few CTAs a row as hold a whole slice in registers, 16 (the most a cluster
+// has) where that takes more; slices up to kMaxSlice are read in batches.
 static int logits_cluster(int vocab, int* slice) {
-  int c = 8;
-  while (c > 1 && vocab < 1024 * c) c /= 2;
   auto per = [&](int k) { return ((vocab + k - 1) / k + 31) / 32 * 32; };
-  if (per(c) > kMaxSlice) c = 16;
+  int c = 1;
+  while (c < 16 && per(c) > kBatch) c *= 2;
   *slice = per(c);
   return c;
 }
@@ -280,7 +335,7 @@ extern "C" int spd_logits_process(const float* logits, int n_rows, int vocab, in
   cfg.numAttrs = 2;
   const double by = 8.0 * n_rows * vocab + 4.0 * (double(p.n_hist) + p.n_path + 2.0 * p.n_bias);
   const int slot = trace_begin(cfg.stream);
-  SPD_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, p));
+  SPD_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, p, C));
   trace_end(slot, cfg.stream, TR_ROWS, 0.0, by);
   return SPD_OK;
 }
