@@ -40,6 +40,10 @@ constexpr uint32_t kKBox = kTK * 128;  // 64 columns of a block of K or V
 constexpr int kThreads = 192;
 constexpr uint32_t kTmemCols = 256;    // S: two buffers [0, 64) and [64, 128); O: [128, 128 + HD)
 constexpr int kItems = 304;            // items that fill the GPU: two CTAs on each of 152 SMs
+// The reference that a row's exponentials are taken against is renewed once its maximum has grown by this much (log2
+// units): weights stay below 2^8, their two terms and the fp32 sums are relative to them, and almost no block pays for the
+// round trip of O through the registers.
+constexpr float kGrown = 8.0f;
 constexpr int kMinBlocks = 2;          // key blocks an item has at the least where keys are split
 
 // Sequences of a launch, the longest first (by value in the parameters: no copy, no wait for one). Items
@@ -325,8 +329,9 @@ __global__ void __launch_bounds__(kThreads, 2)
       const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
       if (j == 0) {
         m_run = mx;
-      } else if (__any_sync(0xffffffffu, mx > m_run)) {
-        // the previous products have completed (those before had when these scores came): O can be rescaled
+      } else if (__any_sync(0xffffffffu, (mx - m_run) * p.scale_log2 > kGrown)) {
+        // a row's weights have outgrown its reference. The previous products have completed (those before had when
+        // these scores came): O can be rescaled
         if (!(ok = __all_sync(0xffffffffu, mbar_wait(o_done, (j - 1) & 1, abort_flag, p.budget)))) break;
         tc_fence_after();
         const float m_new = fmaxf(m_run, mx);
@@ -442,39 +447,74 @@ __global__ void __launch_bounds__(kThreads, 2)
 }
 
 // Rows whose keys were split: states (m_i, l_i, O_i) merged in key order, m = max m_i, l = sum l_i 2^(m_i - m),
-// O = sum O_i 2^(m_i - m). A warp a row (node and head).
-constexpr int kMergeWarps = 4;
+// O = sum O_i 2^(m_i - m). W warps a row (node and head), each a range of the parts, eight of them in flight; the kernel is
+// a handful of dependent loads, so long rows of parts want more warps, not longer loops.
+constexpr int kMergeWarps = 8;
 template <int HD>
 __global__ void __launch_bounds__(kMergeWarps * 32)
-    tree_merge_kernel(const __grid_constant__ TreeArgs p, const __grid_constant__ TreeSeqs sq) {
-  constexpr int D = HD / 32;
+    tree_merge_kernel(const __grid_constant__ TreeArgs p, const __grid_constant__ TreeSeqs sq, int W) {
+  constexpr int D = HD / 32;  // dims a lane
+  __shared__ float wl[kMergeWarps], wo[kMergeWarps][HD];
   pdl_launch_dependents();
   pdl_wait();
   const int e = blockIdx.y, n = sq.nodes[e], parts = sq.parts[e];
-  const int row = blockIdx.x * kMergeWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (parts < 2 || row >= n * p.n_heads) return;
-  const int node = row / p.n_heads, head = row % p.n_heads, hk = head / p.group, hg = head % p.group;
-  const int tiles = (n + p.nodes_tile - 1) / p.nodes_tile * p.chunks;
-  const int tile = node / p.nodes_tile * p.chunks + hg / p.chunk;
-  const int r = node % p.nodes_tile * p.chunk + hg % p.chunk;
-  const size_t first = (size_t(sq.part0[e]) + size_t(hk) * parts * tiles + tile) * p.rows_part + r;
-  const size_t step = size_t(tiles) * p.rows_part;
-  float m = -INFINITY;
-  for (int s = lane; s < parts; s += 32) m = fmaxf(m, p.part_ml[first + s * step].x);
-#pragma unroll
-  for (int off = 16; off; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
-  float l = 0.0f, o[D];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp % W;
+  const int row = blockIdx.x * (kMergeWarps / W) + warp / W;
+  const bool have = parts > 1 && row < n * p.n_heads;
+  float m = -INFINITY, l = 0.0f, o[D];
 #pragma unroll
   for (int x = 0; x < D; ++x) o[x] = 0.0f;
-#pragma unroll 4
-  for (int s = 0; s < parts; ++s) {
-    const float2 ml = p.part_ml[first + s * step];
-    const float f = ml.x == -INFINITY ? 0.0f : exp2f(ml.x - m);
-    const float* po = p.part_o + (first + s * step) * HD + D * lane;
-    l = fmaf(ml.y, f, l);
+  const int node = row / p.n_heads, head = row % p.n_heads;
+  if (have) {
+    const int hk = head / p.group, hg = head % p.group;
+    const int tiles = (n + p.nodes_tile - 1) / p.nodes_tile * p.chunks;
+    const int tile = node / p.nodes_tile * p.chunks + hg / p.chunk;
+    const int r = node % p.nodes_tile * p.chunk + hg % p.chunk;
+    const size_t first = (size_t(sq.part0[e]) + size_t(hk) * parts * tiles + tile) * p.rows_part + r;
+    const size_t step = size_t(tiles) * p.rows_part;
+    for (int s = lane; s < parts; s += 32) m = fmaxf(m, p.part_ml[first + s * step].x);
 #pragma unroll
-    for (int x = 0; x < D; ++x) o[x] = fmaf(po[x], f, o[x]);
+    for (int off = 16; off; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+    const int s1 = (w + 1) * parts / W;
+    for (int s0 = w * parts / W; s0 < s1; s0 += 8) {
+      float2 ml[8];
+      float v[8][D];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const size_t at = first + min(s0 + u, s1 - 1) * step;
+        ml[u] = p.part_ml[at];
+        const float* po = p.part_o + at * HD + D * lane;
+        if constexpr (D == 4) {
+          const float4 f = *reinterpret_cast<const float4*>(po);
+          v[u][0] = f.x, v[u][1] = f.y, v[u][2] = f.z, v[u][3] = f.w;
+        } else {
+          const float2 f = *reinterpret_cast<const float2*>(po);
+          v[u][0] = f.x, v[u][1] = f.y;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        if (s0 + u >= s1 || ml[u].x == -INFINITY) continue;  // a part in which the row sees nothing
+        const float f = exp2f(ml[u].x - m);
+        l = fmaf(ml[u].y, f, l);
+#pragma unroll
+        for (int x = 0; x < D; ++x) o[x] = fmaf(v[u][x], f, o[x]);
+      }
+    }
   }
+  if (W > 1) {
+    if (lane == 0) wl[warp] = l;
+#pragma unroll
+    for (int x = 0; x < D; ++x) wo[warp][D * lane + x] = o[x];
+    __syncthreads();
+    if (w > 0) return;
+    for (int k = 1; k < W; ++k) {
+      l += wl[warp + k];
+#pragma unroll
+      for (int x = 0; x < D; ++x) o[x] += wo[warp + k][D * lane + x];
+    }
+  }
+  if (!have) return;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   const size_t at = size_t(sq.q0[e] + node) * p.n_heads + head;
   uint32_t* to = reinterpret_cast<uint32_t*>(p.o + at * HD + D * lane);
@@ -564,11 +604,18 @@ int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, i
     }
     if (order.empty()) continue;
     std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return blocks(x) > blocks(y); });
-    // blocks an item: an even share of the GPU's places, and no less than kMinBlocks
-    const long long share = std::max<long long>(kMinBlocks, (work + kItems - 1) / kItems);
+    // blocks an item: an even share of the GPU's places and no less than kMinBlocks, more where rounding up would start
+    // a second wave of a few items (and no more than leaves the keys whole)
+    long long share = std::max<long long>(kMinBlocks, (work + kItems - 1) / kItems);
+    auto total = [&]() {
+      long long k = 0;
+      for (int b : order) k += units(b) * ((blocks(b) + share - 1) / share);
+      return k;
+    };
+    while (share < blocks(order[0]) && total() > kItems) share += (share + 15) / 16;
     TreeSeqs sq{};
     long long items = 0;
-    int parts = 0, most = 0;
+    int parts = 0, most = 0, most_parts = 0;
     for (int b : order) {
       const int e = sq.n++;
       const int k = int((blocks(b) + share - 1) / share);
@@ -582,6 +629,7 @@ int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, i
       if (k > 1) {
         parts += int(units(b)) * k;
         most = std::max(most, count(b));
+        most_parts = std::max(most_parts, k);
       }
       items += units(b) * k;
     }
@@ -593,9 +641,13 @@ int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, i
     const int slot = trace_begin(st);
     SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? tree_attn_kernel<128> : tree_attn_kernel<64>, dim3(unsigned(items)), dim3(kThreads),
                             head_dim == 128 ? TreeSmem<128>::bytes : TreeSmem<64>::bytes, st, map, p, sq));
-    if (most > 0)
+    if (most > 0) {
+      int W = 1;
+      while (W < kMergeWarps && most_parts > 8 * W) W *= 2;
       SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? tree_merge_kernel<128> : tree_merge_kernel<64>,
-                              dim3((most * n_heads + kMergeWarps - 1) / kMergeWarps, sq.n), dim3(kMergeWarps * 32), 0, st, p, sq));
+                              dim3((most * n_heads * W + kMergeWarps - 1) / kMergeWarps, sq.n), dim3(kMergeWarps * 32), 0, st, p,
+                              sq, W));
+    }
     trace_end(slot, st, TR_ATTN, fl, by);
   }
   return SPD_OK;
