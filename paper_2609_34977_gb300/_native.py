@@ -201,6 +201,9 @@ def _p(t):
 _DT = {"f32": "float32", "bf16": "bfloat16", "i32": "int32", "u8": "uint8", "i8": "int8"}
 
 
+_torch_dt = {}  # element type names -> torch dtypes, once torch has been imported
+
+
 def _dev(t, dt, n, name, optional=False):
     """Device pointer of argument `name` after checking it: a contiguous CUDA tensor of element
     type dt ('f32', 'bf16', 'i32', 'u8', 'i8') holding at least n elements (the elements the call
@@ -210,14 +213,19 @@ def _dev(t, dt, n, name, optional=False):
         if optional:
             return None
         raise ValueError(f"{name}: a device tensor is required")
-    if isinstance(t, np.ndarray) or not getattr(t, "is_cuda", False):
+    if not getattr(t, "is_cuda", False):
         raise TypeError(f"{name}: device arguments of libspider must be CUDA tensors, got "
                         f"{type(t).__name__} on {getattr(t, 'device', 'the host')}")
-    if str(t.dtype) != "torch." + _DT[dt]:
+    if not _torch_dt:
+        import torch
+        _torch_dt.update({k: getattr(torch, v) for k, v in _DT.items()})
+    if t.dtype is not _torch_dt[dt]:
         raise ValueError(f"{name}: expected {_DT[dt]}, got {t.dtype}")
     if t.numel() < n:
         raise ValueError(f"{name}: {t.numel()} elements, the call touches {int(n)}")
-    return _p(t)
+    if not t.is_contiguous():
+        raise ValueError("tensors passed to libspider must be contiguous")
+    return t.data_ptr()
 
 
 def _host(a, dtype, n, name):
@@ -235,10 +243,18 @@ def _ws(ws):
     return _p(ws), ws.numel() * ws.element_size()
 
 
+_current_stream = None
+
+
 def _stream(stream):
+    global _current_stream
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        if _current_stream is None:  # the raw handle where torch offers it: a Stream object costs 2 us a call
+            import torch
+            raw, dev = (getattr(torch._C, k, None) for k in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+            _current_stream = ((lambda: raw(dev())) if raw and dev
+                               else (lambda: torch.cuda.current_stream().cuda_stream))
+        return _current_stream()
     return int(stream)
 
 

@@ -29,12 +29,18 @@ namespace cg = cooperative_groups;
 // gaps in order would move every row behind the first hole.)
 //
 // Selection: the weights as order-preserving 32-bit keys in shared memory (a cluster of CTAs where a unit has more than
-// one holds), the keep-th largest found two bits a round by counting the keys that reach each of three candidates (no
-// atomics: the usual histograms of exponent bits put most keys on a handful of addresses), then two prefix sums.
-constexpr int kSelThreads = 1024;
-constexpr int kSelWarps = kSelThreads / 32;
+// one holds), the keep-th largest by a radix search of 11, 11 and 10 bits: the first digit, sign, exponent and two bits of
+// the mantissa, spreads weights of any scale over enough counters that the additions do not queue, and the search ends as
+// soon as a digit's keys are all kept, after two digits as a rule. (Counting the keys that reach three candidates a round, two
+// bits at a time and without atomics, took 16 rounds of 1000 cycles, more than all the rest.)
+// A CTA is one chain of loads, passes and prefix sums, whatever its width: units of up to kSelSmall slots get 256 threads, so
+// that several of them share an SM.
+constexpr int kSelSmall = 4096;
+constexpr int kSelWide = 1024;      // threads for longer ones
+constexpr int kBins = 2048;
 constexpr int kSelMost = 49152;     // keys a CTA holds (192 KB)
 constexpr int kSelMaxCluster = 8;
+constexpr int kFusedMoves = 64;
 constexpr int kMaxSeqs = 240;       // sequences whose sizes fit in a launch's parameters
 constexpr uint32_t kHeld = 0xffffffffu;
 
@@ -59,7 +65,8 @@ __device__ __forceinline__ uint32_t weight_key(float a) {
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-// Exclusive prefix sum over the block of a value below 2^16 a thread; *total the block's sum. tmp: kSelWarps ints.
+// Exclusive prefix sum over the T threads of the block; *total the block's sum. tmp: T / 32 ints.
+template <int T>
 __device__ int block_before(int v, int* tmp, int* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int x = v;
@@ -70,7 +77,7 @@ __device__ int block_before(int v, int* tmp, int* total) {
   }
   if (lane == 31) tmp[warp] = x;
   __syncthreads();
-  int w = tmp[lane];
+  int w = lane < T / 32 ? tmp[lane] : 0;
 #pragma unroll
   for (int off = 1; off < 32; off <<= 1) {
     const int y = __shfl_up_sync(0xffffffffu, w, off);
@@ -82,14 +89,18 @@ __device__ int block_before(int v, int* tmp, int* total) {
   return before;
 }
 
-__global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_constant__ EvictArgs p,
-                                                                   const __grid_constant__ EvictSeqs seqs, int per) {
-  extern __shared__ uint32_t key[];  // [per]: this CTA's slots
-  __shared__ int tmp[kSelWarps];
-  __shared__ int part[kSelWarps][3];
-  __shared__ int counts[2][3];       // of this CTA, by round parity: keys that reach each candidate
-  __shared__ int shared_total[2];    // ties; holes (low half) and fills (high half are separate words)
-  __shared__ int shared_moves[2];
+// HD > 0: the kernel also moves the rows (a step's few), else evict_move_kernel does.
+template <int T, int HD>
+__global__ void __launch_bounds__(T, T == 256 ? 6 : 1)
+    evict_select_kernel(uint16_t* kv, const __grid_constant__ EvictArgs p, const __grid_constant__ EvictSeqs seqs, int per) {
+  constexpr int kWarps = T / 32, kEach = kBins / T;  // counters a thread
+  extern __shared__ uint32_t smem[];
+  uint32_t* bins = smem;               // [2][kBins]
+  uint32_t* key = smem + 2 * kBins;    // [per]: this CTA's slots
+  __shared__ int tmp[kWarps];
+  __shared__ int found[3];             // the digit, keys above it, keys with it
+  __shared__ int ties_here, moves_here[2];
+  __shared__ int list[2][kFusedMoves];
   cg::cluster_group cluster = cg::this_cluster();
   const int C = int(cluster.num_blocks()), rank = int(cluster.block_rank());
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -98,6 +109,10 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
   const int ls = at / p.n_kv_heads, g = at - ls * p.n_kv_heads;
   const size_t unit = (size_t(layer) * p.n_seqs + p.seq0 + ls) * p.n_kv_heads + g;
   const int n = seqs.len[ls], keep = min(n, p.budget), next = seqs.next_pos[ls];
+  auto meet = [&]() {
+    if (C > 1) cluster.sync();
+    else __syncthreads();
+  };
   pdl_launch_dependents();
   pdl_wait();
   const float* acc = p.acc_in + unit * p.max_len;
@@ -107,138 +122,159 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
   int32_t* src = p.src ? p.src + unit * p.budget : nullptr;
   const int lo = min(n, rank * per), cnt = min(n, lo + per) - lo;  // this CTA's slots
   if (n <= p.budget) {  // nothing leaves (every CTA of the cluster agrees)
-    for (int i = tid; i < cnt; i += kSelThreads) {
+    for (int i = tid; i < cnt; i += T) {
       acc_out[lo + i] = acc[lo + i];
       if (pos_out) pos_out[lo + i] = pos ? pos[lo + i] : lo + i;
       if (src) src[lo + i] = lo + i;
     }
-    if (rank == 0 && tid == 0) p.moves[unit] = 0;
+    if (HD == 0 && rank == 0 && tid == 0) p.moves[unit] = 0;
     return;
   }
-  for (int i = tid; i < per; i += kSelThreads) {
-    uint32_t k = 0;  // below every weight's key
-    if (i < cnt) {
-      const int q = pos ? pos[lo + i] : lo + i;
-      k = q < p.n_sink || q >= next - p.n_recent ? kHeld : weight_key(acc[lo + i]);
-    }
-    key[i] = k;
+  for (int i = tid; i < 2 * kBins; i += T) bins[i] = 0;
+#pragma unroll 4
+  for (int i = tid; i < cnt; i += T) {
+    const int q = pos ? pos[lo + i] : lo + i;
+    const float a = acc[lo + i];
+    key[i] = q < p.n_sink || q >= next - p.n_recent ? kHeld : weight_key(a);
   }
   __syncthreads();
-  // the largest threshold that at least `keep` keys reach
+  // the keep-th largest key: thr, and how many of its equals stay (the lowest slots)
   uint32_t thr = 0;
-  int reach = n;
-  for (int bit = 30, round = 0; bit >= 0; bit -= 2, ++round) {
-    int c1 = 0, c2 = 0, c3 = 0;
-    const uint32_t t1 = thr | (1u << bit), t2 = thr | (2u << bit), t3 = thr | (3u << bit);
-    for (int i = 4 * tid; i < per; i += 4 * kSelThreads) {
-      const uint4 k = *reinterpret_cast<const uint4*>(key + i);
-      c1 += (k.x >= t1) + (k.y >= t1) + (k.z >= t1) + (k.w >= t1);
-      c2 += (k.x >= t2) + (k.y >= t2) + (k.z >= t2) + (k.w >= t2);
-      c3 += (k.x >= t3) + (k.y >= t3) + (k.z >= t3) + (k.w >= t3);
+  int need = keep, equal = n;
+  for (int pass = 0, shift = 21; pass < 3 && equal != need; ++pass) {
+    const int width = pass < 2 ? 11 : 10;
+    uint32_t* bin = bins + (pass & 1) * kBins;
+    for (int i = tid; i < cnt; i += T)
+      if (pass == 0 || (key[i] >> (shift + width)) == (thr >> (shift + width)))
+        atomicAdd(&bin[(key[i] >> shift) & ((1u << width) - 1)], 1u);
+    meet();
+    // counters from the largest digit down: thread t has kEach of them
+    const int top = kBins - kEach * (tid + 1);
+    uint32_t here[kEach] = {};
+    for (int c = 0; c < C; ++c) {
+      const uint32_t* b = C > 1 ? cluster.map_shared_rank(bin, c) : bin;
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) here[u] += b[top + u];
     }
-    c1 = __reduce_add_sync(0xffffffffu, c1);
-    c2 = __reduce_add_sync(0xffffffffu, c2);
-    c3 = __reduce_add_sync(0xffffffffu, c3);
-    if (lane == 0) {
-      part[warp][0] = c1;
-      part[warp][1] = c2;
-      part[warp][2] = c3;
+    if (pass > 0)  // the counters of the pass before, which nobody reads any more
+      for (int i = tid; i < kBins; i += T) bins[((pass & 1) ^ 1) * kBins + i] = 0;
+    int sum = 0, all;
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) sum += int(here[u]);
+    int above = block_before<T>(sum, tmp, &all);
+    if (above < need && need <= above + sum) {
+#pragma unroll
+      for (int u = kEach - 1; u >= 0; --u) {
+        if (above < need && need <= above + int(here[u])) {
+          found[0] = top + u;
+          found[1] = above;
+          found[2] = int(here[u]);
+        }
+        above += int(here[u]);
+      }
     }
     __syncthreads();
-    if (warp < 3) {
-      const int s = __reduce_add_sync(0xffffffffu, part[lane][warp]);
-      if (lane == 0) counts[round & 1][warp] = s;
-    }
-    if (C > 1) cluster.sync();
-    else __syncthreads();
-    int r1 = 0, r2 = 0, r3 = 0;
-    for (int c = 0; c < C; ++c) {
-      const int* q = C > 1 ? cluster.map_shared_rank(&counts[round & 1][0], c) : &counts[round & 1][0];
-      r1 += q[0];
-      r2 += q[1];
-      r3 += q[2];
-    }
-    if (r3 >= keep) thr = t3, reach = r3;
-    else if (r2 >= keep) thr = t2, reach = r2;
-    else if (r1 >= keep) thr = t1, reach = r1;
-    if (reach == keep) break;  // the same in every thread: the keys that reach it are the kept ones
+    thr |= uint32_t(found[0]) << shift;
+    need -= found[1];
+    equal = found[2];
+    shift -= pass == 0 ? 11 : 10;
+    __syncthreads();  // found has been read
   }
-  // a thread's slots are consecutive, so that prefix sums run in slot order
-  const int each = (per + kSelThreads - 1) / kSelThreads;
+  // kept: key > thr's digits, and of those with thr's digits the first `need` by slot (all of them where equal == need). A
+  // thread's slots are consecutive, so that prefix sums run in slot order.
+  const int each = (per + T - 1) / T;
   const int i0 = min(cnt, tid * each), i1 = min(cnt, i0 + each);
-  int ties = 0, above = 0;
+  const bool split = equal != need;  // only after the last pass: thr is a whole key
+  int ties = 0;
+  if (split) {
+    for (int i = i0; i < i1; ++i) ties += key[i] == thr;
+    int all;
+    ties = block_before<T>(ties, tmp, &all);
+    if (tid == 0) ties_here = all;
+    meet();
+    for (int c = 0; c < rank; ++c) ties += *cluster.map_shared_rank(&ties_here, c);
+  }
+  int both = 0;  // holes in the low half, fills in the high half
   for (int i = i0; i < i1; ++i) {
-    ties += key[i] == thr;
-    above += key[i] > thr;
+    const uint32_t k = key[i];
+    const bool kept = split ? k > thr || (k == thr && ties++ < need) : k >= thr;
+    both += lo + i < keep ? !kept : int(kept) << 16;
+    key[i] = kept;  // from here on
   }
-  int tie_total, all_above;
-  int tie_before = block_before(ties, tmp, &tie_total);
-  block_before(above, tmp, &all_above);
-  if (tid == 0) {
-    shared_total[0] = tie_total;
-    shared_total[1] = all_above;
-  }
-  if (C > 1) cluster.sync();
-  else __syncthreads();
-  int take = keep;  // ties that stay: the lowest slots
-  for (int c = 0; c < C; ++c) {
-    const int* q = C > 1 ? cluster.map_shared_rank(shared_total, c) : shared_total;
-    take -= q[1];
-    if (c < rank) tie_before += q[0];
-  }
-  int holes = 0, fills = 0, t = tie_before;
-  for (int i = i0; i < i1; ++i) {
-    const bool kept = key[i] > thr || (key[i] == thr && t++ < take);
-    holes += !kept && lo + i < keep;
-    fills += kept && lo + i >= keep;
-  }
-  int hole_total, fill_total;
-  int hole_at = block_before(holes, tmp, &hole_total), fill_at = block_before(fills, tmp, &fill_total);
-  if (tid == 0) {
-    shared_moves[0] = hole_total;
-    shared_moves[1] = fill_total;
-  }
-  if (C > 1) cluster.sync();
-  else __syncthreads();
-  int moves = 0;
-  for (int c = 0; c < C; ++c) {
-    const int* q = C > 1 ? cluster.map_shared_rank(shared_moves, c) : shared_moves;
-    moves += q[0];
-    if (c < rank) {
-      hole_at += q[0];
-      fill_at += q[1];
+  int total;
+  both = block_before<T>(both, tmp, &total);
+  int hole_at = both & 0xffff, fill_at = int(uint32_t(both) >> 16), moves = total & 0xffff;
+  if (C > 1) {
+    if (tid == 0) {
+      moves_here[0] = total & 0xffff;
+      moves_here[1] = int(uint32_t(total) >> 16);
     }
-  }
-  int32_t *fill = p.fill + unit * p.budget, *hole = p.hole + unit * p.budget;
-  t = tie_before;
-  for (int i = i0; i < i1; ++i) {
-    const int s = lo + i;
-    const bool kept = key[i] > thr || (key[i] == thr && t++ < take);
-    if (s < keep) {
-      if (kept) {
-        acc_out[s] = acc[s];
-        if (pos_out) pos_out[s] = pos ? pos[s] : s;
-        if (src) src[s] = s;
-      } else {
-        hole[hole_at++] = s;
+    cluster.sync();
+    moves = 0;
+    for (int c = 0; c < C; ++c) {
+      const int* q = cluster.map_shared_rank(moves_here, c);
+      moves += q[0];
+      if (c < rank) {
+        hole_at += q[0];
+        fill_at += q[1];
       }
-    } else if (kept) {
-      fill[fill_at++] = s;
     }
   }
-  __threadfence();  // the lists, for the other CTAs of the cluster
-  if (C > 1) cluster.sync();
-  else __syncthreads();
-  for (int j = rank * kSelThreads + tid; j < moves; j += C * kSelThreads) {
-    const int s = __ldcg(hole + j), f = __ldcg(fill + j);
+  // the lists; a CTA on its own with few moves keeps them to itself
+  const bool in_smem = HD > 0 && C == 1;
+  int32_t *fill = in_smem ? list[0] : p.fill + unit * p.budget, *hole = in_smem ? list[1] : p.hole + unit * p.budget;
+  if (moves > 0)
+    for (int i = i0; i < i1; ++i) {
+      const int s = lo + i;
+      if (s < keep && !key[i]) hole[hole_at++] = s;
+      if (s >= keep && key[i]) fill[fill_at++] = s;
+    }
+  if (!in_smem) __threadfence();  // for the other CTAs of the cluster
+  meet();
+  if constexpr (HD > 0) {
+    // a warp a move, 16 bytes a lane: K's row, V's row (HD = 64: in half of the lanes)
+    constexpr int VEC = HD / 8;
+    const int kvd = p.n_kv_heads * HD, col = (lane / VEC) * kvd + g * HD + (lane % VEC) * 8;
+    uint16_t* base = kv + (unit / p.n_kv_heads) * p.max_len * (2 * size_t(kvd)) + col;
+    for (int j = rank * kWarps + warp; j < moves; j += C * kWarps) {
+      const int s = *(volatile int32_t*)(hole + j), f = *(volatile int32_t*)(fill + j);
+      if (lane < 2 * VEC)
+        *reinterpret_cast<uint4*>(base + size_t(s) * (2 * kvd)) = *reinterpret_cast<const uint4*>(base + size_t(f) * (2 * kvd));
+    }
+  } else {
+    if (rank == 0 && tid == 0) p.moves[unit] = moves;
+  }
+  // rows that stay in their slots (four of a thread's in flight)
+  const int stay = min(cnt, keep - lo);
+  for (int i = tid; i < stay; i += 4 * T) {
+    float a[4];
+    int q[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int x = i + u * T;
+      if (x < stay && key[x]) {
+        a[u] = acc[lo + x];
+        q[u] = pos ? pos[lo + x] : lo + x;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int x = i + u * T;
+      if (x < stay && key[x]) {
+        acc_out[lo + x] = a[u];
+        if (pos_out) pos_out[lo + x] = q[u];
+        if (src) src[lo + x] = lo + x;
+      }
+    }
+  }
+  for (int j = rank * T + tid; j < moves; j += C * T) {
+    const int s = *(volatile int32_t*)(hole + j), f = *(volatile int32_t*)(fill + j);
     acc_out[s] = acc[f];
     if (pos_out) pos_out[s] = pos ? pos[f] : f;
     if (src) src[s] = f;
   }
-  if (rank == 0 && tid == 0) p.moves[unit] = moves;
-  if (C > 1) cluster.sync();  // before the slots past the budget are cleared, which may be the ones read above
-  else __syncthreads();
-  for (int s = keep + rank * kSelThreads + tid; s < n; s += C * kSelThreads) {
+  meet();  // before the slots past the budget are cleared, which may be the ones read above
+  for (int s = keep + rank * T + tid; s < n; s += C * T) {
     acc_out[s] = 0.0f;
     if (pos_out) pos_out[s] = -1;
   }
@@ -373,8 +409,14 @@ extern "C" int spd_cache_evict(uint16_t* kv_cache, int n_layers, int n_seqs, con
   int per = (std::max(longest, 1) + C - 1) / C;
   for (int b = 0; b < n_seqs; ++b) per = std::max(per, (std::min(lens[b], budget) + C - 1) / C);
   per = (per + 3) & ~3;
-  SPD_CUDA_TRY(cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelMost * 4));
-  const size_t smem = longest ? size_t(per) * 4 : 16;
+  // moves that the selecting CTA makes itself: where a unit has few of them, the second launch costs more
+  const bool fused = most_moves <= kFusedMoves, small = per <= kSelSmall;
+  const auto select = small ? (!fused ? evict_select_kernel<256, 0> : head_dim == 128 ? evict_select_kernel<256, 128>
+                                                                                      : evict_select_kernel<256, 64>)
+                            : (!fused ? evict_select_kernel<kSelWide, 0> : head_dim == 128 ? evict_select_kernel<kSelWide, 128>
+                                                                                           : evict_select_kernel<kSelWide, 64>);
+  if (!small) SPD_CUDA_TRY(cudaFuncSetAttribute(select, cudaFuncAttributeMaxDynamicSharedMemorySize, 8 * kBins + 4 * kSelMost));
+  const size_t smem = longest ? 8 * size_t(kBins) + 4 * size_t(per) : 16;
   for (int s0 = 0; s0 < n_seqs; s0 += kMaxSeqs) {
     EvictSeqs sq;
     p.seq0 = s0;
@@ -389,7 +431,7 @@ extern "C" int spd_cache_evict(uint16_t* kv_cache, int n_layers, int n_seqs, con
     const int n = n_layers * p.launch_seqs * n_kv_heads;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(n * C);
-    cfg.blockDim = dim3(kSelThreads);
+    cfg.blockDim = dim3(small ? 256 : kSelWide);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -402,9 +444,9 @@ extern "C" int spd_cache_evict(uint16_t* kv_cache, int n_layers, int n_seqs, con
     cfg.attrs = attr;
     cfg.numAttrs = 2;
     int slot = trace_begin(st);
-    SPD_CUDA_TRY(cudaLaunchKernelEx(&cfg, evict_select_kernel, p, sq, per));
+    SPD_CUDA_TRY(cudaLaunchKernelEx(&cfg, select, kv_cache, p, sq, per));
     trace_end(slot, st, TR_ROWS, 0.0, 16.0 * rows * n_layers * n_kv_heads);
-    if (most_moves > 0) {
+    if (!fused) {
       const int rows_cta = kMoveWarps * kMoveDepth * (128 / head_dim);
       const dim3 grid((most_moves + rows_cta - 1) / rows_cta, n);
       slot = trace_begin(st);

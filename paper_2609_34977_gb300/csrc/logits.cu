@@ -63,9 +63,6 @@ __device__ __forceinline__ unsigned long long order_key(float x, int token) {
   return (static_cast<unsigned long long>((u >> 31) ? ~u : u | 0x80000000u) << 32) | (0xffffffffu - uint32_t(token));
 }
 
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-
 template <bool VEC>
 __global__ void __launch_bounds__(kThreads, 5) logit_rules_kernel(const __grid_constant__ LogitRules p, int C) {
   extern __shared__ uint4 smem4[];

@@ -10,7 +10,9 @@
 // all the rows that see it: the up to 128 rows of an MMA tile are the nodes of a sequence times the query heads of a
 // K/V head's group. An item is one such tile over a range of keys; the ranges are cut so that the items fill the GPU
 // (two CTAs an SM) and every item of a batch of different lengths has about the same number of keys. Parts of a row's
-// keys leave (m, l, O) in fp32, merged by tree_merge_kernel in the order of the keys: the same bits in every run.
+// keys leave states (m, l, O) in fp32, merged in the order of the keys (the same bits in every run): those of a cluster of up to 8
+// items through distributed shared memory, and where a row's keys take more than one cluster, the clusters' by
+// tree_merge_kernel.
 //   warp 4     TMA producer: blocks of 64 keys of K and of V into rings
 //   warp 5     MMA issuer: S = Q K^T into TMEM, then O += P V with P read from TMEM, V in place as an MN-major operand
 //   warps 0-3  a thread a row: the block's 64 scores in registers, online softmax in fp32; a weight is held as the sum of two
@@ -44,16 +46,16 @@ constexpr int kItems = 304;            // items that fill the GPU: two CTAs on e
 // units): weights stay below 2^8, their two terms and the fp32 sums are relative to them, and almost no block pays for the
 // round trip of O through the registers.
 constexpr float kGrown = 8.0f;
-constexpr int kMinBlocks = 2;          // key blocks an item has at the least where keys are split
+constexpr int kMaxCluster = 8;
 
-// Sequences of a launch, the longest first (by value in the parameters: no copy, no wait for one). Items
-// [item0[e], item0[e + 1]) are sequence e's: (K/V head, part of the keys, tile), the tile fastest, so that the tiles that read
-// the same keys run side by side.
+// Sequences of a launch, the longest first (by value in the parameters: no copy, no wait for one). Clusters
+// [item0[e], item0[e + 1]) are sequence e's: (K/V head, group of parts of the keys, tile), the tile fastest, so that the tiles
+// that read the same keys run side by side; the CTAs of a cluster are the parts of its group.
 struct TreeSeqs {
   int n, item0[kMaxSeqs + 1];
   int q0[kMaxSeqs], nodes[kMaxSeqs], ctx[kMaxSeqs], seq[kMaxSeqs];
-  int16_t parts[kMaxSeqs];
-  int part0[kMaxSeqs];  // first slot of the sequence's parts in the workspace (parts > 1)
+  int16_t groups[kMaxSeqs];
+  int part0[kMaxSeqs];  // first slot of the sequence's states in the workspace (groups > 1)
 };
 struct TreeArgs {
   const __nv_bfloat16* q;
@@ -65,8 +67,9 @@ struct TreeArgs {
   float scale_log2;
   __nv_bfloat16* o;
   float* lse;
-  float* part_o;   // [part][rows_part][HD]
-  float2* part_ml; // [part][rows_part]: maximum (log2 units), sum
+  int cluster;     // CTAs a cluster
+  float* part_o;   // [cluster][rows_part][HD] states of sequences of several groups
+  float2* part_ml; // [cluster][rows_part]: maximum (log2 units), sum
   int rows_part;
   int* status;
   long long budget;
@@ -80,8 +83,11 @@ struct TreeSmem {
   static constexpr uint32_t q = 0;
   static constexpr uint32_t k = q + kChunks * kQBox;
   static constexpr uint32_t v = k + kStages * kChunks * kKBox;
-  static constexpr uint32_t bars = v + kStages * kChunks * kKBox;
+  static constexpr uint32_t ml = v + kStages * kChunks * kKBox;  // [128] a row's maximum and sum (in a cluster)
+  static constexpr uint32_t bars = ml + 128 * 8;
   static constexpr uint32_t bytes = bars + 256 + 1024;  // + alignment slack
+  static constexpr uint32_t state = k;  // [128][HD] fp32 O of a cluster's merge, over the rings
+  static_assert(128 * HD * 4 <= ml - k, "the rings hold the tile's O");
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -137,20 +143,21 @@ __global__ void __launch_bounds__(kThreads, 2)
   int* odd_v = reinterpret_cast<int*>(tmem_slot + 2);  // some visible V is not finite
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  // the item's sequence: the last entry that starts at or before it
-  int e = 0;
+  // the cluster's sequence: the last entry that starts at or before it
+  const int C = p.cluster, rank = int(blockIdx.x) % C;
+  int u = int(blockIdx.x) / C, e = 0;
   for (int hi = sq.n; hi - e > 1;) {
     const int mid = (e + hi) >> 1;
-    if (sq.item0[mid] <= int(blockIdx.x)) e = mid;
+    if (sq.item0[mid] <= u) e = mid;
     else hi = mid;
   }
-  const int n = sq.nodes[e], ctx = sq.ctx[e], parts = sq.parts[e];
+  const int n = sq.nodes[e], ctx = sq.ctx[e], groups = sq.groups[e], parts = groups * C;
   const int tiles = (n + p.nodes_tile - 1) / p.nodes_tile * p.chunks;
-  int u = int(blockIdx.x) - sq.item0[e];
+  u -= sq.item0[e];
   const int slot = sq.part0[e] + u;
   const int tile = u % tiles;
   u /= tiles;
-  const int part = u % parts, hk = u / parts;
+  const int part = u % groups * C + rank, hk = u / groups;
   const int n0 = tile / p.chunks * p.nodes_tile, h0 = tile % p.chunks * p.chunk;  // first node, first head of the group
   const int nodes = min(p.nodes_tile, n - n0), rows = nodes * p.chunk;
   const int heads = min(p.chunk, p.group - h0);  // of the chunk's heads, those there are
@@ -238,7 +245,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         mma_commit(&k_empty[s]);
         return true;
       };
-      if (ok) ok = issue_s(0);
+      if (ok && nkb > 0) ok = issue_s(0);  // (a short sequence's parts may be empty)
       for (int j = 0; j < nkb && ok; ++j) {
         const int s = j % NS;
         if (j + 1 < nkb && !(ok = issue_s(j + 1))) break;
@@ -257,7 +264,8 @@ __global__ void __launch_bounds__(kThreads, 2)
         *abort_flag = 1;
         set_status(p.status, SPD_ETIMEOUT);
       }
-      mma_commit(drain);  // arrives once every MMA issued above has completed
+      if (nkb > 0) mma_commit(drain);  // arrives once every MMA issued above has completed
+      else mbar_arrive(drain);
       volatile int no_abort = 0;
       if (!mbar_wait(drain, 0, &no_abort, p.budget)) set_status(p.status, SPD_ETIMEOUT);
     }
@@ -371,6 +379,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     if (!ok) {
       *abort_flag = 1;
       set_status(p.status, SPD_ETIMEOUT);
+      if (C > 1) *reinterpret_cast<float2*>(smem + L::ml + r * 8) = make_float2(-INFINITY, 0.0f);
     } else {
       tc_fence_after();
       if (*reinterpret_cast<volatile int*>(odd_v)) {
@@ -401,7 +410,20 @@ __global__ void __launch_bounds__(kThreads, 2)
       }
       const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
       const float m2 = m_run * p.scale_log2;
-      if (parts > 1) {
+      if (C > 1) {  // to this CTA's shared memory: 16-byte piece j of row r at j ^ r, so that neither side meets in a bank
+        *reinterpret_cast<float2*>(smem + L::ml + r * 8) = make_float2(m2, l_run);
+        if (nkb > 0) {
+#pragma unroll 1
+          for (int c = 0; c < HD / 32; ++c) {
+            float v[32];
+            tmem_ld32(t_o + lanes + c * 32, v);
+#pragma unroll
+            for (int y = 0; y < 8; ++y)
+              *reinterpret_cast<float4*>(smem + L::state + r * (HD * 4) + (((c * 8 + y) ^ (r & (HD / 4 - 1))) << 4)) =
+                  make_float4(v[4 * y], v[4 * y + 1], v[4 * y + 2], v[4 * y + 3]);
+          }
+        }
+      } else if (parts > 1) {
         float* po = p.part_o + (size_t(slot) * p.rows_part + r) * HD;
         if (valid) p.part_ml[size_t(slot) * p.rows_part + r] = make_float2(m2, l_run);
 #pragma unroll 1
@@ -443,10 +465,61 @@ __global__ void __launch_bounds__(kThreads, 2)
   __syncwarp();
   tc_fence_after();
   if (warp == 4) tmem_dealloc(tmem, kTmemCols);
+  if (C > 1) {
+    // every CTA merges its share of the tile's rows, in rank order
+    cluster_arrive();
+    cluster_wait();
+    constexpr int P = HD / 4;  // 16-byte pieces a row
+    const int r1 = rows * (rank + 1) / C;
+    for (int x = rows * rank / C * P + int(threadIdx.x); x < r1 * P; x += kThreads) {
+      const int r = x / P, j = x % P, hc = r % p.chunk;
+      const uint32_t at_ml = smem_u32(smem + L::ml + r * 8);
+      const uint32_t at_o = smem_u32(smem + L::state + r * (HD * 4) + ((j ^ (r & (P - 1))) << 4));
+      float2 ml[kMaxCluster];
+      float4 v[kMaxCluster];
+#pragma unroll
+      for (int k = 0; k < kMaxCluster; ++k) {
+        ml[k] = make_float2(-INFINITY, 0.0f);
+        if (k < C) {
+          uint32_t a, b;
+          asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(at_ml), "r"(k));
+          asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(b) : "r"(at_o), "r"(k));
+          ml[k] = ld_dsmem_v2(a);
+          v[k] = ld_dsmem_v4(b);
+        }
+      }
+      float m = -INFINITY, l = 0.0f;
+#pragma unroll
+      for (int k = 0; k < kMaxCluster; ++k) m = fmaxf(m, ml[k].x);
+      float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int k = 0; k < kMaxCluster; ++k) {
+        if (ml[k].x == -INFINITY) continue;  // a part in which the row sees nothing
+        const float f = exp2f(ml[k].x - m);
+        l = fmaf(ml[k].y, f, l);
+        o.x = fmaf(v[k].x, f, o.x);
+        o.y = fmaf(v[k].y, f, o.y);
+        o.z = fmaf(v[k].z, f, o.z);
+        o.w = fmaf(v[k].w, f, o.w);
+      }
+      if (groups > 1) {
+        const size_t at = size_t(slot) * p.rows_part + r;
+        if (j == 0) p.part_ml[at] = make_float2(m, l);
+        reinterpret_cast<float4*>(p.part_o + at * HD)[j] = o;
+      } else if (hc < heads) {
+        const size_t at = size_t(sq.q0[e] + n0 + r / p.chunk) * p.n_heads + hk * p.group + h0 + hc;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        reinterpret_cast<uint2*>(p.o + at * HD)[j] = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+        if (j == 0 && p.lse) p.lse[at] = fmaf(m, 0.6931471805599453f, logf(l));
+      }
+    }
+    cluster_arrive();  // the others' shared memory outlives the reads
+    cluster_wait();
+  }
   if (threadIdx.x == 0) stamp_end(p.stamp);
 }
 
-// Rows whose keys were split: states (m_i, l_i, O_i) merged in key order, m = max m_i, l = sum l_i 2^(m_i - m),
+// Rows whose keys took several clusters: states (m_i, l_i, O_i) merged in key order, m = max m_i, l = sum l_i 2^(m_i - m),
 // O = sum O_i 2^(m_i - m). W warps a row (node and head), each a range of the parts, eight of them in flight; the kernel is
 // a handful of dependent loads, so long rows of parts want more warps, not longer loops.
 constexpr int kMergeWarps = 8;
@@ -457,7 +530,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
   __shared__ float wl[kMergeWarps], wo[kMergeWarps][HD];
   pdl_launch_dependents();
   pdl_wait();
-  const int e = blockIdx.y, n = sq.nodes[e], parts = sq.parts[e];
+  const int e = blockIdx.y, n = sq.nodes[e], parts = sq.groups[e];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp % W;
   const int row = blockIdx.x * (kMergeWarps / W) + warp / W;
   const bool have = parts > 1 && row < n * p.n_heads;
@@ -534,15 +607,82 @@ TreeTile tree_tile(int n_heads, int n_kv_heads) {
   t.nodes = 128 / t.chunk;
   return t;
 }
-// Rows kept of a part, and parts there can be at once: keys are split only where a sequence has more blocks than an even
-// share of kItems items, which gives at most 2 kItems of them.
+// Rows of a state in the workspace.
 int rows_of_part(const TreeTile& t, int n_q) { return std::min(t.nodes, n_q) * t.chunk; }
-constexpr int kMaxParts = 2 * kItems;
+
+// How the keys of a launch are split: clusters of `cluster` CTAs, and as many of them a tile as leave a CTA `share` blocks
+// of keys. The choice minimises an estimate of the launch's time from what CTAs were measured to take (us, GB300): a CTA
+// kCtaTime besides its blocks (its launch, the first loads, the last products), a block `alone` with the SM to itself and
+// `pair` beside a second CTA (half an SM's share of HBM), a merge in the cluster, one through memory by the rows of its states.
+// Where the CTAs do not fit on the GPU at once, later ones start as earlier ones end, at 1.3 times the even share of the
+// work. Estimated / measured: one token, 321 keys, 32 heads, cluster 1 / 4 / 8: 13 / 9.4 / 8.2 and 11.2 / 9.2 / 8.7; 32
+// trees on 300 to 1958 keys, 4 K/V heads, no split / cluster 2 / 10 blocks a CTA, merged through memory: 43 / 29.5 / 25 and 43.1 /
+// 33.8 / 30.0; eight of 48 nodes, 32 K/V heads, cluster 1 / 2 / 4: 39 / 46 / 59 and 35.3 / 43.4 / 59.0.
+constexpr double kCtaTime = 6.0, kClusterTime = 1.0, kMergeTime = 4.0, kMergeRow = 0.25e-3, kWaveFactor = 1.3;
+constexpr int kMaxStates = kItems;  // states in memory of a launch: those of plans that fit on the GPU at once
+struct TreePlan {
+  int cluster = 1;
+  long long share = 1 << 30;
+  int groups(int blocks) const { return int(std::max<long long>(1, (blocks + share * cluster - 1) / (share * cluster))); }
+};
+// blocks(i), units(i), rows(i): key blocks, (tile, K/V head) pairs and (node, head) rows of sequence i, the longest first;
+// places: CTAs the GPU holds at once.
+template <typename Blocks, typename Units, typename Rows>
+TreePlan tree_plan(size_t n, Blocks blocks, Units units, Rows rows, int places, int head_dim) {
+  const double alone = head_dim == 128 ? 1.2 : 0.93, pair = head_dim == 128 ? 1.45 : 0.93;
+  TreePlan best;
+  double least = 1e30;
+  for (int k = 0; 1 << k <= kMaxCluster; ++k) {
+    // CTAs that fit in clusters: 304, 304, 288 and 256 of the 304 places of 152 SMs (the largest launches that ran as one wave)
+    const int c = 1 << k, room = std::max(c, places - (c == 4 ? places / 19 : c == 8 ? 3 * places / 19 : 0));
+    auto ctas = [&](const TreePlan& t) {
+      long long all = 0;
+      for (size_t i = 0; i < n; ++i) all += units(i) * t.groups(blocks(i)) * c;
+      return all;
+    };
+    auto weigh = [&](const TreePlan& t) {
+      double all = 0.0, blocks_all = 0.0, longest = 0.0, merge = 0.0;
+      long long states = 0;
+      for (size_t i = 0; i < n; ++i) {
+        const int g = t.groups(blocks(i));
+        all += double(units(i)) * g * c;
+        blocks_all += double(units(i)) * blocks(i);
+        longest = std::max(longest, double(blocks(i)) / (g * c));
+        if (g > 1) {
+          states += units(i) * g;
+          merge += kMergeRow * double(rows(i)) * g;
+        }
+      }
+      if (states > kMaxStates) return;
+      const double block = 2 * all > room ? pair : alone;
+      double cost = kCtaTime + longest * block;
+      if (all > room) cost = std::max(cost, kCtaTime + kWaveFactor * (all * kCtaTime + blocks_all * pair) / room);
+      cost += (c > 1 ? kClusterTime : 0.0) + (states ? kMergeTime + merge : 0.0);
+      if (cost < least) {
+        least = cost;
+        best = t;
+      }
+    };
+    TreePlan whole;  // one group
+    whole.cluster = c;
+    weigh(whole);
+    if (ctas(whole) >= room) continue;
+    TreePlan t = whole;  // the smallest share whose CTAs all fit at once
+    long long lo = 0, hi = (blocks(0) + c - 1) / c;  // (lo does not, hi does)
+    while (hi - lo > 1) {
+      t.share = (lo + hi) / 2;
+      (ctas(t) > room ? lo : hi) = t.share;
+    }
+    t.share = hi;
+    weigh(t);
+  }
+  return best;
+}
 
 }  // namespace
 
 size_t tree_attention_bytes(int n_q, int, int n_heads, int n_kv_heads, int head_dim) {
-  const size_t rows = size_t(kMaxParts) * rows_of_part(tree_tile(n_heads, n_kv_heads), n_q);
+  const size_t rows = size_t(kMaxStates) * rows_of_part(tree_tile(n_heads, n_kv_heads), n_q);
   Carve cv(nullptr, ~size_t(0));
   cv.take<float>(rows * head_dim);
   cv.take<float2>(rows);
@@ -573,24 +713,23 @@ int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, i
   p.lse = lse;
   Carve cv(ws, ws_bytes);
   p.rows_part = rows_of_part(t, q_cu[n_seqs]);
-  const size_t rows = size_t(kMaxParts) * p.rows_part;
+  const size_t rows = size_t(kMaxStates) * p.rows_part;
   p.part_o = cv.take<float>(rows * head_dim);
   p.part_ml = cv.take<float2>(rows);
   p.status = cv.status();
   p.budget = kWaitBudget;
-  static bool attr = false;
-  if (!attr) {
-    SPD_CUDA_TRY(cudaFuncSetAttribute(tree_attn_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                      int(TreeSmem<128>::bytes)));
-    SPD_CUDA_TRY(cudaFuncSetAttribute(tree_attn_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                      int(TreeSmem<64>::bytes)));
-    attr = true;
+  const auto kernel = head_dim == 128 ? tree_attn_kernel<128> : tree_attn_kernel<64>;
+  const size_t smem = head_dim == 128 ? TreeSmem<128>::bytes : TreeSmem<64>::bytes;
+  static bool attr[2] = {};
+  if (!attr[head_dim == 128]) {
+    SPD_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+    attr[head_dim == 128] = true;
   }
+  const int places = std::min(kItems, 2 * num_sms());
   std::vector<int> order;
   for (int s0 = 0; s0 < n_seqs; s0 += kMaxSeqs) {
     const int m = std::min(kMaxSeqs, n_seqs - s0);
     order.clear();
-    long long work = 0;  // key blocks of all items
     double pairs = 0.0, keys = 0.0;
     auto count = [&](int b) { return q_cu[b + 1] - q_cu[b]; };
     auto blocks = [&](int b) { return (ctx[b] + count(b) + kTK - 1) / kTK; };
@@ -598,52 +737,61 @@ int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, i
     for (int b = s0; b < s0 + m; ++b) {
       if (count(b) == 0) continue;
       order.push_back(b);
-      work += units(b) * blocks(b);
       keys += ctx[b] + count(b);
       pairs += double(count(b)) * (ctx[b] + count(b));
     }
     if (order.empty()) continue;
     std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return blocks(x) > blocks(y); });
-    // blocks an item: an even share of the GPU's places and no less than kMinBlocks, more where rounding up would start
-    // a second wave of a few items (and no more than leaves the keys whole)
-    long long share = std::max<long long>(kMinBlocks, (work + kItems - 1) / kItems);
-    auto total = [&]() {
-      long long k = 0;
-      for (int b : order) k += units(b) * ((blocks(b) + share - 1) / share);
-      return k;
-    };
-    while (share < blocks(order[0]) && total() > kItems) share += (share + 15) / 16;
+    const TreePlan plan = tree_plan(order.size(), [&](size_t i) { return blocks(order[i]); },
+                                    [&](size_t i) { return units(order[i]); },
+                                    [&](size_t i) { return (long long)count(order[i]) * n_heads; }, places, head_dim);
+    const int C = plan.cluster;
     TreeSeqs sq{};
     long long items = 0;
-    int parts = 0, most = 0, most_parts = 0;
+    int states = 0, most = 0, most_groups = 0;
     for (int b : order) {
       const int e = sq.n++;
-      const int k = int((blocks(b) + share - 1) / share);
+      const int k = plan.groups(blocks(b));
       sq.item0[e] = int(items);
       sq.q0[e] = q_cu[b];
       sq.nodes[e] = count(b);
       sq.ctx[e] = ctx[b];
       sq.seq[e] = b;
-      sq.parts[e] = int16_t(k);
-      sq.part0[e] = parts;
+      sq.groups[e] = int16_t(k);
+      sq.part0[e] = states;
       if (k > 1) {
-        parts += int(units(b)) * k;
+        states += int(units(b)) * k;
         most = std::max(most, count(b));
-        most_parts = std::max(most_parts, k);
+        most_groups = std::max(most_groups, k);
       }
       items += units(b) * k;
     }
-    if (items > 0x7fffffff) return fail(SPD_EUNSUPPORTED, "tree attention of more than 2^31 tiles");
+    if (items * C > 0x7fffffff) return fail(SPD_EUNSUPPORTED, "tree attention of more than 2^31 tiles");
+    if (states > kMaxStates) return fail(SPD_EUNSUPPORTED, "tree attention plan of %d states", states);
     sq.item0[sq.n] = int(items);
+    p.cluster = C;
     const double fl = 4.0 * head_dim * n_heads * pairs;
     const double by = 4.0 * kvd * keys + 4.0 * n_heads * head_dim * (q_cu[s0 + m] - q_cu[s0]);
     p.stamp = stamp_slot(TR_ATTN, fl, by);
     const int slot = trace_begin(st);
-    SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? tree_attn_kernel<128> : tree_attn_kernel<64>, dim3(unsigned(items)), dim3(kThreads),
-                            head_dim == 128 ? TreeSmem<128>::bytes : TreeSmem<64>::bytes, st, map, p, sq));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(items) * C);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute la[2];
+    la[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    la[0].val.programmaticStreamSerializationAllowed = 1;
+    la[1].id = cudaLaunchAttributeClusterDimension;
+    la[1].val.clusterDim.x = C;
+    la[1].val.clusterDim.y = 1;
+    la[1].val.clusterDim.z = 1;
+    cfg.attrs = la;
+    cfg.numAttrs = 2;
+    SPD_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, map, p, sq));
     if (most > 0) {
       int W = 1;
-      while (W < kMergeWarps && most_parts > 8 * W) W *= 2;
+      while (W < kMergeWarps && most_groups > 8 * W) W *= 2;
       SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? tree_merge_kernel<128> : tree_merge_kernel<64>,
                               dim3((most * n_heads * W + kMergeWarps - 1) / kMergeWarps, sq.n), dim3(kMergeWarps * 32), 0, st, p,
                               sq, W));
