@@ -415,6 +415,24 @@ int spd_tree_attention(const uint16_t* q, int n_q, const int32_t* q_cu, const in
                        int n_kv_heads, int head_dim, uint16_t* o, float* lse, void* ws, size_t ws_bytes,
                        void* stream);
 
+/* Workspace bytes of spd_decode_tree for n_q nodes. */
+size_t spd_decode_tree_workspace_size(const spd_model* m, int n_q);
+
+/* A generation step over drafted tokens: x (dev bf16 [n_q][d_model]) holds the embeddings of the nodes of every
+ * sequence's tree, in a cache as spd_prefill_kv leaves it (the first node is the token that spd_decode would take; one node a
+ * sequence, at rotary position ctx_len, is spd_decode's step). Every layer writes node i's K and V to slot ctx_len[b] + i of its
+ * sequence and attends as spd_tree_attention; generated tokens run every sub-layer. pos (HOST int32 [n_q]): rotary
+ * positions (the next position plus the node's depth; they need not be the slots). logits (dev, may be NULL) fp32
+ * [n_q][vocab] of every node. For spd_cache_weights: q_out (dev, may be NULL, 16-byte aligned) bf16
+ * [n_layers][n_q][n_heads * head_dim] receives the rotated queries, lse_out (dev, may be NULL) fp32
+ * [n_layers][n_q][n_heads] their normalisers. q_cu, ctx_len, tree_mask as spd_tree_attention; kv_cache (dev) bf16
+ * [n_layers][n_seqs][max_len][K | V], 16-byte aligned.
+ * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ENOSPC, SPD_ECUDA; device timeouts in the workspace's status word. */
+int spd_decode_tree(const spd_model* m, const uint16_t* x, int n_q, const int32_t* q_cu, const int32_t* ctx_len,
+                    int n_seqs, const int32_t* pos, const uint32_t* tree_mask, int mask_words, uint16_t* kv_cache,
+                    int max_len, float* logits, uint16_t* q_out, float* lse_out, void* ws, size_t ws_bytes,
+                    void* stream);
+
 /* Workspace bytes of spd_tree_commit for paths of n_path nodes in all. */
 size_t spd_tree_commit_workspace_size(int n_seqs, int n_path);
 

@@ -34,7 +34,8 @@ EXPORTS = ("spd_last_error", "spd_workspace_status", "spd_selftest_bounded_wait"
            "spd_step_workspace_size", "spd_step", "spd_step_status",
            "spd_tree_mask", "spd_tree_attention_workspace_size", "spd_tree_attention",
            "spd_tree_commit_workspace_size", "spd_tree_commit", "spd_cache_weights",
-           "spd_cache_evict_workspace_size", "spd_cache_evict", "spd_logits_process")
+           "spd_cache_evict_workspace_size", "spd_cache_evict", "spd_logits_process",
+           "spd_decode_tree_workspace_size", "spd_decode_tree")
 TRACE_GEMM, TRACE_ATTN, TRACE_ROWS, TRACE_PRUNE = 0, 1, 2, 3
 
 
@@ -160,6 +161,8 @@ def lib():
             "spd_tree_mask": (i, [i, vp, vp, i, vp, vp]),
             "spd_tree_attention_workspace_size": (sz, [i, i, i, i, i]),
             "spd_tree_attention": (i, [vp, i, vp, vp, i, vp, i, vp, i, i, i, i, vp, vp, vp, sz, vp]),
+            "spd_decode_tree_workspace_size": (sz, [vp, i]),
+            "spd_decode_tree": (i, [vp, vp, i, vp, vp, i, vp, vp, i, vp, i, vp, vp, vp, vp, sz, vp]),
             "spd_tree_commit_workspace_size": (sz, [i, i]),
             "spd_tree_commit": (i, [vp, i, i, vp, vp, vp, i, i, i, vp, vp, vp, vp, sz, vp]),
             "spd_cache_weights": (i, [vp, vp, i, vp, vp, vp, i, i, vp, i, i, i, i, C.c_float, vp, vp, vp, sz, vp]),
@@ -566,6 +569,29 @@ def spd_tree_attention(q, q_cu, ctx_len, tree_mask, kv, max_len, n_heads, n_kv_h
                                     _dev(kv, "bf16", B * max_len * 2 * n_kv_heads * head_dim, "kv"), max_len, n_heads,
                                     n_kv_heads, head_dim, _dev(o, "bf16", n_q * qd, "o"),
                                     _dev(lse, "f32", n_q * n_heads, "lse", True), wp, wb, _stream(stream)))
+
+
+def spd_decode_tree_workspace_size(model: SpdModel, n_q: int) -> int:
+    return int(lib().spd_decode_tree_workspace_size(model.handle, n_q))
+
+
+def spd_decode_tree(model: SpdModel, x, q_cu, ctx_len, pos, tree_mask, kv_cache, max_len, logits, ws, q_out=None,
+                    lse_out=None, stream=None):
+    """One generation step over the drafted tokens x [n_q][d_model] of every sequence (host q_cu, ctx_len and rotary
+    positions pos; tree_mask: int32 device words [n_q][words] or None for chains); logits [n_q][vocab]."""
+    cu = np.ascontiguousarray(q_cu, dtype=np.int32)
+    B, n_q = len(cu) - 1, int(cu[-1])
+    ctx, rot = _host(ctx_len, np.int32, B, "ctx_len"), _host(pos, np.int32, n_q, "pos")
+    c = model.cfg
+    words = 0 if tree_mask is None else tree_mask.shape[-1]
+    rows = c["n_layers"] * n_q * c["n_heads"]
+    wp, wb = _ws(ws)
+    _check(lib().spd_decode_tree(model.handle, _dev(x, "bf16", n_q * c["d_model"], "x"), n_q, _p(cu), _p(ctx), B, _p(rot),
+                                 _dev(tree_mask, "i32", n_q * words, "tree_mask", True), words,
+                                 _dev(kv_cache, "bf16", spd_kv_cache_bytes(model, B, max_len) // 2, "kv_cache"), max_len,
+                                 _dev(logits, "f32", n_q * c["vocab"], "logits", True),
+                                 _dev(q_out, "bf16", rows * c["head_dim"], "q_out", True),
+                                 _dev(lse_out, "f32", rows, "lse_out", True), wp, wb, _stream(stream)))
 
 
 def spd_tree_commit_workspace_size(n_seqs: int, n_path: int) -> int:

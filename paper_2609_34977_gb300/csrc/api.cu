@@ -575,6 +575,17 @@ struct LayerLists {
   int na, nf, ntiles;
   double ctx;
 };
+// What a step over drafted tokens gives its attention (spd_decode_tree).
+struct TreeStep {
+  const int32_t *q_cu, *ctx;
+  int n_seqs;
+  const uint32_t* mask;
+  int words, max_len;
+  uint16_t* q;  // [n_layers][n_q][n_heads * head_dim], or null: the scratch of one layer
+  float* lse;   // [n_layers][n_q][n_heads] or null
+  void* ws;
+  size_t ws_bytes;
+};
 struct HostPlan {
   std::vector<int32_t> hl;
   std::vector<int> pos_all, seq_of;
@@ -582,6 +593,7 @@ struct HostPlan {
   std::vector<LayerLists> ll;
   size_t pos_off = 0, kvrow_off = 0, last_off = 0, end = 0;
   bool decode = false;  // one query per sequence at its last position (attention_decode_run)
+  const TreeStep* tree = nullptr;  // drafted tokens over the cache (tree_attention_run)
   std::vector<int> by_length;  // decode: the sequences, longest first
 };
 
@@ -604,6 +616,7 @@ void plan_init(HostPlan& P, const spd_model_cfg& c, const int32_t* cu, int B, in
   }
   P.ll.assign(c.n_layers, LayerLists{});
   P.decode = false;
+  P.tree = nullptr;
   size_t off = 0;
   P.pos_off = off;
   for (int t = 0; t < T; ++t) P.hl[off + t] = P.pos_all[t];
@@ -700,6 +713,7 @@ int run_layer(const spd_model* m, int l, const LayerLists& q, const HostPlan& P,
   // matrix-vector path (a few tokens) the GEMM applies the norm itself.
   const KVDest dest = kvd_dest ? *kvd_dest : KVDest{bf.kv, T, false};
   const int32_t* kvrow = dest.cache ? dl + P.kvrow_off : nullptr;
+  uint16_t* qbuf = P.tree && P.tree->q ? P.tree->q + size_t(l) * T * qd : bf.q;
   GemmProblem kvp{};
   kvp.map_w = &W.m_kv;
   kvp.w = W.wkv;
@@ -732,7 +746,7 @@ int run_layer(const spd_model* m, int l, const LayerLists& q, const HostPlan& P,
     qp.w = W.wq;  // Wq rows, then Wk and Wv rows, contiguous
     qp.n_out = qd + 2 * kvd;
     qp.epi = EPI_QKV_BF16;
-    qp.out = bf.q;
+    qp.out = qbuf;
     qp.ldo = qd;
     qp.rows = dl + q.amap;
     qp.out2 = dest.kv;
@@ -747,7 +761,12 @@ int run_layer(const spd_model* m, int l, const LayerLists& q, const HostPlan& P,
     if ((rc = gemm_run(kvp, bf.gs, st))) return rc;
   }
   if (q.na > 0) {
-    if (P.decode)
+    if (P.tree)
+      rc = tree_attention_run(qbuf, P.tree->q_cu, P.tree->ctx, P.tree->n_seqs, P.tree->mask, P.tree->words, dest.kv,
+                              P.tree->max_len, c.n_heads, c.n_kv_heads, hd, bf.o,
+                              P.tree->lse ? P.tree->lse + size_t(l) * T * c.n_heads : nullptr, P.tree->ws, P.tree->ws_bytes,
+                              bf.gs.status, st);
+    else if (P.decode)
       rc = attention_decode_run(bf.q, dest.kv, 2 * kvd, kvd, bf.o, qd,
                                 reinterpret_cast<const int4*>(dl + q.tiles), q.ntiles, c.n_heads,
                                 c.n_kv_heads, hd, st, q.ctx);
@@ -1148,6 +1167,71 @@ extern "C" int spd_decode(const spd_model* m, const uint16_t* x, int B, const in
     if (int rc = run_layer(m, l, P.ll[l], P, bf, dl, h, B, st, &dest)) return rc;
   }
   return run_head(m, P, bf, dl, h, B, logits, st);
+}
+
+// ---- a step over drafted tokens -----------------------------------------------------------------
+namespace {
+// Every node is a row of its own in the executor's lists (its logits are wanted); the attention alone knows the trees.
+size_t carve_tree(const spd_model_cfg& c, int n_q, Carve& cv, PrefillBufs* bf, float** h, void** tree_ws, size_t* tree_bytes) {
+  carve_decode(c, n_q, cv, bf, h);
+  *tree_bytes = tree_attention_bytes(n_q, c.n_heads, c.n_kv_heads, c.head_dim);
+  *tree_ws = cv.take<uint8_t>(*tree_bytes);
+  return cv.used;
+}
+}  // namespace
+
+extern "C" size_t spd_decode_tree_workspace_size(const spd_model* m, int n_q) {
+  if (!m || n_q < 1) return 0;
+  Carve cv(nullptr, ~size_t(0));
+  PrefillBufs bf;
+  float* h;
+  void* tw;
+  size_t tb;
+  return carve_tree(m->cfg, n_q, cv, &bf, &h, &tw, &tb);
+}
+
+extern "C" int spd_decode_tree(const spd_model* m, const uint16_t* x, int n_q, const int32_t* q_cu, const int32_t* ctx_len,
+                               int n_seqs, const int32_t* pos, const uint32_t* tree_mask, int mask_words,
+                               uint16_t* kv_cache, int max_len, float* logits, uint16_t* q_out, float* lse_out, void* ws,
+                               size_t ws_bytes, void* stream) {
+  if (!m || !x || !q_cu || !ctx_len || !pos || !kv_cache || !ws || n_q < 1 || n_seqs < 1 || max_len < 1)
+    return fail(SPD_EINVAL, "bad tree step arguments");
+  if ((reinterpret_cast<uintptr_t>(kv_cache) | reinterpret_cast<uintptr_t>(q_out)) & 15)
+    return fail(SPD_EINVAL, "kv_cache and q_out must be 16-byte aligned");
+  if (int rc = tree_attention_check(q_cu, n_q, ctx_len, n_seqs, tree_mask, mask_words, max_len)) return rc;
+  for (int i = 0; i < n_q; ++i)
+    if (pos[i] < 0) return fail(SPD_EINVAL, "negative rotary position of node %d", i);
+  const spd_model_cfg& c = m->cfg;
+  Carve cv(ws, ws_bytes);
+  PrefillBufs bf;
+  float* h;
+  TreeStep ts{q_cu, ctx_len, n_seqs, tree_mask, mask_words, max_len, q_out, lse_out, nullptr, 0};
+  carve_tree(c, n_q, cv, &bf, &h, &ts.ws, &ts.ws_bytes);
+  if (!cv.fits()) return fail(SPD_ENOSPC, "tree step workspace too small (%zu < %zu)", ws_bytes, cv.used);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  std::vector<int32_t> cu(n_q + 1);
+  for (int i = 0; i <= n_q; ++i) cu[i] = i;
+  static thread_local HostPlan P;
+  plan_init(P, c, cu.data(), n_q, n_q, bf.list_ints);
+  for (int b = 0; b < n_seqs; ++b)
+    for (int i = q_cu[b]; i < q_cu[b + 1]; ++i) {
+      P.hl[P.pos_off + i] = pos[i];
+      P.hl[P.kvrow_off + i] = b * max_len + ctx_len[b] + i - q_cu[b];
+    }
+  plan_layer(P, 0, nullptr, cu.data(), n_q, n_q);  // no sub-layer is skipped: one layer's lists serve all
+  P.tree = &ts;
+  int32_t* dl = bf.lists;
+  const size_t ints = c.n_layers > 1 ? P.ll[1].arows : P.end;
+  SPD_CUDA_TRY(cudaMemcpyAsync(dl, P.hl.data(), ints * sizeof(int32_t), cudaMemcpyHostToDevice, st));
+  GemmCleared cleared;
+  bf.gs.cleared = &cleared;
+  if (int rc = bf16_to_f32_run(x, h, size_t(n_q) * c.d_model, st)) return rc;
+  const size_t layer_rows = size_t(n_seqs) * max_len, row = 2 * size_t(c.n_kv_heads) * c.head_dim;
+  for (int l = 0; l < c.n_layers; ++l) {
+    const KVDest dest{kv_cache + l * layer_rows * row, int(layer_rows), true};
+    if (int rc = run_layer(m, l, P.ll[0], P, bf, dl, h, n_q, st, &dest)) return rc;
+  }
+  return run_head(m, P, bf, dl, h, n_q, logits, st);
 }
 
 

@@ -33,8 +33,9 @@ namespace cg = cooperative_groups;
 // the mantissa, spreads weights of any scale over enough counters that the additions do not queue, and the search ends as
 // soon as a digit's keys are all kept, after two digits as a rule. (Counting the keys that reach three candidates a round, two
 // bits at a time and without atomics, took 16 rounds of 1000 cycles, more than all the rest.)
-// A CTA is one chain of loads, passes and prefix sums, whatever its width: units of up to kSelSmall slots get 256 threads, so
-// that several of them share an SM.
+// A CTA is one chain of loads, passes and prefix sums: units of up to kSelSmall slots get 512 threads where all of them are
+// on the GPU at once (three an SM), 256 (six an SM) beyond. Whole calls, 256 / 512 / 1024 threads: 896 units of 1029 slots
+// 14.3 / 17.9 / 26.8 us, 256 units of 3008 (of which the moves take 25) 50.5 / 44.2 / 44.0.
 constexpr int kSelSmall = 4096;
 constexpr int kSelWide = 1024;      // threads for longer ones
 constexpr int kBins = 2048;
@@ -91,7 +92,7 @@ __device__ int block_before(int v, int* tmp, int* total) {
 
 // HD > 0: the kernel also moves the rows (a step's few), else evict_move_kernel does.
 template <int T, int HD>
-__global__ void __launch_bounds__(T, T == 256 ? 6 : 1)
+__global__ void __launch_bounds__(T, T == 256 ? 6 : T == 512 ? 3 : 1)
     evict_select_kernel(uint16_t* kv, const __grid_constant__ EvictArgs p, const __grid_constant__ EvictSeqs seqs, int per) {
   constexpr int kWarps = T / 32, kEach = kBins / T;  // counters a thread
   extern __shared__ uint32_t smem[];
@@ -280,6 +281,12 @@ __global__ void __launch_bounds__(T, T == 256 ? 6 : 1)
   }
 }
 
+using SelectKernel = void (*)(uint16_t*, EvictArgs, EvictSeqs, int);
+template <int T>
+SelectKernel pick_select(int move) {
+  return move == 128 ? evict_select_kernel<T, 128> : move == 64 ? evict_select_kernel<T, 64> : evict_select_kernel<T, 0>;
+}
+
 // The rows themselves: a warp a move, 16 bytes a lane (half a warp K, half V; HD = 64: a quarter each), four moves in
 // flight a warp.
 constexpr int kMoveWarps = 8, kMoveDepth = 4;
@@ -411,10 +418,11 @@ extern "C" int spd_cache_evict(uint16_t* kv_cache, int n_layers, int n_seqs, con
   per = (per + 3) & ~3;
   // moves that the selecting CTA makes itself: where a unit has few of them, the second launch costs more
   const bool fused = most_moves <= kFusedMoves, small = per <= kSelSmall;
-  const auto select = small ? (!fused ? evict_select_kernel<256, 0> : head_dim == 128 ? evict_select_kernel<256, 128>
-                                                                                      : evict_select_kernel<256, 64>)
-                            : (!fused ? evict_select_kernel<kSelWide, 0> : head_dim == 128 ? evict_select_kernel<kSelWide, 128>
-                                                                                           : evict_select_kernel<kSelWide, 64>);
+  const int threads = !small ? kSelWide : units * C > 3 * size_t(num_sms()) ? 256 : 512;
+  const int move = fused ? head_dim : 0;
+  const auto select = threads == 256   ? pick_select<256>(move)
+                      : threads == 512 ? pick_select<512>(move)
+                                       : pick_select<kSelWide>(move);
   if (!small) SPD_CUDA_TRY(cudaFuncSetAttribute(select, cudaFuncAttributeMaxDynamicSharedMemorySize, 8 * kBins + 4 * kSelMost));
   const size_t smem = longest ? 8 * size_t(kBins) + 4 * size_t(per) : 16;
   for (int s0 = 0; s0 < n_seqs; s0 += kMaxSeqs) {
@@ -431,7 +439,7 @@ extern "C" int spd_cache_evict(uint16_t* kv_cache, int n_layers, int n_seqs, con
     const int n = n_layers * p.launch_seqs * n_kv_heads;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(n * C);
-    cfg.blockDim = dim3(small ? 256 : kSelWide);
+    cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];

@@ -190,6 +190,14 @@ constexpr int kAttnTileQ = 128;  // queries per attention tile
 int attention_decode_run(const void* q, const void* kv, int ldkv, int v_off, void* o, int ldo,
                          const int4* tiles, int n_tiles, int n_heads, int n_kv_heads, int head_dim,
                          cudaStream_t stream, double ctx_sum);
+// Attention of drafted tokens over a layer's cache block (spd_tree_attention after its checks). ws: tree_attention_bytes
+// of scratch; status: word for device timeouts.
+size_t tree_attention_bytes(int n_q, int n_heads, int n_kv_heads, int head_dim);
+int tree_attention_check(const int32_t* q_cu, int n_q, const int32_t* ctx, int n_seqs, const uint32_t* mask, int words,
+                         int max_len);
+int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, int n_seqs, const uint32_t* mask, int words,
+                       const void* kv, int max_len, int n_heads, int n_kv_heads, int head_dim, void* o, float* lse, void* ws,
+                       size_t ws_bytes, int* status, cudaStream_t stream);
 int gemm_run(const GemmProblem& p, const GemmScratch& s, cudaStream_t stream);
 
 // ---- ASL-Skip online scores (Sec. 4.2.1, Eq. 6) -------------------------------------------------

@@ -681,7 +681,7 @@ TreePlan tree_plan(size_t n, Blocks blocks, Units units, Rows rows, int places, 
 
 }  // namespace
 
-size_t tree_attention_bytes(int n_q, int, int n_heads, int n_kv_heads, int head_dim) {
+size_t tree_attention_bytes(int n_q, int n_heads, int n_kv_heads, int head_dim) {
   const size_t rows = size_t(kMaxStates) * rows_of_part(tree_tile(n_heads, n_kv_heads), n_q);
   Carve cv(nullptr, ~size_t(0));
   cv.take<float>(rows * head_dim);
@@ -689,9 +689,23 @@ size_t tree_attention_bytes(int n_q, int, int n_heads, int n_kv_heads, int head_
   return cv.used;
 }
 
+int tree_attention_check(const int32_t* q_cu, int n_q, const int32_t* ctx, int n_seqs, const uint32_t* mask, int words,
+                         int max_len) {
+  if (q_cu[0] != 0 || q_cu[n_seqs] != n_q) return fail(SPD_EINVAL, "q_cu must run from 0 to n_q");
+  for (int b = 0; b < n_seqs; ++b) {
+    const int n = q_cu[b + 1] - q_cu[b];
+    if (n < 0) return fail(SPD_EINVAL, "q_cu decreases at sequence %d", b);
+    if (ctx[b] < 0 || ctx[b] > max_len - n)
+      return fail(SPD_EINVAL, "sequence %d: context and drafts exceed max_len", b);
+    if (mask && n > 32 * words) return fail(SPD_EINVAL, "sequence %d: %d nodes, %d mask words", b, n, words);
+  }
+  if ((long long)n_seqs * max_len > 0x7fffffffLL) return fail(SPD_EUNSUPPORTED, "more than 2^31 - 1 cache rows in a layer");
+  return SPD_OK;
+}
+
 int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, int n_seqs, const uint32_t* mask, int words,
                        const void* kv, int max_len, int n_heads, int n_kv_heads, int head_dim, void* o, float* lse, void* ws,
-                       size_t ws_bytes, cudaStream_t st) {
+                       size_t ws_bytes, int* status, cudaStream_t st) {
   const TreeTile t = tree_tile(n_heads, n_kv_heads);
   const int kvd = n_kv_heads * head_dim;
   CUtensorMap map;
@@ -716,7 +730,7 @@ int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, i
   const size_t rows = size_t(kMaxStates) * p.rows_part;
   p.part_o = cv.take<float>(rows * head_dim);
   p.part_ml = cv.take<float2>(rows);
-  p.status = cv.status();
+  p.status = status;
   p.budget = kWaitBudget;
   const auto kernel = head_dim == 128 ? tree_attn_kernel<128> : tree_attn_kernel<64>;
   const size_t smem = head_dim == 128 ? TreeSmem<128>::bytes : TreeSmem<64>::bytes;
@@ -832,7 +846,7 @@ extern "C" int spd_tree_mask(int n_seqs, const int32_t* q_cu, const int32_t* par
 extern "C" size_t spd_tree_attention_workspace_size(int n_q, int n_seqs, int n_heads, int n_kv_heads, int head_dim) {
   if (n_q < 1 || n_seqs < 1 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads || (head_dim != 64 && head_dim != 128))
     return 0;
-  return tree_attention_bytes(n_q, n_seqs, n_heads, n_kv_heads, head_dim);
+  return tree_attention_bytes(n_q, n_heads, n_kv_heads, head_dim);
 }
 
 extern "C" int spd_tree_attention(const uint16_t* q, int n_q, const int32_t* q_cu, const int32_t* ctx_len, int n_seqs,
@@ -845,17 +859,9 @@ extern "C" int spd_tree_attention(const uint16_t* q, int n_q, const int32_t* q_c
   if (head_dim != 64 && head_dim != 128) return fail(SPD_EUNSUPPORTED, "tree attention supports head_dim 64 and 128");
   if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(kv) | reinterpret_cast<uintptr_t>(o)) & 15)
     return fail(SPD_EINVAL, "q, kv and o must be 16-byte aligned");
-  if (q_cu[0] != 0 || q_cu[n_seqs] != n_q) return fail(SPD_EINVAL, "q_cu must run from 0 to n_q");
-  for (int b = 0; b < n_seqs; ++b) {
-    const int n = q_cu[b + 1] - q_cu[b];
-    if (n < 0) return fail(SPD_EINVAL, "q_cu decreases at sequence %d", b);
-    if (ctx_len[b] < 0 || ctx_len[b] > max_len - n)
-      return fail(SPD_EINVAL, "sequence %d: context and drafts exceed max_len", b);
-    if (tree_mask && n > 32 * mask_words) return fail(SPD_EINVAL, "sequence %d: %d nodes, %d mask words", b, n, mask_words);
-  }
-  if ((long long)n_seqs * max_len > 0x7fffffffLL) return fail(SPD_EUNSUPPORTED, "more than 2^31 - 1 cache rows in a layer");
-  const size_t need = tree_attention_bytes(n_q, n_seqs, n_heads, n_kv_heads, head_dim);
+  if (int rc = tree_attention_check(q_cu, n_q, ctx_len, n_seqs, tree_mask, mask_words, max_len)) return rc;
+  const size_t need = tree_attention_bytes(n_q, n_heads, n_kv_heads, head_dim);
   if (ws_bytes < need) return fail(SPD_ENOSPC, "tree attention workspace too small (%zu < %zu)", ws_bytes, need);
   return tree_attention_run(q, q_cu, ctx_len, n_seqs, tree_mask, mask_words, kv, max_len, n_heads, n_kv_heads, head_dim, o, lse,
-                            ws, ws_bytes, static_cast<cudaStream_t>(stream));
+                            ws, ws_bytes, static_cast<int*>(ws), static_cast<cudaStream_t>(stream));
 }
