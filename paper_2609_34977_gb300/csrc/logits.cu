@@ -26,6 +26,7 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kHeld = 5;                    // 16-byte pieces of its slice that a thread holds in registers
 constexpr int kBatch = kThreads * 4 * kHeld; // tokens a CTA holds at once
+constexpr int kPlaces = 608;                 // CTAs that clusters find room for at once
 constexpr int kMaxSlice = 51200;             // tokens a CTA holds counts for (200 KB)
 constexpr uint32_t kPrompt = 1u << 31;       // the token is in the prompt
 constexpr uint32_t kBiased = 1u << 30;       // the sequence has a bias for it
@@ -63,14 +64,19 @@ __device__ __forceinline__ unsigned long long order_key(float x, int token) {
   return (static_cast<unsigned long long>((u >> 31) ? ~u : u | 0x80000000u) << 32) | (0xffffffffu - uint32_t(token));
 }
 
-template <bool VEC>
+// Whether token i of value v goes before token j of value w.
+__device__ __forceinline__ bool goes_before(float v, int i, float w, int j) { return v > w || (v == w && i < j); }
+
+// CLUSTER: the row's CTAs are a cluster and find its best token together; else each offers its own to best[row], which
+// started as -1.
+template <bool VEC, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads, 5) logit_rules_kernel(const __grid_constant__ LogitRules p, int C) {
   extern __shared__ uint4 smem4[];
   __shared__ unsigned long long warp_best[16 * kWarps];  // of every warp of the row, in the cluster's first CTA
   uint32_t* word = reinterpret_cast<uint32_t*>(smem4);   // [slice]
   const int rank = blockIdx.x % C, row = blockIdx.x / C, tid = threadIdx.x, lane = tid & 31;
   const int t0 = rank * p.slice, n = max(0, min(p.slice, p.vocab - t0));  // this CTA's tokens
-  cluster_arrive();  // waited for before the first access to another CTA's shared memory
+  if (CLUSTER) cluster_arrive();  // waited for before the first access to another CTA's shared memory
   for (int i = tid; i < p.slice / 4; i += kThreads) smem4[i] = make_uint4(0u, 0u, 0u, 0u);
   pdl_launch_dependents();
   pdl_wait();
@@ -228,6 +234,28 @@ __global__ void __launch_bounds__(kThreads, 5) logit_rules_kernel(const __grid_c
       const unsigned long long y = __shfl_xor_sync(0xffffffffu, k, off);
       k = y > k ? y : k;
     }
+    if constexpr (!CLUSTER) {
+      // offers in any order end with the same token: one is replaced only by a token that goes before it, whose own
+      // value is in `out` (written and fenced before its offer)
+      if (lane == 0) warp_best[tid >> 5] = k;
+      __syncthreads();
+      if (tid == 0) {
+        for (int w = 1; w < kWarps; ++w) k = warp_best[w] > k ? warp_best[w] : k;
+        if (k) {
+          const int id = int32_t(0xffffffffu - uint32_t(k));
+          volatile float* row_out = p.out + size_t(row) * p.ld_out;
+          const float v = row_out[id];
+          __threadfence();
+          int cur = *(volatile int32_t*)(p.best + row);
+          while (cur < 0 || goes_before(v, id, row_out[cur], cur)) {
+            const int was = atomicCAS(p.best + row, cur, id);
+            if (was == cur) break;
+            cur = was;
+          }
+        }
+      }
+      return;
+    }
     cluster_wait();  // every CTA of the row has started
     if (lane == 0) {
       const uint32_t to = dsmem_addr(&warp_best[rank * kWarps + (tid >> 5)], 0);
@@ -248,6 +276,13 @@ __global__ void __launch_bounds__(kThreads, 5) logit_rules_kernel(const __grid_c
       if (tid == 0) p.best[row] = k ? int32_t(0xffffffffu - uint32_t(k)) : -1;
     }
   }
+}
+
+__global__ void no_best_kernel(int32_t* best, int n) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int i = blockIdx.x * kThreads + threadIdx.x;
+  if (i < n) best[i] = -1;
 }
 
 }  // namespace
@@ -312,15 +347,22 @@ extern "C" int spd_logits_process(const float* logits, int n_rows, int vocab, in
   p.rule = r->rule;
   const bool vec = vocab % 4 == 0 && ld % 4 == 0 && ld_out % 4 == 0 &&
                    ((reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(out)) & 15) == 0;
-  auto kern = vec ? logit_rules_kernel<true> : logit_rules_kernel<false>;
+  // A cluster needs all of its places at once. Where the rows do not fit on the GPU together, CTAs on their own
+  // fill it better, at the price of a launch that clears `best`.
+  const bool apart = C > 1 && n_rows > kPlaces / C;
+  auto kern = vec ? (apart ? logit_rules_kernel<true, false> : logit_rules_kernel<true, true>)
+                  : (apart ? logit_rules_kernel<false, false> : logit_rules_kernel<false, true>);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (apart && best)
+    SPD_CUDA_TRY(launch_pdl(no_best_kernel, dim3((n_rows + kThreads - 1) / kThreads), dim3(kThreads), 0, st, best, n_rows));
   const size_t smem = size_t(p.slice) * 4;
   SPD_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSlice * 4));
-  if (C > 8) SPD_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+  if (C > 8 && !apart) SPD_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(n_rows * C);
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
-  cfg.stream = static_cast<cudaStream_t>(stream);
+  cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -329,7 +371,7 @@ extern "C" int spd_logits_process(const float* logits, int n_rows, int vocab, in
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 2;
+  cfg.numAttrs = apart ? 1 : 2;
   const double by = 8.0 * n_rows * vocab + 4.0 * (double(p.n_hist) + p.n_path + 2.0 * p.n_bias);
   const int slot = trace_begin(cfg.stream);
   SPD_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, p, C));
