@@ -207,6 +207,12 @@ _DT = {"f32": "float32", "bf16": "bfloat16", "i32": "int32", "u8": "uint8", "i8"
 _torch_dt = {}  # element type names -> torch dtypes, once torch has been imported
 
 
+def _load_dtypes():
+    import torch
+    _torch_dt.update({k: getattr(torch, v) for k, v in _DT.items()})
+    return _torch_dt
+
+
 def _dev(t, dt, n, name, optional=False):
     """Device pointer of argument `name` after checking it: a contiguous CUDA tensor of element
     type dt ('f32', 'bf16', 'i32', 'u8', 'i8') holding at least n elements (the elements the call
@@ -219,10 +225,7 @@ def _dev(t, dt, n, name, optional=False):
     if not getattr(t, "is_cuda", False):
         raise TypeError(f"{name}: device arguments of libspider must be CUDA tensors, got "
                         f"{type(t).__name__} on {getattr(t, 'device', 'the host')}")
-    if not _torch_dt:
-        import torch
-        _torch_dt.update({k: getattr(torch, v) for k, v in _DT.items()})
-    if t.dtype is not _torch_dt[dt]:
+    if t.dtype is not (_torch_dt or _load_dtypes())[dt]:
         raise ValueError(f"{name}: expected {_DT[dt]}, got {t.dtype}")
     if t.numel() < n:
         raise ValueError(f"{name}: {t.numel()} elements, the call touches {int(n)}")
@@ -673,20 +676,24 @@ def spd_logits_process(logits, out, best=None, *, seq_of=None, hist=None, hist_c
     n, v = logits.shape
     if tuple(out.shape) != (n, v):
         raise ValueError(f"out: shape {tuple(out.shape)}, logits are {(n, v)}")
-    per_seq = [t for t in (gen_start, repetition, frequency, presence) if t is not None]
-    starts = [t for t in (hist_cu, bias_cu) if t is not None]
-    B = min([t.numel() for t in per_seq] + [t.numel() - 1 for t in starts], default=n if seq_of is None else 0)
-    cnt = lambda t: 0 if t is None else t.numel()  # noqa: E731
-    n_bias = cnt(bias) if bias_id is None else min(cnt(bias), cnt(bias_id))
+    # the number of sequences is what the lists that come with one entry a sequence hold
+    B = n if seq_of is None else 0
+    for t, more in ((hist_cu, 1), (gen_start, 0), (repetition, 0), (frequency, 0), (presence, 0), (bias_cu, 1)):
+        if t is not None:
+            B = t.numel() - more
+            break
+    n_hist, n_path = 0 if hist is None else hist.numel(), 0 if path is None else path.numel()
+    n_bias = 0 if bias is None else bias.numel()
     words = (v + 31) // 32
     n_rules = 0 if allow is None else allow.numel() // words
-    r = LogitsRules(_dev(seq_of, "i32", n, "seq_of", True), max(B, 0), _dev(hist, "i32", 0, "hist", True),
-                    _dev(hist_cu, "i32", B + 1, "hist_cu", True), _dev(gen_start, "i32", B, "gen_start", True), cnt(hist),
-                    _dev(path, "i32", 0, "path", True), _dev(path_cu, "i32", n + 1, "path_cu", True), cnt(path),
-                    _dev(repetition, "f32", B, "repetition", True), _dev(frequency, "f32", B, "frequency", True),
-                    _dev(presence, "f32", B, "presence", True), _dev(bias_cu, "i32", B + 1, "bias_cu", True),
-                    _dev(bias_id, "i32", n_bias, "bias_id", True), _dev(bias, "f32", n_bias, "bias", True), n_bias,
-                    _dev(allow, "i32", n_rules * words, "allow", True), n_rules, _dev(rule, "i32", n, "rule", True))
+    dev = lambda t, dt, k, name: None if t is None else _dev(t, dt, k, name)  # noqa: E731
+    r = LogitsRules(dev(seq_of, "i32", n, "seq_of"), B, dev(hist, "i32", 0, "hist"), dev(hist_cu, "i32", B + 1, "hist_cu"),
+                    dev(gen_start, "i32", B, "gen_start"), n_hist, dev(path, "i32", 0, "path"),
+                    dev(path_cu, "i32", n + 1, "path_cu"), n_path, dev(repetition, "f32", B, "repetition"),
+                    dev(frequency, "f32", B, "frequency"), dev(presence, "f32", B, "presence"),
+                    dev(bias_cu, "i32", B + 1, "bias_cu"), dev(bias_id, "i32", n_bias, "bias_id"),
+                    dev(bias, "f32", n_bias, "bias"), n_bias, dev(allow, "i32", n_rules * words, "allow"), n_rules,
+                    dev(rule, "i32", n, "rule"))
     _check(lib().spd_logits_process(zp, n, v, ld, C.byref(r), op, ldo, _dev(best, "i32", n, "best", True),
                                     _stream(stream)))
 

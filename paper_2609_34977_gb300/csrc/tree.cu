@@ -527,13 +527,14 @@ template <int HD>
 __global__ void __launch_bounds__(kMergeWarps * 32)
     tree_merge_kernel(const __grid_constant__ TreeArgs p, const __grid_constant__ TreeSeqs sq, int W) {
   constexpr int D = HD / 32;  // dims a lane
-  __shared__ float wl[kMergeWarps], wo[kMergeWarps][HD];
+  __shared__ float2 wml[kMergeWarps];
+  __shared__ float wo[kMergeWarps][HD];
   pdl_launch_dependents();
   pdl_wait();
   const int e = blockIdx.y, n = sq.nodes[e], parts = sq.groups[e];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp % W;
   const int row = blockIdx.x * (kMergeWarps / W) + warp / W;
-  const bool have = parts > 1 && row < n * p.n_heads;
+  const bool have = row < n * p.n_heads;
   float m = -INFINITY, l = 0.0f, o[D];
 #pragma unroll
   for (int x = 0; x < D; ++x) o[x] = 0.0f;
@@ -545,9 +546,6 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
     const int r = node % p.nodes_tile * p.chunk + hg % p.chunk;
     const size_t first = (size_t(sq.part0[e]) + size_t(hk) * parts * tiles + tile) * p.rows_part + r;
     const size_t step = size_t(tiles) * p.rows_part;
-    for (int s = lane; s < parts; s += 32) m = fmaxf(m, p.part_ml[first + s * step].x);
-#pragma unroll
-    for (int off = 16; off; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
     const int s1 = (w + 1) * parts / W;
     for (int s0 = w * parts / W; s0 < s1; s0 += 8) {
       float2 ml[8];
@@ -555,7 +553,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const size_t at = first + min(s0 + u, s1 - 1) * step;
-        ml[u] = p.part_ml[at];
+        ml[u] = s0 + u < s1 ? p.part_ml[at] : make_float2(-INFINITY, 0.0f);
         const float* po = p.part_o + at * HD + D * lane;
         if constexpr (D == 4) {
           const float4 f = *reinterpret_cast<const float4*>(po);
@@ -565,9 +563,18 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
           v[u][0] = f.x, v[u][1] = f.y;
         }
       }
+      float top = m;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) top = fmaxf(top, ml[u].x);
+      if (top == -INFINITY) continue;  // nothing seen so far
+      const float keep = exp2f(m - top);
+      m = top;
+      l *= keep;
+#pragma unroll
+      for (int x = 0; x < D; ++x) o[x] *= keep;
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        if (s0 + u >= s1 || ml[u].x == -INFINITY) continue;  // a part in which the row sees nothing
+        if (ml[u].x == -INFINITY) continue;  // a part in which the row sees nothing
         const float f = exp2f(ml[u].x - m);
         l = fmaf(ml[u].y, f, l);
 #pragma unroll
@@ -576,15 +583,22 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
     }
   }
   if (W > 1) {
-    if (lane == 0) wl[warp] = l;
+    if (lane == 0) wml[warp] = make_float2(m, l);
 #pragma unroll
     for (int x = 0; x < D; ++x) wo[warp][D * lane + x] = o[x];
     __syncthreads();
     if (w > 0) return;
-    for (int k = 1; k < W; ++k) {
-      l += wl[warp + k];
+    for (int k = 1; k < W; ++k) m = fmaxf(m, wml[warp + k].x);
+    l = 0.0f;
 #pragma unroll
-      for (int x = 0; x < D; ++x) o[x] += wo[warp + k][D * lane + x];
+    for (int x = 0; x < D; ++x) o[x] = 0.0f;
+    for (int k = 0; k < W; ++k) {
+      const float2 ml = wml[warp + k];
+      if (ml.x == -INFINITY) continue;
+      const float f = exp2f(ml.x - m);
+      l = fmaf(ml.y, f, l);
+#pragma unroll
+      for (int x = 0; x < D; ++x) o[x] = fmaf(wo[warp + k][D * lane + x], f, o[x]);
     }
   }
   if (!have) return;
@@ -762,7 +776,7 @@ int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, i
     const int C = plan.cluster;
     TreeSeqs sq{};
     long long items = 0;
-    int states = 0, most = 0, most_groups = 0;
+    int states = 0, most = 0, most_groups = 0, split = 0;  // split: sequences of several groups, the first ones
     for (int b : order) {
       const int e = sq.n++;
       const int k = plan.groups(blocks(b));
@@ -774,6 +788,7 @@ int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, i
       sq.groups[e] = int16_t(k);
       sq.part0[e] = states;
       if (k > 1) {
+        ++split;
         states += int(units(b)) * k;
         most = std::max(most, count(b));
         most_groups = std::max(most_groups, k);
@@ -807,7 +822,7 @@ int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, i
       int W = 1;
       while (W < kMergeWarps && most_groups > 8 * W) W *= 2;
       SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? tree_merge_kernel<128> : tree_merge_kernel<64>,
-                              dim3((most * n_heads * W + kMergeWarps - 1) / kMergeWarps, sq.n), dim3(kMergeWarps * 32), 0, st, p,
+                              dim3((most * n_heads * W + kMergeWarps - 1) / kMergeWarps, split), dim3(kMergeWarps * 32), 0, st, p,
                               sq, W));
     }
     trace_end(slot, st, TR_ATTN, fl, by);

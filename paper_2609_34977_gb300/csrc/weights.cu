@@ -323,7 +323,20 @@ extern "C" int spd_cache_weights(const uint16_t* q, const float* lse, int n_q, c
     double keys = 0.0, pairs = 0.0;
     long long work = 0;
     for (int b = s0; b < s0 + sq.n; ++b) work += (long long)((lens[b] + kTile - 1) / kTile) * n_kv_heads * n_layers;
-    p.share = int(std::max<long long>(4, (work + 4 * kPlaces - 1) / (4 * kPlaces)));
+    // blocks an item: few and long ones, since a CTA's start (Q tile, normalisers, first block) costs several blocks'
+    // time: one wave of CTAs where the units allow it, else about two. 8 layers of 32 heads, 24 blocks each, with 6 / 8 / 12 /
+    // 24 blocks an item: 42.0 / 39.7 / 38.3 / 34.5 us; 448 units of 8 to 32 blocks with 4 / 7 / 12 / 16 / 24: 50.4 / 46.2 / 44.4 /
+    // 47.8 / 45.3.
+    auto wave = [&](long long share) {
+      long long k = 0;
+      for (int b = s0; b < s0 + sq.n; ++b) k += ((lens[b] + kTile - 1) / kTile + share - 1) / share;
+      return k * n_kv_heads * n_layers;
+    };
+    const bool fits = wave(1 << 24) <= kPlaces;  // the units do, whole
+    const int waves = fits ? 1 : 2;
+    long long share = std::max<long long>(2, (work + waves * kPlaces - 1) / (waves * kPlaces));
+    while (fits && wave(share) > kPlaces) share += (share + 15) / 16;
+    p.share = int(share);
     long long items = 0;
     for (int i = 0; i < sq.n; ++i) {
       const int b = s0 + i, blocks = (lens[b] + kTile - 1) / kTile;
