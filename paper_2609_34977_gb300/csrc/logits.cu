@@ -24,9 +24,10 @@ namespace spd {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kHeld = 5;                    // 16-byte pieces of its slice that a thread holds in registers
-constexpr int kBatch = kThreads * 4 * kHeld; // tokens a CTA holds at once
-constexpr int kPlaces = 608;                 // CTAs that clusters find room for at once
+constexpr int kHeld = 20;                   // tokens of its slice that a thread holds in registers
+constexpr int kBatch = kThreads * kHeld;     // tokens a CTA holds at once
+constexpr int kAhead = 2;                    // loads of four tokens of the history that go ahead of the logits
+constexpr int kPlaces = 384;                 // CTAs of rows that clusters still serve as well as CTAs on their own
 constexpr int kMaxSlice = 51200;             // tokens a CTA holds counts for (200 KB)
 constexpr uint32_t kPrompt = 1u << 31;       // the token is in the prompt
 constexpr uint32_t kBiased = 1u << 30;       // the sequence has a bias for it
@@ -41,6 +42,7 @@ struct LogitRules {
   int n_seqs;
   const int32_t *hist, *hist_cu, *gen_start;
   int n_hist;
+  bool hist4;  // hist is 16-byte aligned
   const int32_t *path, *path_cu;
   int n_path;
   const float *rep, *freq, *pres;
@@ -69,8 +71,8 @@ __device__ __forceinline__ bool goes_before(float v, int i, float w, int j) { re
 
 // CLUSTER: the row's CTAs are a cluster and find its best token together; else each offers its own to best[row], which
 // started as -1.
-template <bool VEC, bool CLUSTER>
-__global__ void __launch_bounds__(kThreads, 5) logit_rules_kernel(const __grid_constant__ LogitRules p, int C) {
+template <int W, bool CLUSTER>
+__global__ void __launch_bounds__(kThreads, 4) logit_rules_kernel(const __grid_constant__ LogitRules p, int C) {
   extern __shared__ uint4 smem4[];
   __shared__ unsigned long long warp_best[16 * kWarps];  // of every warp of the row, in the cluster's first CTA
   uint32_t* word = reinterpret_cast<uint32_t*>(smem4);   // [slice]
@@ -82,14 +84,19 @@ __global__ void __launch_bounds__(kThreads, 5) logit_rules_kernel(const __grid_c
   pdl_wait();
   const float* z = p.z + size_t(row) * p.ld_in + t0;
   float* out = p.out + size_t(row) * p.ld_out + t0;
-  // the slice's first batch is on its way while the history is counted
-  float4 x[kHeld];
+  // W = 4: 16-byte pieces, where the rows are aligned for them; 1: single tokens. The slice's first batch is on its way
+  // while the history is counted.
+  float x[kHeld];
   auto load = [&](int base) {
-    if constexpr (VEC) {
 #pragma unroll
-      for (int k = 0; k < kHeld; ++k) {
-        const int i = base + 4 * (k * kThreads + tid);
-        if (i < n) x[k] = __ldcs(reinterpret_cast<const float4*>(z + i));
+    for (int k = 0; k < kHeld / W; ++k) {
+      const int i = base + W * (k * kThreads + tid);
+      if (i >= n) continue;
+      if constexpr (W == 4) {
+        const float4 v = __ldcs(reinterpret_cast<const float4*>(z + i));
+        x[4 * k] = v.x, x[4 * k + 1] = v.y, x[4 * k + 2] = v.z, x[4 * k + 3] = v.w;
+      } else {
+        x[k] = __ldcs(z + i);
       }
     }
   };
@@ -103,9 +110,21 @@ __global__ void __launch_bounds__(kThreads, 5) logit_rules_kernel(const __grid_c
   const uint32_t* allow = rule >= 0 && rule < p.n_rules ? p.allow + size_t(rule) * p.words + t0 / 32 : nullptr;
   const float rep = has_seq && p.rep ? p.rep[seq] : 1.0f;
   const float freq = has_seq && p.freq ? p.freq[seq] : 0.0f, pres = has_seq && p.pres ? p.pres[seq] : 0.0f;
-  int first[8];  // of the history, ahead of the logits
+  // four tokens of the history a load, from the 16-byte boundary before its first (those outside it are passed over)
+  auto tokens4 = [&](int i) -> int4 {
+    if (p.hist4 && i + 3 < p.n_hist) return *reinterpret_cast<const int4*>(p.hist + i);
+    int4 t = make_int4(-1, -1, -1, -1);
+    if (i < p.n_hist) t.x = p.hist[i];
+    if (i + 1 < p.n_hist) t.y = p.hist[i + 1];
+    if (i + 2 < p.n_hist) t.z = p.hist[i + 2];
+    if (i + 3 < p.n_hist) t.w = p.hist[i + 3];
+    return t;
+  };
+  const int h0 = (hl.x & ~3) + 4 * tid;
+  int4 first[kAhead];  // ahead of the logits
 #pragma unroll
-  for (int u = 0; u < 8; ++u) first[u] = hl.x + tid + u * kThreads < hl.y ? p.hist[hl.x + tid + u * kThreads] : -1;
+  for (int u = 0; u < kAhead; ++u)
+    first[u] = h0 + u * 4 * kThreads < hl.y ? tokens4(h0 + u * 4 * kThreads) : make_int4(-1, -1, -1, -1);
   // the thread's first entry of the bias list, and the logit that it concerns
   const bool has_bias = bl.x + tid < bl.y;
   const int b_id = has_bias ? p.bias_id[bl.x + tid] : -1;
@@ -117,14 +136,26 @@ __global__ void __launch_bounds__(kThreads, 5) logit_rules_kernel(const __grid_c
   // Placeholders of an image lie outside the vocabulary and so outside every slice. (unsigned: negatives too)
   auto count = [&](int token, int i) {
     const uint32_t t = uint32_t(token) - uint32_t(t0);
-    if (token < 0 || t >= uint32_t(n)) return;
+    if (token < 0 || t >= uint32_t(n) || i < hl.x || i >= hl.y) return;
     if (i >= gen) atomicAdd(&word[t], 1u);
     else if (!(word[t] & kPrompt)) atomicOr(&word[t], kPrompt);  // a prompt may repeat one token throughout
   };
+  auto count4 = [&](const int4& t, int i) {
+    count(t.x, i);
+    count(t.y, i + 1);
+    count(t.z, i + 2);
+    count(t.w, i + 3);
+  };
 #pragma unroll
-  for (int u = 0; u < 8; ++u) count(first[u], hl.x + tid + u * kThreads);
-#pragma unroll 8
-  for (int i = hl.x + tid + 8 * kThreads; i < hl.y; i += kThreads) count(p.hist[i], i);
+  for (int u = 0; u < kAhead; ++u) count4(first[u], h0 + u * 4 * kThreads);
+  for (int i = h0 + kAhead * 4 * kThreads; i < hl.y; i += 16 * kThreads) {
+    int4 t[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      t[u] = i + u * 4 * kThreads < hl.y ? tokens4(i + u * 4 * kThreads) : make_int4(-1, -1, -1, -1);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) count4(t[u], i + u * 4 * kThreads);
+  }
   for (int i = pl.x + tid; i < pl.y; i += kThreads) {
     const uint32_t t = uint32_t(p.path[i] - t0);
     if (t < uint32_t(n)) atomicAdd(&word[t], 1u);
@@ -172,55 +203,51 @@ __global__ void __launch_bounds__(kThreads, 5) logit_rules_kernel(const __grid_c
     const uint32_t t = uint32_t(id - t0);
     if (t < uint32_t(n)) biased(i, id, t, z[t], p.bias[i]);
   }
-  if constexpr (VEC) {
-    for (int base = 0; base < n; base += kBatch) {
-      if (base > 0) load(base);
+  for (int base = 0; base < n; base += kBatch) {
+    if (base > 0) load(base);
 #pragma unroll
-      for (int k = 0; k < kHeld; ++k) {
-        const int i = base + 4 * (k * kThreads + tid);
-        if (i < n) {
-          const uint4 w = smem4[i / 4];
-          const uint32_t a = allow ? allow[i / 32] >> (i % 32) : 15u, any = w.x | w.y | w.z | w.w;
-          float4 v = x[k];
-          if (any) {
-            v.x = penalised(v.x, w.x);
-            v.y = penalised(v.y, w.y);
-            v.z = penalised(v.z, w.z);
-            v.w = penalised(v.w, w.w);
-          }
-          if (!(a & 1u)) v.x = -INFINITY;
-          if (!(a & 2u)) v.y = -INFINITY;
-          if (!(a & 4u)) v.z = -INFINITY;
-          if (!(a & 8u)) v.w = -INFINITY;
-          if (any & kBiased) {  // the biased ones are left to the threads of the bias list
-            const float e[4] = {v.x, v.y, v.z, v.w};
-            const uint32_t f[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-              if (!(f[c] & kBiased)) {
-                out[i + c] = e[c];
-                take(e[c], i + c);
-              }
-          } else {
-            *reinterpret_cast<float4*>(out + i) = v;
-            if (fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)) > best) {
-              take(v.x, i);
-              take(v.y, i + 1);
-              take(v.z, i + 2);
-              take(v.w, i + 3);
-            }
-          }
-        }
+    for (int k = 0; k < kHeld / W; ++k) {
+      const int i = base + W * (k * kThreads + tid);
+      if (i >= n) continue;
+      uint32_t w[W];
+      if constexpr (W == 4) {
+        const uint4 q = smem4[i / 4];
+        w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+      } else {
+        w[0] = word[i];
       }
-    }
-  } else {
-    for (int i = tid; i < n; i += kThreads) {
-      const uint32_t w = word[i];
-      if (w & kBiased) continue;
-      float v = penalised(z[i], w);
-      if (allow && !((allow[i / 32] >> (i % 32)) & 1u)) v = -INFINITY;
-      out[i] = v;
-      take(v, i);
+      const uint32_t a = allow ? allow[i / 32] >> (i % 32) : 15u;
+      float v[W];
+      uint32_t any = 0;
+#pragma unroll
+      for (int c = 0; c < W; ++c) {
+        v[c] = x[W * k + c];
+        any |= w[c];
+      }
+      if (any) {
+#pragma unroll
+        for (int c = 0; c < W; ++c) v[c] = penalised(v[c], w[c]);
+      }
+#pragma unroll
+      for (int c = 0; c < W; ++c)
+        if (!((a >> c) & 1u)) v[c] = -INFINITY;
+      if (any & kBiased) {  // the biased ones are done
+#pragma unroll
+        for (int c = 0; c < W; ++c)
+          if (!(w[c] & kBiased)) {
+            out[i + c] = v[c];
+            take(v[c], i + c);
+          }
+      } else if constexpr (W == 4) {
+        *reinterpret_cast<float4*>(out + i) = make_float4(v[0], v[1], v[2], v[3]);
+        if (fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) > best) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) take(v[c], i + c);
+        }
+      } else {
+        out[i] = v[0];
+        take(v[0], i);
+      }
     }
   }
   if (p.best) {
@@ -331,6 +358,7 @@ extern "C" int spd_logits_process(const float* logits, int n_rows, int vocab, in
   p.hist_cu = r->hist_cu;
   p.gen_start = r->gen_start;
   p.n_hist = r->n_hist;
+  p.hist4 = (reinterpret_cast<uintptr_t>(r->hist) & 15) == 0;
   p.path = r->n_path > 0 ? r->path : nullptr;
   p.path_cu = r->path_cu;
   p.n_path = r->n_path;
@@ -350,8 +378,8 @@ extern "C" int spd_logits_process(const float* logits, int n_rows, int vocab, in
   // A cluster needs all of its places at once. Where the rows do not fit on the GPU together, CTAs on their own
   // fill it better, at the price of a launch that clears `best`.
   const bool apart = C > 1 && n_rows > kPlaces / C;
-  auto kern = vec ? (apart ? logit_rules_kernel<true, false> : logit_rules_kernel<true, true>)
-                  : (apart ? logit_rules_kernel<false, false> : logit_rules_kernel<false, true>);
+  auto kern = vec ? (apart ? logit_rules_kernel<4, false> : logit_rules_kernel<4, true>)
+                  : (apart ? logit_rules_kernel<1, false> : logit_rules_kernel<1, true>);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (apart && best)
     SPD_CUDA_TRY(launch_pdl(no_best_kernel, dim3((n_rows + kThreads - 1) / kThreads), dim3(kThreads), 0, st, best, n_rows));
