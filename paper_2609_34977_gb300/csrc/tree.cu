@@ -634,61 +634,66 @@ int rows_of_part(const TreeTile& t, int n_q) { return std::min(t.nodes, n_q) * t
 // 33.8 / 30.0; eight of 48 nodes, 32 K/V heads, cluster 1 / 2 / 4: 39 / 46 / 59 and 35.3 / 43.4 / 59.0.
 constexpr double kCtaTime = 6.0, kClusterTime = 1.0, kMergeTime = 4.0, kMergeRow = 0.25e-3, kWaveFactor = 1.3;
 constexpr int kMaxStates = kItems;  // states in memory of a launch: those of plans that fit on the GPU at once
-struct TreePlan {
-  int cluster = 1;
-  long long share = 1 << 30;
-  int groups(int blocks) const { return int(std::max<long long>(1, (blocks + share * cluster - 1) / (share * cluster))); }
+struct TreeWork {  // a sequence of the launch: key blocks, (tile, K/V head) pairs, (node, head) rows
+  int seq, blocks;
+  long long units, rows;
 };
-// blocks(i), units(i), rows(i): key blocks, (tile, K/V head) pairs and (node, head) rows of sequence i, the longest first;
-// places: CTAs the GPU holds at once.
-template <typename Blocks, typename Units, typename Rows>
-TreePlan tree_plan(size_t n, Blocks blocks, Units units, Rows rows, int places, int head_dim) {
+struct TreePlan {
+  int cluster = 1, share = 1 << 24;
+  int groups(int blocks) const { return std::max(1, (blocks + share * cluster - 1) / (share * cluster)); }
+};
+// work: the longest first; places: CTAs the GPU holds at once.
+TreePlan tree_plan(const std::vector<TreeWork>& work, int places, int head_dim) {
   const double alone = head_dim == 128 ? 1.2 : 0.93, pair = head_dim == 128 ? 1.45 : 0.93;
   TreePlan best;
   double least = 1e30;
-  for (int k = 0; 1 << k <= kMaxCluster; ++k) {
+  long long units = 0;
+  double blocks_all = 0.0;
+  for (const TreeWork& w : work) {
+    units += w.units;
+    blocks_all += double(w.units) * w.blocks;
+  }
+  for (int c = 1; c <= kMaxCluster; c *= 2) {
     // CTAs that fit in clusters: 304, 304, 288 and 256 of the 304 places of 152 SMs (the largest launches that ran as one wave)
-    const int c = 1 << k, room = std::max(c, places - (c == 4 ? places / 19 : c == 8 ? 3 * places / 19 : 0));
-    auto ctas = [&](const TreePlan& t) {
-      long long all = 0;
-      for (size_t i = 0; i < n; ++i) all += units(i) * t.groups(blocks(i)) * c;
-      return all;
-    };
-    auto weigh = [&](const TreePlan& t) {
-      double all = 0.0, blocks_all = 0.0, longest = 0.0, merge = 0.0;
-      long long states = 0;
-      for (size_t i = 0; i < n; ++i) {
-        const int g = t.groups(blocks(i));
-        all += double(units(i)) * g * c;
-        blocks_all += double(units(i)) * blocks(i);
-        longest = std::max(longest, double(blocks(i)) / (g * c));
+    const int room = std::max(c, places - (c == 4 ? places / 19 : c == 8 ? 3 * places / 19 : 0));
+    // the estimate of a plan, its CTAs in *ctas
+    auto weigh = [&](const TreePlan& t, long long* ctas) {
+      double longest = 0.0, merge = 0.0;
+      long long all = 0, states = 0;
+      for (const TreeWork& w : work) {
+        const int g = t.groups(w.blocks);
+        all += w.units * g * c;
+        longest = std::max(longest, double(w.blocks) / (g * c));
         if (g > 1) {
-          states += units(i) * g;
-          merge += kMergeRow * double(rows(i)) * g;
+          states += w.units * g;
+          merge += kMergeRow * double(w.rows) * g;
         }
       }
-      if (states > kMaxStates) return;
-      const double block = 2 * all > room ? pair : alone;
-      double cost = kCtaTime + longest * block;
+      *ctas = all;
+      double cost = kCtaTime + longest * (2 * all > room ? pair : alone);
       if (all > room) cost = std::max(cost, kCtaTime + kWaveFactor * (all * kCtaTime + blocks_all * pair) / room);
       cost += (c > 1 ? kClusterTime : 0.0) + (states ? kMergeTime + merge : 0.0);
-      if (cost < least) {
+      if (cost < least && states <= kMaxStates) {
         least = cost;
         best = t;
       }
     };
-    TreePlan whole;  // one group
-    whole.cluster = c;
-    weigh(whole);
-    if (ctas(whole) >= room) continue;
-    TreePlan t = whole;  // the smallest share whose CTAs all fit at once
-    long long lo = 0, hi = (blocks(0) + c - 1) / c;  // (lo does not, hi does)
-    while (hi - lo > 1) {
-      t.share = (lo + hi) / 2;
-      (ctas(t) > room ? lo : hi) = t.share;
+    long long ctas;
+    TreePlan t;  // one group a sequence
+    t.cluster = c;
+    weigh(t, &ctas);
+    if (ctas >= room || work[0].blocks <= c) continue;
+    // more groups while all CTAs fit: the share can be no smaller than an even one
+    int share = std::max(1, int(blocks_all / room));
+    for (const int whole = (work[0].blocks + c - 1) / c; share < whole; share += share / 16 + 1) {
+      t.share = share;
+      const double before = least;
+      const TreePlan was = best;
+      weigh(t, &ctas);
+      if (ctas <= room) break;
+      least = before;
+      best = was;
     }
-    t.share = hi;
-    weigh(t);
   }
   return best;
 }
@@ -754,46 +759,44 @@ int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, i
     attr[head_dim == 128] = true;
   }
   const int places = std::min(kItems, 2 * num_sms());
-  std::vector<int> order;
+  std::vector<TreeWork> work;
+  work.reserve(std::min(n_seqs, kMaxSeqs));
   for (int s0 = 0; s0 < n_seqs; s0 += kMaxSeqs) {
     const int m = std::min(kMaxSeqs, n_seqs - s0);
-    order.clear();
+    work.clear();
     double pairs = 0.0, keys = 0.0;
-    auto count = [&](int b) { return q_cu[b + 1] - q_cu[b]; };
-    auto blocks = [&](int b) { return (ctx[b] + count(b) + kTK - 1) / kTK; };
-    auto units = [&](int b) { return (long long)((count(b) + t.nodes - 1) / t.nodes) * t.chunks * n_kv_heads; };
     for (int b = s0; b < s0 + m; ++b) {
-      if (count(b) == 0) continue;
-      order.push_back(b);
-      keys += ctx[b] + count(b);
-      pairs += double(count(b)) * (ctx[b] + count(b));
+      const int n = q_cu[b + 1] - q_cu[b];
+      if (n == 0) continue;
+      work.push_back({b, (ctx[b] + n + kTK - 1) / kTK, (long long)((n + t.nodes - 1) / t.nodes) * t.chunks * n_kv_heads,
+                      (long long)n * n_heads});
+      keys += ctx[b] + n;
+      pairs += double(n) * (ctx[b] + n);
     }
-    if (order.empty()) continue;
-    std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return blocks(x) > blocks(y); });
-    const TreePlan plan = tree_plan(order.size(), [&](size_t i) { return blocks(order[i]); },
-                                    [&](size_t i) { return units(order[i]); },
-                                    [&](size_t i) { return (long long)count(order[i]) * n_heads; }, places, head_dim);
+    if (work.empty()) continue;
+    std::stable_sort(work.begin(), work.end(), [](const TreeWork& x, const TreeWork& y) { return x.blocks > y.blocks; });
+    const TreePlan plan = tree_plan(work, places, head_dim);
     const int C = plan.cluster;
     TreeSeqs sq{};
     long long items = 0;
     int states = 0, most = 0, most_groups = 0, split = 0;  // split: sequences of several groups, the first ones
-    for (int b : order) {
-      const int e = sq.n++;
-      const int k = plan.groups(blocks(b));
+    for (const TreeWork& w : work) {
+      const int e = sq.n++, n = q_cu[w.seq + 1] - q_cu[w.seq];
+      const int k = plan.groups(w.blocks);
       sq.item0[e] = int(items);
-      sq.q0[e] = q_cu[b];
-      sq.nodes[e] = count(b);
-      sq.ctx[e] = ctx[b];
-      sq.seq[e] = b;
+      sq.q0[e] = q_cu[w.seq];
+      sq.nodes[e] = n;
+      sq.ctx[e] = ctx[w.seq];
+      sq.seq[e] = w.seq;
       sq.groups[e] = int16_t(k);
       sq.part0[e] = states;
       if (k > 1) {
         ++split;
-        states += int(units(b)) * k;
-        most = std::max(most, count(b));
+        states += int(w.units) * k;
+        most = std::max(most, n);
         most_groups = std::max(most_groups, k);
       }
-      items += units(b) * k;
+      items += w.units * k;
     }
     if (items * C > 0x7fffffff) return fail(SPD_EUNSUPPORTED, "tree attention of more than 2^31 tiles");
     if (states > kMaxStates) return fail(SPD_EUNSUPPORTED, "tree attention plan of %d states", states);

@@ -196,6 +196,32 @@ def test_tree_attention_past_32_bit_offsets():
     _check_tree(q, small, see, o, ls, ctx, nodes, g, m, d)
 
 
+@pytest.mark.parametrize("g,m,d,most,n", [(4, 7, 128, 2500, 16), (2, 4, 64, 6000, 24), (2, 1, 128, 9000, 5)])
+def test_tree_attention_of_very_different_lengths(g, m, d, most, n):
+    # sequences split over clusters of different sizes, in launches that share the GPU; repeated calls overlap
+    r = np.random.default_rng(n)
+    ctx = [int(x) for x in np.exp(r.uniform(np.log(20), np.log(most), n))] + [most]
+    nodes = [int(x) for x in r.integers(1, 6, n + 1)]
+    q, kv, see, mask, slots = _tree_case(21, g, m, d, ctx, nodes, "tree")
+    total = sum(nodes)
+    qd, kd, md = q.cuda(), kv.cuda(), torch.from_numpy(mask).cuda()
+    ws = torch.zeros(N.spd_tree_attention_workspace_size(total, n + 1, g * m, g, d), dtype=torch.uint8, device="cuda")
+    outs = []
+    for k in range(6):  # other queries every other time, through the same buffer
+        src = qd if k % 2 == 0 else qd.flip(0).contiguous()
+        buf = src.clone() if k == 0 else buf.copy_(src)
+        o = torch.full((total, g * m * d), float("nan"), dtype=torch.bfloat16, device="cuda")
+        ls = torch.full((total, g * m), float("nan"), device="cuda")
+        N.spd_tree_attention(buf, _cu(nodes), ctx, md, kd, slots, g * m, g, d, o, ls, ws)
+        outs.append((o, ls))
+    torch.cuda.synchronize()
+    assert N.spd_workspace_status(ws) == 0
+    _check_tree(q, kv, see, *outs[0], ctx, nodes, g, m, d)
+    _check_tree(q.flip(0), kv, see, *outs[1], ctx, nodes, g, m, d)
+    for k in range(2, 6):
+        assert torch.equal(outs[k][0], outs[k % 2][0]) and torch.equal(outs[k][1], outs[k % 2][1])
+
+
 def test_many_sequences_take_several_launches():
     g, m, d = 1, 2, 64
     r = np.random.default_rng(3)
