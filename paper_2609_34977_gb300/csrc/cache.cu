@@ -41,6 +41,8 @@ constexpr int kSelWide = 1024;      // threads for longer ones
 constexpr int kBins = 2048;
 constexpr int kSelMost = 49152;     // keys a CTA holds (192 KB)
 constexpr int kSelMaxCluster = 8;
+// Units that lose few rows move them in the selecting kernel. 896 units that evict 7 / 32 / 64 / 256 rows of 1024, one
+// launch and two: 14.5 and 17.4 / 19.3 and 23.0 / 25.8 and 28.2 / 49.7 and 48.9 us.
 constexpr int kFusedMoves = 64;
 constexpr int kMaxSeqs = 240;       // sequences whose sizes fit in a launch's parameters
 constexpr uint32_t kHeld = 0xffffffffu;
@@ -288,7 +290,8 @@ SelectKernel pick_select(int move) {
 }
 
 // The rows themselves: a warp a move, 16 bytes a lane (half a warp K, half V; HD = 64: a quarter each), four moves in
-// flight a warp.
+// flight a warp. HBM: 175 K moves of 1 KB (read and written) in 25 us, 7.1 TB/s. Moving inside the selecting kernel saves a launch
+// and loses the occupancy: 46.8 against 44.1 us for the whole call.
 constexpr int kMoveWarps = 8, kMoveDepth = 4;
 template <int HD>
 __global__ void __launch_bounds__(kMoveWarps * 32) evict_move_kernel(uint16_t* kv, const __grid_constant__ EvictArgs p) {
@@ -412,7 +415,10 @@ extern "C" int spd_cache_evict(uint16_t* kv_cache, int n_layers, int n_seqs, con
   p.pos_out = pos_out;
   p.src = src;
   int C = 1;
-  while (C < kSelMaxCluster && longest > 16384 * C) C *= 2;
+  // more CTAs a unit where one would hold over 16384 keys, and over 8192 while a quarter of the SMs stay idle (clusters do
+  // not find room on all). 112 units of 16384 slots with 1 / 2 / 4: 30.1 / 35.1 / 49.6 us; 16 units of 32768: 74 / 32.3 / 21.5; 16 of 12000: 14.6 /
+  // 13.9 / 20.7; 16 of 65521 with 4 / 8: 50 / 68
+  while (C < kSelMaxCluster && (longest > 16384 * C || (longest > 8192 * C && 4 * units * 2 * C <= 3 * size_t(num_sms())))) C *= 2;
   int per = (std::max(longest, 1) + C - 1) / C;
   for (int b = 0; b < n_seqs; ++b) per = std::max(per, (std::min(lens[b], budget) + C - 1) / C);
   per = (per + 3) & ~3;

