@@ -392,6 +392,38 @@ def test_cache_evict_by_slots_without_positions():
     np.testing.assert_array_equal(kvd.view(torch.int16).cpu().numpy().reshape(want[0].shape), want[0])
 
 
+def test_many_sequences_of_weights_and_evictions_take_several_launches():
+    B, g, d, slots = 300, 1, 64, 40
+    r = np.random.default_rng(9)
+    lens = r.integers(0, slots + 1, B).astype(np.int32)
+    rows = np.minimum(r.integers(0, 3, B), lens)
+    n = int(rows.sum())
+    q, kv = _rand((2, n, 2 * d), 31, 2.0), _rand((2, B, slots, 2 * g * d), 32)
+    lse = torch.full((2, n, 2), 3.0)
+    acc = torch.rand(2, B, g, slots, generator=torch.Generator().manual_seed(33))
+    out = torch.zeros(2, B, g, slots, device="cuda")
+    N.spd_cache_weights(q.cuda(), lse.cuda(), None, _cu(rows), kv.cuda(), lens, slots, 2, g, d, 0.5, acc.cuda(), out)
+    got, cu, qn, kn = out.cpu().numpy(), _cu(rows), bf16_np(q), bf16_np(kv)
+    for l in range(2):
+        for b in range(B):
+            k = lens[b]
+            want = 0.5 * acc[l, b, 0, :k].numpy().astype(np.float64)
+            for i in range(rows[b]):
+                K = kn[l, b, :k - rows[b] + i + 1, :d]
+                for j in range(2):
+                    want[:len(K)] += np.exp(K @ qn[l, cu[b] + i, j * d:(j + 1) * d] / 8.0 - 3.0)
+            np.testing.assert_allclose(got[l, b, 0, :k], want, rtol=1e-4)
+            assert (got[l, b, 0, k:] == 0).all()
+    pos = np.broadcast_to(np.arange(slots, dtype=np.int32), acc.shape).copy()
+    ints = torch.randint(-30000, 30000, (2, B, slots, 2 * g * d), dtype=torch.int16)
+    want = _plain_evict(ints.numpy().reshape(2, B, slots, 2, g, d), acc.numpy(), pos, lens, 17, 2, 5, lens, g, d)
+    kvd, a = ints.cuda().view(torch.bfloat16), acc.cuda()
+    ws = torch.zeros(N.spd_cache_evict_workspace_size(2, B, g, 17), dtype=torch.uint8, device="cuda")
+    N.spd_cache_evict(kvd, lens, slots, g, d, 17, 2, 5, None, a, None, a, None, None, ws)
+    np.testing.assert_array_equal(a.cpu().numpy(), want[1])
+    np.testing.assert_array_equal(kvd.view(torch.int16).cpu().numpy().reshape(want[0].shape), want[0])
+
+
 # ---- commit ----------------------------------------------------------------------------------------
 def test_tree_commit():
     L, g, d, ctx, slots = 2, 3, 64, [10, 0, 33], 80
@@ -509,6 +541,40 @@ def test_logit_rules(v, rows_of, hist_len, n_bias, in_place):
     top = got.max(1)
     np.testing.assert_array_equal(best.cpu().numpy(), np.where(np.isneginf(top), -1, got.argmax(1)))
     assert (wide[[0, n + 1]] == 5).all() and (wide[:, v:] == 5).all()
+
+
+@pytest.mark.parametrize("v,n", [(20000, 120), (152064, 30), (32003, 100)])
+def test_logit_rules_of_more_rows_than_fit_at_once(v, n):
+    # CTAs on their own, that offer their best to the row: equal bests in many slices, the first one wins every time
+    rows_of, hist_len = [i % 3 for i in range(n)], [900, 40, 3000]
+    z, hist, gen, path, bias, allow, rule, rep, freq, pres = _logit_case(v + n, v, 3, rows_of, hist_len, 40)
+    z[:, 4001::977] = 90.0
+    z[7] = -np.inf
+    rule[7] = -1
+    want, size = _plain_logits(z, rows_of, hist, gen, path, rep, freq, pres, bias, allow, rule)
+    h_cu, b_cu, p_cu = _cu([len(h) for h in hist]), _cu([len(b) for b in bias]), _cu([len(p) for p in path])
+    zd, out = torch.from_numpy(z).cuda(), torch.zeros(n, v, device="cuda")
+    kw = dict(seq_of=_flat([rows_of], np.int32), hist=_flat(hist, np.int32), hist_cu=torch.from_numpy(h_cu).cuda(),
+              gen_start=torch.from_numpy((h_cu[:-1] + gen).astype(np.int32)).cuda(), path=_flat(path, np.int32),
+              path_cu=torch.from_numpy(p_cu).cuda(), repetition=_flat([rep], np.float32), frequency=_flat([freq], np.float32),
+              presence=_flat([pres], np.float32), bias_cu=torch.from_numpy(b_cu).cuda(),
+              bias_id=_flat([[t for t, _ in b] for b in bias], np.int32), bias=_flat([[x for _, x in b] for b in bias], np.float32),
+              allow=torch.from_numpy(_words(allow, (v + 31) // 32)).cuda(), rule=_flat([rule], np.int32))
+    bests = []
+    for _ in range(4):
+        best = torch.full((n,), 5, dtype=torch.int32, device="cuda")
+        N.spd_logits_process(zd, out, best, **kw)
+        bests.append(best.cpu().numpy())
+    got = out.cpu().numpy().astype(np.float64)
+    inf = np.isinf(want)
+    np.testing.assert_array_equal(np.where(inf, want, 0.0), np.where(np.isinf(got), got, 0.0))
+    assert (np.abs(got[~inf] - want[~inf]) <= 6 * 2.0 ** -24 * size[~inf]).all()
+    top = got.max(1)
+    assert (top > 40).sum() > n // 3 and bests[0][7] == -1
+    for b in bests:
+        np.testing.assert_array_equal(b, np.where(np.isneginf(top), -1, got.argmax(1)))
+    N.spd_logits_process(zd, out, None, **kw)  # without the best token
+    np.testing.assert_array_equal(out.cpu().numpy().astype(np.float64), got)
 
 
 def test_logit_rules_all_off_is_a_copy_and_nan_never_wins():
