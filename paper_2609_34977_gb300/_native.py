@@ -192,7 +192,7 @@ def _p(t):
     if isinstance(t, np.ndarray):
         if not t.flags["C_CONTIGUOUS"]:
             raise ValueError("host arrays passed to libspider must be C-contiguous")
-        return t.ctypes.data
+        return t.__array_interface__["data"][0]
     if not getattr(t, "is_cuda", False):
         raise TypeError(f"device arguments of libspider must be CUDA tensors, got "
                         f"{type(t).__name__} on {getattr(t, 'device', 'the host')}")
@@ -222,6 +222,11 @@ def _dev(t, dt, n, name, optional=False):
         if optional:
             return None
         raise ValueError(f"{name}: a device tensor is required")
+    try:
+        if t.is_cuda and t.dtype is _torch_dt[dt] and t.numel() >= n and t.is_contiguous():
+            return t.data_ptr()
+    except (AttributeError, KeyError):  # not a tensor, or the first one
+        pass
     if not getattr(t, "is_cuda", False):
         raise TypeError(f"{name}: device arguments of libspider must be CUDA tensors, got "
                         f"{type(t).__name__} on {getattr(t, 'device', 'the host')}")
@@ -656,14 +661,19 @@ def spd_cache_evict(kv_cache, lens, max_len, n_kv_heads, head_dim, budget, n_sin
 
 
 def _rows_f32(t, name):
-    """Pointer and row stride of a 2-D fp32 CUDA tensor whose rows are contiguous."""
+    """Pointer, row stride and shape of a 2-D fp32 CUDA tensor whose rows are contiguous."""
     if not getattr(t, "is_cuda", False):
         raise TypeError(f"{name}: device arguments of libspider must be CUDA tensors")
-    if str(t.dtype) != "torch.float32" or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name}: expected fp32 [rows][vocab] with contiguous rows")
-    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+    shape = t.shape
+    if t.dtype is not (_torch_dt or _load_dtypes())["f32"] or len(shape) != 2:
+        raise ValueError(f"{name}: expected fp32 [rows][vocab], got {t.dtype} {tuple(shape)}")
+    n, v = shape
+    ld, step = t.stride()
+    if v > 1 and step != 1:
+        raise ValueError(f"{name}: the tokens of a row must lie side by side")
+    if n > 1 and ld < v:
         raise ValueError(f"{name}: rows overlap")
-    return t.data_ptr(), max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+    return t.data_ptr(), ld if n > 1 else v, (n, v)
 
 
 def spd_logits_process(logits, out, best=None, *, seq_of=None, hist=None, hist_cu=None, gen_start=None, path=None,
@@ -671,11 +681,10 @@ def spd_logits_process(logits, out, best=None, *, seq_of=None, hist=None, hist_c
                        allow=None, rule=None, stream=None):
     """Penalties, biases and grammar masks on logits [n_rows][vocab] (rows may have a stride), into out (may be logits)
     and the best token of every row into best. Lists are device tensors; None switches a rule off."""
-    zp, ld = _rows_f32(logits, "logits")
-    op, ldo = _rows_f32(out, "out")
-    n, v = logits.shape
-    if tuple(out.shape) != (n, v):
-        raise ValueError(f"out: shape {tuple(out.shape)}, logits are {(n, v)}")
+    zp, ld, (n, v) = _rows_f32(logits, "logits")
+    op, ldo, shape = _rows_f32(out, "out")
+    if shape != (n, v):
+        raise ValueError(f"out: shape {shape}, logits are {(n, v)}")
     # the number of sequences is what the lists that come with one entry a sequence hold
     B = n if seq_of is None else 0
     for t, more in ((hist_cu, 1), (gen_start, 0), (repetition, 0), (frequency, 0), (presence, 0), (bias_cu, 1)):
@@ -686,14 +695,13 @@ def spd_logits_process(logits, out, best=None, *, seq_of=None, hist=None, hist_c
     n_bias = 0 if bias is None else bias.numel()
     words = (v + 31) // 32
     n_rules = 0 if allow is None else allow.numel() // words
-    dev = lambda t, dt, k, name: None if t is None else _dev(t, dt, k, name)  # noqa: E731
-    r = LogitsRules(dev(seq_of, "i32", n, "seq_of"), B, dev(hist, "i32", 0, "hist"), dev(hist_cu, "i32", B + 1, "hist_cu"),
-                    dev(gen_start, "i32", B, "gen_start"), n_hist, dev(path, "i32", 0, "path"),
-                    dev(path_cu, "i32", n + 1, "path_cu"), n_path, dev(repetition, "f32", B, "repetition"),
-                    dev(frequency, "f32", B, "frequency"), dev(presence, "f32", B, "presence"),
-                    dev(bias_cu, "i32", B + 1, "bias_cu"), dev(bias_id, "i32", n_bias, "bias_id"),
-                    dev(bias, "f32", n_bias, "bias"), n_bias, dev(allow, "i32", n_rules * words, "allow"), n_rules,
-                    dev(rule, "i32", n, "rule"))
+    r = LogitsRules(_dev(seq_of, "i32", n, "seq_of", True), B, _dev(hist, "i32", 0, "hist", True),
+                    _dev(hist_cu, "i32", B + 1, "hist_cu", True), _dev(gen_start, "i32", B, "gen_start", True), n_hist,
+                    _dev(path, "i32", 0, "path", True), _dev(path_cu, "i32", n + 1, "path_cu", True), n_path,
+                    _dev(repetition, "f32", B, "repetition", True), _dev(frequency, "f32", B, "frequency", True),
+                    _dev(presence, "f32", B, "presence", True), _dev(bias_cu, "i32", B + 1, "bias_cu", True),
+                    _dev(bias_id, "i32", n_bias, "bias_id", True), _dev(bias, "f32", n_bias, "bias", True), n_bias,
+                    _dev(allow, "i32", n_rules * words, "allow", True), n_rules, _dev(rule, "i32", n, "rule", True))
     _check(lib().spd_logits_process(zp, n, v, ld, C.byref(r), op, ldo, _dev(best, "i32", n, "best", True),
                                     _stream(stream)))
 

@@ -74,6 +74,8 @@ class TreeAnswer:
         c = self.cfg
         cu = np.asarray(cu, np.int64)
         n = np.diff(cu)
+        if len(n) != self.B or n.min() < 2 or window < 1:
+            raise ValueError("start: a prompt of two tokens at least for every sequence, and a window")
         tail = np.minimum(window, n - 1)
         at = lambda lo, hi: np.concatenate([np.arange(a, b) for a, b in zip(lo, hi)])  # noqa: E731
         head = at(cu[:-1], cu[1:] - tail)

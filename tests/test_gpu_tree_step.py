@@ -138,6 +138,16 @@ def test_answers_with_and_without_drafts():
         assert steps <= 4  # nine tokens, up to four a step
 
 
+def test_answers_refuse_prompts_without_a_window():
+    _, _, embed, tokens, _, run = _answers(71, [5, 1])
+    for cu, kw in (([0, 5, 6], {}), ([0, 6], {}), ([0, 3, 6], dict(window=0))):
+        with pytest.raises(ValueError, match="start"):
+            _start(run, embed, tokens, cu, **kw)
+    with pytest.raises(ValueError, match="drafts"):
+        run.pending = [1, 1]
+        run.step([[(1, 0)] * 40, []])
+
+
 def test_answers_within_a_budget():
     # the rows that stay are rows of the whole cache, at the positions that the bookkeeping says
     N.spd_set_deterministic(True)
