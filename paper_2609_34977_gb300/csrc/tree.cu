@@ -42,7 +42,7 @@
 namespace spd {
 namespace {
 
-constexpr int kMaxSeqs = 128;          // sequences whose sizes fit in a launch's parameters (4 KB)
+constexpr int kMaxSeqs = 112;          // sequences whose sizes fit in a launch's parameters (4 KB)
 constexpr int kTK = 64;                // keys a block
 constexpr uint32_t kQBox = 128 * 128;  // 64 columns of the Q tile
 constexpr uint32_t kKBox = kTK * 128;  // 64 columns of a block of K or V
@@ -55,14 +55,17 @@ constexpr int kItems = 304;            // items that fill the GPU: two CTAs on e
 constexpr float kGrown = 8.0f;
 constexpr int kMaxCluster = 8;
 
-// Sequences of a launch, the longest first (by value in the parameters: no copy, no wait for one). Clusters
-// [item0[e], item0[e + 1]) are sequence e's: (K/V head, group of parts of the keys, tile), the tile fastest, so that the tiles
-// that read the same keys run side by side; the CTAs of a cluster are the parts of its group.
+// Sequences of a launch, the longest first, in the launch's parameters (no copy, no wait for one). Clusters from item0 on are
+// the sequence's: (K/V head, group of parts of the keys, tile), the tile fastest, so that the tiles that read the same keys
+// run side by side; the CTAs of a cluster are the parts of its group. A CTA reads one entry, half a line of parameter
+// memory: with an array a field the look-up took 1400 to 2100 cycles.
+struct TreeSeq {
+  int item0, q0, nodes, ctx, seq, tiles, groups;
+  int part0;  // first slot of the sequence's states in the workspace (groups > 1)
+};
 struct TreeSeqs {
-  int n, item0[kMaxSeqs + 1];
-  int q0[kMaxSeqs], nodes[kMaxSeqs], ctx[kMaxSeqs], seq[kMaxSeqs];
-  int16_t groups[kMaxSeqs];
-  int part0[kMaxSeqs];  // first slot of the sequence's states in the workspace (groups > 1)
+  int n, pad[7];
+  TreeSeq s[kMaxSeqs];
 };
 struct TreeArgs {
   const __nv_bfloat16* q;
@@ -151,26 +154,28 @@ __global__ void __launch_bounds__(kThreads, 2)
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // the cluster's sequence: the last entry that starts at or before it
-  const int C = p.cluster, rank = int(blockIdx.x) % C;
-  int u = int(blockIdx.x) / C, e = 0;
+  const int C = p.cluster, rank = int(blockIdx.x) & (C - 1);
+  uint32_t u = blockIdx.x / uint32_t(C);
+  int e = 0;
   for (int hi = sq.n; hi - e > 1;) {
     const int mid = (e + hi) >> 1;
-    if (sq.item0[mid] <= u) e = mid;
+    if (uint32_t(sq.s[mid].item0) <= u) e = mid;
     else hi = mid;
   }
-  const int n = sq.nodes[e], ctx = sq.ctx[e], groups = sq.groups[e], parts = groups * C;
-  const int tiles = (n + p.nodes_tile - 1) / p.nodes_tile * p.chunks;
-  u -= sq.item0[e];
-  const int slot = sq.part0[e] + u;
-  const int tile = u % tiles;
-  u /= tiles;
-  const int part = u % groups * C + rank, hk = u / groups;
+  const TreeSeq& sh = sq.s[e];
+  const int n = sh.nodes, ctx = sh.ctx, groups = sh.groups, parts = groups * C, tiles = sh.tiles;
+  u -= uint32_t(sh.item0);
+  const int slot = sh.part0 + int(u);
+  const int tile = int(u % uint32_t(tiles));
+  u /= uint32_t(tiles);
+  const int part = int(u % uint32_t(groups)) * C + rank, hk = int(u / uint32_t(groups));
   const int n0 = tile / p.chunks * p.nodes_tile, h0 = tile % p.chunks * p.chunk;  // first node, first head of the group
   const int nodes = min(p.nodes_tile, n - n0), rows = nodes * p.chunk;
   const int heads = min(p.chunk, p.group - h0);  // of the chunk's heads, those there are
   const int total = ctx + n, blocks = (total + kTK - 1) / kTK;
-  const int b0 = int((long long)part * blocks / parts), nkb = int((long long)(part + 1) * blocks / parts) - b0;
-  const int row0 = sq.seq[e] * p.max_len;  // the cache slot's first row
+  const int even = int(uint32_t(blocks) / uint32_t(parts)), more = blocks - even * parts;  // the first `more` parts have one more
+  const int b0 = part * even + min(part, more), nkb = even + (part < more);
+  const int row0 = sh.seq * p.max_len;  // the cache slot's first row
   const int nw = (rows + 31) / 32;         // softmax warps with rows
   if (threadIdx.x == 0) {
     for (int s = 0; s < NS; ++s) {
@@ -282,7 +287,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     const int node = n0 + min(r / p.chunk, nodes - 1), hc = r % p.chunk;
     const bool valid = r < rows && hc < heads;
     const int head = hk * p.group + h0 + min(hc, heads - 1);
-    const size_t qrow = sq.q0[e] + node;  // rows without a node repeat the last one's, and are not stored
+    const size_t qrow = sh.q0 + node;  // rows without a node repeat the last one's, and are not stored
     const __nv_bfloat16* qsrc = p.q + (qrow * p.n_heads + head) * HD;
     const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
     {  // the Q tile in the 128-byte swizzle: 16-byte piece j of row r at j ^ (r % 8)
@@ -514,7 +519,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         if (j == 0) p.part_ml[at] = make_float2(m, l);
         reinterpret_cast<float4*>(p.part_o + at * HD)[j] = o;
       } else if (hc < heads) {
-        const size_t at = size_t(sq.q0[e] + n0 + r / p.chunk) * p.n_heads + hk * p.group + h0 + hc;
+        const size_t at = size_t(sh.q0 + n0 + r / p.chunk) * p.n_heads + hk * p.group + h0 + hc;
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
         reinterpret_cast<uint2*>(p.o + at * HD)[j] = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
         if (j == 0 && p.lse) p.lse[at] = fmaf(m, 0.6931471805599453f, logf(l));
@@ -538,7 +543,8 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
   __shared__ float wo[kMergeWarps][HD];
   pdl_launch_dependents();
   pdl_wait();
-  const int e = blockIdx.y, n = sq.nodes[e], parts = sq.groups[e];
+  const TreeSeq& sh = sq.s[blockIdx.y];
+  const int n = sh.nodes, parts = sh.groups;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp % W;
   const int row = blockIdx.x * (kMergeWarps / W) + warp / W;
   const bool have = row < n * p.n_heads;
@@ -548,10 +554,10 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
   const int node = row / p.n_heads, head = row % p.n_heads;
   if (have) {
     const int hk = head / p.group, hg = head % p.group;
-    const int tiles = (n + p.nodes_tile - 1) / p.nodes_tile * p.chunks;
+    const int tiles = sh.tiles;
     const int tile = node / p.nodes_tile * p.chunks + hg / p.chunk;
     const int r = node % p.nodes_tile * p.chunk + hg % p.chunk;
-    const size_t first = (size_t(sq.part0[e]) + size_t(hk) * parts * tiles + tile) * p.rows_part + r;
+    const size_t first = (size_t(sh.part0) + size_t(hk) * parts * tiles + tile) * p.rows_part + r;
     const size_t step = size_t(tiles) * p.rows_part;
     const int s1 = (w + 1) * parts / W;
     for (int s0 = w * parts / W; s0 < s1; s0 += 8) {
@@ -610,7 +616,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
   }
   if (!have) return;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  const size_t at = size_t(sq.q0[e] + node) * p.n_heads + head;
+  const size_t at = size_t(sh.q0 + node) * p.n_heads + head;
   uint32_t* to = reinterpret_cast<uint32_t*>(p.o + at * HD + D * lane);
 #pragma unroll
   for (int x = 0; x < D / 2; ++x) to[x] = pack_bf16(o[2 * x] * inv, o[2 * x + 1] * inv);
@@ -788,15 +794,8 @@ int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, i
     long long items = 0;
     int states = 0, most = 0, most_groups = 0, split = 0;  // split: sequences of several groups, the first ones
     for (const TreeWork& w : work) {
-      const int e = sq.n++, n = q_cu[w.seq + 1] - q_cu[w.seq];
-      const int k = plan.groups(w.blocks);
-      sq.item0[e] = int(items);
-      sq.q0[e] = q_cu[w.seq];
-      sq.nodes[e] = n;
-      sq.ctx[e] = ctx[w.seq];
-      sq.seq[e] = w.seq;
-      sq.groups[e] = int16_t(k);
-      sq.part0[e] = states;
+      const int n = q_cu[w.seq + 1] - q_cu[w.seq], k = plan.groups(w.blocks);
+      sq.s[sq.n++] = {int(items), q_cu[w.seq], n, ctx[w.seq], w.seq, (n + t.nodes - 1) / t.nodes * t.chunks, k, states};
       if (k > 1) {
         ++split;
         states += int(w.units) * k;
@@ -807,7 +806,6 @@ int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, i
     }
     if (items * C > 0x7fffffff) return fail(SPD_EUNSUPPORTED, "tree attention of more than 2^31 tiles");
     if (states > kMaxStates) return fail(SPD_EUNSUPPORTED, "tree attention plan of %d states", states);
-    sq.item0[sq.n] = int(items);
     p.cluster = C;
     const double fl = 4.0 * head_dim * n_heads * pairs;
     const double by = 4.0 * kvd * keys + 4.0 * n_heads * head_dim * (q_cu[s0 + m] - q_cu[s0]);

@@ -27,7 +27,7 @@
 namespace spd {
 namespace {
 
-constexpr int kMaxSeqs = 128;            // sequences whose sizes fit in a launch's parameters (4 KB)
+constexpr int kMaxSeqs = 112;            // sequences whose sizes fit in a launch's parameters (4 KB)
 constexpr int kTile = 128;               // keys a block, and (row, head) pairs a pass
 constexpr uint32_t kBox = kTile * 128;   // 64 columns of 128 rows
 constexpr int kThreads = 192;
@@ -35,15 +35,18 @@ constexpr int kStages = 2;
 constexpr uint32_t kTmemCols = 256;      // two accumulators of up to 128 columns
 constexpr int kPlaces = 304;             // CTAs the GPU holds at once (two on each of 152 SMs)
 
-struct WeightSeqs {  // by value in the launch's parameters; item0: first item (K/V head, part of the keys) of a sequence
-  int n, item0[kMaxSeqs + 1];
-  int len[kMaxSeqs], rows[kMaxSeqs], row0[kMaxSeqs];
+struct WeightSeq {  // item0: the sequence's first item (K/V head, part of the keys)
+  int item0, len, rows, row0, blocks, parts, pad[2];
+};
+struct WeightSeqs {  // by value in the launch's parameters
+  int n, pad[7];
+  WeightSeq s[kMaxSeqs];
 };
 struct WeightArgs {
   const __nv_bfloat16* q;
   const float* lse;
   const int32_t* rows;
-  int n_q, n_seqs, seq0, max_len, n_heads, n_kv_heads, share;  // share: blocks an item
+  int n_q, n_seqs, seq0, max_len, n_heads, n_kv_heads;
   float scale_log2, decay;
   const float* acc_in;
   float* acc_out;
@@ -91,13 +94,15 @@ __global__ void __launch_bounds__(kThreads, 2)
   int e = 0;
   for (int hi = sq.n; hi - e > 1;) {
     const int mid = (e + hi) >> 1;
-    if (sq.item0[mid] <= int(blockIdx.x)) e = mid;
+    if (sq.s[mid].item0 <= int(blockIdx.x)) e = mid;
     else hi = mid;
   }
-  const int len = sq.len[e], n = sq.rows[e], G = p.n_heads / p.n_kv_heads, pairs = n * G;
-  const int blocks = (len + kTile - 1) / kTile, parts = (blocks + p.share - 1) / p.share;
-  const int local = int(blockIdx.x) - sq.item0[e], part = local % parts, hk = local / parts, layer = blockIdx.y;
-  const int b0 = int((long long)part * blocks / parts), nb = int((long long)(part + 1) * blocks / parts) - b0;
+  const WeightSeq& sh = sq.s[e];
+  const int len = sh.len, n = sh.rows, G = p.n_heads / p.n_kv_heads, pairs = n * G, blocks = sh.blocks, parts = sh.parts;
+  const uint32_t local = blockIdx.x - uint32_t(sh.item0);
+  const int part = int(local % uint32_t(parts)), hk = int(local / uint32_t(parts)), layer = blockIdx.y;
+  const int even = int(uint32_t(blocks) / uint32_t(parts)), more = blocks - even * parts;  // the first `more` parts have one more
+  const int b0 = part * even + min(part, more), nb = even + (part < more);
   const int passes = (pairs + kTile - 1) / kTile;
   const int seq = layer * p.n_seqs + p.seq0 + e, row_k = seq * p.max_len;  // first row of the cache slot
   if (threadIdx.x == 0) {
@@ -197,7 +202,7 @@ __global__ void __launch_bounds__(kThreads, 2)
       if (it % nb == 0) {
         // the pass's pairs, in the 128-byte swizzle (16-byte piece j of row t at j ^ (t % 8)); pairs past the
         // last, and rows outside the queries, as zeros with a normaliser that leaves no weight
-        const int x = pass * kTile + t, i = x / G, at = x < pairs ? (p.rows ? p.rows[sq.row0[e] + i] : sq.row0[e] + i) : -1;
+        const int x = pass * kTile + t, i = x / G, at = x < pairs ? (p.rows ? p.rows[sh.row0 + i] : sh.row0 + i) : -1;
         const bool have = at >= 0 && at < p.n_q;
         const size_t row = (size_t(layer) * p.n_q + (have ? at : 0)) * p.n_heads + hk * G + (x < pairs ? x % G : 0);
         if (it > 0 && !(ok = all_meet())) break;  // every warp is done with the last pass's normalisers, the MMAs with its Q
@@ -339,20 +344,16 @@ extern "C" int spd_cache_weights(const uint16_t* q, const float* lse, int n_q, c
     const int waves = fits ? 1 : 2;
     long long share = std::max<long long>(2, (work + waves * kPlaces - 1) / (waves * kPlaces));
     while (fits && wave(share) > kPlaces) share += (share + 15) / 16;
-    p.share = int(share);
     long long items = 0;
     for (int i = 0; i < sq.n; ++i) {
       const int b = s0 + i, blocks = (lens[b] + kTile - 1) / kTile;
-      sq.len[i] = lens[b];
-      sq.rows[i] = rows_cu[b + 1] - rows_cu[b];
-      sq.row0[i] = rows_cu[b];
-      sq.item0[i] = int(items);
-      items += (long long)n_kv_heads * ((blocks + p.share - 1) / p.share);
+      const int parts = int((blocks + share - 1) / share), rows_b = rows_cu[b + 1] - rows_cu[b];
+      sq.s[i] = {int(items), lens[b], rows_b, rows_cu[b], blocks, parts, {}};
+      items += (long long)n_kv_heads * parts;
       keys += lens[b];
-      pairs += double(lens[b]) * sq.rows[i];
+      pairs += double(lens[b]) * rows_b;
     }
     if (items > 0x7fffffff) return fail(SPD_EUNSUPPORTED, "cache weights of more than 2^31 blocks");
-    sq.item0[sq.n] = int(items);
     if (items == 0) continue;
     const double fl = 2.0 * head_dim * n_heads * pairs * n_layers, by = keys * n_layers * n_kv_heads * (2.0 * head_dim + 8.0);
     p.stamp = stamp_slot(TR_ATTN, fl, by);
