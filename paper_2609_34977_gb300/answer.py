@@ -12,6 +12,8 @@ the caller (a small model, the prompt's own n-grams). `python -m paper_2609_3497
 """
 from __future__ import annotations
 
+import itertools
+
 import numpy as np
 import torch
 
@@ -35,6 +37,8 @@ class TreeAnswer:
         self.budget, self.n_sink, self.n_recent, self.decay = budget, n_sink, n_recent, decay
         if budget is not None and not n_sink + n_recent <= budget <= max_len - max_nodes:
             raise ValueError("budget: needs room for sinks and recent tokens, and for a step's drafts up to max_len")
+        if tuple(embed.shape) != (c["vocab"], c["d_model"]):
+            raise ValueError(f"embed: {tuple(embed.shape)}, expected {(c['vocab'], c['d_model'])}")
         self.rules = dict(rules or {})
         self.rule = self.rules.pop("rule", None)
         L, G = c["n_layers"], c["n_kv_heads"]
@@ -76,6 +80,8 @@ class TreeAnswer:
         n = np.diff(cu)
         if len(n) != self.B or n.min() < 2 or window < 1:
             raise ValueError("start: a prompt of two tokens at least for every sequence, and a window")
+        self.acc.zero_()  # nothing of an earlier answer stays
+        self.pos.copy_(torch.arange(self.max_len, dtype=torch.int32, device="cuda").expand(self.pos.shape))
         tail = np.minimum(window, n - 1)
         at = lambda lo, hi: np.concatenate([np.arange(a, b) for a, b in zip(lo, hi)])  # noqa: E731
         head = at(cu[:-1], cu[1:] - tail)
@@ -105,6 +111,8 @@ class TreeAnswer:
         rules leave no token gains -1 and ends: its next steps are empty)."""
         live = [p is not None and p >= 0 for p in self.pending]
         drafts = drafts or [[] for _ in range(self.B)]
+        if any(not 0 <= t < self.cfg["vocab"] for d in drafts for t, _ in d):
+            raise ValueError("drafts: a token outside the vocabulary")
         tok, parent = [], []
         for b in range(self.B):
             if not live[b]:
@@ -189,13 +197,14 @@ class TreeAnswer:
         return N.spd_workspace_status(self.ws)
 
 
-def ngram_drafts(text, n: int, width: int = 2):
+def ngram_drafts(text, n: int, width: int = 2, vocab: int | None = None):
     """Drafts from the text so far: the continuations of the last `width` tokens' most recent earlier occurrence, as a chain
-    of up to n tokens."""
+    of up to n tokens, up to the first outside the vocabulary (an image's placeholder)."""
     key = text[-width:]
     for i in range(len(text) - width - 1, -1, -1):
         if text[i:i + width] == key:
-            return [(t, k) for k, t in enumerate(text[i + width:i + width + n])]
+            return [(t, k) for k, t in enumerate(itertools.takewhile(lambda t: vocab is None or 0 <= t < vocab,
+                                                                     text[i + width:i + width + n]))]
     return []
 
 
@@ -216,7 +225,7 @@ def main():
     said = [[t] for t in run.start(x, [0, lens[0], sum(lens)], tokens)]
     steps = 0
     while min(len(s) for s in said) < 48:
-        drafts = [ngram_drafts(run.hist[b] + [run.pending[b]], 5) for b in range(2)]
+        drafts = [ngram_drafts(run.hist[b] + [run.pending[b]], 5, vocab=cfg["vocab"]) for b in range(2)]
         for s, new in zip(said, run.step(drafts)):
             s.extend(new)
         steps += 1

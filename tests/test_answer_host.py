@@ -19,3 +19,19 @@ def test_a_budget_needs_room(kw):
         cfg = dict(n_layers=1, n_kv_heads=1, head_dim=64, n_heads=1, vocab=8, d_model=64)
     with pytest.raises(ValueError, match="budget"):
         TreeAnswer(Model, None, 1, 128, **kw)
+
+
+def test_ngram_drafts_stop_at_an_images_placeholders():
+    text = [1, 2, 3, -1, -1, 4, 1, 2]
+    assert ngram_drafts(text, 5) == [(3, 0), (-1, 1), (-1, 2), (4, 3), (1, 4)]
+    assert ngram_drafts(text, 5, vocab=8) == [(3, 0)] and ngram_drafts(text, 5, vocab=3) == []
+
+
+def test_the_embedding_is_the_vocabulary_s():
+    class Model:
+        cfg = dict(n_layers=1, n_kv_heads=1, head_dim=64, n_heads=1, vocab=8, d_model=64)
+
+    class Embed:
+        shape = (7, 64)
+    with pytest.raises(ValueError, match="embed"):
+        TreeAnswer(Model, Embed, 1, 128)

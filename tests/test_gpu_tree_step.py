@@ -148,6 +148,35 @@ def test_answers_refuse_prompts_without_a_window():
         run.step([[(1, 0)] * 40, []])
 
 
+def test_answers_refuse_drafts_outside_the_vocabulary():
+    cfg, _, embed, tokens, cu, run = _answers(71, [40, 23])
+    _start(run, embed, tokens, cu, window=8)
+    for t in (-1, cfg["vocab"]):
+        with pytest.raises(ValueError, match="vocabulary"):
+            run.step([[], [(3, 0), (t, 1)]])
+    assert run.lens.tolist() == [40, 23] and all(len(x) == 1 for x in run.step())
+
+
+def test_a_second_answer_begins_afresh():
+    N.spd_set_deterministic(True)
+    try:
+        kw = dict(max_nodes=4, budget=64, n_recent=16)
+        _, _, embed, tokens, cu, run = _answers(91, [120, 50], **kw)
+        _start(run, embed, tokens, cu, window=16)
+        for _ in range(3):
+            run.step([[(5, 0)], [(3, 0)]])
+        said = [_start(r, embed, tokens, cu, window=16) for r in (run, _answers(91, [120, 50], **kw)[5])]
+        new = _answers(91, [120, 50], **kw)[5]
+        assert said[0] == said[1] == _start(new, embed, tokens, cu, window=16)
+        assert run.lens.tolist() == new.lens.tolist() and run.next_pos.tolist() == new.next_pos.tolist()
+        for b, n in enumerate(run.lens):
+            assert torch.equal(run.acc[:, b, :, :n], new.acc[:, b, :, :n])
+            assert torch.equal(run.pos[:, b, :, :n], new.pos[:, b, :, :n])
+            assert torch.equal(run.kv[:, b, :n].view(torch.int16), new.kv[:, b, :n].view(torch.int16))
+    finally:
+        N.spd_set_deterministic(False)
+
+
 def test_answers_within_a_budget():
     # the rows that stay are rows of the whole cache, at the positions that the bookkeeping says
     N.spd_set_deterministic(True)
