@@ -227,9 +227,9 @@ __global__ void __launch_bounds__(kThreads, 2)
           for (int j = 0; j < HD / 8; ++j)
             *reinterpret_cast<uint4*>(smem + L::q + (j >> 3) * kBox + t * 128 + (((j & 7) ^ (t & 7)) << 4)) = v[j];
         }
-        // lse log2(e) to twice the bits
+        // lse log2(e) to twice the bits (an infinite one leaves no weight, of either sign)
         const float l = have ? p.lse[row] : -INFINITY, hi = l * kLog2eHi;
-        s_lse[t] = l == -INFINITY ? make_float2(INFINITY, 0.0f) : make_float2(hi, fmaf(l, kLog2eHi, -hi) + l * kLog2eLo);
+        s_lse[t] = isinf(l) ? make_float2(INFINITY, 0.0f) : make_float2(hi, fmaf(l, kLog2eHi, -hi) + l * kLog2eLo);
         s_lim[t] = len - n + i + 1;
         fence_proxy_async_smem();
         if (!(ok = all_meet())) break;
@@ -251,6 +251,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         tc_fence_after();
         const uint32_t td = tmem + kTile * (st & 1) + lanes;
         const int m = min(kSub, cols - c0);
+        const float was = sum;
         if (m <= 8) {
           float v[8], u[8];
           tmem_ld8x2(td, v, td + kSub, u);
@@ -268,6 +269,18 @@ __global__ void __launch_bounds__(kThreads, 2)
 #pragma unroll
               for (int c = 0; c < 16; ++c) add(v[c], u[c], c0 + d + c);
             }
+          }
+        }
+        if (__any_sync(0xffffffffu, isnan(sum))) {
+          // a key that is not finite: again without the pairs that add nothing, whose zeros became NaN
+          sum = was;
+#pragma unroll 1
+          for (int d = 0; d < m; d += 8) {
+            float v[8], u[8];
+            tmem_ld8x2(td + d, v, td + kSub + d, u);
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+              if (!isinf(s_lse[c0 + d + c].x)) add(v[c], u[c], c0 + d + c);
           }
         }
         tc_fence_before();
@@ -318,6 +331,9 @@ extern "C" int spd_cache_weights(const uint16_t* q, const float* lse, int n_q, c
     if (lens[b] < 0 || lens[b] > max_len) return fail(SPD_EINVAL, "length of sequence %d outside [0, max_len]", b);
     if (rows_cu[b + 1] < rows_cu[b] || rows_cu[b + 1] - rows_cu[b] > lens[b])
       return fail(SPD_EINVAL, "sequence %d: rows_cu decreases, or more rows than cached tokens", b);
+    const long long pairs = (long long)(rows_cu[b + 1] - rows_cu[b]) * (n_heads / n_kv_heads);
+    if ((pairs + kTile - 1) / kTile * ((lens[b] + kTile - 1) / kTile) > 0x7fffffffLL / kTile)
+      return fail(SPD_EUNSUPPORTED, "sequence %d: too many (row, head, slot) triples", b);
   }
   if (!rows && rows_cu[n_seqs] > n_q) return fail(SPD_EINVAL, "rows_cu runs past the queries");
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -333,7 +349,8 @@ extern "C" int spd_cache_weights(const uint16_t* q, const float* lse, int n_q, c
   p.n_heads = n_heads;
   p.n_kv_heads = n_kv_heads;
   const double scale = 1.4426950408889634 / sqrt(double(head_dim));
-  p.scale_hi = float(scale);
+  // rounded down, so that the low part is positive and an infinite score stays what it is
+  p.scale_hi = float(scale) > scale ? nextafterf(float(scale), 0.0f) : float(scale);
   p.scale_lo = float(scale - double(p.scale_hi));
   p.decay = decay;
   p.acc_in = acc_in;
