@@ -408,7 +408,7 @@ size_t spd_tree_attention_workspace_size(int n_q, int n_seqs, int n_heads, int n
  * q_cu (HOST) int32 [n_seqs + 1] from 0 to n_q; ctx_len (HOST) int32 [n_seqs]; tree_mask (dev) uint32
  * [n_q][mask_words] as spd_tree_mask makes it (any bits are allowed, a row of zeros too), or NULL: node i sees drafts
  * 0..i; kv (dev) bf16 [n_seqs][max_len][K | V], a layer's block of the cache, K rotated; lse (dev) fp32 [n_q][n_heads],
- * natural logarithm, may be NULL. head_dim 64 or 128; q, o and kv 16-byte aligned.
+ * natural logarithm, may be NULL. head_dim 64 or 128; q, o, kv and ws 16-byte aligned.
  * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ENOSPC, SPD_ECUDA; device timeouts in the workspace's status word. */
 int spd_tree_attention(const uint16_t* q, int n_q, const int32_t* q_cu, const int32_t* ctx_len, int n_seqs,
                        const uint32_t* tree_mask, int mask_words, const uint16_t* kv, int max_len, int n_heads,
@@ -426,7 +426,7 @@ size_t spd_decode_tree_workspace_size(const spd_model* m, int n_q);
  * [n_q][vocab] of every node. For spd_cache_weights: q_out (dev, may be NULL, 16-byte aligned) bf16
  * [n_layers][n_q][n_heads * head_dim] receives the rotated queries, lse_out (dev, may be NULL) fp32
  * [n_layers][n_q][n_heads] their normalisers. q_cu, ctx_len, tree_mask as spd_tree_attention; kv_cache (dev) bf16
- * [n_layers][n_seqs][max_len][K | V], 16-byte aligned.
+ * [n_layers][n_seqs][max_len][K | V]; ws and kv_cache 16-byte aligned.
  * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ENOSPC, SPD_ECUDA; device timeouts in the workspace's status word. */
 int spd_decode_tree(const spd_model* m, const uint16_t* x, int n_q, const int32_t* q_cu, const int32_t* ctx_len,
                     int n_seqs, const int32_t* pos, const uint32_t* tree_mask, int mask_words, uint16_t* kv_cache,
@@ -439,7 +439,7 @@ size_t spd_tree_commit_workspace_size(int n_seqs, int n_path);
 /* The accepted drafts join the context: in every layer the cache rows of sequence b's nodes path[path_cu[b]] ..
  * path[path_cu[b + 1] - 1] (HOST int32, ascending) move from slots ctx_len[b] + node to slots ctx_len[b], ctx_len[b] + 1,
  * ..., in place. The caller's context grows by the length of the path. kv_cache (dev) bf16
- * [n_layers][n_seqs][max_len][K | V], 16-byte aligned; pos (dev, may be NULL) int32 [n_layers][n_seqs][n_kv_heads][max_len]
+ * [n_layers][n_seqs][max_len][K | V]; ws and kv_cache 16-byte aligned; pos (dev, may be NULL) int32 [n_layers][n_seqs][n_kv_heads][max_len]
  * receives next_pos[b] + i (HOST int32 [n_seqs]) in the new slots, acc (dev, may be NULL) fp32 of the same shape zeros.
  * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ENOSPC, SPD_ECUDA. */
 int spd_tree_commit(uint16_t* kv_cache, int n_layers, int n_seqs, const int32_t* path, const int32_t* path_cu,
@@ -451,7 +451,7 @@ int spd_tree_commit(uint16_t* kv_cache, int n_layers, int n_seqs, const int32_t*
  *                   exp(q_ih . k_slot / sqrt(head_dim) - lse_ih),
  * row i of the n rows of a sequence of lens[b] cached rows seeing slots 0 .. lens[b] - n + i: the rows are the last n
  * cached tokens in order (the accepted drafts after a step, or a window at the end of the prompt). Rows whose lse is
- * -inf add nothing.
+ * infinite add nothing, whatever the keys hold.
  * q (dev) bf16 [n_layers][n_q][n_heads * head_dim] and lse (dev) fp32 [n_layers][n_q][n_heads], of spd_tree_attention
  * or spd_decode_tree; rows (dev) int32: the query row of every row, sequence b's at [rows_cu[b], rows_cu[b + 1]) (HOST
  * int32 [n_seqs + 1] from 0), NULL = row i is query row i; indices outside [0, n_q) add nothing. lens (HOST) int32 [n_seqs]; kv_cache as
@@ -478,7 +478,7 @@ size_t spd_cache_evict_workspace_size(int n_layers, int n_seqs, int n_kv_heads, 
  * and pos_in, pos_out (dev) int32, all [n_layers][n_seqs][n_kv_heads][max_len]: weight and rotary position of every
  * slot, moved along; an out may be its in, or apart; slots from the new length to lens[b] get 0 and -1. pos_in NULL = the slot
  * is the position (then pos_out may be NULL). src (dev, may be NULL) int32 [n_layers][n_seqs][n_kv_heads][budget]: the
- * slot that every kept row came from. At most 393216 rows in a sequence that loses some.
+ * slot that every kept row came from. At most 393216 rows in a sequence that loses some; ws 16-byte aligned.
  * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ENOSPC, SPD_ECUDA. */
 int spd_cache_evict(uint16_t* kv_cache, int n_layers, int n_seqs, const int32_t* lens, int max_len, int n_kv_heads,
                     int head_dim, int budget, int n_sink, int n_recent, const int32_t* next_pos,

@@ -7,6 +7,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <exception>
 #include <mutex>
 #include <memory>
 #include <vector>
@@ -1193,11 +1194,11 @@ extern "C" size_t spd_decode_tree_workspace_size(const spd_model* m, int n_q) {
 extern "C" int spd_decode_tree(const spd_model* m, const uint16_t* x, int n_q, const int32_t* q_cu, const int32_t* ctx_len,
                                int n_seqs, const int32_t* pos, const uint32_t* tree_mask, int mask_words,
                                uint16_t* kv_cache, int max_len, float* logits, uint16_t* q_out, float* lse_out, void* ws,
-                               size_t ws_bytes, void* stream) {
+                               size_t ws_bytes, void* stream) try {
   if (!m || !x || !q_cu || !ctx_len || !pos || !kv_cache || !ws || n_q < 1 || n_seqs < 1 || max_len < 1)
     return fail(SPD_EINVAL, "bad tree step arguments");
-  if ((reinterpret_cast<uintptr_t>(kv_cache) | reinterpret_cast<uintptr_t>(q_out)) & 15)
-    return fail(SPD_EINVAL, "kv_cache and q_out must be 16-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(kv_cache) | reinterpret_cast<uintptr_t>(q_out) | reinterpret_cast<uintptr_t>(ws)) & 15)
+    return fail(SPD_EINVAL, "kv_cache, q_out and ws must be 16-byte aligned");
   if (int rc = tree_attention_check(q_cu, n_q, ctx_len, n_seqs, tree_mask, mask_words, max_len)) return rc;
   for (int i = 0; i < n_q; ++i)
     if (pos[i] < 0) return fail(SPD_EINVAL, "negative rotary position of node %d", i);
@@ -1232,6 +1233,8 @@ extern "C" int spd_decode_tree(const spd_model* m, const uint16_t* x, int n_q, c
     if (int rc = run_layer(m, l, P.ll[0], P, bf, dl, h, n_q, st, &dest)) return rc;
   }
   return run_head(m, P, bf, dl, h, n_q, logits, st);
+} catch (const std::exception&) {  // the host lists
+  return fail(SPD_EUNSUPPORTED, "tree step: out of host memory for %d nodes", n_q);
 }
 
 

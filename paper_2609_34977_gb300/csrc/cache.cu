@@ -10,6 +10,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <exception>
 #include <vector>
 
 #include "internal.h"
@@ -383,7 +384,8 @@ extern "C" int spd_cache_evict(uint16_t* kv_cache, int n_layers, int n_seqs, con
   if (head_dim != 64 && head_dim != 128) return fail(SPD_EUNSUPPORTED, "head_dim must be 64 or 128");
   if (pos_in && !next_pos) return fail(SPD_EINVAL, "positions need next_pos");
   if (pos_in && !pos_out) return fail(SPD_EINVAL, "positions need pos_out");
-  if (reinterpret_cast<uintptr_t>(kv_cache) & 15) return fail(SPD_EINVAL, "the cache must be 16-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(kv_cache) | reinterpret_cast<uintptr_t>(ws)) & 15)
+    return fail(SPD_EINVAL, "the cache and ws must be 16-byte aligned");
   int longest = 0, most_moves = 0;
   for (int b = 0; b < n_seqs; ++b) {
     if (lens[b] < 0 || lens[b] > max_len) return fail(SPD_EINVAL, "length of sequence %d outside [0, max_len]", b);
@@ -481,12 +483,13 @@ extern "C" size_t spd_tree_commit_workspace_size(int n_seqs, int n_path) {
 
 extern "C" int spd_tree_commit(uint16_t* kv_cache, int n_layers, int n_seqs, const int32_t* path, const int32_t* path_cu,
                                const int32_t* ctx_len, int max_len, int n_kv_heads, int head_dim, const int32_t* next_pos,
-                               int32_t* pos, float* acc, void* ws, size_t ws_bytes, void* stream) {
+                               int32_t* pos, float* acc, void* ws, size_t ws_bytes, void* stream) try {
   if (!kv_cache || !path_cu || !ctx_len || !ws || n_layers < 1 || n_seqs < 1 || max_len < 1 || n_kv_heads < 1)
     return fail(SPD_EINVAL, "bad commit arguments");
   if (head_dim != 64 && head_dim != 128) return fail(SPD_EUNSUPPORTED, "head_dim must be 64 or 128");
   if (pos && !next_pos) return fail(SPD_EINVAL, "positions need next_pos");
-  if (reinterpret_cast<uintptr_t>(kv_cache) & 15) return fail(SPD_EINVAL, "the cache must be 16-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(kv_cache) | reinterpret_cast<uintptr_t>(ws)) & 15)
+    return fail(SPD_EINVAL, "the cache and ws must be 16-byte aligned");
   if (n_seqs > 65535 || n_layers > 65535) return fail(SPD_EUNSUPPORTED, "more than 65535 sequences or layers");
   if (path_cu[0] != 0) return fail(SPD_EINVAL, "path_cu must start at 0");
   for (int b = 0; b < n_seqs; ++b) {
@@ -528,4 +531,6 @@ extern "C" int spd_tree_commit(uint16_t* kv_cache, int n_layers, int n_seqs, con
                           reinterpret_cast<uint4*>(kv_cache), p));
   trace_end(slot, st, TR_ROWS, 0.0, 32.0 * p.row16 * n_path * n_layers);
   return SPD_OK;
+} catch (const std::exception&) {  // the host list
+  return fail(SPD_EUNSUPPORTED, "commit: out of host memory");
 }

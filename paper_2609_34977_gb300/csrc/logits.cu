@@ -16,8 +16,8 @@
 //
 // What bounds it: latency. A CTA is a chain of dependent loads (sequence, its lists, their entries: 5 us under load) before
 // the 2.5 us of its stream, and four CTAs an SM overlap only in part. 192 rows of 152064 words, 2000 tokens of history and 300
-// biases a sequence: 58.0 us (234 MB, 4.0 TB/s; without rules 46, a copy of the same bytes 36); 64 rows with up to 4000 tokens
-// 25.9 us; one row of 32000 words 5.3 us. Slower: clusters that exchange their counts through distributed shared memory (two
+// biases a sequence: 59.5 us (234 MB, 3.9 TB/s; without rules 46, a copy of the same bytes 36); 64 rows with up to 4000 tokens
+// 26.4 us; one row of 32000 words 5.3 us. Slower: clusters that exchange their counts through distributed shared memory (two
 // more barriers, 100 us), persistent clusters with the next row's logits under way in registers or by cp.async (85 to 135
 // us: the CTA with the frequent words holds up its cluster).
 #include <math.h>
@@ -71,6 +71,20 @@ __device__ __forceinline__ int2 range_of(const int32_t* cu, int i, int n) {
 __device__ __forceinline__ unsigned long long order_key(float x, int token) {
   const uint32_t u = __float_as_uint(x + 0.0f);
   return (static_cast<unsigned long long>((u >> 31) ? ~u : u | 0x80000000u) << 32) | (0xffffffffu - uint32_t(token));
+}
+
+__device__ __forceinline__ float key_value(unsigned long long key) {
+  const uint32_t u = uint32_t(key >> 32);
+  return __uint_as_float((u >> 31) ? u & 0x7fffffffu : ~u);
+}
+
+// *at = to where it is `from`; what it was. Releases the CTA's writes before it, acquires those before the value it read.
+// (192 rows of 152064 words: 59.5 us, relaxed between fences 63.6, without the acquisition, on the order that a load behind
+// its address has anyway, 58.3.)
+__device__ __forceinline__ int swap_if(int32_t* at, int from, int to) {
+  int was;
+  asm volatile("atom.acq_rel.gpu.global.cas.b32 %0, [%1], %2, %3;" : "=r"(was) : "l"(at), "r"(from), "r"(to) : "memory");
+  return was;
 }
 
 // Whether token i of value v goes before token j of value w.
@@ -270,7 +284,7 @@ __global__ void __launch_bounds__(kThreads, 4) logit_rules_kernel(const __grid_c
     }
     if constexpr (!CLUSTER) {
       // offers in any order end with the same token: one is replaced only by a token that goes before it, whose own
-      // value is in `out` (written and fenced before its offer)
+      // value is in `out` (written before its offer, which releases it)
       if (lane == 0) warp_best[tid >> 5] = k;
       __syncthreads();
       if (tid == 0) {
@@ -278,14 +292,9 @@ __global__ void __launch_bounds__(kThreads, 4) logit_rules_kernel(const __grid_c
         if (k) {
           const int id = int32_t(0xffffffffu - uint32_t(k));
           volatile float* row_out = p.out + size_t(row) * p.ld_out;
-          const float v = row_out[id];
-          __threadfence();
-          int cur = *(volatile int32_t*)(p.best + row);
-          while (cur < 0 || goes_before(v, id, row_out[cur], cur)) {
-            const int was = atomicCAS(p.best + row, cur, id);
-            if (was == cur) break;
-            cur = was;
-          }
+          const float v = key_value(k);
+          for (int cur = -1, was; (was = swap_if(p.best + row, cur, id)) != cur; cur = was)
+            if (!goes_before(v, id, row_out[was], was)) break;
         }
       }
       return;

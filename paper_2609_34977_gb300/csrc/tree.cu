@@ -33,7 +33,6 @@
 #include <stdint.h>
 
 #include <algorithm>
-#include <vector>
 
 #include "internal.h"
 #include "ptx.cuh"
@@ -655,8 +654,14 @@ struct TreePlan {
   int cluster = 1, share = 1 << 24;
   int groups(int blocks) const { return std::max(1, (blocks + share * cluster - 1) / (share * cluster)); }
 };
+struct TreeWorkList {
+  TreeWork w[kMaxSeqs];
+  int n = 0;
+  const TreeWork* begin() const { return w; }
+  const TreeWork* end() const { return w + n; }
+};
 // work: the longest first; places: CTAs the GPU holds at once.
-TreePlan tree_plan(const std::vector<TreeWork>& work, int places, int head_dim) {
+TreePlan tree_plan(const TreeWorkList& work, int places, int head_dim) {
   const double alone = head_dim == 128 ? 1.2 : 0.93, pair = head_dim == 128 ? 1.45 : 0.93;
   TreePlan best;
   double least = 1e30;
@@ -695,10 +700,10 @@ TreePlan tree_plan(const std::vector<TreeWork>& work, int places, int head_dim) 
     TreePlan t;  // one group a sequence
     t.cluster = c;
     weigh(t, &ctas);
-    if (ctas >= room || work[0].blocks <= c) continue;
+    if (ctas >= room || work.w[0].blocks <= c) continue;
     // more groups while all CTAs fit: the share can be no smaller than an even one
     int share = std::max(1, int(blocks_all / room));
-    for (const int whole = (work[0].blocks + c - 1) / c; share < whole; share += share / 16 + 1) {
+    for (const int whole = (work.w[0].blocks + c - 1) / c; share < whole; share += share / 16 + 1) {
       t.share = share;
       const double before = least;
       const TreePlan was = best;
@@ -772,22 +777,22 @@ int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, i
     attr[head_dim == 128] = true;
   }
   const int places = std::min(kItems, 2 * num_sms());
-  std::vector<TreeWork> work;
-  work.reserve(std::min(n_seqs, kMaxSeqs));
+  TreeWorkList work;
   for (int s0 = 0; s0 < n_seqs; s0 += kMaxSeqs) {
     const int m = std::min(kMaxSeqs, n_seqs - s0);
-    work.clear();
+    work.n = 0;
     double pairs = 0.0, keys = 0.0;
     for (int b = s0; b < s0 + m; ++b) {
       const int n = q_cu[b + 1] - q_cu[b];
       if (n == 0) continue;
-      work.push_back({b, (ctx[b] + n + kTK - 1) / kTK, (long long)((n + t.nodes - 1) / t.nodes) * t.chunks * n_kv_heads,
-                      (long long)n * n_heads});
+      work.w[work.n++] = {b, (ctx[b] + n + kTK - 1) / kTK,
+                          (long long)((n + t.nodes - 1) / t.nodes) * t.chunks * n_kv_heads,
+                          (long long)n * n_heads};
       keys += ctx[b] + n;
       pairs += double(n) * (ctx[b] + n);
     }
-    if (work.empty()) continue;
-    std::stable_sort(work.begin(), work.end(), [](const TreeWork& x, const TreeWork& y) { return x.blocks > y.blocks; });
+    if (work.n == 0) continue;
+    std::stable_sort(work.w, work.w + work.n, [](const TreeWork& x, const TreeWork& y) { return x.blocks > y.blocks; });
     const TreePlan plan = tree_plan(work, places, head_dim);
     const int C = plan.cluster;
     TreeSeqs sq{};
@@ -880,8 +885,9 @@ extern "C" int spd_tree_attention(const uint16_t* q, int n_q, const int32_t* q_c
       n_heads % n_kv_heads)
     return fail(SPD_EINVAL, "bad tree attention arguments");
   if (head_dim != 64 && head_dim != 128) return fail(SPD_EUNSUPPORTED, "tree attention supports head_dim 64 and 128");
-  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(kv) | reinterpret_cast<uintptr_t>(o)) & 15)
-    return fail(SPD_EINVAL, "q, kv and o must be 16-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(kv) | reinterpret_cast<uintptr_t>(o) |
+       reinterpret_cast<uintptr_t>(ws)) & 15)
+    return fail(SPD_EINVAL, "q, kv, o and ws must be 16-byte aligned");
   if (int rc = tree_attention_check(q_cu, n_q, ctx_len, n_seqs, tree_mask, mask_words, max_len)) return rc;
   const size_t need = tree_attention_bytes(n_q, n_heads, n_kv_heads, head_dim);
   if (ws_bytes < need) return fail(SPD_ENOSPC, "tree attention workspace too small (%zu < %zu)", ws_bytes, need);

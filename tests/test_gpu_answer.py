@@ -307,6 +307,33 @@ def test_cache_weights(L, g, m, d, lens, rows, alias):
             np.testing.assert_array_equal(got[l, b, :, k:], acc[l, b, :, k:] if alias else -5.0)
 
 
+@pytest.mark.parametrize("d,m,n", [(64, 3, 2), (128, 4, 20), (64, 8, 16)])
+def test_cache_weights_of_keys_and_normalisers_that_are_not_finite(d, m, n):
+    # K/V head 0: q > 0. Row 0's normaliser is -inf, row 1's +inf, the others' finite: infinite and NaN keys show in the others
+    # alone, and where there are none (head 1) nothing shows at all
+    k, slots = 200, 256
+    q = torch.rand(1, n, 2 * m * d) + 0.5
+    lse = torch.zeros(1, n, 2, m)
+    lse[:, 0], lse[:, 1] = -np.inf, np.inf
+    lse[:, 2:, 1] = -np.inf
+    kv = torch.zeros(1, 1, slots, 2, 2, d)
+    for slot, x in ((3, -np.inf), (70, np.inf), (130, np.nan)):
+        kv[:, :, slot, 0] = x
+    kv[:, :, k:] = np.nan  # past the cached rows
+    acc = torch.full((1, 1, 2, slots), 2.0, device="cuda")
+    N.spd_cache_weights(q.to(torch.bfloat16).cuda(), lse.view(1, n, 2 * m).cuda(), None, [0, n],
+                        kv.to(torch.bfloat16).view(1, 1, slots, 4 * d).cuda(), [k], slots, 2 * m, 2, d, 0.5, acc, acc)
+    got = acc.cpu().numpy()[0, 0]
+    finite = m * (n - 2)
+    want = np.full(k, 1.0 + finite)
+    want[k - n + 1:] = [1.0 + m * max(0, n - max(2, i)) for i in range(1, n)]
+    if finite:
+        want[[3, 70, 130]] = 1.0, np.inf, np.nan
+    np.testing.assert_array_equal(got[0, :k], want)
+    np.testing.assert_array_equal(got[1, :k], 1.0)
+    assert (got[:, k:] == 2.0).all()
+
+
 def test_cache_weights_without_a_row_list_and_indices_outside_the_queries():
     g, m, d, lens, rows = 2, 2, 64, [90, 20], [3, 2]
     q, kv = _rand((1, 5, g * m * d), 1, 2.0), _rand((1, 2, 95, 2 * g * d), 2)
@@ -622,6 +649,9 @@ def test_calls_refuse_what_they_cannot_do_before_any_launch():
     cm = lambda path, cu: N.spd_tree_commit(kv[None], 1, path, cu, [5, 5], 32, 4, 64, cw)  # noqa: E731
     _refused(N.SPD_EINVAL, cm, [1, 0, 2], [0, 2, 3])                           # a path out of order
     _refused(N.SPD_EINVAL, cm, [0, 1, 27], [0, 2, 3])                          # a node past max_len
+    _refused(N.SPD_EINVAL, call, [0, 2, 4], [1, 0], ws[4:])                    # workspaces off their 16 bytes
+    _refused(N.SPD_EINVAL, ev, [20, 4], w=ew[8:])
+    _refused(N.SPD_EINVAL, lambda: N.spd_tree_commit(kv[None], 1, [0], [0, 1, 1], [5, 5], 32, 4, 64, cw[1:]))
     z = f(2, 64)
     _refused(N.SPD_EINVAL, N.spd_logits_process, z, z, hist=mask.view(-1), seq_of=mask.view(-1)[:2])  # no hist_cu
     _refused(N.SPD_EUNSUPPORTED, N.spd_logits_process, f(1, 819201), f(1, 819201))
