@@ -25,9 +25,9 @@
 // What bounds it: with two CTAs an SM a block of 64 keys takes 1140 cycles of the SM, below its share of HBM (1400): the K/V
 // stream, with the tensor pipe at 800 and the softmax at 525 under it (single CTAs take 1700 to 2300, S and P V
 // waiting for each other). A CTA costs about 6 us besides: launch and set-up 1, the first loads 2 to 3 (everybody asks at
-// once), the last products, state and merge 2 to 3. 16 nodes on 65521 keys, 28 heads on 4 of 128: 35.9 us, 3.7 TB/s (the
-// merge through memory 5); eight trees of 48 on 640 to 1417 keys, 32 K/V heads: 35.1 us, 4.2 TB/s (the SMs with the two
-// longest sequences); 32 trees on 300 to 1943 keys: 29.4 us; one token, 321 keys, 32 heads: 8.7 us.
+// once), the last products, state and merge 2 to 3. 16 nodes on 65521 keys, 28 heads on 4 of 128: 35.2 us, 3.8 TB/s (the
+// merge through memory 5); eight trees of 48 on 640 to 1417 keys, 32 K/V heads: 35.9 us, 4.1 TB/s (the SMs with the two
+// longest sequences); 32 trees on 300 to 1943 keys: 27.8 us; one token, 321 keys, 32 heads: 8.4 us.
 #include <cuda_bf16.h>
 #include <math.h>
 #include <stdint.h>
@@ -531,9 +531,10 @@ __global__ void __launch_bounds__(kThreads, 2)
 }
 
 // Rows whose keys took several clusters: states (m_i, l_i, O_i) merged in key order, m = max m_i, l = sum l_i 2^(m_i - m),
-// O = sum O_i 2^(m_i - m). W warps a row (node and head), each a range of the parts, eight of them in flight; the kernel is
-// a handful of dependent loads, so long rows of parts want more warps, not longer loops.
-constexpr int kMergeWarps = 8;
+// O = sum O_i 2^(m_i - m). W warps a row (node and head), each a range of the parts, four of them in flight; the kernel is
+// a handful of dependent loads, so long rows of parts want more warps, not longer loops. Whole calls with 4 / 8 parts in
+// flight: 32 trees in 2 to 4 parts 27.8 / 28.6 us, one in 18 parts 35.1 / 35.0; four warps a CTA instead of eight 27.6 and 36.7.
+constexpr int kMergeWarps = 8, kMergeAhead = 4;
 template <int HD>
 __global__ void __launch_bounds__(kMergeWarps * 32)
     tree_merge_kernel(const __grid_constant__ TreeArgs p, const __grid_constant__ TreeSeqs sq, int W) {
@@ -559,13 +560,15 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
     const size_t first = (size_t(sh.part0) + size_t(hk) * parts * tiles + tile) * p.rows_part + r;
     const size_t step = size_t(tiles) * p.rows_part;
     const int s1 = (w + 1) * parts / W;
-    for (int s0 = w * parts / W; s0 < s1; s0 += 8) {
-      float2 ml[8];
-      float v[8][D];
+    for (int s0 = w * parts / W; s0 < s1; s0 += kMergeAhead) {
+      float2 ml[kMergeAhead];
+      float v[kMergeAhead][D];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const size_t at = first + min(s0 + u, s1 - 1) * step;
-        ml[u] = s0 + u < s1 ? p.part_ml[at] : make_float2(-INFINITY, 0.0f);
+      for (int u = 0; u < kMergeAhead; ++u) {
+        ml[u] = make_float2(-INFINITY, 0.0f);
+        if (s0 + u >= s1) continue;
+        const size_t at = first + (s0 + u) * step;
+        ml[u] = p.part_ml[at];
         const float* po = p.part_o + at * HD + D * lane;
         if constexpr (D == 4) {
           const float4 f = *reinterpret_cast<const float4*>(po);
@@ -577,7 +580,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
       }
       float top = m;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) top = fmaxf(top, ml[u].x);
+      for (int u = 0; u < kMergeAhead; ++u) top = fmaxf(top, ml[u].x);
       if (top == -INFINITY) continue;  // nothing seen so far
       const float keep = exp2f(m - top);
       m = top;
@@ -585,7 +588,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
 #pragma unroll
       for (int x = 0; x < D; ++x) o[x] *= keep;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
+      for (int u = 0; u < kMergeAhead; ++u) {
         if (ml[u].x == -INFINITY) continue;  // a part in which the row sees nothing
         const float f = exp2f(ml[u].x - m);
         l = fmaf(ml[u].y, f, l);
@@ -833,7 +836,7 @@ int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, i
     SPD_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, map, p, sq));
     if (most > 0) {
       int W = 1;
-      while (W < kMergeWarps && most_groups > 8 * W) W *= 2;
+      while (W < kMergeWarps && most_groups > kMergeAhead * W) W *= 2;
       SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? tree_merge_kernel<128> : tree_merge_kernel<64>,
                               dim3((most * n_heads * W + kMergeWarps - 1) / kMergeWarps, split), dim3(kMergeWarps * 32), 0, st, p,
                               sq, W));

@@ -5,7 +5,7 @@
 // The normalisers are known, so nothing has to be carried from key to key and V is not read: the call is one pass over K
 // (2 head_dim bytes a slot and K/V head) and one exponential a (slot, row, head).
 //
-// The product is taken the other way round than in attention: S^T = K Q^T with 128 keys as the MMA's M and up to 128 (row,
+// The product is taken the other way round than in attention: S^T = K Q^T with 128 keys as the MMA's M and up to 64 (row,
 // head) pairs as its N. A thread then owns a key (TMEM lane), its sum over the rows stays in its registers, and a
 // decode step's few rows cost few columns instead of 128 mostly empty rows. More than 128 pairs take further passes over the
 // item's keys (from L2), added in order by the same thread. Sums have a fixed order: the same bits in every run.
@@ -374,8 +374,8 @@ extern "C" int spd_cache_weights(const uint16_t* q, const float* lse, int n_q, c
     for (int b = s0; b < s0 + sq.n; ++b) work += (long long)((lens[b] + kTile - 1) / kTile) * n_kv_heads * n_layers;
     // blocks an item: few and long ones, since a CTA's start (Q tile, normalisers, first block) costs several blocks'
     // time: one wave of CTAs where the units allow it, else about two. 8 layers of 32 heads, 24 blocks each, with 6 / 8 / 12 /
-    // 24 blocks an item: 42.0 / 39.7 / 38.3 / 34.5 us; 448 units of 8 to 32 blocks with 4 / 7 / 12 / 16 / 24: 50.4 / 46.2 / 44.4 /
-    // 47.8 / 45.3.
+    // 24 blocks an item: 45.1 / 42.3 / 39.4 / 35.5 us; 448 units of 8 to 32 blocks with 4 / 7 / 12 / 16 / 24: 50.7 / 46.9 / 44.9 /
+    // 49.3 / 46.1.
     auto wave = [&](long long share) {
       long long k = 0;
       for (int b = s0; b < s0 + sq.n; ++b) k += ((lens[b] + kTile - 1) / kTile + share - 1) / share;
