@@ -25,9 +25,9 @@
 // What bounds it: with two CTAs an SM a block of 64 keys takes 1140 cycles of the SM, below its share of HBM (1400): the K/V
 // stream, with the tensor pipe at 800 and the softmax at 525 under it (single CTAs take 1700 to 2300, S and P V
 // waiting for each other). A CTA costs about 6 us besides: launch and set-up 1, the first loads 2 to 3 (everybody asks at
-// once), the last products, state and merge 2 to 3. 16 nodes on 65521 keys, 28 heads on 4 of 128: 35.2 us, 3.8 TB/s (the
-// merge through memory 5); eight trees of 48 on 640 to 1417 keys, 32 K/V heads: 35.9 us, 4.1 TB/s (the SMs with the two
-// longest sequences); 32 trees on 300 to 1943 keys: 27.8 us; one token, 321 keys, 32 heads: 8.4 us.
+// once), the last products, state and merge 2 to 3. 16 nodes on 65521 keys, 28 heads on 4 of 128: 34.8 us, 3.9 TB/s (the
+// merge through memory 4); eight trees of 48 on 640 to 1417 keys, 32 K/V heads: 35.9 us, 4.1 TB/s (the SMs with the two
+// longest sequences); 32 trees on 300 to 1943 keys: 27.5 us; one token, 321 keys, 32 heads: 8.4 us.
 #include <cuda_bf16.h>
 #include <math.h>
 #include <stdint.h>
@@ -534,6 +534,7 @@ __global__ void __launch_bounds__(kThreads, 2)
 // O = sum O_i 2^(m_i - m). W warps a row (node and head), each a range of the parts, four of them in flight; the kernel is
 // a handful of dependent loads, so long rows of parts want more warps, not longer loops. Whole calls with 4 / 8 parts in
 // flight: 32 trees in 2 to 4 parts 27.8 / 28.6 us, one in 18 parts 35.1 / 35.0; four warps a CTA instead of eight 27.6 and 36.7.
+// Where a row's states are is worked out before the wait for them (27.5 and 34.8).
 constexpr int kMergeWarps = 8, kMergeAhead = 4;
 template <int HD>
 __global__ void __launch_bounds__(kMergeWarps * 32)
@@ -542,25 +543,24 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
   __shared__ float2 wml[kMergeWarps];
   __shared__ float wo[kMergeWarps][HD];
   pdl_launch_dependents();
-  pdl_wait();
   const TreeSeq& sh = sq.s[blockIdx.y];
-  const int n = sh.nodes, parts = sh.groups;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp % W;
-  const int row = blockIdx.x * (kMergeWarps / W) + warp / W;
-  const bool have = row < n * p.n_heads;
+  const uint32_t parts = sh.groups, tiles = sh.tiles;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp & (W - 1);
+  const uint32_t row = (blockIdx.x * kMergeWarps + warp) / uint32_t(W);
+  const bool have = row < uint32_t(sh.nodes * p.n_heads);
   float m = -INFINITY, l = 0.0f, o[D];
 #pragma unroll
   for (int x = 0; x < D; ++x) o[x] = 0.0f;
-  const int node = row / p.n_heads, head = row % p.n_heads;
+  const uint32_t node = row / uint32_t(p.n_heads), head = row - node * p.n_heads;
+  const uint32_t hk = head / uint32_t(p.group), hg = head - hk * p.group, chunk = hg / uint32_t(p.chunk);
+  const uint32_t across = node / uint32_t(p.nodes_tile), tile = across * p.chunks + chunk;
+  const uint32_t r = (node - across * p.nodes_tile) * p.chunk + hg - chunk * p.chunk;
+  const size_t first = (size_t(sh.part0) + size_t(hk) * parts * tiles + tile) * p.rows_part + r;
+  const size_t step = size_t(tiles) * p.rows_part;
+  const int s1 = int((w + 1) * parts / uint32_t(W));
+  pdl_wait();
   if (have) {
-    const int hk = head / p.group, hg = head % p.group;
-    const int tiles = sh.tiles;
-    const int tile = node / p.nodes_tile * p.chunks + hg / p.chunk;
-    const int r = node % p.nodes_tile * p.chunk + hg % p.chunk;
-    const size_t first = (size_t(sh.part0) + size_t(hk) * parts * tiles + tile) * p.rows_part + r;
-    const size_t step = size_t(tiles) * p.rows_part;
-    const int s1 = (w + 1) * parts / W;
-    for (int s0 = w * parts / W; s0 < s1; s0 += kMergeAhead) {
+    for (int s0 = int(w * parts / uint32_t(W)); s0 < s1; s0 += kMergeAhead) {
       float2 ml[kMergeAhead];
       float v[kMergeAhead][D];
 #pragma unroll
@@ -646,7 +646,7 @@ int rows_of_part(const TreeTile& t, int n_q) { return std::min(t.nodes, n_q) * t
 // Where the CTAs do not fit on the GPU at once, later ones start as earlier ones end, at 1.3 times the even share of the
 // work. Estimated / measured: one token, 321 keys, 32 heads, cluster 1 / 4 / 8: 13 / 9.4 / 8.2 and 11.2 / 9.2 / 8.7; 32
 // trees on 300 to 1958 keys, 4 K/V heads, no split / cluster 2 / 10 blocks a CTA, merged through memory: 43 / 29.5 / 25 and 43.1 /
-// 33.8 / 30.0; eight of 48 nodes, 32 K/V heads, cluster 1 / 2 / 4: 39 / 46 / 59 and 35.3 / 43.4 / 59.0.
+// 33.8 / 30.0 (27.5 with the present merge); eight of 48 nodes, 32 K/V heads, cluster 1 / 2 / 4: 39 / 46 / 59 and 35.3 / 43.4 / 59.0.
 constexpr double kCtaTime = 6.0, kClusterTime = 1.0, kMergeTime = 4.0, kMergeRow = 0.25e-3, kWaveFactor = 1.3;
 constexpr int kMaxStates = kItems;  // states in memory of a launch: those of plans that fit on the GPU at once
 struct TreeWork {  // a sequence of the launch: key blocks, (tile, K/V head) pairs, (node, head) rows
