@@ -16,8 +16,8 @@
 //
 // What bounds it: latency. A CTA is a chain of dependent loads (sequence, its lists, their entries: 5 us under load) before
 // the 2.5 us of its stream, and four CTAs an SM overlap only in part. 192 rows of 152064 words, 2000 tokens of history and 300
-// biases a sequence: 59.5 us (234 MB, 3.9 TB/s; without rules 46, a copy of the same bytes 36); 64 rows with up to 4000 tokens
-// 26.4 us; one row of 32000 words 5.3 us. Slower: clusters that exchange their counts through distributed shared memory (two
+// biases a sequence: 57.1 us (234 MB, 4.1 TB/s; a copy of the same bytes 36); 64 rows with up to 4000 tokens
+// 26.2 us; one row of 32000 words 5.3 us. Slower: clusters that exchange their counts through distributed shared memory (two
 // more barriers, 100 us), persistent clusters with the next row's logits under way in registers or by cp.async (85 to 135
 // us: the CTA with the frequent words holds up its cluster).
 #include <math.h>
@@ -30,8 +30,11 @@
 namespace spd {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kHeld = 20;                   // tokens of its slice that a thread holds in registers
+// Four CTAs an SM: fewer and larger ones overlap too little of their starts, more find no room for their counts. 192 and 64 rows
+// of 152064 words with 128 x 20 (threads x tokens held), 256 x 20, 320 x 16, 384 x 20 and 512 x 20: 74.3 and 36.2 / 59.5 and
+// 26.4 / 57.1 and 26.2 / 82.1 and 35.0 / 74.8 and 30.6 us.
+constexpr int kThreads = 320, kWarps = kThreads / 32;
+constexpr int kHeld = 16;                   // tokens of its slice that a thread holds in registers
 constexpr int kBatch = kThreads * kHeld;     // tokens a CTA holds at once
 constexpr int kAhead = 2;                    // loads of four tokens of the history that go ahead of the logits
 constexpr int kPlaces = 384;                 // CTAs of rows that clusters still serve as well as CTAs on their own
@@ -79,7 +82,7 @@ __device__ __forceinline__ float key_value(unsigned long long key) {
 }
 
 // *at = to where it is `from`; what it was. Releases the CTA's writes before it, acquires those before the value it read.
-// (192 rows of 152064 words: 59.5 us, relaxed between fences 63.6, without the acquisition, on the order that a load behind
+// (192 rows of 152064 words with 256 threads a CTA: 59.5 us, relaxed between fences 63.6, without the acquisition, on the order that a load behind
 // its address has anyway, 58.3.)
 __device__ __forceinline__ int swap_if(int32_t* at, int from, int to) {
   int was;
