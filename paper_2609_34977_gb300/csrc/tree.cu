@@ -15,9 +15,9 @@
 // tree_merge_kernel.
 //   warp 4     TMA producer: blocks of 64 keys of K and of V into rings
 //   warp 5     MMA issuer: S = Q K^T into TMEM, then O += P V with P read from TMEM, V in place as an MN-major operand
-//   warps 0-3  a thread a row: the block's 64 scores in registers, online softmax in fp32; a weight is held as the sum of two
-//              bf16 terms (16 bits of it, two products: the tensor pipe has the time while K and V stream), the row
-//              sum over the whole weights
+//   warps 0-3  a thread a row: the block's 64 scores in registers, online softmax in fp32; a weight is held as the sum of
+//              three bf16 terms, all 24 bits of it (three products: the tensor pipe has the time while K and V stream): two
+//              over the scores in TMEM, where O leaves no room for more, the third in shared memory
 // Only blocks that reach past the committed rows are masked; there the softmax warps also clear the rows of V behind the last
 // draft (recycled memory) and those that are not finite, which a weight of zero would turn into NaN for rows that
 // do not see them; rows that do see one add it at the end.
@@ -92,11 +92,14 @@ struct TreeSmem {
   static constexpr uint32_t q = 0;
   static constexpr uint32_t k = q + kChunks * kQBox;
   static constexpr uint32_t v = k + kStages * kChunks * kKBox;
-  static constexpr uint32_t ml = v + kStages * kChunks * kKBox;  // [128] a row's maximum and sum (in a cluster)
-  static constexpr uint32_t bars = ml + 128 * 8;
-  static constexpr uint32_t bytes = bars + 256 + 1024;  // + alignment slack
-  static constexpr uint32_t state = k;  // [128][HD] fp32 O of a cluster's merge, over the rings
-  static_assert(128 * HD * 4 <= ml - k, "the rings hold the tile's O");
+  static constexpr uint32_t p3 = v + kStages * kChunks * kKBox;  // [128][64] third terms of a block's weights
+  static constexpr uint32_t bars = p3 + 128 * 128;
+  static constexpr uint32_t bytes = bars + 256;  // (two CTAs an SM: at most 113 KB)
+  // after the last product, of a cluster's merge
+  static constexpr uint32_t ml = q;     // [128] a row's maximum and sum, over the Q tile
+  static constexpr uint32_t state = k;  // [128][HD] fp32 O, over the rings
+  static_assert(128 * HD * 4 <= p3 - k, "the rings hold the tile's O");
+  static_assert(bytes <= 113 * 1024, "two CTAs an SM");
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -136,8 +139,7 @@ __global__ void __launch_bounds__(kThreads, 2)
                      const __grid_constant__ TreeSeqs sq) {
   using L = TreeSmem<HD>;
   constexpr int NS = L::kStages;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  extern __shared__ __align__(1024) uint8_t smem[];  // (the swizzle's atoms; no room to round the address up)
   uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + L::bars);  // [NS] K block landed
   uint64_t* k_empty = k_full + NS;                                 // [NS] its S product has completed
   uint64_t* v_full = k_empty + NS;                                 // [NS] V block landed
@@ -151,6 +153,11 @@ __global__ void __launch_bounds__(kThreads, 2)
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* odd_v = reinterpret_cast<int*>(tmem_slot + 2);  // some visible V is not finite
 
+  if (smem_u32(smem) & 1023) {  // every CTA alike
+    pdl_wait();
+    if (threadIdx.x == 0) set_status(p.status, SPD_ECUDA);
+    return;
+  }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // the cluster's sequence: the last entry that starts at or before it
   const int C = p.cluster, rank = int(blockIdx.x) & (C - 1);
@@ -239,7 +246,7 @@ __global__ void __launch_bounds__(kThreads, 2)
       // ---- MMA issuer ----
       const uint32_t id_s = idesc_bf16_f32(128, kTK);
       const uint32_t id_o = idesc_bf16_f32(128, HD) | (1u << 16);  // V is MN-major
-      const uint32_t sa = smem_u32(smem + L::q);
+      const uint32_t sa = smem_u32(smem + L::q), sp = smem_u32(smem + L::p3);
       bool ok = mbar_wait(q_full, 0, abort_flag, p.budget);
       auto issue_s = [&](int j) -> bool {
         const int s = j % NS;
@@ -265,9 +272,14 @@ __global__ void __launch_bounds__(kThreads, 2)
         tc_fence_after();
         const uint32_t sv = smem_u32(smem + L::v + s * L::kChunks * kKBox);
 #pragma unroll
-        for (int kk = 0; kk < 2 * (kTK / 16); ++kk)  // the weights' first terms, then their second
-          mma_bf16_ts(t_o, tmem + kTK * (j & 1) + 8 * kk, sdesc_mn128(sv + (kk % (kTK / 16)) * 2048, kKBox), id_o,
-                      (j > 0 || kk > 0) ? 1u : 0u);
+        for (int kk = 0; kk < 2 * (kTK / 16); ++kk) {  // the weights' first terms, then their second, then their third
+          const int x = kk % (kTK / 16), term = kk / (kTK / 16);
+          mma_bf16_ts(t_o, tmem + kTK * (j & 1) + 16 * x + 8 * term, sdesc_mn128(sv + x * 2048, kKBox),
+                      id_o, (j > 0 || kk > 0) ? 1u : 0u);
+        }
+#pragma unroll
+        for (int x = 0; x < kTK / 16; ++x)
+          mma_bf16(t_o, sdesc_k128(sp + x * 32), sdesc_mn128(sv + x * 2048, kKBox), id_o, 1u);
         mma_commit(o_done);
         mma_commit(&v_empty[s]);
       }
@@ -368,20 +380,35 @@ __global__ void __launch_bounds__(kThreads, 2)
       }
       const float off = m_run == -INFINITY ? 0.0f : m_run * p.scale_log2;  // nothing seen yet: all weights are 0
       float r4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-      float first[32], second[32];  // the two terms of keys 2 i and 2 i + 1 in word i
+      uint32_t third[kTK / 2];  // keys 2 i and 2 i + 1 in word i
 #pragma unroll
-      for (int i = 0; i < kTK; i += 2) {
-        const float p0 = ex2(fmaf(v[i], p.scale_log2, -off)), p1 = ex2(fmaf(v[i + 1], p.scale_log2, -off));
-        r4[i & 2] += p0;
-        r4[(i & 2) + 1] += p1;
-        const uint32_t hi = pack_bf16(p0, p1);
-        first[i >> 1] = __uint_as_float(hi);
-        second[i >> 1] =
-            __uint_as_float(pack_bf16(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u)));
+      for (int x = 0; x < kTK / 16; ++x) {
+        float first[8], second[8];  // the terms of keys 16 x + 2 i and 16 x + 2 i + 1 in word i
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int k = 16 * x + 2 * i;
+          const float p0 = ex2(fmaf(v[k], p.scale_log2, -off)), p1 = ex2(fmaf(v[k + 1], p.scale_log2, -off));
+          r4[k & 2] += p0;
+          r4[(k & 2) + 1] += p1;
+          const uint32_t hi = pack_bf16(p0, p1);
+          const float a = p0 - __uint_as_float(hi << 16), b = p1 - __uint_as_float(hi & 0xffff0000u);
+          const uint32_t mid = pack_bf16(a, b);
+          first[i] = __uint_as_float(hi);
+          second[i] = __uint_as_float(mid);
+          third[k >> 1] = pack_bf16(a - __uint_as_float(mid << 16), b - __uint_as_float(mid & 0xffff0000u));
+        }
+        tmem_st8(t_s + 16 * x, first);  // over the scores
+        tmem_st8(t_s + 16 * x + 8, second);
       }
       l_run += (r4[0] + r4[1]) + (r4[2] + r4[3]);
-      tmem_st32(t_s, first);  // over the scores
-      tmem_st32(t_s + 32, second);
+      // the third terms' place is free when the block before has been multiplied
+      if (j > 0 && !(ok = __all_sync(0xffffffffu, mbar_wait(o_done, (j - 1) & 1, abort_flag, p.budget)))) break;
+#pragma unroll
+      for (int y = 0; y < 8; ++y)
+        *reinterpret_cast<uint4*>(smem + L::p3 + r * 128 + ((y ^ (r & 7)) << 4)) =
+            make_uint4(third[4 * y], third[4 * y + 1], third[4 * y + 2], third[4 * y + 3]);
+      fence_proxy_async_smem();
+      tmem_st_wait();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&p_full[j & 1]);

@@ -1,0 +1,78 @@
+"""Drafted-token attention where the values are hard: weights that have to keep their bits.
+Plain values in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_34977_gb300 import _native as N
+from tests.gpu_util import bf16_np
+
+pytestmark = pytest.mark.gpu
+LONG = {64: 9000, 128: 9000}  # contexts whose states go through memory (asserted where it matters)
+
+
+def _cu(v):
+    return np.concatenate([[0], np.cumsum(v)]).astype(np.int32)
+
+
+def _call(q, kv, ctx, nodes, g, m, d, mask=None):
+    """o and lse in float64, and whether the workspace holds states (of rows merged through memory)."""
+    n = sum(nodes)
+    o = torch.full((n, g * m * d), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((n, g * m), 7.0, device="cuda")
+    ws = torch.zeros(N.spd_tree_attention_workspace_size(n, len(ctx), g * m, g, d), dtype=torch.uint8, device="cuda")
+    N.spd_tree_attention(q.to(torch.bfloat16).cuda(), _cu(nodes), ctx, mask, kv.to(torch.bfloat16).cuda(), kv.shape[1], g * m, g,
+                         d, o, lse, ws)
+    torch.cuda.synchronize()
+    assert N.spd_workspace_status(ws) == 0
+    return bf16_np(o), lse.cpu().numpy().astype(np.float64), bool((ws[256:] != 0).any())
+
+
+def _bf16(x):
+    return torch.as_tensor(np.asarray(x, np.float32)).to(torch.bfloat16).double().numpy()
+
+
+def _hard_scores(scale):
+    """Four bf16 keys a > 0 whose weights e^(-a scale) lose most in two bf16 terms, all downwards (and by less than 0.85 of the
+    second term's half unit, so that the exponential's own rounding does not turn the loss over)."""
+    a = np.unique(_bf16(np.linspace(0.05, 2.5, 4000)))
+    p = np.exp(-a * scale).astype(np.float32).astype(np.float64)
+    first = p - _bf16(p)
+    loss = first - _bf16(first)
+    safe = np.abs(loss) < 0.85 * 2.0 ** (np.floor(np.log2(np.abs(first))) - 8)
+    return a[np.argsort(-np.where(safe, loss / p, -1.0))[:4]]
+
+
+@pytest.mark.parametrize("d,ctx,at,memory", [(128, 7, 0, False), (64, 7, 0, False), (128, 300, 130, False), (64, 700, 449, False),
+                                             (128, LONG[128], 4100, True), (64, LONG[64], 6000, True)])
+def test_weights_keep_their_24_bits(d, ctx, at, memory):
+    # Scores are exact (one column of q and k); four keys have weights that two bf16 terms do not hold, three keys of weight 1
+    # take their sum away again down to 2^-25 of it, all other weights are below 2^-60. What is left shows a weight's bits.
+    # Tolerance, of sum p |v|: the exponential 2^-22 and its argument 2^-22, products and sums 3 x 2^-23 (three terms, one
+    # slice of 16 keys at most two): below 2^-20; and the output's rounding to bf16. Two terms would lose 2^-18.4.
+    scale = 8.0 / math.sqrt(d)
+    a = _hard_scores(scale)
+    p = np.exp(-a * scale)
+    r = np.random.default_rng(d + ctx)
+    v = _bf16(r.uniform(1.0, 2.0, (4, d)))
+    rest, back = p @ v, []
+    for _ in range(3):
+        back.append(_bf16(-rest))
+        rest = rest + back[-1]
+    q = torch.zeros(1, d)
+    q[0, 0] = 8.0
+    kv = torch.from_numpy(r.standard_normal((1, ctx + 1, 2 * d)).astype(np.float32))
+    kv[0, :, :d] = 0.0
+    kv[0, :, 0] = -64.0
+    kv[0, at:at + 7, 0] = torch.from_numpy(np.concatenate([-a, np.zeros(3)]))
+    kv[0, at:at + 7, d:] = torch.from_numpy(np.concatenate([v, np.stack(back)]))
+    o, _, through_memory = _call(q, kv, [ctx], [1], 1, 1, d)
+    assert through_memory == memory
+    total = p.sum() + 3.0
+    want, size = rest / total, (p @ np.abs(v) + np.abs(np.stack(back)).sum(0)) / total
+    tol = 2.0 ** -8 * np.abs(want) + 2.0 ** -20 * size
+    two = _bf16(p) + _bf16(p - _bf16(p))
+    assert (np.abs((two - p) @ v / total) > tol).all()  # what this test is about
+    assert (np.abs(o[0] - want) <= tol).all(), np.abs(o[0] - want).max() / size.max()
