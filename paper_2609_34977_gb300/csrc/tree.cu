@@ -532,7 +532,7 @@ __global__ void __launch_bounds__(kThreads, 2)
       float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
       for (int k = 0; k < kMaxCluster; ++k) {
-        if (ml[k].x == -INFINITY) continue;  // a part in which the row sees nothing
+        if (ml[k].y == 0.0f) continue;  // a part in which the row sees nothing
         const float f = exp2f(ml[k].x - m);
         l = fmaf(ml[k].y, f, l);
         o.x = fmaf(v[k].x, f, o.x);
@@ -558,7 +558,8 @@ __global__ void __launch_bounds__(kThreads, 2)
 }
 
 // Rows whose keys took several clusters: states (m_i, l_i, O_i) merged in key order, m = max m_i, l = sum l_i 2^(m_i - m),
-// O = sum O_i 2^(m_i - m). W warps a row (node and head), each a range of the parts, four of them in flight; the kernel is
+// O = sum O_i 2^(m_i - m). A part in which the row sees nothing has l_i = 0. (Its maximum does not tell: fmaxf passes over
+// those of parts whose scores are all NaN, whose sums are NaN and stay so.) W warps a row (node and head), each a range of the parts, four of them in flight; the kernel is
 // a handful of dependent loads, so long rows of parts want more warps, not longer loops. Whole calls with 4 / 8 parts in
 // flight: 32 trees in 2 to 4 parts 27.8 / 28.6 us, one in 18 parts 35.1 / 35.0; four warps a CTA instead of eight 27.6 and 36.7.
 // Where a row's states are is worked out before the wait for them (27.5 and 34.8).
@@ -606,9 +607,13 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
         }
       }
       float top = m;
+      bool some = false;
 #pragma unroll
-      for (int u = 0; u < kMergeAhead; ++u) top = fmaxf(top, ml[u].x);
-      if (top == -INFINITY) continue;  // nothing seen so far
+      for (int u = 0; u < kMergeAhead; ++u) {
+        top = fmaxf(top, ml[u].x);
+        some |= ml[u].y != 0.0f;
+      }
+      if (!some) continue;
       const float keep = exp2f(m - top);
       m = top;
       l *= keep;
@@ -616,7 +621,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
       for (int x = 0; x < D; ++x) o[x] *= keep;
 #pragma unroll
       for (int u = 0; u < kMergeAhead; ++u) {
-        if (ml[u].x == -INFINITY) continue;  // a part in which the row sees nothing
+        if (ml[u].y == 0.0f) continue;  // a part in which the row sees nothing
         const float f = exp2f(ml[u].x - m);
         l = fmaf(ml[u].y, f, l);
 #pragma unroll
@@ -636,7 +641,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
     for (int x = 0; x < D; ++x) o[x] = 0.0f;
     for (int k = 0; k < W; ++k) {
       const float2 ml = wml[warp + k];
-      if (ml.x == -INFINITY) continue;
+      if (ml.y == 0.0f) continue;
       const float f = exp2f(ml.x - m);
       l = fmaf(ml.y, f, l);
 #pragma unroll

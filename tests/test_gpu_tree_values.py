@@ -1,4 +1,4 @@
-"""Drafted-token attention where the values are hard: weights that have to keep their bits.
+"""Drafted-token attention where the values are hard: weights that have to keep their bits, NaN in queries and keys.
 Plain values in 64 bits."""
 import math
 
@@ -76,3 +76,49 @@ def test_weights_keep_their_24_bits(d, ctx, at, memory):
     two = _bf16(p) + _bf16(p - _bf16(p))
     assert (np.abs((two - p) @ v / total) > tol).all()  # what this test is about
     assert (np.abs(o[0] - want) <= tol).all(), np.abs(o[0] - want).max() / size.max()
+
+
+# heads, contexts, nodes, and whether the states go through memory: one CTA, a cluster, several tiles a sequence
+PLANS = [(2, 2, 64, [50], [3], False), (32, 1, 128, [321], [1], False), (2, 2, 64, [700, 20], [5, 2], False),
+         (4, 7, 128, [4096], [1], True), (1, 2, 64, [9000], [5], True), (1, 7, 128, [9000], [40], True),
+         (4, 7, 128, [3000, 6000, 40], [4, 9, 1], True)]
+
+
+def _random(seed, g, m, d, ctx, nodes):
+    r = torch.Generator().manual_seed(seed)
+    slots = max(c + n for c, n in zip(ctx, nodes)) + 1
+    q = torch.randn(sum(nodes), g * m * d, generator=r).to(torch.bfloat16)
+    return q, torch.randn(len(ctx), slots, 2 * g * d, generator=r).to(torch.bfloat16)
+
+
+@pytest.mark.parametrize("g,m,d,ctx,nodes,memory", PLANS)
+def test_a_query_that_is_nan_shows_in_its_row_and_head(g, m, d, ctx, nodes, memory):
+    q, kv = _random(1, g, m, d, ctx, nodes)
+    want, want_lse, through_memory = _call(q, kv, ctx, nodes, g, m, d)
+    assert through_memory == memory
+    row, head = sum(nodes) - 1, g * m - 1
+    q[row, head * d + 3] = float("nan")
+    o, lse, _ = _call(q, kv, ctx, nodes, g, m, d)
+    bad = np.zeros_like(want, bool)
+    bad[row, head * d:] = True
+    assert np.isnan(o[bad]).all() and np.isnan(lse[row, head])
+    lse[row, head] = want_lse[row, head]
+    np.testing.assert_array_equal(o[~bad], want[~bad])
+    np.testing.assert_array_equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("g,m,d,ctx,nodes,memory", PLANS)
+@pytest.mark.parametrize("first,last", [(0.0, 0.0), (0.0, 0.3), (0.5, 0.5), (0.6, 1.0), (0.0, 1.0)])
+def test_committed_keys_that_are_nan_show_in_every_row_of_their_head(g, m, d, ctx, nodes, memory, first, last):
+    # single keys, whole parts of a row's keys, all of them; the other K/V heads and sequences do not see them
+    q, kv = _random(2, g, m, d, ctx, nodes)
+    want, want_lse, _ = _call(q, kv, ctx, nodes, g, m, d)
+    kv[0, int(first * (ctx[0] - 1)):int(last * (ctx[0] - 1)) + 1, :d] = float("nan")
+    o, lse, through_memory = _call(q, kv, ctx, nodes, g, m, d)
+    assert through_memory == memory
+    bad = np.zeros_like(want, bool)
+    bad[:nodes[0], :m * d] = True
+    assert np.isnan(o[bad]).all() and np.isnan(lse[:nodes[0], :m]).all()
+    lse[:nodes[0], :m] = want_lse[:nodes[0], :m]
+    np.testing.assert_array_equal(o[~bad], want[~bad])
+    np.testing.assert_array_equal(lse, want_lse)
