@@ -402,7 +402,9 @@ size_t spd_tree_attention_workspace_size(int n_q, int n_seqs, int n_heads, int n
  * and behind them, at slots ctx_len[b] + i, the rows of its nodes i = 0 .. q_cu[b + 1] - q_cu[b] - 1. Per head (head h
  * reads K/V head h / (n_heads / n_kv_heads)), over the committed rows and the drafts of its own sequence that node i sees:
  *   o_i = sum_j softmax_j(q_i . k_j / sqrt(head_dim)) v_j,   lse_i = log sum_j exp(q_i . k_j / sqrt(head_dim)).
- * A row that sees nothing gets o = 0 and lse = -inf. What a row does not see contributes nothing, whatever it holds.
+ * A row that sees nothing gets o = 0 and lse = -inf. What a row does not see contributes nothing, whatever it holds. NaN in a
+ * query or in a key that is seen gives NaN; an infinite V that is seen gives the infinity (perhaps NaN where its
+ * weight is below 2^-100 of the row's largest).
  * One node a sequence is a decode step; a chain (tree_mask NULL) is a causal window.
  * q, o (dev) bf16 [n_q][n_heads * head_dim], the nodes of sequence b in rows [q_cu[b], q_cu[b + 1]) (none is allowed);
  * q_cu (HOST) int32 [n_seqs + 1] from 0 to n_q; ctx_len (HOST) int32 [n_seqs]; tree_mask (dev) uint32

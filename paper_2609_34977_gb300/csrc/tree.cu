@@ -420,6 +420,40 @@ __global__ void __launch_bounds__(kThreads, 2)
       if (C > 1) *reinterpret_cast<float2*>(smem + L::ml + r * 8) = make_float2(-INFINITY, 0.0f);
     } else {
       tc_fence_after();
+      // A committed V that is infinite: the products of a weight's terms, which can be 0 or negative, are NaN together. Which
+      // infinity a column has is the same for every row (all see every committed key, with a weight above 0).
+      float sick = 0.0f;  // NaN where a column is not finite
+#pragma unroll 1
+      for (int c = 0; c < HD / 32; ++c) {
+        float ov[32];
+        tmem_ld32(t_o + lanes + c * 32, ov);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) sick = fmaf(ov[i], 0.0f, sick);
+      }
+      const bool mend = valid && isnan(sick) && !isnan(l_run);  // (scores that are NaN leave the row NaN)
+      if (__any_sync(0xffffffffu, mend)) {
+        constexpr int E = HD / 32;  // columns a lane looks through
+        const size_t ld = 2 * size_t(p.n_kv_heads) * HD;
+        const __nv_bfloat16* vc = p.kv + size_t(row0) * ld + (size_t(p.n_kv_heads) + hk) * HD + E * lane;
+        uint32_t has = 0;  // of column e in bits 4 e: +inf, -inf, NaN
+        for (int k = b0 * kTK; k < min(ctx, (b0 + nkb) * kTK); ++k)
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const float x = __bfloat162float(vc[k * ld + e]);
+            has |= (isnan(x) ? 4u : x == INFINITY ? 1u : x == -INFINITY ? 2u : 0u) << (4 * e);
+          }
+#pragma unroll 1
+        for (int c = 0; c < HD / 32; ++c) {
+          float ov[32];
+          tmem_ld32(t_o + lanes + c * 32, ov);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const uint32_t h = (__shfl_sync(0xffffffffu, has, (c * 32 + i) / E) >> (4 * (i % E))) & 15u;
+            if (mend && isnan(ov[i]) && (h == 1u || h == 2u)) ov[i] = h == 1u ? INFINITY : -INFINITY;
+          }
+          tmem_st32(t_o + lanes + c * 32, ov);
+        }
+      }
       if (*reinterpret_cast<volatile int*>(odd_v)) {
         // drafts whose V was cleared: rows that see one add p v in fp32 (the score again from q and k)
         const float off = m_run == -INFINITY ? 0.0f : m_run * p.scale_log2;

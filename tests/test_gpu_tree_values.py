@@ -1,4 +1,5 @@
-"""Drafted-token attention where the values are hard: weights that have to keep their bits, NaN in queries and keys.
+"""Drafted-token attention where the values are hard: weights that have to keep their bits, NaN in queries and keys,
+infinite values.
 Plain values in 64 bits."""
 import math
 
@@ -121,4 +122,57 @@ def test_committed_keys_that_are_nan_show_in_every_row_of_their_head(g, m, d, ct
     assert np.isnan(o[bad]).all() and np.isnan(lse[:nodes[0], :m]).all()
     lse[:nodes[0], :m] = want_lse[:nodes[0], :m]
     np.testing.assert_array_equal(o[~bad], want[~bad])
+    np.testing.assert_array_equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("g,m,d,ctx,nodes,memory", PLANS)
+def test_infinite_committed_values_show_as_what_they_are(g, m, d, ctx, nodes, memory):
+    # columns of the first K/V head's V: one infinity early, one in every slot (the row's largest weight too, whose first term
+    # is the whole weight), the other sign late, both signs, NaN. Weights of a row are within 2^15 of each other.
+    q, kv = _random(3, g, m, d, ctx, nodes)
+    q = (0.3 * q).to(torch.bfloat16)
+    want, want_lse, through_memory = _call(q, kv, ctx, nodes, g, m, d)
+    assert through_memory == memory
+    v, n, inf = kv[0, :, g * d:], ctx[0], float("inf")
+    v[1, 5] = inf
+    v[:n, 17] = inf
+    v[n - 1, d - 1] = -inf
+    v[0, 20], v[n - 2, 20] = inf, -inf
+    v[n // 2, 33] = float("nan")
+    o, lse, _ = _call(q, kv, ctx, nodes, g, m, d)
+    for h in range(m):
+        for c, x in ((5, inf), (17, inf), (d - 1, -inf), (20, np.nan), (33, np.nan)):
+            np.testing.assert_array_equal(o[:nodes[0], h * d + c], x)
+            o[:nodes[0], h * d + c] = want[:nodes[0], h * d + c]
+    np.testing.assert_array_equal(o, want)
+    np.testing.assert_array_equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("d,ctx,at", [(128, 7, 3), (64, 300, 140), (128, 9000, 4107)])
+def test_an_infinite_value_under_a_small_weight(d, ctx, at):
+    # e^-62 = 2^-89.4 of the weight of its neighbour, which is the row's largest
+    q, kv = torch.zeros(1, d), torch.ones(1, ctx + 1, 2 * d)
+    q[0, 0] = 8.0
+    kv[0, :, 0] = -80.0 * math.sqrt(d) / 8.0
+    kv[0, at - 1, 0] = 0.0
+    kv[0, at, 0] = -62.0 * math.sqrt(d) / 8.0
+    kv[0, at, d + 7] = float("inf")
+    o, _, _ = _call(q, kv, [ctx], [1], 1, 1, d)
+    assert np.isposinf(o[0, 7]) and (np.delete(o[0], 7) == 1.0).all()
+
+
+@pytest.mark.parametrize("g,m,d,ctx,nodes,memory", PLANS)
+def test_infinite_values_of_drafts_show_in_the_rows_that_see_them(g, m, d, ctx, nodes, memory):
+    q, kv = _random(4, g, m, d, ctx, nodes)
+    q = (0.3 * q).to(torch.bfloat16)
+    want, want_lse, through_memory = _call(q, kv, ctx, nodes, g, m, d)
+    assert through_memory == memory
+    at = nodes[0] // 2  # a chain: the nodes from `at` on see it
+    kv[0, ctx[0] + at, g * d + 9] = -float("inf")
+    o, lse, _ = _call(q, kv, ctx, nodes, g, m, d)
+    for h in range(m):
+        assert np.isneginf(o[at:nodes[0], h * d + 9]).all()
+        o[at:nodes[0], h * d + 9] = want[at:nodes[0], h * d + 9]
+    # the draft's other values enter in fp32 products of their own: the outputs' two roundings to bf16 at most
+    np.testing.assert_allclose(o, want, rtol=2.0 ** -7, atol=2.0 ** -12)
     np.testing.assert_array_equal(lse, want_lse)
