@@ -28,6 +28,9 @@ class TreeAnswer:
     first and n_recent last positions stay, the others by the weight that they received (decay: what a step leaves of the
     total). rules: what spd_logits_process takes per sequence (repetition, frequency, presence: fp32 [n_seqs]; bias_cu,
     bias_id, bias; allow), and `rule`, a callable (sequence, generated tokens) -> row of allow or -1.
+
+    Where a device-side wait ran out, start() and step() raise SpiderError before they take over any token, and so does every
+    later call: what the cache holds is not to be relied on.
     """
 
     def __init__(self, model: N.SpdModel, embed, n_seqs: int, max_len: int, *, max_nodes: int = 32, budget: int | None = None,
@@ -55,13 +58,15 @@ class TreeAnswer:
         self.ws_evict = None
         if budget is not None:
             self.ws_evict = torch.zeros(N.spd_cache_evict_workspace_size(L, n_seqs, G, budget), dtype=torch.uint8, **dev)
-        self._n = 0
+        self._status = 0                              # the first failure of workspaces that are gone
+        self._n, self.ws = 0, None
         self._room(n_seqs * max_nodes)
 
     def _room(self, n):
         """Buffers of a step of up to n nodes in all."""
         if n <= self._n:
             return
+        self._note(self.ws)  # (it is replaced below)
         self._n = n
         c, dev = self.cfg, dict(device="cuda")
         self.logits = torch.empty(n, c["vocab"], **dev)
@@ -100,7 +105,7 @@ class TreeAnswer:
         self._room(int(q_cu[-1]))
         xt = x.index_select(0, torch.from_numpy(at(cu[1:] - tail, cu[1:])).to(x.device))
         depth = at(np.zeros_like(tail), tail)
-        best = self._forward(xt, q_cu, None, depth, [[] for _ in range(len(depth))])
+        best = self._forward(xt, q_cu, None, depth, [[] for _ in range(len(depth))], ws)
         self._accept([list(range(k)) for k in tail], q_cu)
         self.pending = [int(best[q_cu[b + 1] - 1]) for b in range(self.B)]
         return list(self.pending)
@@ -150,8 +155,8 @@ class TreeAnswer:
         self._accept(accepted, q_cu)
         return gained
 
-    def _forward(self, x, q_cu, mask, depth, paths):
-        """A pass over packed nodes; returns the best token of each after the rules (host)."""
+    def _forward(self, x, q_cu, mask, depth, paths, ws_prompt=None):
+        """A pass over packed nodes; returns the best token of each after the rules (host), or raises what the device recorded."""
         c, n = self.cfg, int(q_cu[-1])
         per = np.repeat(self.next_pos, np.diff(q_cu))
         N.spd_decode_tree(self.model, x, q_cu, self.lens, per + depth, mask, self.kv, self.max_len, self.logits, self.ws,
@@ -169,7 +174,11 @@ class TreeAnswer:
             said = [self.hist[b][self.n_prompt[b]:] for b in range(self.B)]
             kw["rule"] = up([self.rule(int(b), said[b] + p) if self.rule else 0 for b, p in zip(seq, paths)])
         N.spd_logits_process(self.logits[:n], self.logits[:n], self.best, seq_of=up(seq), **kw)
-        return self.best[:n].cpu().numpy()
+        best = self.best[:n].cpu().numpy()
+        self._note(ws_prompt)
+        if self.status():
+            raise N.SpiderError(self.status(), "a device-side wait of this answer ran out")
+        return best
 
     def _accept(self, paths, q_cu):
         """Commits every sequence's accepted nodes, adds the weight they gave, and evicts back to the budget."""
@@ -192,9 +201,15 @@ class TreeAnswer:
             self.lens = N.spd_cache_evict(self.kv, self.lens, self.max_len, G, d, self.budget, self.n_sink, self.n_recent,
                                           self.next_pos, self.acc, self.pos, self.acc, self.pos, None, self.ws_evict)
 
+    def _note(self, ws):
+        """Keeps a failure that a workspace holds, unless there is an earlier one."""
+        if ws is not None and not self._status:
+            self._status = N.spd_workspace_status(ws)
+
     def status(self) -> int:
-        """First device-side failure recorded by the steps (0 = OK; synchronises)."""
-        return N.spd_workspace_status(self.ws)
+        """First device-side failure recorded by prompts and steps (0 = OK; synchronises)."""
+        self._note(self.ws)
+        return self._status
 
 
 def ngram_drafts(text, n: int, width: int = 2, vocab: int | None = None):
