@@ -492,8 +492,9 @@ extern "C" int spd_tree_commit(uint16_t* kv_cache, int n_layers, int n_seqs, con
     return fail(SPD_EINVAL, "the cache and ws must be 16-byte aligned");
   if (n_seqs > 65535 || n_layers > 65535) return fail(SPD_EUNSUPPORTED, "more than 65535 sequences or layers");
   if (path_cu[0] != 0) return fail(SPD_EINVAL, "path_cu must start at 0");
-  for (int b = 0; b < n_seqs; ++b) {
+  for (int b = 0; b < n_seqs; ++b)
     if (path_cu[b + 1] < path_cu[b]) return fail(SPD_EINVAL, "path_cu decreases at sequence %d", b);
+  for (int b = 0; b < n_seqs; ++b) {  // (path holds path_cu[n_seqs] entries, which no range passes now)
     if (ctx_len[b] < 0 || ctx_len[b] > max_len) return fail(SPD_EINVAL, "context of sequence %d outside [0, max_len]", b);
     for (int i = path_cu[b]; i < path_cu[b + 1]; ++i) {
       if (!path) return fail(SPD_EINVAL, "null path");

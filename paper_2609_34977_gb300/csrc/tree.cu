@@ -923,7 +923,9 @@ extern "C" int spd_tree_mask(int n_seqs, const int32_t* q_cu, const int32_t* par
     const int n = q_cu[b + 1] - q_cu[b];
     if (n < 0) return fail(SPD_EINVAL, "q_cu decreases at sequence %d", b);
     if (n > 32 * words) return fail(SPD_EINVAL, "sequence %d: %d nodes do not fit in %d mask words", b, n, words);
-    for (int i = 0; i < n; ++i) {
+  }
+  for (int b = 0; b < n_seqs; ++b) {  // (parent holds q_cu[n_seqs] entries, which no range passes now)
+    for (int i = 0; i < q_cu[b + 1] - q_cu[b]; ++i) {
       const int up = parent[q_cu[b] + i];
       if (up < -1 || up >= i) return fail(SPD_EINVAL, "sequence %d: the parent of node %d must come before it", b, i);
     }
