@@ -22,5 +22,5 @@ def test_lists_are_not_read_past_their_end(lib, cu):  # noqa: F811
     n, ws = len(cu) - 1, _Somewhere("uint8", 1 << 12)
     whole = np.array([0, 1, 2, 0, 0], np.int32)
     with pytest.raises(N.SpiderError, match="path_cu decreases") as e:
-        N.spd_tree_commit(_Somewhere("bfloat16", n * 16 * 256), 1, whole[:3], cu, [1] * n, 16, 2, 64, ws)
+        N.spd_tree_commit(_Somewhere("bfloat16", n * 16 * 256), 1, whole[:3], cu, [1] * n, 16, 2, 64, ws, stream=0)
     assert e.value.code == N.SPD_EINVAL
