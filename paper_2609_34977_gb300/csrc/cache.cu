@@ -291,16 +291,16 @@ SelectKernel pick_select(int move) {
 }
 
 // The rows themselves: a warp a move, 16 bytes a lane (half a warp K, half V; HD = 64: a quarter each), four moves in
-// flight a warp. HBM: 175 K moves of 1 KB (read and written) in 25 us, 7.1 TB/s. Moving inside the selecting kernel saves a launch
+// flight a warp; `ctas` CTAs a unit, side by side. HBM: 175 K moves of 1 KB (read and written) in 25 us, 7.1 TB/s. Moving inside the selecting kernel saves a launch
 // and loses the occupancy: 46.8 against 44.1 us for the whole call.
 constexpr int kMoveWarps = 8, kMoveDepth = 4;
 template <int HD>
-__global__ void __launch_bounds__(kMoveWarps * 32) evict_move_kernel(uint16_t* kv, const __grid_constant__ EvictArgs p) {
+__global__ void __launch_bounds__(kMoveWarps * 32) evict_move_kernel(uint16_t* kv, const __grid_constant__ EvictArgs p, int ctas) {
   constexpr int VEC = HD / 8;  // 16-byte pieces of a head's K or V row
   constexpr int ROWS = 32 / (2 * VEC);  // moves a warp takes at once
   pdl_launch_dependents();
   pdl_wait();
-  const int local = blockIdx.y, per_layer = p.launch_seqs * p.n_kv_heads, layer = local / per_layer;
+  const int local = int(blockIdx.x / uint32_t(ctas)), per_layer = p.launch_seqs * p.n_kv_heads, layer = local / per_layer;
   const int at = local - layer * per_layer, ls = at / p.n_kv_heads, g = at - ls * p.n_kv_heads;
   const size_t seq = size_t(layer) * p.n_seqs + p.seq0 + ls, unit = seq * p.n_kv_heads + g;
   const int moves = p.moves[unit];
@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(kMoveWarps * 32) evict_move_kernel(uint16_t* k
   const int col = (e / VEC) * kvd + g * HD + (e % VEC) * 8;
   uint16_t* base = kv + seq * p.max_len * (2 * size_t(kvd)) + col;
   const int32_t *fill = p.fill + unit * p.budget, *hole = p.hole + unit * p.budget;
-  const int j0 = (blockIdx.x * kMoveWarps + warp) * (kMoveDepth * ROWS) + sub;
+  const int j0 = (int(blockIdx.x - uint32_t(local) * ctas) * kMoveWarps + warp) * (kMoveDepth * ROWS) + sub;
   uint4 v[kMoveDepth];
 #pragma unroll
   for (int u = 0; u < kMoveDepth; ++u)
@@ -397,7 +397,6 @@ extern "C" int spd_cache_evict(uint16_t* kv_cache, int n_layers, int n_seqs, con
   if (longest > kSelMost * kSelMaxCluster)
     return fail(SPD_EUNSUPPORTED, "eviction from more than %d rows", kSelMost * kSelMaxCluster);
   const size_t units = size_t(n_layers) * n_seqs * n_kv_heads;
-  if (units > 65535) return fail(SPD_EUNSUPPORTED, "more than 65535 layers x sequences x K/V heads");
   Carve cv(ws, ws_bytes);
   EvictArgs p{};
   p.fill = cv.take<int32_t>(units * budget);
@@ -426,6 +425,9 @@ extern "C" int spd_cache_evict(uint16_t* kv_cache, int n_layers, int n_seqs, con
   per = (per + 3) & ~3;
   // moves that the selecting CTA makes itself: where a unit has few of them, the second launch costs more
   const bool fused = most_moves <= kFusedMoves, small = per <= kSelSmall;
+  const int rows_cta = kMoveWarps * kMoveDepth * (128 / head_dim), ctas = (most_moves + rows_cta - 1) / rows_cta;
+  if (units * std::max(C, ctas) > 0x7fffffff)
+    return fail(SPD_EUNSUPPORTED, "eviction from %zu layers x sequences x K/V heads of up to %d rows", units, longest);
   const int threads = !small ? kSelWide : units * C > 3 * size_t(num_sms()) ? 256 : 512;
   const int move = fused ? head_dim : 0;
   const auto select = threads == 256   ? pick_select<256>(move)
@@ -463,11 +465,9 @@ extern "C" int spd_cache_evict(uint16_t* kv_cache, int n_layers, int n_seqs, con
     SPD_CUDA_TRY(cudaLaunchKernelEx(&cfg, select, kv_cache, p, sq, per));
     trace_end(slot, st, TR_ROWS, 0.0, 16.0 * rows * n_layers * n_kv_heads);
     if (!fused) {
-      const int rows_cta = kMoveWarps * kMoveDepth * (128 / head_dim);
-      const dim3 grid((most_moves + rows_cta - 1) / rows_cta, n);
       slot = trace_begin(st);
-      SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? evict_move_kernel<128> : evict_move_kernel<64>, grid, dim3(kMoveWarps * 32), 0,
-                              st, kv_cache, p));
+      SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? evict_move_kernel<128> : evict_move_kernel<64>, dim3(unsigned(n) * ctas),
+                              dim3(kMoveWarps * 32), 0, st, kv_cache, p, ctas));
       trace_end(slot, st, TR_ROWS, 0.0, 8.0 * head_dim * moved * n_layers * n_kv_heads);
     }
   }
