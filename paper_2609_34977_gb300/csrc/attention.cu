@@ -319,12 +319,10 @@ int launch(const CUtensorMap& mq, const CUtensorMap& mkv, void* o, int ldo, cons
            int n_tiles, const int32_t* q_pos, int n_heads, int n_kv_heads, int v_off, int* status,
            cudaStream_t stream, unsigned long long* stamp) {
   using L = AttnSmem<HD>;
-  static bool attr = false;
-  if (!attr) {
-    SPD_CUDA_TRY(cudaFuncSetAttribute(attn_tc_kernel<HD>,
-                                      cudaFuncAttributeMaxDynamicSharedMemorySize, int(L::bytes)));
-    attr = true;
-  }
+  static DeviceOnce attr;
+  SPD_CUDA_TRY(once_per_device(attr, [] {
+    return cudaFuncSetAttribute(attn_tc_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(L::bytes));
+  }));
   const float scale_log2 = 1.4426950408889634f / sqrtf(float(HD));
   SPD_CUDA_TRY(launch_pdl(attn_tc_kernel<HD>, dim3(n_tiles * n_heads), dim3(kThreads), L::bytes,
                           stream, mq, mkv, static_cast<__nv_bfloat16*>(o), ldo, tiles, n_tiles, q_pos,

@@ -7,6 +7,7 @@
 
 #include <utility>
 
+#include "device_once.h"
 #include "spider.h"
 
 namespace spd {
@@ -26,6 +27,13 @@ constexpr long long kWaitBudget = 1ll << 30;
 
 int num_sms();  // SM count of the current device
 
+// set() (a cudaError_t) once for the current device, as DeviceOnce::run.
+template <typename F>
+cudaError_t once_per_device(DeviceOnce& once, F&& set) {
+  int dev = 0;
+  if (cudaError_t e = cudaGetDevice(&dev)) return e;
+  return static_cast<cudaError_t>(once.run(dev, [&] { return static_cast<int>(set()); }));
+}
 
 // Launches a kernel with programmatic stream serialization: it may be scheduled while the previous
 // kernel of the stream is still running, and orders itself after it with griddepcontrol.wait.

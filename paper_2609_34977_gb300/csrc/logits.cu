@@ -403,13 +403,11 @@ extern "C" int spd_logits_process(const float* logits, int n_rows, int vocab, in
   if (apart && best)
     SPD_CUDA_TRY(launch_pdl(no_best_kernel, dim3((n_rows + kThreads - 1) / kThreads), dim3(kThreads), 0, st, best, n_rows));
   const size_t smem = size_t(p.slice) * 4;
-  static bool prepared[4] = {};
-  bool& set = prepared[2 * vec + apart];
-  if (!set) {
-    SPD_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSlice * 4));
-    SPD_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-    set = true;
-  }
+  static DeviceOnce prepared[4];
+  SPD_CUDA_TRY(once_per_device(prepared[2 * vec + apart], [&] {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSlice * 4);
+    return e ? e : cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  }));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(n_rows * C);
   cfg.blockDim = dim3(kThreads);

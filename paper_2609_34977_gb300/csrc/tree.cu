@@ -840,11 +840,10 @@ int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, i
   p.budget = kWaitBudget;
   const auto kernel = head_dim == 128 ? tree_attn_kernel<128> : tree_attn_kernel<64>;
   const size_t smem = head_dim == 128 ? TreeSmem<128>::bytes : TreeSmem<64>::bytes;
-  static bool attr[2] = {};
-  if (!attr[head_dim == 128]) {
-    SPD_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
-    attr[head_dim == 128] = true;
-  }
+  static DeviceOnce attr[2];
+  SPD_CUDA_TRY(once_per_device(attr[head_dim == 128], [&] {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+  }));
   const int places = std::min(kItems, 2 * num_sms());
   TreeWorkList work;
   for (int s0 = 0; s0 < n_seqs; s0 += kMaxSeqs) {

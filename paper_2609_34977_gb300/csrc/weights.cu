@@ -357,14 +357,12 @@ extern "C" int spd_cache_weights(const uint16_t* q, const float* lse, int n_q, c
   p.acc_out = acc_out;
   p.status = static_cast<int*>(ws);
   p.budget = kWaitBudget;
-  static bool attr = false;
-  if (!attr) {
-    SPD_CUDA_TRY(cudaFuncSetAttribute(weights_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                      int(WeightSmem<128>::bytes)));
-    SPD_CUDA_TRY(cudaFuncSetAttribute(weights_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                      int(WeightSmem<64>::bytes)));
-    attr = true;
-  }
+  const auto kernel = head_dim == 128 ? weights_kernel<128> : weights_kernel<64>;
+  const size_t smem = head_dim == 128 ? WeightSmem<128>::bytes : WeightSmem<64>::bytes;
+  static DeviceOnce attr[2];
+  SPD_CUDA_TRY(once_per_device(attr[head_dim == 128], [&] {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+  }));
   for (int s0 = 0; s0 < n_seqs; s0 += kMaxSeqs) {
     WeightSeqs sq{};
     sq.n = std::min(kMaxSeqs, n_seqs - s0);
@@ -399,8 +397,7 @@ extern "C" int spd_cache_weights(const uint16_t* q, const float* lse, int n_q, c
     const double fl = 2.0 * head_dim * n_heads * pairs * n_layers, by = keys * n_layers * n_kv_heads * (2.0 * head_dim + 8.0);
     p.stamp = stamp_slot(TR_ATTN, fl, by);
     const int slot = trace_begin(st);
-    SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? weights_kernel<128> : weights_kernel<64>, dim3(unsigned(items), n_layers),
-                            dim3(kThreads), head_dim == 128 ? WeightSmem<128>::bytes : WeightSmem<64>::bytes, st, map, p, sq));
+    SPD_CUDA_TRY(launch_pdl(kernel, dim3(unsigned(items), n_layers), dim3(kThreads), smem, st, map, p, sq));
     trace_end(slot, st, TR_ATTN, fl, by);
   }
   return SPD_OK;
