@@ -9,6 +9,7 @@ import torch
 
 from paper_2609_34977_gb300 import _native as N
 from tests.gpu_util import bf16_np
+from tests.test_gpu_answer import _plain_rows, _tree_case
 
 pytestmark = pytest.mark.gpu
 LONG = {64: 9000, 128: 9000}  # contexts whose states go through memory (asserted where it matters)
@@ -176,3 +177,23 @@ def test_infinite_values_of_drafts_show_in_the_rows_that_see_them(g, m, d, ctx, 
     # the draft's other values enter in fp32 products of their own: the outputs' two roundings to bf16 at most
     np.testing.assert_allclose(o, want, rtol=2.0 ** -7, atol=2.0 ** -12)
     np.testing.assert_array_equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("g,m,d,ctx,nodes,form", [
+    (1, 7, 128, [9000], [40], "tree"),           # three tiles of 18 nodes a part
+    (1, 200, 64, [6000], [3], "tree"),           # a group of heads wider than a tile: two tiles a node
+    (1, 2, 64, [9000], [130], "chain"),          # three tiles of 64 nodes
+    (2, 3, 128, [7000, 5000, 30], [60, 3, 90], "any"),  # sequences of several parts and of one, each of several tiles
+])
+def test_merge_through_memory_of_several_tiles(g, m, d, ctx, nodes, form):
+    q, kv, see, mask, _ = _tree_case(17, g, m, d, ctx, nodes, form)
+    o, lse, through_memory = _call(q, kv, ctx, nodes, g, m, d, torch.from_numpy(mask).cuda())
+    assert through_memory
+    cu, q = _cu(nodes), bf16_np(q)
+    for b, (c, n) in enumerate(zip(ctx, nodes)):
+        rows = slice(cu[b], cu[b + 1])
+        full = np.concatenate([np.ones((n, c), bool), see[b]], 1)
+        want, want_lse, tol, tol_lse = _plain_rows(q[rows], bf16_np(kv[b, :c + n]), full, g, m, d)
+        assert (np.abs(lse[rows] - want_lse) <= tol_lse).all()
+        bad = np.abs(o[rows] - want) > tol
+        assert not bad.any(), (b, bad.sum(), np.abs(o[rows] - want).max())
