@@ -694,6 +694,8 @@ def spd_logits_process(logits, out, best=None, *, seq_of=None, hist=None, hist_c
     n_hist, n_path = 0 if hist is None else hist.numel(), 0 if path is None else path.numel()
     n_bias = 0 if bias is None else bias.numel()
     words = (v + 31) // 32
+    if allow is not None and (allow.numel() % words or (len(allow.shape) > 1 and allow.shape[-1] != words)):
+        raise ValueError(f"allow: shape {tuple(allow.shape)}, a grammar's row is {words} words of 32 tokens")
     n_rules = 0 if allow is None else allow.numel() // words
     r = LogitsRules(_dev(seq_of, "i32", n, "seq_of", True), B, _dev(hist, "i32", 0, "hist", True),
                     _dev(hist_cu, "i32", B + 1, "hist_cu", True), _dev(gen_start, "i32", B, "gen_start", True), n_hist,

@@ -24,3 +24,20 @@ def test_lists_are_not_read_past_their_end(lib, cu):  # noqa: F811
     with pytest.raises(N.SpiderError, match="path_cu decreases") as e:
         N.spd_tree_commit(_Somewhere("bfloat16", n * 16 * 256), 1, whole[:3], cu, [1] * n, 16, 2, 64, ws, stream=0)
     assert e.value.code == N.SPD_EINVAL
+
+
+class _Rows(_Somewhere):
+    def __init__(self, dtype, *shape):
+        super().__init__(dtype, int(np.prod(shape)))
+        self.shape = shape
+
+    def stride(self):
+        return self.shape[-1], 1
+
+
+@pytest.mark.parametrize("shape", [(4, 4), (2, 6), (1, 4), (13,), (2, 2, 10)])
+def test_grammars_of_another_width_are_refused(lib, shape):  # noqa: F811
+    # 150 tokens are 5 words; a row stride of 4, 6 or 10 would put every grammar but the first in the wrong place
+    z, rule = _Rows("float32", 3, 150), _Rows("int32", 3)
+    with pytest.raises(ValueError, match="allow"):
+        N.spd_logits_process(z, z, allow=_Rows("int32", *shape), rule=rule, stream=0)
