@@ -291,8 +291,8 @@ SelectKernel pick_select(int move) {
 }
 
 // The rows themselves: a warp a move, 16 bytes a lane (half a warp K, half V; HD = 64: a quarter each), four moves in
-// flight a warp; `ctas` CTAs a unit, side by side. HBM: 175 K moves of 1 KB (read and written) in 25 us, 7.1 TB/s. Moving inside the selecting kernel saves a launch
-// and loses the occupancy: 46.8 against 44.1 us for the whole call.
+// flight a warp; `ctas` CTAs a unit, side by side. HBM: 175 K moves of 1 KB (read and written) in 25 us, 7.1 TB/s. Moving
+// inside the selecting kernel saves a launch and loses the occupancy: 46.8 against 44.1 us for the whole call.
 constexpr int kMoveWarps = 8, kMoveDepth = 4;
 template <int HD>
 __global__ void __launch_bounds__(kMoveWarps * 32) evict_move_kernel(uint16_t* kv, const __grid_constant__ EvictArgs p, int ctas) {

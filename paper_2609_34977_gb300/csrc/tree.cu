@@ -22,12 +22,14 @@
 // draft (recycled memory) and those that are not finite, which a weight of zero would turn into NaN for rows that
 // do not see them; rows that do see one add it at the end.
 //
-// What bounds it: with two CTAs an SM a block of 64 keys takes 1140 cycles of the SM, below its share of HBM (1400): the K/V
-// stream, with the tensor pipe at 800 and the softmax at 525 under it (single CTAs take 1700 to 2300, S and P V
-// waiting for each other). A CTA costs about 6 us besides: launch and set-up 1, the first loads 2 to 3 (everybody asks at
-// once), the last products, state and merge 2 to 3. 16 nodes on 65521 keys, 28 heads on 4 of 128: 34.8 us, 3.9 TB/s (the
-// merge through memory 4); eight trees of 48 on 640 to 1417 keys, 32 K/V heads: 35.9 us, 4.1 TB/s (the SMs with the two
-// longest sequences); 32 trees on 300 to 1943 keys: 27.5 us; one token, 321 keys, 32 heads: 8.4 us.
+// What bounds it: the tensor pipe and the K/V stream about alike. With two CTAs an SM a block of 64 keys takes 0.77 us of the
+// SM (0.70 with heads of 64) where K and V come from L2, 1150 of its 1500 cycles in products (S 384, P V 768); its share
+// of HBM is 0.73. Two terms a weight took 256 cycles less, and 35.5 instead of 40.5 us a call for the first of the
+// cases below. A single CTA takes 1.2 us a block, S and P V waiting for each other. A CTA costs about 6 us besides: launch and
+// set-up 1, the first loads 2 to 3 (everybody asks at once), the last products, state and merge 2 to 3. 16 nodes on 65521 keys,
+// 28 heads on 4 of 128: 39.7 us, 3.4 TB/s (the merge through memory 4); eight trees of 48 on 640 to 1417 keys, 32 K/V heads:
+// 41.8 us, 3.5 TB/s (the SMs with the two longest sequences); 32 trees on 300 to 1943 keys: 31.3 us; one token, 321 keys, 32
+// heads: 9.2 us.
 #include <cuda_bf16.h>
 #include <math.h>
 #include <stdint.h>
@@ -593,10 +595,11 @@ __global__ void __launch_bounds__(kThreads, 2)
 
 // Rows whose keys took several clusters: states (m_i, l_i, O_i) merged in key order, m = max m_i, l = sum l_i 2^(m_i - m),
 // O = sum O_i 2^(m_i - m). A part in which the row sees nothing has l_i = 0. (Its maximum does not tell: fmaxf passes over
-// those of parts whose scores are all NaN, whose sums are NaN and stay so.) W warps a row (node and head), each a range of the parts, four of them in flight; the kernel is
-// a handful of dependent loads, so long rows of parts want more warps, not longer loops. Whole calls with 4 / 8 parts in
-// flight: 32 trees in 2 to 4 parts 27.8 / 28.6 us, one in 18 parts 35.1 / 35.0; four warps a CTA instead of eight 27.6 and 36.7.
-// Where a row's states are is worked out before the wait for them (27.5 and 34.8).
+// those of parts whose scores are all NaN, whose sums are NaN and stay so.) W warps a row (node and head), each a range of the
+// parts, four of them in flight; the kernel is a handful of dependent loads, so long rows of parts want more warps, not longer
+// loops. Whole calls with 4 / 8 parts in flight, before weights had a third term: 32 trees in 2 to 4 parts 27.8 / 28.6 us, one
+// in 18 parts 35.1 / 35.0; four warps a CTA instead of eight 27.6 and 36.7. Where a row's states are is worked out before the
+// wait for them (27.5 and 34.8).
 constexpr int kMergeWarps = 8, kMergeAhead = 4;
 template <int HD>
 __global__ void __launch_bounds__(kMergeWarps * 32)
@@ -710,9 +713,10 @@ int rows_of_part(const TreeTile& t, int n_q) { return std::min(t.nodes, n_q) * t
 // kCtaTime besides its blocks (its launch, the first loads, the last products), a block `alone` with the SM to itself and
 // `pair` beside a second CTA (half an SM's share of HBM), a merge in the cluster, one through memory by the rows of its states.
 // Where the CTAs do not fit on the GPU at once, later ones start as earlier ones end, at 1.3 times the even share of the
-// work. Estimated / measured: one token, 321 keys, 32 heads, cluster 1 / 4 / 8: 13 / 9.4 / 8.2 and 11.2 / 9.2 / 8.7; 32
-// trees on 300 to 1958 keys, 4 K/V heads, no split / cluster 2 / 10 blocks a CTA, merged through memory: 43 / 29.5 / 25 and 43.1 /
-// 33.8 / 30.0 (27.5 with the present merge); eight of 48 nodes, 32 K/V heads, cluster 1 / 2 / 4: 39 / 46 / 59 and 35.3 / 43.4 / 59.0.
+// work. Estimated / measured: one token, 321 keys, 32 heads, cluster 1 / 2 / 4 / 8: 13.2 / 10.6 / 8.8 / 8.2 and 12.6 / 11.4 / 8.6 /
+// 9.2; 32 trees on 300 to 1958 keys, 4 K/V heads, no split / cluster 2 / 10 blocks a CTA, merged through memory: 43.2 / 30.9 /
+// 29.8 and 53.7 / 37.9 / 31.3; eight of 48 nodes, 32 K/V heads, cluster 1 / 2 / 4: 41.4 / 49.2 / 65.4 and 41.8 / 48.0 / 63.2. A
+// batch with more units than the GPU holds CTAs is not split by length: its time is that of its longest sequence.
 constexpr double kCtaTime = 6.0, kClusterTime = 1.0, kMergeTime = 4.0, kMergeRow = 0.25e-3, kWaveFactor = 1.3;
 constexpr int kMaxStates = kItems;  // states in memory of a launch: those of plans that fit on the GPU at once
 struct TreeWork {  // a sequence of the launch: key blocks, (tile, K/V head) pairs, (node, head) rows
@@ -731,7 +735,7 @@ struct TreeWorkList {
 };
 // work: the longest first; places: CTAs the GPU holds at once.
 TreePlan tree_plan(const TreeWorkList& work, int places, int head_dim) {
-  const double alone = head_dim == 128 ? 1.2 : 0.93, pair = head_dim == 128 ? 1.45 : 0.93;
+  const double alone = head_dim == 128 ? 1.2 : 1.1, pair = head_dim == 128 ? 1.54 : 1.39;
   TreePlan best;
   double least = 1e30;
   long long units = 0;
