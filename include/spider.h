@@ -523,6 +523,106 @@ int spd_logits_process(const float* logits, int n_rows, int vocab, int ld, const
                        float* out, int ld_out, int32_t* best, void* stream);
 
 /* ------------------------------------------------------------------------------------------ */
+/* A paged cache: sequences that share pages, prompts in chunks, beams                          */
+/* ------------------------------------------------------------------------------------------ */
+
+/* A pool is bf16 [n_layers][n_pages][page_size][K of every K/V head | V of every K/V head] (dev, 16-byte aligned); page_size a
+ * multiple of 16, n_pages * page_size below 2^31, head_dim 64 or 128. Row r of sequence b lies in page table[b][r / page_size], at its row
+ * r % page_size. table (dev) int32 [n_seqs][max_pages]; entries behind a sequence's rows are not read. A page outside [0, n_pages)
+ * where a row should be is reported as SPD_EINVAL in the workspace's status word: nothing is read or written there, and what depends
+ * on it is not to be relied on. ref (dev) int32 [n_pages] counts the tables that list a page; 0 (or less): free.
+ * The lists q_cu and len are the same for spd_rope_pages and spd_paged_attention: sequence b's new tokens are rows
+ * [q_cu[b], q_cu[b + 1]) (HOST int32 [n_seqs + 1] from 0; none is allowed) and the last of its len[b] cached rows (HOST int32). */
+
+/* New tokens into the cache: rotary positions on Q and K, and K and V into one layer's pages. Pair (j, j + head_dim / 2) of a head turns
+ * by pos[axis[j]][t] * theta^(-2 j / head_dim): text has one axis, images and video have several (time, height, width).
+ * q (dev) bf16 [n_tok] rows of n_heads * head_dim, stride ldq; kv (dev) bf16 [n_tok] rows [K | V], stride ldkv (strides in
+ * values, multiples of 8); pos (dev) int32 [n_axes][n_tok], any values; axis (HOST) uint8 [head_dim / 2], NULL = all pairs by
+ * axis 0; a pair whose axis is n_axes or more does not turn. q_out (dev) bf16 [n_tok][n_heads * head_dim], may be q (then ldq is its
+ * width). pool: the layer's block [n_pages][page_size][K | V]. Rotation in fp32 with the angle modulo 2 pi exact to 2^-24 of a turn,
+ * one rounding to bf16. Two new tokens must not share a row (a page that several sequences list is written by one of them).
+ * q, kv and q_out 16-byte aligned. ws (dev, at least 4 bytes, may be NULL): only its status word is used.
+ * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ECUDA. */
+int spd_rope_pages(const uint16_t* q, int ldq, const uint16_t* kv, int ldkv, int n_tok, const int32_t* pos, int n_axes,
+                   const uint8_t* axis, float theta, const int32_t* q_cu, const int32_t* len, int n_seqs, const int32_t* table,
+                   int max_pages, uint16_t* pool, int n_pages, int page_size, int n_heads, int n_kv_heads, int head_dim,
+                   uint16_t* q_out, void* ws, void* stream);
+
+/* Workspace bytes of spd_paged_attention (0 on invalid arguments). */
+size_t spd_paged_attention_workspace_size(int n_q, int n_seqs, int n_heads, int n_kv_heads, int head_dim);
+
+/* Attention of new tokens over one layer's pages, from one token a sequence to whole prompts. New token i of the n of sequence b sees
+ * rows 0 .. max(len[b] - n + i, prefix[b] - 1): those up to itself, and all of the first prefix[b] rows (an image whose rows see one
+ * another; HOST int32 [n_seqs] in [0, len[b]], NULL = none). Per head, head h reading K/V head h / (n_heads / n_kv_heads):
+ *   o_i = sum_j softmax_j(q_i . k_j / sqrt(head_dim)) v_j,   lse_i = log sum_j exp(q_i . k_j / sqrt(head_dim)).
+ * What a row does not see contributes nothing, whatever it holds. NaN in a query or in a key that is seen gives NaN; an infinite V
+ * that is seen gives the infinity (perhaps NaN where its weight is below 2^-100 of the row's largest).
+ * q, o (dev) bf16 [n_q][n_heads * head_dim]; lse (dev) fp32 [n_q][n_heads], natural logarithm, may be NULL; pool: the layer's block.
+ * The same bits in every run. q, o, pool and ws 16-byte aligned.
+ * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ENOSPC, SPD_ECUDA; device timeouts in the workspace's status word. */
+int spd_paged_attention(const uint16_t* q, int n_q, const int32_t* q_cu, const int32_t* len, const int32_t* prefix, int n_seqs,
+                        const int32_t* table, int max_pages, const uint16_t* pool, int n_pages, int page_size, int n_heads,
+                        int n_kv_heads, int head_dim, uint16_t* o, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace bytes of spd_decode_paged for n_q new tokens of n_seqs sequences. */
+size_t spd_decode_paged_workspace_size(const spd_model* m, int n_q, int n_seqs);
+
+/* A pass over new tokens with a paged cache: chunks of prompts and single tokens alike. x (dev bf16 [n_q][d_model]) holds their
+ * embeddings; at least one token of every sequence. Every layer rotates and appends as spd_rope_pages (with the model's rotary base; Q and
+ * K are rounded to bf16 before and after) and attends as spd_paged_attention; every token runs every sub-layer. pool (dev) bf16
+ * [n_layers][n_pages][page_size][K | V]; logits (dev, may be NULL) fp32 [n_seqs][vocab] of every sequence's last new token. Other
+ * arguments as the two calls; ws and pool 16-byte aligned.
+ * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ENOSPC, SPD_ECUDA; device timeouts and bad pages in the workspace's status word. */
+int spd_decode_paged(const spd_model* m, const uint16_t* x, int n_q, const int32_t* q_cu, const int32_t* len,
+                     const int32_t* prefix, int n_seqs, const int32_t* pos, int n_axes, const uint8_t* axis, const int32_t* table,
+                     int max_pages, uint16_t* pool, int n_pages, int page_size, float* logits, void* ws, size_t ws_bytes,
+                     void* stream);
+
+/* Workspace bytes of spd_pages_update and spd_pages_compact for n_seqs sequences before or after (0 on invalid arguments). */
+size_t spd_pages_workspace_size(int n_pages, int n_seqs);
+
+/* Sequences fork, end and grow. Output b continues input parent[b] ((dev) int32 [n_out], NULL: b; outside [0, n_in): an empty
+ * sequence) and gets room for grow[b] more rows ((dev) int32 [n_out], NULL: none): its table lists the parent's pages, its length is
+ * len_in[parent[b]] + grow[b]. An input that nobody continues ends. ref follows. A last page that is not full and that other tables list
+ * too is not written by several: of the outputs that end in it the one that holds most of it, the first of these, keeps it (nobody where
+ * the page is listed anywhere else besides), the others that grow get a copy of its rows, in every layer. New pages are the
+ * lowest free ones (those that this call frees among them), in the order of the outputs, of each its copy first.
+ * Where no free page is left the entry is -1 and the workspace's status word SPD_ENOSPC. Lengths that a table does not hold (or
+ * negative ones) are cut to it and reported as SPD_EINVAL, and so is ref where it does not count what the tables list.
+ * pool (dev) bf16 [n_layers][n_pages][page_size][K | V]; ref_in, ref_out (dev) int32 [n_pages], the same buffer or apart; table_in
+ * (dev) int32 [n_in][max_pages], len_in (dev) int32 [n_in]; table_out (dev) int32 [n_out][max_pages], -1 behind a sequence's pages,
+ * len_out (dev) int32 [n_out], both apart from the inputs. ws 16-byte aligned. The same result in every run.
+ * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ENOSPC, SPD_ECUDA; as above in the status word. */
+int spd_pages_update(uint16_t* pool, int n_layers, int n_pages, int page_size, int n_kv_heads, int head_dim, const int32_t* ref_in,
+                     const int32_t* table_in, const int32_t* len_in, int n_in, const int32_t* parent, const int32_t* grow, int n_out,
+                     int max_pages, int32_t* ref_out, int32_t* table_out, int32_t* len_out, void* ws, size_t ws_bytes,
+                     void* stream);
+
+/* Compaction: the pages in use (ref > 0) move to the front of the pool, in every layer. With `used` of them, the j-th page in use at or
+ * behind `used` moves into the j-th free page before it; ref and the tables follow. used (dev) int32 [1]. table_out may be table_in,
+ * ref_out ref_in; entries outside [0, n_pages) stay what they are; entries of pages that ref does not count stay and are reported as
+ * SPD_EINVAL in the status word. Every table that lists a page has to be among the n_seqs. Pages behind `used` keep what they held.
+ * Other arguments and errors as spd_pages_update. */
+int spd_pages_compact(uint16_t* pool, int n_layers, int n_pages, int page_size, int n_kv_heads, int head_dim, const int32_t* ref_in,
+                      const int32_t* table_in, int n_seqs, int max_pages, int32_t* ref_out, int32_t* table_out, int32_t* used, void* ws,
+                      size_t ws_bytes, void* stream);
+
+/* Workspace bytes of spd_beam_select (0 on invalid arguments). */
+size_t spd_beam_select_workspace_size(int n_seqs, int n_in, int n_out, int vocab);
+
+/* Beam search's selection. Beam w of request b has score scores[b][w] ((dev) fp32 [n_seqs][n_in], the logarithm of its probability) and
+ * logits row b * n_in + w ((dev) fp32, vocab values, stride ld). Of the candidates
+ *   total(w, t) = scores[b][w] + z[t] - log sum_u exp z[u],   t != eos (eos -1: none), z[t] above -inf,
+ * the n_out largest, ties to the lower beam, then to the lower token (totals in fp64): parent (dev) int32 [n_seqs][n_out] receives
+ * b * n_in + w, as spd_pages_update takes it, token (dev) int32 the token, scores_out (dev) fp32 the total; -1, -1 and -inf where there
+ * are fewer. A beam whose score is not finite, or whose logits hold NaN, +inf or nothing above -inf, offers nothing.
+ * ended (dev, may be NULL) fp32 [n_seqs][n_in]: total(w, eos) where fewer than n_out candidates of the request go before it, the ends of
+ * other beams counted, else -inf. n_in and n_out up to 32, up to 65535 beams in all; ws 16-byte aligned. The same result in every run.
+ * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ENOSPC, SPD_ECUDA. */
+int spd_beam_select(const float* logits, int n_seqs, int n_in, int vocab, int ld, const float* scores, int n_out, int eos,
+                    int32_t* parent, int32_t* token, float* scores_out, float* ended, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------ */
 /* Single kernels, exposed for composition and per-kernel tests                                 */
 /* ------------------------------------------------------------------------------------------ */
 

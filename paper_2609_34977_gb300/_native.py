@@ -35,7 +35,10 @@ EXPORTS = ("spd_last_error", "spd_workspace_status", "spd_selftest_bounded_wait"
            "spd_tree_mask", "spd_tree_attention_workspace_size", "spd_tree_attention",
            "spd_tree_commit_workspace_size", "spd_tree_commit", "spd_cache_weights",
            "spd_cache_evict_workspace_size", "spd_cache_evict", "spd_logits_process",
-           "spd_decode_tree_workspace_size", "spd_decode_tree")
+           "spd_decode_tree_workspace_size", "spd_decode_tree", "spd_rope_pages",
+           "spd_paged_attention_workspace_size", "spd_paged_attention", "spd_decode_paged_workspace_size",
+           "spd_decode_paged", "spd_pages_workspace_size", "spd_pages_update", "spd_pages_compact",
+           "spd_beam_select_workspace_size", "spd_beam_select")
 TRACE_GEMM, TRACE_ATTN, TRACE_ROWS, TRACE_PRUNE = 0, 1, 2, 3
 
 
@@ -169,6 +172,16 @@ def lib():
             "spd_cache_evict_workspace_size": (sz, [i, i, i, i]),
             "spd_cache_evict": (i, [vp, i, i, vp, i, i, i, i, i, i, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
             "spd_logits_process": (i, [vp, i, i, i, C.POINTER(LogitsRules), vp, i, vp, vp]),
+            "spd_rope_pages": (i, [vp, i, vp, i, i, vp, i, vp, C.c_float, vp, vp, i, vp, i, vp, i, i, i, i, i, vp, vp, vp]),
+            "spd_paged_attention_workspace_size": (sz, [i, i, i, i, i]),
+            "spd_paged_attention": (i, [vp, i, vp, vp, vp, i, vp, i, vp, i, i, i, i, i, vp, vp, vp, sz, vp]),
+            "spd_decode_paged_workspace_size": (sz, [vp, i, i]),
+            "spd_decode_paged": (i, [vp, vp, i, vp, vp, vp, i, vp, i, vp, vp, i, vp, i, i, vp, vp, sz, vp]),
+            "spd_pages_workspace_size": (sz, [i, i]),
+            "spd_pages_update": (i, [vp, i, i, i, i, i, vp, vp, vp, i, vp, vp, i, i, vp, vp, vp, vp, sz, vp]),
+            "spd_pages_compact": (i, [vp, i, i, i, i, i, vp, vp, i, i, vp, vp, vp, vp, sz, vp]),
+            "spd_beam_select_workspace_size": (sz, [i, i, i, i]),
+            "spd_beam_select": (i, [vp, i, i, i, i, vp, i, i, vp, vp, vp, vp, vp, sz, vp]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -706,6 +719,162 @@ def spd_logits_process(logits, out, best=None, *, seq_of=None, hist=None, hist_c
                     _dev(allow, "i32", n_rules * words, "allow", True), n_rules, _dev(rule, "i32", n, "rule", True))
     _check(lib().spd_logits_process(zp, n, v, ld, C.byref(r), op, ldo, _dev(best, "i32", n, "best", True),
                                     _stream(stream)))
+
+
+def _pool(pool, n_kv_heads, head_dim, layers=True):
+    """Pointer and sizes (layers, pages, rows a page) of a pool [layers][pages][rows a page][K | V], or of one layer's block."""
+    ptr = _dev(pool, "bf16", 1, "pool")
+    shape = tuple(pool.shape)
+    if len(shape) != (4 if layers else 3) or shape[-1] != 2 * n_kv_heads * head_dim:
+        raise ValueError(f"pool: shape {shape}, expected {'[layers]' if layers else ''}[pages][rows][{2 * n_kv_heads * head_dim}]")
+    return (ptr, *(shape[:3] if layers else (1, *shape[:2])))
+
+
+def _table(table, n, name="table"):
+    """Pointer and width of a page table of n sequences."""
+    if len(table.shape) != 2 or table.shape[0] < n:
+        raise ValueError(f"{name}: shape {tuple(table.shape)}, expected [{n}][pages]")
+    return _dev(table, "i32", n * table.shape[1], name), table.shape[1]
+
+
+def _rows_bf16(t, width, name):
+    """Pointer and row stride of a 2-D bf16 CUDA tensor whose rows are contiguous and `width` wide."""
+    if not getattr(t, "is_cuda", False):
+        raise TypeError(f"{name}: device arguments of libspider must be CUDA tensors")
+    if t.dtype is not (_torch_dt or _load_dtypes())["bf16"] or len(t.shape) != 2 or t.shape[1] != width:
+        raise ValueError(f"{name}: expected bf16 [tokens][{width}], got {t.dtype} {tuple(t.shape)}")
+    ld, step = t.stride()
+    if width > 1 and step != 1:
+        raise ValueError(f"{name}: the values of a row must lie side by side")
+    if t.shape[0] > 1 and ld < width:
+        raise ValueError(f"{name}: rows overlap")
+    return t.data_ptr(), ld if t.shape[0] > 1 else width
+
+
+def _axes(pos, axis, n_tok, head_dim):
+    """Pointers of positions [axes][tokens] (or [tokens]) and of the pairs' axes, and the number of axes."""
+    n = 1 if len(pos.shape) == 1 else pos.shape[0]
+    if pos.shape[-1] != n_tok:
+        raise ValueError(f"pos: shape {tuple(pos.shape)}, expected [axes][{n_tok}]")
+    ax = None if axis is None else _host(axis, np.uint8, head_dim // 2, "axis")
+    return _dev(pos, "i32", n * n_tok, "pos"), n, ax
+
+
+def spd_rope_pages(q, kv, pos, axis, theta, q_cu, lens, table, pool, n_heads, n_kv_heads, head_dim, q_out, ws=None,
+                   stream=None):
+    """Rotates the new tokens' Q [n][n_heads * head_dim] into q_out and K of kv [n][K | V] (rows may have a stride), and writes
+    K and V into a layer's block of the pool, [pages][rows][K | V]; pos int32 [axes][n], axis: host uint8 [head_dim / 2] or None."""
+    cu = np.ascontiguousarray(q_cu, dtype=np.int32)
+    B, n = len(cu) - 1, int(cu[-1])
+    ln = _host(lens, np.int32, B, "lens")
+    qp, ldq = _rows_bf16(q, n_heads * head_dim, "q")
+    kp, ldkv = _rows_bf16(kv, 2 * n_kv_heads * head_dim, "kv")
+    if q.shape[0] < n or kv.shape[0] < n:
+        raise ValueError(f"q, kv: {q.shape[0]} and {kv.shape[0]} rows, the call reads {n}")
+    pp, axes, ax = _axes(pos, axis, n, head_dim)
+    tp, width = _table(table, B)
+    pool_p, _, pages, rows = _pool(pool, n_kv_heads, head_dim, layers=False)
+    _check(lib().spd_rope_pages(qp, ldq, kp, ldkv, n, pp, axes, _p(ax), float(theta), _p(cu), _p(ln), B, tp, width, pool_p, pages,
+                                rows, n_heads, n_kv_heads, head_dim, _dev(q_out, "bf16", n * n_heads * head_dim, "q_out"),
+                                None if ws is None else _ws(ws)[0], _stream(stream)))
+
+
+def spd_paged_attention_workspace_size(n_q: int, n_seqs: int, n_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    return int(lib().spd_paged_attention_workspace_size(n_q, n_seqs, n_heads, n_kv_heads, head_dim))
+
+
+def spd_paged_attention(q, q_cu, lens, table, pool, n_heads, n_kv_heads, head_dim, o, lse, ws, prefix=None, stream=None):
+    """Attention of the new tokens q over a layer's block of the pool, [pages][rows][K | V]: sequence b's are the last of its
+    lens[b] rows; prefix (host int32): rows that every new token of a sequence sees, or None."""
+    cu = np.ascontiguousarray(q_cu, dtype=np.int32)
+    B, n = len(cu) - 1, int(cu[-1])
+    ln = _host(lens, np.int32, B, "lens")
+    pre = None if prefix is None else _host(prefix, np.int32, B, "prefix")
+    tp, width = _table(table, B)
+    pool_p, _, pages, rows = _pool(pool, n_kv_heads, head_dim, layers=False)
+    qd = n_heads * head_dim
+    wp, wb = _ws(ws)
+    _check(lib().spd_paged_attention(_dev(q, "bf16", n * qd, "q"), n, _p(cu), _p(ln), _p(pre), B, tp, width, pool_p, pages, rows,
+                                     n_heads, n_kv_heads, head_dim, _dev(o, "bf16", n * qd, "o"),
+                                     _dev(lse, "f32", n * n_heads, "lse", True), wp, wb, _stream(stream)))
+
+
+def spd_decode_paged_workspace_size(model: SpdModel, n_q: int, n_seqs: int) -> int:
+    return int(lib().spd_decode_paged_workspace_size(model.handle, n_q, n_seqs))
+
+
+def spd_decode_paged(model: SpdModel, x, q_cu, lens, pos, table, pool, logits, ws, axis=None, prefix=None, stream=None):
+    """A pass over the new tokens x [n][d_model] of every sequence with a paged cache, pool [layers][pages][rows][K | V];
+    pos: device int32 [axes][n]; logits fp32 [n_seqs][vocab] of the sequences' last tokens, or None."""
+    cu = np.ascontiguousarray(q_cu, dtype=np.int32)
+    B, n = len(cu) - 1, int(cu[-1])
+    c = model.cfg
+    ln = _host(lens, np.int32, B, "lens")
+    pre = None if prefix is None else _host(prefix, np.int32, B, "prefix")
+    pp, axes, ax = _axes(pos, axis, n, c["head_dim"])
+    tp, width = _table(table, B)
+    pool_p, layers, pages, rows = _pool(pool, c["n_kv_heads"], c["head_dim"])
+    if layers < c["n_layers"]:
+        raise ValueError(f"pool: {layers} layers, the model has {c['n_layers']}")
+    wp, wb = _ws(ws)
+    _check(lib().spd_decode_paged(model.handle, _dev(x, "bf16", n * c["d_model"], "x"), n, _p(cu), _p(ln), _p(pre), B, pp, axes,
+                                  _p(ax), tp, width, pool_p, pages, rows, _dev(logits, "f32", B * c["vocab"], "logits", True),
+                                  wp, wb, _stream(stream)))
+
+
+def spd_pages_workspace_size(n_pages: int, n_seqs: int) -> int:
+    return int(lib().spd_pages_workspace_size(n_pages, n_seqs))
+
+
+def spd_pages_update(pool, n_kv_heads, head_dim, ref_in, table_in, len_in, parent, grow, ref_out, table_out, len_out, ws,
+                     stream=None):
+    """Sequences fork, end and grow: output b continues input parent[b] (None: b) with room for grow[b] more rows (None: none).
+    pool [layers][pages][rows][K | V]; tables [n_in or n_out][max_pages]; all lists are device int32."""
+    pool_p, layers, pages, rows = _pool(pool, n_kv_heads, head_dim)
+    n_in, n_out = len_in.numel(), len_out.numel()
+    tp, width = _table(table_in, n_in, "table_in")
+    op, width_out = _table(table_out, n_out, "table_out")
+    if width_out != width:
+        raise ValueError(f"table_out: {width_out} pages a sequence, table_in has {width}")
+    wp, wb = _ws(ws)
+    _check(lib().spd_pages_update(pool_p, layers, pages, rows, n_kv_heads, head_dim, _dev(ref_in, "i32", pages, "ref_in"), tp,
+                                  _dev(len_in, "i32", n_in, "len_in"), n_in, _dev(parent, "i32", n_out, "parent", True),
+                                  _dev(grow, "i32", n_out, "grow", True), n_out, width, _dev(ref_out, "i32", pages, "ref_out"), op,
+                                  _dev(len_out, "i32", n_out, "len_out"), wp, wb, _stream(stream)))
+
+
+def spd_pages_compact(pool, n_kv_heads, head_dim, ref_in, table_in, ref_out, table_out, used, ws, stream=None):
+    """Moves the pages in use to the front of the pool [layers][pages][rows][K | V]; used: device int32 [1], their number."""
+    pool_p, layers, pages, rows = _pool(pool, n_kv_heads, head_dim)
+    n = table_in.shape[0]
+    tp, width = _table(table_in, n, "table_in")
+    op, width_out = _table(table_out, n, "table_out")
+    if width_out != width:
+        raise ValueError(f"table_out: {width_out} pages a sequence, table_in has {width}")
+    wp, wb = _ws(ws)
+    _check(lib().spd_pages_compact(pool_p, layers, pages, rows, n_kv_heads, head_dim, _dev(ref_in, "i32", pages, "ref_in"), tp, n,
+                                   width, _dev(ref_out, "i32", pages, "ref_out"), op, _dev(used, "i32", 1, "used"), wp, wb,
+                                   _stream(stream)))
+
+
+def spd_beam_select_workspace_size(n_seqs: int, n_in: int, n_out: int, vocab: int) -> int:
+    return int(lib().spd_beam_select_workspace_size(n_seqs, n_in, n_out, vocab))
+
+
+def spd_beam_select(logits, scores, eos, parent, token, scores_out, ended, ws, stream=None):
+    """The best continuations of every request's beams: logits [n_seqs * n_in][vocab] (rows may have a stride), scores
+    [n_seqs][n_in]; parent, token, scores_out [n_seqs][n_out]; ended [n_seqs][n_in] or None; eos -1: none."""
+    zp, ld, (n, v) = _rows_f32(logits, "logits")
+    if len(scores.shape) != 2 or len(parent.shape) != 2 or parent.shape[0] != scores.shape[0]:
+        raise ValueError(f"scores, parent: shapes {tuple(scores.shape)} and {tuple(parent.shape)}, expected [requests][beams]")
+    (B, n_in), n_out = scores.shape, parent.shape[1]
+    if n < B * n_in:
+        raise ValueError(f"logits: {n} rows, the call reads {B * n_in}")
+    wp, wb = _ws(ws)
+    _check(lib().spd_beam_select(zp, B, n_in, v, ld, _dev(scores, "f32", B * n_in, "scores"), n_out, eos,
+                                 _dev(parent, "i32", B * n_out, "parent"), _dev(token, "i32", B * n_out, "token"),
+                                 _dev(scores_out, "f32", B * n_out, "scores_out"), _dev(ended, "f32", B * n_in, "ended", True), wp,
+                                 wb, _stream(stream)))
 
 
 def spd_linear_workspace_size(M: int, N: int) -> int:

@@ -587,6 +587,20 @@ struct TreeStep {
   void* ws;
   size_t ws_bytes;
 };
+// What a pass over a paged cache gives its attention (spd_decode_paged).
+struct PagedStep {
+  const int32_t *q_cu, *len, *prefix;
+  int n_seqs;
+  const int32_t* pos;  // (dev) [n_axes][n_q]
+  int n_axes;
+  const uint8_t* axis;
+  const int32_t* table;
+  int max_pages;
+  uint16_t* pool;  // all layers
+  int n_pages, page_size;
+  void* ws;
+  size_t ws_bytes;
+};
 struct HostPlan {
   std::vector<int32_t> hl;
   std::vector<int> pos_all, seq_of;
@@ -595,6 +609,7 @@ struct HostPlan {
   size_t pos_off = 0, kvrow_off = 0, last_off = 0, end = 0;
   bool decode = false;  // one query per sequence at its last position (attention_decode_run)
   const TreeStep* tree = nullptr;  // drafted tokens over the cache (tree_attention_run)
+  const PagedStep* paged = nullptr;  // new tokens over pages (paged_attention_run)
   std::vector<int> by_length;  // decode: the sequences, longest first
 };
 
@@ -618,6 +633,7 @@ void plan_init(HostPlan& P, const spd_model_cfg& c, const int32_t* cu, int B, in
   P.ll.assign(c.n_layers, LayerLists{});
   P.decode = false;
   P.tree = nullptr;
+  P.paged = nullptr;
   size_t off = 0;
   P.pos_off = off;
   for (int t = 0; t < T; ++t) P.hl[off + t] = P.pos_all[t];
@@ -762,7 +778,14 @@ int run_layer(const spd_model* m, int l, const LayerLists& q, const HostPlan& P,
     if ((rc = gemm_run(kvp, bf.gs, st))) return rc;
   }
   if (q.na > 0) {
-    if (P.tree)
+    if (const PagedStep* g = P.paged) {
+      uint16_t* pool = g->pool + size_t(l) * g->n_pages * g->page_size * 2 * kvd;
+      rc = rope_pages_run(qbuf, qd, dest.kv, 2 * kvd, g->pos, g->n_axes, g->axis, c.rope_theta, g->q_cu, g->len, g->n_seqs, g->table,
+                          g->max_pages, pool, g->n_pages, g->page_size, c.n_heads, c.n_kv_heads, hd, qbuf, bf.gs.status, st);
+      if (!rc)
+        rc = paged_attention_run(qbuf, g->q_cu, g->len, g->prefix, g->n_seqs, g->table, g->max_pages, pool, g->n_pages, g->page_size,
+                                 c.n_heads, c.n_kv_heads, hd, bf.o, nullptr, g->ws, g->ws_bytes, bf.gs.status, st);
+    } else if (P.tree)
       rc = tree_attention_run(qbuf, P.tree->q_cu, P.tree->ctx, P.tree->n_seqs, P.tree->mask, P.tree->words, dest.kv,
                               P.tree->max_len, c.n_heads, c.n_kv_heads, hd, bf.o,
                               P.tree->lse ? P.tree->lse + size_t(l) * T * c.n_heads : nullptr, P.tree->ws, P.tree->ws_bytes,
@@ -1237,6 +1260,63 @@ extern "C" int spd_decode_tree(const spd_model* m, const uint16_t* x, int n_q, c
   return fail(SPD_EUNSUPPORTED, "tree step: out of host memory for %d nodes", n_q);
 }
 
+// ---- a pass over a paged cache --------------------------------------------------------------------
+namespace {
+size_t carve_paged(const spd_model_cfg& c, int n_q, int n_seqs, Carve& cv, PrefillBufs* bf, float** h, void** ws, size_t* bytes) {
+  *bf = carve_prefill(c, n_q, n_seqs, cv);
+  *h = cv.take<float>(size_t(n_q) * c.d_model);
+  *bytes = paged_attention_bytes(n_q, c.n_heads, c.n_kv_heads, c.head_dim);
+  *ws = cv.take<uint8_t>(*bytes);
+  return cv.used;
+}
+}  // namespace
+
+extern "C" size_t spd_decode_paged_workspace_size(const spd_model* m, int n_q, int n_seqs) {
+  if (!m || n_q < 1 || n_seqs < 1) return 0;
+  Carve cv(nullptr, ~size_t(0));
+  PrefillBufs bf;
+  float* h;
+  void* w;
+  size_t b;
+  return carve_paged(m->cfg, n_q, n_seqs, cv, &bf, &h, &w, &b);
+}
+
+extern "C" int spd_decode_paged(const spd_model* m, const uint16_t* x, int n_q, const int32_t* q_cu, const int32_t* len,
+                                const int32_t* prefix, int n_seqs, const int32_t* pos, int n_axes, const uint8_t* axis,
+                                const int32_t* table, int max_pages, uint16_t* pool, int n_pages, int page_size, float* logits,
+                                void* ws, size_t ws_bytes, void* stream) try {
+  if (!m || !x || !q_cu || !len || !pos || !table || !ws || n_q < 1 || n_seqs < 1 || n_axes < 1 || n_axes > 255)
+    return fail(SPD_EINVAL, "bad paged step arguments");
+  const spd_model_cfg& c = m->cfg;
+  if (int rc = pool_check(pool, c.n_layers, n_pages, page_size, c.n_kv_heads, c.head_dim, max_pages)) return rc;
+  if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(SPD_EINVAL, "ws must be 16-byte aligned");
+  if (int rc = paged_check(q_cu, n_q, len, prefix, n_seqs, max_pages, page_size)) return rc;
+  for (int b = 0; b < n_seqs; ++b)
+    if (q_cu[b + 1] == q_cu[b]) return fail(SPD_EINVAL, "sequence %d has no new token", b);
+  Carve cv(ws, ws_bytes);
+  PrefillBufs bf;
+  float* h;
+  PagedStep ps{q_cu, len, prefix, n_seqs, pos, n_axes, axis, table, max_pages, pool, n_pages, page_size, nullptr, 0};
+  carve_paged(c, n_q, n_seqs, cv, &bf, &h, &ps.ws, &ps.ws_bytes);
+  if (!cv.fits()) return fail(SPD_ENOSPC, "paged step workspace too small (%zu < %zu)", ws_bytes, cv.used);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  static thread_local HostPlan P;
+  plan_init(P, c, q_cu, n_seqs, n_q, bf.list_ints);
+  for (int t = 0; t < n_q; ++t) P.hl[P.pos_off + t] = 0;  // the projections' own rotation turns nothing
+  plan_layer(P, 0, nullptr, q_cu, n_seqs, n_q);           // no sub-layer is skipped: one layer's lists serve all
+  P.paged = &ps;
+  int32_t* dl = bf.lists;
+  const size_t ints = c.n_layers > 1 ? P.ll[1].arows : P.end;
+  SPD_CUDA_TRY(cudaMemcpyAsync(dl, P.hl.data(), ints * sizeof(int32_t), cudaMemcpyHostToDevice, st));
+  GemmCleared cleared;
+  bf.gs.cleared = &cleared;
+  if (int rc = bf16_to_f32_run(x, h, size_t(n_q) * c.d_model, st)) return rc;
+  for (int l = 0; l < c.n_layers; ++l)
+    if (int rc = run_layer(m, l, P.ll[0], P, bf, dl, h, n_q, st)) return rc;
+  return run_head(m, P, bf, dl, h, n_seqs, logits, st);
+} catch (const std::exception&) {  // the host lists
+  return fail(SPD_EUNSUPPORTED, "paged step: out of host memory for %d tokens", n_q);
+}
 
 // ---- the hot path's contract names (thin forms of the calls above) --------------------------------
 extern "C" size_t spd_prune_workspace(const spd_prune_cfg* cfg) { return spd_prune_workspace_size(cfg); }

@@ -208,6 +208,21 @@ int tree_attention_run(const void* q, const int32_t* q_cu, const int32_t* ctx, i
                        size_t ws_bytes, int* status, cudaStream_t stream);
 int gemm_run(const GemmProblem& p, const GemmScratch& s, cudaStream_t stream);
 
+// ---- paged cache -------------------------------------------------------------------------------
+// Checks of a pool's shape, and of the sequences' new tokens [q_cu[b], q_cu[b + 1]) and rows len[b], the new ones among them.
+int pool_check(const void* pool, int n_layers, int n_pages, int page_size, int n_kv_heads, int head_dim, int max_pages);
+int paged_check(const int32_t* q_cu, int n_q, const int32_t* len, const int32_t* prefix, int n_seqs, int max_pages, int page_size);
+// spd_rope_pages and spd_paged_attention after their checks.
+int rope_pages_run(const void* q, int ldq, const void* kv, int ldkv, const int32_t* pos, int n_axes, const uint8_t* axis,
+                   double theta, const int32_t* q_cu, const int32_t* len, int n_seqs, const int32_t* table, int max_pages,
+                   void* pool, int n_pages, int page_size, int n_heads, int n_kv_heads, int head_dim, void* q_out, int* status,
+                   cudaStream_t st);
+size_t paged_attention_bytes(int n_q, int n_heads, int n_kv_heads, int head_dim);
+int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, const int32_t* prefix, int n_seqs,
+                        const int32_t* table, int max_pages, const void* pool, int n_pages, int page_size, int n_heads,
+                        int n_kv_heads, int head_dim, void* o, float* lse, void* ws, size_t ws_bytes, int* status,
+                        cudaStream_t st);
+
 // ---- ASL-Skip online scores (Sec. 4.2.1, Eq. 6) -------------------------------------------------
 // For candidate n (token cand[n], sequence seq_of[token]): E = entropy of softmax(logits[n]) / log V
 // (mode kSkipEntropy, else 0; from lse, the float4 statistics of EPI_LSE_F32, [n_cand][lse_groups(V)],
