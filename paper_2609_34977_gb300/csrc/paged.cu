@@ -1,4 +1,21 @@
-// Attention of new tokens over a paged KV cache.
+// Attention of new tokens over a paged KV cache: chunks of prompts (paged_attn_kernel).
+//
+// New token i of sequence b, one of its n, sees rows 0 .. lim_i - 1 with lim_i = max(len - n + i + 1, prefix):
+//   s_ij = q_i . k_j / sqrt(head_dim),  lse_i = log sum_j e^s_ij,  o_i = sum_j e^(s_ij - lse_i) v_j.
+// What a row does not see contributes nothing, whatever it holds.
+//
+// A unit is a tile of up to 128 rows (tokens times the query heads of a K/V head's group) over the keys that its last token
+// sees, in blocks of 64. All blocks of a launch form one list, unit after unit, and every CTA takes an equal stretch of it,
+// whole units and parts of two: no CTA waits for a longest sequence, and 1.5 tiles a CTA cost 1.5 tiles. Parts of a unit leave
+// states (m, l, O) in fp32, which paged_merge_kernel joins in the order of the keys (the same bits in every run).
+//   warp 4     TMA producer: K and V blocks into rings, a lane a box of rows that lie in one page
+//   warp 5     MMA issuer: S = Q K^T into TMEM, then O += P V with P read from TMEM, V in place as an MN-major operand
+//   warps 0-3  a thread a row: the block's 64 scores in registers, online softmax in fp32; a weight is held as the sum of
+//              three bf16 terms, all 24 bits of it: two over the scores in TMEM, where O leaves no room for more, the third in
+//              shared memory
+// Only blocks that reach past the first token's limit are masked; there the softmax warps also clear the values of V that are
+// not finite (recycled memory behind the sequence among them), which a weight of zero would turn into NaN for rows that do not
+// see them; rows that do see one add it at the end.
 #include <cuda_bf16.h>
 #include <math.h>
 #include <stdint.h>
@@ -12,65 +29,713 @@
 namespace spd {
 namespace {
 
-constexpr int kMaxSeqs = 112;  // sequences whose sizes fit in a launch's parameters (4 KB)
+constexpr int kMaxSeqs = 112;          // sequences whose sizes fit in a launch's parameters (4 KB)
+constexpr int kTK = 64;                // keys a block
+constexpr uint32_t kQBox = 128 * 128;  // 64 columns of the Q tile
+constexpr uint32_t kKBox = kTK * 128;  // 64 columns of a block of K or V
+constexpr int kThreads = 192;
+constexpr uint32_t kTmemCols = 256;    // S: two buffers [0, 64) and [64, 128); O: [128, 128 + HD)
+constexpr int kCtas = 304;             // CTAs that fill the GPU: two on each of 152 SMs
+// The reference that a row's exponentials are taken against is renewed once its maximum has grown by this much (log2
+// units): weights stay below 2^8, their terms and the fp32 sums are relative to them, and almost no block pays for the
+// round trip of O through the registers.
+constexpr float kGrown = 8.0f;
 
+// A sequence with new tokens. Its units are (K/V head, tile), the tile fastest; the tiles of a head have head_blocks blocks.
 struct PagedSeq {
-  int q0, n, len, prefix, seq;
+  int block0;  // its first block in the launch's list
+  int q0, n, len, prefix, seq, head_blocks, tiles;
+};
+struct PagedSeqs {
+  int n, pad[7];
+  PagedSeq s[kMaxSeqs];
 };
 struct PagedArgs {
   const __nv_bfloat16 *q, *pool;
   const int32_t* table;
-  int max_pages, n_pages, page_size, n_heads, n_kv_heads, n_seqs;
-  float scale;
+  int max_pages, n_pages, page_size, box;  // box: rows that one TMA load brings (they divide the page and the block)
+  int n_heads, n_kv_heads;
+  int group, chunk, chunks, tokens;  // heads a group; of them in a tile; tiles across; tokens a tile
+  float scale_log2;
   __nv_bfloat16* o;
   float* lse;
+  int total, ctas, warps;            // blocks; CTAs; softmax warps with rows
+  float* part_o;                     // [2 ctas][rows_part][HD] states of parts: slot 2 c of the part that goes on with a unit
+  float2* part_ml;                   // (CTA c), 2 c + 1 of the one that begins one; maximum (log2 units) and sum
+  int rows_part;
   int* status;
-  PagedSeq s[kMaxSeqs];
+  long long budget;
+  unsigned long long* stamp;
 };
 
-// A warp a row and head, a lane HD / 32 of its dims.
 template <int HD>
-__global__ void __launch_bounds__(256) paged_simple_kernel(const __grid_constant__ PagedArgs p) {
-  constexpr int D = HD / 32;
+struct PagedSmem {
+  static constexpr int kChunks = HD / 64;
+  static constexpr int kStages = 256 / HD;  // 64 KB of K and V in flight a CTA
+  static constexpr uint32_t q = 0;
+  static constexpr uint32_t k = q + kChunks * kQBox;
+  static constexpr uint32_t v = k + kStages * kChunks * kKBox;
+  static constexpr uint32_t p3 = v + kStages * kChunks * kKBox;  // [128][64] third terms of a block's weights
+  static constexpr uint32_t bars = p3 + 128 * 128;
+  static constexpr uint32_t bytes = bars + 256;  // (two CTAs an SM: at most 113 KB)
+  static_assert(bytes <= 113 * 1024, "two CTAs an SM");
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<uint32_t*>(&v);
+}
+__device__ __forceinline__ bool not_finite(uint32_t two) {  // either of two bf16
+  return (two & 0x7f80u) == 0x7f80u || (two & 0x7f800000u) == 0x7f800000u;
+}
+__device__ __forceinline__ uint32_t finite_of(uint32_t two) {  // those of two bf16 that are finite, 0 for the others
+  if ((two & 0x7f80u) == 0x7f80u) two &= 0xffff0000u;
+  return (two & 0x7f800000u) == 0x7f800000u ? two & 0xffffu : two;
+}
+
+// Rows that token i of a sequence sees.
+__host__ __device__ __forceinline__ int limit_of(const PagedSeq& s, int i) {
+  const int own = s.len - s.n + i + 1;
+  return own > s.prefix ? own : s.prefix;
+}
+// Blocks of the tiles that begin with token i.
+__host__ __device__ __forceinline__ int blocks_at(const PagedSeq& s, int i, int tokens) {
+  const int last = i + tokens < s.n ? i + tokens : s.n;
+  return (limit_of(s, last - 1) + kTK - 1) / kTK;
+}
+// First block of CTA c's stretch.
+__device__ __forceinline__ int first_block(const PagedArgs& p, int c) { return int((long long)c * p.total / p.ctas); }
+
+// A CTA's place in the list of blocks: the unit (sequence e, K/V head hk, tile), its blocks, and the stretch's blocks lo .. hi - 1
+// of them.
+struct Place {
+  int e, hk, tile, blocks, lo, hi, left;  // left: blocks of the stretch from lo on
+  __device__ __forceinline__ void size(const PagedArgs& p, const PagedSeqs& sq) {
+    blocks = blocks_at(sq.s[e], tile / p.chunks * p.tokens, p.tokens);
+    hi = min(blocks, lo + left);
+  }
+  // The unit of block `at` of the list (a whole warp, all lanes with the same arguments).
+  __device__ __forceinline__ void seek(const PagedArgs& p, const PagedSeqs& sq, int at, int n) {
+    e = 0;
+    for (int top = sq.n; top - e > 1;) {
+      const int mid = (e + top) >> 1;
+      if (sq.s[mid].block0 <= at) e = mid;
+      else top = mid;
+    }
+    const PagedSeq& s = sq.s[e];
+    lo = at - s.block0;
+    hk = int(uint32_t(lo) / uint32_t(s.head_blocks));
+    lo -= hk * s.head_blocks;
+    const int lane = threadIdx.x & 31;
+    for (int t0 = 0;; t0 += 32) {
+      const int t = t0 + lane, mine = t < s.tiles ? blocks_at(s, t / p.chunks * p.tokens, p.tokens) : 0;
+      int sum = mine;
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, sum, off);
+        if (lane >= off) sum += y;
+      }
+      const uint32_t past = __ballot_sync(0xffffffffu, sum > lo);
+      if (past || t0 + 32 >= s.tiles) {
+        const int at_lane = past ? __ffs(past) - 1 : 0;
+        lo -= __shfl_sync(0xffffffffu, sum - mine, at_lane);
+        tile = t0 + at_lane;
+        break;
+      }
+      lo -= __shfl_sync(0xffffffffu, sum, 31);
+    }
+    left = n;
+    size(p, sq);
+  }
+  __device__ __forceinline__ bool next(const PagedArgs& p, const PagedSeqs& sq) {
+    left -= hi - lo;
+    if (left <= 0) return false;
+    lo = 0;
+    if (++tile == sq.s[e].tiles) {
+      tile = 0;
+      if (++hk == p.n_kv_heads) {
+        hk = 0;
+        ++e;
+      }
+    }
+    size(p, sq);
+    return true;
+  }
+};
+
+// Row of the pool that holds row `key` of a sequence; behind the pool (loads there read zeros) where its page is none.
+__device__ __forceinline__ int pool_row(const PagedArgs& p, int seq, int key) {
+  const int k = int(uint32_t(key) / uint32_t(p.page_size)), page = p.table[size_t(seq) * p.max_pages + k];
+  if (unsigned(page) >= unsigned(p.n_pages)) {
+    set_status(p.status, SPD_EINVAL);
+    return p.n_pages * p.page_size;
+  }
+  return page * p.page_size + (key - k * p.page_size);
+}
+
+template <int HD>
+__global__ void __launch_bounds__(kThreads, 2)
+    paged_attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ PagedArgs p,
+                      const __grid_constant__ PagedSeqs sq) {
+  using L = PagedSmem<HD>;
+  constexpr int NS = L::kStages;
+  extern __shared__ __align__(1024) uint8_t smem[];  // (the swizzle's atoms; no room to round the address up)
+  uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + L::bars);  // [NS] K block landed
+  uint64_t* k_empty = k_full + NS;                                 // [NS] its S product has completed
+  uint64_t* v_full = k_empty + NS;                                 // [NS] V block landed
+  uint64_t* v_empty = v_full + NS;                                 // [NS] its PV products have completed
+  uint64_t* q_full = v_empty + NS;   // a unit's Q tile is in shared memory
+  uint64_t* s_full = q_full + 1;     // [2] S of block j is in TMEM buffer j % 2
+  uint64_t* p_full = s_full + 2;     // [2] P of block j written and O rescaled
+  uint64_t* o_done = p_full + 2;     // [2] PV products of block j completed
+  uint64_t* drain = o_done + 2;      // every MMA completed
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int* odd_v = reinterpret_cast<int*>(tmem_slot + 2);  // the last unit (counted from 1) with a V that is not finite
+
+  if (smem_u32(smem) & 1023) {  // every CTA alike
+    pdl_wait();
+    if (threadIdx.x == 0) set_status(p.status, SPD_ECUDA);
+    return;
+  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int first = first_block(p, blockIdx.x), count = first_block(p, blockIdx.x + 1) - first;
+  const int nw = p.warps;
+  Place at;
+  at.seek(p, sq, first, count);
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < NS; ++s) {
+      mbar_init(&k_full[s], 1);
+      mbar_init(&k_empty[s], 1);
+      mbar_init(&v_full[s], 1);
+      mbar_init(&v_empty[s], 1);
+    }
+    mbar_init(q_full, nw);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&s_full[s], 1);
+      mbar_init(&p_full[s], nw);  // one arrival per softmax warp
+      mbar_init(&o_done[s], 1);
+    }
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    *odd_v = 0;
+    fence_mbar_init();
+    prefetch_tmap(&map_kv);
+  }
+  if (warp == 4) {
+    tmem_alloc(tmem_slot, kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const uint32_t t_o = tmem + 2 * kTK;
+
   pdl_launch_dependents();
   pdl_wait();
-  const PagedSeq& s = p.s[blockIdx.z];
-  const int row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, h = blockIdx.y;
-  if (row >= s.n) return;
-  const int g = h / (p.n_heads / p.n_kv_heads), kvd = p.n_kv_heads * HD;
-  const int limit = max(s.len - s.n + row + 1, s.prefix);
-  const size_t at = (size_t(s.q0) + row) * p.n_heads + h;
-  float q[D], o[D] = {}, m = -INFINITY, l = 0.0f;
-  for (int x = 0; x < D; ++x) q[x] = __bfloat162float(p.q[at * HD + lane * D + x]);
-  for (int j = 0; j < limit; ++j) {
-    const int page = p.table[size_t(s.seq) * p.max_pages + j / p.page_size];
-    if (unsigned(page) >= unsigned(p.n_pages)) {
-      if (lane == 0) set_status(p.status, SPD_EINVAL);
-      continue;
+  if (threadIdx.x == 0) stamp_start(p.stamp);
+
+  int issued_k = 0, issued_v = 0;
+  if (warp == 4) {
+    // ---- TMA producer ----
+    const uint64_t pol = policy_evict_last();
+    const int boxes = kTK / p.box;
+    int j = 0;  // block of the CTA
+    bool ok = true;
+    do {
+      const PagedSeq& s = sq.s[at.e];
+      const int t = at.tile / p.chunks * p.tokens, limit = limit_of(s, min(s.n, t + p.tokens) - 1);
+      auto row_at = [&](int blk) {  // of the lane's box; -1: none of its rows is seen
+        const int key = blk * kTK + lane * p.box;
+        return lane < boxes && key < limit ? pool_row(p, s.seq, key) : -1;
+      };
+      int row = row_at(at.lo);
+      for (int blk = at.lo; blk < at.hi && ok; ++blk, ++j) {
+        const int here = row;
+        if (blk + 1 < at.hi) row = row_at(blk + 1);  // a block ahead
+        const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, here >= 0)) * p.box * 128u * L::kChunks;
+        const int st = j % NS;
+        auto load = [&](uint64_t* full, uint64_t* empty, uint32_t to, int x0) -> bool {
+          if (j >= NS && !__all_sync(0xffffffffu, mbar_wait(&empty[st], (j / NS - 1) & 1, abort_flag, p.budget))) return false;
+          if (lane == 0) mbar_arrive_expect_tx(&full[st], bytes);
+          __syncwarp();
+          if (here >= 0)
+            for (int c = 0; c < L::kChunks; ++c)
+              tma_load_2d(smem + to + (st * L::kChunks + c) * kKBox + lane * p.box * 128, &map_kv, &full[st], x0 + c * 64, here, pol);
+          return true;
+        };
+        if (!(ok = load(k_full, k_empty, L::k, at.hk * HD))) break;
+        issued_k = j + 1;
+        if (!(ok = load(v_full, v_empty, L::v, (p.n_kv_heads + at.hk) * HD))) break;
+        issued_v = j + 1;
+      }
+    } while (ok && at.next(p, sq));
+    if (!ok && lane == 0) {
+      *abort_flag = 1;
+      set_status(p.status, SPD_ETIMEOUT);
     }
-    const __nv_bfloat16* kr = p.pool + (size_t(page) * p.page_size + j % p.page_size) * (2 * size_t(kvd)) + g * HD + lane * D;
-    float d = 0.0f;
-    for (int x = 0; x < D; ++x) d = fmaf(q[x], __bfloat162float(kr[x]), d);
-    for (int off = 16; off; off >>= 1) d += __shfl_xor_sync(0xffffffffu, d, off);
-    d *= p.scale;
-    const float mn = fmaxf(m, d), f = mn == -INFINITY ? 1.0f : expf(m - mn), w = mn == -INFINITY && !isnan(d) ? 0.0f : expf(d - mn);
-    m = mn;
-    l = l * f + w;
-    for (int x = 0; x < D; ++x) o[x] = o[x] * f + (w == 0.0f ? 0.0f : w * __bfloat162float(kr[kvd + x]));
+  } else if (warp == 5) {
+    if (lane == 0) {
+      // ---- MMA issuer ----
+      const uint32_t id_s = idesc_bf16_f32(128, kTK);
+      const uint32_t id_o = idesc_bf16_f32(128, HD) | (1u << 16);  // V is MN-major
+      const uint32_t sa = smem_u32(smem + L::q), sp = smem_u32(smem + L::p3);
+      bool ok = true;
+      auto issue_s = [&](int j) -> bool {
+        const int s = j % NS;
+        if (!mbar_wait(&k_full[s], (j / NS) & 1, abort_flag, p.budget)) return false;
+        // S buffer j % 2 holds P of block j - 2 until its PV products have completed
+        if (j > 1 && !mbar_wait(&o_done[j & 1], ((j >> 1) - 1) & 1, abort_flag, p.budget)) return false;
+        tc_fence_after();
+        const uint32_t sk = smem_u32(smem + L::k + s * L::kChunks * kKBox);
+#pragma unroll
+        for (int kk = 0; kk < HD / 16; ++kk)
+          mma_bf16(tmem + kTK * (j & 1), sdesc_k128(sa + (kk >> 2) * kQBox + (kk & 3) * 32),
+                   sdesc_k128(sk + (kk >> 2) * kKBox + (kk & 3) * 32), id_s, kk > 0 ? 1u : 0u);
+        mma_commit(&s_full[j & 1]);
+        mma_commit(&k_empty[s]);
+        return true;
+      };
+      int j = 0, left = count, unit = 0;
+      int n = at.hi - at.lo;  // blocks of the unit
+      for (;; ++unit) {
+        ok = mbar_wait(q_full, unit & 1, abort_flag, p.budget) && issue_s(j);
+        for (int u = 0; u < n && ok; ++u, ++j) {
+          const int s = j % NS;
+          if (u + 1 < n && !(ok = issue_s(j + 1))) break;
+          if (!(ok = mbar_wait(&v_full[s], (j / NS) & 1, abort_flag, p.budget))) break;
+          if (!(ok = mbar_wait(&p_full[j & 1], (j >> 1) & 1, abort_flag, p.budget))) break;
+          tc_fence_after();
+          const uint32_t sv = smem_u32(smem + L::v + s * L::kChunks * kKBox);
+#pragma unroll
+          for (int kk = 0; kk < 2 * (kTK / 16); ++kk) {  // the weights' first terms, then their second, then their third
+            const int x = kk % (kTK / 16), term = kk / (kTK / 16);
+            mma_bf16_ts(t_o, tmem + kTK * (j & 1) + 16 * x + 8 * term, sdesc_mn128(sv + x * 2048, kKBox), id_o,
+                        (u > 0 || kk > 0) ? 1u : 0u);
+          }
+#pragma unroll
+          for (int x = 0; x < kTK / 16; ++x)
+            mma_bf16(t_o, sdesc_k128(sp + x * 32), sdesc_mn128(sv + x * 2048, kKBox), id_o, 1u);
+          mma_commit(&o_done[j & 1]);
+          mma_commit(&v_empty[s]);
+        }
+        left -= n;
+        if (!ok || left <= 0) break;
+        at.next(p, sq);
+        n = at.hi - at.lo;
+      }
+      if (!ok) {
+        *abort_flag = 1;
+        set_status(p.status, SPD_ETIMEOUT);
+      }
+      mma_commit(drain);  // arrives once every MMA issued above has completed
+      volatile int no_abort = 0;
+      if (!mbar_wait(drain, 0, &no_abort, p.budget)) set_status(p.status, SPD_ETIMEOUT);
+    }
+  } else if (warp < nw) {
+    // ---- softmax: warp w reads TMEM lanes [32 w, 32 w + 32) ----
+    const int r = warp * 32 + lane, T = nw * 32;
+    const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
+    // a unit's rows: the thread's token, head and query row
+    struct Row {
+      int token, hc;
+      bool valid;
+      size_t row;  // token of the call times n_heads + head
+    };
+    auto row_of = [&](const Place& u) {
+      const PagedSeq& s = sq.s[u.e];
+      const int t = u.tile / p.chunks, h0 = (u.tile - t * p.chunks) * p.chunk, n0 = t * p.tokens;
+      const int tokens = min(p.tokens, s.n - n0), heads = min(p.chunk, p.group - h0);
+      Row w;
+      w.token = n0 + min(r / p.chunk, tokens - 1);  // rows without a token repeat the last one's, and are not stored
+      w.hc = r % p.chunk;
+      w.valid = r < tokens * p.chunk && w.hc < heads;
+      w.row = (size_t(s.q0) + w.token) * p.n_heads + u.hk * p.group + h0 + min(w.hc, heads - 1);
+      return w;
+    };
+    auto load_q = [&](const Row& w) {  // in the 128-byte swizzle: 16-byte piece j of row r at j ^ (r % 8)
+      const uint4* src = reinterpret_cast<const uint4*>(p.q + w.row * HD);
+#pragma unroll
+      for (int h = 0; h < HD / 64; ++h) {
+        uint4 v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = src[8 * h + j];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(smem + L::q + h * kQBox + r * 128 + ((j ^ (r & 7)) << 4)) = v[j];
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_full);
+    };
+    bool ok = true;
+    int j = 0;  // block of the CTA
+    Row row = row_of(at);
+    load_q(row);
+    for (int unit = 0;; ++unit) {
+      const PagedSeq& s = sq.s[at.e];
+      const int n0 = at.tile / p.chunks * p.tokens;
+      const int lim = limit_of(s, row.token);                            // what the row sees,
+      const int lim_all = limit_of(s, n0), lim_any = limit_of(s, min(s.n, n0 + p.tokens) - 1);  // every row, some row
+      float m_run = -INFINITY, l_run = 0.0f;  // the row's maximum so far (raw scores) and sum of weights
+      for (int blk = at.lo; blk < at.hi; ++blk, ++j) {
+        const uint32_t t_s = tmem + kTK * (j & 1) + lanes;
+        const int kb = blk * kTK;
+        const bool partly = kb + kTK > lim_all;  // the block holds keys that not every row sees, or none at all
+        if (partly) {
+          if (!(ok = __all_sync(0xffffffffu, mbar_wait(&v_full[j % NS], (j / NS) & 1, abort_flag, p.budget)))) break;
+          bool odd = false;
+          for (int x = threadIdx.x; x < kTK * L::kChunks; x += T) {
+            if (kb + x % kTK < lim_all) continue;
+            uint4* vr = reinterpret_cast<uint4*>(smem + L::v + (j % NS) * L::kChunks * kKBox + x * 128);
+            bool here = false;
+#pragma unroll
+            for (int y = 0; y < 8; ++y) {
+              uint4 w = vr[y];
+              const bool some = not_finite(w.x) || not_finite(w.y) || not_finite(w.z) || not_finite(w.w);
+              if (some) vr[y] = make_uint4(finite_of(w.x), finite_of(w.y), finite_of(w.z), finite_of(w.w));
+              here |= some;
+            }
+            odd |= here && kb + x % kTK < lim_any;
+          }
+          if (odd) atomicMax(odd_v, unit + 1);
+          fence_proxy_async_smem();
+          // (every softmax warp arrives on p_full after its share, so the products see all of them)
+        }
+        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s_full[j & 1], (j >> 1) & 1, abort_flag, p.budget)))) break;
+        tc_fence_after();
+        float v[kTK];
+        tmem_ld64(t_s, v);
+        if (partly) {
+#pragma unroll
+          for (int i = 0; i < kTK; ++i)
+            if (kb + i >= lim) v[i] = -INFINITY;
+        }
+        float m4[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+        for (int i = 4; i < kTK; ++i) m4[i & 3] = fmaxf(m4[i & 3], v[i]);
+        const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+        if (blk == at.lo) {
+          m_run = mx;
+        } else if (__any_sync(0xffffffffu, (mx - m_run) * p.scale_log2 > kGrown)) {
+          // a row's weights have outgrown its reference. The products before have completed once o_done says so: O can be
+          // rescaled
+          if (!(ok = __all_sync(0xffffffffu, mbar_wait(&o_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort_flag, p.budget)))) break;
+          tc_fence_after();
+          const float m_new = fmaxf(m_run, mx);
+          const float corr = m_new == m_run ? 1.0f : ex2((m_run - m_new) * p.scale_log2);
+          m_run = m_new;
+          l_run *= corr;
+#pragma unroll 1
+          for (int c = 0; c < HD / 32; ++c) {
+            float ov[32];
+            tmem_ld32(t_o + lanes + c * 32, ov);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) ov[i] *= corr;
+            tmem_st32(t_o + lanes + c * 32, ov);
+          }
+        }
+        const float off = m_run == -INFINITY ? 0.0f : m_run * p.scale_log2;  // nothing seen yet: all weights are 0
+        float r4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        uint32_t third[kTK / 2];  // keys 2 i and 2 i + 1 in word i
+#pragma unroll
+        for (int x = 0; x < kTK / 16; ++x) {
+          float first_t[8], second_t[8];  // the terms of keys 16 x + 2 i and 16 x + 2 i + 1 in word i
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int k = 16 * x + 2 * i;
+            const float p0 = ex2(fmaf(v[k], p.scale_log2, -off)), p1 = ex2(fmaf(v[k + 1], p.scale_log2, -off));
+            r4[k & 2] += p0;
+            r4[(k & 2) + 1] += p1;
+            const uint32_t hi = pack_bf16(p0, p1);
+            const float a = p0 - __uint_as_float(hi << 16), b = p1 - __uint_as_float(hi & 0xffff0000u);
+            const uint32_t mid = pack_bf16(a, b);
+            first_t[i] = __uint_as_float(hi);
+            second_t[i] = __uint_as_float(mid);
+            third[k >> 1] = pack_bf16(a - __uint_as_float(mid << 16), b - __uint_as_float(mid & 0xffff0000u));
+          }
+          tmem_st8(t_s + 16 * x, first_t);  // over the scores
+          tmem_st8(t_s + 16 * x + 8, second_t);
+        }
+        l_run += (r4[0] + r4[1]) + (r4[2] + r4[3]);
+        // the third terms' place is free when the block before has been multiplied
+        if (j > 0 && !(ok = __all_sync(0xffffffffu, mbar_wait(&o_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort_flag, p.budget)))) break;
+#pragma unroll
+        for (int y = 0; y < 8; ++y)
+          *reinterpret_cast<uint4*>(smem + L::p3 + r * 128 + ((y ^ (r & 7)) << 4)) =
+              make_uint4(third[4 * y], third[4 * y + 1], third[4 * y + 2], third[4 * y + 3]);
+        fence_proxy_async_smem();
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_full[j & 1]);
+      }
+      if (!ok) break;
+      // the next unit's Q goes in while the last products run (their S has been read, so Q is free)
+      Place then = at;
+      const bool more = then.next(p, sq);
+      const Row now = row;
+      if (more) {
+        row = row_of(then);
+        load_q(row);
+      }
+      if (!(ok = __all_sync(0xffffffffu, mbar_wait(&o_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort_flag, p.budget)))) break;
+      tc_fence_after();
+      // A V that every row sees and that is infinite: the products of a weight's terms, which can be 0 or negative, are NaN
+      // together. Which infinity a column has is the same for every row (each has a weight above 0 for it).
+      float sick = 0.0f;  // NaN where a column is not finite
+#pragma unroll 1
+      for (int c = 0; c < HD / 32; ++c) {
+        float ov[32];
+        tmem_ld32(t_o + lanes + c * 32, ov);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) sick = fmaf(ov[i], 0.0f, sick);
+      }
+      const int key0 = at.lo * kTK, key1 = min(at.hi * kTK, lim_any);
+      const __nv_bfloat16* vcol = p.pool + (size_t(p.n_kv_heads) + at.hk) * HD;
+      const size_t ld = 2 * size_t(p.n_kv_heads) * HD;
+      const int rows_all = p.n_pages * p.page_size;
+      const bool mend = now.valid && isnan(sick) && !isnan(l_run);  // (scores that are NaN leave the row NaN)
+      if (__any_sync(0xffffffffu, mend)) {
+        constexpr int E = HD / 32;  // columns a lane looks through
+        uint32_t has = 0;  // of column e in bits 4 e: +inf, -inf, NaN
+        for (int k = key0; k < min(lim_all, key1); ++k) {
+          const int at_row = pool_row(p, s.seq, k);
+          if (at_row >= rows_all) continue;
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const float x = __bfloat162float(vcol[at_row * ld + E * lane + e]);
+            has |= (isnan(x) ? 4u : x == INFINITY ? 1u : x == -INFINITY ? 2u : 0u) << (4 * e);
+          }
+        }
+#pragma unroll 1
+        for (int c = 0; c < HD / 32; ++c) {
+          float ov[32];
+          tmem_ld32(t_o + lanes + c * 32, ov);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const uint32_t h = (__shfl_sync(0xffffffffu, has, (c * 32 + i) / E) >> (4 * (i % E))) & 15u;
+            if (mend && isnan(ov[i]) && (h == 1u || h == 2u)) ov[i] = h == 1u ? INFINITY : -INFINITY;
+          }
+          tmem_st32(t_o + lanes + c * 32, ov);
+        }
+      }
+      if (*reinterpret_cast<volatile int*>(odd_v) > unit) {
+        // values of V that were cleared: rows that see one add p v in fp32 (the score again from q and k)
+        const float off = m_run == -INFINITY ? 0.0f : m_run * p.scale_log2;
+        const __nv_bfloat16* qsrc = p.q + now.row * HD;
+        for (int k = max(lim_all, key0); k < key1; ++k) {
+          const int at_row = pool_row(p, s.seq, k);
+          if (at_row >= rows_all) continue;
+          const bool sees = now.valid && k < lim;
+          const __nv_bfloat16* kr = p.pool + at_row * ld + at.hk * HD;
+          const __nv_bfloat16* vr = vcol + at_row * ld;
+          for (int c = 0; c < L::kChunks; ++c) {
+            const uint32_t two = *reinterpret_cast<const uint32_t*>(vr + c * 64 + 2 * lane);
+            if (!__any_sync(0xffffffffu, not_finite(two))) continue;
+            float d = 0.0f;
+            if (sees)
+              for (int x = 0; x < HD; ++x) d = fmaf(__bfloat162float(qsrc[x]), __bfloat162float(kr[x]), d);
+            const float w = ex2(fmaf(d, p.scale_log2, -off));
+#pragma unroll 1
+            for (int b = 0; b < 2; ++b) {
+              float ov[32];
+              tmem_ld32(t_o + lanes + c * 64 + b * 32, ov);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                const float x = __bfloat162float(vr[c * 64 + b * 32 + i]);
+                if (sees && !isfinite(x)) ov[i] = fmaf(w, x, ov[i]);
+              }
+              tmem_st32(t_o + lanes + c * 64 + b * 32, ov);
+            }
+          }
+        }
+      }
+      const float m2 = m_run * p.scale_log2;
+      if (at.hi - at.lo < at.blocks) {
+        const size_t slot = (2 * size_t(blockIdx.x) + (at.lo == 0)) * p.rows_part + r;
+        if (now.valid) p.part_ml[slot] = make_float2(m2, l_run);
+        float* po = p.part_o + slot * HD;
+#pragma unroll 1
+        for (int c = 0; c < HD / 32; ++c) {
+          float v[32];
+          tmem_ld32(t_o + lanes + c * 32, v);
+          if (now.valid) {
+#pragma unroll
+            for (int y = 0; y < 8; ++y)
+              reinterpret_cast<float4*>(po + c * 32)[y] = make_float4(v[4 * y], v[4 * y + 1], v[4 * y + 2], v[4 * y + 3]);
+          }
+        }
+      } else {
+        const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
+        __nv_bfloat16* orow = p.o + now.row * HD;
+        if (now.valid && p.lse) p.lse[now.row] = fmaf(m2, 0.6931471805599453f, logf(l_run));
+#pragma unroll 1
+        for (int c = 0; c < HD / 32; ++c) {
+          float v[32];
+          tmem_ld32(t_o + lanes + c * 32, v);
+          if (now.valid) {
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+              reinterpret_cast<uint4*>(orow + c * 32)[y] =
+                  make_uint4(pack_bf16(v[8 * y] * inv, v[8 * y + 1] * inv), pack_bf16(v[8 * y + 2] * inv, v[8 * y + 3] * inv),
+                             pack_bf16(v[8 * y + 4] * inv, v[8 * y + 5] * inv), pack_bf16(v[8 * y + 6] * inv, v[8 * y + 7] * inv));
+          }
+        }
+      }
+      tc_fence_before();  // (O is written again by products that wait for this warp's next arrival)
+      if (!more) break;
+      at = then;
+    }
+    if (!ok) {
+      *abort_flag = 1;
+      set_status(p.status, SPD_ETIMEOUT);
+    }
   }
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 128 && *abort_flag) {
+    // loads issued but never consumed land before the CTA exits
+    volatile int no_abort = 0;
+    for (int j = max(0, issued_k - NS); j < issued_k; ++j) mbar_wait(&k_full[j % NS], (j / NS) & 1, &no_abort, p.budget);
+    for (int j = max(0, issued_v - NS); j < issued_v; ++j) mbar_wait(&v_full[j % NS], (j / NS) & 1, &no_abort, p.budget);
+  }
+  __syncwarp();
+  tc_fence_after();
+  if (warp == 4) tmem_dealloc(tmem, kTmemCols);
+  if (threadIdx.x == 0) stamp_end(p.stamp);
+}
+
+// Units whose blocks several CTAs had: states (m_i, l_i, O_i) joined in key order, m = max m_i, l = sum l_i 2^(m_i - m),
+// O = sum O_i 2^(m_i - m). A part in which a row sees nothing has l_i = 0. (Its maximum does not tell: fmaxf passes over those of
+// parts whose scores are all NaN, whose sums are NaN and stay so.) blockIdx.x stands for the border between two CTAs; the first
+// border inside a unit has it. W warps a row, each a range of the parts, four of them in flight.
+constexpr int kMergeWarps = 8, kMergeAhead = 4;
+template <int HD>
+__global__ void __launch_bounds__(kMergeWarps * 32)
+    paged_merge_kernel(const __grid_constant__ PagedArgs p, const __grid_constant__ PagedSeqs sq, int W) {
+  constexpr int D = HD / 32;  // dims a lane
+  __shared__ float2 wml[kMergeWarps];
+  __shared__ float wo[kMergeWarps][HD];
+  pdl_launch_dependents();
+  const int c = int(blockIdx.x) + 1, border = first_block(p, c);
+  Place u;
+  u.seek(p, sq, border, 1);
+  const int start = border - u.lo, end = start + u.blocks;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp & (W - 1);
+  const int r = (int(blockIdx.y) * kMergeWarps + warp) / W;
+  const PagedSeq& s = sq.s[u.e];
+  const int t = u.tile / p.chunks, h0 = (u.tile - t * p.chunks) * p.chunk, n0 = t * p.tokens;
+  const int hc = r % p.chunk, token = n0 + r / p.chunk;
+  const bool mine = u.lo > 0 && first_block(p, c - 1) <= start;  // (all threads alike)
+  const bool have = mine && r < min(p.tokens, s.n - n0) * p.chunk && hc < min(p.chunk, p.group - h0);
+  const int parts = int(((long long)end * p.ctas + p.total - 1) / p.total) - (c - 1);
+  pdl_wait();
+  if (!mine) return;
+  float m = -INFINITY, l = 0.0f, o[D];
+#pragma unroll
+  for (int x = 0; x < D; ++x) o[x] = 0.0f;
+  if (have) {
+    const int s1 = int((w + 1) * parts / W);
+    for (int s0 = int(w * parts / W); s0 < s1; s0 += kMergeAhead) {
+      float2 ml[kMergeAhead];
+      float v[kMergeAhead][D];
+#pragma unroll
+      for (int k = 0; k < kMergeAhead; ++k) {
+        ml[k] = make_float2(-INFINITY, 0.0f);
+        if (s0 + k >= s1) continue;
+        const size_t slot = (2 * size_t(c - 1 + s0 + k) + (s0 + k == 0)) * p.rows_part + r;
+        ml[k] = p.part_ml[slot];
+        const float* po = p.part_o + slot * HD + D * lane;
+        if constexpr (D == 4) {
+          const float4 f = *reinterpret_cast<const float4*>(po);
+          v[k][0] = f.x, v[k][1] = f.y, v[k][2] = f.z, v[k][3] = f.w;
+        } else {
+          const float2 f = *reinterpret_cast<const float2*>(po);
+          v[k][0] = f.x, v[k][1] = f.y;
+        }
+      }
+      float top = m;
+      bool some = false;
+#pragma unroll
+      for (int k = 0; k < kMergeAhead; ++k) {
+        top = fmaxf(top, ml[k].x);
+        some |= ml[k].y != 0.0f;
+      }
+      if (!some) continue;
+      const float keep = exp2f(m - top);
+      m = top;
+      l *= keep;
+#pragma unroll
+      for (int x = 0; x < D; ++x) o[x] *= keep;
+#pragma unroll
+      for (int k = 0; k < kMergeAhead; ++k) {
+        if (ml[k].y == 0.0f) continue;  // a part in which the row sees nothing
+        const float f = exp2f(ml[k].x - m);
+        l = fmaf(ml[k].y, f, l);
+#pragma unroll
+        for (int x = 0; x < D; ++x) o[x] = fmaf(v[k][x], f, o[x]);
+      }
+    }
+  }
+  if (W > 1) {
+    if (lane == 0) wml[warp] = make_float2(m, l);
+#pragma unroll
+    for (int x = 0; x < D; ++x) wo[warp][D * lane + x] = o[x];
+    __syncthreads();
+    if (w > 0) return;
+    for (int k = 1; k < W; ++k) m = fmaxf(m, wml[warp + k].x);
+    l = 0.0f;
+#pragma unroll
+    for (int x = 0; x < D; ++x) o[x] = 0.0f;
+    for (int k = 0; k < W; ++k) {
+      const float2 ml = wml[warp + k];
+      if (ml.y == 0.0f) continue;
+      const float f = exp2f(ml.x - m);
+      l = fmaf(ml.y, f, l);
+#pragma unroll
+      for (int x = 0; x < D; ++x) o[x] = fmaf(wo[warp + k][D * lane + x], f, o[x]);
+    }
+  }
+  if (!have) return;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  for (int x = 0; x < D; ++x) p.o[at * HD + lane * D + x] = __float2bfloat16(o[x] * inv);
-  if (p.lse && lane == 0) p.lse[at] = m + logf(l);
+  const size_t at = (size_t(s.q0) + token) * p.n_heads + u.hk * p.group + h0 + hc;
+  uint32_t* to = reinterpret_cast<uint32_t*>(p.o + at * HD + D * lane);
+#pragma unroll
+  for (int x = 0; x < D / 2; ++x) to[x] = pack_bf16(o[2 * x] * inv, o[2 * x + 1] * inv);
+  if (p.lse && lane == 0) p.lse[at] = fmaf(m, 0.6931471805599453f, logf(l));
+}
+
+// Rows of a state: a tile's, or as many as the call has.
+int rows_of_part(int n_q, int n_heads, int n_kv_heads) {
+  const int chunk = std::min(n_heads / n_kv_heads, 128);
+  return std::min(128 / chunk, n_q) * chunk;
 }
 
 }  // namespace
 
-size_t paged_attention_bytes(int, int, int, int) { return 256; }
+size_t paged_attention_bytes(int n_q, int n_heads, int n_kv_heads, int head_dim) {
+  const size_t rows = 2 * size_t(kCtas) * rows_of_part(n_q, n_heads, n_kv_heads);
+  Carve cv(nullptr, ~size_t(0));
+  cv.take<float>(rows * head_dim);
+  cv.take<float2>(rows);
+  return cv.used;
+}
 
 int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, const int32_t* prefix, int n_seqs,
                         const int32_t* table, int max_pages, const void* pool, int n_pages, int page_size, int n_heads,
-                        int n_kv_heads, int head_dim, void* o, float* lse, void*, size_t, int* status, cudaStream_t st) {
+                        int n_kv_heads, int head_dim, void* o, float* lse, void* ws, size_t ws_bytes, int* status, cudaStream_t st) {
+  const int kvd = n_kv_heads * head_dim;
   PagedArgs p{};
+  p.box = 64;
+  while (page_size % p.box) p.box /= 2;  // (pages are multiples of 16 rows)
+  CUtensorMap map;
+  if (int rc = make_operand_map(&map, pool, 2 * kvd, n_pages * page_size, p.box)) return rc;
   p.q = static_cast<const __nv_bfloat16*>(q);
   p.pool = static_cast<const __nv_bfloat16*>(pool);
   p.table = table;
@@ -79,22 +744,70 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
   p.page_size = page_size;
   p.n_heads = n_heads;
   p.n_kv_heads = n_kv_heads;
-  p.scale = float(1.0 / sqrt(double(head_dim)));
+  p.group = n_heads / n_kv_heads;
+  p.chunk = std::min(p.group, 128);
+  p.chunks = (p.group + 127) / 128;
+  p.tokens = 128 / p.chunk;
+  p.scale_log2 = float(1.4426950408889634 / sqrt(double(head_dim)));
   p.o = static_cast<__nv_bfloat16*>(o);
   p.lse = lse;
+  Carve cv(ws, ws_bytes);
+  p.rows_part = rows_of_part(q_cu[n_seqs], n_heads, n_kv_heads);
+  const size_t rows = 2 * size_t(kCtas) * p.rows_part;
+  p.part_o = cv.take<float>(rows * head_dim);
+  p.part_ml = cv.take<float2>(rows);
   p.status = status;
+  p.budget = kWaitBudget;
+  const auto kernel = head_dim == 128 ? paged_attn_kernel<128> : paged_attn_kernel<64>;
+  const size_t smem = head_dim == 128 ? PagedSmem<128>::bytes : PagedSmem<64>::bytes;
+  static DeviceOnce attr[2];
+  SPD_CUDA_TRY(once_per_device(attr[head_dim == 128], [&] {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+  }));
+  const int places = std::min(kCtas, 2 * num_sms());
   for (int s0 = 0; s0 < n_seqs; s0 += kMaxSeqs) {
-    int most = 0;
-    p.n_seqs = 0;
+    PagedSeqs sq{};
+    long long total = 0;
+    int most = 0, longest = 0;
+    double pairs = 0.0, keys = 0.0, tokens = 0.0;
     for (int b = s0; b < std::min(n_seqs, s0 + kMaxSeqs); ++b) {
       const int n = q_cu[b + 1] - q_cu[b];
       if (n == 0) continue;
-      p.s[p.n_seqs++] = {q_cu[b], n, len[b], prefix ? prefix[b] : 0, b};
+      PagedSeq& s = sq.s[sq.n++];
+      s = {int(total), q_cu[b], n, len[b], prefix ? prefix[b] : 0, b, 0, (n + p.tokens - 1) / p.tokens * p.chunks};
+      long long blocks = 0;
+      for (int i = 0; i < n; i += p.tokens) {
+        const int here = blocks_at(s, i, p.tokens);
+        longest = std::max(longest, here);
+        blocks += (long long)here * p.chunks;
+      }
+      total += blocks * n_kv_heads;
+      if (total > 0x7fffffff / 2) return fail(SPD_EUNSUPPORTED, "paged attention of more than 2^30 blocks of keys");
+      s.head_blocks = int(blocks);
       most = std::max(most, n);
+      keys += len[b];
+      tokens += n;
+      pairs += double(n) * len[b] - 0.5 * double(n) * (n - 1);
     }
-    if (p.n_seqs == 0) continue;
-    SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? paged_simple_kernel<128> : paged_simple_kernel<64>,
-                            dim3((most + 7) / 8, n_heads, p.n_seqs), dim3(256), 0, st, p));
+    if (sq.n == 0) continue;
+    p.total = int(total);
+    p.ctas = int(std::min<long long>(places, total));
+    p.warps = (std::min(most, p.tokens) * p.chunk + 31) / 32;
+    const double fl = 4.0 * head_dim * n_heads * pairs;
+    const double by = 4.0 * kvd * keys + 4.0 * n_heads * head_dim * tokens;
+    p.stamp = stamp_slot(TR_ATTN, fl, by);
+    const int slot = trace_begin(st);
+    SPD_CUDA_TRY(launch_pdl(kernel, dim3(p.ctas), dim3(kThreads), smem, st, map, p, sq));
+    if (p.ctas > 1) {
+      const int parts = int((long long)longest * p.ctas / total) + 2;  // of a unit, at most
+      int W = 1;
+      while (W < kMergeWarps && parts > kMergeAhead * W) W *= 2;
+      const int rows_unit = std::min(most, p.tokens) * p.chunk;
+      SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? paged_merge_kernel<128> : paged_merge_kernel<64>,
+                              dim3(p.ctas - 1, (rows_unit * W + kMergeWarps - 1) / kMergeWarps), dim3(kMergeWarps * 32), 0, st, p, sq,
+                              W));
+    }
+    trace_end(slot, st, TR_ATTN, fl, by);
   }
   return SPD_OK;
 }
