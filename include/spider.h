@@ -613,12 +613,12 @@ size_t spd_beam_select_workspace_size(int n_seqs, int n_in, int n_out, int vocab
 /* Beam search's selection. Beam w of request b has score scores[b][w] ((dev) fp32 [n_seqs][n_in], the logarithm of its probability) and
  * logits row b * n_in + w ((dev) fp32, vocab values, stride ld). Of the candidates
  *   total(w, t) = scores[b][w] + z[t] - log sum_u exp z[u],   t != eos (eos -1: none), z[t] above -inf,
- * the n_out largest, ties to the lower beam, then to the lower token (totals in fp64): parent (dev) int32 [n_seqs][n_out] receives
+ * the n_out largest, ties to the lower beam, then to the lower token (totals are held in 48 bits): parent (dev) int32 [n_seqs][n_out] receives
  * b * n_in + w, as spd_pages_update takes it, token (dev) int32 the token, scores_out (dev) fp32 the total; -1, -1 and -inf where there
  * are fewer. A beam whose score is not finite, or whose logits hold NaN, +inf or nothing above -inf, offers nothing.
  * ended (dev, may be NULL) fp32 [n_seqs][n_in]: total(w, eos) where fewer than n_out candidates of the request go before it, the ends of
  * other beams counted, else -inf. n_in and n_out up to 32, up to 65535 beams in all; ws 16-byte aligned. The same result in every run.
- * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ENOSPC, SPD_ECUDA. */
+ * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ENOSPC, SPD_ECUDA; device timeouts in the workspace's status word. */
 int spd_beam_select(const float* logits, int n_seqs, int n_in, int vocab, int ld, const float* scores, int n_out, int eos,
                     int32_t* parent, int32_t* token, float* scores_out, float* ended, void* ws, size_t ws_bytes, void* stream);
 

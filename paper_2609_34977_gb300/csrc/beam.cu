@@ -7,10 +7,10 @@
 // A row's tokens are split over CTAs (slices). Of one row the order of the totals is that of the logits, so of a slice only its
 // n_out best can be among the request's best. A CTA streams its slice through registers: the maximum and the sum of
 // exponentials a thread, and those tokens that beat the n_out-th best so far go to a list in shared memory, which is cut back to
-// n_out when it has grown. The first bound: of n_out or more groups of threads the least of their maxima. Where more tokens beat
+// n_out when it has doubled. The first bound: of n_out or more groups of threads the least of their maxima. Where more tokens beat
 // the bound than the list holds (rising or equal logits) the batch's n_out best are taken one by one.
-// A warp a request then takes the best of the lists' heads n_out times. Totals are fp64, the sums of the slices too: candidates
-// of different beams may lie closer together than fp32 tells.
+// A warp a request then takes the best of the lists' heads n_out times. Candidates of different beams may lie closer together than
+// fp32 tells, and fp64 is slow here, so totals are pairs of fp32 values (a sum and what it was rounded by).
 #include <math.h>
 #include <stdint.h>
 
@@ -23,13 +23,15 @@
 namespace spd {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kThreads = 128, kWarps = kThreads / 32;
 constexpr int kHeld = 16;                  // tokens a thread holds
 constexpr int kBatch = kThreads * kHeld;
 constexpr int kMaxBeams = 32;
-constexpr int kList = 512;                 // candidates a CTA holds
-constexpr int kFull = 256;                 // cut back to n_out from here on
+constexpr int kList = 384;                 // candidates a CTA holds
 constexpr int kMergeThreads = 256;
+constexpr int kStages = 4;                 // batches on their way into shared memory
+constexpr int kCtasSm = 6;                 // CTAs an SM
+constexpr int kMergeBytes = 200 * 1024;    // shared memory for a request's lists
 
 struct BeamArgs {
   const float* z;
@@ -39,6 +41,8 @@ struct BeamArgs {
   float2* sums;              // [row][slice] maximum, sum of exp(z - maximum)
   int32_t *parent, *token;
   float *out, *ended;
+  int* status;
+  long long budget;
 };
 
 // A value's place in the order of floats, the token in the low half so that the first of equals wins (0: none).
@@ -66,6 +70,8 @@ __device__ __forceinline__ float exp_less(float x, float m) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"((x - m) * 1.4426950408889634f));
   return y;
 }
+// The least value above a key's.
+__device__ __forceinline__ float above(unsigned long long key) { return key_value(key + (1ull << 32)); }
 // The sum of states (maximum, sum): NaN stays, -inf adds nothing.
 __device__ __forceinline__ float2 join(float2 a, float2 b) {
   const float m = fmaxf(a.x, b.x);
@@ -73,9 +79,12 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
   return make_float2(m, a.y * exp_less(a.x, m) + b.y * exp_less(b.x, m));
 }
 
-// W = 4: rows whose 16-byte pieces are aligned; 1: any.
+// W = 4: rows whose 16-byte pieces are aligned, batches by bulk copies into shared memory; 1: any rows, through registers.
 template <int W>
-__global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_constant__ BeamArgs p) {
+__global__ void __launch_bounds__(kThreads, kCtasSm) beam_slice_kernel(const __grid_constant__ BeamArgs p) {
+  extern __shared__ __align__(128) float ring[];  // [kStages][kBatch]
+  __shared__ uint64_t full[kStages];
+  __shared__ int aborted;
   __shared__ unsigned long long list[kList], top[kMaxBeams], wbest[2][kWarps];
   __shared__ float group[kMaxBeams];
   __shared__ float2 wsum[kWarps];
@@ -88,23 +97,34 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
   pdl_wait();
   const float* z = p.z + size_t(row) * p.ld + t0;
   auto place = [&](int base, int k) { return base + (W == 4 ? (k >> 2) * (4 * kThreads) + 4 * tid + (k & 3) : k * kThreads + tid); };
-  float next[kHeld];
-  auto load = [&](int base) {
+  float next[W == 4 ? 1 : kHeld];
+  auto fetch = [&](int base, int b) {
+    if constexpr (W == 4) {
+      if (tid == 0 && base < n) {
+        const uint32_t bytes = 4u * uint32_t(min(kBatch, n - base));  // (slices are multiples of four)
+        mbar_arrive_expect_tx(&full[b % kStages], bytes);
+        bulk_load(ring + (b % kStages) * kBatch, z + base, bytes, &full[b % kStages]);
+      }
+    } else {
 #pragma unroll
-    for (int k = 0; k < kHeld; k += W) {
-      const int i = place(base, k);
-      if constexpr (W == 4) {  // (slices are multiples of four)
-        float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-        if (i < n) v = __ldcs(reinterpret_cast<const float4*>(z + i));
-        next[k] = v.x, next[k + 1] = v.y, next[k + 2] = v.z, next[k + 3] = v.w;
-      } else {
+      for (int k = 0; k < kHeld; ++k) {
+        const int i = place(base, k);
         next[k] = i < n ? __ldcs(z + i) : -INFINITY;
       }
     }
   };
-  load(0);
+  if constexpr (W == 4) {
+    if (tid == 0) {
+      aborted = 0;
+      for (int b = 0; b < kStages; ++b) mbar_init(&full[b], 1);
+      fence_mbar_init();
+      for (int b = 0; b < kStages; ++b) fetch(b * kBatch, b);
+    }
+  } else {
+    fetch(0, 0);
+  }
   float m = -INFINITY, s = 0.0f;   // of the thread's tokens
-  float bound = -INFINITY;         // a token that is not above it is not among the best
+  float low = 0.0f;                // a later token below it is not among the best
   int have = 0;                    // entries of the list
   bool sorted = true;
   __syncthreads();
@@ -120,13 +140,27 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
     if (tid < min(all, K)) list[tid] = top[tid];
     have = min(all, K);
     sorted = true;
-    if (have == K) bound = key_value(top[K - 1]);
+    if (have == K) low = above(top[K - 1]);
   };
   for (int base = 0, b = 0; base < n; base += kBatch, ++b) {
     float x[kHeld];
+    if constexpr (W == 4) {
+      if (!mbar_wait(&full[b % kStages], (b / kStages) & 1, &aborted, p.budget)) {
+        aborted = 1;
+        set_status(p.status, SPD_ETIMEOUT);
+      }
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k) x[k] = next[k];
-    if (base + kBatch < n) load(base + kBatch);
+      for (int k = 0; k < kHeld; k += 4) {
+        const int i = place(base, k);
+        float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+        if (i < n) v = *reinterpret_cast<const float4*>(ring + (b % kStages) * kBatch + i - base);
+        x[k] = v.x, x[k + 1] = v.y, x[k + 2] = v.z, x[k + 3] = v.w;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k) x[k] = next[k];
+      if (base + kBatch < n) fetch(base + kBatch, b + 1);
+    }
     float t4[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
     for (int k = 4; k < kHeld; ++k) t4[k & 3] = fmaxf(t4[k & 3], x[k]);
@@ -146,32 +180,40 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
       }
     }
     const bool first = base == 0;
-    if (first) {  // the least of the maxima of 8 warps, or of 32 groups of eight threads
+    if (first) {  // the least of the maxima of 4, 8, 16 or 32 groups of threads
+      const int width = K <= 4 ? 32 : K <= 8 ? 16 : K <= 16 ? 8 : 4;
       float g = most;
 #pragma unroll
-      for (int off = 1; off < 8; off <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, off));
-      if (K <= kWarps) {
-#pragma unroll
-        for (int off = 8; off < 32; off <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, off));
+      for (int off = 1; off < 32; off <<= 1) {
+        const float y = __shfl_xor_sync(0xffffffffu, g, off);
+        if (off < width) g = fmaxf(g, y);
       }
-      if ((lane & 7) == 0) group[tid >> 3] = g;
+      if ((lane & 3) == 0) group[tid >> 2] = g;
       __syncthreads();
       g = group[lane];
 #pragma unroll
       for (int off = 16; off; off >>= 1) g = fminf(g, __shfl_xor_sync(0xffffffffu, g, off));
-      bound = g;
+      low = fmaxf(g, -3.402823466e38f);  // (-inf is no candidate)
     }
-    if (most > bound || (first && most == bound && most > -INFINITY)) {
+    if (most >= low) {
+      uint32_t some = 0;
 #pragma unroll
-      for (int k = 0; k < kHeld; ++k) {
-        if (x[k] > bound || (first && x[k] == bound && x[k] > -INFINITY)) {
-          const int at = have + atomicAdd(&pushed[b % 3], 1);
-          if (at < kList) list[at] = order_key(x[k], t0 + place(base, k));
+      for (int k = 0; k < kHeld; ++k) some |= x[k] >= low ? 1u << k : 0u;
+      int at = have + atomicAdd(&pushed[b % 3], __popc(some));
+      if constexpr (W == 4) {
+        for (; some && at < kList; some &= some - 1, ++at) {
+          const int i = place(base, __ffs(some) - 1);
+          list[at] = order_key(ring[(b % kStages) * kBatch + i - base], t0 + i);
         }
+      } else {
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k)
+          if (((some >> k) & 1u) && at < kList) list[at++] = order_key(x[k], t0 + place(base, k));
       }
     }
     if (tid == 0) pushed[(b + 1) % 3] = 0;  // (read last before the barrier of the batch before)
     __syncthreads();
+    if constexpr (W == 4) fetch(base + kStages * kBatch, b + kStages);  // (the batch is in registers)
     const int all = have + pushed[b % 3];
     if (all > kList) {
       // the list as it was, and this batch's tokens one by one: the k-th largest of both in round k
@@ -206,9 +248,9 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
       }
       __syncthreads();
       sorted = true;
-      if (have == K) bound = key_value(top[K - 1]);
+      if (have == K) low = above(top[K - 1]);
     } else if (all > have) {
-      if (first || all > kFull) {
+      if (first || all > 2 * K) {
         cut(all);
       } else {
         have = all;
@@ -234,40 +276,59 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
   if (tid < K) p.best[at * K + tid] = tid < have ? top[tid] : 0;
 }
 
-// A candidate's order: its total, then the beam, then the token.
-struct Candidate {
-  uint32_t hi, lo;  // the total as an integer of the same order, 0: none
-  uint32_t beam, token;
-};
-__device__ __forceinline__ void set_total(Candidate& c, double t) {
-  const unsigned long long u = static_cast<unsigned long long>(__double_as_longlong(t + 0.0));
-  const unsigned long long k = (u >> 63) ? ~u : u | (1ull << 63);
-  c.hi = uint32_t(k >> 32);
-  c.lo = uint32_t(k);
+// hi + lo = a + b exactly, hi the rounded sum.
+__device__ __forceinline__ float2 two_sum(float a, float b) {
+  const float hi = __fadd_rn(a, b), x = __fsub_rn(hi, a);
+  return make_float2(hi, __fadd_rn(__fsub_rn(a, __fsub_rn(hi, x)), __fsub_rn(b, x)));
 }
-__device__ __forceinline__ double total_of(const Candidate& c) {
-  const unsigned long long k = (static_cast<unsigned long long>(c.hi) << 32) | c.lo;
-  return __longlong_as_double(static_cast<long long>((k >> 63) ? k & ~(1ull << 63) : ~k));
+// (a.x + a.y) + b as such a pair.
+__device__ __forceinline__ float2 add_pair(float2 a, float b) {
+  const float2 s = two_sum(a.x, b);
+  return two_sum(s.x, __fadd_rn(s.y, a.y));
 }
-__device__ __forceinline__ bool none(const Candidate& c) { return (c.hi | c.lo) == 0; }
-__device__ __forceinline__ bool before(const Candidate& a, const Candidate& b) {
-  if (a.hi != b.hi) return a.hi > b.hi;
-  if (a.lo != b.lo) return a.lo > b.lo;
-  return !none(a) && (a.beam != b.beam ? a.beam < b.beam : a.token < b.token);
+// The natural logarithm of l > 0 as a pair: l = 2^k f with f in [3/4, 3/2), k ln 2 in two parts.
+__device__ __forceinline__ float2 log_pair(float l) {
+  int k;
+  float f = frexpf(l, &k);  // [1/2, 1)
+  if (f < 0.75f) {
+    f *= 2.0f;
+    --k;
+  }
+  const float kh = float(k) * 0.693145751953125f;  // 16 bits of ln 2: exact
+  return add_pair(two_sum(kh, float(k) * 1.42860682030941723e-6f), log1pf(f - 1.0f));
 }
 
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t u = __float_as_uint(x + 0.0f);
+  return (u >> 31) ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float order_value(uint32_t u) { return __uint_as_float((u >> 31) ? u & 0x7fffffffu : ~u); }
+// A candidate's total as integers of the same order (the pair's values), where the beam's logits are added to `norm`; .x 0: none.
+__device__ __forceinline__ uint2 total_of(float2 norm, float z) {
+  const float2 s = add_pair(norm, z);
+  return isfinite(s.x) ? make_uint2(order_of(s.x), order_of(s.y)) : make_uint2(0u, 0u);
+}
+__device__ __forceinline__ bool more(uint2 a, uint2 b) { return a.x != b.x ? a.x > b.x : a.y > b.y; }
+
 __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const __grid_constant__ BeamArgs p) {
-  __shared__ double norm[kMaxBeams];  // what a beam's logits are added to: score - log sum; NaN where it offers nothing
-  __shared__ Candidate got[kMaxBeams], ends[kMaxBeams];
-  extern __shared__ unsigned long long keys[];  // [n_in * slices][n_out], then the heads of the lists
+  __shared__ float2 norm[kMaxBeams];  // what a beam's logits are added to: score - log sum; NaN where it offers nothing
+  __shared__ uint2 ends[kMaxBeams], got[kMaxBeams];
+  __shared__ int got_at[kMaxBeams];
+  extern __shared__ uint2 total[];    // [n_in * slices][n_out], then as many tokens, then the heads of the lists
   const int req = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int lists = p.n_in * p.slices, K = p.n_out;
-  uint8_t* head = reinterpret_cast<uint8_t*>(keys + size_t(lists) * K);
+  int* token = reinterpret_cast<int*>(total + size_t(lists) * K);
+  uint8_t* head = reinterpret_cast<uint8_t*>(token + size_t(lists) * K);
   for (int i = tid; i < lists; i += kMergeThreads) head[i] = 0;
+  int stages = 1;  // of a sum over the slices
+  while (stages < p.slices && stages < 32) stages *= 2;
   pdl_launch_dependents();
   pdl_wait();
   const unsigned long long* best = p.best + size_t(req) * lists * K;
-  for (int i = tid; i < lists * K; i += kMergeThreads) keys[i] = best[i];
+  constexpr int kAhead = 2;  // keys of a thread on their way while the sums are added up
+  unsigned long long ahead[kAhead];
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) ahead[u] = tid + u * kMergeThreads < lists * K ? best[tid + u * kMergeThreads] : 0;
   for (int w = warp; w < p.n_in; w += kMergeThreads / 32) {
     const size_t row = size_t(req) * p.n_in + w;
     const float score = p.scores[row];
@@ -276,77 +337,91 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const __grid_
     const float2 mine = lane < p.slices ? sums[lane] : make_float2(-INFINITY, 0.0f);
     float m = mine.x;
     for (int i = lane + 32; i < p.slices; i += 32) m = fmaxf(m, sums[i].x);
-#pragma unroll
-    for (int off = 16; off; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
-    auto part = [&](float2 s) { return s.x == -INFINITY ? double(s.y) : double(s.y) * double(expf(s.x - m)); };
-    double l = part(mine);
-    for (int i = lane + 32; i < p.slices; i += 32) l += part(sums[i]);
-#pragma unroll
-    for (int off = 16; off; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
-    const double c = double(score) - (double(m) + log(l));
+    for (int off = stages / 2; off; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+    auto part = [&](float2 s) { return s.x == -INFINITY ? s.y : s.y * expf(s.x - m); };
+    float2 l = make_float2(part(mine), 0.0f);
+    for (int i = lane + 32; i < p.slices; i += 32) l = add_pair(l, part(sums[i]));
+    for (int off = stages / 2; off; off >>= 1) {
+      const float2 o = make_float2(__shfl_xor_sync(0xffffffffu, l.x, off), __shfl_xor_sync(0xffffffffu, l.y, off));
+      l = add_pair(add_pair(l, o.x), o.y);
+    }
     if (lane == 0) {
-      norm[w] = isfinite(c) ? c : nan("");
-      Candidate e{0u, 0u, uint32_t(w), uint32_t(p.eos)};
-      if (isfinite(c) && end > -INFINITY) set_total(e, c + double(end));
-      ends[w] = e;
+      const float2 g = log_pair(l.x);
+      float2 c = add_pair(two_sum(score, -m), -g.x);
+      c = add_pair(c, -g.y - l.y / l.x);  // (l.y: what l.x was rounded by)
+      norm[w] = isfinite(c.x) && isfinite(c.y) ? c : make_float2(NAN, NAN);
+      ends[w] = total_of(norm[w], end);
     }
   }
   __syncthreads();
+  for (int i = tid, u = 0; i < lists * K; i += kMergeThreads, ++u) {
+    const unsigned long long key = u == 0 ? ahead[0] : u == 1 ? ahead[1] : best[i];
+    total[i] = key ? total_of(norm[i / (p.slices * K)], key_value(key)) : make_uint2(0u, 0u);
+    token[i] = int(0xffffffffu - uint32_t(key));
+  }
+  __syncthreads();
   if (warp > 0) return;
-  Candidate mine;
-  int from = 0;
-  auto refresh = [&]() {  // the best head of the lane's lists
-    mine = Candidate{0u, 0u, 0u, 0u};
+  // The best head of the lane's lists. A lane's lists ascend in (beam, token), so the first of equals is the one that goes first.
+  uint2 mine;
+  int from = 0;  // its place
+  auto refresh = [&]() {
+    mine = make_uint2(0u, 0u);
     for (int i = lane; i < lists; i += 32) {
-      const int w = i / p.slices, k = head[i];
-      const unsigned long long key = k < K ? keys[i * K + k] : 0;
-      if (key == 0 || isnan(norm[w])) continue;
-      Candidate c{0u, 0u, uint32_t(w), 0xffffffffu - uint32_t(key)};
-      set_total(c, norm[w] + double(key_value(key)));
-      if (before(c, mine)) {
+      const int k = head[i];
+      const uint2 c = k < K ? total[i * K + k] : make_uint2(0u, 0u);
+      if (more(c, mine)) {
         mine = c;
-        from = i;
+        from = i * K + k;
       }
     }
   };
   refresh();
   for (int k = 0; k < K; ++k) {
-    const uint32_t hi = __reduce_max_sync(0xffffffffu, mine.hi);
-    bool in = mine.hi == hi;
-    const uint32_t lo = __reduce_max_sync(0xffffffffu, in ? mine.lo : 0u);
-    in &= mine.lo == lo;
-    const uint32_t beam = __reduce_min_sync(0xffffffffu, in ? mine.beam : 0xffffffffu);
-    in &= mine.beam == beam;
-    const uint32_t token = __reduce_min_sync(0xffffffffu, in ? mine.token : 0xffffffffu);
-    in &= mine.token == token;
-    const bool any = (hi | lo) != 0;
-    if (lane == 0) got[k] = Candidate{hi, lo, beam, token};
-    if (any && in) {
-      ++head[from];
-      refresh();
+    const uint32_t hi = __reduce_max_sync(0xffffffffu, mine.x);
+    bool in = mine.x == hi;
+    const uint32_t lo = __reduce_max_sync(0xffffffffu, in ? mine.y : 0u);
+    in &= mine.y == lo;
+    uint32_t who = __ballot_sync(0xffffffffu, in);
+    // equal totals: the lowest list (beams, then slices) has the lowest beam and token
+    if (who & (who - 1)) {
+      const uint32_t first = __reduce_min_sync(0xffffffffu, in ? uint32_t(from) : ~0u);
+      who = __ballot_sync(0xffffffffu, in && uint32_t(from) == first);
     }
-    __syncwarp();
+    const bool won = lane == __ffs(who) - 1;
+    if (won) {
+      got[k] = mine;
+      got_at[k] = from;
+      if (hi != 0) {
+        ++head[from / K];
+        refresh();
+      }
+    }
   }
+  __syncwarp();
   for (int i = lane; i < K; i += 32) {
-    const Candidate c = got[i];
+    const uint2 c = got[i];
     const size_t at = size_t(req) * K + i;
-    p.parent[at] = none(c) ? -1 : req * p.n_in + int(c.beam);
-    p.token[at] = none(c) ? -1 : int(c.token);
-    p.out[at] = none(c) ? -INFINITY : float(total_of(c));
+    p.parent[at] = c.x ? req * p.n_in + got_at[i] / (p.slices * K) : -1;
+    p.token[at] = c.x ? token[got_at[i]] : -1;
+    p.out[at] = c.x ? order_value(c.x) : -INFINITY;
   }
   if (p.ended && lane < p.n_in) {
-    const Candidate e = ends[lane];
-    int ahead = 0;
-    for (int k = 0; k < K; ++k) ahead += before(got[k], e);
-    for (int w = 0; w < p.n_in; ++w) ahead += before(ends[w], e);
-    p.ended[size_t(req) * p.n_in + lane] = !none(e) && ahead < K ? float(total_of(e)) : -INFINITY;
+    const uint2 e = ends[lane];
+    int first = 0;  // candidates that go before it
+    for (int k = 0; k < K; ++k) {
+      const uint2 c = got[k];
+      const int w = got_at[k] / (p.slices * K);
+      first += more(c, e) || (c.x == e.x && c.y == e.y && (w != lane ? w < lane : token[got_at[k]] < p.eos));
+    }
+    for (int w = 0; w < p.n_in; ++w) first += more(ends[w], e) || (ends[w].x == e.x && ends[w].y == e.y && w < lane);
+    p.ended[size_t(req) * p.n_in + lane] = e.x && first < K ? order_value(e.x) : -INFINITY;
   }
 }
 
-// Slices a row: as many as fill the GPU (four CTAs on each of 152 SMs), of a batch at least.
-int slices_of(int rows, int vocab) {
-  const int most = (vocab + kBatch - 1) / kBatch;
-  return std::max(1, std::min(most, 4 * 152 / std::max(1, rows)));
+// Slices a row: as many as fill the GPU (kCtasSm CTAs on each of 152 SMs), of a batch at least, whose lists a merging CTA can hold.
+int slices_of(int n_seqs, int n_in, int n_out, int vocab) {
+  const int most = std::min((vocab + kBatch - 1) / kBatch, kMergeBytes / (n_in * (12 * n_out + 1)));
+  return std::max(1, std::min(most, kCtasSm * 152 / std::max(1, n_seqs * n_in)));
 }
 
 }  // namespace
@@ -356,7 +431,7 @@ using namespace spd;
 
 extern "C" size_t spd_beam_select_workspace_size(int n_seqs, int n_in, int n_out, int vocab) {
   if (n_seqs < 1 || n_in < 1 || n_out < 1 || vocab < 1 || n_in > kMaxBeams || n_out > kMaxBeams) return 0;
-  const size_t lists = size_t(n_seqs) * n_in * slices_of(n_seqs * n_in, vocab);
+  const size_t lists = size_t(n_seqs) * n_in * slices_of(n_seqs, n_in, n_out, vocab);
   Carve cv(nullptr, ~size_t(0));
   cv.take<unsigned long long>(lists * n_out);
   cv.take<float2>(lists);
@@ -378,7 +453,7 @@ extern "C" int spd_beam_select(const float* logits, int n_seqs, int n_in, int vo
   p.ld = ld;
   p.n_in = n_in;
   p.n_out = n_out;
-  p.slices = slices_of(n_seqs * n_in, vocab);
+  p.slices = slices_of(n_seqs, n_in, n_out, vocab);
   p.slice = ((vocab + p.slices - 1) / p.slices + 3) & ~3;
   p.eos = eos;
   p.scores = scores;
@@ -391,15 +466,20 @@ extern "C" int spd_beam_select(const float* logits, int n_seqs, int n_in, int vo
   p.token = token;
   p.out = scores_out;
   p.ended = ended;
+  p.status = cv.status();
+  p.budget = kWaitBudget;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int slot = trace_begin(st);
   const bool vec = vocab % 4 == 0 && ld % 4 == 0 && (reinterpret_cast<uintptr_t>(logits) & 15) == 0;
-  const size_t smem = size_t(n_in) * p.slices * (8 * size_t(n_out) + 1);
+  const size_t smem = size_t(n_in) * p.slices * (12 * size_t(n_out) + 1);
+  constexpr int kRing = kStages * kBatch * 4;
   static DeviceOnce once;
   SPD_CUDA_TRY(once_per_device(once, [] {
-    return cudaFuncSetAttribute(beam_merge_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+    const cudaError_t e = cudaFuncSetAttribute(beam_merge_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMergeBytes);
+    return e ? e : cudaFuncSetAttribute(beam_slice_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRing);
   }));
-  SPD_CUDA_TRY(launch_pdl(vec ? beam_slice_kernel<4> : beam_slice_kernel<1>, dim3(p.slices, n_seqs * n_in), dim3(kThreads), 0, st, p));
+  SPD_CUDA_TRY(launch_pdl(vec ? beam_slice_kernel<4> : beam_slice_kernel<1>, dim3(p.slices, n_seqs * n_in), dim3(kThreads),
+                          vec ? kRing : 0, st, p));
   SPD_CUDA_TRY(launch_pdl(beam_merge_kernel, dim3(n_seqs), dim3(kMergeThreads), smem, st, p));
   trace_end(slot, st, TR_ROWS, 0.0, 4.0 * n_seqs * n_in * double(vocab));
   return SPD_OK;

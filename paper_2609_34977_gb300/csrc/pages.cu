@@ -22,8 +22,11 @@ namespace cg = cooperative_groups;
 // Pair (j, j + d/2) of a head turns by pos[axis_j] theta^(-2j/d). An angle is kept in turns: theta^(-2j/d) / 2 pi as a 64-bit
 // fraction times the integer position, modulo 2^64, is exact but for the fraction's own rounding (2^-56 a position), so far
 // positions lose nothing; its upper 32 bits go through sincospi.
-// A thread has 8 pairs of a token (16 bytes of either half) for U heads, so that it works its angles out once.
+// A thread has 8 pairs of a token (16 bytes of either half) for U heads, so that it works its angles out once for four of them
+// where there are threads enough. Heads of 128, 36 of 64 / 256 / 1024 / 4096 tokens with one and with four: 3.5 and 4.8 / 6.7 and
+// 5.0 / 10.6 and 8.8 / 34.9 and 19.9 us; 96 of 64 / 4096: 5.1 and 4.9 / 73 and 39 (199 MB, 5.1 TB/s).
 constexpr int kRopeThreads = 256;
+constexpr long long kRopeSingle = 40000;  // threads of a head each up to which it is one
 constexpr int kRopeSeqs = 384;  // sequences whose places fit in a launch's parameters
 
 struct RopeSeq {
@@ -48,7 +51,7 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 }
 
 template <int HD, int U>
-__global__ void __launch_bounds__(kRopeThreads) rope_pages_kernel(const __grid_constant__ RopeArgs p) {
+__global__ void __launch_bounds__(kRopeThreads, 4) rope_pages_kernel(const __grid_constant__ RopeArgs p) {
   constexpr int P = HD / 16;  // threads a head
   const int heads = p.n_heads + 2 * p.n_kv_heads, slots = (heads + U - 1) / U;  // a thread's heads are `slots` apart
   const unsigned at = blockIdx.x * kRopeThreads + threadIdx.x;
@@ -131,11 +134,10 @@ struct UpdateArgs {
   int n_pages, page_size, n_in, n_out, max_pages;
   const int32_t *ref_in, *table_in, *len_in, *parent, *grow;
   int32_t *ref_out, *table_out, *len_out;
-  int32_t *kids, *count;        // [n_in], [n_pages]
-  unsigned long long* owner;    // [n_pages]
-  int32_t *first, *copy_at;     // [n_out] index of its first page among the new ones; of its copy, or -1
-  int32_t* free_list;           // [n_pages]
-  PageCopy* copies;             // [n_out]
+  int32_t *count, *free_list;                                  // counters and lists in the workspace
+  unsigned long long* owner;
+  int32_t *kids, *rows, *from, *more, *tail, *first, *copy_at;
+  PageCopy* copies;                                            // [n_out]
   int* n_copies;
   int* status;
 };
@@ -166,55 +168,72 @@ __device__ int page_prefix(int v, int* tmp, int* total) {
 // ceil(rows / page)
 __device__ __forceinline__ int pages_for(int rows, int page) { return int((unsigned(rows) + unsigned(page) - 1u) / unsigned(page)); }
 
-__global__ void __launch_bounds__(kPageThreads, 1) pages_update_kernel(const __grid_constant__ UpdateArgs p) {
+// What bounds it: a chain of dependent loads, phases that wait for each other. So the counters live in shared memory where they fit
+// (kPageShared: about 8000 pages and 1000 sequences), in the workspace beyond; the lists are read once, side by side.
+constexpr size_t kPageShared = 200 * 1024;
+__host__ __device__ inline size_t page_bytes(int n_pages, int n_in, int n_out) {
+  return 20 * size_t(n_pages) + 8 * size_t(n_in) + 20 * size_t(n_out);
+}
+
+__global__ void __launch_bounds__(kPageThreads, 1) pages_update_kernel(const __grid_constant__ UpdateArgs p, bool shared) {
   __shared__ int tmp[kPageWarps];
+  extern __shared__ unsigned long long mem[];
   const int tid = threadIdx.x, room = int(min(0x7fffffffLL, (long long)p.max_pages * p.page_size));
+  unsigned long long* owner = shared ? mem : p.owner;                                         // [n_pages]
+  int* count = shared ? reinterpret_cast<int*>(mem + p.n_pages) : p.count;                    // [n_pages]
+  int* ref = shared ? count + p.n_pages : p.ref_out;                                          // [n_pages]
+  int* free_list = shared ? ref + p.n_pages : p.free_list;                                    // [n_pages]
+  int* kids = shared ? free_list + p.n_pages : p.kids;                                        // [n_in]
+  int* rows = shared ? kids + p.n_in : p.rows;                                                // [n_in] rows that it holds
+  int* from = shared ? rows + p.n_in : p.from;                                                // [n_out] parent, or -1
+  int* more = shared ? from + p.n_out : p.more;                                               // [n_out] rows that it grows by
+  int* tail = shared ? more + p.n_out : p.tail;                                               // [n_out] its last page if not full, or -1
+  int* first = shared ? tail + p.n_out : p.first;                                             // [n_out] its first new page among all
+  int* copy_at = shared ? first + p.n_out : p.copy_at;                                        // [n_out] its copy, or -1
   pdl_launch_dependents();
   pdl_wait();
-  auto parent_of = [&](int b) {
-    const int i = p.parent ? p.parent[b] : b;
-    return unsigned(i) < unsigned(p.n_in) ? i : -1;
-  };
-  auto rows_of = [&](int i) {
-    if (i < 0) return 0;
+  auto page_of = [&](int q) { return unsigned(q) < unsigned(p.n_pages) ? q : -1; };
+  // this thread's first entry of the tables, on its way while the lengths are read
+  const unsigned width = unsigned(p.max_pages), entries = unsigned(p.n_in) * width, entries_out = unsigned(p.n_out) * width;
+  const int entry = unsigned(tid) < entries ? p.table_in[tid] : -1;
+  for (int i = tid; i < p.n_in; i += kPageThreads) {
     const int n = p.len_in[i];
     if (n < 0 || n > room) set_status(p.status, SPD_EINVAL);
-    return min(max(n, 0), room);
-  };
-  auto grow_of = [&](int b, int held) {
-    const int n = p.grow ? p.grow[b] : 0;
-    if (n < 0 || n > room - held) set_status(p.status, SPD_EINVAL);
-    return min(max(n, 0), room - held);
-  };
-  auto listed = [&](int i, int k) {  // page k of input i, or -1
-    const int q = p.table_in[size_t(i) * p.max_pages + k];
-    return unsigned(q) < unsigned(p.n_pages) ? q : -1;
-  };
-  for (int i = tid; i < p.n_in; i += kPageThreads) p.kids[i] = 0;
-  for (int i = tid; i < p.n_pages; i += kPageThreads) {
-    p.ref_out[i] = p.ref_in[i];
-    p.count[i] = 0;
-    p.owner[i] = 0;
+    rows[i] = min(max(n, 0), room);
+    kids[i] = 0;
   }
-  __syncthreads();
   for (int b = tid; b < p.n_out; b += kPageThreads) {
-    const int i = parent_of(b);
-    if (i < 0) continue;
-    atomicAdd(&p.kids[i], 1);
-    const int held = rows_of(i), part = held % p.page_size;
-    if (part == 0) continue;
-    const int q = listed(i, held / p.page_size);
-    if (q < 0) continue;
-    atomicAdd(&p.count[q], 1);
-    atomicMax(&p.owner[q], (static_cast<unsigned long long>(part) << 32) | (0xffffffffu - unsigned(b)));
+    const int i = p.parent ? p.parent[b] : b;
+    from[b] = unsigned(i) < unsigned(p.n_in) ? i : -1;
+    more[b] = p.grow ? p.grow[b] : 0;
+  }
+  for (int i = tid; i < p.n_pages; i += kPageThreads) {
+    ref[i] = p.ref_in[i];
+    count[i] = 0;
+    owner[i] = 0;
   }
   __syncthreads();
-  for (size_t x = tid; x < size_t(p.n_in) * p.max_pages; x += kPageThreads) {
-    const int i = int(x / p.max_pages), k = int(x - size_t(i) * p.max_pages);
-    if (k >= pages_for(rows_of(i), p.page_size)) continue;
-    const int q = listed(i, k), more = p.kids[i] - 1;
+  auto held_by = [&](int b) { return from[b] < 0 ? 0 : rows[from[b]]; };
+  for (int b = tid; b < p.n_out; b += kPageThreads) {
+    const int i = from[b], held = held_by(b), part = held % p.page_size, n = more[b];
+    if (n < 0 || n > room - held) set_status(p.status, SPD_EINVAL);
+    more[b] = min(max(n, 0), room - held);
+    tail[b] = -1;
+    if (i < 0) continue;
+    atomicAdd(&kids[i], 1);
+    if (part == 0) continue;
+    const int q = tail[b] = page_of(p.table_in[size_t(i) * p.max_pages + held / p.page_size]);
+    if (q < 0) continue;
+    atomicAdd(&count[q], 1);
+    atomicMax(&owner[q], (static_cast<unsigned long long>(part) << 32) | (0xffffffffu - unsigned(b)));
+  }
+  __syncthreads();
+  for (unsigned x = tid; x < entries; x += kPageThreads) {
+    const int i = int(x / width), k = int(x - i * width);
+    if (k >= pages_for(rows[i], p.page_size)) continue;
+    const int q = page_of(x == unsigned(tid) ? entry : p.table_in[x]), change = kids[i] - 1;
     if (q < 0) set_status(p.status, SPD_EINVAL);
-    else if (more != 0 && atomicAdd(&p.ref_out[q], more) + more < 0) set_status(p.status, SPD_EINVAL);
+    else if (change != 0 && atomicAdd(&ref[q], change) + change < 0) set_status(p.status, SPD_EINVAL);
   }
   __syncthreads();
   int need = 0, copies = 0;
@@ -222,20 +241,16 @@ __global__ void __launch_bounds__(kPageThreads, 1) pages_update_kernel(const __g
     const int b = b0 + tid;
     int fresh = 0, copy = 0;
     if (b < p.n_out) {
-      const int i = parent_of(b), held = rows_of(i), more = grow_of(b, held), part = held % p.page_size;
-      const int q = part > 0 && more > 0 ? listed(i, held / p.page_size) : -1;
-      if (q >= 0) {
-        const bool mine = uint32_t(p.owner[q]) == 0xffffffffu - unsigned(b);
-        copy = !(mine && p.ref_out[q] == p.count[q]);
-      }
-      fresh = pages_for(held + more, p.page_size) - pages_for(held, p.page_size) + copy;
-      p.len_out[b] = held + more;
+      const int held = held_by(b), q = more[b] > 0 ? tail[b] : -1;
+      if (q >= 0) copy = !(uint32_t(owner[q]) == 0xffffffffu - unsigned(b) && ref[q] == count[q]);
+      fresh = pages_for(held + more[b], p.page_size) - pages_for(held, p.page_size) + copy;
+      p.len_out[b] = held + more[b];
     }
     int all, all_copies;
     const int at = page_prefix(fresh, tmp, &all), c = page_prefix(copy, tmp, &all_copies);
     if (b < p.n_out) {
-      p.first[b] = need + at;
-      p.copy_at[b] = copy ? copies + c : -1;
+      first[b] = need + at;
+      copy_at[b] = copy ? copies + c : -1;
     }
     need += all;
     copies += all_copies;
@@ -243,39 +258,40 @@ __global__ void __launch_bounds__(kPageThreads, 1) pages_update_kernel(const __g
   if (tid == 0) *p.n_copies = copies;
   __syncthreads();
   for (int b = tid; b < p.n_out; b += kPageThreads)
-    if (p.copy_at[b] >= 0) {
-      const int i = parent_of(b);
-      atomicSub(&p.ref_out[listed(i, rows_of(i) / p.page_size)], 1);
-    }
+    if (copy_at[b] >= 0) atomicSub(&ref[tail[b]], 1);
   __syncthreads();
   int found = 0;
   for (int q0 = 0; q0 < p.n_pages && found < need; q0 += kPageThreads) {
     const int q = q0 + tid;
-    const int is = q < p.n_pages && p.ref_out[q] <= 0;
+    const int is = q < p.n_pages && ref[q] <= 0;
     int all;
     const int at = page_prefix(is, tmp, &all);
-    if (is && found + at < need) p.free_list[found + at] = q;
+    if (is && found + at < need) free_list[found + at] = q;
     found += all;
   }
   const int got = min(found, need);
   if (found < need && tid == 0) set_status(p.status, SPD_ENOSPC);
   __syncthreads();
-  for (size_t x = tid; x < size_t(p.n_out) * p.max_pages; x += kPageThreads) {
-    const int b = int(x / p.max_pages), k = int(x - size_t(b) * p.max_pages);
-    const int i = parent_of(b), held = rows_of(i), copy = p.copy_at[b];
+  for (unsigned x = tid; x < entries_out; x += kPageThreads) {
+    const int b = int(x / width), k = int(x - b * width);
+    const int held = held_by(b), copy = copy_at[b];
     const int have = pages_for(held, p.page_size), at = have - (copy >= 0);
     int q = -1;
     if (k < at) {
-      q = listed(i, k);
-    } else if (k < pages_for(p.len_out[b], p.page_size)) {
-      const int f = p.first[b] + k - at;
+      q = page_of(p.table_in[size_t(from[b]) * p.max_pages + k]);
+    } else if (k < pages_for(held + more[b], p.page_size)) {
+      const int f = first[b] + k - at;
       if (f < got) {
-        q = p.free_list[f];
-        p.ref_out[q] = 1;
+        q = free_list[f];
+        ref[q] = 1;
       }
-      if (k < have) p.copies[copy] = {listed(i, k), q, held % p.page_size};
+      if (k < have) p.copies[copy] = {tail[b], q, held % p.page_size};
     }
     p.table_out[x] = q;
+  }
+  if (shared) {
+    __syncthreads();
+    for (int i = tid; i < p.n_pages; i += kPageThreads) p.ref_out[i] = ref[i];
   }
 }
 
@@ -375,7 +391,7 @@ int copy_pages(uint16_t* pool, const PageCopy* copies, const int* n, int n_layer
 }
 
 struct PagesWs {
-  int32_t *kids, *count, *first, *copy_at, *free_list;
+  int32_t *count, *free_list, *kids, *rows, *from, *more, *tail, *first, *copy_at;
   unsigned long long* owner;
   PageCopy* copies;
   int* n_copies;
@@ -386,9 +402,7 @@ PagesWs carve_pages(Carve& cv, int n_pages, int n_seqs) {
   w.owner = cv.take<unsigned long long>(n_pages);
   w.count = cv.take<int32_t>(n_pages);
   w.free_list = cv.take<int32_t>(n_pages);
-  w.kids = cv.take<int32_t>(n_seqs);
-  w.first = cv.take<int32_t>(n_seqs);
-  w.copy_at = cv.take<int32_t>(n_seqs);
+  for (int32_t** list : {&w.kids, &w.rows, &w.from, &w.more, &w.tail, &w.first, &w.copy_at}) *list = cv.take<int32_t>(n_seqs);
   w.copies = cv.take<PageCopy>(most);
   w.n_copies = cv.take<int>(1);
   return w;
@@ -440,10 +454,23 @@ int rope_pages_run(const void* q, int ldq, const void* kv, int ldkv, const int32
   p.pool = static_cast<uint16_t*>(pool);
   p.q_out = static_cast<uint16_t*>(q_out);
   p.status = status;
+  // (64 powers take 3 us: a thread keeps those of the base that it used last)
+  static thread_local struct {
+    double theta = 0.0;
+    int head_dim = 0;
+    uint64_t turns[64];
+  } kept;
+  if (kept.theta != theta || kept.head_dim != head_dim) {
+    kept.theta = theta;
+    kept.head_dim = head_dim;
+    for (int j = 0; j < head_dim / 2; ++j) {
+      const double f = pow(theta, -2.0 * j / head_dim) / 6.283185307179586476925;
+      kept.turns[j] = uint64_t((f - floor(f)) * 18446744073709551616.0);
+    }
+  }
   for (int j = 0; j < head_dim / 2; ++j) {
-    const double f = pow(theta, -2.0 * j / head_dim) / 6.283185307179586476925;
-    p.turns[j] = uint64_t((f - floor(f)) * 18446744073709551616.0);
-    p.axis[j] = axis && axis[j] >= n_axes ? uint8_t(n_axes) : axis ? axis[j] : 0;
+    p.turns[j] = kept.turns[j];
+    p.axis[j] = !axis ? 0 : axis[j] < n_axes ? axis[j] : uint8_t(n_axes);
   }
   const int heads = n_heads + 2 * n_kv_heads, P = head_dim / 16;
   for (int s0 = 0; s0 < n_seqs; s0 += kRopeSeqs) {
@@ -454,12 +481,14 @@ int rope_pages_run(const void* q, int ldq, const void* kv, int ldkv, const int32
     p.table = table + size_t(s0) * max_pages;
     for (int b = 0; b < p.n_seqs; ++b)
       p.seq[b] = {q_cu[s0 + b], len[s0 + b] - (q_cu[s0 + b + 1] - q_cu[s0 + b])};
-    const int U = 1;
+    const long long single = (long long)p.n_tok * heads * P;
+    if (single > 0x7fffffffLL) return fail(SPD_EUNSUPPORTED, "%d tokens of %d heads in one call", p.n_tok, heads);
+    const int U = single > kRopeSingle ? 4 : 1;
     const long long threads = (long long)p.n_tok * ((heads + U - 1) / U) * P;
-    if (threads > 0x7fffffffLL) return fail(SPD_EUNSUPPORTED, "%d tokens of %d heads in one call", p.n_tok, heads);
+    const auto kernel = head_dim == 128 ? (U == 4 ? rope_pages_kernel<128, 4> : rope_pages_kernel<128, 1>)
+                                        : (U == 4 ? rope_pages_kernel<64, 4> : rope_pages_kernel<64, 1>);
     const int slot = trace_begin(st);
-    SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? rope_pages_kernel<128, 1> : rope_pages_kernel<64, 1>,
-                            dim3(unsigned((threads + kRopeThreads - 1) / kRopeThreads)), dim3(kRopeThreads), 0, st, p));
+    SPD_CUDA_TRY(launch_pdl(kernel, dim3(unsigned((threads + kRopeThreads - 1) / kRopeThreads)), dim3(kRopeThreads), 0, st, p));
     trace_end(slot, st, TR_ROWS, 0.0, 4.0 * p.n_tok * heads * head_dim);
   }
   return SPD_OK;
@@ -508,11 +537,42 @@ extern "C" int spd_pages_update(uint16_t* pool, int n_layers, int n_pages, int p
   Carve cv(ws, ws_bytes);
   const PagesWs w = carve_pages(cv, n_pages, std::max(n_in, n_out));
   if (!cv.fits()) return fail(SPD_ENOSPC, "page workspace too small (%zu < %zu)", ws_bytes, cv.used);
-  UpdateArgs p{n_pages,   page_size, n_in,    n_out,   max_pages, ref_in,  table_in,    len_in,   parent,     grow,        ref_out,
-               table_out, len_out,   w.kids,  w.count, w.owner,   w.first, w.copy_at, w.free_list, w.copies, w.n_copies, cv.status()};
+  UpdateArgs p{};
+  p.n_pages = n_pages;
+  p.page_size = page_size;
+  p.n_in = n_in;
+  p.n_out = n_out;
+  p.max_pages = max_pages;
+  p.ref_in = ref_in;
+  p.table_in = table_in;
+  p.len_in = len_in;
+  p.parent = parent;
+  p.grow = grow;
+  p.ref_out = ref_out;
+  p.table_out = table_out;
+  p.len_out = len_out;
+  p.count = w.count;
+  p.free_list = w.free_list;
+  p.owner = w.owner;
+  p.kids = w.kids;
+  p.rows = w.rows;
+  p.from = w.from;
+  p.more = w.more;
+  p.tail = w.tail;
+  p.first = w.first;
+  p.copy_at = w.copy_at;
+  p.copies = w.copies;
+  p.n_copies = w.n_copies;
+  p.status = cv.status();
+  const size_t smem = page_bytes(n_pages, n_in, n_out);
+  const bool shared = smem <= kPageShared;
+  static DeviceOnce once;
+  SPD_CUDA_TRY(once_per_device(once, [] {
+    return cudaFuncSetAttribute(pages_update_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kPageShared));
+  }));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int slot = trace_begin(st);
-  SPD_CUDA_TRY(launch_pdl(pages_update_kernel, dim3(1), dim3(kPageThreads), 0, st, p));
+  SPD_CUDA_TRY(launch_pdl(pages_update_kernel, dim3(1), dim3(kPageThreads), shared ? smem : 0, st, p, shared));
   const int rc = copy_pages(pool, w.copies, w.n_copies, n_layers, n_pages, page_size, n_kv_heads * head_dim / 4, st);
   trace_end(slot, st, TR_ROWS, 0.0, 8.0 * n_pages + 4.0 * (double(n_in) + n_out) * max_pages);
   return rc;

@@ -26,7 +26,8 @@ def _plain(z, scores, eos, n_out):
             if not np.isfinite(scores[b, w]) or np.isnan(row).any() or np.isposinf(row).any() or np.isneginf(row).all():
                 continue
             top = row.max()
-            t = float(scores[b, w]) + row - (top + np.log(np.exp(row - top).sum()))
+            # (the maximum first: a logit of -3e38 would swallow the logarithm, in 64 bits too)
+            t = float(scores[b, w]) + ((row - top) - np.log(np.exp(row - top).sum()))
             keep = np.argsort(-t, kind="stable")[:n_out + 2]
             cand += [(-t[i], w, int(i)) for i in np.union1d(keep, [eos] if eos >= 0 else []).astype(int) if t[i] > -np.inf]
         cand.sort()
