@@ -56,6 +56,7 @@ struct PagedArgs {
   int max_pages, n_pages, page_size, box;  // box: rows that one TMA load brings (they divide the page and the block)
   int n_heads, n_kv_heads;
   int group, chunk, chunks, tokens;  // heads a group; of them in a tile; tiles across; tokens a tile
+  int keys;                          // a block's
   float scale_log2;
   __nv_bfloat16* o;
   float* lse;
@@ -104,9 +105,9 @@ __host__ __device__ __forceinline__ int limit_of(const PagedSeq& s, int i) {
   return own > s.prefix ? own : s.prefix;
 }
 // Blocks of the tiles that begin with token i.
-__host__ __device__ __forceinline__ int blocks_at(const PagedSeq& s, int i, int tokens) {
+__host__ __device__ __forceinline__ int blocks_at(const PagedSeq& s, int i, int tokens, int keys) {
   const int last = i + tokens < s.n ? i + tokens : s.n;
-  return (limit_of(s, last - 1) + kTK - 1) / kTK;
+  return int(uint32_t(limit_of(s, last - 1) + keys - 1) / uint32_t(keys));
 }
 // First block of CTA c's stretch.
 __device__ __forceinline__ int first_block(const PagedArgs& p, int c) { return int((long long)c * p.total / p.ctas); }
@@ -116,7 +117,7 @@ __device__ __forceinline__ int first_block(const PagedArgs& p, int c) { return i
 struct Place {
   int e, hk, tile, blocks, lo, hi, left;  // left: blocks of the stretch from lo on
   __device__ __forceinline__ void size(const PagedArgs& p, const PagedSeqs& sq) {
-    blocks = blocks_at(sq.s[e], tile / p.chunks * p.tokens, p.tokens);
+    blocks = blocks_at(sq.s[e], tile / p.chunks * p.tokens, p.tokens, p.keys);
     hi = min(blocks, lo + left);
   }
   // The unit of block `at` of the list (a whole warp, all lanes with the same arguments).
@@ -133,7 +134,7 @@ struct Place {
     lo -= hk * s.head_blocks;
     const int lane = threadIdx.x & 31;
     for (int t0 = 0;; t0 += 32) {
-      const int t = t0 + lane, mine = t < s.tiles ? blocks_at(s, t / p.chunks * p.tokens, p.tokens) : 0;
+      const int t = t0 + lane, mine = t < s.tiles ? blocks_at(s, t / p.chunks * p.tokens, p.tokens, p.keys) : 0;
       int sum = mine;
 #pragma unroll
       for (int off = 1; off < 32; off <<= 1) {
@@ -611,15 +612,415 @@ __global__ void __launch_bounds__(kThreads, 2)
   if (threadIdx.x == 0) stamp_end(p.stamp);
 }
 
+// ---- single tokens --------------------------------------------------------------------------------
+// A sequence's one new token with up to 16 query heads a K/V head (heads of 128): too few rows to fill an MMA's 128, so
+// keys and dims are its rows: S^T = K Q^T (128 keys x 16 heads), O^T += V^T P^T (128 dims x 64), V in place as an MN-major
+// operand, P^T through shared memory. P^T's columns are the three bf16 terms of every head's weights, side by side (48 of 64), so
+// V is read once for all of them and a term that is zero or negative does not meet an infinite V in another's sum. One CTA an
+// SM, three blocks of 128 keys on their way:
+//   warp 4     TMA producer          warp 5     MMA issuer          warp 6     the units' Q, a unit ahead
+//   warps 0-3  a thread a key: exponentials against a reference a head, renewed for all of them once a score has
+//              outgrown one by kGrown; sums a thread, added up at the end. In the end a thread a dim: O out of TMEM.
+constexpr int kTokenKeys = 128, kTokenHeads = 16, kTokenStages = 3;
+constexpr int kTokenThreads = 224;
+struct TokenSmem {
+  static constexpr uint32_t box = kTokenKeys * 128;        // 64 columns of a block of K or V
+  static constexpr uint32_t qbox = kTokenHeads * 128;      // 64 columns of Q
+  static constexpr uint32_t k = 0;
+  static constexpr uint32_t v = k + kTokenStages * 2 * box;
+  static constexpr uint32_t p = v + kTokenStages * 2 * box;  // [128 keys][64]
+  static constexpr uint32_t q = p + box;                     // two units'
+  static constexpr uint32_t bars = q + 2 * 2 * qbox;
+  static constexpr uint32_t red = bars + 256;                // [4 warps][16]
+  static constexpr uint32_t bytes = red + 256;
+  static_assert(bytes <= 227 * 1024, "one CTA an SM");
+};
+__device__ __forceinline__ void sync_softmax() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ bool any_softmax(bool mine) {
+  uint32_t all;
+  asm volatile(
+      "{\n\t.reg .pred a, b;\n\tsetp.ne.u32 a, %1, 0;\n\tbarrier.cta.red.or.pred b, 2, 128, a;\n\tselp.u32 %0, 1, 0, b;\n\t}"
+      : "=r"(all)
+      : "r"(uint32_t(mine))
+      : "memory");
+  return all != 0;
+}
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return (u >> 31) ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float order_value(uint32_t u) { return __uint_as_float((u >> 31) ? u & 0x7fffffffu : ~u); }
+
+// R: heads a thread works on, 8 or 16 (those past the group's are of zeros and are not stored).
+template <int R>
+__global__ void __launch_bounds__(kTokenThreads, 1)
+    paged_token_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ PagedArgs p,
+                       const __grid_constant__ PagedSeqs sq) {
+  using L = TokenSmem;
+  constexpr int HD = 128, NS = kTokenStages;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + L::bars);  // [NS] K block landed
+  uint64_t* k_empty = k_full + NS;                                 // [NS] its product has completed
+  uint64_t* v_full = k_empty + NS;
+  uint64_t* v_empty = v_full + NS;
+  uint64_t* q_full = v_empty + NS;   // [2] unit u's Q is in buffer u % 2
+  uint64_t* q_empty = q_full + 2;    // [2] its products have completed
+  uint64_t* s_full = q_empty + 2;    // [2] S of block j is in TMEM buffer j % 2
+  uint64_t* p_full = s_full + 2;     // P of the block written and O rescaled
+  uint64_t* o_done = p_full + 1;     // PV product of the block completed
+  uint64_t* drain = o_done + 1;      // every MMA completed
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  float* red = reinterpret_cast<float*>(smem + L::red);
+
+  if (smem_u32(smem) & 1023) {  // every CTA alike
+    pdl_wait();
+    if (threadIdx.x == 0) set_status(p.status, SPD_ECUDA);
+    return;
+  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int first = first_block(p, blockIdx.x), count = first_block(p, blockIdx.x + 1) - first;
+  Place at;
+  at.seek(p, sq, first, count);
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < NS; ++s) {
+      mbar_init(&k_full[s], 1);
+      mbar_init(&k_empty[s], 1);
+      mbar_init(&v_full[s], 1);
+      mbar_init(&v_empty[s], 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&q_full[s], 1);
+      mbar_init(&q_empty[s], 1);
+      mbar_init(&s_full[s], 1);
+    }
+    mbar_init(p_full, 4);  // one arrival per softmax warp
+    mbar_init(o_done, 1);
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+    prefetch_tmap(&map_kv);
+  }
+  for (uint32_t i = threadIdx.x; i < L::box / 16; i += kTokenThreads)  // the columns that nobody writes are zero
+    reinterpret_cast<uint4*>(smem + L::p)[i] = make_uint4(0u, 0u, 0u, 0u);
+  fence_proxy_async_smem();
+  if (warp == 4) {
+    tmem_alloc(tmem_slot, 128);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const uint32_t t_o = tmem + 64;  // S: two buffers of 16 columns
+
+  pdl_launch_dependents();
+  pdl_wait();
+  if (threadIdx.x == 0) stamp_start(p.stamp);
+
+  int issued_k = 0, issued_v = 0;
+  bool ok = true;
+  if (warp == 4) {
+    // ---- TMA producer ----
+    const uint64_t pol = policy_evict_first();
+    const int boxes = kTokenKeys / p.box;
+    int j = 0;  // block of the CTA
+    do {
+      const PagedSeq& s = sq.s[at.e];
+      auto row_at = [&](int blk) {  // of the lane's box; -1: none of its rows is there
+        const int key = blk * kTokenKeys + lane * p.box;
+        return lane < boxes && key < s.len ? pool_row(p, s.seq, key) : -1;
+      };
+      int row = row_at(at.lo);
+      for (int blk = at.lo; blk < at.hi && ok; ++blk, ++j) {
+        const int here = row;
+        if (blk + 1 < at.hi) row = row_at(blk + 1);  // a block ahead
+        const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, here >= 0)) * p.box * 256u;
+        const int st = j % NS;
+        auto load = [&](uint64_t* full, uint64_t* empty, uint32_t to, int x0) -> bool {
+          if (j >= NS && !__all_sync(0xffffffffu, mbar_wait(&empty[st], (j / NS - 1) & 1, abort_flag, p.budget))) return false;
+          if (lane == 0) mbar_arrive_expect_tx(&full[st], bytes);
+          __syncwarp();
+          if (here >= 0)
+            for (int c = 0; c < 2; ++c)
+              tma_load_2d(smem + to + (st * 2 + c) * L::box + lane * p.box * 128, &map_kv, &full[st], x0 + c * 64, here, pol);
+          return true;
+        };
+        if (!(ok = load(k_full, k_empty, L::k, at.hk * HD))) break;
+        issued_k = j + 1;
+        if (!(ok = load(v_full, v_empty, L::v, (p.n_kv_heads + at.hk) * HD))) break;
+        issued_v = j + 1;
+      }
+    } while (ok && at.next(p, sq));
+  } else if (warp == 5) {
+    if (lane == 0) {
+      // ---- MMA issuer ----
+      const uint32_t id_s = idesc_bf16_f32(128, kTokenHeads);
+      const uint32_t id_o = idesc_bf16_f32(128, 64) | (3u << 15);  // V and P are MN-major
+      auto issue_s = [&](int j, int unit) -> bool {
+        const int s = j % NS;
+        if (!mbar_wait(&k_full[s], (j / NS) & 1, abort_flag, p.budget)) return false;
+        // (the scores of block j - 2 have been read: its weights have arrived)
+        tc_fence_after();
+        const uint32_t sk = smem_u32(smem + L::k + s * 2 * L::box), qa = smem_u32(smem + L::q + (unit & 1) * 2 * L::qbox);
+#pragma unroll
+        for (int kk = 0; kk < HD / 16; ++kk)
+          mma_bf16(tmem + kTokenHeads * (j & 1), sdesc_k128(sk + (kk >> 2) * L::box + (kk & 3) * 32),
+                   sdesc_k128(qa + (kk >> 2) * L::qbox + (kk & 3) * 32), id_s, kk > 0 ? 1u : 0u);
+        mma_commit(&s_full[j & 1]);
+        mma_commit(&k_empty[s]);
+        return true;
+      };
+      int j = 0, left = count, unit = 0;
+      int n = at.hi - at.lo;  // blocks of the unit
+      ok = mbar_wait(&q_full[0], 0, abort_flag, p.budget) && issue_s(0, 0);
+      while (ok) {
+        Place then = at;
+        const bool more = then.next(p, sq);
+        for (int u = 0; u < n && ok; ++u, ++j) {
+          const int s = j % NS;
+          if (u + 1 < n) {
+            if (!(ok = issue_s(j + 1, unit))) break;
+          } else {
+            mma_commit(&q_empty[unit & 1]);
+            // the next unit's first block
+            if (more && !(ok = mbar_wait(&q_full[(unit + 1) & 1], ((unit + 1) >> 1) & 1, abort_flag, p.budget) && issue_s(j + 1, unit + 1)))
+              break;
+          }
+          if (!(ok = mbar_wait(&v_full[s], (j / NS) & 1, abort_flag, p.budget))) break;
+          if (!(ok = mbar_wait(p_full, j & 1, abort_flag, p.budget))) break;
+          tc_fence_after();
+          const uint32_t sv = smem_u32(smem + L::v + s * 2 * L::box), sp = smem_u32(smem + L::p);
+#pragma unroll
+          for (int x = 0; x < kTokenKeys / 16; ++x)
+            mma_bf16(t_o, sdesc_mn128(sv + x * 2048, L::box), sdesc_mn128(sp + x * 2048, L::box), id_o, (u > 0 || x > 0) ? 1u : 0u);
+          mma_commit(o_done);
+          mma_commit(&v_empty[s]);
+        }
+        left -= n;
+        if (!ok || !more) break;
+        at = then;
+        n = at.hi - at.lo;
+        ++unit;
+      }
+      if (!ok) {
+        *abort_flag = 1;
+        set_status(p.status, SPD_ETIMEOUT);
+      }
+      mma_commit(drain);  // arrives once every MMA issued above has completed
+      volatile int no_abort = 0;
+      if (!mbar_wait(drain, 0, &no_abort, p.budget)) set_status(p.status, SPD_ETIMEOUT);
+      ok = true;
+    }
+  } else if (warp == 6) {
+    // ---- Q: 16 rows of 128, those past the group's zero, in the 128-byte swizzle ----
+    int unit = 0;
+    do {
+      const uint4* src = reinterpret_cast<const uint4*>(p.q + (size_t(sq.s[at.e].q0) * p.n_heads + at.hk * p.group) * HD);
+      uint4 v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int row = 2 * i + (lane >> 4);
+        v[i] = row < p.group ? src[row * (HD / 8) + (lane & 15)] : make_uint4(0u, 0u, 0u, 0u);
+      }
+      const int b = unit & 1;
+      if (unit >= 2 && !(ok = __all_sync(0xffffffffu, mbar_wait(&q_empty[b], ((unit >> 1) - 1) & 1, abort_flag, p.budget)))) break;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int row = 2 * i + (lane >> 4), piece = lane & 15;
+        *reinterpret_cast<uint4*>(smem + L::q + (b * 2 + (piece >> 3)) * L::qbox + row * 128 + (((piece & 7) ^ (row & 7)) << 4)) = v[i];
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&q_full[b]);
+      ++unit;
+    } while (at.next(p, sq));
+  } else {
+    // A wait that gives up must not part the four warps, which meet at barriers: it ends the loop for all of them at the next.
+    const int t = threadIdx.x;  // key of the block; dim of the output
+    const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
+    int j = 0;  // block of the CTA
+    for (;;) {
+      const PagedSeq& s = sq.s[at.e];
+      float m[R], l[R];  // the heads' references (raw scores); the thread's sums of weights
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        m[r] = -INFINITY;
+        l[r] = 0.0f;
+      }
+      for (int blk = at.lo; blk < at.hi; ++blk, ++j) {
+        const bool there = blk * kTokenKeys + t < s.len;
+        if ((blk + 1) * kTokenKeys > s.len) {  // behind the last row: values that a weight of zero would turn into NaN
+          ok = ok && mbar_wait(&v_full[j % NS], (j / NS) & 1, abort_flag, p.budget);
+          if (!there) {
+            uint4* vr = reinterpret_cast<uint4*>(smem + L::v + (j % NS) * 2 * L::box + t * 128);
+#pragma unroll
+            for (int y = 0; y < 16; ++y) vr[(y >> 3) * (L::box / 16) + ((y + t) & 7)] = make_uint4(0u, 0u, 0u, 0u);
+          }
+          fence_proxy_async_smem();
+        }
+        ok = ok && mbar_wait(&s_full[j & 1], (j >> 1) & 1, abort_flag, p.budget);
+        __syncwarp();
+        tc_fence_after();
+        float v[R];
+        {
+          const uint32_t t_s = tmem + kTokenHeads * (j & 1) + lanes;
+          float a[8];
+          if constexpr (R == 8) {
+            tmem_ld8(t_s, a);
+          } else {
+            float b[8];
+            tmem_ld8x2(t_s, a, t_s + 8, b);
+#pragma unroll
+            for (int r = 0; r < 8; ++r) v[8 + r] = b[r];
+          }
+#pragma unroll
+          for (int r = 0; r < 8; ++r) v[r] = a[r];
+        }
+        bool over = false;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          if (!there) v[r] = -INFINITY;
+          over |= (v[r] - m[r]) * p.scale_log2 > kGrown;
+        }
+        // the product before has read P and O is whole; every warp has read its scores
+        if (j > 0) ok = ok && mbar_wait(o_done, (j - 1) & 1, abort_flag, p.budget);
+        if (any_softmax(over || !ok)) {
+          if (any_softmax(!ok)) {  // (all of them leave together)
+            ok = false;
+            break;
+          }
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const uint32_t top = __reduce_max_sync(0xffffffffu, order_of(fmaxf(v[r], -INFINITY)));
+            if (lane == 0) red[warp * kTokenHeads + r] = order_value(top);
+          }
+          sync_softmax();
+          float corr[R];
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const float n = fmaxf(m[r], fmaxf(fmaxf(red[r], red[kTokenHeads + r]), fmaxf(red[2 * kTokenHeads + r], red[3 * kTokenHeads + r])));
+            corr[r] = n == m[r] ? 1.0f : ex2((m[r] - n) * p.scale_log2);
+            m[r] = n;
+            l[r] *= corr[r];
+          }
+          if (blk > at.lo) {
+            tc_fence_after();
+#pragma unroll
+            for (int x = 0; x < 3 * (R / 8); ++x) {
+              const uint32_t col = t_o + lanes + (x / (R / 8)) * kTokenHeads + (x % (R / 8)) * 8;
+              float o[8];
+              tmem_ld8(col, o);
+#pragma unroll
+              for (int r = 0; r < 8; ++r) o[r] *= corr[(x % (R / 8)) * 8 + r];
+              tmem_st8(col, o);
+            }
+            tmem_st_wait();
+          }
+          sync_softmax();  // red is free
+        }
+        uint32_t term[3][R / 2];
+#pragma unroll
+        for (int r = 0; r < R; r += 2) {
+          const float f0 = m[r] == -INFINITY ? 0.0f : m[r] * p.scale_log2, f1 = m[r + 1] == -INFINITY ? 0.0f : m[r + 1] * p.scale_log2;
+          const float p0 = ex2(fmaf(v[r], p.scale_log2, -f0)), p1 = ex2(fmaf(v[r + 1], p.scale_log2, -f1));
+          l[r] += p0;
+          l[r + 1] += p1;
+          const uint32_t hi = pack_bf16(p0, p1);
+          const float a = p0 - __uint_as_float(hi << 16), b = p1 - __uint_as_float(hi & 0xffff0000u);
+          const uint32_t mid = pack_bf16(a, b);
+          term[0][r / 2] = hi;
+          term[1][r / 2] = mid;
+          term[2][r / 2] = pack_bf16(a - __uint_as_float(mid << 16), b - __uint_as_float(mid & 0xffff0000u));
+        }
+#pragma unroll
+        for (int x = 0; x < 3; ++x)
+#pragma unroll
+          for (int y = 0; y < R / 8; ++y)
+            *reinterpret_cast<uint4*>(smem + L::p + t * 128 + (((2 * x + y) ^ (t & 7)) << 4)) =
+                make_uint4(term[x][4 * y], term[x][4 * y + 1], term[x][4 * y + 2], term[x][4 * y + 3]);
+        fence_proxy_async_smem();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full);
+      }
+      if (!ok) break;
+      // the sums of all keys, then the outputs
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int off = 16; off; off >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], off);
+      if (lane == 0) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) red[warp * kTokenHeads + r] = l[r];
+      }
+      sync_softmax();
+#pragma unroll
+      for (int r = 0; r < R; ++r) l[r] = (red[r] + red[kTokenHeads + r]) + (red[2 * kTokenHeads + r] + red[3 * kTokenHeads + r]);
+      ok = mbar_wait(o_done, (j - 1) & 1, abort_flag, p.budget);
+      if (any_softmax(!ok)) {
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      const size_t row = size_t(s.q0) * p.n_heads + at.hk * p.group;
+      const bool whole = at.hi - at.lo == at.blocks;
+      const size_t slot = (2 * size_t(blockIdx.x) + (at.lo == 0)) * p.rows_part;
+#pragma unroll
+      for (int y = 0; y < R / 8; ++y) {
+        float o[8], mid[8], lo[8];
+        tmem_ld8(t_o + lanes + 8 * y, o);
+        tmem_ld8x2(t_o + lanes + kTokenHeads + 8 * y, mid, t_o + lanes + 2 * kTokenHeads + 8 * y, lo);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int r = 8 * y + i;
+          if (r >= p.group) continue;
+          if (isfinite(o[i])) o[i] += mid[i] + lo[i];  // (an infinite V meets lower terms that are 0 or negative)
+          if (whole) p.o[(row + r) * HD + t] = __float2bfloat16(l[r] == 0.0f ? 0.0f : o[i] * (1.0f / l[r]));
+          else p.part_o[(slot + r) * HD + t] = o[i];
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (t != r || r >= p.group) continue;
+        const float m2 = m[r] * p.scale_log2;
+        if (!whole) p.part_ml[slot + r] = make_float2(m2, l[r]);
+        else if (p.lse) p.lse[row + r] = fmaf(m2, 0.6931471805599453f, logf(l[r]));
+      }
+      sync_softmax();  // red is free
+      tc_fence_before();
+      if (!at.next(p, sq)) break;
+    }
+  }
+  if (!ok) {
+    *abort_flag = 1;
+    set_status(p.status, SPD_ETIMEOUT);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 128 && *abort_flag) {
+    // loads issued but never consumed land before the CTA exits
+    volatile int no_abort = 0;
+    for (int j = max(0, issued_k - NS); j < issued_k; ++j) mbar_wait(&k_full[j % NS], (j / NS) & 1, &no_abort, p.budget);
+    for (int j = max(0, issued_v - NS); j < issued_v; ++j) mbar_wait(&v_full[j % NS], (j / NS) & 1, &no_abort, p.budget);
+  }
+  __syncwarp();
+  tc_fence_after();
+  if (warp == 4) tmem_dealloc(tmem, 128);
+  if (threadIdx.x == 0) stamp_end(p.stamp);
+}
+
 // Units whose blocks several CTAs had: states (m_i, l_i, O_i) joined in key order, m = max m_i, l = sum l_i 2^(m_i - m),
 // O = sum O_i 2^(m_i - m). A part in which a row sees nothing has l_i = 0. (Its maximum does not tell: fmaxf passes over those of
 // parts whose scores are all NaN, whose sums are NaN and stay so.) blockIdx.x stands for the border between two CTAs; the first
-// border inside a unit has it. W warps a row, each a range of the parts, four of them in flight.
-constexpr int kMergeWarps = 8, kMergeAhead = 4;
-template <int HD>
+// border inside a unit has it. R = 1: W warps a row, each a range of the parts, four of them in flight; R = 4: a warp has four rows at a
+// time, one part of each in flight.
+constexpr int kMergeWarps = 8, kMergeAhead = 4, kMergeRows = 32;
+template <int HD, int R>
 __global__ void __launch_bounds__(kMergeWarps * 32)
     paged_merge_kernel(const __grid_constant__ PagedArgs p, const __grid_constant__ PagedSeqs sq, int W) {
-  constexpr int D = HD / 32;  // dims a lane
+  constexpr int D = HD / 32;            // dims a lane
+  constexpr int A = R == 1 ? kMergeAhead : 1;
   __shared__ float2 wml[kMergeWarps];
   __shared__ float wo[kMergeWarps][HD];
   pdl_launch_dependents();
@@ -628,87 +1029,102 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
   u.seek(p, sq, border, 1);
   const int start = border - u.lo, end = start + u.blocks;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp & (W - 1);
-  const int r = (int(blockIdx.y) * kMergeWarps + warp) / W;
+  const int r0 = (int(blockIdx.y) * kMergeWarps + warp) / W * R;
   const PagedSeq& s = sq.s[u.e];
   const int t = u.tile / p.chunks, h0 = (u.tile - t * p.chunks) * p.chunk, n0 = t * p.tokens;
-  const int hc = r % p.chunk, token = n0 + r / p.chunk;
   const bool mine = u.lo > 0 && first_block(p, c - 1) <= start;  // (all threads alike)
-  const bool have = mine && r < min(p.tokens, s.n - n0) * p.chunk && hc < min(p.chunk, p.group - h0);
+  const int rows = mine ? min(p.tokens, s.n - n0) * p.chunk : 0, heads = min(p.chunk, p.group - h0);
   const int parts = int(((long long)end * p.ctas + p.total - 1) / p.total) - (c - 1);
   pdl_wait();
   if (!mine) return;
-  float m = -INFINITY, l = 0.0f, o[D];
+  float m[R], l[R], o[R][D];
 #pragma unroll
-  for (int x = 0; x < D; ++x) o[x] = 0.0f;
-  if (have) {
+  for (int i = 0; i < R; ++i) {
+    m[i] = -INFINITY;
+    l[i] = 0.0f;
+#pragma unroll
+    for (int x = 0; x < D; ++x) o[i][x] = 0.0f;
+  }
+  if (r0 < rows) {
     const int s1 = int((w + 1) * parts / W);
-    for (int s0 = int(w * parts / W); s0 < s1; s0 += kMergeAhead) {
-      float2 ml[kMergeAhead];
-      float v[kMergeAhead][D];
+    for (int s0 = int(w * parts / W); s0 < s1; s0 += A) {
+      float2 ml[R][A];
+      float v[R][A][D];
 #pragma unroll
-      for (int k = 0; k < kMergeAhead; ++k) {
-        ml[k] = make_float2(-INFINITY, 0.0f);
-        if (s0 + k >= s1) continue;
-        const size_t slot = (2 * size_t(c - 1 + s0 + k) + (s0 + k == 0)) * p.rows_part + r;
-        ml[k] = p.part_ml[slot];
-        const float* po = p.part_o + slot * HD + D * lane;
-        if constexpr (D == 4) {
-          const float4 f = *reinterpret_cast<const float4*>(po);
-          v[k][0] = f.x, v[k][1] = f.y, v[k][2] = f.z, v[k][3] = f.w;
-        } else {
-          const float2 f = *reinterpret_cast<const float2*>(po);
-          v[k][0] = f.x, v[k][1] = f.y;
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int k = 0; k < A; ++k) {
+          ml[i][k] = make_float2(-INFINITY, 0.0f);
+          if (s0 + k >= s1 || r0 + i >= rows) continue;
+          const size_t slot = (2 * size_t(c - 1 + s0 + k) + (s0 + k == 0)) * p.rows_part + r0 + i;
+          ml[i][k] = p.part_ml[slot];
+          const float* po = p.part_o + slot * HD + D * lane;
+          if constexpr (D == 4) {
+            const float4 f = *reinterpret_cast<const float4*>(po);
+            v[i][k][0] = f.x, v[i][k][1] = f.y, v[i][k][2] = f.z, v[i][k][3] = f.w;
+          } else {
+            const float2 f = *reinterpret_cast<const float2*>(po);
+            v[i][k][0] = f.x, v[i][k][1] = f.y;
+          }
+        }
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        float top = m[i];
+        bool some = false;
+#pragma unroll
+        for (int k = 0; k < A; ++k) {
+          top = fmaxf(top, ml[i][k].x);
+          some |= ml[i][k].y != 0.0f;
+        }
+        if (!some) continue;
+        const float keep = exp2f(m[i] - top);
+        m[i] = top;
+        l[i] *= keep;
+#pragma unroll
+        for (int x = 0; x < D; ++x) o[i][x] *= keep;
+#pragma unroll
+        for (int k = 0; k < A; ++k) {
+          if (ml[i][k].y == 0.0f) continue;  // a part in which the row sees nothing
+          const float f = exp2f(ml[i][k].x - top);
+          l[i] = fmaf(ml[i][k].y, f, l[i]);
+#pragma unroll
+          for (int x = 0; x < D; ++x) o[i][x] = fmaf(v[i][k][x], f, o[i][x]);
         }
       }
-      float top = m;
-      bool some = false;
+    }
+  }
+  if constexpr (R == 1) {
+    if (W > 1) {
+      if (lane == 0) wml[warp] = make_float2(m[0], l[0]);
 #pragma unroll
-      for (int k = 0; k < kMergeAhead; ++k) {
-        top = fmaxf(top, ml[k].x);
-        some |= ml[k].y != 0.0f;
-      }
-      if (!some) continue;
-      const float keep = exp2f(m - top);
-      m = top;
-      l *= keep;
+      for (int x = 0; x < D; ++x) wo[warp][D * lane + x] = o[0][x];
+      __syncthreads();
+      if (w > 0) return;
+      for (int k = 1; k < W; ++k) m[0] = fmaxf(m[0], wml[warp + k].x);
+      l[0] = 0.0f;
 #pragma unroll
-      for (int x = 0; x < D; ++x) o[x] *= keep;
+      for (int x = 0; x < D; ++x) o[0][x] = 0.0f;
+      for (int k = 0; k < W; ++k) {
+        const float2 ml = wml[warp + k];
+        if (ml.y == 0.0f) continue;
+        const float f = exp2f(ml.x - m[0]);
+        l[0] = fmaf(ml.y, f, l[0]);
 #pragma unroll
-      for (int k = 0; k < kMergeAhead; ++k) {
-        if (ml[k].y == 0.0f) continue;  // a part in which the row sees nothing
-        const float f = exp2f(ml[k].x - m);
-        l = fmaf(ml[k].y, f, l);
-#pragma unroll
-        for (int x = 0; x < D; ++x) o[x] = fmaf(v[k][x], f, o[x]);
+        for (int x = 0; x < D; ++x) o[0][x] = fmaf(wo[warp + k][D * lane + x], f, o[0][x]);
       }
     }
   }
-  if (W > 1) {
-    if (lane == 0) wml[warp] = make_float2(m, l);
 #pragma unroll
-    for (int x = 0; x < D; ++x) wo[warp][D * lane + x] = o[x];
-    __syncthreads();
-    if (w > 0) return;
-    for (int k = 1; k < W; ++k) m = fmaxf(m, wml[warp + k].x);
-    l = 0.0f;
+  for (int i = 0; i < R; ++i) {
+    const int r = r0 + i, hc = r % p.chunk;
+    if (r >= rows || hc >= heads) continue;
+    const float inv = l[i] == 0.0f ? 0.0f : 1.0f / l[i];
+    const size_t at = (size_t(s.q0) + n0 + r / p.chunk) * p.n_heads + u.hk * p.group + h0 + hc;
+    uint32_t* to = reinterpret_cast<uint32_t*>(p.o + at * HD + D * lane);
 #pragma unroll
-    for (int x = 0; x < D; ++x) o[x] = 0.0f;
-    for (int k = 0; k < W; ++k) {
-      const float2 ml = wml[warp + k];
-      if (ml.y == 0.0f) continue;
-      const float f = exp2f(ml.x - m);
-      l = fmaf(ml.y, f, l);
-#pragma unroll
-      for (int x = 0; x < D; ++x) o[x] = fmaf(wo[warp + k][D * lane + x], f, o[x]);
-    }
+    for (int x = 0; x < D / 2; ++x) to[x] = pack_bf16(o[i][2 * x] * inv, o[i][2 * x + 1] * inv);
+    if (p.lse && lane == 0) p.lse[at] = fmaf(m[i], 0.6931471805599453f, logf(l[i]));
   }
-  if (!have) return;
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  const size_t at = (size_t(s.q0) + token) * p.n_heads + u.hk * p.group + h0 + hc;
-  uint32_t* to = reinterpret_cast<uint32_t*>(p.o + at * HD + D * lane);
-#pragma unroll
-  for (int x = 0; x < D / 2; ++x) to[x] = pack_bf16(o[2 * x] * inv, o[2 * x + 1] * inv);
-  if (p.lse && lane == 0) p.lse[at] = fmaf(m, 0.6931471805599453f, logf(l));
 }
 
 // Rows of a state: a tile's, or as many as the call has.
@@ -732,10 +1148,6 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
                         int n_kv_heads, int head_dim, void* o, float* lse, void* ws, size_t ws_bytes, int* status, cudaStream_t st) {
   const int kvd = n_kv_heads * head_dim;
   PagedArgs p{};
-  p.box = 64;
-  while (page_size % p.box) p.box /= 2;  // (pages are multiples of 16 rows)
-  CUtensorMap map;
-  if (int rc = make_operand_map(&map, pool, 2 * kvd, n_pages * page_size, p.box)) return rc;
   p.q = static_cast<const __nv_bfloat16*>(q);
   p.pool = static_cast<const __nv_bfloat16*>(pool);
   p.table = table;
@@ -745,9 +1157,6 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
   p.n_heads = n_heads;
   p.n_kv_heads = n_kv_heads;
   p.group = n_heads / n_kv_heads;
-  p.chunk = std::min(p.group, 128);
-  p.chunks = (p.group + 127) / 128;
-  p.tokens = 128 / p.chunk;
   p.scale_log2 = float(1.4426950408889634 / sqrt(double(head_dim)));
   p.o = static_cast<__nv_bfloat16*>(o);
   p.lse = lse;
@@ -758,56 +1167,85 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
   p.part_ml = cv.take<float2>(rows);
   p.status = status;
   p.budget = kWaitBudget;
-  const auto kernel = head_dim == 128 ? paged_attn_kernel<128> : paged_attn_kernel<64>;
-  const size_t smem = head_dim == 128 ? PagedSmem<128>::bytes : PagedSmem<64>::bytes;
-  static DeviceOnce attr[2];
-  SPD_CUDA_TRY(once_per_device(attr[head_dim == 128], [&] {
-    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
-  }));
-  const int places = std::min(kCtas, 2 * num_sms());
-  for (int s0 = 0; s0 < n_seqs; s0 += kMaxSeqs) {
-    PagedSeqs sq{};
-    long long total = 0;
-    int most = 0, longest = 0;
-    double pairs = 0.0, keys = 0.0, tokens = 0.0;
-    for (int b = s0; b < std::min(n_seqs, s0 + kMaxSeqs); ++b) {
-      const int n = q_cu[b + 1] - q_cu[b];
-      if (n == 0) continue;
-      PagedSeq& s = sq.s[sq.n++];
-      s = {int(total), q_cu[b], n, len[b], prefix ? prefix[b] : 0, b, 0, (n + p.tokens - 1) / p.tokens * p.chunks};
-      long long blocks = 0;
-      for (int i = 0; i < n; i += p.tokens) {
-        const int here = blocks_at(s, i, p.tokens);
-        longest = std::max(longest, here);
-        blocks += (long long)here * p.chunks;
+  const bool tokens_apart = head_dim == 128 && p.group <= kTokenHeads;
+  const int sms = std::min(kCtas / 2, num_sms());
+  // sequences of one new token on their own where the token kernel takes them; up to kMaxSeqs a launch
+  for (int form = 0; form < 2; ++form) {
+    const bool token = form == 0;
+    if (token && !tokens_apart) continue;
+    p.keys = token ? kTokenKeys : kTK;
+    p.chunk = token ? p.group : std::min(p.group, 128);
+    p.chunks = token ? 1 : (p.group + 127) / 128;
+    p.tokens = token ? 1 : 128 / p.chunk;
+    p.box = p.keys;
+    while (page_size % p.box) p.box /= 2;  // (pages are multiples of 16 rows)
+    CUtensorMap map;
+    bool mapped = false;
+    for (int next = 0; next < n_seqs;) {
+      PagedSeqs sq;
+      sq.n = 0;
+      long long total = 0;
+      int most = 0, longest = 0;
+      double pairs = 0.0, keys = 0.0, tokens = 0.0;
+      for (; next < n_seqs && sq.n < kMaxSeqs; ++next) {
+        const int b = next, n = q_cu[b + 1] - q_cu[b];
+        if (n == 0 || (tokens_apart && (n == 1) != token)) continue;
+        PagedSeq& s = sq.s[sq.n++];
+        s = {int(total), q_cu[b], n, len[b], prefix ? prefix[b] : 0, b, 0, (n + p.tokens - 1) / p.tokens * p.chunks};
+        long long blocks = 0;
+        for (int i = 0; i < n; i += p.tokens) {
+          const int here = blocks_at(s, i, p.tokens, p.keys);
+          longest = std::max(longest, here);
+          blocks += (long long)here * p.chunks;
+        }
+        total += blocks * n_kv_heads;
+        if (total > 0x3fffffff) return fail(SPD_EUNSUPPORTED, "paged attention of more than 2^30 blocks of keys");
+        s.head_blocks = int(blocks);
+        most = std::max(most, n);
+        keys += len[b];
+        tokens += n;
+        pairs += double(n) * len[b] - 0.5 * double(n) * (n - 1);
       }
-      total += blocks * n_kv_heads;
-      if (total > 0x7fffffff / 2) return fail(SPD_EUNSUPPORTED, "paged attention of more than 2^30 blocks of keys");
-      s.head_blocks = int(blocks);
-      most = std::max(most, n);
-      keys += len[b];
-      tokens += n;
-      pairs += double(n) * len[b] - 0.5 * double(n) * (n - 1);
+      if (sq.n == 0) continue;
+      if (!mapped) {
+        if (int rc = make_operand_map(&map, pool, 2 * kvd, n_pages * page_size, p.box)) return rc;
+        mapped = true;
+      }
+      p.total = int(total);
+      p.ctas = int(std::min<long long>(token ? sms : 2 * sms, total));
+      p.warps = (std::min(most, p.tokens) * p.chunk + 31) / 32;
+      const double fl = 4.0 * head_dim * n_heads * pairs;
+      const double by = 4.0 * kvd * keys + 4.0 * n_heads * head_dim * tokens;
+      p.stamp = stamp_slot(TR_ATTN, fl, by);
+      const int slot = trace_begin(st);
+      const int which = token ? (p.group <= 8 ? 0 : 1) : head_dim == 64 ? 2 : 3;
+      const auto kernel = which == 0   ? paged_token_kernel<8>
+                          : which == 1 ? paged_token_kernel<16>
+                          : which == 2 ? paged_attn_kernel<64>
+                                       : paged_attn_kernel<128>;
+      const uint32_t smem = token ? TokenSmem::bytes : head_dim == 64 ? PagedSmem<64>::bytes : PagedSmem<128>::bytes;
+      static DeviceOnce attr[4];
+      SPD_CUDA_TRY(once_per_device(attr[which], [&] {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+      }));
+      SPD_CUDA_TRY(launch_pdl(kernel, dim3(p.ctas), dim3(token ? kTokenThreads : kThreads), smem, st, map, p, sq));
+      if (p.ctas > 1) {
+        const int parts = int((long long)longest * p.ctas / total) + 2;  // of a unit, at most
+        const int rows_unit = std::min(most, p.tokens) * p.chunk;
+        if (rows_unit > kMergeRows) {  // many rows of few parts
+          SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? paged_merge_kernel<128, 4> : paged_merge_kernel<64, 4>,
+                                  dim3(p.ctas - 1, (rows_unit + 4 * kMergeWarps - 1) / (4 * kMergeWarps)), dim3(kMergeWarps * 32), 0, st,
+                                  p, sq, 1));
+        } else {
+          int W = 1;
+          while (W < kMergeWarps && parts > kMergeAhead * W) W *= 2;
+          SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? paged_merge_kernel<128, 1> : paged_merge_kernel<64, 1>,
+                                  dim3(p.ctas - 1, (rows_unit * W + kMergeWarps - 1) / kMergeWarps), dim3(kMergeWarps * 32), 0, st, p,
+                                  sq, W));
+        }
+      }
+      trace_end(slot, st, TR_ATTN, fl, by);
     }
-    if (sq.n == 0) continue;
-    p.total = int(total);
-    p.ctas = int(std::min<long long>(places, total));
-    p.warps = (std::min(most, p.tokens) * p.chunk + 31) / 32;
-    const double fl = 4.0 * head_dim * n_heads * pairs;
-    const double by = 4.0 * kvd * keys + 4.0 * n_heads * head_dim * tokens;
-    p.stamp = stamp_slot(TR_ATTN, fl, by);
-    const int slot = trace_begin(st);
-    SPD_CUDA_TRY(launch_pdl(kernel, dim3(p.ctas), dim3(kThreads), smem, st, map, p, sq));
-    if (p.ctas > 1) {
-      const int parts = int((long long)longest * p.ctas / total) + 2;  // of a unit, at most
-      int W = 1;
-      while (W < kMergeWarps && parts > kMergeAhead * W) W *= 2;
-      const int rows_unit = std::min(most, p.tokens) * p.chunk;
-      SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? paged_merge_kernel<128> : paged_merge_kernel<64>,
-                              dim3(p.ctas - 1, (rows_unit * W + kMergeWarps - 1) / kMergeWarps), dim3(kMergeWarps * 32), 0, st, p, sq,
-                              W));
-    }
-    trace_end(slot, st, TR_ATTN, fl, by);
   }
   return SPD_OK;
 }
