@@ -91,6 +91,28 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);
 }
+// Two fp32 operations in one instruction.
+struct Two {
+  float lo, hi;
+};
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+  Two d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.lo), "=f"(d.hi)
+      : "f"(a.lo), "f"(a.hi), "f"(b.lo), "f"(b.hi), "f"(c.lo), "f"(c.hi));
+  return d;
+}
+__device__ __forceinline__ Two add2(Two a, Two b) {
+  Two d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.lo), "=f"(d.hi)
+      : "f"(a.lo), "f"(a.hi), "f"(b.lo), "f"(b.hi));
+  return d;
+}
+// The values of two bf16.
+__device__ __forceinline__ Two two_of(uint32_t w) { return Two{__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)}; }
 __device__ __forceinline__ bool not_finite(uint32_t two) {  // either of two bf16
   return (two & 0x7f80u) == 0x7f80u || (two & 0x7f800000u) == 0x7f800000u;
 }
@@ -397,9 +419,10 @@ __global__ void __launch_bounds__(kThreads, 2)
             bool here = false;
 #pragma unroll
             for (int y = 0; y < 8; ++y) {
-              uint4 w = vr[y];
+              const int at_piece = (y + x) & 7;  // (rows begin at the same bank)
+              uint4 w = vr[at_piece];
               const bool some = not_finite(w.x) || not_finite(w.y) || not_finite(w.z) || not_finite(w.w);
-              if (some) vr[y] = make_uint4(finite_of(w.x), finite_of(w.y), finite_of(w.z), finite_of(w.w));
+              if (some) vr[at_piece] = make_uint4(finite_of(w.x), finite_of(w.y), finite_of(w.z), finite_of(w.w));
               here |= some;
             }
             odd |= here && kb + x % kTK < lim_any;
@@ -442,7 +465,8 @@ __global__ void __launch_bounds__(kThreads, 2)
           }
         }
         const float off = m_run == -INFINITY ? 0.0f : m_run * p.scale_log2;  // nothing seen yet: all weights are 0
-        float r4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        const Two scale{p.scale_log2, p.scale_log2}, less{-off, -off}, minus{-1.0f, -1.0f};
+        Two sum[2] = {Two{0.0f, 0.0f}, Two{0.0f, 0.0f}};
         uint32_t third[kTK / 2];  // keys 2 i and 2 i + 1 in word i
 #pragma unroll
         for (int x = 0; x < kTK / 16; ++x) {
@@ -450,20 +474,21 @@ __global__ void __launch_bounds__(kThreads, 2)
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int k = 16 * x + 2 * i;
-            const float p0 = ex2(fmaf(v[k], p.scale_log2, -off)), p1 = ex2(fmaf(v[k + 1], p.scale_log2, -off));
-            r4[k & 2] += p0;
-            r4[(k & 2) + 1] += p1;
-            const uint32_t hi = pack_bf16(p0, p1);
-            const float a = p0 - __uint_as_float(hi << 16), b = p1 - __uint_as_float(hi & 0xffff0000u);
-            const uint32_t mid = pack_bf16(a, b);
+            Two w = fma2(Two{v[k], v[k + 1]}, scale, less);
+            w = Two{ex2(w.lo), ex2(w.hi)};
+            sum[i & 1] = add2(sum[i & 1], w);
+            const uint32_t hi = pack_bf16(w.lo, w.hi);
+            w = fma2(two_of(hi), minus, w);  // what is left
+            const uint32_t mid = pack_bf16(w.lo, w.hi);
             first_t[i] = __uint_as_float(hi);
             second_t[i] = __uint_as_float(mid);
-            third[k >> 1] = pack_bf16(a - __uint_as_float(mid << 16), b - __uint_as_float(mid & 0xffff0000u));
+            w = fma2(two_of(mid), minus, w);
+            third[k >> 1] = pack_bf16(w.lo, w.hi);
           }
           tmem_st8(t_s + 16 * x, first_t);  // over the scores
           tmem_st8(t_s + 16 * x + 8, second_t);
         }
-        l_run += (r4[0] + r4[1]) + (r4[2] + r4[3]);
+        l_run += (sum[0].lo + sum[0].hi) + (sum[1].lo + sum[1].hi);
         // the third terms' place is free when the block before has been multiplied
         if (j > 0 && !(ok = __all_sync(0xffffffffu, mbar_wait(&o_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort_flag, p.budget)))) break;
 #pragma unroll
