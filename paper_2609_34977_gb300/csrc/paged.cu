@@ -8,9 +8,10 @@
 // sees, in blocks of 64. All blocks of a launch form one list, unit after unit, and every CTA takes an equal stretch of it,
 // whole units and parts of two: no CTA waits for a longest sequence, and 1.5 tiles a CTA cost 1.5 tiles. Parts of a unit leave
 // states (m, l, O) in fp32, which paged_merge_kernel joins in the order of the keys (the same bits in every run).
-//   warp 4     TMA producer: K and V blocks into rings, a lane a box of rows that lie in one page
-//   warp 5     MMA issuer: S = Q K^T into TMEM, then O += P V with P read from TMEM, V in place as an MN-major operand
-//   warps 0-3  a thread a row: the block's 64 scores in registers, online softmax in fp32; a weight is held as the sum of
+//   warp 8     TMA producer: K and V blocks into rings, a lane a box of rows that lie in one page
+//   warp 9     MMA issuer: S = Q K^T into TMEM, then O += P V with P read from TMEM, V in place as an MN-major operand, each
+//              as its operands come
+//   warps 0-7  two threads a row, half of the block's 64 scores each: online softmax in fp32; a weight is held as the sum of
 //              three bf16 terms, all 24 bits of it: two over the scores in TMEM, where O leaves no room for more, the third in
 //              shared memory
 // Only blocks that reach past the first token's limit are masked; there the softmax warps also clear the values of V that are
@@ -33,7 +34,7 @@ constexpr int kMaxSeqs = 112;          // sequences whose sizes fit in a launch'
 constexpr int kTK = 64;                // keys a block
 constexpr uint32_t kQBox = 128 * 128;  // 64 columns of the Q tile
 constexpr uint32_t kKBox = kTK * 128;  // 64 columns of a block of K or V
-constexpr int kThreads = 192;
+constexpr int kThreads = 320;
 constexpr uint32_t kTmemCols = 256;    // S: two buffers [0, 64) and [64, 128); O: [128, 128 + HD)
 constexpr int kCtas = 304;             // CTAs that fill the GPU: two on each of 152 SMs
 // The reference that a row's exponentials are taken against is renewed once its maximum has grown by this much (log2
@@ -60,7 +61,7 @@ struct PagedArgs {
   float scale_log2;
   __nv_bfloat16* o;
   float* lse;
-  int total, ctas, warps;            // blocks; CTAs; softmax warps with rows
+  int total, ctas, warps;            // blocks; CTAs; quarters of the tile (32 rows) that have rows
   float* part_o;                     // [2 ctas][rows_part][HD] states of parts: slot 2 c of the part that goes on with a unit
   float2* part_ml;                   // (CTA c), 2 c + 1 of the one that begins one; maximum (log2 units) and sum
   int rows_part;
@@ -69,17 +70,24 @@ struct PagedArgs {
   unsigned long long* stamp;
 };
 
+// The third terms of a block's weights, [128][64], take the place of its K, which has been read when they are written (heads of
+// 128: the same 16 KB), or one of two places of their own: they need not wait for the products of the block before.
 template <int HD>
 struct PagedSmem {
   static constexpr int kChunks = HD / 64;
-  static constexpr int kStages = 256 / HD;  // 64 KB of K and V in flight a CTA
+  static constexpr uint32_t third = 128 * 128;
+  static constexpr int kStages = HD == 128 ? 3 : 4;   // of K
+  static constexpr int kStagesV = HD == 128 ? 2 : 4;
   static constexpr uint32_t q = 0;
   static constexpr uint32_t k = q + kChunks * kQBox;
   static constexpr uint32_t v = k + kStages * kChunks * kKBox;
-  static constexpr uint32_t p3 = v + kStages * kChunks * kKBox;  // [128][64] third terms of a block's weights
-  static constexpr uint32_t bars = p3 + 128 * 128;
-  static constexpr uint32_t bytes = bars + 256;  // (two CTAs an SM: at most 113 KB)
+  static constexpr uint32_t p3 = v + kStagesV * kChunks * kKBox;
+  static constexpr uint32_t bars = p3 + (HD == 128 ? 0 : 2 * third);
+  static constexpr uint32_t red = bars + 256;    // [128] what the two threads of a row tell each other
+  static constexpr uint32_t bytes = red + 512;   // (two CTAs an SM: at most 113 KB)
   static_assert(bytes <= 113 * 1024, "two CTAs an SM");
+  static_assert(HD != 128 || kChunks * kKBox == third, "third terms in a block's K");
+  __device__ static uint32_t third_at(int j) { return HD == 128 ? k + (j % kStages) * third : p3 + (j & 1) * third; }
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -191,6 +199,18 @@ struct Place {
   }
 };
 
+// Barriers of the two warps that have the same rows.
+__device__ __forceinline__ void pair_sync(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ bool pair_or(int id, bool mine) {
+  uint32_t all;
+  asm volatile(
+      "{\n\t.reg .pred a, b;\n\tsetp.ne.u32 a, %1, 0;\n\tbarrier.cta.red.or.pred b, %2, 64, a;\n\tselp.u32 %0, 1, 0, b;\n\t}"
+      : "=r"(all)
+      : "r"(uint32_t(mine)), "r"(id)
+      : "memory");
+  return all != 0;
+}
+
 // Row of the pool that holds row `key` of a sequence; behind the pool (loads there read zeros) where its page is none.
 __device__ __forceinline__ int pool_row(const PagedArgs& p, int seq, int key) {
   const int k = int(uint32_t(key) / uint32_t(p.page_size)), page = p.table[size_t(seq) * p.max_pages + k];
@@ -206,13 +226,13 @@ __global__ void __launch_bounds__(kThreads, 2)
     paged_attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ PagedArgs p,
                       const __grid_constant__ PagedSeqs sq) {
   using L = PagedSmem<HD>;
-  constexpr int NS = L::kStages;
+  constexpr int NS = L::kStages, NV = L::kStagesV;
   extern __shared__ __align__(1024) uint8_t smem[];  // (the swizzle's atoms; no room to round the address up)
   uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + L::bars);  // [NS] K block landed
-  uint64_t* k_empty = k_full + NS;                                 // [NS] its S product has completed
-  uint64_t* v_full = k_empty + NS;                                 // [NS] V block landed
-  uint64_t* v_empty = v_full + NS;                                 // [NS] its PV products have completed
-  uint64_t* q_full = v_empty + NS;   // a unit's Q tile is in shared memory
+  uint64_t* k_empty = k_full + NS;                                 // [NS] its S product (third terms in it: its PV products) completed
+  uint64_t* v_full = k_empty + NS;                                 // [NV] V block landed
+  uint64_t* v_empty = v_full + NV;                                 // [NV] its PV products have completed
+  uint64_t* q_full = v_empty + NV;   // a unit's Q tile is in shared memory
   uint64_t* s_full = q_full + 1;     // [2] S of block j is in TMEM buffer j % 2
   uint64_t* p_full = s_full + 2;     // [2] P of block j written and O rescaled
   uint64_t* o_done = p_full + 2;     // [2] PV products of block j completed
@@ -235,13 +255,15 @@ __global__ void __launch_bounds__(kThreads, 2)
     for (int s = 0; s < NS; ++s) {
       mbar_init(&k_full[s], 1);
       mbar_init(&k_empty[s], 1);
+    }
+    for (int s = 0; s < NV; ++s) {
       mbar_init(&v_full[s], 1);
       mbar_init(&v_empty[s], 1);
     }
-    mbar_init(q_full, nw);
+    mbar_init(q_full, 2 * nw);
     for (int s = 0; s < 2; ++s) {
       mbar_init(&s_full[s], 1);
-      mbar_init(&p_full[s], nw);  // one arrival per softmax warp
+      mbar_init(&p_full[s], 2 * nw);  // one arrival per softmax warp
       mbar_init(&o_done[s], 1);
     }
     mbar_init(drain, 1);
@@ -250,7 +272,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     fence_mbar_init();
     prefetch_tmap(&map_kv);
   }
-  if (warp == 4) {
+  if (warp == 8) {
     tmem_alloc(tmem_slot, kTmemCols);
     tmem_relinquish();
   }
@@ -265,7 +287,7 @@ __global__ void __launch_bounds__(kThreads, 2)
   if (threadIdx.x == 0) stamp_start(p.stamp);
 
   int issued_k = 0, issued_v = 0;
-  if (warp == 4) {
+  if (warp == 8) {
     // ---- TMA producer ----
     const uint64_t pol = policy_evict_last();
     const int boxes = kTK / p.box;
@@ -283,9 +305,9 @@ __global__ void __launch_bounds__(kThreads, 2)
         const int here = row;
         if (blk + 1 < at.hi) row = row_at(blk + 1);  // a block ahead
         const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, here >= 0)) * p.box * 128u * L::kChunks;
-        const int st = j % NS;
-        auto load = [&](uint64_t* full, uint64_t* empty, uint32_t to, int x0) -> bool {
-          if (j >= NS && !__all_sync(0xffffffffu, mbar_wait(&empty[st], (j / NS - 1) & 1, abort_flag, p.budget))) return false;
+        auto load = [&](uint64_t* full, uint64_t* empty, int stages, uint32_t to, int x0) -> bool {
+          const int st = j % stages;
+          if (j >= stages && !__all_sync(0xffffffffu, mbar_wait(&empty[st], (j / stages - 1) & 1, abort_flag, p.budget))) return false;
           if (lane == 0) mbar_arrive_expect_tx(&full[st], bytes);
           __syncwarp();
           if (here >= 0)
@@ -293,9 +315,9 @@ __global__ void __launch_bounds__(kThreads, 2)
               tma_load_2d(smem + to + (st * L::kChunks + c) * kKBox + lane * p.box * 128, &map_kv, &full[st], x0 + c * 64, here, pol);
           return true;
         };
-        if (!(ok = load(k_full, k_empty, L::k, at.hk * HD))) break;
+        if (!(ok = load(k_full, k_empty, NS, L::k, at.hk * HD))) break;
         issued_k = j + 1;
-        if (!(ok = load(v_full, v_empty, L::v, (p.n_kv_heads + at.hk) * HD))) break;
+        if (!(ok = load(v_full, v_empty, NV, L::v, (p.n_kv_heads + at.hk) * HD))) break;
         issued_v = j + 1;
       }
     } while (ok && at.next(p, sq));
@@ -303,55 +325,69 @@ __global__ void __launch_bounds__(kThreads, 2)
       *abort_flag = 1;
       set_status(p.status, SPD_ETIMEOUT);
     }
-  } else if (warp == 5) {
+  } else if (warp == 9) {
     if (lane == 0) {
       // ---- MMA issuer ----
       const uint32_t id_s = idesc_bf16_f32(128, kTK);
       const uint32_t id_o = idesc_bf16_f32(128, HD) | (1u << 16);  // V is MN-major
-      const uint32_t sa = smem_u32(smem + L::q), sp = smem_u32(smem + L::p3);
-      bool ok = true;
-      auto issue_s = [&](int j) -> bool {
-        const int s = j % NS;
-        if (!mbar_wait(&k_full[s], (j / NS) & 1, abort_flag, p.budget)) return false;
-        // S buffer j % 2 holds P of block j - 2 until its PV products have completed
-        if (j > 1 && !mbar_wait(&o_done[j & 1], ((j >> 1) - 1) & 1, abort_flag, p.budget)) return false;
-        tc_fence_after();
-        const uint32_t sk = smem_u32(smem + L::k + s * L::kChunks * kKBox);
+      const uint32_t sa = smem_u32(smem + L::q);
+      auto ready = [&](uint64_t* bar, int phase) { return mbar_test(bar, phase & 1); };
+      // Blocks in order, S and PV as their operands come: S of block js where K and Q are there and the S buffer is free (the PV
+      // products of block js - 2 completed), PV of block jp where V and P are there.
+      int js = 0, jp = 0, unit = 0, unit_end = at.hi - at.lo;  // js's unit, and the first block behind it
+      int pv_begin = 0, pv_end = unit_end;                     // jp's unit
+      Place pv = at;
+      bool q_there = false, ok = true;
+      long long since = clock64();
+      while (jp < count && ok) {
+        bool did = false;
+        if (js < count) {
+          if (js == unit_end) {
+            at.next(p, sq);
+            unit_end += at.hi - at.lo;
+            ++unit;
+            q_there = false;
+          }
+          if (!q_there) q_there = ready(q_full, unit);
+          const int s = js % NS;
+          if (q_there && (js < 2 || ready(&o_done[js & 1], (js >> 1) - 1)) && ready(&k_full[s], js / NS)) {
+            tc_fence_after();
+            const uint32_t sk = smem_u32(smem + L::k + s * L::kChunks * kKBox);
 #pragma unroll
-        for (int kk = 0; kk < HD / 16; ++kk)
-          mma_bf16(tmem + kTK * (j & 1), sdesc_k128(sa + (kk >> 2) * kQBox + (kk & 3) * 32),
-                   sdesc_k128(sk + (kk >> 2) * kKBox + (kk & 3) * 32), id_s, kk > 0 ? 1u : 0u);
-        mma_commit(&s_full[j & 1]);
-        mma_commit(&k_empty[s]);
-        return true;
-      };
-      int j = 0, left = count, unit = 0;
-      int n = at.hi - at.lo;  // blocks of the unit
-      for (;; ++unit) {
-        ok = mbar_wait(q_full, unit & 1, abort_flag, p.budget) && issue_s(j);
-        for (int u = 0; u < n && ok; ++u, ++j) {
-          const int s = j % NS;
-          if (u + 1 < n && !(ok = issue_s(j + 1))) break;
-          if (!(ok = mbar_wait(&v_full[s], (j / NS) & 1, abort_flag, p.budget))) break;
-          if (!(ok = mbar_wait(&p_full[j & 1], (j >> 1) & 1, abort_flag, p.budget))) break;
+            for (int kk = 0; kk < HD / 16; ++kk)
+              mma_bf16(tmem + kTK * (js & 1), sdesc_k128(sa + (kk >> 2) * kQBox + (kk & 3) * 32),
+                       sdesc_k128(sk + (kk >> 2) * kKBox + (kk & 3) * 32), id_s, kk > 0 ? 1u : 0u);
+            mma_commit(&s_full[js & 1]);
+            if (HD != 128) mma_commit(&k_empty[s]);
+            ++js;
+            did = true;
+          }
+        }
+        if (jp < js && ready(&p_full[jp & 1], jp >> 1) && ready(&v_full[jp % NV], jp / NV)) {
+          if (jp == pv_end) {
+            pv.next(p, sq);
+            pv_begin = pv_end;
+            pv_end += pv.hi - pv.lo;
+          }
           tc_fence_after();
-          const uint32_t sv = smem_u32(smem + L::v + s * L::kChunks * kKBox);
+          const uint32_t sv = smem_u32(smem + L::v + (jp % NV) * L::kChunks * kKBox), sp = smem_u32(smem + L::third_at(jp));
 #pragma unroll
           for (int kk = 0; kk < 2 * (kTK / 16); ++kk) {  // the weights' first terms, then their second, then their third
             const int x = kk % (kTK / 16), term = kk / (kTK / 16);
-            mma_bf16_ts(t_o, tmem + kTK * (j & 1) + 16 * x + 8 * term, sdesc_mn128(sv + x * 2048, kKBox), id_o,
-                        (u > 0 || kk > 0) ? 1u : 0u);
+            mma_bf16_ts(t_o, tmem + kTK * (jp & 1) + 16 * x + 8 * term, sdesc_mn128(sv + x * 2048, kKBox), id_o,
+                        (jp > pv_begin || kk > 0) ? 1u : 0u);
           }
 #pragma unroll
           for (int x = 0; x < kTK / 16; ++x)
             mma_bf16(t_o, sdesc_k128(sp + x * 32), sdesc_mn128(sv + x * 2048, kKBox), id_o, 1u);
-          mma_commit(&o_done[j & 1]);
-          mma_commit(&v_empty[s]);
+          mma_commit(&o_done[jp & 1]);
+          mma_commit(&v_empty[jp % NV]);
+          if (HD == 128) mma_commit(&k_empty[jp % NS]);
+          ++jp;
+          did = true;
         }
-        left -= n;
-        if (!ok || left <= 0) break;
-        at.next(p, sq);
-        n = at.hi - at.lo;
+        if (did) since = clock64();
+        else if (*abort_flag || clock64() - since > p.budget) ok = false;
       }
       if (!ok) {
         *abort_flag = 1;
@@ -361,36 +397,47 @@ __global__ void __launch_bounds__(kThreads, 2)
       volatile int no_abort = 0;
       if (!mbar_wait(drain, 0, &no_abort, p.budget)) set_status(p.status, SPD_ETIMEOUT);
     }
-  } else if (warp < nw) {
-    // ---- softmax: warp w reads TMEM lanes [32 w, 32 w + 32) ----
-    const int r = warp * 32 + lane, T = nw * 32;
-    const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
+  } else if ((warp & 3) < nw) {
+    // ---- softmax: warps w and w + 4 read TMEM lanes [32 w, 32 w + 32), of S, O and P half of the columns each ----
+    // A wait that gives up must not part the two, which meet at barriers: it ends the loop for both at the next.
+    const int quad = warp & 3, half = warp >> 2, r = quad * 32 + lane, T = nw * 64, tid = half * (nw * 32) + r;
+    const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16;
+    constexpr int HC = HD / 2;  // columns of O a thread
+    const uint32_t t_oh = t_o + lanes + half * HC;
+    float* red = reinterpret_cast<float*>(smem + L::red) + r;
+    auto any_pair = [&](bool mine) { return pair_or(quad + 1, mine); };
+    auto share = [&](float mine, bool most) {  // the larger or the sum of the two threads' values, for both
+      if (half) *red = mine;
+      pair_sync(quad + 1);
+      if (!half) *red = mine = most ? fmaxf(mine, *red) : mine + *red;
+      pair_sync(quad + 1);
+      return half ? *red : mine;
+    };
     // a unit's rows: the thread's token, head and query row
     struct Row {
-      int token, hc;
+      int token;
       bool valid;
       size_t row;  // token of the call times n_heads + head
     };
     auto row_of = [&](const Place& u) {
       const PagedSeq& s = sq.s[u.e];
       const int t = u.tile / p.chunks, h0 = (u.tile - t * p.chunks) * p.chunk, n0 = t * p.tokens;
-      const int tokens = min(p.tokens, s.n - n0), heads = min(p.chunk, p.group - h0);
+      const int tokens = min(p.tokens, s.n - n0), heads = min(p.chunk, p.group - h0), hc = r % p.chunk;
       Row w;
       w.token = n0 + min(r / p.chunk, tokens - 1);  // rows without a token repeat the last one's, and are not stored
-      w.hc = r % p.chunk;
-      w.valid = r < tokens * p.chunk && w.hc < heads;
-      w.row = (size_t(s.q0) + w.token) * p.n_heads + u.hk * p.group + h0 + min(w.hc, heads - 1);
+      w.valid = r < tokens * p.chunk && hc < heads;
+      w.row = (size_t(s.q0) + w.token) * p.n_heads + u.hk * p.group + h0 + min(hc, heads - 1);
       return w;
     };
     auto load_q = [&](const Row& w) {  // in the 128-byte swizzle: 16-byte piece j of row r at j ^ (r % 8)
-      const uint4* src = reinterpret_cast<const uint4*>(p.q + w.row * HD);
+      const uint4* src = reinterpret_cast<const uint4*>(p.q + w.row * HD) + half * (HD / 16);
+      uint4 v[HD / 16];
 #pragma unroll
-      for (int h = 0; h < HD / 64; ++h) {
-        uint4 v[8];
+      for (int j = 0; j < HD / 16; ++j) v[j] = src[j];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = src[8 * h + j];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(smem + L::q + h * kQBox + r * 128 + ((j ^ (r & 7)) << 4)) = v[j];
+      for (int j = 0; j < HD / 16; ++j) {
+        const int piece = half * (HD / 16) + j;
+        *reinterpret_cast<uint4*>(smem + L::q + (piece >> 3) * kQBox + r * 128 + (((piece & 7) ^ (r & 7)) << 4)) = v[j];
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -405,19 +452,19 @@ __global__ void __launch_bounds__(kThreads, 2)
       const int n0 = at.tile / p.chunks * p.tokens;
       const int lim = limit_of(s, row.token);                            // what the row sees,
       const int lim_all = limit_of(s, n0), lim_any = limit_of(s, min(s.n, n0 + p.tokens) - 1);  // every row, some row
-      float m_run = -INFINITY, l_run = 0.0f;  // the row's maximum so far (raw scores) and sum of weights
+      float m_run = -INFINITY, l_run = 0.0f;  // the row's reference (raw scores); the thread's sum of weights
       for (int blk = at.lo; blk < at.hi; ++blk, ++j) {
-        const uint32_t t_s = tmem + kTK * (j & 1) + lanes;
+        const uint32_t t_s = tmem + kTK * (j & 1) + lanes + half * (kTK / 2);
         const int kb = blk * kTK;
         const bool partly = kb + kTK > lim_all;  // the block holds keys that not every row sees, or none at all
         if (partly) {
-          if (!(ok = __all_sync(0xffffffffu, mbar_wait(&v_full[j % NS], (j / NS) & 1, abort_flag, p.budget)))) break;
+          ok = ok && mbar_wait(&v_full[j % NV], (j / NV) & 1, abort_flag, p.budget);
           bool odd = false;
-          for (int x = threadIdx.x; x < kTK * L::kChunks; x += T) {
+          for (int x = tid; x < kTK * L::kChunks; x += T) {
             if (kb + x % kTK < lim_all) continue;
-            uint4* vr = reinterpret_cast<uint4*>(smem + L::v + (j % NS) * L::kChunks * kKBox + x * 128);
+            uint4* vr = reinterpret_cast<uint4*>(smem + L::v + (j % NV) * L::kChunks * kKBox + x * 128);
             bool here = false;
-#pragma unroll
+#pragma unroll 2
             for (int y = 0; y < 8; ++y) {
               const int at_piece = (y + x) & 7;  // (rows begin at the same bank)
               uint4 w = vr[at_piece];
@@ -431,46 +478,53 @@ __global__ void __launch_bounds__(kThreads, 2)
           fence_proxy_async_smem();
           // (every softmax warp arrives on p_full after its share, so the products see all of them)
         }
-        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s_full[j & 1], (j >> 1) & 1, abort_flag, p.budget)))) break;
+        ok = ok && mbar_wait(&s_full[j & 1], (j >> 1) & 1, abort_flag, p.budget);
+        __syncwarp();
         tc_fence_after();
-        float v[kTK];
-        tmem_ld64(t_s, v);
+        float v[kTK / 2];
+        tmem_ld32(t_s, v);
         if (partly) {
+          const int sees = lim - kb - half * (kTK / 2);
 #pragma unroll
-          for (int i = 0; i < kTK; ++i)
-            if (kb + i >= lim) v[i] = -INFINITY;
+          for (int i = 0; i < kTK / 2; ++i)
+            if (i >= sees) v[i] = -INFINITY;
         }
         float m4[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-        for (int i = 4; i < kTK; ++i) m4[i & 3] = fmaxf(m4[i & 3], v[i]);
+        for (int i = 4; i < kTK / 2; ++i) m4[i & 3] = fmaxf(m4[i & 3], v[i]);
         const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-        if (blk == at.lo) {
-          m_run = mx;
-        } else if (__any_sync(0xffffffffu, (mx - m_run) * p.scale_log2 > kGrown)) {
-          // a row's weights have outgrown its reference. The products before have completed once o_done says so: O can be
-          // rescaled
-          if (!(ok = __all_sync(0xffffffffu, mbar_wait(&o_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort_flag, p.budget)))) break;
-          tc_fence_after();
-          const float m_new = fmaxf(m_run, mx);
+        if (any_pair(blk == at.lo || (mx - m_run) * p.scale_log2 > kGrown || !ok)) {
+          // the references are taken anew. O can be rescaled once the products before have completed
+          if (blk > at.lo) ok = ok && mbar_wait(&o_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort_flag, p.budget);
+          if (any_pair(!ok)) {
+            ok = false;
+            break;
+          }
+          const float m_new = fmaxf(m_run, share(mx, true));
           const float corr = m_new == m_run ? 1.0f : ex2((m_run - m_new) * p.scale_log2);
           m_run = m_new;
           l_run *= corr;
+          if (blk > at.lo) {
+            __syncwarp();
+            tc_fence_after();
 #pragma unroll 1
-          for (int c = 0; c < HD / 32; ++c) {
-            float ov[32];
-            tmem_ld32(t_o + lanes + c * 32, ov);
+            for (int c = 0; c < HC; c += 8) {
+              float ov[8];
+              tmem_ld8(t_oh + c, ov);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) ov[i] *= corr;
-            tmem_st32(t_o + lanes + c * 32, ov);
+              for (int i = 0; i < 8; ++i) ov[i] *= corr;
+              tmem_st8(t_oh + c, ov);
+            }
+            tmem_st_wait();
           }
         }
         const float off = m_run == -INFINITY ? 0.0f : m_run * p.scale_log2;  // nothing seen yet: all weights are 0
         const Two scale{p.scale_log2, p.scale_log2}, less{-off, -off}, minus{-1.0f, -1.0f};
         Two sum[2] = {Two{0.0f, 0.0f}, Two{0.0f, 0.0f}};
-        uint32_t third[kTK / 2];  // keys 2 i and 2 i + 1 in word i
 #pragma unroll
-        for (int x = 0; x < kTK / 16; ++x) {
-          float first_t[8], second_t[8];  // the terms of keys 16 x + 2 i and 16 x + 2 i + 1 in word i
+        for (int x = 0; x < kTK / 32; ++x) {
+          float first_t[8], second_t[8];  // the terms of keys 16 x + 2 i and 16 x + 2 i + 1 of the half in word i
+          uint32_t third[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int k = 16 * x + 2 * i;
@@ -483,18 +537,17 @@ __global__ void __launch_bounds__(kThreads, 2)
             first_t[i] = __uint_as_float(hi);
             second_t[i] = __uint_as_float(mid);
             w = fma2(two_of(mid), minus, w);
-            third[k >> 1] = pack_bf16(w.lo, w.hi);
+            third[i] = pack_bf16(w.lo, w.hi);
           }
           tmem_st8(t_s + 16 * x, first_t);  // over the scores
           tmem_st8(t_s + 16 * x + 8, second_t);
+          uint8_t* to = smem + L::third_at(j) + r * 128;
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+            *reinterpret_cast<uint4*>(to + (((half * 4 + 2 * x + y) ^ (r & 7)) << 4)) =
+                make_uint4(third[4 * y], third[4 * y + 1], third[4 * y + 2], third[4 * y + 3]);
         }
         l_run += (sum[0].lo + sum[0].hi) + (sum[1].lo + sum[1].hi);
-        // the third terms' place is free when the block before has been multiplied
-        if (j > 0 && !(ok = __all_sync(0xffffffffu, mbar_wait(&o_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort_flag, p.budget)))) break;
-#pragma unroll
-        for (int y = 0; y < 8; ++y)
-          *reinterpret_cast<uint4*>(smem + L::p3 + r * 128 + ((y ^ (r & 7)) << 4)) =
-              make_uint4(third[4 * y], third[4 * y + 1], third[4 * y + 2], third[4 * y + 3]);
         fence_proxy_async_smem();
         tmem_st_wait();
         tc_fence_before();
@@ -510,25 +563,31 @@ __global__ void __launch_bounds__(kThreads, 2)
         row = row_of(then);
         load_q(row);
       }
-      if (!(ok = __all_sync(0xffffffffu, mbar_wait(&o_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort_flag, p.budget)))) break;
+      ok = mbar_wait(&o_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort_flag, p.budget);
+      if (any_pair(!ok)) {
+        ok = false;
+        break;
+      }
+      l_run = share(l_run, false);
+      __syncwarp();
       tc_fence_after();
       // A V that every row sees and that is infinite: the products of a weight's terms, which can be 0 or negative, are NaN
       // together. Which infinity a column has is the same for every row (each has a weight above 0 for it).
       float sick = 0.0f;  // NaN where a column is not finite
 #pragma unroll 1
-      for (int c = 0; c < HD / 32; ++c) {
+      for (int c = 0; c < HC; c += 32) {
         float ov[32];
-        tmem_ld32(t_o + lanes + c * 32, ov);
+        tmem_ld32(t_oh + c, ov);
 #pragma unroll
         for (int i = 0; i < 32; ++i) sick = fmaf(ov[i], 0.0f, sick);
       }
       const int key0 = at.lo * kTK, key1 = min(at.hi * kTK, lim_any);
-      const __nv_bfloat16* vcol = p.pool + (size_t(p.n_kv_heads) + at.hk) * HD;
+      const __nv_bfloat16* vcol = p.pool + (size_t(p.n_kv_heads) + at.hk) * HD + half * HC;
       const size_t ld = 2 * size_t(p.n_kv_heads) * HD;
       const int rows_all = p.n_pages * p.page_size;
       const bool mend = now.valid && isnan(sick) && !isnan(l_run);  // (scores that are NaN leave the row NaN)
       if (__any_sync(0xffffffffu, mend)) {
-        constexpr int E = HD / 32;  // columns a lane looks through
+        constexpr int E = HC / 32;  // columns a lane looks through
         uint32_t has = 0;  // of column e in bits 4 e: +inf, -inf, NaN
         for (int k = key0; k < min(lim_all, key1); ++k) {
           const int at_row = pool_row(p, s.seq, k);
@@ -540,16 +599,17 @@ __global__ void __launch_bounds__(kThreads, 2)
           }
         }
 #pragma unroll 1
-        for (int c = 0; c < HD / 32; ++c) {
-          float ov[32];
-          tmem_ld32(t_o + lanes + c * 32, ov);
+        for (int c = 0; c < HC; c += 8) {
+          float ov[8];
+          tmem_ld8(t_oh + c, ov);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const uint32_t h = (__shfl_sync(0xffffffffu, has, (c * 32 + i) / E) >> (4 * (i % E))) & 15u;
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t h = (__shfl_sync(0xffffffffu, has, (c + i) / E) >> (4 * ((c + i) % E))) & 15u;
             if (mend && isnan(ov[i]) && (h == 1u || h == 2u)) ov[i] = h == 1u ? INFINITY : -INFINITY;
           }
-          tmem_st32(t_o + lanes + c * 32, ov);
+          tmem_st8(t_oh + c, ov);
         }
+        tmem_st_wait();
       }
       if (*reinterpret_cast<volatile int*>(odd_v) > unit) {
         // values of V that were cleared: rows that see one add p v in fp32 (the score again from q and k)
@@ -561,54 +621,54 @@ __global__ void __launch_bounds__(kThreads, 2)
           const bool sees = now.valid && k < lim;
           const __nv_bfloat16* kr = p.pool + at_row * ld + at.hk * HD;
           const __nv_bfloat16* vr = vcol + at_row * ld;
-          for (int c = 0; c < L::kChunks; ++c) {
-            const uint32_t two = *reinterpret_cast<const uint32_t*>(vr + c * 64 + 2 * lane);
-            if (!__any_sync(0xffffffffu, not_finite(two))) continue;
-            float d = 0.0f;
-            if (sees)
-              for (int x = 0; x < HD; ++x) d = fmaf(__bfloat162float(qsrc[x]), __bfloat162float(kr[x]), d);
-            const float w = ex2(fmaf(d, p.scale_log2, -off));
+          bool some = false;
+          for (int x = lane; x < HC; x += 32) some |= !isfinite(__bfloat162float(vr[x]));
+          if (!__any_sync(0xffffffffu, some)) continue;
+          float d = 0.0f;
+          if (sees)
+            for (int x = 0; x < HD; ++x) d = fmaf(__bfloat162float(qsrc[x]), __bfloat162float(kr[x]), d);
+          const float w = ex2(fmaf(d, p.scale_log2, -off));
 #pragma unroll 1
-            for (int b = 0; b < 2; ++b) {
-              float ov[32];
-              tmem_ld32(t_o + lanes + c * 64 + b * 32, ov);
+          for (int c = 0; c < HC; c += 8) {
+            float ov[8];
+            tmem_ld8(t_oh + c, ov);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                const float x = __bfloat162float(vr[c * 64 + b * 32 + i]);
-                if (sees && !isfinite(x)) ov[i] = fmaf(w, x, ov[i]);
-              }
-              tmem_st32(t_o + lanes + c * 64 + b * 32, ov);
+            for (int i = 0; i < 8; ++i) {
+              const float x = __bfloat162float(vr[c + i]);
+              if (sees && !isfinite(x)) ov[i] = fmaf(w, x, ov[i]);
             }
+            tmem_st8(t_oh + c, ov);
           }
+          tmem_st_wait();
         }
       }
       const float m2 = m_run * p.scale_log2;
       if (at.hi - at.lo < at.blocks) {
         const size_t slot = (2 * size_t(blockIdx.x) + (at.lo == 0)) * p.rows_part + r;
-        if (now.valid) p.part_ml[slot] = make_float2(m2, l_run);
-        float* po = p.part_o + slot * HD;
+        if (now.valid && !half) p.part_ml[slot] = make_float2(m2, l_run);
+        float* po = p.part_o + slot * HD + half * HC;
 #pragma unroll 1
-        for (int c = 0; c < HD / 32; ++c) {
+        for (int c = 0; c < HC; c += 32) {
           float v[32];
-          tmem_ld32(t_o + lanes + c * 32, v);
+          tmem_ld32(t_oh + c, v);
           if (now.valid) {
 #pragma unroll
             for (int y = 0; y < 8; ++y)
-              reinterpret_cast<float4*>(po + c * 32)[y] = make_float4(v[4 * y], v[4 * y + 1], v[4 * y + 2], v[4 * y + 3]);
+              reinterpret_cast<float4*>(po + c)[y] = make_float4(v[4 * y], v[4 * y + 1], v[4 * y + 2], v[4 * y + 3]);
           }
         }
       } else {
         const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
-        __nv_bfloat16* orow = p.o + now.row * HD;
-        if (now.valid && p.lse) p.lse[now.row] = fmaf(m2, 0.6931471805599453f, logf(l_run));
+        __nv_bfloat16* orow = p.o + now.row * HD + half * HC;
+        if (now.valid && !half && p.lse) p.lse[now.row] = fmaf(m2, 0.6931471805599453f, logf(l_run));
 #pragma unroll 1
-        for (int c = 0; c < HD / 32; ++c) {
+        for (int c = 0; c < HC; c += 32) {
           float v[32];
-          tmem_ld32(t_o + lanes + c * 32, v);
+          tmem_ld32(t_oh + c, v);
           if (now.valid) {
 #pragma unroll
             for (int y = 0; y < 4; ++y)
-              reinterpret_cast<uint4*>(orow + c * 32)[y] =
+              reinterpret_cast<uint4*>(orow + c)[y] =
                   make_uint4(pack_bf16(v[8 * y] * inv, v[8 * y + 1] * inv), pack_bf16(v[8 * y + 2] * inv, v[8 * y + 3] * inv),
                              pack_bf16(v[8 * y + 4] * inv, v[8 * y + 5] * inv), pack_bf16(v[8 * y + 6] * inv, v[8 * y + 7] * inv));
           }
@@ -625,15 +685,15 @@ __global__ void __launch_bounds__(kThreads, 2)
   }
   tc_fence_before();
   __syncthreads();
-  if (threadIdx.x == 128 && *abort_flag) {
+  if (threadIdx.x == 256 && *abort_flag) {
     // loads issued but never consumed land before the CTA exits
     volatile int no_abort = 0;
     for (int j = max(0, issued_k - NS); j < issued_k; ++j) mbar_wait(&k_full[j % NS], (j / NS) & 1, &no_abort, p.budget);
-    for (int j = max(0, issued_v - NS); j < issued_v; ++j) mbar_wait(&v_full[j % NS], (j / NS) & 1, &no_abort, p.budget);
+    for (int j = max(0, issued_v - NV); j < issued_v; ++j) mbar_wait(&v_full[j % NV], (j / NV) & 1, &no_abort, p.budget);
   }
   __syncwarp();
   tc_fence_after();
-  if (warp == 4) tmem_dealloc(tmem, kTmemCols);
+  if (warp == 8) tmem_dealloc(tmem, kTmemCols);
   if (threadIdx.x == 0) stamp_end(p.stamp);
 }
 
@@ -930,6 +990,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
             l[r] *= corr[r];
           }
           if (blk > at.lo) {
+            __syncwarp();
             tc_fence_after();
 #pragma unroll
             for (int x = 0; x < 3 * (R / 8); ++x) {
@@ -987,6 +1048,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
         ok = false;
         break;
       }
+      __syncwarp();
       tc_fence_after();
       const size_t row = size_t(s.q0) * p.n_heads + at.hk * p.group;
       const bool whole = at.hi - at.lo == at.blocks;
