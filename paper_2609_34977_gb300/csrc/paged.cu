@@ -199,6 +199,31 @@ struct Place {
   }
 };
 
+// Products and commits by a whole warp in step, of which one lane issues: descriptors then stay in uniform registers. (A lane on its own
+// moves every operand there for each product: 1000 cycles a block of keys, and more than the products take.)
+__device__ __forceinline__ void issue_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(add))
+      : "memory");
+}
+__device__ __forceinline__ void issue_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(uint32_t(add))
+      : "memory");
+}
+__device__ __forceinline__ void issue_commit(uint64_t* bar) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar))
+      : "memory");
+}
+// A value that all lanes hold, in a uniform register.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_max_sync(0xffffffffu, x); }
+
 // Barriers of the two warps that have the same rows.
 __device__ __forceinline__ void pair_sync(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
 __device__ __forceinline__ bool pair_or(int id, bool mine) {
@@ -326,77 +351,76 @@ __global__ void __launch_bounds__(kThreads, 2)
       set_status(p.status, SPD_ETIMEOUT);
     }
   } else if (warp == 9) {
-    if (lane == 0) {
-      // ---- MMA issuer ----
-      const uint32_t id_s = idesc_bf16_f32(128, kTK);
-      const uint32_t id_o = idesc_bf16_f32(128, HD) | (1u << 16);  // V is MN-major
-      const uint32_t sa = smem_u32(smem + L::q);
-      auto ready = [&](uint64_t* bar, int phase) { return mbar_test(bar, phase & 1); };
-      // Blocks in order, S and PV as their operands come: S of block js where K and Q are there and the S buffer is free (the PV
-      // products of block js - 2 completed), PV of block jp where V and P are there.
-      int js = 0, jp = 0, unit = 0, unit_end = at.hi - at.lo;  // js's unit, and the first block behind it
-      int pv_begin = 0, pv_end = unit_end;                     // jp's unit
-      Place pv = at;
-      bool q_there = false, ok = true;
-      long long since = clock64();
-      while (jp < count && ok) {
-        bool did = false;
-        if (js < count) {
-          if (js == unit_end) {
-            at.next(p, sq);
-            unit_end += at.hi - at.lo;
-            ++unit;
-            q_there = false;
-          }
-          if (!q_there) q_there = ready(q_full, unit);
-          const int s = js % NS;
-          if (q_there && (js < 2 || ready(&o_done[js & 1], (js >> 1) - 1)) && ready(&k_full[s], js / NS)) {
-            tc_fence_after();
-            const uint32_t sk = smem_u32(smem + L::k + s * L::kChunks * kKBox);
-#pragma unroll
-            for (int kk = 0; kk < HD / 16; ++kk)
-              mma_bf16(tmem + kTK * (js & 1), sdesc_k128(sa + (kk >> 2) * kQBox + (kk & 3) * 32),
-                       sdesc_k128(sk + (kk >> 2) * kKBox + (kk & 3) * 32), id_s, kk > 0 ? 1u : 0u);
-            mma_commit(&s_full[js & 1]);
-            if (HD != 128) mma_commit(&k_empty[s]);
-            ++js;
-            did = true;
-          }
+    // ---- MMA issuer (all lanes in step) ----
+    const uint32_t id_s = idesc_bf16_f32(128, kTK);
+    const uint32_t id_o = idesc_bf16_f32(128, HD) | (1u << 16);  // V is MN-major
+    const uint32_t base = smem_u32(smem), t_all = uniform(tmem);
+    const int blocks = int(uniform(uint32_t(count)));
+    auto ready = [&](uint64_t* bar, int phase) { return __all_sync(0xffffffffu, mbar_test(bar, phase & 1)) != 0; };
+    // Blocks in order, S and PV as their operands come: S of block js where K and Q are there and the S buffer is free (the PV
+    // products of block js - 2 completed), PV of block jp where V and P are there.
+    int js = 0, jp = 0, unit = 0, unit_end = at.hi - at.lo;  // js's unit, and the first block behind it
+    int pv_begin = 0, pv_end = unit_end;                     // jp's unit
+    Place pv = at;
+    bool q_there = false, ok = true;
+    long long since = clock64();
+    while (jp < blocks && ok) {
+      bool did = false;
+      if (js < blocks) {
+        if (js == unit_end) {
+          at.next(p, sq);
+          unit_end += at.hi - at.lo;
+          ++unit;
+          q_there = false;
         }
-        if (jp < js && ready(&p_full[jp & 1], jp >> 1) && ready(&v_full[jp % NV], jp / NV)) {
-          if (jp == pv_end) {
-            pv.next(p, sq);
-            pv_begin = pv_end;
-            pv_end += pv.hi - pv.lo;
-          }
+        if (!q_there) q_there = ready(q_full, unit);
+        const int s = js % NS;
+        if (q_there && (js < 2 || ready(&o_done[js & 1], (js >> 1) - 1)) && ready(&k_full[s], js / NS)) {
           tc_fence_after();
-          const uint32_t sv = smem_u32(smem + L::v + (jp % NV) * L::kChunks * kKBox), sp = smem_u32(smem + L::third_at(jp));
+          const uint64_t dk = sdesc_k128(base + L::k + s * L::kChunks * kKBox), dq = sdesc_k128(base + L::q);
 #pragma unroll
-          for (int kk = 0; kk < 2 * (kTK / 16); ++kk) {  // the weights' first terms, then their second, then their third
-            const int x = kk % (kTK / 16), term = kk / (kTK / 16);
-            mma_bf16_ts(t_o, tmem + kTK * (jp & 1) + 16 * x + 8 * term, sdesc_mn128(sv + x * 2048, kKBox), id_o,
-                        (jp > pv_begin || kk > 0) ? 1u : 0u);
-          }
-#pragma unroll
-          for (int x = 0; x < kTK / 16; ++x)
-            mma_bf16(t_o, sdesc_k128(sp + x * 32), sdesc_mn128(sv + x * 2048, kKBox), id_o, 1u);
-          mma_commit(&o_done[jp & 1]);
-          mma_commit(&v_empty[jp % NV]);
-          if (HD == 128) mma_commit(&k_empty[jp % NS]);
-          ++jp;
+          for (int kk = 0; kk < HD / 16; ++kk)
+            issue_ss(t_all + kTK * (js & 1), dq + (((kk >> 2) * kQBox + (kk & 3) * 32) >> 4),
+                     dk + (((kk >> 2) * kKBox + (kk & 3) * 32) >> 4), id_s, kk > 0);
+          issue_commit(&s_full[js & 1]);
+          if (HD != 128) issue_commit(&k_empty[s]);
+          ++js;
           did = true;
         }
-        if (did) since = clock64();
-        else if (*abort_flag || clock64() - since > p.budget) ok = false;
       }
-      if (!ok) {
-        *abort_flag = 1;
-        set_status(p.status, SPD_ETIMEOUT);
+      const int s = jp % NV;
+      if (jp < js && ready(&p_full[jp & 1], jp >> 1) && ready(&v_full[s], jp / NV)) {
+        if (jp == pv_end) {
+          pv.next(p, sq);
+          pv_begin = pv_end;
+          pv_end += pv.hi - pv.lo;
+        }
+        tc_fence_after();
+        const uint32_t t_ov = t_all + 2 * kTK, t_p = t_all + kTK * (jp & 1);
+        const uint64_t dv = sdesc_mn128(base + L::v + s * L::kChunks * kKBox, kKBox), dp = sdesc_k128(base + L::third_at(jp));
+#pragma unroll
+        for (int kk = 0; kk < 2 * (kTK / 16); ++kk) {  // the weights' first terms, then their second, then their third
+          const int k = kk % (kTK / 16), term = kk / (kTK / 16);
+          issue_ts(t_ov, t_p + 16 * k + 8 * term, dv + ((k * 2048) >> 4), id_o, jp > pv_begin || kk > 0);
+        }
+#pragma unroll
+        for (int k = 0; k < kTK / 16; ++k) issue_ss(t_ov, dp + ((k * 32) >> 4), dv + ((k * 2048) >> 4), id_o, true);
+        issue_commit(&o_done[jp & 1]);
+        issue_commit(&v_empty[s]);
+        if (HD == 128) issue_commit(&k_empty[jp % NS]);
+        ++jp;
+        did = true;
       }
-      mma_commit(drain);  // arrives once every MMA issued above has completed
-      volatile int no_abort = 0;
-      if (!mbar_wait(drain, 0, &no_abort, p.budget)) set_status(p.status, SPD_ETIMEOUT);
+      if (did) since = clock64();
+      else ok = __all_sync(0xffffffffu, !*abort_flag && clock64() - since <= p.budget);
     }
+    if (!ok) {
+      *abort_flag = 1;
+      set_status(p.status, SPD_ETIMEOUT);
+    }
+    issue_commit(drain);  // arrives once every MMA issued above has completed
+    volatile int no_abort = 0;
+    if (!mbar_wait(drain, 0, &no_abort, p.budget)) set_status(p.status, SPD_ETIMEOUT);
   } else if ((warp & 3) < nw) {
     // ---- softmax: warps w and w + 4 read TMEM lanes [32 w, 32 w + 32), of S, O and P half of the columns each ----
     // A wait that gives up must not part the two, which meet at barriers: it ends the loop for both at the next.
@@ -838,65 +862,62 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
       }
     } while (ok && at.next(p, sq));
   } else if (warp == 5) {
-    if (lane == 0) {
-      // ---- MMA issuer ----
-      const uint32_t id_s = idesc_bf16_f32(128, kTokenHeads);
-      const uint32_t id_o = idesc_bf16_f32(128, 64) | (3u << 15);  // V and P are MN-major
-      auto issue_s = [&](int j, int unit) -> bool {
+    // ---- MMA issuer (all lanes in step) ----
+    const uint32_t id_s = idesc_bf16_f32(128, kTokenHeads);
+    const uint32_t id_o = idesc_bf16_f32(128, 64) | (3u << 15);  // V and P are MN-major
+    const uint32_t base = smem_u32(smem), t_all = uniform(tmem);
+    auto wait = [&](uint64_t* bar, int phase) { return __all_sync(0xffffffffu, mbar_wait(bar, phase & 1, abort_flag, p.budget)) != 0; };
+    auto issue_s = [&](int j, int unit) -> bool {
+      const int s = j % NS;
+      if (!wait(&k_full[s], j / NS)) return false;
+      // (the scores of block j - 2 have been read: its weights have arrived)
+      tc_fence_after();
+      const uint64_t dk = sdesc_k128(base + L::k + s * 2 * L::box), dq = sdesc_k128(base + L::q + (unit & 1) * 2 * L::qbox);
+#pragma unroll
+      for (int kk = 0; kk < HD / 16; ++kk)
+        issue_ss(t_all + kTokenHeads * (j & 1), dk + (((kk >> 2) * L::box + (kk & 3) * 32) >> 4),
+                 dq + (((kk >> 2) * L::qbox + (kk & 3) * 32) >> 4), id_s, kk > 0);
+      issue_commit(&s_full[j & 1]);
+      issue_commit(&k_empty[s]);
+      return true;
+    };
+    int j = 0, unit = 0;
+    int n = at.hi - at.lo;  // blocks of the unit
+    ok = wait(&q_full[0], 0) && issue_s(0, 0);
+    while (ok) {
+      Place then = at;
+      const bool more = then.next(p, sq);
+      for (int u = 0; u < n && ok; ++u, ++j) {
         const int s = j % NS;
-        if (!mbar_wait(&k_full[s], (j / NS) & 1, abort_flag, p.budget)) return false;
-        // (the scores of block j - 2 have been read: its weights have arrived)
-        tc_fence_after();
-        const uint32_t sk = smem_u32(smem + L::k + s * 2 * L::box), qa = smem_u32(smem + L::q + (unit & 1) * 2 * L::qbox);
-#pragma unroll
-        for (int kk = 0; kk < HD / 16; ++kk)
-          mma_bf16(tmem + kTokenHeads * (j & 1), sdesc_k128(sk + (kk >> 2) * L::box + (kk & 3) * 32),
-                   sdesc_k128(qa + (kk >> 2) * L::qbox + (kk & 3) * 32), id_s, kk > 0 ? 1u : 0u);
-        mma_commit(&s_full[j & 1]);
-        mma_commit(&k_empty[s]);
-        return true;
-      };
-      int j = 0, left = count, unit = 0;
-      int n = at.hi - at.lo;  // blocks of the unit
-      ok = mbar_wait(&q_full[0], 0, abort_flag, p.budget) && issue_s(0, 0);
-      while (ok) {
-        Place then = at;
-        const bool more = then.next(p, sq);
-        for (int u = 0; u < n && ok; ++u, ++j) {
-          const int s = j % NS;
-          if (u + 1 < n) {
-            if (!(ok = issue_s(j + 1, unit))) break;
-          } else {
-            mma_commit(&q_empty[unit & 1]);
-            // the next unit's first block
-            if (more && !(ok = mbar_wait(&q_full[(unit + 1) & 1], ((unit + 1) >> 1) & 1, abort_flag, p.budget) && issue_s(j + 1, unit + 1)))
-              break;
-          }
-          if (!(ok = mbar_wait(&v_full[s], (j / NS) & 1, abort_flag, p.budget))) break;
-          if (!(ok = mbar_wait(p_full, j & 1, abort_flag, p.budget))) break;
-          tc_fence_after();
-          const uint32_t sv = smem_u32(smem + L::v + s * 2 * L::box), sp = smem_u32(smem + L::p);
-#pragma unroll
-          for (int x = 0; x < kTokenKeys / 16; ++x)
-            mma_bf16(t_o, sdesc_mn128(sv + x * 2048, L::box), sdesc_mn128(sp + x * 2048, L::box), id_o, (u > 0 || x > 0) ? 1u : 0u);
-          mma_commit(o_done);
-          mma_commit(&v_empty[s]);
+        if (u + 1 < n) {
+          if (!(ok = issue_s(j + 1, unit))) break;
+        } else {
+          issue_commit(&q_empty[unit & 1]);
+          // the next unit's first block
+          if (more && !(ok = wait(&q_full[(unit + 1) & 1], (unit + 1) >> 1) && issue_s(j + 1, unit + 1))) break;
         }
-        left -= n;
-        if (!ok || !more) break;
-        at = then;
-        n = at.hi - at.lo;
-        ++unit;
+        if (!(ok = wait(&v_full[s], j / NS))) break;
+        if (!(ok = wait(p_full, j))) break;
+        tc_fence_after();
+        const uint64_t dv = sdesc_mn128(base + L::v + s * 2 * L::box, L::box), dp = sdesc_mn128(base + L::p, L::box);
+#pragma unroll
+        for (int x = 0; x < kTokenKeys / 16; ++x)
+          issue_ss(t_all + 64, dv + ((x * 2048) >> 4), dp + ((x * 2048) >> 4), id_o, u > 0 || x > 0);
+        issue_commit(o_done);
+        issue_commit(&v_empty[s]);
       }
-      if (!ok) {
-        *abort_flag = 1;
-        set_status(p.status, SPD_ETIMEOUT);
-      }
-      mma_commit(drain);  // arrives once every MMA issued above has completed
-      volatile int no_abort = 0;
-      if (!mbar_wait(drain, 0, &no_abort, p.budget)) set_status(p.status, SPD_ETIMEOUT);
-      ok = true;
+      if (!ok || !more) break;
+      at = then;
+      n = at.hi - at.lo;
+      ++unit;
     }
+    issue_commit(drain);  // arrives once every MMA issued above has completed
+    volatile int no_abort = 0;
+    if (!ok) {
+      *abort_flag = 1;
+      set_status(p.status, SPD_ETIMEOUT);
+    }
+    if (!mbar_wait(drain, 0, &no_abort, p.budget)) set_status(p.status, SPD_ETIMEOUT);
   } else if (warp == 6) {
     // ---- Q: 16 rows of 128, those past the group's zero, in the 128-byte swizzle ----
     int unit = 0;
