@@ -35,7 +35,7 @@ constexpr int kTK = 64;                // keys a block
 constexpr uint32_t kQBox = 128 * 128;  // 64 columns of the Q tile
 constexpr uint32_t kKBox = kTK * 128;  // 64 columns of a block of K or V
 constexpr int kThreads = 320;
-constexpr uint32_t kTmemCols = 256;    // S: two buffers [0, 64) and [64, 128); O: [128, 128 + HD)
+constexpr uint32_t kTmemCols = 256;    // S: 256 / HD + 1, at most three buffers of 64 columns less what O takes behind them
 constexpr int kCtas = 304;             // CTAs that fill the GPU: two on each of 152 SMs
 // The reference that a row's exponentials are taken against is renewed once its maximum has grown by this much (log2
 // units): weights stay below 2^8, their terms and the fp32 sums are relative to them, and almost no block pays for the
@@ -71,23 +71,24 @@ struct PagedArgs {
 };
 
 // The third terms of a block's weights, [128][64], take the place of its K, which has been read when they are written (heads of
-// 128: the same 16 KB), or one of two places of their own: they need not wait for the products of the block before.
+// 128: the same 16 KB), or one of three places of their own: they need not wait for the products of the block before.
 template <int HD>
 struct PagedSmem {
   static constexpr int kChunks = HD / 64;
   static constexpr uint32_t third = 128 * 128;
-  static constexpr int kStages = HD == 128 ? 3 : 4;   // of K
-  static constexpr int kStagesV = HD == 128 ? 2 : 4;
+  static constexpr int kBufs = HD == 128 ? 2 : 3;      // of S in TMEM, behind them O
+  static constexpr int kStages = 3;                    // of K
+  static constexpr int kStagesV = HD == 128 ? 2 : 3;
   static constexpr uint32_t q = 0;
   static constexpr uint32_t k = q + kChunks * kQBox;
   static constexpr uint32_t v = k + kStages * kChunks * kKBox;
   static constexpr uint32_t p3 = v + kStagesV * kChunks * kKBox;
-  static constexpr uint32_t bars = p3 + (HD == 128 ? 0 : 2 * third);
+  static constexpr uint32_t bars = p3 + (HD == 128 ? 0 : kBufs * third);
   static constexpr uint32_t red = bars + 256;    // [128] what the two threads of a row tell each other
   static constexpr uint32_t bytes = red + 512;   // (two CTAs an SM: at most 113 KB)
   static_assert(bytes <= 113 * 1024, "two CTAs an SM");
   static_assert(HD != 128 || kChunks * kKBox == third, "third terms in a block's K");
-  __device__ static uint32_t third_at(int j) { return HD == 128 ? k + (j % kStages) * third : p3 + (j & 1) * third; }
+  __device__ static uint32_t third_at(int j) { return HD == 128 ? k + (j % kStages) * third : p3 + (j % kBufs) * third; }
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -251,17 +252,17 @@ __global__ void __launch_bounds__(kThreads, 2)
     paged_attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ PagedArgs p,
                       const __grid_constant__ PagedSeqs sq) {
   using L = PagedSmem<HD>;
-  constexpr int NS = L::kStages, NV = L::kStagesV;
+  constexpr int NS = L::kStages, NV = L::kStagesV, NB = L::kBufs;
   extern __shared__ __align__(1024) uint8_t smem[];  // (the swizzle's atoms; no room to round the address up)
   uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + L::bars);  // [NS] K block landed
   uint64_t* k_empty = k_full + NS;                                 // [NS] its S product (third terms in it: its PV products) completed
   uint64_t* v_full = k_empty + NS;                                 // [NV] V block landed
   uint64_t* v_empty = v_full + NV;                                 // [NV] its PV products have completed
   uint64_t* q_full = v_empty + NV;   // a unit's Q tile is in shared memory
-  uint64_t* s_full = q_full + 1;     // [2] S of block j is in TMEM buffer j % 2
-  uint64_t* p_full = s_full + 2;     // [2] P of block j written and O rescaled
-  uint64_t* o_done = p_full + 2;     // [2] PV products of block j completed
-  uint64_t* drain = o_done + 2;      // every MMA completed
+  uint64_t* s_full = q_full + 1;     // [NB] S of block j is in TMEM buffer j % NB
+  uint64_t* p_full = s_full + NB;    // [NB] P of block j written and O rescaled
+  uint64_t* o_done = p_full + NB;    // [NB] PV products of block j completed
+  uint64_t* drain = o_done + NB;     // every MMA completed
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* odd_v = reinterpret_cast<int*>(tmem_slot + 2);  // the last unit (counted from 1) with a V that is not finite
@@ -286,7 +287,7 @@ __global__ void __launch_bounds__(kThreads, 2)
       mbar_init(&v_empty[s], 1);
     }
     mbar_init(q_full, 2 * nw);
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < NB; ++s) {
       mbar_init(&s_full[s], 1);
       mbar_init(&p_full[s], 2 * nw);  // one arrival per softmax warp
       mbar_init(&o_done[s], 1);
@@ -305,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 2)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  const uint32_t t_o = tmem + 2 * kTK;
+  const uint32_t t_o = tmem + NB * kTK;
 
   pdl_launch_dependents();
   pdl_wait();
@@ -358,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     const int blocks = int(uniform(uint32_t(count)));
     auto ready = [&](uint64_t* bar, int phase) { return __all_sync(0xffffffffu, mbar_test(bar, phase & 1)) != 0; };
     // Blocks in order, S and PV as their operands come: S of block js where K and Q are there and the S buffer is free (the PV
-    // products of block js - 2 completed), PV of block jp where V and P are there.
+    // products of block js - NB completed), PV of block jp where V and P are there.
     int js = 0, jp = 0, unit = 0, unit_end = at.hi - at.lo;  // js's unit, and the first block behind it
     int pv_begin = 0, pv_end = unit_end;                     // jp's unit
     Place pv = at;
@@ -375,28 +376,28 @@ __global__ void __launch_bounds__(kThreads, 2)
         }
         if (!q_there) q_there = ready(q_full, unit);
         const int s = js % NS;
-        if (q_there && (js < 2 || ready(&o_done[js & 1], (js >> 1) - 1)) && ready(&k_full[s], js / NS)) {
+        if (q_there && (js < NB || ready(&o_done[js % NB], js / NB - 1)) && ready(&k_full[s], js / NS)) {
           tc_fence_after();
           const uint64_t dk = sdesc_k128(base + L::k + s * L::kChunks * kKBox), dq = sdesc_k128(base + L::q);
 #pragma unroll
           for (int kk = 0; kk < HD / 16; ++kk)
-            issue_ss(t_all + kTK * (js & 1), dq + (((kk >> 2) * kQBox + (kk & 3) * 32) >> 4),
+            issue_ss(t_all + kTK * (js % NB), dq + (((kk >> 2) * kQBox + (kk & 3) * 32) >> 4),
                      dk + (((kk >> 2) * kKBox + (kk & 3) * 32) >> 4), id_s, kk > 0);
-          issue_commit(&s_full[js & 1]);
+          issue_commit(&s_full[js % NB]);
           if (HD != 128) issue_commit(&k_empty[s]);
           ++js;
           did = true;
         }
       }
       const int s = jp % NV;
-      if (jp < js && ready(&p_full[jp & 1], jp >> 1) && ready(&v_full[s], jp / NV)) {
+      if (jp < js && ready(&p_full[jp % NB], jp / NB) && ready(&v_full[s], jp / NV)) {
         if (jp == pv_end) {
           pv.next(p, sq);
           pv_begin = pv_end;
           pv_end += pv.hi - pv.lo;
         }
         tc_fence_after();
-        const uint32_t t_ov = t_all + 2 * kTK, t_p = t_all + kTK * (jp & 1);
+        const uint32_t t_ov = t_all + NB * kTK, t_p = t_all + kTK * (jp % NB);
         const uint64_t dv = sdesc_mn128(base + L::v + s * L::kChunks * kKBox, kKBox), dp = sdesc_k128(base + L::third_at(jp));
 #pragma unroll
         for (int kk = 0; kk < 2 * (kTK / 16); ++kk) {  // the weights' first terms, then their second, then their third
@@ -405,7 +406,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         }
 #pragma unroll
         for (int k = 0; k < kTK / 16; ++k) issue_ss(t_ov, dp + ((k * 32) >> 4), dv + ((k * 2048) >> 4), id_o, true);
-        issue_commit(&o_done[jp & 1]);
+        issue_commit(&o_done[jp % NB]);
         issue_commit(&v_empty[s]);
         if (HD == 128) issue_commit(&k_empty[jp % NS]);
         ++jp;
@@ -478,7 +479,7 @@ __global__ void __launch_bounds__(kThreads, 2)
       const int lim_all = limit_of(s, n0), lim_any = limit_of(s, min(s.n, n0 + p.tokens) - 1);  // every row, some row
       float m_run = -INFINITY, l_run = 0.0f;  // the row's reference (raw scores); the thread's sum of weights
       for (int blk = at.lo; blk < at.hi; ++blk, ++j) {
-        const uint32_t t_s = tmem + kTK * (j & 1) + lanes + half * (kTK / 2);
+        const uint32_t t_s = tmem + kTK * (j % NB) + lanes + half * (kTK / 2);
         const int kb = blk * kTK;
         const bool partly = kb + kTK > lim_all;  // the block holds keys that not every row sees, or none at all
         if (partly) {
@@ -502,7 +503,7 @@ __global__ void __launch_bounds__(kThreads, 2)
           fence_proxy_async_smem();
           // (every softmax warp arrives on p_full after its share, so the products see all of them)
         }
-        ok = ok && mbar_wait(&s_full[j & 1], (j >> 1) & 1, abort_flag, p.budget);
+        ok = ok && mbar_wait(&s_full[j % NB], (j / NB) & 1, abort_flag, p.budget);
         __syncwarp();
         tc_fence_after();
         float v[kTK / 2];
@@ -519,7 +520,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
         if (any_pair(blk == at.lo || (mx - m_run) * p.scale_log2 > kGrown || !ok)) {
           // the references are taken anew. O can be rescaled once the products before have completed
-          if (blk > at.lo) ok = ok && mbar_wait(&o_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort_flag, p.budget);
+          if (blk > at.lo) ok = ok && mbar_wait(&o_done[(j - 1) % NB], ((j - 1) / NB) & 1, abort_flag, p.budget);
           if (any_pair(!ok)) {
             ok = false;
             break;
@@ -576,7 +577,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&p_full[j & 1]);
+        if (lane == 0) mbar_arrive(&p_full[j % NB]);
       }
       if (!ok) break;
       // the next unit's Q goes in while the last products run (their S has been read, so Q is free)
@@ -587,7 +588,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         row = row_of(then);
         load_q(row);
       }
-      ok = mbar_wait(&o_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort_flag, p.budget);
+      ok = mbar_wait(&o_done[(j - 1) % NB], ((j - 1) / NB) & 1, abort_flag, p.budget);
       if (any_pair(!ok)) {
         ok = false;
         break;
