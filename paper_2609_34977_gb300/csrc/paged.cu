@@ -62,9 +62,10 @@ struct PagedArgs {
   __nv_bfloat16* o;
   float* lse;
   int total, ctas, warps;            // blocks; CTAs; quarters of the tile (32 rows) that have rows
-  float* part_o;                     // [2 ctas][rows_part][HD] states of parts: slot 2 c of the part that goes on with a unit
-  float2* part_ml;                   // (CTA c), 2 c + 1 of the one that begins one; maximum (log2 units) and sum
+  float* part_o;                     // [2 ctas][rows_part HD] states of parts: slot 2 c of the part that goes on with a unit (CTA
+  float2* part_ml;                   // c), 2 c + 1 of the one that begins one; [2 ctas][rows_part] maximum (log2 units) and sum
   int rows_part;
+  bool by_row;                       // states [rows_part][HD], else [HD / 4][rows_part][4]
   int* status;
   long long budget;
   unsigned long long* stamp;
@@ -671,7 +672,9 @@ __global__ void __launch_bounds__(kThreads, 2)
       if (at.hi - at.lo < at.blocks) {
         const size_t slot = (2 * size_t(blockIdx.x) + (at.lo == 0)) * p.rows_part + r;
         if (now.valid && !half) p.part_ml[slot] = make_float2(m2, l_run);
-        float* po = p.part_o + slot * HD + half * HC;
+        // [HD / 4][rows_part][4]: the rows of a warp side by side; few rows: [rows_part][HD]
+        float4* po = reinterpret_cast<float4*>(p.part_o) + (p.by_row ? slot * (HD / 4) : (slot - r) * (HD / 4) + r);
+        const int step = p.by_row ? 1 : p.rows_part;
 #pragma unroll 1
         for (int c = 0; c < HC; c += 32) {
           float v[32];
@@ -679,7 +682,7 @@ __global__ void __launch_bounds__(kThreads, 2)
           if (now.valid) {
 #pragma unroll
             for (int y = 0; y < 8; ++y)
-              reinterpret_cast<float4*>(po + c)[y] = make_float4(v[4 * y], v[4 * y + 1], v[4 * y + 2], v[4 * y + 3]);
+              po[((half * HC + c) / 4 + y) * step] = make_float4(v[4 * y], v[4 * y + 1], v[4 * y + 2], v[4 * y + 3]);
           }
         }
       } else {
@@ -1122,118 +1125,145 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
 // Units whose blocks several CTAs had: states (m_i, l_i, O_i) joined in key order, m = max m_i, l = sum l_i 2^(m_i - m),
 // O = sum O_i 2^(m_i - m). A part in which a row sees nothing has l_i = 0. (Its maximum does not tell: fmaxf passes over those of
 // parts whose scores are all NaN, whose sums are NaN and stay so.) blockIdx.x stands for the border between two CTAs; the first
-// border inside a unit has it. R = 1: W warps a row, each a range of the parts, four of them in flight; R = 4: a warp has four rows at a
-// time, one part of each in flight.
+// border inside a unit has it.
+struct Split {
+  Place u;
+  int c, parts;  // the CTA that begins the unit; CTAs that have a part of it
+  bool mine;     // this border is the first inside the unit (all threads alike)
+  __device__ __forceinline__ void find(const PagedArgs& p, const PagedSeqs& sq) {
+    const int border = first_block(p, int(blockIdx.x) + 1);
+    c = int(blockIdx.x);
+    u.seek(p, sq, border, 1);
+    const int start = border - u.lo;
+    mine = u.lo > 0 && first_block(p, c) <= start;
+    parts = int(((long long)(start + u.blocks) * p.ctas + p.total - 1) / p.total) - c;
+  }
+  __device__ __forceinline__ size_t slot(int part) const { return 2 * size_t(c + part) + (part == 0); }
+};
+struct State {
+  float m = -INFINITY, l = 0.0f;
+};
+// A part's state joined to a row's: what both sums are multiplied by.
+__device__ __forceinline__ float2 join(State& s, float2 ml) {
+  if (ml.y == 0.0f) return make_float2(1.0f, 0.0f);
+  const float m = fmaxf(s.m, ml.x), keep = exp2f(s.m - m), f = exp2f(ml.x - m);
+  s.l = fmaf(ml.y, f, s.l * keep);
+  s.m = m;
+  return make_float2(keep, f);
+}
+
+// Tiles: a thread a row and eight columns, so that the rows of a warp lie side by side in every load; three parts in flight.
+constexpr int kMergeThreads = 256;
+template <int HD>
+__global__ void __launch_bounds__(kMergeThreads)
+    paged_merge_kernel(const __grid_constant__ PagedArgs p, const __grid_constant__ PagedSeqs sq) {
+  constexpr int A = 3;
+  pdl_launch_dependents();
+  Split x;
+  x.find(p, sq);
+  const PagedSeq& s = sq.s[x.u.e];
+  const int t = x.u.tile / p.chunks, h0 = (x.u.tile - t * p.chunks) * p.chunk, n0 = t * p.tokens;
+  const int at = int(blockIdx.y) * kMergeThreads + int(threadIdx.x), col = at / p.rows_part, r = at - col * p.rows_part;
+  const int hc = r % p.chunk, token = r / p.chunk;
+  pdl_wait();
+  if (!x.mine || col >= HD / 8 || token >= min(p.tokens, s.n - n0) || hc >= min(p.chunk, p.group - h0)) return;
+  State st;
+  float o[8] = {};
+  for (int k0 = 0; k0 < x.parts; k0 += A) {
+    float2 ml[A];
+    float4 v[A][2];
+#pragma unroll
+    for (int k = 0; k < A; ++k) {
+      ml[k] = make_float2(-INFINITY, 0.0f);
+      if (k0 + k >= x.parts) continue;
+      const size_t slot = x.slot(k0 + k) * p.rows_part;
+      const float4* po = reinterpret_cast<const float4*>(p.part_o) + slot * (HD / 4) + 2 * col * p.rows_part + r;
+      ml[k] = p.part_ml[slot + r];
+      v[k][0] = po[0];
+      v[k][1] = po[p.rows_part];
+    }
+#pragma unroll
+    for (int k = 0; k < A; ++k) {
+      if (ml[k].y == 0.0f) continue;  // a part in which the row sees nothing
+      const float2 f = join(st, ml[k]);
+      const float w[8] = {v[k][0].x, v[k][0].y, v[k][0].z, v[k][0].w, v[k][1].x, v[k][1].y, v[k][1].z, v[k][1].w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] = fmaf(w[i], f.y, o[i] * f.x);
+    }
+  }
+  const float inv = st.l == 0.0f ? 0.0f : 1.0f / st.l;
+  const size_t row = (size_t(s.q0) + n0 + token) * p.n_heads + x.u.hk * p.group + h0 + hc;
+  *reinterpret_cast<uint4*>(p.o + row * HD + 8 * col) = make_uint4(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv),
+                                                                  pack_bf16(o[4] * inv, o[5] * inv), pack_bf16(o[6] * inv, o[7] * inv));
+  if (p.lse && col == 0) p.lse[row] = fmaf(st.m, 0.6931471805599453f, logf(st.l));
+}
+
+// Few rows of many parts: W warps a row, a lane HD / 32 columns, each warp a range of the parts, four in flight.
 constexpr int kMergeWarps = 8, kMergeAhead = 4, kMergeRows = 32;
-template <int HD, int R>
+template <int HD>
 __global__ void __launch_bounds__(kMergeWarps * 32)
-    paged_merge_kernel(const __grid_constant__ PagedArgs p, const __grid_constant__ PagedSeqs sq, int W) {
-  constexpr int D = HD / 32;            // dims a lane
-  constexpr int A = R == 1 ? kMergeAhead : 1;
+    row_merge_kernel(const __grid_constant__ PagedArgs p, const __grid_constant__ PagedSeqs sq, int W) {
+  constexpr int A = kMergeAhead, D = HD / 32;
   __shared__ float2 wml[kMergeWarps];
   __shared__ float wo[kMergeWarps][HD];
   pdl_launch_dependents();
-  const int c = int(blockIdx.x) + 1, border = first_block(p, c);
-  Place u;
-  u.seek(p, sq, border, 1);
-  const int start = border - u.lo, end = start + u.blocks;
+  Split x;
+  x.find(p, sq);
+  const PagedSeq& s = sq.s[x.u.e];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp & (W - 1);
-  const int r0 = (int(blockIdx.y) * kMergeWarps + warp) / W * R;
-  const PagedSeq& s = sq.s[u.e];
-  const int t = u.tile / p.chunks, h0 = (u.tile - t * p.chunks) * p.chunk, n0 = t * p.tokens;
-  const bool mine = u.lo > 0 && first_block(p, c - 1) <= start;  // (all threads alike)
-  const int rows = mine ? min(p.tokens, s.n - n0) * p.chunk : 0, heads = min(p.chunk, p.group - h0);
-  const int parts = int(((long long)end * p.ctas + p.total - 1) / p.total) - (c - 1);
+  const int r = (int(blockIdx.y) * kMergeWarps + warp) / W;
+  const int t = x.u.tile / p.chunks, h0 = (x.u.tile - t * p.chunks) * p.chunk, n0 = t * p.tokens;
+  const int hc = r % p.chunk, token = r / p.chunk;
+  const bool have = token < min(p.tokens, s.n - n0) && hc < min(p.chunk, p.group - h0);
   pdl_wait();
-  if (!mine) return;
-  float m[R], l[R], o[R][D];
+  if (!x.mine) return;
+  State st;
+  float o[D] = {};
+  auto add = [&](float2 ml, const float* v) {
+    if (ml.y == 0.0f) return;  // nothing was seen
+    const float2 f = join(st, ml);
 #pragma unroll
-  for (int i = 0; i < R; ++i) {
-    m[i] = -INFINITY;
-    l[i] = 0.0f;
+    for (int i = 0; i < D; ++i) o[i] = fmaf(v[i], f.y, o[i] * f.x);
+  };
+  if (have) {
+    const int k1 = (w + 1) * x.parts / W;
+    for (int k0 = w * x.parts / W; k0 < k1; k0 += A) {
+      float2 ml[A];
+      float v[A][D];
 #pragma unroll
-    for (int x = 0; x < D; ++x) o[i][x] = 0.0f;
-  }
-  if (r0 < rows) {
-    const int s1 = int((w + 1) * parts / W);
-    for (int s0 = int(w * parts / W); s0 < s1; s0 += A) {
-      float2 ml[R][A];
-      float v[R][A][D];
-#pragma unroll
-      for (int i = 0; i < R; ++i)
-#pragma unroll
-        for (int k = 0; k < A; ++k) {
-          ml[i][k] = make_float2(-INFINITY, 0.0f);
-          if (s0 + k >= s1 || r0 + i >= rows) continue;
-          const size_t slot = (2 * size_t(c - 1 + s0 + k) + (s0 + k == 0)) * p.rows_part + r0 + i;
-          ml[i][k] = p.part_ml[slot];
-          const float* po = p.part_o + slot * HD + D * lane;
-          if constexpr (D == 4) {
-            const float4 f = *reinterpret_cast<const float4*>(po);
-            v[i][k][0] = f.x, v[i][k][1] = f.y, v[i][k][2] = f.z, v[i][k][3] = f.w;
-          } else {
-            const float2 f = *reinterpret_cast<const float2*>(po);
-            v[i][k][0] = f.x, v[i][k][1] = f.y;
-          }
-        }
-#pragma unroll
-      for (int i = 0; i < R; ++i) {
-        float top = m[i];
-        bool some = false;
-#pragma unroll
-        for (int k = 0; k < A; ++k) {
-          top = fmaxf(top, ml[i][k].x);
-          some |= ml[i][k].y != 0.0f;
-        }
-        if (!some) continue;
-        const float keep = exp2f(m[i] - top);
-        m[i] = top;
-        l[i] *= keep;
-#pragma unroll
-        for (int x = 0; x < D; ++x) o[i][x] *= keep;
-#pragma unroll
-        for (int k = 0; k < A; ++k) {
-          if (ml[i][k].y == 0.0f) continue;  // a part in which the row sees nothing
-          const float f = exp2f(ml[i][k].x - top);
-          l[i] = fmaf(ml[i][k].y, f, l[i]);
-#pragma unroll
-          for (int x = 0; x < D; ++x) o[i][x] = fmaf(v[i][k][x], f, o[i][x]);
+      for (int k = 0; k < A; ++k) {
+        ml[k] = make_float2(-INFINITY, 0.0f);
+        if (k0 + k >= k1) continue;
+        const size_t slot = x.slot(k0 + k) * p.rows_part + r;
+        ml[k] = p.part_ml[slot];
+        const float* po = p.part_o + slot * HD + D * lane;
+        if constexpr (D == 4) {
+          const float4 f = *reinterpret_cast<const float4*>(po);
+          v[k][0] = f.x, v[k][1] = f.y, v[k][2] = f.z, v[k][3] = f.w;
+        } else {
+          const float2 f = *reinterpret_cast<const float2*>(po);
+          v[k][0] = f.x, v[k][1] = f.y;
         }
       }
+#pragma unroll
+      for (int k = 0; k < A; ++k) add(ml[k], v[k]);
     }
   }
-  if constexpr (R == 1) {
-    if (W > 1) {
-      if (lane == 0) wml[warp] = make_float2(m[0], l[0]);
+  if (W > 1) {
+    if (lane == 0) wml[warp] = make_float2(st.m, st.l);
 #pragma unroll
-      for (int x = 0; x < D; ++x) wo[warp][D * lane + x] = o[0][x];
-      __syncthreads();
-      if (w > 0) return;
-      for (int k = 1; k < W; ++k) m[0] = fmaxf(m[0], wml[warp + k].x);
-      l[0] = 0.0f;
-#pragma unroll
-      for (int x = 0; x < D; ++x) o[0][x] = 0.0f;
-      for (int k = 0; k < W; ++k) {
-        const float2 ml = wml[warp + k];
-        if (ml.y == 0.0f) continue;
-        const float f = exp2f(ml.x - m[0]);
-        l[0] = fmaf(ml.y, f, l[0]);
-#pragma unroll
-        for (int x = 0; x < D; ++x) o[0][x] = fmaf(wo[warp + k][D * lane + x], f, o[0][x]);
-      }
-    }
+    for (int i = 0; i < D; ++i) wo[warp][D * lane + i] = o[i];
+    __syncthreads();
+    if (w > 0) return;
+    for (int k = 1; k < W; ++k) add(wml[warp + k], &wo[warp + k][D * lane]);
   }
+  if (!have) return;
+  const float inv = st.l == 0.0f ? 0.0f : 1.0f / st.l;
+  const size_t row = (size_t(s.q0) + n0 + token) * p.n_heads + x.u.hk * p.group + h0 + hc;
+  uint32_t* to = reinterpret_cast<uint32_t*>(p.o + row * HD + D * lane);
 #pragma unroll
-  for (int i = 0; i < R; ++i) {
-    const int r = r0 + i, hc = r % p.chunk;
-    if (r >= rows || hc >= heads) continue;
-    const float inv = l[i] == 0.0f ? 0.0f : 1.0f / l[i];
-    const size_t at = (size_t(s.q0) + n0 + r / p.chunk) * p.n_heads + u.hk * p.group + h0 + hc;
-    uint32_t* to = reinterpret_cast<uint32_t*>(p.o + at * HD + D * lane);
-#pragma unroll
-    for (int x = 0; x < D / 2; ++x) to[x] = pack_bf16(o[i][2 * x] * inv, o[i][2 * x + 1] * inv);
-    if (p.lse && lane == 0) p.lse[at] = fmaf(m[i], 0.6931471805599453f, logf(l[i]));
-  }
+  for (int i = 0; i < D / 2; ++i) to[i] = pack_bf16(o[2 * i] * inv, o[2 * i + 1] * inv);
+  if (p.lse && lane == 0) p.lse[row] = fmaf(st.m, 0.6931471805599453f, logf(st.l));
 }
 
 // Rows of a state: a tile's, or as many as the call has.
@@ -1322,6 +1352,7 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
       }
       p.total = int(total);
       p.ctas = int(std::min<long long>(token ? sms : 2 * sms, total));
+      p.by_row = token || std::min(most, p.tokens) * p.chunk <= kMergeRows;
       p.warps = (std::min(most, p.tokens) * p.chunk + 31) / 32;
       const double fl = 4.0 * head_dim * n_heads * pairs;
       const double by = 4.0 * kvd * keys + 4.0 * n_heads * head_dim * tokens;
@@ -1339,18 +1370,18 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
       }));
       SPD_CUDA_TRY(launch_pdl(kernel, dim3(p.ctas), dim3(token ? kTokenThreads : kThreads), smem, st, map, p, sq));
       if (p.ctas > 1) {
-        const int parts = int((long long)longest * p.ctas / total) + 2;  // of a unit, at most
-        const int rows_unit = std::min(most, p.tokens) * p.chunk;
-        if (rows_unit > kMergeRows) {  // many rows of few parts
-          SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? paged_merge_kernel<128, 4> : paged_merge_kernel<64, 4>,
-                                  dim3(p.ctas - 1, (rows_unit + 4 * kMergeWarps - 1) / (4 * kMergeWarps)), dim3(kMergeWarps * 32), 0, st,
-                                  p, sq, 1));
-        } else {
+        if (p.by_row) {
+          const int parts = int((long long)longest * p.ctas / total) + 2;  // of a unit, at most
+          const int rows_unit = std::min(most, p.tokens) * p.chunk;
           int W = 1;
           while (W < kMergeWarps && parts > kMergeAhead * W) W *= 2;
-          SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? paged_merge_kernel<128, 1> : paged_merge_kernel<64, 1>,
+          SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? row_merge_kernel<128> : row_merge_kernel<64>,
                                   dim3(p.ctas - 1, (rows_unit * W + kMergeWarps - 1) / kMergeWarps), dim3(kMergeWarps * 32), 0, st, p,
                                   sq, W));
+        } else {
+          const int threads = p.rows_part * (head_dim / 8);
+          SPD_CUDA_TRY(launch_pdl(head_dim == 128 ? paged_merge_kernel<128> : paged_merge_kernel<64>,
+                                  dim3(p.ctas - 1, (threads + kMergeThreads - 1) / kMergeThreads), dim3(kMergeThreads), 0, st, p, sq));
         }
       }
       trace_end(slot, st, TR_ATTN, fl, by);
