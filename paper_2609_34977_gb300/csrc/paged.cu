@@ -726,25 +726,27 @@ __global__ void __launch_bounds__(kThreads, 2)
 }
 
 // ---- single tokens --------------------------------------------------------------------------------
-// A sequence's one new token with up to 16 query heads a K/V head (heads of 128): too few rows to fill an MMA's 128, so
-// keys and dims are its rows: S^T = K Q^T (128 keys x 16 heads), O^T += V^T P^T (128 dims x 64), V in place as an MN-major
-// operand, P^T through shared memory. P^T's columns are the three bf16 terms of every head's weights, side by side (48 of 64), so
+// A sequence's one new token with up to 16 query heads a K/V head: too few rows to fill an MMA's 128, so keys and dims are its
+// rows: S^T = K Q^T (128 keys x 16 heads), O^T += V^T P^T (128 dims x 64; of heads of 64 the other half is what lies behind V,
+// and is not read), V in place as an MN-major operand, P^T through shared memory. P^T's columns are the three bf16 terms of every head's weights, side by side (48 of 64), so
 // V is read once for all of them and a term that is zero or negative does not meet an infinite V in another's sum. One CTA an
-// SM, three blocks of 128 keys on their way:
+// SM, 192 KB of K and V on their way:
 //   warp 4     TMA producer          warp 5     MMA issuer          warp 6     the units' Q, a unit ahead
 //   warps 0-3  a thread a key: exponentials against a reference a head, renewed for all of them once a score has
 //              outgrown one by kGrown; sums a thread, added up at the end. In the end a thread a dim: O out of TMEM.
-constexpr int kTokenKeys = 128, kTokenHeads = 16, kTokenStages = 3;
+constexpr int kTokenKeys = 128, kTokenHeads = 16;
 constexpr int kTokenThreads = 224;
+template <int HD>
 struct TokenSmem {
+  static constexpr int kStages = 384 / HD, kChunks = HD / 64;
   static constexpr uint32_t box = kTokenKeys * 128;        // 64 columns of a block of K or V
   static constexpr uint32_t qbox = kTokenHeads * 128;      // 64 columns of Q
   static constexpr uint32_t k = 0;
-  static constexpr uint32_t v = k + kTokenStages * 2 * box;
-  static constexpr uint32_t p = v + kTokenStages * 2 * box;  // [128 keys][64]
-  static constexpr uint32_t q = p + box;                     // two units'
-  static constexpr uint32_t bars = q + 2 * 2 * qbox;
-  static constexpr uint32_t red = bars + 256;                // [4 warps][16]
+  static constexpr uint32_t v = k + kStages * kChunks * box;
+  static constexpr uint32_t p = v + kStages * kChunks * box;  // [128 keys][64]
+  static constexpr uint32_t q = p + box;                      // two units'
+  static constexpr uint32_t bars = q + 2 * kChunks * qbox;
+  static constexpr uint32_t red = bars + 320;                 // [4 warps][16]
   static constexpr uint32_t bytes = red + 256;
   static_assert(bytes <= 227 * 1024, "one CTA an SM");
 };
@@ -765,12 +767,12 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 __device__ __forceinline__ float order_value(uint32_t u) { return __uint_as_float((u >> 31) ? u & 0x7fffffffu : ~u); }
 
 // R: heads a thread works on, 8 or 16 (those past the group's are of zeros and are not stored).
-template <int R>
+template <int HD, int R>
 __global__ void __launch_bounds__(kTokenThreads, 1)
     paged_token_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ PagedArgs p,
                        const __grid_constant__ PagedSeqs sq) {
-  using L = TokenSmem;
-  constexpr int HD = 128, NS = kTokenStages;
+  using L = TokenSmem<HD>;
+  constexpr int NS = L::kStages, NC = L::kChunks;
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + L::bars);  // [NS] K block landed
   uint64_t* k_empty = k_full + NS;                                 // [NS] its product has completed
@@ -848,15 +850,15 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
       for (int blk = at.lo; blk < at.hi && ok; ++blk, ++j) {
         const int here = row;
         if (blk + 1 < at.hi) row = row_at(blk + 1);  // a block ahead
-        const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, here >= 0)) * p.box * 256u;
+        const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, here >= 0)) * p.box * 128u * NC;
         const int st = j % NS;
         auto load = [&](uint64_t* full, uint64_t* empty, uint32_t to, int x0) -> bool {
           if (j >= NS && !__all_sync(0xffffffffu, mbar_wait(&empty[st], (j / NS - 1) & 1, abort_flag, p.budget))) return false;
           if (lane == 0) mbar_arrive_expect_tx(&full[st], bytes);
           __syncwarp();
           if (here >= 0)
-            for (int c = 0; c < 2; ++c)
-              tma_load_2d(smem + to + (st * 2 + c) * L::box + lane * p.box * 128, &map_kv, &full[st], x0 + c * 64, here, pol);
+            for (int c = 0; c < NC; ++c)
+              tma_load_2d(smem + to + (st * NC + c) * L::box + lane * p.box * 128, &map_kv, &full[st], x0 + c * 64, here, pol);
           return true;
         };
         if (!(ok = load(k_full, k_empty, L::k, at.hk * HD))) break;
@@ -876,7 +878,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
       if (!wait(&k_full[s], j / NS)) return false;
       // (the scores of block j - 2 have been read: its weights have arrived)
       tc_fence_after();
-      const uint64_t dk = sdesc_k128(base + L::k + s * 2 * L::box), dq = sdesc_k128(base + L::q + (unit & 1) * 2 * L::qbox);
+      const uint64_t dk = sdesc_k128(base + L::k + s * NC * L::box), dq = sdesc_k128(base + L::q + (unit & 1) * NC * L::qbox);
 #pragma unroll
       for (int kk = 0; kk < HD / 16; ++kk)
         issue_ss(t_all + kTokenHeads * (j & 1), dk + (((kk >> 2) * L::box + (kk & 3) * 32) >> 4),
@@ -903,7 +905,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
         if (!(ok = wait(&v_full[s], j / NS))) break;
         if (!(ok = wait(p_full, j))) break;
         tc_fence_after();
-        const uint64_t dv = sdesc_mn128(base + L::v + s * 2 * L::box, L::box), dp = sdesc_mn128(base + L::p, L::box);
+        const uint64_t dv = sdesc_mn128(base + L::v + s * NC * L::box, L::box), dp = sdesc_mn128(base + L::p, L::box);
 #pragma unroll
         for (int x = 0; x < kTokenKeys / 16; ++x)
           issue_ss(t_all + 64, dv + ((x * 2048) >> 4), dp + ((x * 2048) >> 4), id_o, u > 0 || x > 0);
@@ -923,22 +925,23 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
     }
     if (!mbar_wait(drain, 0, &no_abort, p.budget)) set_status(p.status, SPD_ETIMEOUT);
   } else if (warp == 6) {
-    // ---- Q: 16 rows of 128, those past the group's zero, in the 128-byte swizzle ----
+    // ---- Q: 16 rows, those past the group's zero, in the 128-byte swizzle ----
+    constexpr int P = HD / 8, N = 16 * P / 32;  // 16-byte pieces a row, a lane
     int unit = 0;
     do {
       const uint4* src = reinterpret_cast<const uint4*>(p.q + (size_t(sq.s[at.e].q0) * p.n_heads + at.hk * p.group) * HD);
-      uint4 v[8];
+      uint4 v[N];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int row = 2 * i + (lane >> 4);
-        v[i] = row < p.group ? src[row * (HD / 8) + (lane & 15)] : make_uint4(0u, 0u, 0u, 0u);
+      for (int i = 0; i < N; ++i) {
+        const int row = (32 * i + lane) / P, piece = lane % P;
+        v[i] = row < p.group ? src[row * P + piece] : make_uint4(0u, 0u, 0u, 0u);
       }
       const int b = unit & 1;
       if (unit >= 2 && !(ok = __all_sync(0xffffffffu, mbar_wait(&q_empty[b], ((unit >> 1) - 1) & 1, abort_flag, p.budget)))) break;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int row = 2 * i + (lane >> 4), piece = lane & 15;
-        *reinterpret_cast<uint4*>(smem + L::q + (b * 2 + (piece >> 3)) * L::qbox + row * 128 + (((piece & 7) ^ (row & 7)) << 4)) = v[i];
+      for (int i = 0; i < N; ++i) {
+        const int row = (32 * i + lane) / P, piece = lane % P;
+        *reinterpret_cast<uint4*>(smem + L::q + (b * NC + (piece >> 3)) * L::qbox + row * 128 + (((piece & 7) ^ (row & 7)) << 4)) = v[i];
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -963,9 +966,9 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
         if ((blk + 1) * kTokenKeys > s.len) {  // behind the last row: values that a weight of zero would turn into NaN
           ok = ok && mbar_wait(&v_full[j % NS], (j / NS) & 1, abort_flag, p.budget);
           if (!there) {
-            uint4* vr = reinterpret_cast<uint4*>(smem + L::v + (j % NS) * 2 * L::box + t * 128);
+            uint4* vr = reinterpret_cast<uint4*>(smem + L::v + (j % NS) * NC * L::box + t * 128);
 #pragma unroll
-            for (int y = 0; y < 16; ++y) vr[(y >> 3) * (L::box / 16) + ((y + t) & 7)] = make_uint4(0u, 0u, 0u, 0u);
+            for (int y = 0; y < 8 * NC; ++y) vr[(y >> 3) * (L::box / 16) + ((y + t) & 7)] = make_uint4(0u, 0u, 0u, 0u);
           }
           fence_proxy_async_smem();
         }
@@ -1086,7 +1089,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int r = 8 * y + i;
-          if (r >= p.group) continue;
+          if (r >= p.group || t >= HD) continue;
           if (isfinite(o[i])) o[i] += mid[i] + lo[i];  // (an infinite V meets lower terms that are 0 or negative)
           if (whole) p.o[(row + r) * HD + t] = __float2bfloat16(l[r] == 0.0f ? 0.0f : o[i] * (1.0f / l[r]));
           else p.part_o[(slot + r) * HD + t] = o[i];
@@ -1306,7 +1309,7 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
   p.part_ml = cv.take<float2>(rows);
   p.status = status;
   p.budget = kWaitBudget;
-  const bool tokens_apart = head_dim == 128 && p.group <= kTokenHeads;
+  const bool tokens_apart = p.group <= kTokenHeads;
   const int sms = std::min(kCtas / 2, num_sms());
   // sequences of one new token on their own where the token kernel takes them; up to kMaxSeqs a launch
   for (int form = 0; form < 2; ++form) {
@@ -1358,13 +1361,15 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
       const double by = 4.0 * kvd * keys + 4.0 * n_heads * head_dim * tokens;
       p.stamp = stamp_slot(TR_ATTN, fl, by);
       const int slot = trace_begin(st);
-      const int which = token ? (p.group <= 8 ? 0 : 1) : head_dim == 64 ? 2 : 3;
-      const auto kernel = which == 0   ? paged_token_kernel<8>
-                          : which == 1 ? paged_token_kernel<16>
-                          : which == 2 ? paged_attn_kernel<64>
-                                       : paged_attn_kernel<128>;
-      const uint32_t smem = token ? TokenSmem::bytes : head_dim == 64 ? PagedSmem<64>::bytes : PagedSmem<128>::bytes;
-      static DeviceOnce attr[4];
+      using Kernel = void (*)(CUtensorMap, PagedArgs, PagedSeqs);
+      static constexpr Kernel kernels[6] = {paged_token_kernel<64, 8>,   paged_token_kernel<128, 8>, paged_token_kernel<64, 16>,
+                                            paged_token_kernel<128, 16>, paged_attn_kernel<64>,      paged_attn_kernel<128>};
+      static constexpr uint32_t bytes[6] = {TokenSmem<64>::bytes,  TokenSmem<128>::bytes, TokenSmem<64>::bytes,
+                                            TokenSmem<128>::bytes, PagedSmem<64>::bytes,  PagedSmem<128>::bytes};
+      const int which = (token ? 2 * (p.group > 8) : 4) + (head_dim == 128);
+      const Kernel kernel = kernels[which];
+      const uint32_t smem = bytes[which];
+      static DeviceOnce attr[6];
       SPD_CUDA_TRY(once_per_device(attr[which], [&] {
         return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
       }));
