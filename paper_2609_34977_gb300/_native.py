@@ -721,41 +721,60 @@ def spd_logits_process(logits, out, best=None, *, seq_of=None, hist=None, hist_c
                                     _stream(stream)))
 
 
+_bytes = C.c_char * 0
+
+
+def _hp(a):
+    """_p of a C-contiguous numpy array or None, at half the cost where the array is writable."""
+    if a is None:
+        return None
+    try:
+        return _bytes.from_buffer(a)
+    except (TypeError, ValueError):
+        return _p(a)
+
+
 def _pool(pool, n_kv_heads, head_dim, layers=True):
     """Pointer and sizes (layers, pages, rows a page) of a pool [layers][pages][rows a page][K | V], or of one layer's block."""
     ptr = _dev(pool, "bf16", 1, "pool")
-    shape = tuple(pool.shape)
+    shape = pool.shape
     if len(shape) != (4 if layers else 3) or shape[-1] != 2 * n_kv_heads * head_dim:
-        raise ValueError(f"pool: shape {shape}, expected {'[layers]' if layers else ''}[pages][rows][{2 * n_kv_heads * head_dim}]")
-    return (ptr, *(shape[:3] if layers else (1, *shape[:2])))
+        raise ValueError(f"pool: shape {tuple(shape)}, expected {'[layers]' if layers else ''}[pages][rows]"
+                         f"[{2 * n_kv_heads * head_dim}]")
+    return (ptr, *shape[:3]) if layers else (ptr, 1, shape[0], shape[1])
 
 
 def _table(table, n, name="table"):
     """Pointer and width of a page table of n sequences."""
-    if len(table.shape) != 2 or table.shape[0] < n:
-        raise ValueError(f"{name}: shape {tuple(table.shape)}, expected [{n}][pages]")
-    return _dev(table, "i32", n * table.shape[1], name), table.shape[1]
+    shape = table.shape
+    if len(shape) != 2 or shape[0] < n:
+        raise ValueError(f"{name}: shape {tuple(shape)}, expected [{n}][pages]")
+    return _dev(table, "i32", n * shape[1], name), shape[1]
 
 
-def _rows_bf16(t, width, name):
-    """Pointer and row stride of a 2-D bf16 CUDA tensor whose rows are contiguous and `width` wide."""
+def _rows_bf16(t, n, width, name):
+    """Pointer and row stride of a 2-D bf16 CUDA tensor of at least n rows, contiguous and `width` wide."""
     if not getattr(t, "is_cuda", False):
         raise TypeError(f"{name}: device arguments of libspider must be CUDA tensors")
-    if t.dtype is not (_torch_dt or _load_dtypes())["bf16"] or len(t.shape) != 2 or t.shape[1] != width:
-        raise ValueError(f"{name}: expected bf16 [tokens][{width}], got {t.dtype} {tuple(t.shape)}")
+    shape = t.shape
+    if t.dtype is not (_torch_dt or _load_dtypes())["bf16"] or len(shape) != 2 or shape[1] != width:
+        raise ValueError(f"{name}: expected bf16 [tokens][{width}], got {t.dtype} {tuple(shape)}")
+    if shape[0] < n:
+        raise ValueError(f"{name}: {shape[0]} rows, the call reads {n}")
     ld, step = t.stride()
     if width > 1 and step != 1:
         raise ValueError(f"{name}: the values of a row must lie side by side")
-    if t.shape[0] > 1 and ld < width:
+    if shape[0] > 1 and ld < width:
         raise ValueError(f"{name}: rows overlap")
-    return t.data_ptr(), ld if t.shape[0] > 1 else width
+    return t.data_ptr(), ld if shape[0] > 1 else width
 
 
 def _axes(pos, axis, n_tok, head_dim):
     """Pointers of positions [axes][tokens] (or [tokens]) and of the pairs' axes, and the number of axes."""
-    n = 1 if len(pos.shape) == 1 else pos.shape[0]
-    if pos.shape[-1] != n_tok:
-        raise ValueError(f"pos: shape {tuple(pos.shape)}, expected [axes][{n_tok}]")
+    shape = pos.shape
+    n = 1 if len(shape) == 1 else shape[0]
+    if shape[-1] != n_tok:
+        raise ValueError(f"pos: shape {tuple(shape)}, expected [axes][{n_tok}]")
     ax = None if axis is None else _host(axis, np.uint8, head_dim // 2, "axis")
     return _dev(pos, "i32", n * n_tok, "pos"), n, ax
 
@@ -767,14 +786,12 @@ def spd_rope_pages(q, kv, pos, axis, theta, q_cu, lens, table, pool, n_heads, n_
     cu = np.ascontiguousarray(q_cu, dtype=np.int32)
     B, n = len(cu) - 1, int(cu[-1])
     ln = _host(lens, np.int32, B, "lens")
-    qp, ldq = _rows_bf16(q, n_heads * head_dim, "q")
-    kp, ldkv = _rows_bf16(kv, 2 * n_kv_heads * head_dim, "kv")
-    if q.shape[0] < n or kv.shape[0] < n:
-        raise ValueError(f"q, kv: {q.shape[0]} and {kv.shape[0]} rows, the call reads {n}")
+    qp, ldq = _rows_bf16(q, n, n_heads * head_dim, "q")
+    kp, ldkv = _rows_bf16(kv, n, 2 * n_kv_heads * head_dim, "kv")
     pp, axes, ax = _axes(pos, axis, n, head_dim)
     tp, width = _table(table, B)
     pool_p, _, pages, rows = _pool(pool, n_kv_heads, head_dim, layers=False)
-    _check(lib().spd_rope_pages(qp, ldq, kp, ldkv, n, pp, axes, _p(ax), float(theta), _p(cu), _p(ln), B, tp, width, pool_p, pages,
+    _check(lib().spd_rope_pages(qp, ldq, kp, ldkv, n, pp, axes, _hp(ax), float(theta), _hp(cu), _hp(ln), B, tp, width, pool_p, pages,
                                 rows, n_heads, n_kv_heads, head_dim, _dev(q_out, "bf16", n * n_heads * head_dim, "q_out"),
                                 None if ws is None else _ws(ws)[0], _stream(stream)))
 
@@ -794,7 +811,7 @@ def spd_paged_attention(q, q_cu, lens, table, pool, n_heads, n_kv_heads, head_di
     pool_p, _, pages, rows = _pool(pool, n_kv_heads, head_dim, layers=False)
     qd = n_heads * head_dim
     wp, wb = _ws(ws)
-    _check(lib().spd_paged_attention(_dev(q, "bf16", n * qd, "q"), n, _p(cu), _p(ln), _p(pre), B, tp, width, pool_p, pages, rows,
+    _check(lib().spd_paged_attention(_dev(q, "bf16", n * qd, "q"), n, _hp(cu), _hp(ln), _hp(pre), B, tp, width, pool_p, pages, rows,
                                      n_heads, n_kv_heads, head_dim, _dev(o, "bf16", n * qd, "o"),
                                      _dev(lse, "f32", n * n_heads, "lse", True), wp, wb, _stream(stream)))
 
@@ -817,8 +834,8 @@ def spd_decode_paged(model: SpdModel, x, q_cu, lens, pos, table, pool, logits, w
     if layers < c["n_layers"]:
         raise ValueError(f"pool: {layers} layers, the model has {c['n_layers']}")
     wp, wb = _ws(ws)
-    _check(lib().spd_decode_paged(model.handle, _dev(x, "bf16", n * c["d_model"], "x"), n, _p(cu), _p(ln), _p(pre), B, pp, axes,
-                                  _p(ax), tp, width, pool_p, pages, rows, _dev(logits, "f32", B * c["vocab"], "logits", True),
+    _check(lib().spd_decode_paged(model.handle, _dev(x, "bf16", n * c["d_model"], "x"), n, _hp(cu), _hp(ln), _hp(pre), B, pp, axes,
+                                  _hp(ax), tp, width, pool_p, pages, rows, _dev(logits, "f32", B * c["vocab"], "logits", True),
                                   wp, wb, _stream(stream)))
 
 
