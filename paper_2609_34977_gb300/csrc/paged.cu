@@ -61,6 +61,7 @@ struct PagedArgs {
   float scale_log2;
   __nv_bfloat16* o;
   float* lse;
+  bool whole;                        // a CTA has one unit (block0: a sequence's first), not an equal stretch of all blocks
   int total, ctas, warps;            // blocks; CTAs; quarters of the tile (32 rows) that have rows
   float* part_o;                     // [2 ctas][rows_part HD] states of parts: slot 2 c of the part that goes on with a unit (CTA
   float2* part_ml;                   // c), 2 c + 1 of the one that begins one; [2 ctas][rows_part] maximum (log2 units) and sum
@@ -152,14 +153,34 @@ struct Place {
     blocks = blocks_at(sq.s[e], tile / p.chunks * p.tokens, p.tokens, p.keys);
     hi = min(blocks, lo + left);
   }
-  // The unit of block `at` of the list (a whole warp, all lanes with the same arguments).
-  __device__ __forceinline__ void seek(const PagedArgs& p, const PagedSeqs& sq, int at, int n) {
+  // CTA c's stretch (a whole warp, all lanes with the same arguments); its number of blocks.
+  __device__ __forceinline__ int begin(const PagedArgs& p, const PagedSeqs& sq, int c) {
+    if (!p.whole) {
+      const int at = first_block(p, c);
+      seek(p, sq, at, first_block(p, c + 1) - at);
+      return left;
+    }
+    find(sq, c);
+    tile = c - sq.s[e].block0;
+    hk = int(uint32_t(tile) / uint32_t(sq.s[e].tiles));
+    tile -= hk * sq.s[e].tiles;
+    lo = 0;
+    left = 1 << 30;
+    size(p, sq);
+    return left = blocks;
+  }
+  // The last sequence that begins at or before `at`.
+  __device__ __forceinline__ void find(const PagedSeqs& sq, int at) {
     e = 0;
     for (int top = sq.n; top - e > 1;) {
       const int mid = (e + top) >> 1;
       if (sq.s[mid].block0 <= at) e = mid;
       else top = mid;
     }
+  }
+  // The unit of block `at` of the list, `n` blocks from there on.
+  __device__ __forceinline__ void seek(const PagedArgs& p, const PagedSeqs& sq, int at, int n) {
+    find(sq, at);
     const PagedSeq& s = sq.s[e];
     lo = at - s.block0;
     hk = int(uint32_t(lo) / uint32_t(s.head_blocks));
@@ -274,10 +295,9 @@ __global__ void __launch_bounds__(kThreads, 2)
     return;
   }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int first = first_block(p, blockIdx.x), count = first_block(p, blockIdx.x + 1) - first;
   const int nw = p.warps;
   Place at;
-  at.seek(p, sq, first, count);
+  const int count = at.begin(p, sq, int(blockIdx.x));
   if (threadIdx.x == 0) {
     for (int s = 0; s < NS; ++s) {
       mbar_init(&k_full[s], 1);
@@ -794,9 +814,8 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
     return;
   }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int first = first_block(p, blockIdx.x), count = first_block(p, blockIdx.x + 1) - first;
   Place at;
-  at.seek(p, sq, first, count);
+  const int count = at.begin(p, sq, int(blockIdx.x));
   if (threadIdx.x == 0) {
     for (int s = 0; s < NS; ++s) {
       mbar_init(&k_full[s], 1);
@@ -1326,7 +1345,7 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
     for (int next = 0; next < n_seqs;) {
       PagedSeqs sq;
       sq.n = 0;
-      long long total = 0;
+      long long total = 0, units = 0;
       int most = 0, longest = 0;
       double pairs = 0.0, keys = 0.0, tokens = 0.0;
       for (; next < n_seqs && sq.n < kMaxSeqs; ++next) {
@@ -1343,6 +1362,7 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
         total += blocks * n_kv_heads;
         if (total > 0x3fffffff) return fail(SPD_EUNSUPPORTED, "paged attention of more than 2^30 blocks of keys");
         s.head_blocks = int(blocks);
+        units += (long long)s.tiles * n_kv_heads;
         most = std::max(most, n);
         keys += len[b];
         tokens += n;
@@ -1354,7 +1374,20 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
         mapped = true;
       }
       p.total = int(total);
-      p.ctas = int(std::min<long long>(token ? sms : 2 * sms, total));
+      const int places = token ? sms : 2 * sms;
+      p.ctas = int(std::min<long long>(places, total));
+      // Parts of units are written, read and joined, at the price of some blocks a CTA, of more the more CTAs do so at once. One unit
+      // a CTA and equal stretches: 700 tokens of 32 heads of 128 (192 units of 2 to 11 blocks) 26 and 33 us, 18 tokens over 400 rows of
+      // 28 heads on 4 (4 units of 7) 16.0 and 11.5, 32 sequences of 4 over 1500 rows (128 units of 24) 39.9 and 32.9.
+      p.whole = !token && units <= places && longest <= total / p.ctas + 3 + 10 * units / places;
+      if (p.whole) {
+        p.ctas = int(units);
+        int first = 0;
+        for (int e = 0; e < sq.n; ++e) {
+          sq.s[e].block0 = first;
+          first += sq.s[e].tiles * n_kv_heads;
+        }
+      }
       p.by_row = token || std::min(most, p.tokens) * p.chunk <= kMergeRows;
       p.warps = (std::min(most, p.tokens) * p.chunk + 31) / 32;
       const double fl = 4.0 * head_dim * n_heads * pairs;
@@ -1374,7 +1407,7 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
         return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
       }));
       SPD_CUDA_TRY(launch_pdl(kernel, dim3(p.ctas), dim3(token ? kTokenThreads : kThreads), smem, st, map, p, sq));
-      if (p.ctas > 1) {
+      if (p.ctas > 1 && !p.whole) {
         if (p.by_row) {
           const int parts = int((long long)longest * p.ctas / total) + 2;  // of a unit, at most
           const int rows_unit = std::min(most, p.tokens) * p.chunk;
