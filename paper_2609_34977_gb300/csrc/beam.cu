@@ -9,8 +9,9 @@
 // exponentials a thread, and those tokens that beat the n_out-th best so far go to a list in shared memory, which is cut back to
 // n_out when it has doubled. The first bound: of n_out or more groups of threads the least of their maxima. Where more tokens beat
 // the bound than the list holds (rising or equal logits) the batch's n_out best are taken one by one.
-// A warp a request then takes the best of the lists' heads n_out times. Candidates of different beams may lie closer together than
-// fp32 tells, and fp64 is slow here, so totals are pairs of fp32 values (a sum and what it was rounded by).
+// A CTA a request then takes the n_out lists of the best heads, and of their candidates that are not behind the last of these heads the
+// n_out best, by counting how many go before each. Candidates of different beams may lie closer together than fp32 tells, and fp64
+// is slow here, so totals are pairs of fp32 values (a sum and what it was rounded by).
 #include <math.h>
 #include <stdint.h>
 
@@ -303,25 +304,31 @@ __device__ __forceinline__ uint32_t order_of(float x) {
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float order_value(uint32_t u) { return __uint_as_float((u >> 31) ? u & 0x7fffffffu : ~u); }
-// A candidate's total as integers of the same order (the pair's values), where the beam's logits are added to `norm`; .x 0: none.
-__device__ __forceinline__ uint2 total_of(float2 norm, float z) {
+// A candidate's total as an integer of the same order (the pair's values), where the beam's logits are added to `norm`; 0: none.
+using Total = unsigned long long;
+__device__ __forceinline__ Total total_of(float2 norm, float z) {
   const float2 s = add_pair(norm, z);
-  return isfinite(s.x) ? make_uint2(order_of(s.x), order_of(s.y)) : make_uint2(0u, 0u);
+  return isfinite(s.x) ? (Total(order_of(s.x)) << 32) | order_of(s.y) : 0;
 }
-__device__ __forceinline__ bool more(uint2 a, uint2 b) { return a.x != b.x ? a.x > b.x : a.y > b.y; }
+// Whether candidate i of total a goes before candidate j of total b: lists ascend in beam and slice, and in a list equal totals in
+// their tokens, so places tell the order of equals. (No branches: 64 of them in a row are 4500 cycles.)
+__device__ __forceinline__ int before(Total a, int i, Total b, int j) { return int(a > b) | (int(a == b) & int(i < j)); }
 
 __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const __grid_constant__ BeamArgs p) {
   __shared__ float2 norm[kMaxBeams];  // what a beam's logits are added to: score - log sum; NaN where it offers nothing
-  __shared__ uint2 ends[kMaxBeams], got[kMaxBeams];
-  __shared__ int got_at[kMaxBeams];
-  extern __shared__ uint2 total[];    // [n_in * slices][n_out], then as many tokens, then the heads of the lists
+  __shared__ Total ends[kMaxBeams], front[kMaxBeams * kMaxBeams], last_total;
+  __shared__ int front_at[kMaxBeams * kMaxBeams], fronts, last_at;
+  extern __shared__ Total total[];    // [n_in * slices][n_out], then as many tokens
   const int req = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int lists = p.n_in * p.slices, K = p.n_out;
   int* token = reinterpret_cast<int*>(total + size_t(lists) * K);
-  uint8_t* head = reinterpret_cast<uint8_t*>(token + size_t(lists) * K);
-  for (int i = tid; i < lists; i += kMergeThreads) head[i] = 0;
   int stages = 1;  // of a sum over the slices
   while (stages < p.slices && stages < 32) stages *= 2;
+  if (tid == 0) {
+    fronts = 0;
+    last_total = 0;  // fewer lists than places: nothing is behind it
+    last_at = 0x7fffffff;
+  }
   pdl_launch_dependents();
   pdl_wait();
   const unsigned long long* best = p.best + size_t(req) * lists * K;
@@ -339,16 +346,17 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const __grid_
     for (int i = lane + 32; i < p.slices; i += 32) m = fmaxf(m, sums[i].x);
     for (int off = stages / 2; off; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
     auto part = [&](float2 s) { return s.x == -INFINITY ? s.y : s.y * expf(s.x - m); };
-    float2 l = make_float2(part(mine), 0.0f);
-    for (int i = lane + 32; i < p.slices; i += 32) l = add_pair(l, part(sums[i]));
-    for (int off = stages / 2; off; off >>= 1) {
-      const float2 o = make_float2(__shfl_xor_sync(0xffffffffu, l.x, off), __shfl_xor_sync(0xffffffffu, l.y, off));
-      l = add_pair(add_pair(l, o.x), o.y);
-    }
+    float2 l = make_float2(part(mine), 0.0f);  // a sum, and what it was rounded by
+    auto add = [&](float x, float y) {
+      const float2 t = two_sum(l.x, x);
+      l = make_float2(t.x, t.y + (l.y + y));
+    };
+    for (int i = lane + 32; i < p.slices; i += 32) add(part(sums[i]), 0.0f);
+    for (int off = stages / 2; off; off >>= 1) add(__shfl_xor_sync(0xffffffffu, l.x, off), __shfl_xor_sync(0xffffffffu, l.y, off));
     if (lane == 0) {
       const float2 g = log_pair(l.x);
       float2 c = add_pair(two_sum(score, -m), -g.x);
-      c = add_pair(c, -g.y - l.y / l.x);  // (l.y: what l.x was rounded by)
+      c = add_pair(c, -g.y - l.y / l.x);
       norm[w] = isfinite(c.x) && isfinite(c.y) ? c : make_float2(NAN, NAN);
       ends[w] = total_of(norm[w], end);
     }
@@ -356,71 +364,69 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const __grid_
   __syncthreads();
   for (int i = tid, u = 0; i < lists * K; i += kMergeThreads, ++u) {
     const unsigned long long key = u == 0 ? ahead[0] : u == 1 ? ahead[1] : best[i];
-    total[i] = key ? total_of(norm[i / (p.slices * K)], key_value(key)) : make_uint2(0u, 0u);
+    total[i] = key ? total_of(norm[i / (p.slices * K)], key_value(key)) : 0;
     token[i] = int(0xffffffffu - uint32_t(key));
   }
   __syncthreads();
-  if (warp > 0) return;
-  // The best head of the lane's lists. A lane's lists ascend in (beam, token), so the first of equals is the one that goes first.
-  uint2 mine;
-  int from = 0;  // its place
-  auto refresh = [&]() {
-    mine = make_uint2(0u, 0u);
-    for (int i = lane; i < lists; i += 32) {
-      const int k = head[i];
-      const uint2 c = k < K ? total[i * K + k] : make_uint2(0u, 0u);
-      if (more(c, mine)) {
-        mine = c;
-        from = i * K + k;
-      }
-    }
-  };
-  refresh();
-  for (int k = 0; k < K; ++k) {
-    const uint32_t hi = __reduce_max_sync(0xffffffffu, mine.x);
-    bool in = mine.x == hi;
-    const uint32_t lo = __reduce_max_sync(0xffffffffu, in ? mine.y : 0u);
-    in &= mine.y == lo;
-    uint32_t who = __ballot_sync(0xffffffffu, in);
-    // equal totals: the lowest list (beams, then slices) has the lowest beam and token
-    if (who & (who - 1)) {
-      const uint32_t first = __reduce_min_sync(0xffffffffu, in ? uint32_t(from) : ~0u);
-      who = __ballot_sync(0xffffffffu, in && uint32_t(from) == first);
-    }
-    const bool won = lane == __ffs(who) - 1;
-    if (won) {
-      got[k] = mine;
-      got_at[k] = from;
-      if (hi != 0) {
-        ++head[from / K];
-        refresh();
-      }
+  // the n_out-th best head: what goes behind it is not among the best
+  for (int i = tid; i < lists; i += kMergeThreads) {
+    const Total mine = total[i * K];
+    int first = 0;
+#pragma unroll 8
+    for (int j = 0; j < lists; ++j) first += before(total[j * K], j, mine, i);
+    if (first == K - 1) {
+      last_total = mine;
+      last_at = i * K;
     }
   }
-  __syncwarp();
-  for (int i = lane; i < K; i += 32) {
-    const uint2 c = got[i];
+  __syncthreads();
+  const Total last = last_total;
+  const int behind = last_at;
+  for (int i = tid; i < lists * K; i += kMergeThreads) {
+    const Total c = total[i];
+    if (c == 0 || before(last, behind, c, i)) continue;
+    const int at = atomicAdd(&fronts, 1);  // (of n_out lists, so at most n_out^2)
+    front[at] = c;
+    front_at[at] = i;
+  }
+  __syncthreads();
+  const int n = fronts;
+  for (int i = tid; i < n; i += kMergeThreads) {
+    const Total c = front[i];
+    const int from = front_at[i];
+    int first = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) first += before(front[j], front_at[j], c, from);
+    if (first >= K) continue;
+    const size_t at = size_t(req) * K + first;
+    p.parent[at] = req * p.n_in + from / (p.slices * K);
+    p.token[at] = token[from];
+    p.out[at] = order_value(uint32_t(c >> 32));
+  }
+  for (int i = n + tid; i < K; i += kMergeThreads) {
     const size_t at = size_t(req) * K + i;
-    p.parent[at] = c.x ? req * p.n_in + got_at[i] / (p.slices * K) : -1;
-    p.token[at] = c.x ? token[got_at[i]] : -1;
-    p.out[at] = c.x ? order_value(c.x) : -INFINITY;
+    p.parent[at] = p.token[at] = -1;
+    p.out[at] = -INFINITY;
   }
-  if (p.ended && lane < p.n_in) {
-    const uint2 e = ends[lane];
-    int first = 0;  // candidates that go before it
-    for (int k = 0; k < K; ++k) {
-      const uint2 c = got[k];
-      const int w = got_at[k] / (p.slices * K);
-      first += more(c, e) || (c.x == e.x && c.y == e.y && (w != lane ? w < lane : token[got_at[k]] < p.eos));
+  if (p.ended && tid >= kMergeThreads - p.n_in) {  // (other warps than those of the few fronts)
+    const int w = tid - (kMergeThreads - p.n_in), own = p.slices * K;
+    const Total e = ends[w];
+    int first = 0;  // candidates that go before it: were they n_out in all, those of the fronts are as many
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) {
+      const Total c = front[j];
+      const int at = front_at[j];
+      // of equal totals those of a lower beam, and of the beam's own the lower tokens
+      first += int(c > e) | (int(c == e) & (int(at < w * own) | (int(at < (w + 1) * own) & int(token[at] < p.eos))));
     }
-    for (int w = 0; w < p.n_in; ++w) first += more(ends[w], e) || (ends[w].x == e.x && ends[w].y == e.y && w < lane);
-    p.ended[size_t(req) * p.n_in + lane] = e.x && first < K ? order_value(e.x) : -INFINITY;
+    for (int v = 0; v < p.n_in; ++v) first += before(ends[v], v, e, w);
+    p.ended[size_t(req) * p.n_in + w] = e && first < K ? order_value(uint32_t(e >> 32)) : -INFINITY;
   }
 }
 
 // Slices a row: as many as fill the GPU (kCtasSm CTAs on each of 152 SMs), of a batch at least, whose lists a merging CTA can hold.
 int slices_of(int n_seqs, int n_in, int n_out, int vocab) {
-  const int most = std::min((vocab + kBatch - 1) / kBatch, kMergeBytes / (n_in * (12 * n_out + 1)));
+  const int most = std::min((vocab + kBatch - 1) / kBatch, kMergeBytes / (n_in * 12 * n_out));
   return std::max(1, std::min(most, kCtasSm * 152 / std::max(1, n_seqs * n_in)));
 }
 
@@ -471,7 +477,7 @@ extern "C" int spd_beam_select(const float* logits, int n_seqs, int n_in, int vo
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int slot = trace_begin(st);
   const bool vec = vocab % 4 == 0 && ld % 4 == 0 && (reinterpret_cast<uintptr_t>(logits) & 15) == 0;
-  const size_t smem = size_t(n_in) * p.slices * (12 * size_t(n_out) + 1);
+  const size_t smem = size_t(n_in) * p.slices * 12 * size_t(n_out);
   constexpr int kRing = kStages * kBatch * 4;
   static DeviceOnce once;
   SPD_CUDA_TRY(once_per_device(once, [] {
