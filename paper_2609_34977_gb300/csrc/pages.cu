@@ -356,6 +356,7 @@ __global__ void __launch_bounds__(kPageThreads, 1) pages_compact_kernel(const __
 
 // The rows of the copies of a list, in every layer. A page's rows lie side by side, so a copy is one stretch of bytes.
 constexpr int kCopyThreads = 256, kCopyDepth = 4, kCopyChunk = kCopyThreads * kCopyDepth;  // 16-byte pieces
+constexpr int kCopyCtas = 16;  // an SM, two waves
 __global__ void __launch_bounds__(kCopyThreads)
     pages_copy_kernel(uint4* pool, const PageCopy* copies, const int* n_copies, int n_layers, size_t layer16, size_t page16, int row16,
                       int chunks) {
@@ -381,11 +382,13 @@ __global__ void __launch_bounds__(kCopyThreads)
   }
 }
 
-int copy_pages(uint16_t* pool, const PageCopy* copies, const int* n, int n_layers, int n_pages, int page_size, int row16,
+// most: copies at most.
+int copy_pages(uint16_t* pool, const PageCopy* copies, const int* n, int most, int n_layers, int n_pages, int page_size, int row16,
                cudaStream_t st) {
   const size_t page16 = size_t(page_size) * row16;
   const int chunks = int((page16 + kCopyChunk - 1) / kCopyChunk);
-  SPD_CUDA_TRY(launch_pdl(pages_copy_kernel, dim3(8 * num_sms()), dim3(kCopyThreads), 0, st, reinterpret_cast<uint4*>(pool), copies, n,
+  const long long ctas = std::min((long long)kCopyCtas * num_sms(), (long long)most * n_layers * chunks);
+  SPD_CUDA_TRY(launch_pdl(pages_copy_kernel, dim3(unsigned(ctas)), dim3(kCopyThreads), 0, st, reinterpret_cast<uint4*>(pool), copies, n,
                           n_layers, page16 * n_pages, page16, row16, chunks));
   return SPD_OK;
 }
@@ -573,7 +576,7 @@ extern "C" int spd_pages_update(uint16_t* pool, int n_layers, int n_pages, int p
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int slot = trace_begin(st);
   SPD_CUDA_TRY(launch_pdl(pages_update_kernel, dim3(1), dim3(kPageThreads), shared ? smem : 0, st, p, shared));
-  const int rc = copy_pages(pool, w.copies, w.n_copies, n_layers, n_pages, page_size, n_kv_heads * head_dim / 4, st);
+  const int rc = copy_pages(pool, w.copies, w.n_copies, n_out, n_layers, n_pages, page_size, n_kv_heads * head_dim / 4, st);
   trace_end(slot, st, TR_ROWS, 0.0, 8.0 * n_pages + 4.0 * (double(n_in) + n_out) * max_pages);
   return rc;
 }
@@ -593,7 +596,7 @@ extern "C" int spd_pages_compact(uint16_t* pool, int n_layers, int n_pages, int 
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int slot = trace_begin(st);
   SPD_CUDA_TRY(launch_pdl(pages_compact_kernel, dim3(1), dim3(kPageThreads), 0, st, p));
-  const int rc = copy_pages(pool, w.copies, w.n_copies, n_layers, n_pages, page_size, n_kv_heads * head_dim / 4, st);
+  const int rc = copy_pages(pool, w.copies, w.n_copies, (n_pages + 1) / 2, n_layers, n_pages, page_size, n_kv_heads * head_dim / 4, st);
   trace_end(slot, st, TR_ROWS, 0.0, 8.0 * n_pages + 8.0 * double(n_seqs) * max_pages);
   return rc;
 }
