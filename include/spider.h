@@ -556,7 +556,8 @@ size_t spd_paged_attention_workspace_size(int n_q, int n_seqs, int n_heads, int 
  * another; HOST int32 [n_seqs] in [0, len[b]], NULL = none). Per head, head h reading K/V head h / (n_heads / n_kv_heads):
  *   o_i = sum_j softmax_j(q_i . k_j / sqrt(head_dim)) v_j,   lse_i = log sum_j exp(q_i . k_j / sqrt(head_dim)).
  * What a row does not see contributes nothing, whatever it holds. NaN in a query or in a key that is seen gives NaN; an infinite V
- * that is seen gives the infinity (perhaps NaN where its weight is below 2^-100 of the row's largest).
+ * that is seen gives the infinity (perhaps NaN where its weight is below 2^-100 of the row's largest). Where all scores of a row are
+ * -inf o is 0 and lse -inf. Weights of up to 2^8 are multiplied with V and added up in fp32: V above 2^100 may overflow.
  * q, o (dev) bf16 [n_q][n_heads * head_dim]; lse (dev) fp32 [n_q][n_heads], natural logarithm, may be NULL; pool: the layer's block.
  * The same bits in every run. q, o, pool and ws 16-byte aligned.
  * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ENOSPC, SPD_ECUDA; device timeouts in the workspace's status word. */
@@ -615,7 +616,7 @@ size_t spd_beam_select_workspace_size(int n_seqs, int n_in, int n_out, int vocab
  *   total(w, t) = scores[b][w] + z[t] - log sum_u exp z[u],   t != eos (eos -1: none), z[t] above -inf,
  * the n_out largest, ties to the lower beam, then to the lower token (totals are held in 48 bits): parent (dev) int32 [n_seqs][n_out] receives
  * b * n_in + w, as spd_pages_update takes it, token (dev) int32 the token, scores_out (dev) fp32 the total; -1, -1 and -inf where there
- * are fewer. A beam whose score is not finite, or whose logits hold NaN, +inf or nothing above -inf, offers nothing.
+ * are fewer; scores_out may be scores where n_in is n_out. A beam whose score is not finite, or whose logits hold NaN, +inf or nothing above -inf, offers nothing.
  * ended (dev, may be NULL) fp32 [n_seqs][n_in]: total(w, eos) where fewer than n_out candidates of the request go before it, the ends of
  * other beams counted, else -inf. n_in and n_out up to 32, up to 65535 beams in all; ws 16-byte aligned. The same result in every run.
  * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ENOSPC, SPD_ECUDA; device timeouts in the workspace's status word. */

@@ -450,6 +450,7 @@ extern "C" int spd_beam_select(const float* logits, int n_seqs, int n_in, int vo
   if (!logits || !scores || !parent || !token || !scores_out || !ws || n_seqs < 1 || n_in < 1 || n_out < 1 || vocab < 1 || ld < vocab)
     return fail(SPD_EINVAL, "bad beam arguments");
   if (n_in > kMaxBeams || n_out > kMaxBeams) return fail(SPD_EUNSUPPORTED, "more than %d beams", kMaxBeams);
+  if (vocab > 1 << 30) return fail(SPD_EUNSUPPORTED, "vocabulary of %d tokens", vocab);
   if ((long long)n_seqs * n_in > 65535) return fail(SPD_EUNSUPPORTED, "more than 65535 beams in all");
   if (eos < -1 || eos >= vocab) return fail(SPD_EINVAL, "eos outside the vocabulary (-1: none)");
   if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(SPD_EINVAL, "ws must be 16-byte aligned");

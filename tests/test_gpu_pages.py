@@ -235,6 +235,11 @@ def _check(q, pool, table, new, lens, g, m, d, prefix, o, ls):
     (1, 200, 64, [3], [70], 32, None),                            # more heads a group than a tile has rows
     (3, 1, 64, [300], [1111], 16 * 7, None),                      # a page that is no power of two
     (1, 28, 128, [17], [400], 64, None),
+    (32, 1, 128, [256], [256], 64, None),                         # a unit a CTA
+    (32, 2, 64, [100], [130], 32, [50]),
+    (2, 16, 64, [1, 1, 3], [129, 1, 700], 16, None),              # single tokens beside others
+    (2, 9, 128, [1, 1, 1], [128, 127, 300], 16, [0, 100, 300]),   # (a prefix tells a last token nothing)
+    (1, 17, 128, [1], [500], 16, None),                           # one head too many for the single tokens' form
 ])
 def test_attention(g, m, d, new, lens, page, prefix):
     q, pool, table = _case(5, g, m, d, new, lens, page)
@@ -309,6 +314,45 @@ def test_values_that_are_not_finite_show_only_where_they_are_seen(new, ln, prefi
             other = torch.arange(d) != 5
             assert torch.equal(hit[..., other.cuda()], ref[sees, 1][..., other.cuda()])
             assert (torch.isnan if what == "nan_v" else torch.isinf)(hit[..., 5]).all()
+
+
+def test_pools_of_more_than_two_to_the_32_elements():
+    # rows at element offsets past 2^32: written, read and copied there
+    h, g, d, page = 32, 32, 128, 64
+    pages = (1 << 32) // (page * 2 * g * d) + 40
+    pool = torch.full((1, pages, page, 2 * g * d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    new, lens = [100, 130], [100, 130]
+    table = np.array([[pages - 1, 3, -1, -1], [pages - 20, pages - 7, 1, -1]], np.int32)
+    fill, q = _rand((230, 2 * g * d), 1), _rand((230, h * d), 2, 2.0)
+    pos, turned = torch.zeros(1, 230, dtype=torch.int32, device="cuda"), torch.empty(230, h * d, dtype=torch.bfloat16, device="cuda")
+    N.spd_rope_pages(q.cuda(), fill.cuda(), pos, None, 1e4, _cu(new), lens, _i32(table), pool[0], h, g, d, turned)
+    assert torch.equal(turned.cpu(), q)  # position 0 turns nothing
+    for b, n in enumerate(lens):
+        rows = torch.from_numpy(_rows(table[b], page, 0, n)).cuda()
+        assert torch.equal(pool.view(-1, 2 * g * d)[rows].cpu(), fill[100 * b:100 * b + n])
+    small = torch.cat([fill[:100], torch.zeros(28, 2 * g * d).bfloat16(), fill[100:], torch.zeros(62, 2 * g * d).bfloat16()])
+    near = np.array([[0, 1, -1], [2, 3, 4]], np.int32)
+    for k in ([100, 130], [1, 1]):  # tiles, and the single tokens' form
+        sub = torch.cat([q[100 - k[0]:100], q[230 - k[1]:]])
+        ws = torch.zeros(N.spd_paged_attention_workspace_size(sum(k), 2, h, g, d), dtype=torch.uint8, device="cuda")
+        o = torch.empty(sum(k), h * d, dtype=torch.bfloat16, device="cuda")
+        N.spd_paged_attention(sub.cuda(), _cu(k), lens, _i32(table), pool[0], h, g, d, o, None, ws)
+        want, _ = _attend(sub, small.view(5, page, 2 * g * d), near, k, lens, h, 1, d)
+        assert torch.equal(o, want) and N.spd_workspace_status(ws) == 0
+    ref = np.ones(pages, np.int32)  # everything is held but three pages at the end, and the tables' pages by their tables
+    ref[[pages - 2, pages - 3, pages - 4]] = 0
+    r, t, _, status = _run_update(pool, ref, table, lens, [0, 0, 1], [1, 1, 0], g, d)
+    assert status == 0 and t[1, 1] == pages - 4 and t[0, 1] == 3
+    assert torch.equal(pool[0, pages - 4, :36].cpu(), fill[64:100])
+    compacted, used = _i32(table), _i32([0])
+    live = np.zeros(pages, np.int32)
+    live[table[table >= 0]] = 1
+    ws = torch.zeros(N.spd_pages_workspace_size(pages, 2), dtype=torch.uint8, device="cuda")
+    N.spd_pages_compact(pool, g, d, _i32(live), compacted, _i32(live), compacted, used, ws)
+    assert int(used) == 5 and compacted.max() < 5
+    for b, n in enumerate(lens):
+        rows = torch.from_numpy(_rows(compacted.cpu().numpy()[b], page, 0, n)).cuda()
+        assert torch.equal(pool.view(-1, 2 * g * d)[rows].cpu(), fill[100 * b:100 * b + n])
 
 
 def test_two_streams_and_a_graph():
