@@ -62,7 +62,9 @@ struct PagedArgs {
   __nv_bfloat16* o;
   float* lse;
   bool whole;                        // a CTA has one unit (block0: a sequence's first), not an equal stretch of all blocks
-  int total, ctas, warps;            // blocks; CTAs; quarters of the tile (32 rows) that have rows
+  int box_rows;                      // tokens that a load of Q brings
+  int total, ctas, share, more;      // stretches of share blocks, the first `more` of one more
+  int warps;                         // of 32 rows of the tile
   float* part_o;                     // [2 ctas][rows_part HD] states of parts: slot 2 c of the part that goes on with a unit (CTA
   float2* part_ml;                   // c), 2 c + 1 of the one that begins one; [2 ctas][rows_part] maximum (log2 units) and sum
   int rows_part;
@@ -143,7 +145,13 @@ __host__ __device__ __forceinline__ int blocks_at(const PagedSeq& s, int i, int 
   return int(uint32_t(limit_of(s, last - 1) + keys - 1) / uint32_t(keys));
 }
 // First block of CTA c's stretch.
-__device__ __forceinline__ int first_block(const PagedArgs& p, int c) { return int((long long)c * p.total / p.ctas); }
+__device__ __forceinline__ int first_block(const PagedArgs& p, int c) { return c * p.share + min(c, p.more); }
+// CTAs whose stretches begin before block `at`.
+__device__ __forceinline__ int ctas_before(const PagedArgs& p, int at) {
+  const int wide = p.more * (p.share + 1);  // blocks of the stretches of one more
+  return at <= wide ? int((uint32_t(at) + uint32_t(p.share)) / uint32_t(p.share + 1))
+                    : p.more + int((uint32_t(at - wide) + uint32_t(p.share) - 1u) / uint32_t(p.share));
+}
 
 // A CTA's place in the list of blocks: the unit (sequence e, K/V head hk, tile), its blocks, and the stretch's blocks lo .. hi - 1
 // of them.
@@ -271,7 +279,8 @@ __device__ __forceinline__ int pool_row(const PagedArgs& p, int seq, int key) {
 
 template <int HD>
 __global__ void __launch_bounds__(kThreads, 2)
-    paged_attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ PagedArgs p,
+    paged_attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ CUtensorMap map_q,
+                      const __grid_constant__ PagedArgs p,
                       const __grid_constant__ PagedSeqs sq) {
   using L = PagedSmem<HD>;
   constexpr int NS = L::kStages, NV = L::kStagesV, NB = L::kBufs;
@@ -281,7 +290,8 @@ __global__ void __launch_bounds__(kThreads, 2)
   uint64_t* v_full = k_empty + NS;                                 // [NV] V block landed
   uint64_t* v_empty = v_full + NV;                                 // [NV] its PV products have completed
   uint64_t* q_full = v_empty + NV;   // a unit's Q tile is in shared memory
-  uint64_t* s_full = q_full + 1;     // [NB] S of block j is in TMEM buffer j % NB
+  uint64_t* q_empty = q_full + 1;    // its S products have completed
+  uint64_t* s_full = q_empty + 1;    // [NB] S of block j is in TMEM buffer j % NB
   uint64_t* p_full = s_full + NB;    // [NB] P of block j written and O rescaled
   uint64_t* o_done = p_full + NB;    // [NB] PV products of block j completed
   uint64_t* drain = o_done + NB;     // every MMA completed
@@ -307,7 +317,8 @@ __global__ void __launch_bounds__(kThreads, 2)
       mbar_init(&v_full[s], 1);
       mbar_init(&v_empty[s], 1);
     }
-    mbar_init(q_full, 2 * nw);
+    mbar_init(q_full, 1);
+    mbar_init(q_empty, 1);
     for (int s = 0; s < NB; ++s) {
       mbar_init(&s_full[s], 1);
       mbar_init(&p_full[s], 2 * nw);  // one arrival per softmax warp
@@ -318,6 +329,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     *odd_v = 0;
     fence_mbar_init();
     prefetch_tmap(&map_kv);
+    prefetch_tmap(&map_q);
   }
   if (warp == 8) {
     tmem_alloc(tmem_slot, kTmemCols);
@@ -333,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, 2)
   pdl_wait();
   if (threadIdx.x == 0) stamp_start(p.stamp);
 
-  int issued_k = 0, issued_v = 0;
+  int issued_q = 0, issued_k = 0, issued_v = 0;
   if (warp == 8) {
     // ---- TMA producer ----
     const uint64_t pol = policy_evict_last();
@@ -342,6 +354,17 @@ __global__ void __launch_bounds__(kThreads, 2)
     bool ok = true;
     do {
       const PagedSeq& s = sq.s[at.e];
+      {  // the tile's rows: `chunk` heads of a token side by side
+        if (issued_q > 0 && !(ok = __all_sync(0xffffffffu, mbar_wait(q_empty, (issued_q - 1) & 1, abort_flag, p.budget)))) break;
+        if (lane == 0) {
+          mbar_arrive_expect_tx(q_full, uint32_t(L::kChunks * 128 * p.chunk * p.box_rows));
+          const int across = at.tile / p.chunks, h0 = (at.tile - across * p.chunks) * p.chunk;
+          for (int c = 0; c < L::kChunks; ++c)
+            tma_load_3d(smem + L::q + c * kQBox, &map_q, q_full, c * 64, at.hk * p.group + h0, s.q0 + across * p.tokens, pol);
+        }
+        __syncwarp();
+        ++issued_q;
+      }
       const int t = at.tile / p.chunks * p.tokens, limit = limit_of(s, min(s.n, t + p.tokens) - 1);
       auto row_at = [&](int blk) {  // of the lane's box; -1: none of its rows is seen
         const int key = blk * kTK + lane * p.box;
@@ -405,6 +428,7 @@ __global__ void __launch_bounds__(kThreads, 2)
             issue_ss(t_all + kTK * (js % NB), dq + (((kk >> 2) * kQBox + (kk & 3) * 32) >> 4),
                      dk + (((kk >> 2) * kKBox + (kk & 3) * 32) >> 4), id_s, kk > 0);
           issue_commit(&s_full[js % NB]);
+          if (js + 1 == unit_end) issue_commit(q_empty);
           if (HD != 128) issue_commit(&k_empty[s]);
           ++js;
           did = true;
@@ -475,28 +499,13 @@ __global__ void __launch_bounds__(kThreads, 2)
       w.row = (size_t(s.q0) + w.token) * p.n_heads + u.hk * p.group + h0 + min(hc, heads - 1);
       return w;
     };
-    auto load_q = [&](const Row& w) {  // in the 128-byte swizzle: 16-byte piece j of row r at j ^ (r % 8)
-      const uint4* src = reinterpret_cast<const uint4*>(p.q + w.row * HD) + half * (HD / 16);
-      uint4 v[HD / 16];
-#pragma unroll
-      for (int j = 0; j < HD / 16; ++j) v[j] = src[j];
-#pragma unroll
-      for (int j = 0; j < HD / 16; ++j) {
-        const int piece = half * (HD / 16) + j;
-        *reinterpret_cast<uint4*>(smem + L::q + (piece >> 3) * kQBox + r * 128 + (((piece & 7) ^ (r & 7)) << 4)) = v[j];
-      }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(q_full);
-    };
     bool ok = true;
     int j = 0;  // block of the CTA
-    Row row = row_of(at);
-    load_q(row);
     for (int unit = 0;; ++unit) {
       const PagedSeq& s = sq.s[at.e];
+      const Row now = row_of(at);
       const int n0 = at.tile / p.chunks * p.tokens;
-      const int lim = limit_of(s, row.token);                            // what the row sees,
+      const int lim = limit_of(s, now.token);                            // what the row sees,
       const int lim_all = limit_of(s, n0), lim_any = limit_of(s, min(s.n, n0 + p.tokens) - 1);  // every row, some row
       float m_run = -INFINITY, l_run = 0.0f;  // the row's reference (raw scores); the thread's sum of weights
       for (int blk = at.lo; blk < at.hi; ++blk, ++j) {
@@ -506,19 +515,15 @@ __global__ void __launch_bounds__(kThreads, 2)
         if (partly) {
           ok = ok && mbar_wait(&v_full[j % NV], (j / NV) & 1, abort_flag, p.budget);
           bool odd = false;
-          for (int x = tid; x < kTK * L::kChunks; x += T) {
-            if (kb + x % kTK < lim_all) continue;
-            uint4* vr = reinterpret_cast<uint4*>(smem + L::v + (j % NV) * L::kChunks * kKBox + x * 128);
-            bool here = false;
-#pragma unroll 2
-            for (int y = 0; y < 8; ++y) {
-              const int at_piece = (y + x) & 7;  // (rows begin at the same bank)
-              uint4 w = vr[at_piece];
-              const bool some = not_finite(w.x) || not_finite(w.y) || not_finite(w.z) || not_finite(w.w);
-              if (some) vr[at_piece] = make_uint4(finite_of(w.x), finite_of(w.y), finite_of(w.z), finite_of(w.w));
-              here |= some;
+          for (int x = tid; x < kTK * L::kChunks * 8; x += T) {  // 16 bytes each
+            const int key = kb + (x >> 3) % kTK;
+            if (key < lim_all) continue;
+            uint4* at_v = reinterpret_cast<uint4*>(smem + L::v + (j % NV) * L::kChunks * kKBox) + x;
+            const uint4 w = *at_v;
+            if (not_finite(w.x) || not_finite(w.y) || not_finite(w.z) || not_finite(w.w)) {
+              *at_v = make_uint4(finite_of(w.x), finite_of(w.y), finite_of(w.z), finite_of(w.w));
+              odd |= key < lim_any;
             }
-            odd |= here && kb + x % kTK < lim_any;
           }
           if (odd) atomicMax(odd_v, unit + 1);
           fence_proxy_async_smem();
@@ -539,7 +544,7 @@ __global__ void __launch_bounds__(kThreads, 2)
 #pragma unroll
         for (int i = 4; i < kTK / 2; ++i) m4[i & 3] = fmaxf(m4[i & 3], v[i]);
         const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-        if (any_pair(blk == at.lo || (mx - m_run) * p.scale_log2 > kGrown || !ok)) {
+        if (any_pair(blk == at.lo || (now.valid && (mx - m_run) * p.scale_log2 > kGrown) || !ok)) {
           // the references are taken anew. O can be rescaled once the products before have completed
           if (blk > at.lo) ok = ok && mbar_wait(&o_done[(j - 1) % NB], ((j - 1) / NB) & 1, abort_flag, p.budget);
           if (any_pair(!ok)) {
@@ -601,14 +606,6 @@ __global__ void __launch_bounds__(kThreads, 2)
         if (lane == 0) mbar_arrive(&p_full[j % NB]);
       }
       if (!ok) break;
-      // the next unit's Q goes in while the last products run (their S has been read, so Q is free)
-      Place then = at;
-      const bool more = then.next(p, sq);
-      const Row now = row;
-      if (more) {
-        row = row_of(then);
-        load_q(row);
-      }
       ok = mbar_wait(&o_done[(j - 1) % NB], ((j - 1) / NB) & 1, abort_flag, p.budget);
       if (any_pair(!ok)) {
         ok = false;
@@ -622,10 +619,10 @@ __global__ void __launch_bounds__(kThreads, 2)
       float sick = 0.0f;  // NaN where a column is not finite
 #pragma unroll 1
       for (int c = 0; c < HC; c += 32) {
-        float ov[32];
-        tmem_ld32(t_oh + c, ov);
+        float v[32];
+        tmem_ld32(t_oh + c, v);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) sick = fmaf(ov[i], 0.0f, sick);
+        for (int i = 0; i < 32; ++i) sick = fmaf(v[i], 0.0f, sick);
       }
       const int key0 = at.lo * kTK, key1 = min(at.hi * kTK, lim_any);
       const __nv_bfloat16* vcol = p.pool + (size_t(p.n_kv_heads) + at.hk) * HD + half * HC;
@@ -688,43 +685,36 @@ __global__ void __launch_bounds__(kThreads, 2)
           tmem_st_wait();
         }
       }
-      const float m2 = m_run * p.scale_log2;
-      if (at.hi - at.lo < at.blocks) {
-        const size_t slot = (2 * size_t(blockIdx.x) + (at.lo == 0)) * p.rows_part + r;
-        if (now.valid && !half) p.part_ml[slot] = make_float2(m2, l_run);
-        // [HD / 4][rows_part][4]: the rows of a warp side by side; few rows: [rows_part][HD]
-        float4* po = reinterpret_cast<float4*>(p.part_o) + (p.by_row ? slot * (HD / 4) : (slot - r) * (HD / 4) + r);
-        const int step = p.by_row ? 1 : p.rows_part;
+      // the outputs, or the part's state
+      const bool part = at.hi - at.lo < at.blocks;
+      const size_t slot = (2 * size_t(blockIdx.x) + (at.lo == 0)) * p.rows_part + r;
+      const float m2 = m_run * p.scale_log2, inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
+      if (now.valid && !half) {
+        if (part) p.part_ml[slot] = make_float2(m2, l_run);
+        else if (p.lse) p.lse[now.row] = fmaf(m2, 0.6931471805599453f, logf(l_run));
+      }
 #pragma unroll 1
-        for (int c = 0; c < HC; c += 32) {
-          float v[32];
-          tmem_ld32(t_oh + c, v);
-          if (now.valid) {
+      for (int c = 0; c < HC; c += 32) {
+        float v[32];
+        tmem_ld32(t_oh + c, v);
+        if (!now.valid) continue;
+        if (part) {
+          // [HD / 4][rows_part][4]: the rows of a warp side by side; few rows: [rows_part][HD]
+          float4* po = reinterpret_cast<float4*>(p.part_o) + (p.by_row ? slot * (HD / 4) : (slot - r) * (HD / 4) + r);
+          const int step = p.by_row ? 1 : p.rows_part;
 #pragma unroll
-            for (int y = 0; y < 8; ++y)
-              po[((half * HC + c) / 4 + y) * step] = make_float4(v[4 * y], v[4 * y + 1], v[4 * y + 2], v[4 * y + 3]);
-          }
-        }
-      } else {
-        const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
-        __nv_bfloat16* orow = p.o + now.row * HD + half * HC;
-        if (now.valid && !half && p.lse) p.lse[now.row] = fmaf(m2, 0.6931471805599453f, logf(l_run));
-#pragma unroll 1
-        for (int c = 0; c < HC; c += 32) {
-          float v[32];
-          tmem_ld32(t_oh + c, v);
-          if (now.valid) {
+          for (int y = 0; y < 8; ++y)
+            po[((half * HC + c) / 4 + y) * step] = make_float4(v[4 * y], v[4 * y + 1], v[4 * y + 2], v[4 * y + 3]);
+        } else {
+          uint4* to = reinterpret_cast<uint4*>(p.o + now.row * HD + half * HC + c);
 #pragma unroll
-            for (int y = 0; y < 4; ++y)
-              reinterpret_cast<uint4*>(orow + c)[y] =
-                  make_uint4(pack_bf16(v[8 * y] * inv, v[8 * y + 1] * inv), pack_bf16(v[8 * y + 2] * inv, v[8 * y + 3] * inv),
-                             pack_bf16(v[8 * y + 4] * inv, v[8 * y + 5] * inv), pack_bf16(v[8 * y + 6] * inv, v[8 * y + 7] * inv));
-          }
+          for (int y = 0; y < 4; ++y)
+            to[y] = make_uint4(pack_bf16(v[8 * y] * inv, v[8 * y + 1] * inv), pack_bf16(v[8 * y + 2] * inv, v[8 * y + 3] * inv),
+                               pack_bf16(v[8 * y + 4] * inv, v[8 * y + 5] * inv), pack_bf16(v[8 * y + 6] * inv, v[8 * y + 7] * inv));
         }
       }
       tc_fence_before();  // (O is written again by products that wait for this warp's next arrival)
-      if (!more) break;
-      at = then;
+      if (!at.next(p, sq)) break;
     }
     if (!ok) {
       *abort_flag = 1;
@@ -736,6 +726,7 @@ __global__ void __launch_bounds__(kThreads, 2)
   if (threadIdx.x == 256 && *abort_flag) {
     // loads issued but never consumed land before the CTA exits
     volatile int no_abort = 0;
+    if (issued_q > 0) mbar_wait(q_full, (issued_q - 1) & 1, &no_abort, p.budget);
     for (int j = max(0, issued_k - NS); j < issued_k; ++j) mbar_wait(&k_full[j % NS], (j / NS) & 1, &no_abort, p.budget);
     for (int j = max(0, issued_v - NV); j < issued_v; ++j) mbar_wait(&v_full[j % NV], (j / NV) & 1, &no_abort, p.budget);
   }
@@ -789,8 +780,8 @@ __device__ __forceinline__ float order_value(uint32_t u) { return __uint_as_floa
 // R: heads a thread works on, 8 or 16 (those past the group's are of zeros and are not stored).
 template <int HD, int R>
 __global__ void __launch_bounds__(kTokenThreads, 1)
-    paged_token_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ PagedArgs p,
-                       const __grid_constant__ PagedSeqs sq) {
+    paged_token_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ CUtensorMap,
+                       const __grid_constant__ PagedArgs p, const __grid_constant__ PagedSeqs sq) {
   using L = TokenSmem<HD>;
   constexpr int NS = L::kStages, NC = L::kChunks;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -1158,7 +1149,7 @@ struct Split {
     u.seek(p, sq, border, 1);
     const int start = border - u.lo;
     mine = u.lo > 0 && first_block(p, c) <= start;
-    parts = int(((long long)(start + u.blocks) * p.ctas + p.total - 1) / p.total) - c;
+    parts = ctas_before(p, start + u.blocks) - c;
   }
   __device__ __forceinline__ size_t slot(int part) const { return 2 * size_t(c + part) + (part == 0); }
 };
@@ -1307,7 +1298,7 @@ size_t paged_attention_bytes(int n_q, int n_heads, int n_kv_heads, int head_dim)
 int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, const int32_t* prefix, int n_seqs,
                         const int32_t* table, int max_pages, const void* pool, int n_pages, int page_size, int n_heads,
                         int n_kv_heads, int head_dim, void* o, float* lse, void* ws, size_t ws_bytes, int* status, cudaStream_t st) {
-  const int kvd = n_kv_heads * head_dim;
+  const int kvd = n_kv_heads * head_dim, n_q = q_cu[n_seqs];
   PagedArgs p{};
   p.q = static_cast<const __nv_bfloat16*>(q);
   p.pool = static_cast<const __nv_bfloat16*>(pool);
@@ -1322,7 +1313,7 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
   p.o = static_cast<__nv_bfloat16*>(o);
   p.lse = lse;
   Carve cv(ws, ws_bytes);
-  p.rows_part = rows_of_part(q_cu[n_seqs], n_heads, n_kv_heads);
+  p.rows_part = rows_of_part(n_q, n_heads, n_kv_heads);
   const size_t rows = 2 * size_t(kCtas) * p.rows_part;
   p.part_o = cv.take<float>(rows * head_dim);
   p.part_ml = cv.take<float2>(rows);
@@ -1340,7 +1331,8 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
     p.tokens = token ? 1 : 128 / p.chunk;
     p.box = p.keys;
     while (page_size % p.box) p.box /= 2;  // (pages are multiples of 16 rows)
-    CUtensorMap map;
+    p.box_rows = std::min(p.tokens, n_q);
+    CUtensorMap map_kv, map_q;
     bool mapped = false;
     for (int next = 0; next < n_seqs;) {
       PagedSeqs sq;
@@ -1370,7 +1362,9 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
       }
       if (sq.n == 0) continue;
       if (!mapped) {
-        if (int rc = make_operand_map(&map, pool, 2 * kvd, n_pages * page_size, p.box)) return rc;
+        if (int rc = make_operand_map(&map_kv, pool, 2 * kvd, n_pages * page_size, p.box)) return rc;
+        if (token) map_q = map_kv;  // (not used)
+        else if (int rc = make_heads_map(&map_q, q, head_dim, n_heads, n_q, p.chunk, p.box_rows)) return rc;
         mapped = true;
       }
       p.total = int(total);
@@ -1388,13 +1382,15 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
           first += sq.s[e].tiles * n_kv_heads;
         }
       }
+      p.share = p.total / p.ctas;
+      p.more = p.total - p.share * p.ctas;
       p.by_row = token || std::min(most, p.tokens) * p.chunk <= kMergeRows;
       p.warps = (std::min(most, p.tokens) * p.chunk + 31) / 32;
       const double fl = 4.0 * head_dim * n_heads * pairs;
       const double by = 4.0 * kvd * keys + 4.0 * n_heads * head_dim * tokens;
       p.stamp = stamp_slot(TR_ATTN, fl, by);
       const int slot = trace_begin(st);
-      using Kernel = void (*)(CUtensorMap, PagedArgs, PagedSeqs);
+      using Kernel = void (*)(CUtensorMap, CUtensorMap, PagedArgs, PagedSeqs);
       static constexpr Kernel kernels[6] = {paged_token_kernel<64, 8>,   paged_token_kernel<128, 8>, paged_token_kernel<64, 16>,
                                             paged_token_kernel<128, 16>, paged_attn_kernel<64>,      paged_attn_kernel<128>};
       static constexpr uint32_t bytes[6] = {TokenSmem<64>::bytes,  TokenSmem<128>::bytes, TokenSmem<64>::bytes,
@@ -1406,7 +1402,7 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
       SPD_CUDA_TRY(once_per_device(attr[which], [&] {
         return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
       }));
-      SPD_CUDA_TRY(launch_pdl(kernel, dim3(p.ctas), dim3(token ? kTokenThreads : kThreads), smem, st, map, p, sq));
+      SPD_CUDA_TRY(launch_pdl(kernel, dim3(p.ctas), dim3(token ? kTokenThreads : kThreads), smem, st, map_kv, map_q, p, sq));
       if (p.ctas > 1 && !p.whole) {
         if (p.by_row) {
           const int parts = int((long long)longest * p.ctas / total) + 2;  // of a unit, at most
