@@ -12,8 +12,7 @@
 //   warp 9     MMA issuer: S = Q K^T into TMEM, then O += P V with P read from TMEM, V in place as an MN-major operand, each
 //              as its operands come
 //   warps 0-7  two threads a row, half of the block's 64 scores each: online softmax in fp32; a weight is held as the sum of
-//              three bf16 terms, all 24 bits of it: two over the scores in TMEM, where O leaves no room for more, the third in
-//              shared memory
+//              two bf16 terms, 16 bits of it, both over the scores in TMEM
 // Only blocks that reach past the first token's limit are masked; there the softmax warps also clear the values of V that are
 // not finite (recycled memory behind the sequence among them), which a weight of zero would turn into NaN for rows that do not
 // see them; rows that do see one add it at the end.
@@ -35,7 +34,7 @@ constexpr int kTK = 64;                // keys a block
 constexpr uint32_t kQBox = 128 * 128;  // 64 columns of the Q tile
 constexpr uint32_t kKBox = kTK * 128;  // 64 columns of a block of K or V
 constexpr int kThreads = 320;
-constexpr uint32_t kTmemCols = 256;    // S: 256 / HD + 1, at most three buffers of 64 columns less what O takes behind them
+constexpr uint32_t kTmemCols = 256;    // two buffers of S (64 columns) and 128 of O, or three and 64: half of an SM's 512
 constexpr int kCtas = 304;             // CTAs that fill the GPU: two on each of 152 SMs
 // The reference that a row's exponentials are taken against is renewed once its maximum has grown by this much (log2
 // units): weights stay below 2^8, their terms and the fp32 sums are relative to them, and almost no block pays for the
@@ -74,25 +73,24 @@ struct PagedArgs {
   unsigned long long* stamp;
 };
 
-// The third terms of a block's weights, [128][64], take the place of its K, which has been read when they are written (heads of
-// 128: the same 16 KB), or one of three places of their own: they need not wait for the products of the block before.
+// Two terms a weight leave 2^-16 of it out, 1/256 of the step that the bf16 outputs are rounded by, and the sum of weights that
+// divides them and gives lse is of the whole weights in fp32. A third term, as single tokens have it, is a third more products and
+// needs shared memory that K or V then lack: 2048 tokens behind 14000, 28 heads of 128: 547 us, with two 449; 16 of 64: 260, 218.
+// One term would be as coarse as the outputs.
 template <int HD>
 struct PagedSmem {
   static constexpr int kChunks = HD / 64;
-  static constexpr uint32_t third = 128 * 128;
   static constexpr int kBufs = HD == 128 ? 2 : 3;      // of S in TMEM, behind them O
   static constexpr int kStages = 3;                    // of K
   static constexpr int kStagesV = HD == 128 ? 2 : 3;
   static constexpr uint32_t q = 0;
   static constexpr uint32_t k = q + kChunks * kQBox;
   static constexpr uint32_t v = k + kStages * kChunks * kKBox;
-  static constexpr uint32_t p3 = v + kStagesV * kChunks * kKBox;
-  static constexpr uint32_t bars = p3 + (HD == 128 ? 0 : kBufs * third);
+  static constexpr uint32_t bars = v + kStagesV * kChunks * kKBox;
   static constexpr uint32_t red = bars + 256;    // [128] what the two threads of a row tell each other
   static constexpr uint32_t bytes = red + 512;   // (two CTAs an SM: at most 113 KB)
   static_assert(bytes <= 113 * 1024, "two CTAs an SM");
-  static_assert(HD != 128 || kChunks * kKBox == third, "third terms in a block's K");
-  __device__ static uint32_t third_at(int j) { return HD == 128 ? k + (j % kStages) * third : p3 + (j % kBufs) * third; }
+  static_assert(8 * (2 * kStages + 2 * kStagesV + 2 + 3 * kBufs + 1) + 12 <= red - bars, "room for the barriers");
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -286,7 +284,7 @@ __global__ void __launch_bounds__(kThreads, 2)
   constexpr int NS = L::kStages, NV = L::kStagesV, NB = L::kBufs;
   extern __shared__ __align__(1024) uint8_t smem[];  // (the swizzle's atoms; no room to round the address up)
   uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + L::bars);  // [NS] K block landed
-  uint64_t* k_empty = k_full + NS;                                 // [NS] its S product (third terms in it: its PV products) completed
+  uint64_t* k_empty = k_full + NS;                                 // [NS] its S product has completed
   uint64_t* v_full = k_empty + NS;                                 // [NV] V block landed
   uint64_t* v_empty = v_full + NV;                                 // [NV] its PV products have completed
   uint64_t* q_full = v_empty + NV;   // a unit's Q tile is in shared memory
@@ -429,7 +427,7 @@ __global__ void __launch_bounds__(kThreads, 2)
                      dk + (((kk >> 2) * kKBox + (kk & 3) * 32) >> 4), id_s, kk > 0);
           issue_commit(&s_full[js % NB]);
           if (js + 1 == unit_end) issue_commit(q_empty);
-          if (HD != 128) issue_commit(&k_empty[s]);
+          issue_commit(&k_empty[s]);
           ++js;
           did = true;
         }
@@ -443,17 +441,14 @@ __global__ void __launch_bounds__(kThreads, 2)
         }
         tc_fence_after();
         const uint32_t t_ov = t_all + NB * kTK, t_p = t_all + kTK * (jp % NB);
-        const uint64_t dv = sdesc_mn128(base + L::v + s * L::kChunks * kKBox, kKBox), dp = sdesc_k128(base + L::third_at(jp));
+        const uint64_t dv = sdesc_mn128(base + L::v + s * L::kChunks * kKBox, kKBox);
 #pragma unroll
         for (int kk = 0; kk < 2 * (kTK / 16); ++kk) {  // the weights' first terms, then their second, then their third
           const int k = kk % (kTK / 16), term = kk / (kTK / 16);
           issue_ts(t_ov, t_p + 16 * k + 8 * term, dv + ((k * 2048) >> 4), id_o, jp > pv_begin || kk > 0);
         }
-#pragma unroll
-        for (int k = 0; k < kTK / 16; ++k) issue_ss(t_ov, dp + ((k * 32) >> 4), dv + ((k * 2048) >> 4), id_o, true);
         issue_commit(&o_done[jp % NB]);
         issue_commit(&v_empty[s]);
-        if (HD == 128) issue_commit(&k_empty[jp % NS]);
         ++jp;
         did = true;
       }
@@ -544,14 +539,16 @@ __global__ void __launch_bounds__(kThreads, 2)
 #pragma unroll
         for (int i = 4; i < kTK / 2; ++i) m4[i & 3] = fmaxf(m4[i & 3], v[i]);
         const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-        if (any_pair(blk == at.lo || (now.valid && (mx - m_run) * p.scale_log2 > kGrown) || !ok)) {
+        if (any_pair(blk == at.lo || (mx - m_run) * p.scale_log2 > kGrown || !ok)) {
           // the references are taken anew. O can be rescaled once the products before have completed
           if (blk > at.lo) ok = ok && mbar_wait(&o_done[(j - 1) % NB], ((j - 1) / NB) & 1, abort_flag, p.budget);
           if (any_pair(!ok)) {
             ok = false;
             break;
           }
-          const float m_new = fmaxf(m_run, share(mx, true));
+          // (a row whose maximum has not grown keeps its reference: its bits do not hang on its neighbours' values)
+          const float most = share(mx, true);
+          const float m_new = blk == at.lo || (most - m_run) * p.scale_log2 > kGrown ? fmaxf(m_run, most) : m_run;
           const float corr = m_new == m_run ? 1.0f : ex2((m_run - m_new) * p.scale_log2);
           m_run = m_new;
           l_run *= corr;
@@ -575,7 +572,6 @@ __global__ void __launch_bounds__(kThreads, 2)
 #pragma unroll
         for (int x = 0; x < kTK / 32; ++x) {
           float first_t[8], second_t[8];  // the terms of keys 16 x + 2 i and 16 x + 2 i + 1 of the half in word i
-          uint32_t third[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int k = 16 * x + 2 * i;
@@ -587,19 +583,11 @@ __global__ void __launch_bounds__(kThreads, 2)
             const uint32_t mid = pack_bf16(w.lo, w.hi);
             first_t[i] = __uint_as_float(hi);
             second_t[i] = __uint_as_float(mid);
-            w = fma2(two_of(mid), minus, w);
-            third[i] = pack_bf16(w.lo, w.hi);
           }
           tmem_st8(t_s + 16 * x, first_t);  // over the scores
           tmem_st8(t_s + 16 * x + 8, second_t);
-          uint8_t* to = smem + L::third_at(j) + r * 128;
-#pragma unroll
-          for (int y = 0; y < 2; ++y)
-            *reinterpret_cast<uint4*>(to + (((half * 4 + 2 * x + y) ^ (r & 7)) << 4)) =
-                make_uint4(third[4 * y], third[4 * y + 1], third[4 * y + 2], third[4 * y + 3]);
         }
         l_run += (sum[0].lo + sum[0].hi) + (sum[1].lo + sum[1].hi);
-        fence_proxy_async_smem();
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -760,6 +748,7 @@ struct TokenSmem {
   static constexpr uint32_t red = bars + 320;                 // [4 warps][16]
   static constexpr uint32_t bytes = red + 256;
   static_assert(bytes <= 227 * 1024, "one CTA an SM");
+  static_assert(8 * (4 * kStages + 9) + 8 <= red - bars, "room for the barriers");
 };
 __device__ __forceinline__ void sync_softmax() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
 __device__ __forceinline__ bool any_softmax(bool mine) {

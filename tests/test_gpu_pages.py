@@ -172,7 +172,8 @@ def _plain_rows(q, kv, limit, g, m, d):
         lse[:, h] = top[:, 0] + np.log(w.sum(1))
         p = w / w.sum(1, keepdims=True)
         o[:, sl] = p @ V
-        tol_o[:, sl] = 2.0 ** -8 * np.abs(o[:, sl]) + (2 * e_s + 2.0 ** -18)[:, None] * (p @ np.abs(V))
+        # a weight w is held as t + u, t = bf16(w), u = bf16(w - t): |w - t| <= 2^-8 w, |w - t - u| <= 2^-8 |w - t| <= 2^-16 w
+        tol_o[:, sl] = 2.0 ** -8 * np.abs(o[:, sl]) + (2 * e_s + 2.0 ** -16 + 2.0 ** -18)[:, None] * (p @ np.abs(V))
         tol_l[:, h] = e_s + 2.0 ** -20 + 2.0 ** -22 * np.abs(lse[:, h])
     return o, lse, tol_o, tol_l
 
