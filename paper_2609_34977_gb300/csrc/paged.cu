@@ -1359,10 +1359,13 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
       p.total = int(total);
       const int places = token ? sms : 2 * sms;
       p.ctas = int(std::min<long long>(places, total));
-      // Parts of units are written, read and joined, at the price of some blocks a CTA, of more the more CTAs do so at once. One unit
-      // a CTA and equal stretches: 700 tokens of 32 heads of 128 (192 units of 2 to 11 blocks) 26 and 33 us, 18 tokens over 400 rows of
-      // 28 heads on 4 (4 units of 7) 16.0 and 11.5, 32 sequences of 4 over 1500 rows (128 units of 24) 39.9 and 32.9.
-      p.whole = !token && units <= places && longest <= total / p.ctas + 3 + 10 * units / places;
+      // Parts of units are written, read and joined, at the price of a launch and some blocks a CTA, of more the more CTAs do so at
+      // once. One unit a CTA and equal stretches: 700 tokens of 32 heads of 128 (192 units of 2 to 11 blocks) 26 and 33 us, 18 tokens
+      // over 400 rows of 28 heads on 4 (4 units of 7) 16.0 and 11.5, 32 sequences of 4 over 1500 rows (128 units of 24) 39.9 and 32.9.
+      // Single tokens: over 200 rows of 32 heads (32 units of 2) 6.4 and 7.2, 350 (of 3) 7.9 and 7.6 and 3 us less for the host, 700
+      // (of 6) 12.4 and 9.0; 4 sequences over 1100 (128 units of 9, 7.6 a CTA) 17.8 and 19.7, of 2000 (of 16, 13.5) 29.3 and 29.1.
+      p.whole = units <= places && (token ? longest <= 3 || 2 * longest <= 2 * total / p.ctas + 3
+                                          : longest <= total / p.ctas + 3 + 10 * units / places);
       if (p.whole) {
         p.ctas = int(units);
         int first = 0;
