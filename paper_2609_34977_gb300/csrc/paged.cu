@@ -8,11 +8,10 @@
 // sees, in blocks of 64. All blocks of a launch form one list, unit after unit, and every CTA takes an equal stretch of it,
 // whole units and parts of two: no CTA waits for a longest sequence, and 1.5 tiles a CTA cost 1.5 tiles. Parts of a unit leave
 // states (m, l, O) in fp32, which paged_merge_kernel joins in the order of the keys (the same bits in every run).
-//   warp 8     TMA producer: K and V blocks into rings, a lane a box of rows that lie in one page
-//   warp 9     MMA issuer: S = Q K^T into TMEM, then O += P V with P read from TMEM, V in place as an MN-major operand, each
-//              as its operands come
-//   warps 0-7  two threads a row, half of the block's 64 scores each: online softmax in fp32; a weight is held as the sum of
-//              two bf16 terms, 16 bits of it, both over the scores in TMEM
+//   warps 0-3  a thread a row: online softmax in fp32; a weight is held as the sum of two bf16 terms, 16 bits of it, both over
+//              the scores in TMEM
+//   warp 4     TMA producer: Q, and K and V blocks into rings, a lane a box of rows that lie in one page
+//   warps 5, 6 MMA issuers: S = Q K^T into TMEM; O += P V with P read from TMEM, V in place as an MN-major operand
 // Only blocks that reach past the first token's limit are masked; there the softmax warps also clear the values of V that are
 // not finite (recycled memory behind the sequence among them), which a weight of zero would turn into NaN for rows that do not
 // see them; rows that do see one add it at the end.
@@ -33,7 +32,7 @@ constexpr int kMaxSeqs = 112;          // sequences whose sizes fit in a launch'
 constexpr int kTK = 64;                // keys a block
 constexpr uint32_t kQBox = 128 * 128;  // 64 columns of the Q tile
 constexpr uint32_t kKBox = kTK * 128;  // 64 columns of a block of K or V
-constexpr int kThreads = 320;
+constexpr int kThreads = 224;
 constexpr uint32_t kTmemCols = 256;    // two buffers of S (64 columns) and 128 of O, or three and 64: half of an SM's 512
 constexpr int kCtas = 304;             // CTAs that fill the GPU: two on each of 152 SMs
 // The reference that a row's exponentials are taken against is renewed once its maximum has grown by this much (log2
@@ -87,10 +86,9 @@ struct PagedSmem {
   static constexpr uint32_t k = q + kChunks * kQBox;
   static constexpr uint32_t v = k + kStages * kChunks * kKBox;
   static constexpr uint32_t bars = v + kStagesV * kChunks * kKBox;
-  static constexpr uint32_t red = bars + 256;    // [128] what the two threads of a row tell each other
-  static constexpr uint32_t bytes = red + 512;   // (two CTAs an SM: at most 113 KB)
+  static constexpr uint32_t bytes = bars + 256;  // (two CTAs an SM: at most 113 KB)
   static_assert(bytes <= 113 * 1024, "two CTAs an SM");
-  static_assert(8 * (2 * kStages + 2 * kStagesV + 2 + 3 * kBufs + 1) + 12 <= red - bars, "room for the barriers");
+  static_assert(8 * (2 * kStages + 2 * kStagesV + 2 + 3 * kBufs + 1) + 12 <= bytes - bars, "room for the barriers");
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -253,18 +251,6 @@ __device__ __forceinline__ void issue_commit(uint64_t* bar) {
 // A value that all lanes hold, in a uniform register.
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_max_sync(0xffffffffu, x); }
 
-// Barriers of the two warps that have the same rows.
-__device__ __forceinline__ void pair_sync(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
-__device__ __forceinline__ bool pair_or(int id, bool mine) {
-  uint32_t all;
-  asm volatile(
-      "{\n\t.reg .pred a, b;\n\tsetp.ne.u32 a, %1, 0;\n\tbarrier.cta.red.or.pred b, %2, 64, a;\n\tselp.u32 %0, 1, 0, b;\n\t}"
-      : "=r"(all)
-      : "r"(uint32_t(mine)), "r"(id)
-      : "memory");
-  return all != 0;
-}
-
 // Row of the pool that holds row `key` of a sequence; behind the pool (loads there read zeros) where its page is none.
 __device__ __forceinline__ int pool_row(const PagedArgs& p, int seq, int key) {
   const int k = int(uint32_t(key) / uint32_t(p.page_size)), page = p.table[size_t(seq) * p.max_pages + k];
@@ -319,17 +305,17 @@ __global__ void __launch_bounds__(kThreads, 2)
     mbar_init(q_empty, 1);
     for (int s = 0; s < NB; ++s) {
       mbar_init(&s_full[s], 1);
-      mbar_init(&p_full[s], 2 * nw);  // one arrival per softmax warp
+      mbar_init(&p_full[s], nw);  // one arrival per softmax warp
       mbar_init(&o_done[s], 1);
     }
-    mbar_init(drain, 1);
+    mbar_init(drain, 2);
     *abort_flag = 0;
     *odd_v = 0;
     fence_mbar_init();
     prefetch_tmap(&map_kv);
     prefetch_tmap(&map_q);
   }
-  if (warp == 8) {
+  if (warp == 4) {
     tmem_alloc(tmem_slot, kTmemCols);
     tmem_relinquish();
   }
@@ -344,7 +330,7 @@ __global__ void __launch_bounds__(kThreads, 2)
   if (threadIdx.x == 0) stamp_start(p.stamp);
 
   int issued_q = 0, issued_k = 0, issued_v = 0;
-  if (warp == 8) {
+  if (warp == 4) {
     // ---- TMA producer ----
     const uint64_t pol = policy_evict_last();
     const int boxes = kTK / p.box;
@@ -393,67 +379,69 @@ __global__ void __launch_bounds__(kThreads, 2)
       *abort_flag = 1;
       set_status(p.status, SPD_ETIMEOUT);
     }
-  } else if (warp == 9) {
-    // ---- MMA issuer (all lanes in step) ----
-    const uint32_t id_s = idesc_bf16_f32(128, kTK);
-    const uint32_t id_o = idesc_bf16_f32(128, HD) | (1u << 16);  // V is MN-major
+  } else if (warp == 5 || warp == 6) {
+    // ---- MMA issuers, all lanes in step: warp 5 the scores, warp 6 the products with V ----
+    // Their loops are short because a block's instructions here are on its critical path: even lanes watch one of the two
+    // barriers that a block waits for, odd lanes the other.
     const uint32_t base = smem_u32(smem), t_all = uniform(tmem);
     const int blocks = int(uniform(uint32_t(count)));
-    auto ready = [&](uint64_t* bar, int phase) { return __all_sync(0xffffffffu, mbar_test(bar, phase & 1)) != 0; };
-    // Blocks in order, S and PV as their operands come: S of block js where K and Q are there and the S buffer is free (the PV
-    // products of block js - NB completed), PV of block jp where V and P are there.
-    int js = 0, jp = 0, unit = 0, unit_end = at.hi - at.lo;  // js's unit, and the first block behind it
-    int pv_begin = 0, pv_end = unit_end;                     // jp's unit
-    Place pv = at;
-    bool q_there = false, ok = true;
-    long long since = clock64();
-    while (jp < blocks && ok) {
-      bool did = false;
-      if (js < blocks) {
-        if (js == unit_end) {
+    const bool odd = lane & 1;
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, p.budget)) != 0; };
+    int stage = 0, buf = 0;              // of K or V, of S and P
+    uint32_t round = 0, buf_round = 0;   // parity of their rounds
+    int unit_end = at.hi - at.lo;        // the first block behind the unit
+    bool ok = true, first = true;        // of the unit
+    if (warp == 5) {
+      constexpr uint32_t id_s = idesc_bf16_f32(128, kTK);
+      uint32_t q_round = 0;
+      for (int j = 0; j < blocks; ++j) {
+        if (first) {
+          if (!(ok = wait(q_full, q_round))) break;
+          q_round ^= 1;
+          first = false;
+        }
+        // (the buffer's last P has been multiplied; none before the first round, whose parity a new barrier has completed)
+        if (!(ok = wait(odd ? &o_done[buf] : &k_full[stage], odd ? buf_round ^ 1 : round))) break;
+        tc_fence_after();
+        const uint64_t dk = sdesc_k128(base + L::k + stage * L::kChunks * kKBox), dq = sdesc_k128(base + L::q);
+#pragma unroll
+        for (int kk = 0; kk < HD / 16; ++kk)
+          issue_ss(t_all + kTK * buf, dq + (((kk >> 2) * kQBox + (kk & 3) * 32) >> 4),
+                   dk + (((kk >> 2) * kKBox + (kk & 3) * 32) >> 4), id_s, kk > 0);
+        issue_commit(&s_full[buf]);
+        issue_commit(&k_empty[stage]);
+        if (++stage == NS) stage = 0, round ^= 1;
+        if (++buf == NB) buf = 0, buf_round ^= 1;
+        if (j + 1 == unit_end) {
+          issue_commit(q_empty);
           at.next(p, sq);
           unit_end += at.hi - at.lo;
-          ++unit;
-          q_there = false;
-        }
-        if (!q_there) q_there = ready(q_full, unit);
-        const int s = js % NS;
-        if (q_there && (js < NB || ready(&o_done[js % NB], js / NB - 1)) && ready(&k_full[s], js / NS)) {
-          tc_fence_after();
-          const uint64_t dk = sdesc_k128(base + L::k + s * L::kChunks * kKBox), dq = sdesc_k128(base + L::q);
-#pragma unroll
-          for (int kk = 0; kk < HD / 16; ++kk)
-            issue_ss(t_all + kTK * (js % NB), dq + (((kk >> 2) * kQBox + (kk & 3) * 32) >> 4),
-                     dk + (((kk >> 2) * kKBox + (kk & 3) * 32) >> 4), id_s, kk > 0);
-          issue_commit(&s_full[js % NB]);
-          if (js + 1 == unit_end) issue_commit(q_empty);
-          issue_commit(&k_empty[s]);
-          ++js;
-          did = true;
+          first = true;
         }
       }
-      const int s = jp % NV;
-      if (jp < js && ready(&p_full[jp % NB], jp / NB) && ready(&v_full[s], jp / NV)) {
-        if (jp == pv_end) {
-          pv.next(p, sq);
-          pv_begin = pv_end;
-          pv_end += pv.hi - pv.lo;
-        }
+    } else {
+      constexpr uint32_t id_o = idesc_bf16_f32(128, HD) | (1u << 16);  // V is MN-major
+      for (int j = 0; j < blocks; ++j) {
+        if (!(ok = wait(odd ? &p_full[buf] : &v_full[stage], odd ? buf_round : round))) break;
         tc_fence_after();
-        const uint32_t t_ov = t_all + NB * kTK, t_p = t_all + kTK * (jp % NB);
-        const uint64_t dv = sdesc_mn128(base + L::v + s * L::kChunks * kKBox, kKBox);
+        const uint32_t t_o_all = t_all + NB * kTK, t_p = t_all + kTK * buf;
+        const uint64_t dv = sdesc_mn128(base + L::v + stage * L::kChunks * kKBox, kKBox);
 #pragma unroll
-        for (int kk = 0; kk < 2 * (kTK / 16); ++kk) {  // the weights' first terms, then their second, then their third
+        for (int kk = 0; kk < 2 * (kTK / 16); ++kk) {  // the weights' first terms, then their second
           const int k = kk % (kTK / 16), term = kk / (kTK / 16);
-          issue_ts(t_ov, t_p + 16 * k + 8 * term, dv + ((k * 2048) >> 4), id_o, jp > pv_begin || kk > 0);
+          issue_ts(t_o_all, t_p + 16 * k + 8 * term, dv + ((k * 2048) >> 4), id_o, !first || kk > 0);
         }
-        issue_commit(&o_done[jp % NB]);
-        issue_commit(&v_empty[s]);
-        ++jp;
-        did = true;
+        issue_commit(&o_done[buf]);
+        issue_commit(&v_empty[stage]);
+        first = false;
+        if (++stage == NV) stage = 0, round ^= 1;
+        if (++buf == NB) buf = 0, buf_round ^= 1;
+        if (j + 1 == unit_end) {
+          at.next(p, sq);
+          unit_end += at.hi - at.lo;
+          first = true;
+        }
       }
-      if (did) since = clock64();
-      else ok = __all_sync(0xffffffffu, !*abort_flag && clock64() - since <= p.budget);
     }
     if (!ok) {
       *abort_flag = 1;
@@ -462,22 +450,12 @@ __global__ void __launch_bounds__(kThreads, 2)
     issue_commit(drain);  // arrives once every MMA issued above has completed
     volatile int no_abort = 0;
     if (!mbar_wait(drain, 0, &no_abort, p.budget)) set_status(p.status, SPD_ETIMEOUT);
-  } else if ((warp & 3) < nw) {
-    // ---- softmax: warps w and w + 4 read TMEM lanes [32 w, 32 w + 32), of S, O and P half of the columns each ----
-    // A wait that gives up must not part the two, which meet at barriers: it ends the loop for both at the next.
-    const int quad = warp & 3, half = warp >> 2, r = quad * 32 + lane, T = nw * 64, tid = half * (nw * 32) + r;
-    const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16;
-    constexpr int HC = HD / 2;  // columns of O a thread
-    const uint32_t t_oh = t_o + lanes + half * HC;
-    float* red = reinterpret_cast<float*>(smem + L::red) + r;
-    auto any_pair = [&](bool mine) { return pair_or(quad + 1, mine); };
-    auto share = [&](float mine, bool most) {  // the larger or the sum of the two threads' values, for both
-      if (half) *red = mine;
-      pair_sync(quad + 1);
-      if (!half) *red = mine = most ? fmaxf(mine, *red) : mine + *red;
-      pair_sync(quad + 1);
-      return half ? *red : mine;
-    };
+  } else if (warp < nw) {
+    // ---- softmax: warp w has TMEM lanes [32 w, 32 w + 32) of S, P and O ----
+    const int r = threadIdx.x, T = nw * 32;
+    const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
+      const uint32_t t_oh = t_o + lanes;
+    auto any = [](bool mine) { return __any_sync(0xffffffffu, mine) != 0; };
     // a unit's rows: the thread's token, head and query row
     struct Row {
       int token;
@@ -504,13 +482,13 @@ __global__ void __launch_bounds__(kThreads, 2)
       const int lim_all = limit_of(s, n0), lim_any = limit_of(s, min(s.n, n0 + p.tokens) - 1);  // every row, some row
       float m_run = -INFINITY, l_run = 0.0f;  // the row's reference (raw scores); the thread's sum of weights
       for (int blk = at.lo; blk < at.hi; ++blk, ++j) {
-        const uint32_t t_s = tmem + kTK * (j % NB) + lanes + half * (kTK / 2);
+        const uint32_t t_s = tmem + kTK * (j % NB) + lanes;
         const int kb = blk * kTK;
         const bool partly = kb + kTK > lim_all;  // the block holds keys that not every row sees, or none at all
         if (partly) {
           ok = ok && mbar_wait(&v_full[j % NV], (j / NV) & 1, abort_flag, p.budget);
           bool odd = false;
-          for (int x = tid; x < kTK * L::kChunks * 8; x += T) {  // 16 bytes each
+          for (int x = r; x < kTK * L::kChunks * 8; x += T) {  // 16 bytes each
             const int key = kb + (x >> 3) % kTK;
             if (key < lim_all) continue;
             uint4* at_v = reinterpret_cast<uint4*>(smem + L::v + (j % NV) * L::kChunks * kKBox) + x;
@@ -527,28 +505,27 @@ __global__ void __launch_bounds__(kThreads, 2)
         ok = ok && mbar_wait(&s_full[j % NB], (j / NB) & 1, abort_flag, p.budget);
         __syncwarp();
         tc_fence_after();
-        float v[kTK / 2];
-        tmem_ld32(t_s, v);
+        float v[kTK];
+        tmem_ld64(t_s, v);
         if (partly) {
-          const int sees = lim - kb - half * (kTK / 2);
+          const int sees = lim - kb;
 #pragma unroll
-          for (int i = 0; i < kTK / 2; ++i)
+          for (int i = 0; i < kTK; ++i)
             if (i >= sees) v[i] = -INFINITY;
         }
         float m4[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-        for (int i = 4; i < kTK / 2; ++i) m4[i & 3] = fmaxf(m4[i & 3], v[i]);
+        for (int i = 4; i < kTK; ++i) m4[i & 3] = fmaxf(m4[i & 3], v[i]);
         const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-        if (any_pair(blk == at.lo || (mx - m_run) * p.scale_log2 > kGrown || !ok)) {
+        if (any(blk == at.lo || (mx - m_run) * p.scale_log2 > kGrown || !ok)) {
           // the references are taken anew. O can be rescaled once the products before have completed
           if (blk > at.lo) ok = ok && mbar_wait(&o_done[(j - 1) % NB], ((j - 1) / NB) & 1, abort_flag, p.budget);
-          if (any_pair(!ok)) {
+          if (any(!ok)) {
             ok = false;
             break;
           }
           // (a row whose maximum has not grown keeps its reference: its bits do not hang on its neighbours' values)
-          const float most = share(mx, true);
-          const float m_new = blk == at.lo || (most - m_run) * p.scale_log2 > kGrown ? fmaxf(m_run, most) : m_run;
+          const float m_new = blk == at.lo || (mx - m_run) * p.scale_log2 > kGrown ? fmaxf(m_run, mx) : m_run;
           const float corr = m_new == m_run ? 1.0f : ex2((m_run - m_new) * p.scale_log2);
           m_run = m_new;
           l_run *= corr;
@@ -556,7 +533,7 @@ __global__ void __launch_bounds__(kThreads, 2)
             __syncwarp();
             tc_fence_after();
 #pragma unroll 1
-            for (int c = 0; c < HC; c += 8) {
+            for (int c = 0; c < HD; c += 8) {
               float ov[8];
               tmem_ld8(t_oh + c, ov);
 #pragma unroll
@@ -570,8 +547,8 @@ __global__ void __launch_bounds__(kThreads, 2)
         const Two scale{p.scale_log2, p.scale_log2}, less{-off, -off}, minus{-1.0f, -1.0f};
         Two sum[2] = {Two{0.0f, 0.0f}, Two{0.0f, 0.0f}};
 #pragma unroll
-        for (int x = 0; x < kTK / 32; ++x) {
-          float first_t[8], second_t[8];  // the terms of keys 16 x + 2 i and 16 x + 2 i + 1 of the half in word i
+        for (int x = 0; x < kTK / 16; ++x) {
+          float first_t[8], second_t[8];  // the terms of keys 16 x + 2 i and 16 x + 2 i + 1 in word i
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int k = 16 * x + 2 * i;
@@ -595,30 +572,29 @@ __global__ void __launch_bounds__(kThreads, 2)
       }
       if (!ok) break;
       ok = mbar_wait(&o_done[(j - 1) % NB], ((j - 1) / NB) & 1, abort_flag, p.budget);
-      if (any_pair(!ok)) {
+      if (any(!ok)) {
         ok = false;
         break;
       }
-      l_run = share(l_run, false);
       __syncwarp();
       tc_fence_after();
       // A V that every row sees and that is infinite: the products of a weight's terms, which can be 0 or negative, are NaN
       // together. Which infinity a column has is the same for every row (each has a weight above 0 for it).
       float sick = 0.0f;  // NaN where a column is not finite
 #pragma unroll 1
-      for (int c = 0; c < HC; c += 32) {
+      for (int c = 0; c < HD; c += 32) {
         float v[32];
         tmem_ld32(t_oh + c, v);
 #pragma unroll
         for (int i = 0; i < 32; ++i) sick = fmaf(v[i], 0.0f, sick);
       }
       const int key0 = at.lo * kTK, key1 = min(at.hi * kTK, lim_any);
-      const __nv_bfloat16* vcol = p.pool + (size_t(p.n_kv_heads) + at.hk) * HD + half * HC;
+      const __nv_bfloat16* vcol = p.pool + (size_t(p.n_kv_heads) + at.hk) * HD;
       const size_t ld = 2 * size_t(p.n_kv_heads) * HD;
       const int rows_all = p.n_pages * p.page_size;
       const bool mend = now.valid && isnan(sick) && !isnan(l_run);  // (scores that are NaN leave the row NaN)
       if (__any_sync(0xffffffffu, mend)) {
-        constexpr int E = HC / 32;  // columns a lane looks through
+        constexpr int E = HD / 32;  // columns a lane looks through
         uint32_t has = 0;  // of column e in bits 4 e: +inf, -inf, NaN
         for (int k = key0; k < min(lim_all, key1); ++k) {
           const int at_row = pool_row(p, s.seq, k);
@@ -630,7 +606,7 @@ __global__ void __launch_bounds__(kThreads, 2)
           }
         }
 #pragma unroll 1
-        for (int c = 0; c < HC; c += 8) {
+        for (int c = 0; c < HD; c += 8) {
           float ov[8];
           tmem_ld8(t_oh + c, ov);
 #pragma unroll
@@ -653,14 +629,14 @@ __global__ void __launch_bounds__(kThreads, 2)
           const __nv_bfloat16* kr = p.pool + at_row * ld + at.hk * HD;
           const __nv_bfloat16* vr = vcol + at_row * ld;
           bool some = false;
-          for (int x = lane; x < HC; x += 32) some |= !isfinite(__bfloat162float(vr[x]));
+          for (int x = lane; x < HD; x += 32) some |= !isfinite(__bfloat162float(vr[x]));
           if (!__any_sync(0xffffffffu, some)) continue;
           float d = 0.0f;
           if (sees)
             for (int x = 0; x < HD; ++x) d = fmaf(__bfloat162float(qsrc[x]), __bfloat162float(kr[x]), d);
           const float w = ex2(fmaf(d, p.scale_log2, -off));
 #pragma unroll 1
-          for (int c = 0; c < HC; c += 8) {
+          for (int c = 0; c < HD; c += 8) {
             float ov[8];
             tmem_ld8(t_oh + c, ov);
 #pragma unroll
@@ -677,12 +653,12 @@ __global__ void __launch_bounds__(kThreads, 2)
       const bool part = at.hi - at.lo < at.blocks;
       const size_t slot = (2 * size_t(blockIdx.x) + (at.lo == 0)) * p.rows_part + r;
       const float m2 = m_run * p.scale_log2, inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
-      if (now.valid && !half) {
+      if (now.valid) {
         if (part) p.part_ml[slot] = make_float2(m2, l_run);
         else if (p.lse) p.lse[now.row] = fmaf(m2, 0.6931471805599453f, logf(l_run));
       }
 #pragma unroll 1
-      for (int c = 0; c < HC; c += 32) {
+      for (int c = 0; c < HD; c += 32) {
         float v[32];
         tmem_ld32(t_oh + c, v);
         if (!now.valid) continue;
@@ -692,9 +668,9 @@ __global__ void __launch_bounds__(kThreads, 2)
           const int step = p.by_row ? 1 : p.rows_part;
 #pragma unroll
           for (int y = 0; y < 8; ++y)
-            po[((half * HC + c) / 4 + y) * step] = make_float4(v[4 * y], v[4 * y + 1], v[4 * y + 2], v[4 * y + 3]);
+            po[((c) / 4 + y) * step] = make_float4(v[4 * y], v[4 * y + 1], v[4 * y + 2], v[4 * y + 3]);
         } else {
-          uint4* to = reinterpret_cast<uint4*>(p.o + now.row * HD + half * HC + c);
+          uint4* to = reinterpret_cast<uint4*>(p.o + now.row * HD + c);
 #pragma unroll
           for (int y = 0; y < 4; ++y)
             to[y] = make_uint4(pack_bf16(v[8 * y] * inv, v[8 * y + 1] * inv), pack_bf16(v[8 * y + 2] * inv, v[8 * y + 3] * inv),
@@ -711,7 +687,7 @@ __global__ void __launch_bounds__(kThreads, 2)
   }
   tc_fence_before();
   __syncthreads();
-  if (threadIdx.x == 256 && *abort_flag) {
+  if (threadIdx.x == 128 && *abort_flag) {
     // loads issued but never consumed land before the CTA exits
     volatile int no_abort = 0;
     if (issued_q > 0) mbar_wait(q_full, (issued_q - 1) & 1, &no_abort, p.budget);
@@ -720,7 +696,7 @@ __global__ void __launch_bounds__(kThreads, 2)
   }
   __syncwarp();
   tc_fence_after();
-  if (warp == 8) tmem_dealloc(tmem, kTmemCols);
+  if (warp == 4) tmem_dealloc(tmem, kTmemCols);
   if (threadIdx.x == 0) stamp_end(p.stamp);
 }
 
