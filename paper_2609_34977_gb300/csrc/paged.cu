@@ -1336,12 +1336,14 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
       const int places = token ? sms : 2 * sms;
       p.ctas = int(std::min<long long>(places, total));
       // Parts of units are written, read and joined, at the price of a launch and some blocks a CTA, of more the more CTAs do so at
-      // once. One unit a CTA and equal stretches: 700 tokens of 32 heads of 128 (192 units of 2 to 11 blocks) 26 and 33 us, 18 tokens
-      // over 400 rows of 28 heads on 4 (4 units of 7) 16.0 and 11.5, 32 sequences of 4 over 1500 rows (128 units of 24) 39.9 and 32.9.
+      // once. One unit a CTA and equal stretches: 500 tokens behind 700 of 32 heads of 128 (128 units of 13 to 19 blocks, 6.9 a CTA)
+      // 27.9 and 31.4 us, 300 behind 1500 (96 of 25 to 29, 8.7) 36.9 and 32.9, 18 behind 400 of 28 heads on 4 (4 of 7, 1) 11.9 and
+      // 10.0, 32 sequences of 4 behind 1500 (128 of 24, 10.1) 33.4 and 32.0; 700 fresh tokens of 16 heads of 64 on 8 (88 of up to 11,
+      // 1.7) 13.0 and 15.8.
       // Single tokens: over 200 rows of 32 heads (32 units of 2) 6.4 and 7.2, 350 (of 3) 7.9 and 7.6 and 3 us less for the host, 700
       // (of 6) 12.4 and 9.0; 4 sequences over 1100 (128 units of 9, 7.6 a CTA) 17.8 and 19.7, of 2000 (of 16, 13.5) 29.3 and 29.1.
       p.whole = units <= places && (token ? longest <= 3 || 2 * longest <= 2 * total / p.ctas + 3
-                                          : longest <= total / p.ctas + 3 + 10 * units / places);
+                                          : (longest - 2ll) * p.ctas <= total + 27 * units * p.ctas / places);
       if (p.whole) {
         p.ctas = int(units);
         int first = 0;
