@@ -9,9 +9,13 @@
 // exponentials a thread, and those tokens that beat the n_out-th best so far go to a list in shared memory, which is cut back to
 // n_out when it has doubled. The first bound: of n_out or more groups of threads the least of their maxima. Where more tokens beat
 // the bound than the list holds (rising or equal logits) the batch's n_out best are taken one by one.
-// A CTA a request then takes the n_out lists of the best heads, and of their candidates that are not behind the last of these heads the
-// n_out best, by counting how many go before each. Candidates of different beams may lie closer together than fp32 tells, and fp64
-// is slow here, so totals are pairs of fp32 values (a sum and what it was rounded by).
+// A CTA a request then takes the n_out lists of the best heads, and of their candidates that are not behind the last of these
+// heads the n_out best, by counting how many go before each. Candidates of different beams may lie closer together than fp32
+// tells, and fp64 is slow here, so totals are pairs of fp32 values (a sum and what it was rounded by).
+//
+// What bounds it: of many rows the stream and the instructions a logit takes (an exponential, two maxima, a comparison): 128 rows
+// of 152064 19.3 us with the merge, 78 MB; of one request a chain, 6 us. 256 threads a CTA, or twice as many tokens a thread, took
+// longer.
 #include <math.h>
 #include <stdint.h>
 
@@ -32,7 +36,10 @@ constexpr int kList = 384;                 // candidates a CTA holds
 constexpr int kMergeThreads = 256;
 constexpr int kStages = 4;                 // batches on their way into shared memory
 constexpr int kCtasSm = 6;                 // CTAs an SM
-constexpr int kMergeBytes = 200 * 1024;    // shared memory for a request's lists
+// Lists a request, of which the merging CTA has one a thread: of 12 and 4 rows of 152064 with up to 48 / 96 / 128 / 192 / 256 lists 18.6 /
+// 15.9 / 13.9 / 15.5 / 15.4 and 10.1 / 8.8 / 8.7 / 10.5 / 11.5 us.
+constexpr int kMostLists = 128;
+static_assert(kMaxBeams <= kMostLists && kMostLists <= kMergeThreads, "a list a thread");
 
 struct BeamArgs {
   const float* z;
@@ -315,13 +322,12 @@ __device__ __forceinline__ Total total_of(float2 norm, float z) {
 __device__ __forceinline__ int before(Total a, int i, Total b, int j) { return int(a > b) | (int(a == b) & int(i < j)); }
 
 __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const __grid_constant__ BeamArgs p) {
+  constexpr int kFronts = kMaxBeams * (kMaxBeams + 1) / 2;
   __shared__ float2 norm[kMaxBeams];  // what a beam's logits are added to: score - log sum; NaN where it offers nothing
-  __shared__ Total ends[kMaxBeams], front[kMaxBeams * kMaxBeams], last_total;
-  __shared__ int front_at[kMaxBeams * kMaxBeams], fronts, last_at;
-  extern __shared__ Total total[];    // [n_in * slices][n_out], then as many tokens
+  __shared__ Total ends[kMaxBeams], head[kMostLists], front[kFronts], last_total;
+  __shared__ int chosen[kMaxBeams], front_at[kFronts], front_token[kFronts], fronts, last_at;
   const int req = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int lists = p.n_in * p.slices, K = p.n_out;
-  int* token = reinterpret_cast<int*>(total + size_t(lists) * K);
   int stages = 1;  // of a sum over the slices
   while (stages < p.slices && stages < 32) stages *= 2;
   if (tid == 0) {
@@ -332,10 +338,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const __grid_
   pdl_launch_dependents();
   pdl_wait();
   const unsigned long long* best = p.best + size_t(req) * lists * K;
-  constexpr int kAhead = 2;  // keys of a thread on their way while the sums are added up
-  unsigned long long ahead[kAhead];
-#pragma unroll
-  for (int u = 0; u < kAhead; ++u) ahead[u] = tid + u * kMergeThreads < lists * K ? best[tid + u * kMergeThreads] : 0;
+  const unsigned long long head_key = tid < lists ? best[size_t(tid) * K] : 0;  // on its way while the sums are added up
   for (int w = warp; w < p.n_in; w += kMergeThreads / 32) {
     const size_t row = size_t(req) * p.n_in + w;
     const float score = p.scores[row];
@@ -362,32 +365,35 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const __grid_
     }
   }
   __syncthreads();
-  for (int i = tid, u = 0; i < lists * K; i += kMergeThreads, ++u) {
-    const unsigned long long key = u == 0 ? ahead[0] : u == 1 ? ahead[1] : best[i];
-    total[i] = key ? total_of(norm[i / (p.slices * K)], key_value(key)) : 0;
-    token[i] = int(0xffffffffu - uint32_t(key));
-  }
+  auto total_at = [&](int list, unsigned long long key) { return key ? total_of(norm[list / p.slices], key_value(key)) : 0; };
+  // the n_out best heads
+  if (tid < lists) head[tid] = total_at(tid, head_key);
   __syncthreads();
-  // the n_out-th best head: what goes behind it is not among the best
-  for (int i = tid; i < lists; i += kMergeThreads) {
-    const Total mine = total[i * K];
+  if (tid < lists) {
+    const Total mine = head[tid];
     int first = 0;
 #pragma unroll 8
-    for (int j = 0; j < lists; ++j) first += before(total[j * K], j, mine, i);
+    for (int j = 0; j < lists; ++j) first += before(head[j], j, mine, tid);
+    if (first < K) chosen[first] = tid;
     if (first == K - 1) {
       last_total = mine;
-      last_at = i * K;
+      last_at = tid * K;
     }
   }
   __syncthreads();
+  // Their candidates, but for what goes behind the last of these heads. What is k-th of the list whose head is r-th has r + k before it.
   const Total last = last_total;
   const int behind = last_at;
-  for (int i = tid; i < lists * K; i += kMergeThreads) {
-    const Total c = total[i];
+  for (int x = tid; x < min(K, lists) * K; x += kMergeThreads) {
+    const int r = x / K, k = x - r * K, list = chosen[r], i = list * K + k;
+    if (r + k >= K) continue;
+    const unsigned long long key = best[i];
+    const Total c = total_at(list, key);
     if (c == 0 || before(last, behind, c, i)) continue;
-    const int at = atomicAdd(&fronts, 1);  // (of n_out lists, so at most n_out^2)
-    front[at] = c;
-    front_at[at] = i;
+    const int y = atomicAdd(&fronts, 1);
+    front[y] = c;
+    front_at[y] = i;
+    front_token[y] = int(0xffffffffu - uint32_t(key));
   }
   __syncthreads();
   const int n = fronts;
@@ -400,7 +406,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const __grid_
     if (first >= K) continue;
     const size_t at = size_t(req) * K + first;
     p.parent[at] = req * p.n_in + from / (p.slices * K);
-    p.token[at] = token[from];
+    p.token[at] = front_token[i];
     p.out[at] = order_value(uint32_t(c >> 32));
   }
   for (int i = n + tid; i < K; i += kMergeThreads) {
@@ -417,16 +423,16 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const __grid_
       const Total c = front[j];
       const int at = front_at[j];
       // of equal totals those of a lower beam, and of the beam's own the lower tokens
-      first += int(c > e) | (int(c == e) & (int(at < w * own) | (int(at < (w + 1) * own) & int(token[at] < p.eos))));
+      first += int(c > e) | (int(c == e) & (int(at < w * own) | (int(at < (w + 1) * own) & int(front_token[j] < p.eos))));
     }
     for (int v = 0; v < p.n_in; ++v) first += before(ends[v], v, e, w);
     p.ended[size_t(req) * p.n_in + w] = e && first < K ? order_value(uint32_t(e >> 32)) : -INFINITY;
   }
 }
 
-// Slices a row: as many as fill the GPU (kCtasSm CTAs on each of 152 SMs), of a batch at least, whose lists a merging CTA can hold.
-int slices_of(int n_seqs, int n_in, int n_out, int vocab) {
-  const int most = std::min((vocab + kBatch - 1) / kBatch, kMergeBytes / (n_in * 12 * n_out));
+// Slices a row: as many as fill the GPU (kCtasSm CTAs on each of 152 SMs), of a batch at least, kMostLists lists a request at most.
+int slices_of(int n_seqs, int n_in, int vocab) {
+  const int most = std::min((vocab + kBatch - 1) / kBatch, kMostLists / n_in);
   return std::max(1, std::min(most, kCtasSm * 152 / std::max(1, n_seqs * n_in)));
 }
 
@@ -437,7 +443,7 @@ using namespace spd;
 
 extern "C" size_t spd_beam_select_workspace_size(int n_seqs, int n_in, int n_out, int vocab) {
   if (n_seqs < 1 || n_in < 1 || n_out < 1 || vocab < 1 || n_in > kMaxBeams || n_out > kMaxBeams) return 0;
-  const size_t lists = size_t(n_seqs) * n_in * slices_of(n_seqs, n_in, n_out, vocab);
+  const size_t lists = size_t(n_seqs) * n_in * slices_of(n_seqs, n_in, vocab);
   Carve cv(nullptr, ~size_t(0));
   cv.take<unsigned long long>(lists * n_out);
   cv.take<float2>(lists);
@@ -460,7 +466,7 @@ extern "C" int spd_beam_select(const float* logits, int n_seqs, int n_in, int vo
   p.ld = ld;
   p.n_in = n_in;
   p.n_out = n_out;
-  p.slices = slices_of(n_seqs, n_in, n_out, vocab);
+  p.slices = slices_of(n_seqs, n_in, vocab);
   p.slice = ((vocab + p.slices - 1) / p.slices + 3) & ~3;
   p.eos = eos;
   p.scores = scores;
@@ -478,16 +484,14 @@ extern "C" int spd_beam_select(const float* logits, int n_seqs, int n_in, int vo
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int slot = trace_begin(st);
   const bool vec = vocab % 4 == 0 && ld % 4 == 0 && (reinterpret_cast<uintptr_t>(logits) & 15) == 0;
-  const size_t smem = size_t(n_in) * p.slices * 12 * size_t(n_out);
   constexpr int kRing = kStages * kBatch * 4;
   static DeviceOnce once;
   SPD_CUDA_TRY(once_per_device(once, [] {
-    const cudaError_t e = cudaFuncSetAttribute(beam_merge_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMergeBytes);
-    return e ? e : cudaFuncSetAttribute(beam_slice_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRing);
+    return cudaFuncSetAttribute(beam_slice_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRing);
   }));
   SPD_CUDA_TRY(launch_pdl(vec ? beam_slice_kernel<4> : beam_slice_kernel<1>, dim3(p.slices, n_seqs * n_in), dim3(kThreads),
                           vec ? kRing : 0, st, p));
-  SPD_CUDA_TRY(launch_pdl(beam_merge_kernel, dim3(n_seqs), dim3(kMergeThreads), smem, st, p));
+  SPD_CUDA_TRY(launch_pdl(beam_merge_kernel, dim3(n_seqs), dim3(kMergeThreads), 0, st, p));
   trace_end(slot, st, TR_ROWS, 0.0, 4.0 * n_seqs * n_in * double(vocab));
   return SPD_OK;
 }

@@ -93,6 +93,20 @@ def test_selection(B, n_in, n_out, v, eos):
     _check(z, scores, eos, n_out)
 
 
+@pytest.mark.parametrize("n_in,n_out,v,eos", [(12, 12, 152064, 3), (32, 32, 60001, 9), (9, 32, 152064, -1), (6, 1, 152064, 5)])
+def test_one_request_over_many_lists(n_in, n_out, v, eos):
+    z, scores = _rand(11, 1, n_in, v)
+    _check(z, scores, eos, n_out)
+    # equal rows, twenty equal bests all over them
+    r = np.random.default_rng(12)
+    row = np.zeros(v, np.float32)
+    best = np.sort(r.choice(np.arange(16, v), 20, replace=False))
+    row[best] = 3.0
+    p, t, _, _ = _run(row[None].repeat(n_in, 0), np.zeros((1, n_in), np.float32), eos, n_out)
+    np.testing.assert_array_equal(p[0], (np.arange(n_out) // 20).astype(int))
+    np.testing.assert_array_equal(t[0], np.tile(best, 2)[:n_out])
+
+
 def test_ties_go_to_the_lower_beam_and_token():
     z = np.zeros((6, 5000), np.float32)
     z[:, 4100:4110] = 2.0  # ten equal bests across two batches of a slice, in equal rows
