@@ -557,7 +557,8 @@ size_t spd_paged_attention_workspace_size(int n_q, int n_seqs, int n_heads, int 
  *   o_i = sum_j softmax_j(q_i . k_j / sqrt(head_dim)) v_j,   lse_i = log sum_j exp(q_i . k_j / sqrt(head_dim)).
  * What a row does not see contributes nothing, whatever it holds. NaN in a query or in a key that is seen gives NaN; an infinite V
  * that is seen gives the infinity (perhaps NaN where its weight is below 2^-100 of the row's largest). Where all scores of a row are
- * -inf o is 0 and lse -inf. Weights of up to 2^8 are multiplied with V and added up in fp32: V above 2^100 may overflow.
+ * -inf o is 0 and lse -inf. Weights of up to 2^8, in 16 bits or more, are multiplied with V and added up in fp32: V above 2^100 may
+ * overflow. lse is of whole fp32 weights.
  * q, o (dev) bf16 [n_q][n_heads * head_dim]; lse (dev) fp32 [n_q][n_heads], natural logarithm, may be NULL; pool: the layer's block.
  * The same bits in every run. q, o, pool and ws 16-byte aligned.
  * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ENOSPC, SPD_ECUDA; device timeouts in the workspace's status word. */

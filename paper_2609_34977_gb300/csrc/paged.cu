@@ -1,4 +1,4 @@
-// Attention of new tokens over a paged KV cache: chunks of prompts (paged_attn_kernel).
+// Attention of new tokens over a paged KV cache: chunks of prompts (paged_attn_kernel), single tokens (paged_token_kernel).
 //
 // New token i of sequence b, one of its n, sees rows 0 .. lim_i - 1 with lim_i = max(len - n + i + 1, prefix):
 //   s_ij = q_i . k_j / sqrt(head_dim),  lse_i = log sum_j e^s_ij,  o_i = sum_j e^(s_ij - lse_i) v_j.
@@ -15,6 +15,14 @@
 // Only blocks that reach past the first token's limit are masked; there the softmax warps also clear the values of V that are
 // not finite (recycled memory behind the sequence among them), which a weight of zero would turn into NaN for rows that do not
 // see them; rows that do see one add it at the end.
+//
+// What bounds chunks: the tensor pipe, with two products of P V a block 1792 cycles for a block of each of an SM's two CTAs at
+// heads of 128 (a product of 128 x 64 x 16 with both operands in shared memory takes 48 cycles, not 32: it reads 6 KB), 900 at
+// heads of 64, and what an SM's pairs of blocks take is 2050 and 1770. 2048 tokens behind 14333 rows, 28 heads on 4: 434 us, 1.04
+// PFLOP/s of S and P V, 1.56 of what is issued; 2048 behind 14000, 16 heads of 64 on 8: 185 us. Heads of 64 are bound by the chain
+// of a block: 350 cycles for scores and maximum, 600 for exponentials and terms, 300 between, 400 waiting for S.
+// One warp that issued both products took 437 and 205 us (its instructions for a block were 1000 cycles and on the chain); two
+// threads a row, with a barrier a block for what they have to agree on, 449 and 218.
 #include <cuda_bf16.h>
 #include <math.h>
 #include <stdint.h>
@@ -226,8 +234,8 @@ struct Place {
   }
 };
 
-// Products and commits by a whole warp in step, of which one lane issues: descriptors then stay in uniform registers. (A lane on its own
-// moves every operand there for each product: 1000 cycles a block of keys, and more than the products take.)
+// Products and commits by a whole warp in step, of which one lane issues: descriptors then stay in uniform registers. (A lane on
+// its own moves every operand there for each product: 1000 cycles a block of keys, and more than the products take.)
 __device__ __forceinline__ void issue_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
   asm volatile(
       "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
@@ -361,7 +369,8 @@ __global__ void __launch_bounds__(kThreads, 2)
         const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, here >= 0)) * p.box * 128u * L::kChunks;
         auto load = [&](uint64_t* full, uint64_t* empty, int stages, uint32_t to, int x0) -> bool {
           const int st = j % stages;
-          if (j >= stages && !__all_sync(0xffffffffu, mbar_wait(&empty[st], (j / stages - 1) & 1, abort_flag, p.budget))) return false;
+          if (j >= stages && !__all_sync(0xffffffffu, mbar_wait(&empty[st], (j / stages - 1) & 1, abort_flag, p.budget)))
+            return false;
           if (lane == 0) mbar_arrive_expect_tx(&full[st], bytes);
           __syncwarp();
           if (here >= 0)
@@ -703,9 +712,11 @@ __global__ void __launch_bounds__(kThreads, 2)
 // ---- single tokens --------------------------------------------------------------------------------
 // A sequence's one new token with up to 16 query heads a K/V head: too few rows to fill an MMA's 128, so keys and dims are its
 // rows: S^T = K Q^T (128 keys x 16 heads), O^T += V^T P^T (128 dims x 64; of heads of 64 the other half is what lies behind V,
-// and is not read), V in place as an MN-major operand, P^T through shared memory. P^T's columns are the three bf16 terms of every head's weights, side by side (48 of 64), so
-// V is read once for all of them and a term that is zero or negative does not meet an infinite V in another's sum. One CTA an
-// SM, 192 KB of K and V on their way:
+// and is not read), V in place as an MN-major operand, P^T through shared memory. P^T's columns are the three bf16 terms of every
+// head's weights, side by side (48 of 64), all 24 bits of them (the tensor pipe has the time): V is read once for all of them
+// and a term that is zero or negative does not meet an infinite V in another's sum. One CTA an SM, 192 KB of K and V on their way.
+// What bounds it: the stream of K and V. 48 sequences over 301 to 8432 rows, 28 heads on 4: 0.43 GB in 75 us, 5.7 TB/s; a token
+// over 322 rows of 32 heads 7.5 us, a chain of launch, first loads, product, exponentials, product, output.
 //   warp 4     TMA producer          warp 5     MMA issuer          warp 6     the units' Q, a unit ahead
 //   warps 0-3  a thread a key: exponentials against a reference a head, renewed for all of them once a score has
 //              outgrown one by kGrown; sums a thread, added up at the end. In the end a thread a dim: O out of TMEM.
@@ -1262,7 +1273,8 @@ size_t paged_attention_bytes(int n_q, int n_heads, int n_kv_heads, int head_dim)
 
 int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, const int32_t* prefix, int n_seqs,
                         const int32_t* table, int max_pages, const void* pool, int n_pages, int page_size, int n_heads,
-                        int n_kv_heads, int head_dim, void* o, float* lse, void* ws, size_t ws_bytes, int* status, cudaStream_t st) {
+                        int n_kv_heads, int head_dim, void* o, float* lse, void* ws, size_t ws_bytes, int* status,
+                        cudaStream_t st) {
   const int kvd = n_kv_heads * head_dim, n_q = q_cu[n_seqs];
   PagedArgs p{};
   p.q = static_cast<const __nv_bfloat16*>(q);
@@ -1335,13 +1347,14 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
       p.total = int(total);
       const int places = token ? sms : 2 * sms;
       p.ctas = int(std::min<long long>(places, total));
-      // Parts of units are written, read and joined, at the price of a launch and some blocks a CTA, of more the more CTAs do so at
-      // once. One unit a CTA and equal stretches: 500 tokens behind 700 of 32 heads of 128 (128 units of 13 to 19 blocks, 6.9 a CTA)
-      // 27.9 and 31.4 us, 300 behind 1500 (96 of 25 to 29, 8.7) 36.9 and 32.9, 18 behind 400 of 28 heads on 4 (4 of 7, 1) 11.9 and
-      // 10.0, 32 sequences of 4 behind 1500 (128 of 24, 10.1) 33.4 and 32.0; 700 fresh tokens of 16 heads of 64 on 8 (88 of up to 11,
-      // 1.7) 13.0 and 15.8.
-      // Single tokens: over 200 rows of 32 heads (32 units of 2) 6.4 and 7.2, 350 (of 3) 7.9 and 7.6 and 3 us less for the host, 700
-      // (of 6) 12.4 and 9.0; 4 sequences over 1100 (128 units of 9, 7.6 a CTA) 17.8 and 19.7, of 2000 (of 16, 13.5) 29.3 and 29.1.
+      // Parts of units are written, read and joined, at the price of a launch and some blocks a CTA, of more the more CTAs do so
+      // at once. One unit a CTA and equal stretches, us: 500 tokens behind 700 of 32 heads of 128 (128 units of 13 to 19 blocks,
+      // 6.9 a CTA) 27.6 and 31.4, 300 behind 1500 (96 of 25 to 29, 8.7) 36.9 and 33.0, 18 behind 400 of 28 heads on 4 (4 of 7, 1)
+      // 11.9 and 10.0, 32 sequences of 4 behind 1500 (128 of 24, 10.1) 33.4 and 32.0; 700 fresh tokens of 16 heads of 64 on 8 (88 of
+      // up to 11, 1.7) 13.0 and 15.8.
+      // Single tokens: over 200 rows of 32 heads (32 units of 2) 6.4 and 7.2, 350 (of 3) 7.9 and 7.6 and 3 us less for the host,
+      // 700 (of 6) 12.4 and 9.0; 4 sequences over 1100 (128 units of 9, 7.6 a CTA) 17.8 and 19.7, of 2000 (of 16, 13.5) 29.3 and
+      // 29.1.
       p.whole = units <= places && (token ? longest <= 3 || 2 * longest <= 2 * total / p.ctas + 3
                                           : (longest - 2ll) * p.ctas <= total + 27 * units * p.ctas / places);
       if (p.whole) {

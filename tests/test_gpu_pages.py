@@ -241,6 +241,9 @@ def _check(q, pool, table, new, lens, g, m, d, prefix, o, ls):
     (2, 16, 64, [1, 1, 3], [129, 1, 700], 16, None),              # single tokens beside others
     (2, 9, 128, [1, 1, 1], [128, 127, 300], 16, [0, 100, 300]),   # (a prefix tells a last token nothing)
     (1, 17, 128, [1], [500], 16, None),                           # one head too many for the single tokens' form
+    (32, 1, 128, [1] * 3, [384, 1, 200], 16, None),               # single tokens, a unit a CTA,
+    (4, 7, 64, [1] * 30, [1150 - 7 * i for i in range(30)], 48, None),
+    (32, 1, 128, [1], [385], 64, None),                           # and in parts
 ])
 def test_attention(g, m, d, new, lens, page, prefix):
     q, pool, table = _case(5, g, m, d, new, lens, page)
@@ -258,6 +261,19 @@ def test_attention_of_many_sequences():
     q, pool, table = _case(6, g, m, d, new, lens, page)
     o, ls = _attend(q, pool, table, new, lens, g, m, d)
     _check(q, pool, table, new, lens, g, m, d, None, o, ls)
+
+
+@pytest.mark.parametrize("g,m,d,new,ln", [(2, 3, 128, 40, 700), (2, 1, 64, 300, 900)])
+def test_a_row_does_not_hang_on_its_neighbours(g, m, d, new, ln):
+    # the scores of the other rows of a tile grow from block to block: the row's bits stay
+    q, pool, table = _case(31, g, m, d, [new], [ln], 16)
+    o, ls = _attend(q, pool, table, [new], [ln], g, m, d)
+    keep = torch.arange(new) % 7 == 3
+    other = q.clone()
+    other[~keep] *= 20
+    o2, ls2 = _attend(other, pool, table, [new], [ln], g, m, d)
+    assert torch.equal(o[keep], o2[keep]) and torch.equal(ls[keep], ls2[keep])
+    assert not torch.equal(o[~keep], o2[~keep])
 
 
 @pytest.mark.parametrize("d,new,ln", [(128, 1, 777), (64, 90, 400)])
