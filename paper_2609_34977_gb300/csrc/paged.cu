@@ -172,10 +172,10 @@ struct Place {
       seek(p, sq, at, first_block(p, c + 1) - at);
       return left;
     }
-    find(sq, c);
-    tile = c - sq.s[e].block0;
-    hk = int(uint32_t(tile) / uint32_t(sq.s[e].tiles));
-    tile -= hk * sq.s[e].tiles;
+    find(sq, c);  // a sequence's last tiles, the longest, first
+    const int x = c - sq.s[e].block0, back = int(uint32_t(x) / uint32_t(p.n_kv_heads));
+    hk = x - back * p.n_kv_heads;
+    tile = sq.s[e].tiles - 1 - back;
     lo = 0;
     left = 1 << 30;
     size(p, sq);
@@ -1316,6 +1316,7 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
       sq.n = 0;
       long long total = 0, units = 0;
       int most = 0, longest = 0;
+      int sizes[256] = {};  // tiles of as many blocks, from 128 on of 128 times (the index - 128) or more
       double pairs = 0.0, keys = 0.0, tokens = 0.0;
       for (; next < n_seqs && sq.n < kMaxSeqs; ++next) {
         const int b = next, n = q_cu[b + 1] - q_cu[b];
@@ -1326,6 +1327,7 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
         for (int i = 0; i < n; i += p.tokens) {
           const int here = blocks_at(s, i, p.tokens, p.keys);
           longest = std::max(longest, here);
+          sizes[here < 128 ? here : 128 + std::min(127, here >> 7)] += p.chunks;
           blocks += (long long)here * p.chunks;
         }
         total += blocks * n_kv_heads;
@@ -1348,16 +1350,35 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
       const int places = token ? sms : 2 * sms;
       p.ctas = int(std::min<long long>(places, total));
       // Parts of units are written, read and joined, at the price of a launch and some blocks a CTA, of more the more CTAs do so
-      // at once. One unit a CTA and equal stretches, us: 500 tokens behind 700 of 32 heads of 128 (128 units of 13 to 19 blocks,
-      // 6.9 a CTA) 27.6 and 31.4, 300 behind 1500 (96 of 25 to 29, 8.7) 36.9 and 33.0, 18 behind 400 of 28 heads on 4 (4 of 7, 1)
-      // 11.9 and 10.0, 32 sequences of 4 behind 1500 (128 of 24, 10.1) 33.4 and 32.0; 700 fresh tokens of 16 heads of 64 on 8 (88 of
-      // up to 11, 1.7) 13.0 and 15.8.
+      // at once; a CTA that goes on from one unit to the next does nothing for some 4 us. One unit a CTA, the longest first, and equal
+      // stretches, us. 28 heads of 128 on 4: 1500 fresh tokens (336 units of 1 to 24 blocks, 13.8 a place) 33 and 65, 2000 (448, 24.5)
+      // 42 and 91, 19 prompts of 2 to 1079 (612) 34 and 85, 1500 behind 1500 (336 of 24 to 47, 40) 73 and 75, 2048 behind 4000 (456
+      // of 63 to 95, 120) 177 and 166, 18 behind 400 (4 of 7, 1) 11.9 and 10.0. 32 heads of 128: 500 behind 700 (128 of 13 to 19, 6.9)
+      // 27.6 and 31.4, 300 behind 1500 (96 of 25 to 29, 8.7) 36.9 and 33.0. 16 heads of 64 on 8: 700 fresh (88 of 1 to 11, 1.7) 13.0
+      // and 15.8, 3000 (376, 29) 44 and 53, 2048 behind 2000 (256 of 32 to 64, 40) 58 and 53. Few rows a unit, whose parts are small: 32
+      // sequences of 4 behind 1500 (128 of 24, 10.1) 33.4 and 32.0, 31 of 2 behind 50, 32 heads (992 of 1, 3.3) 33 and 27.
       // Single tokens: over 200 rows of 32 heads (32 units of 2) 6.4 and 7.2, 350 (of 3) 7.9 and 7.6 and 3 us less for the host,
       // 700 (of 6) 12.4 and 9.0; 4 sequences over 1100 (128 units of 9, 7.6 a CTA) 17.8 and 19.7, of 2000 (of 16, 13.5) 29.3 and
-      // 29.1.
-      p.whole = units <= places && (token ? longest <= 3 || 2 * longest <= 2 * total / p.ctas + 3
-                                          : (longest - 2ll) * p.ctas <= total + 27 * units * p.ctas / places);
+      // 29.1. (Their form has the next unit's scores under way; the tiles' form takes 33 us for 31 tokens over 50 rows of 32 heads,
+      // theirs 24.)
+      const bool few = std::min(most, p.tokens) * p.chunk <= kMergeRows;
+      if (token) {
+        p.whole = units <= places && (longest <= 3 || 2 * longest <= 2 * total / p.ctas + 3);
+      } else {
+        long long load = longest;  // blocks of the fullest place
+        if (units > places) {
+          int size = 0;  // of the units that begin last
+          for (long long left = units % places; left > 0; ++size) left -= (long long)sizes[size] * n_kv_heads;
+          load = std::max(load, total / places + (size <= 128 ? size : (size - 128) * 128));
+        }
+        const long long price = std::min<long long>(27 * units * p.ctas / places, (few ? 10ll : head_dim == 64 ? 16ll : 27ll) * p.ctas);
+        p.whole = (units <= places || !few) && (load - 2) * p.ctas <= total + price;
+      }
       if (p.whole) {
+        if (units > places)
+          std::sort(sq.s, sq.s + sq.n, [&](const PagedSeq& a, const PagedSeq& b) {
+            return limit_of(a, a.n - 1) > limit_of(b, b.n - 1);
+          });
         p.ctas = int(units);
         int first = 0;
         for (int e = 0; e < sq.n; ++e) {
@@ -1367,7 +1388,7 @@ int paged_attention_run(const void* q, const int32_t* q_cu, const int32_t* len, 
       }
       p.share = p.total / p.ctas;
       p.more = p.total - p.share * p.ctas;
-      p.by_row = token || std::min(most, p.tokens) * p.chunk <= kMergeRows;
+      p.by_row = token || few;
       p.warps = (std::min(most, p.tokens) * p.chunk + 31) / 32;
       const double fl = 4.0 * head_dim * n_heads * pairs;
       const double by = 4.0 * kvd * keys + 4.0 * n_heads * head_dim * tokens;

@@ -244,6 +244,9 @@ def _check(q, pool, table, new, lens, g, m, d, prefix, o, ls):
     (32, 1, 128, [1] * 3, [384, 1, 200], 16, None),               # single tokens, a unit a CTA,
     (4, 7, 64, [1] * 30, [1150 - 7 * i for i in range(30)], 48, None),
     (32, 1, 128, [1], [385], 64, None),                           # and in parts
+    (32, 1, 128, [1300], [1300], 64, None),                       # more units than the GPU holds at once, the longest first
+    (40, 1, 64, [130, 700, 0, 260], [400, 700, 9, 260], 48, [0, 600, 0, 0]),
+    (150, 2, 64, [40, 3], [40, 900], 16, None),
 ])
 def test_attention(g, m, d, new, lens, page, prefix):
     q, pool, table = _case(5, g, m, d, new, lens, page)
