@@ -1277,20 +1277,6 @@ int make_operand_map(CUtensorMap* map, const void* ptr, int inner, int outer, in
   return make_map(map, ptr, inner, outer, box_outer);
 }
 
-int make_heads_map(CUtensorMap* map, const void* ptr, int head_dim, int heads, int rows, int box_heads, int box_rows) {
-  EncodeFn fn = encode_fn();
-  if (!fn) return fail(SPD_ECUDA, "cuTensorMapEncodeTiled unavailable");
-  cuuint64_t dims[3] = {cuuint64_t(head_dim), cuuint64_t(heads), cuuint64_t(rows)};
-  cuuint64_t strides[2] = {cuuint64_t(head_dim) * 2, cuuint64_t(heads) * head_dim * 2};
-  cuuint32_t box[3] = {kBK, cuuint32_t(box_heads), cuuint32_t(box_rows)};
-  cuuint32_t estr[3] = {1, 1, 1};
-  CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) return fail(SPD_ECUDA, "cuTensorMapEncodeTiled failed (%d)", int(r));
-  return SPD_OK;
-}
-
 namespace {
 
 // ---- matrix-vector path (one token, or up to 16: a decode step) -----------------------------------

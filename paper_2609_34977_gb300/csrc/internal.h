@@ -183,8 +183,6 @@ int make_weight_map(CUtensorMap* map, const void* w, int n_out, int k);
 // Tensor map of a dense bf16 matrix [outer][inner] (row stride inner elements) read in boxes of
 // 64 columns x box_outer rows with the 128-byte swizzle; rows past `outer` read as zeros.
 int make_operand_map(CUtensorMap* map, const void* ptr, int inner, int outer, int box_outer);
-// ... of rows of heads, bf16 [rows][heads][head_dim], in boxes of 64 columns x box_heads x box_rows (16-byte aligned).
-int make_heads_map(CUtensorMap* map, const void* ptr, int head_dim, int heads, int rows, int box_heads, int box_rows);
 
 // ---- attention (tcgen05) ---------------------------------------------------------------------
 // Causal attention of n_q active queries (q [n_q][n_heads * head_dim], rows grouped by sequence,

@@ -5,9 +5,10 @@
 // What a row does not see contributes nothing, whatever it holds.
 //
 // A unit is a tile of up to 128 rows (tokens times the query heads of a K/V head's group) over the keys that its last token
-// sees, in blocks of 64. All blocks of a launch form one list, unit after unit, and every CTA takes an equal stretch of it,
-// whole units and parts of two: no CTA waits for a longest sequence, and 1.5 tiles a CTA cost 1.5 tiles. Parts of a unit leave
-// states (m, l, O) in fp32, which paged_merge_kernel joins in the order of the keys (the same bits in every run).
+// sees, in blocks of 64. A CTA has one unit, the longest units first, where that is about as even as it gets. Else all blocks of a
+// launch form one list, unit after unit, and every CTA takes an equal stretch of it, whole units and parts of two: no CTA waits
+// for a longest sequence, and 1.5 tiles a CTA cost 1.5 tiles. Parts of a unit leave states (m, l, O) in fp32, which
+// paged_merge_kernel joins in the order of the keys (the same bits in every run).
 //   warps 0-3  a thread a row: online softmax in fp32; a weight is held as the sum of two bf16 terms, 16 bits of it, both over
 //              the scores in TMEM
 //   warp 4     TMA producer: Q, and K and V blocks into rings, a lane a box of rows that lie in one page
@@ -1259,6 +1260,28 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
 int rows_of_part(int n_q, int n_heads, int n_kv_heads) {
   const int chunk = std::min(n_heads / n_kv_heads, 128);
   return std::min(128 / chunk, n_q) * chunk;
+}
+
+// Tensor map of rows of heads, bf16 [rows][heads][head_dim], in boxes of 64 columns x box_heads x box_rows (16-byte aligned).
+int make_heads_map(CUtensorMap* map, const void* ptr, int head_dim, int heads, int rows, int box_heads, int box_rows) {
+  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                              CUtensorMapFloatOOBfill);
+  static const Encode encode = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    const bool ok = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) == cudaSuccess &&
+                    found == cudaDriverEntryPointSuccess;
+    return ok ? reinterpret_cast<Encode>(f) : nullptr;
+  }();
+  if (!encode) return fail(SPD_ECUDA, "cuTensorMapEncodeTiled unavailable");
+  const cuuint64_t dims[3] = {cuuint64_t(head_dim), cuuint64_t(heads), cuuint64_t(rows)};
+  const cuuint64_t strides[2] = {cuuint64_t(head_dim) * 2, cuuint64_t(heads) * head_dim * 2};
+  const cuuint32_t box[3] = {64, cuuint32_t(box_heads), cuuint32_t(box_rows)}, every[3] = {1, 1, 1};
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, every,
+                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? SPD_OK : fail(SPD_ECUDA, "cuTensorMapEncodeTiled failed (%d)", int(r));
 }
 
 }  // namespace
