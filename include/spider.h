@@ -573,7 +573,8 @@ size_t spd_decode_paged_workspace_size(const spd_model* m, int n_q, int n_seqs);
  * embeddings; at least one token of every sequence. Every layer rotates and appends as spd_rope_pages (with the model's rotary base; Q and
  * K are rounded to bf16 before and after) and attends as spd_paged_attention; every token runs every sub-layer. pool (dev) bf16
  * [n_layers][n_pages][page_size][K | V]; logits (dev, may be NULL) fp32 [n_seqs][vocab] of every sequence's last new token. Other
- * arguments as the two calls; ws and pool 16-byte aligned.
+ * arguments as the two calls; ws and pool 16-byte aligned. It uploads lists from the host and is refused (SPD_EUNSUPPORTED) on a
+ * stream that is being captured into a graph.
  * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ENOSPC, SPD_ECUDA; device timeouts and bad pages in the workspace's status word. */
 int spd_decode_paged(const spd_model* m, const uint16_t* x, int n_q, const int32_t* q_cu, const int32_t* len,
                      const int32_t* prefix, int n_seqs, const int32_t* pos, int n_axes, const uint8_t* axis, const int32_t* table,

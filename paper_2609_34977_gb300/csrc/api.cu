@@ -1300,6 +1300,10 @@ extern "C" int spd_decode_paged(const spd_model* m, const uint16_t* x, int n_q, 
   carve_paged(c, n_q, n_seqs, cv, &bf, &h, &ps.ws, &ps.ws_bytes);
   if (!cv.fits()) return fail(SPD_ENOSPC, "paged step workspace too small (%zu < %zu)", ws_bytes, cv.used);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;  // (a replay would upload what the lists hold by then)
+  SPD_CUDA_TRY(cudaStreamIsCapturing(st, &capture));
+  if (capture != cudaStreamCaptureStatusNone)
+    return fail(SPD_EUNSUPPORTED, "a paged step uploads lists of the host: it cannot be captured into a graph");
   static thread_local HostPlan P;
   plan_init(P, c, q_cu, n_seqs, n_q, bf.list_ints);
   for (int t = 0; t < n_q; ++t) P.hl[P.pos_off + t] = 0;  // the projections' own rotation turns nothing

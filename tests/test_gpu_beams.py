@@ -38,6 +38,10 @@ def _embed(cfg, seed=0):
     return torch.randn(cfg["vocab"], cfg["d_model"], generator=g).to(torch.bfloat16).cuda()
 
 
+def _i32(a):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()
+
+
 def _cu(v):
     return np.concatenate([[0], np.cumsum(v)]).astype(np.int32)
 
@@ -110,6 +114,24 @@ def test_pass_refusals():
         assert e.value.code == code
     with pytest.raises(ValueError, match="layers"):
         N.spd_decode_paged(model, x, [0, 1, 3], [1, 2], pos, t, pool[:cfg["n_layers"] - 1], None, ws)
+
+
+def test_a_pass_is_not_captured():
+    # it uploads lists from host memory, which a replay would find changed
+    cfg, _, model = _model()
+    pool = torch.zeros(cfg["n_layers"], 2, 16, 2 * cfg["n_kv_heads"] * cfg["head_dim"], dtype=torch.bfloat16, device="cuda")
+    t, x, pos = _i32([[0]]), _embed(cfg)[:3], torch.zeros(1, 3, dtype=torch.int32, device="cuda")
+    ws = torch.zeros(N.spd_decode_paged_workspace_size(model, 3, 1), dtype=torch.uint8, device="cuda")
+    y = torch.zeros(1, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(N.SpiderError, match="captured") as e:
+            N.spd_decode_paged(model, x, [0, 3], [3], pos, t, pool, None, ws)
+        y += 1  # the capture goes on
+    assert e.value.code == N.SPD_EUNSUPPORTED
+    graph.replay()
+    torch.cuda.synchronize()
+    assert float(y) == 1 and (pool == 0).all()
 
 
 def _logprobs(model, cfg, embed, tokens, n_prompt):
