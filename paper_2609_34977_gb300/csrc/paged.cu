@@ -464,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     // ---- softmax: warp w has TMEM lanes [32 w, 32 w + 32) of S, P and O ----
     const int r = threadIdx.x, T = nw * 32;
     const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
-      const uint32_t t_oh = t_o + lanes;
+    const uint32_t t_oh = t_o + lanes;
     auto any = [](bool mine) { return __any_sync(0xffffffffu, mine) != 0; };
     // a unit's rows: the thread's token, head and query row
     struct Row {
