@@ -22,11 +22,15 @@ namespace cg = cooperative_groups;
 // Pair (j, j + d/2) of a head turns by pos[axis_j] theta^(-2j/d). An angle is kept in turns: theta^(-2j/d) / 2 pi as a 64-bit
 // fraction times the integer position, modulo 2^64, is exact but for the fraction's own rounding (2^-56 a position), so far
 // positions lose nothing; its upper 32 bits go through sincospi.
-// A thread has 8 pairs of a token (16 bytes of either half) for U heads, so that it works its angles out once for four of them
-// where there are threads enough. Heads of 128, 36 of 64 / 256 / 1024 / 4096 tokens with one and with four: 3.5 and 4.8 / 6.7 and
-// 5.0 / 10.6 and 8.8 / 34.9 and 19.9 us; 96 of 64 / 4096: 5.1 and 4.9 / 73 and 39 (199 MB, 5.1 TB/s).
+// A thread has 8 pairs of a token (16 bytes of either half) for one, four or eight heads (eight: four and four), so that it works
+// its angles out once for them where there are threads enough. Heads of 128, 36 of 64 / 256 / 1024 / 4096 tokens with one and with
+// four: 3.5 and 4.8 / 6.7 and 5.0 / 10.6 and 8.8 / 34.9 and 19.9 us; 96 of 64 / 4096: 5.1 and 4.9 / 73 and 39. With four and with
+// eight: 36 of 2000 / 2600 / 4096 / 8000 tokens 9.2 and 10.9 / 11.3 and 11.3 / 15.8 and 13.7 / 30.8 and 27.2, 96 of 500 / 800 / 2000 /
+// 4048 8.8 and 8.9 / 9.2 and 8.8 / 20.3 and 16.4 / 38.0 and 33.8 (199 MB, 5.9 TB/s); heads of 64, 32 of 4096 / 8000 / 16000 7.8 and
+// 9.8 / 11.9 and 11.5 / 24.8 and 23.1.
 constexpr int kRopeThreads = 256;
-constexpr long long kRopeSingle = 40000;  // threads of a head each up to which it is one
+constexpr long long kRopeSingle = 40000;  // threads of a head each up to which it is one,
+constexpr long long kRopeEight = 800000;  // beyond which it is eight
 constexpr int kRopeSeqs = 384;  // sequences whose places fit in a launch's parameters
 
 struct RopeSeq {
@@ -50,10 +54,10 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-template <int HD, int U>
+template <int HD, int U, int R>
 __global__ void __launch_bounds__(kRopeThreads, 4) rope_pages_kernel(const __grid_constant__ RopeArgs p) {
   constexpr int P = HD / 16;  // threads a head
-  const int heads = p.n_heads + 2 * p.n_kv_heads, slots = (heads + U - 1) / U;  // a thread's heads are `slots` apart
+  const int heads = p.n_heads + 2 * p.n_kv_heads, slots = (heads + U * R - 1) / (U * R);  // a thread's heads are `slots` apart
   const unsigned at = blockIdx.x * kRopeThreads + threadIdx.x;
   const unsigned tok = at / unsigned(slots * P), rest = at - tok * unsigned(slots * P);
   const int piece = int(rest % P), h0 = int(rest / P);
@@ -62,14 +66,17 @@ __global__ void __launch_bounds__(kRopeThreads, 4) rope_pages_kernel(const __gri
   if (tok >= unsigned(p.n_tok)) return;
   const int t = p.tok0 + int(tok);
   uint4 a[U], b[U];
+  auto load = [&](int r) {
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int h = h0 + u * slots;
-    if (h >= heads) continue;
-    const uint16_t* src = h < p.n_heads ? p.q + size_t(t) * p.ldq + h * HD : p.kv + size_t(t) * p.ldkv + (h - p.n_heads) * HD;
-    a[u] = *reinterpret_cast<const uint4*>(src + 8 * piece);
-    b[u] = *reinterpret_cast<const uint4*>(src + HD / 2 + 8 * piece);
-  }
+    for (int u = 0; u < U; ++u) {
+      const int h = h0 + (r * U + u) * slots;
+      if (h >= heads) continue;
+      const uint16_t* src = h < p.n_heads ? p.q + size_t(t) * p.ldq + h * HD : p.kv + size_t(t) * p.ldkv + (h - p.n_heads) * HD;
+      a[u] = *reinterpret_cast<const uint4*>(src + 8 * piece);
+      b[u] = *reinterpret_cast<const uint4*>(src + HD / 2 + 8 * piece);
+    }
+  };
+  load(0);
   float c[8], s[8];
   if (h0 < p.n_heads + p.n_kv_heads) {
     int32_t at_axis[8];
@@ -85,7 +92,7 @@ __global__ void __launch_bounds__(kRopeThreads, 4) rope_pages_kernel(const __gri
     }
   }
   uint16_t* row = nullptr;  // the token's row in the pool
-  if (h0 + (U - 1) * slots >= p.n_heads) {
+  if (h0 + (U * R - 1) * slots >= p.n_heads) {
     int e = 0;
     for (int hi = p.n_seqs; hi - e > 1;) {
       const int mid = (e + hi) >> 1;
@@ -98,24 +105,28 @@ __global__ void __launch_bounds__(kRopeThreads, 4) rope_pages_kernel(const __gri
       row = p.pool + (size_t(page) * p.page_size + (slot - k * p.page_size)) * (2 * size_t(p.n_kv_heads) * HD);
     else set_status(p.status, SPD_EINVAL);
   }
+#pragma unroll 1
+  for (int r = 0; r < R; ++r) {
+    if (r > 0) load(r);
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int h = h0 + u * slots;
-    if (h >= heads) continue;
-    uint16_t* dst = h < p.n_heads ? p.q_out + (size_t(t) * p.n_heads + h) * HD : row ? row + (h - p.n_heads) * HD : nullptr;
-    if (!dst) continue;
-    uint32_t x[4] = {a[u].x, a[u].y, a[u].z, a[u].w}, y[4] = {b[u].x, b[u].y, b[u].z, b[u].w};
-    if (h < p.n_heads + p.n_kv_heads) {
+    for (int u = 0; u < U; ++u) {
+      const int h = h0 + (r * U + u) * slots;
+      if (h >= heads) continue;
+      uint16_t* dst = h < p.n_heads ? p.q_out + (size_t(t) * p.n_heads + h) * HD : row ? row + (h - p.n_heads) * HD : nullptr;
+      if (!dst) continue;
+      uint32_t x[4] = {a[u].x, a[u].y, a[u].z, a[u].w}, y[4] = {b[u].x, b[u].y, b[u].z, b[u].w};
+      if (h < p.n_heads + p.n_kv_heads) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float x0 = __uint_as_float(x[i] << 16), x1 = __uint_as_float(x[i] & 0xffff0000u);
-        const float y0 = __uint_as_float(y[i] << 16), y1 = __uint_as_float(y[i] & 0xffff0000u);
-        x[i] = bf16_pair(x0 * c[2 * i] - y0 * s[2 * i], x1 * c[2 * i + 1] - y1 * s[2 * i + 1]);
-        y[i] = bf16_pair(x0 * s[2 * i] + y0 * c[2 * i], x1 * s[2 * i + 1] + y1 * c[2 * i + 1]);
+        for (int i = 0; i < 4; ++i) {
+          const float x0 = __uint_as_float(x[i] << 16), x1 = __uint_as_float(x[i] & 0xffff0000u);
+          const float y0 = __uint_as_float(y[i] << 16), y1 = __uint_as_float(y[i] & 0xffff0000u);
+          x[i] = bf16_pair(x0 * c[2 * i] - y0 * s[2 * i], x1 * c[2 * i + 1] - y1 * s[2 * i + 1]);
+          y[i] = bf16_pair(x0 * s[2 * i] + y0 * c[2 * i], x1 * s[2 * i + 1] + y1 * c[2 * i + 1]);
+        }
       }
+      *reinterpret_cast<uint4*>(dst + 8 * piece) = make_uint4(x[0], x[1], x[2], x[3]);
+      *reinterpret_cast<uint4*>(dst + HD / 2 + 8 * piece) = make_uint4(y[0], y[1], y[2], y[3]);
     }
-    *reinterpret_cast<uint4*>(dst + 8 * piece) = make_uint4(x[0], x[1], x[2], x[3]);
-    *reinterpret_cast<uint4*>(dst + HD / 2 + 8 * piece) = make_uint4(y[0], y[1], y[2], y[3]);
   }
 }
 
@@ -489,10 +500,12 @@ int rope_pages_run(const void* q, int ldq, const void* kv, int ldkv, const int32
       p.seq[b] = {q_cu[s0 + b], len[s0 + b] - (q_cu[s0 + b + 1] - q_cu[s0 + b])};
     const long long single = (long long)p.n_tok * heads * P;
     if (single > 0x7fffffffLL) return fail(SPD_EUNSUPPORTED, "%d tokens of %d heads in one call", p.n_tok, heads);
-    const int U = single > kRopeSingle ? 4 : 1;
-    const long long threads = (long long)p.n_tok * ((heads + U - 1) / U) * P;
-    const auto kernel = head_dim == 128 ? (U == 4 ? rope_pages_kernel<128, 4> : rope_pages_kernel<128, 1>)
-                                        : (U == 4 ? rope_pages_kernel<64, 4> : rope_pages_kernel<64, 1>);
+    const int each = single > kRopeEight ? 8 : single > kRopeSingle ? 4 : 1;
+    const long long threads = (long long)p.n_tok * ((heads + each - 1) / each) * P;
+    using Kernel = void (*)(RopeArgs);
+    static constexpr Kernel kernels[2][3] = {{rope_pages_kernel<64, 1, 1>, rope_pages_kernel<64, 4, 1>, rope_pages_kernel<64, 4, 2>},
+                                             {rope_pages_kernel<128, 1, 1>, rope_pages_kernel<128, 4, 1>, rope_pages_kernel<128, 4, 2>}};
+    const Kernel kernel = kernels[head_dim == 128][each == 8 ? 2 : each == 4];
     const int slot = trace_begin(st);
     SPD_CUDA_TRY(launch_pdl(kernel, dim3(unsigned((threads + kRopeThreads - 1) / kRopeThreads)), dim3(kRopeThreads), 0, st, p));
     trace_end(slot, st, TR_ROWS, 0.0, 4.0 * p.n_tok * heads * head_dim);

@@ -73,6 +73,8 @@ def _axis(kind, d):
     (2, 2, 128, 64, [70], [1], "sections", (1 << 31) - 200, 1e6),
     (3, 3, 128, 16, [40], [2], "one", -300000, 0.5),
     (32, 32, 128, 64, [257, 100], [3, 0], "one", 5000, 1e4),
+    (33, 1, 128, 64, [2860, 40], [5, 0], "sections", 0, 1e6),  # eight heads a thread, numbers of heads that eight does not divide
+    (15, 3, 64, 32, [9600], [11], "turns", 1 << 20, 1e4),
 ])
 def test_rope_pages(h, g, d, page, new, old, kind, far, theta):
     r = np.random.default_rng(len(new) + d + page)
