@@ -378,10 +378,13 @@ __global__ void __launch_bounds__(kCopyThreads)
   pdl_wait();
   const long long all = (long long)*n_copies * n_layers * chunks;
   for (long long w = blockIdx.x; w < all; w += gridDim.x) {
-    const int chunk = int(w % chunks);
-    const long long rest = w / chunks;
-    const int layer = int(rest % n_layers);
-    const PageCopy c = copies[rest / n_layers];
+    // (division of 64 bits is a hundred instructions)
+    const bool narrow = all <= 0xffffffffll;
+    const long long rest = narrow ? uint32_t(w) / uint32_t(chunks) : w / chunks;
+    const int chunk = int(w - rest * chunks);
+    const long long copy = narrow ? uint32_t(rest) / uint32_t(n_layers) : rest / n_layers;
+    const int layer = int(rest - copy * n_layers);
+    const PageCopy c = copies[copy];
     const size_t n = size_t(c.rows) * row16, at = size_t(chunk) * kCopyChunk + threadIdx.x;
     if (c.from < 0 || c.to < 0) continue;
     const uint4* from = pool + layer * layer16 + c.from * page16;
