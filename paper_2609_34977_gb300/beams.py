@@ -17,6 +17,12 @@ import torch
 from . import _native as N
 
 
+def select_workspace_size(n_seqs: int, n_beams: int, vocab: int) -> int:
+    """Workspace bytes of both selections of a search: of the prompts, a row a request, and of the beams. (One row of a request may be
+    cut into more slices than its beams have together.)"""
+    return max(N.spd_beam_select_workspace_size(n_seqs, n_in, n_beams, vocab) for n_in in (1, n_beams))
+
+
 class BeamAnswer:
     """Cache, tables and texts of n_seqs requests with n_beams beams each.
 
@@ -47,7 +53,7 @@ class BeamAnswer:
         self.now, self.B = 0, n_seqs
         self.used = torch.zeros(1, **i32)
         self.ws_pages = torch.zeros(N.spd_pages_workspace_size(n_pages, B), dtype=torch.uint8, **dev)
-        self.ws_beam = torch.zeros(N.spd_beam_select_workspace_size(n_seqs, n_beams, n_beams, c["vocab"]), dtype=torch.uint8, **dev)
+        self.ws_beam = torch.zeros(select_workspace_size(n_seqs, n_beams, c["vocab"]), dtype=torch.uint8, **dev)
         self.logits = torch.empty(B, c["vocab"], **dev)
         self.parent, self.token = torch.zeros(n_seqs, n_beams, **i32), torch.zeros(n_seqs, n_beams, **i32)
         self.scores = torch.zeros(n_seqs, n_beams, **dev)

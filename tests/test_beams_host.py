@@ -1,0 +1,87 @@
+"""The host side of beam search (no GPU): tensors on the CPU, the library's calls as stand-ins, its size functions as they are."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_34977_gb300 import _native as N
+from paper_2609_34977_gb300 import beams
+from paper_2609_34977_gb300.beams import BeamAnswer
+from tests.test_abi import lib  # noqa: F401  (the fixture that builds the library)
+
+CALLS = ("spd_pages_update", "spd_decode_paged", "spd_beam_select", "spd_pages_compact")
+
+
+class _Library:
+    """Stand-ins that record their calls and arguments; `fails` maps a call to the status that it leaves in its workspace. Selection r
+    (from 0) takes the beams 0, 1, ... of every request (all of them beam 0 of the prompts) and token r."""
+
+    def __init__(self, monkeypatch):
+        self.calls, self.args, self.fails, self.ended = [], [], {}, None
+
+        class Torch:
+            def __getattr__(self, name):
+                f = getattr(torch, name)
+                if name in ("zeros", "empty", "full", "arange", "tensor"):
+                    return lambda *a, **k: f(*a, **{x: y for x, y in k.items() if x != "device"})
+                return f
+        monkeypatch.setattr(beams, "torch", Torch())
+        monkeypatch.setattr(torch.Tensor, "cuda", lambda t: t)
+        for name in CALLS:
+            monkeypatch.setattr(N, name, self._stand_in(name))
+        monkeypatch.setattr(N, "spd_decode_paged_workspace_size", lambda model, n, seqs: 64)
+        monkeypatch.setattr(N, "spd_workspace_status", self._status)
+
+    @staticmethod
+    def _status(ws):  # reads and clears
+        code = int(ws[:4].view(torch.int32))
+        ws[:4] = 0
+        return code
+
+    def of(self, name):
+        return [a for c, a in zip(self.calls, self.args) if c == name]
+
+    def _stand_in(self, name):
+        ws_at = dict(spd_pages_update=11, spd_decode_paged=8, spd_beam_select=7, spd_pages_compact=8)[name]
+
+        def call(*a, **k):
+            if name == "spd_decode_paged":
+                assert a[4].is_contiguous()  # (positions)
+            if name == "spd_beam_select":
+                logits, scores, _, parent, token, out, ended, ws = a
+                (R, n_in), W = scores.shape, parent.shape[1]
+                assert ws.numel() >= N.spd_beam_select_workspace_size(R, n_in, W, logits.shape[1])
+                parent.copy_(torch.arange(R)[:, None] * n_in + torch.arange(W)[None] % n_in)
+                token.fill_(len(self.of(name)))
+                out.fill_(-float(len(self.of(name)) + 1))
+                ended.fill_(-float("inf") if self.ended is None else self.ended)
+            self.calls.append(name)
+            self.args.append((a, k))
+            if name in self.fails:
+                a[ws_at][:4] = torch.tensor([self.fails[name]], dtype=torch.int32).view(torch.uint8)
+        return call
+
+
+def _answer(n=2, W=3, vocab=8, **kw):
+    class Model:
+        cfg = dict(n_layers=2, n_kv_heads=1, head_dim=64, n_heads=2, vocab=vocab, d_model=64)
+    return BeamAnswer(Model, torch.zeros(vocab, 64), n, W, n_pages=32, max_pages=8, page_size=16, **kw)
+
+
+def _prompt(run, lens=(20, 7), **kw):
+    return run.start(torch.zeros(sum(lens), 64), np.concatenate([[0], np.cumsum(lens)]), **kw)
+
+
+@pytest.mark.parametrize("vocab", [8, 32000, 152064, 262144])
+def test_the_workspace_holds_both_selections(lib, vocab):  # noqa: F811
+    for R in range(1, 129):
+        for W in range(1, 33):
+            size = beams.select_workspace_size(R, W, vocab)
+            assert size >= N.spd_beam_select_workspace_size(R, 1, W, vocab) and size >= N.spd_beam_select_workspace_size(R, W, W, vocab)
+
+
+def test_a_search_of_many_requests_and_a_large_vocabulary_begins(lib, monkeypatch):  # noqa: F811
+    _Library(monkeypatch)
+    run = _answer(16, 8, 152064)  # the stand-in looks at the workspace
+    _prompt(run, [1] * 16)
+    run.step()
+    assert run.texts.shape == (128, 2) and run.status() == 0
