@@ -116,7 +116,8 @@ class BeamAnswer:
             whole = self.tables[self.now]
             if len(live) < self.R:  # (a pass takes at least one token of every sequence that it is given)
                 self.tables[self.now] = whole[torch.from_numpy(live).cuda()].contiguous()
-            self._pass(x.index_select(0, idx.to(x.device)), step[live], done[live], torch.from_numpy(host[:, at].astype(np.int32)).cuda(),
+            there = np.ascontiguousarray(host[:, at], dtype=np.int32)  # (columns picked by numpy lie one after the other)
+            self._pass(x.index_select(0, idx.to(x.device)), step[live], done[live], torch.from_numpy(there).cuda(),
                        None if prefix is None else np.asarray(prefix)[live])
             self.tables[self.now] = whole
             logits[torch.from_numpy(live).cuda()] = self.logits[:len(live)]

@@ -85,3 +85,17 @@ def test_a_search_of_many_requests_and_a_large_vocabulary_begins(lib, monkeypatc
     _prompt(run, [1] * 16)
     run.step()
     assert run.texts.shape == (128, 2) and run.status() == 0
+
+
+def test_positions_with_several_axes_pass_chunk_by_chunk(lib, monkeypatch):  # noqa: F811
+    L = _Library(monkeypatch)
+    run = _answer(chunk=8, axis=np.arange(32) % 3)
+    pos = np.arange(3 * 27).reshape(3, 27) % 50
+    _prompt(run, pos=pos)
+    run.step()
+    passes = [a for a, _ in L.of("spd_decode_paged")]
+    want = [list(range(8)) + list(range(20, 27)), list(range(8, 16)), list(range(16, 20))]
+    for a, idx in zip(passes, want):
+        np.testing.assert_array_equal(a[4].numpy(), pos[:, idx])
+    first = [pos[:, :20].max() + 1, pos[:, 20:].max() + 1]
+    np.testing.assert_array_equal(passes[3][4].numpy(), np.tile(np.repeat(first, 3), (3, 1)))
