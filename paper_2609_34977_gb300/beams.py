@@ -30,8 +30,8 @@ class BeamAnswer:
     that ends an answer (-1: none). axis: the axis of every rotary pair (host uint8 [head_dim / 2]) where positions have several.
     Prompts pass in chunks of up to `chunk` tokens a request.
 
-    Where the pool is too small, or a device-side wait ran out, start() and step() raise SpiderError, and so does every later call:
-    what the cache holds is not to be relied on.
+    Where the pool is too small, or a device-side wait ran out, the call that meets it raises SpiderError before it takes over a token or
+    an ended answer, and so does every later call but status(): what the cache holds is not to be relied on.
     """
 
     def __init__(self, model: N.SpdModel, embed, n_seqs: int, n_beams: int, *, n_pages: int, max_pages: int, page_size: int = 64,
@@ -88,6 +88,7 @@ class BeamAnswer:
     def start(self, x, cu, pos=None, prefix=None):
         """The prompts: x bf16 [n][d_model] packed by cu; pos int32 [axes][n] (host or device; None: 0, 1, ... of every request);
         prefix: leading rows of every request that see one another (an image), or None. The first tokens are chosen."""
+        self._raise()
         cu = np.asarray(cu, np.int64)
         n = np.diff(cu)
         if len(n) != self.R or n.min() < 1:
@@ -105,6 +106,7 @@ class BeamAnswer:
         self.ref.zero_()
         self.rows[self.now].zero_()
         self.answers = [[] for _ in range(self.R)]
+        self.texts = torch.zeros(self.R, 0, dtype=torch.int32, device="cuda")
         logits = torch.empty(self.R, self.cfg["vocab"], device="cuda")
         while (done < n).any():
             step = np.minimum(np.where(done == 0, first, self.chunk), n - done)
@@ -122,20 +124,20 @@ class BeamAnswer:
             self.tables[self.now] = whole
             logits[torch.from_numpy(live).cuda()] = self.logits[:len(live)]
         self.lens[:] = n
-        self.texts = torch.zeros(self.R, 0, dtype=torch.int32, device="cuda")
         self._select(logits, torch.zeros(self.R, 1, device="cuda"), torch.arange(self.R, dtype=torch.int32, device="cuda")[:, None])
 
     def _select(self, logits, scores, spare):
         """The beams' next tokens, and the pages of those that go on; spare: what a beam without a candidate stands in for (its score
-        is -inf, and stays so)."""
+        is -inf, and stays so). Raises what the device recorded before anything is taken over."""
         n_in = scores.shape[1]
         ended = self.ended[:, :n_in].contiguous()
         new = torch.empty_like(self.scores)
         N.spd_beam_select(logits, scores, self.eos, self.parent, self.token, new, ended, self.ws_beam)
-        self.scores = new
         none = self.parent < 0
         parent = torch.where(none, spare.expand_as(self.parent), self.parent).flatten()
         token = torch.where(none, 0, self.token).flatten()
+        self._update(parent, [1] * (self.R * self.W))
+        self._check()
         if self.eos >= 0:
             over = ended.cpu().numpy()
             if np.isfinite(over).any():
@@ -143,26 +145,29 @@ class BeamAnswer:
                 for b, w in zip(*np.nonzero(np.isfinite(over))):
                     self.answers[b].append((float(over[b, w]), texts[b, w].tolist()))
         self.texts = torch.cat([self.texts.index_select(0, parent), token[:, None]], 1)
-        self._update(parent, [1] * (self.R * self.W))
+        self.scores = new
         self.lens += 1
-        self._check()
 
     def step(self):
         """One token of every beam."""
+        self._raise()
         pos = np.repeat(self.next_pos, self.W).astype(np.int32)
-        self.next_pos += 1
         x = self.embed.index_select(0, self.texts[:, -1])
         self._pass(x, np.ones(self.R * self.W, np.int32), np.repeat(self.lens, self.W), torch.from_numpy(np.tile(pos, (self.axes, 1))).cuda())
         self._select(self.logits, self.scores, self.first)
+        self.next_pos += 1
 
     def compact(self) -> int:
         """Moves the pages in use to the front of the pool; returns their number (synchronises)."""
+        self._raise()
         t = self.tables[self.now][:self.B]
         N.spd_pages_compact(self.pool, self.cfg["n_kv_heads"], self.cfg["head_dim"], self.ref, t, self.ref, t, self.used, self.ws_pages)
+        self._check()
         return int(self.used)
 
     def best(self, penalty: float = 0.0):
         """Every request's answers, ended or not, best first: (score / length ** penalty, tokens)."""
+        self._raise()
         scores, texts = self.scores.cpu().numpy(), self.texts.cpu().numpy().reshape(self.R, self.W, -1)
         out = []
         for b in range(self.R):
@@ -175,10 +180,15 @@ class BeamAnswer:
         if ws is not None and not self._status:
             self._status = N.spd_workspace_status(ws)
 
-    def _check(self):
-        if self.status():
-            raise N.SpiderError(self.status(), "the pool has no page left" if self.status() == N.SPD_ENOSPC
+    def _raise(self):
+        """Raises a failure that is known."""
+        if self._status:
+            raise N.SpiderError(self._status, "the pool has no page left" if self._status == N.SPD_ENOSPC
                                 else "a device-side failure of this answer")
+
+    def _check(self):
+        self.status()
+        self._raise()
 
     def status(self) -> int:
         """First device-side failure recorded (0 = OK; synchronises)."""

@@ -99,3 +99,52 @@ def test_positions_with_several_axes_pass_chunk_by_chunk(lib, monkeypatch):  # n
         np.testing.assert_array_equal(a[4].numpy(), pos[:, idx])
     first = [pos[:, :20].max() + 1, pos[:, 20:].max() + 1]
     np.testing.assert_array_equal(passes[3][4].numpy(), np.tile(np.repeat(first, 3), (3, 1)))
+
+
+def _state(run):
+    return (run.texts.tolist(), run.scores.tolist(), run.lens.tolist(), run.next_pos.tolist(), [list(a) for a in run.answers])
+
+
+@pytest.mark.parametrize("call,code", [("spd_decode_paged", N.SPD_EINVAL), ("spd_beam_select", -6), ("spd_pages_update", N.SPD_ENOSPC)])
+def test_a_step_that_failed_takes_over_nothing_and_every_later_call_says_so(lib, monkeypatch, call, code):  # noqa: F811
+    L = _Library(monkeypatch)
+    run = _answer(eos=5)
+    _prompt(run)
+    run.step()
+    was = _state(run)
+    L.fails[call], L.ended = code, -3.0  # (ends that the failed step would add)
+    with pytest.raises(N.SpiderError) as e:
+        run.step()
+    assert e.value.code == code == run.status() and _state(run) == was
+    L.fails.clear()
+    n = len(L.calls)
+    for later in (run.step, run.best, run.compact, lambda: _prompt(run)):
+        with pytest.raises(N.SpiderError) as e:
+            later()
+        assert e.value.code == code
+    assert len(L.calls) == n and _state(run) == was and run.status() == code
+
+
+@pytest.mark.parametrize("call,code", [("spd_decode_paged", N.SPD_EINVAL), ("spd_beam_select", -6), ("spd_pages_update", N.SPD_ENOSPC)])
+def test_prompts_that_failed_give_no_answers(lib, monkeypatch, call, code):  # noqa: F811
+    L = _Library(monkeypatch)
+    run = _answer(eos=5)
+    L.fails[call], L.ended = code, -3.0
+    with pytest.raises(N.SpiderError):
+        _prompt(run)
+    assert run.answers == [[], []] and run.texts.shape[1] == 0
+    L.fails.clear()
+    for later in (run.best, run.compact, run.step):
+        with pytest.raises(N.SpiderError):
+            later()
+
+
+def test_a_compaction_that_failed_says_so(lib, monkeypatch):  # noqa: F811
+    L = _Library(monkeypatch)
+    run = _answer()
+    _prompt(run)
+    L.fails["spd_pages_compact"] = N.SPD_EINVAL
+    with pytest.raises(N.SpiderError):
+        run.compact()
+    with pytest.raises(N.SpiderError):
+        run.step()
