@@ -73,8 +73,8 @@ class BeamAnswer:
                            self.tables[new][:n_out], self.rows[new][:n_out], self.ws_pages)
         self.now, self.B = new, n_out
 
-    def _pass(self, x, new, lens, pos, prefix=None):
-        """A pass over new[b] more tokens of every sequence; logits of their last ones."""
+    def _pass(self, x, new, lens, pos, table, prefix=None):
+        """A pass over new[b] more tokens of every sequence of the table; logits of their last ones."""
         n, B = int(np.sum(new)), len(new)
         if n > self._n or self.ws is None:
             self._note(self.ws)
@@ -82,7 +82,7 @@ class BeamAnswer:
             size = N.spd_decode_paged_workspace_size(self.model, n, self.R * self.W)
             self.ws = torch.zeros(size, dtype=torch.uint8, device="cuda")
         cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
-        N.spd_decode_paged(self.model, x, cu, lens, pos, self.tables[self.now][:B], self.pool, self.logits[:B], self.ws,
+        N.spd_decode_paged(self.model, x, cu, lens, pos, table, self.pool, self.logits[:B], self.ws,
                            axis=self.axis, prefix=prefix)
 
     def start(self, x, cu, pos=None, prefix=None):
@@ -90,17 +90,23 @@ class BeamAnswer:
         prefix: leading rows of every request that see one another (an image), or None. The first tokens are chosen."""
         self._raise()
         cu = np.asarray(cu, np.int64)
-        n = np.diff(cu)
-        if len(n) != self.R or n.min() < 1:
-            raise ValueError("start: a prompt for every request")
+        n, room = np.diff(cu), self.tables[0].shape[1] * self.pool.shape[2]
+        if len(n) != self.R or n.min() < 1 or cu[0] != 0 or cu[-1] > len(x):
+            raise ValueError(f"start: a prompt for every request, packed from 0, in {len(x)} rows")
+        if n.max() > room:
+            raise ValueError(f"start: a prompt of {n.max()} tokens, a table holds {room} rows")
         axes = 1 if pos is None else len(pos)
         host = np.concatenate([np.arange(k) for k in n])[None] if pos is None else np.asarray(torch.as_tensor(pos).cpu())
         if host.shape != (axes, cu[-1]):
             raise ValueError(f"pos: shape {host.shape}, expected {(axes, int(cu[-1]))}")
+        if prefix is not None:
+            prefix = np.asarray(prefix, np.int64)
+            if prefix.shape != n.shape or (prefix < 0).any() or (prefix > n).any():
+                raise ValueError("prefix: a number of a prompt's rows for every request")
         self.axes = axes
         self.next_pos = np.array([host[:, a:b].max() + 1 for a, b in zip(cu[:-1], cu[1:])])
         # (an image's rows must be there before they see one another: a prefix passes as one chunk)
-        first = np.maximum(self.chunk, 0 if prefix is None else np.asarray(prefix, np.int64))
+        first = np.maximum(self.chunk, 0 if prefix is None else prefix)
         done = np.zeros(self.R, np.int64)
         self.B, self.lens[:] = self.R, 0
         self.ref.zero_()
@@ -115,13 +121,12 @@ class BeamAnswer:
             at = np.concatenate([np.arange(cu[b] + done[b], cu[b] + done[b] + step[b]) for b in live])
             done += step
             idx = torch.from_numpy(at).cuda()
-            whole = self.tables[self.now]
+            table = self.tables[self.now][:self.R]
             if len(live) < self.R:  # (a pass takes at least one token of every sequence that it is given)
-                self.tables[self.now] = whole[torch.from_numpy(live).cuda()].contiguous()
+                table = table[torch.from_numpy(live).cuda()].contiguous()
             there = np.ascontiguousarray(host[:, at], dtype=np.int32)  # (columns picked by numpy lie one after the other)
-            self._pass(x.index_select(0, idx.to(x.device)), step[live], done[live], torch.from_numpy(there).cuda(),
-                       None if prefix is None else np.asarray(prefix)[live])
-            self.tables[self.now] = whole
+            self._pass(x.index_select(0, idx.to(x.device)), step[live], done[live], torch.from_numpy(there).cuda(), table,
+                       None if prefix is None else prefix[live])
             logits[torch.from_numpy(live).cuda()] = self.logits[:len(live)]
         self.lens[:] = n
         self._select(logits, torch.zeros(self.R, 1, device="cuda"), torch.arange(self.R, dtype=torch.int32, device="cuda")[:, None])
@@ -150,10 +155,11 @@ class BeamAnswer:
 
     def step(self):
         """One token of every beam."""
-        self._raise()
+        self._begun()
         pos = np.repeat(self.next_pos, self.W).astype(np.int32)
         x = self.embed.index_select(0, self.texts[:, -1])
-        self._pass(x, np.ones(self.R * self.W, np.int32), np.repeat(self.lens, self.W), torch.from_numpy(np.tile(pos, (self.axes, 1))).cuda())
+        self._pass(x, np.ones(self.R * self.W, np.int32), np.repeat(self.lens, self.W),
+                   torch.from_numpy(np.tile(pos, (self.axes, 1))).cuda(), self.tables[self.now])
         self._select(self.logits, self.scores, self.first)
         self.next_pos += 1
 
@@ -167,7 +173,7 @@ class BeamAnswer:
 
     def best(self, penalty: float = 0.0):
         """Every request's answers, ended or not, best first: (score / length ** penalty, tokens)."""
-        self._raise()
+        self._begun()
         scores, texts = self.scores.cpu().numpy(), self.texts.cpu().numpy().reshape(self.R, self.W, -1)
         out = []
         for b in range(self.R):
@@ -185,6 +191,11 @@ class BeamAnswer:
         if self._status:
             raise N.SpiderError(self._status, "the pool has no page left" if self._status == N.SPD_ENOSPC
                                 else "a device-side failure of this answer")
+
+    def _begun(self):
+        self._raise()
+        if self.texts.shape[1] == 0:
+            raise ValueError("the prompts have not passed: start() first")
 
     def _check(self):
         self.status()

@@ -148,3 +148,52 @@ def test_a_compaction_that_failed_says_so(lib, monkeypatch):  # noqa: F811
         run.compact()
     with pytest.raises(N.SpiderError):
         run.step()
+
+
+@pytest.mark.parametrize("match,lens,kw,rows", [
+    ("prompt for", [20, 7], {}, 26),                                   # fewer rows than cu says: they would be read past the end
+    ("prompt for", [20, 0], {}, 20),
+    ("128 rows", [20, 129], {}, 149),                               # more than a table holds
+    ("prefix", [20, 7], dict(prefix=[0, 8]), 27),
+    ("prefix", [20, 7], dict(prefix=[-1, 0]), 27),
+    ("prefix", [20, 7], dict(prefix=[3]), 27),
+    ("pos", [20, 7], dict(pos=np.zeros((3, 26))), 27),
+    ("pos", [20, 7], dict(pos=np.zeros(27)), 27),
+])
+def test_prompts_are_refused_before_anything_changes(lib, monkeypatch, match, lens, kw, rows):  # noqa: F811
+    L = _Library(monkeypatch)
+    run = _answer()
+    _prompt(run)
+    run.step()
+    was, n = _state(run), len(L.calls)
+    with pytest.raises(ValueError, match=match):
+        run.start(torch.zeros(rows, 64), np.concatenate([[0], np.cumsum(lens)]), **kw)
+    assert _state(run) == was and len(L.calls) == n
+    run.step()
+
+
+@pytest.mark.parametrize("cu", [[-3, 20, 27], [1, 20, 27], [0, 27], [0, 20, 27, 30]])
+def test_prompts_that_do_not_begin_at_0(lib, monkeypatch, cu):  # noqa: F811
+    _Library(monkeypatch)
+    run = _answer()
+    with pytest.raises(ValueError, match="prompt"):
+        run.start(torch.zeros(30, 64), cu, pos=np.zeros((1, 27)))
+
+
+def test_a_refused_pass_leaves_room_for_other_prompts(lib, monkeypatch):  # noqa: F811
+    L = _Library(monkeypatch)
+    run = _answer(chunk=8)
+    with monkeypatch.context() as m:
+        def refuse(*a, **k):
+            if len(L.of("spd_decode_paged")) == 1:  # the second chunk, of one of two requests
+                raise N.SpiderError(N.SPD_EINVAL, "refused")
+            L._stand_in("spd_decode_paged")(*a, **k)
+        m.setattr(N, "spd_decode_paged", refuse)
+        with pytest.raises(N.SpiderError, match="refused"):
+            _prompt(run)
+    for early in (run.step, run.best):
+        with pytest.raises(ValueError, match="start"):
+            early()
+    _prompt(run)
+    run.step()
+    assert run.texts.shape == (6, 2) and len(run.best()) == 2
