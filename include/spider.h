@@ -591,7 +591,8 @@ size_t spd_pages_workspace_size(int n_pages, int n_seqs);
  * the page is listed anywhere else besides), the others that grow get a copy of its rows, in every layer. New pages are the
  * lowest free ones (those that this call frees among them), in the order of the outputs, of each its copy first.
  * Where no free page is left the entry is -1 and the workspace's status word SPD_ENOSPC. Lengths that a table does not hold (or
- * negative ones) are cut to it and reported as SPD_EINVAL, and so is ref where it does not count what the tables list.
+ * negative ones) are cut to it and reported as SPD_EINVAL, and so is a count below the number of input tables that list a page, which is
+ * taken for that number. (A count above it holds the page for tables outside the call, and is no error.)
  * pool (dev) bf16 [n_layers][n_pages][page_size][K | V]; ref_in, ref_out (dev) int32 [n_pages], the same buffer or apart; table_in
  * (dev) int32 [n_in][max_pages], len_in (dev) int32 [n_in]; table_out (dev) int32 [n_out][max_pages], -1 behind a sequence's pages,
  * len_out (dev) int32 [n_out], both apart from the inputs. ws 16-byte aligned. The same result in every run.

@@ -195,6 +195,7 @@ __global__ void __launch_bounds__(kPageThreads, 1) pages_update_kernel(const __g
   int* count = shared ? reinterpret_cast<int*>(mem + p.n_pages) : p.count;                    // [n_pages]
   int* ref = shared ? count + p.n_pages : p.ref_out;                                          // [n_pages]
   int* free_list = shared ? ref + p.n_pages : p.free_list;                                    // [n_pages]
+  int* listed = free_list;  // until the free pages are looked for: entries of the outputs' tables that list a page, before copies
   int* kids = shared ? free_list + p.n_pages : p.kids;                                        // [n_in]
   int* rows = shared ? kids + p.n_in : p.rows;                                                // [n_in] rows that it holds
   int* from = shared ? rows + p.n_in : p.from;                                                // [n_out] parent, or -1
@@ -222,6 +223,7 @@ __global__ void __launch_bounds__(kPageThreads, 1) pages_update_kernel(const __g
   for (int i = tid; i < p.n_pages; i += kPageThreads) {
     ref[i] = p.ref_in[i];
     count[i] = 0;
+    listed[i] = 0;
     owner[i] = 0;
   }
   __syncthreads();
@@ -244,8 +246,22 @@ __global__ void __launch_bounds__(kPageThreads, 1) pages_update_kernel(const __g
     const int i = int(x / width), k = int(x - i * width);
     if (k >= pages_for(rows[i], p.page_size)) continue;
     const int q = page_of(x == unsigned(tid) ? entry : p.table_in[x]), change = kids[i] - 1;
-    if (q < 0) set_status(p.status, SPD_EINVAL);
-    else if (change != 0 && atomicAdd(&ref[q], change) + change < 0) set_status(p.status, SPD_EINVAL);
+    if (q < 0) {
+      set_status(p.status, SPD_EINVAL);
+      continue;
+    }
+    if (change >= 0) atomicAdd(&listed[q], change + 1);
+    if (change != 0 && atomicAdd(&ref[q], change) + change < 0) set_status(p.status, SPD_EINVAL);
+  }
+  __syncthreads();
+  // A count below the tables' entries shows here (where none of the inputs goes on: above, as a negative one). Taken for their number, no
+  // page that a table lists counts as free, and no copy's source is another's target.
+  for (int i = tid; i < p.n_pages; i += kPageThreads) {
+    const int n = listed[i];
+    if (n > 0 && n > ref[i]) {
+      set_status(p.status, SPD_EINVAL);
+      ref[i] = n;
+    }
   }
   __syncthreads();
   int need = 0, copies = 0;
