@@ -628,7 +628,8 @@ __global__ void __launch_bounds__(kThreads, 2)
         }
         tmem_st_wait();
       }
-      if (*reinterpret_cast<volatile int*>(odd_v) > unit) {
+      // (a warp that is a unit ahead may raise it meanwhile: the lanes, which work together below, decide together)
+      if (any(*reinterpret_cast<volatile int*>(odd_v) > unit)) {
         // values of V that were cleared: rows that see one add p v in fp32 (the score again from q and k)
         const float off = m_run == -INFINITY ? 0.0f : m_run * p.scale_log2;
         const __nv_bfloat16* qsrc = p.q + now.row * HD;
@@ -645,6 +646,7 @@ __global__ void __launch_bounds__(kThreads, 2)
           if (sees)
             for (int x = 0; x < HD; ++x) d = fmaf(__bfloat162float(qsrc[x]), __bfloat162float(kr[x]), d);
           const float w = ex2(fmaf(d, p.scale_log2, -off));
+          __syncwarp();
 #pragma unroll 1
           for (int c = 0; c < HD; c += 8) {
             float ov[8];
@@ -670,6 +672,7 @@ __global__ void __launch_bounds__(kThreads, 2)
 #pragma unroll 1
       for (int c = 0; c < HD; c += 32) {
         float v[32];
+        __syncwarp();
         tmem_ld32(t_oh + c, v);
         if (!now.valid) continue;
         if (part) {
@@ -1071,6 +1074,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1)
 #pragma unroll
       for (int y = 0; y < R / 8; ++y) {
         float o[8], mid[8], lo[8];
+        __syncwarp();
         tmem_ld8(t_o + lanes + 8 * y, o);
         tmem_ld8x2(t_o + lanes + kTokenHeads + 8 * y, mid, t_o + lanes + 2 * kTokenHeads + 8 * y, lo);
 #pragma unroll
