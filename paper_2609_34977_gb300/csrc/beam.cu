@@ -152,9 +152,11 @@ __global__ void __launch_bounds__(kThreads, kCtasSm) beam_slice_kernel(const __g
   };
   for (int base = 0, b = 0; base < n; base += kBatch, ++b) {
     float x[kHeld];
+    bool gave_up = false;
     if constexpr (W == 4) {
       if (!mbar_wait(&full[b % kStages], (b / kStages) & 1, &aborted, p.budget)) {
         aborted = 1;
+        gave_up = true;
         set_status(p.status, SPD_ETIMEOUT);
       }
 #pragma unroll
@@ -220,8 +222,17 @@ __global__ void __launch_bounds__(kThreads, kCtasSm) beam_slice_kernel(const __g
       }
     }
     if (tid == 0) pushed[(b + 1) % 3] = 0;  // (read last before the barrier of the batch before)
-    __syncthreads();
-    if constexpr (W == 4) fetch(base + kStages * kBatch, b + kStages);  // (the batch is in registers)
+    if constexpr (W == 4) {
+      if (__syncthreads_or(gave_up)) {  // the batches under way land before the CTA exits; no others are fetched
+        volatile int no_abort = 0;
+        if (tid == 0)
+          for (int i = b; i < b + kStages && i * kBatch < n; ++i) mbar_wait(&full[i % kStages], (i / kStages) & 1, &no_abort, p.budget);
+        break;
+      }
+      fetch(base + kStages * kBatch, b + kStages);  // (the batch is in registers)
+    } else {
+      __syncthreads();
+    }
     const int all = have + pushed[b % 3];
     if (all > kList) {
       // the list as it was, and this batch's tokens one by one: the k-th largest of both in round k
