@@ -2,7 +2,6 @@
 //
 // A pool is bf16 [layer][page][row of the page][K of every K/V head | V of every K/V head]; row r of a sequence lies in page
 // table[r / page_size], row r % page_size. ref counts the tables that list a page; 0 is free.
-#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <math.h>
 #include <stdint.h>
@@ -15,8 +14,6 @@
 
 namespace spd {
 namespace {
-
-namespace cg = cooperative_groups;
 
 // ---- rotary positions with several axes, K/V into pages -------------------------------------------
 // Pair (j, j + d/2) of a head turns by pos[axis_j] theta^(-2j/d). An angle is kept in turns: theta^(-2j/d) / 2 pi as a 64-bit
