@@ -470,7 +470,6 @@ extern "C" int spd_beam_select(const float* logits, int n_seqs, int n_in, int vo
   if (vocab > 1 << 30) return fail(SPD_EUNSUPPORTED, "vocabulary of %d tokens", vocab);
   if ((long long)n_seqs * n_in > 65535) return fail(SPD_EUNSUPPORTED, "more than 65535 beams in all");
   if (eos < -1 || eos >= vocab) return fail(SPD_EINVAL, "eos outside the vocabulary (-1: none)");
-  if (scores_out == scores && n_in != n_out) return fail(SPD_EINVAL, "scores_out may be scores only where n_in is n_out");
   if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(SPD_EINVAL, "ws must be 16-byte aligned");
   BeamArgs p{};
   p.z = logits;
@@ -487,6 +486,7 @@ extern "C" int spd_beam_select(const float* logits, int n_seqs, int n_in, int vo
   p.best = cv.take<unsigned long long>(lists * n_out);
   p.sums = cv.take<float2>(lists);
   if (!cv.fits()) return fail(SPD_ENOSPC, "beam workspace too small (%zu < %zu)", ws_bytes, cv.used);
+  if (scores_out == scores && n_in != n_out) return fail(SPD_EINVAL, "scores_out may be scores only where n_in is n_out");
   p.parent = parent;
   p.token = token;
   p.out = scores_out;
