@@ -92,7 +92,7 @@ template <int W>
 __global__ void __launch_bounds__(kThreads, kCtasSm) beam_slice_kernel(const __grid_constant__ BeamArgs p) {
   extern __shared__ __align__(128) float ring[];  // [kStages][kBatch]
   __shared__ uint64_t full[kStages];
-  __shared__ int aborted;
+  __shared__ int aborted;  // 1 + the first batch that a thread gave up waiting for; none is fetched from then on
   __shared__ unsigned long long list[kList], top[kMaxBeams], wbest[2][kWarps];
   __shared__ float group[kMaxBeams];
   __shared__ float2 wsum[kWarps];
@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(kThreads, kCtasSm) beam_slice_kernel(const __g
   float next[W == 4 ? 1 : kHeld];
   auto fetch = [&](int base, int b) {
     if constexpr (W == 4) {
-      if (tid == 0 && base < n) {
+      if (tid == 0 && base < n && !aborted) {
         const uint32_t bytes = 4u * uint32_t(min(kBatch, n - base));  // (slices are multiples of four)
         mbar_arrive_expect_tx(&full[b % kStages], bytes);
         bulk_load(ring + (b % kStages) * kBatch, z + base, bytes, &full[b % kStages]);
@@ -152,11 +152,9 @@ __global__ void __launch_bounds__(kThreads, kCtasSm) beam_slice_kernel(const __g
   };
   for (int base = 0, b = 0; base < n; base += kBatch, ++b) {
     float x[kHeld];
-    bool gave_up = false;
     if constexpr (W == 4) {
       if (!mbar_wait(&full[b % kStages], (b / kStages) & 1, &aborted, p.budget)) {
-        aborted = 1;
-        gave_up = true;
+        if (!aborted) aborted = b + 1;
         set_status(p.status, SPD_ETIMEOUT);
       }
 #pragma unroll
@@ -222,17 +220,8 @@ __global__ void __launch_bounds__(kThreads, kCtasSm) beam_slice_kernel(const __g
       }
     }
     if (tid == 0) pushed[(b + 1) % 3] = 0;  // (read last before the barrier of the batch before)
-    if constexpr (W == 4) {
-      if (__syncthreads_or(gave_up)) {  // the batches under way land before the CTA exits; no others are fetched
-        volatile int no_abort = 0;
-        if (tid == 0)
-          for (int i = b; i < b + kStages && i * kBatch < n; ++i) mbar_wait(&full[i % kStages], (i / kStages) & 1, &no_abort, p.budget);
-        break;
-      }
-      fetch(base + kStages * kBatch, b + kStages);  // (the batch is in registers)
-    } else {
-      __syncthreads();
-    }
+    __syncthreads();
+    if constexpr (W == 4) fetch(base + kStages * kBatch, b + kStages);  // (the batch is in registers)
     const int all = have + pushed[b % 3];
     if (all > kList) {
       // the list as it was, and this batch's tokens one by one: the k-th largest of both in round k
@@ -275,6 +264,13 @@ __global__ void __launch_bounds__(kThreads, kCtasSm) beam_slice_kernel(const __g
         have = all;
         sorted = false;
       }
+    }
+  }
+  if constexpr (W == 4) {
+    if (tid == 0 && aborted) {  // batches under way land before the CTA exits
+      volatile int no_abort = 0;
+      for (int i = aborted - 1; i < aborted - 1 + kStages && i * kBatch < n; ++i)
+        mbar_wait(&full[i % kStages], (i / kStages) & 1, &no_abort, p.budget);
     }
   }
   if (!sorted) {
