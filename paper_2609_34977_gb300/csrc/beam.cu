@@ -87,6 +87,12 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
   return make_float2(m, a.y * exp_less(a.x, m) + b.y * exp_less(b.x, m));
 }
 
+// Waits for the batches from `first` on that were fetched: they land before the CTA exits.
+__device__ __noinline__ void land(uint64_t* full, int first, int n, long long budget) {
+  volatile int no_abort = 0;
+  for (int i = first; i < first + kStages && i * kBatch < n; ++i) mbar_wait(&full[i % kStages], (i / kStages) & 1, &no_abort, budget);
+}
+
 // W = 4: rows whose 16-byte pieces are aligned, batches by bulk copies into shared memory; 1: any rows, through registers.
 template <int W>
 __global__ void __launch_bounds__(kThreads, kCtasSm) beam_slice_kernel(const __grid_constant__ BeamArgs p) {
@@ -266,13 +272,6 @@ __global__ void __launch_bounds__(kThreads, kCtasSm) beam_slice_kernel(const __g
       }
     }
   }
-  if constexpr (W == 4) {
-    if (tid == 0 && aborted) {  // batches under way land before the CTA exits
-      volatile int no_abort = 0;
-      for (int i = aborted - 1; i < aborted - 1 + kStages && i * kBatch < n; ++i)
-        mbar_wait(&full[i % kStages], (i / kStages) & 1, &no_abort, p.budget);
-    }
-  }
   if (!sorted) {
     __syncthreads();
     cut(have);
@@ -289,6 +288,7 @@ __global__ void __launch_bounds__(kThreads, kCtasSm) beam_slice_kernel(const __g
     p.sums[at] = sum;
   }
   if (tid < K) p.best[at * K + tid] = tid < have ? top[tid] : 0;
+  if (W == 4 && tid == 0 && aborted) land(full, aborted - 1, n, p.budget);
 }
 
 // hi + lo = a + b exactly, hi the rounded sum.
