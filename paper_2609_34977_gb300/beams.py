@@ -6,8 +6,8 @@
     spd_pages_compact  the pages in use to the front of the pool (on demand)
 
 This module owns buffers and keeps the texts; every computation runs in the CUDA library. A request's beams have the same
-length, so the host knows every length without waiting for what the device selects. `python -m paper_2609_34977_gb300.beams`
-runs a small model.
+length, so the host keeps the lengths. A step ends with a look at what the device recorded, and waits for it.
+`python -m paper_2609_34977_gb300.beams` runs a small model.
 """
 from __future__ import annotations
 

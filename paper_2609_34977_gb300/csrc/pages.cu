@@ -17,8 +17,8 @@ namespace {
 
 // ---- rotary positions with several axes, K/V into pages -------------------------------------------
 // Pair (j, j + d/2) of a head turns by pos[axis_j] theta^(-2j/d). An angle is kept in turns: theta^(-2j/d) / 2 pi as a 64-bit
-// fraction times the integer position, modulo 2^64, is exact but for the fraction's own rounding (2^-56 a position), so far
-// positions lose nothing; its upper 32 bits go through sincospi.
+// fraction times the integer position, modulo 2^64, is exact but for the fraction's own error (below 2^-54 a position where
+// theta is 1 or more: 2^-23 of a turn at a position of 2^31); its upper 32 bits go through sincospi.
 // A thread has 8 pairs of a token (16 bytes of either half) for one, four or eight heads (eight: four and four), so that it works
 // its angles out once for them where there are threads enough. Heads of 128, 36 of 64 / 256 / 1024 / 4096 tokens with one and with
 // four: 3.5 and 4.8 / 6.7 and 5.0 / 10.6 and 8.8 / 34.9 and 19.9 us; 96 of 64 / 4096: 5.1 and 4.9 / 73 and 39. With four and with
