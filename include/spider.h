@@ -540,7 +540,8 @@ int spd_logits_process(const float* logits, int n_rows, int vocab, int ld, const
  * values, multiples of 8); pos (dev) int32 [n_axes][n_tok], any values; axis (HOST) uint8 [head_dim / 2], NULL = all pairs by
  * axis 0; a pair whose axis is n_axes or more does not turn. q_out (dev) bf16 [n_tok][n_heads * head_dim], may be q (then ldq is its
  * width). pool: the layer's block [n_pages][page_size][K | V]. Rotation in fp32 with the angle modulo 2 pi exact to 2^-23 of a turn
- * (theta of 1 or more, any position), one rounding to bf16. Two new tokens must not share a row (a page that several sequences list is written by one of them).
+ * (theta of 1 or more, any position), one rounding to bf16. Two new tokens must not share a row (a page that several sequences list is
+ * written by one of them).
  * q, kv and q_out 16-byte aligned. ws (dev, at least 4 bytes, may be NULL): only its status word is used.
  * Errors: SPD_EINVAL, SPD_EUNSUPPORTED, SPD_ECUDA. */
 int spd_rope_pages(const uint16_t* q, int ldq, const uint16_t* kv, int ldkv, int n_tok, const int32_t* pos, int n_axes,
@@ -618,7 +619,7 @@ size_t spd_beam_select_workspace_size(int n_seqs, int n_in, int n_out, int vocab
  * logits row b * n_in + w ((dev) fp32, vocab values, stride ld). Of the candidates
  *   total(w, t) = scores[b][w] + z[t] - log sum_u exp z[u],   t != eos (eos -1: none), z[t] above -inf,
  * the n_out largest, ties to the lower beam, then to the lower token. Totals are held in 48 bits, so that those of one beam keep the order of
- * its logits (unless they differ by less than 2^-48 of the total); the logarithm of a beam's sum, in fp32, is off by up to 2^-20, and totals of
+ * its logits (unless they differ by less than 2^-48 of the total); the logarithm of a beam's sum, in fp32, is off by about 2^-20, and totals of
  * two beams that are closer together than that may go in either order.
  * parent (dev) int32 [n_seqs][n_out] receives b * n_in + w, as spd_pages_update takes it, token (dev) int32 the token, scores_out (dev)
  * fp32 the total; -1, -1 and -inf where there are fewer; scores_out may be scores where n_in is n_out. A beam whose score is not finite,

@@ -12,7 +12,7 @@
 // A CTA a request then takes the n_out lists of the best heads, and of their candidates that are not behind the last of these
 // heads the n_out best, by counting how many go before each. Rounded to fp32 totals of one
 // beam would tie that differ, and fp64 is slow here, so totals are pairs of fp32 values (a sum and what it was rounded by). The logarithm
-// of a beam's sum itself is off by up to 2^-20 (exponentials of a few units, sums in fp32), which is what separates beams.
+// of a beam's sum itself is off by about 2^-20 (exponentials of a few units, sums in fp32), which is what separates beams.
 //
 // What bounds it: of many rows the stream and the instructions a logit takes (an exponential, two maxima, a comparison): 128 rows
 // of 152064 19.4 us with the merge, 78 MB; of one request a chain, 6 us. 256 threads a CTA, or twice as many tokens a thread, took
