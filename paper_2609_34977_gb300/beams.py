@@ -51,6 +51,7 @@ class BeamAnswer:
         self.tables = [torch.full((B, max_pages), -1, **i32) for _ in range(2)]
         self.rows = [torch.zeros(B, **i32) for _ in range(2)]
         self.now, self.B = 0, n_seqs
+        self.room = max_pages * page_size  # rows that a table holds
         self.used = torch.zeros(1, **i32)
         self.ws_pages = torch.zeros(N.spd_pages_workspace_size(n_pages, B), dtype=torch.uint8, **dev)
         self.ws_beam = torch.zeros(select_workspace_size(n_seqs, n_beams, c["vocab"]), dtype=torch.uint8, **dev)
@@ -90,11 +91,11 @@ class BeamAnswer:
         prefix: leading rows of every request that see one another (an image), or None. The first tokens are chosen."""
         self._raise()
         cu = np.asarray(cu, np.int64)
-        n, room = np.diff(cu), self.tables[0].shape[1] * self.pool.shape[2]
+        n = np.diff(cu)
         if len(n) != self.R or n.min() < 1 or cu[0] != 0 or cu[-1] > len(x):
             raise ValueError(f"start: a prompt for every request, packed from 0, in {len(x)} rows")
-        if n.max() > room:
-            raise ValueError(f"start: a prompt of {n.max()} tokens, a table holds {room} rows")
+        if n.max() >= self.room:
+            raise ValueError(f"start: a prompt of {n.max()} tokens and the first one behind it, a table holds {self.room} rows")
         axes = 1 if pos is None else len(pos)
         host = np.concatenate([np.arange(k) for k in n])[None] if pos is None else np.asarray(torch.as_tensor(pos).cpu())
         if host.shape != (axes, cu[-1]):
@@ -154,8 +155,10 @@ class BeamAnswer:
         self.lens += 1
 
     def step(self):
-        """One token of every beam."""
+        """One token of every beam. Refused where a table has no row for it; the answers so far stay."""
         self._begun()
+        if self.lens.max() >= self.room:
+            raise N.SpiderError(N.SPD_EINVAL, f"a table holds {self.room} rows")
         pos = np.repeat(self.next_pos, self.W).astype(np.int32)
         x = self.embed.index_select(0, self.texts[:, -1])
         self._pass(x, np.ones(self.R * self.W, np.int32), np.repeat(self.lens, self.W),

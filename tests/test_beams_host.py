@@ -197,3 +197,20 @@ def test_a_refused_pass_leaves_room_for_other_prompts(lib, monkeypatch):  # noqa
     _prompt(run)
     run.step()
     assert run.texts.shape == (6, 2) and len(run.best()) == 2
+
+
+def test_a_full_table_is_told_before_a_step_and_the_answers_stay(lib, monkeypatch):  # noqa: F811
+    L = _Library(monkeypatch)
+    run = _answer()
+    with pytest.raises(ValueError, match="128 rows"):  # (no row for the first token)
+        _prompt(run, [128, 7])
+    _prompt(run, [126, 7])
+    run.step()
+    was, best, n = _state(run), run.best(), len(L.calls)
+    for _ in range(2):
+        with pytest.raises(N.SpiderError, match="128 rows") as e:
+            run.step()
+        assert e.value.code == N.SPD_EINVAL
+    assert _state(run) == was and run.best() == best and run.status() == 0 and len(L.calls) == n
+    _prompt(run)  # and others may follow
+    run.step()
